@@ -188,7 +188,7 @@ def prepare(case, seed):
         st["k_out"] = torch.empty((rows, hkv, d), dtype=dt, device=DEV)
         if op == "rotary_bwd" and case["norm"]:
             st["dqw"], st["dkw"] = torch.empty(d, **f32), torch.empty(d, **f32)
-            ws = pa.padoc_qk_rotary_bwd_workspace_size(st["rotary"], rows, hq, hkv)
+            ws = pa.padoc_qk_rotary_bwd_workspace_size(st["rotary"], rows)
             st["ws"] = torch.empty(max(ws, 256), dtype=torch.uint8, device=DEV)
         if case["kv"] == "e4m3":
             st["pool"] = pa.E4M3Pool.over(st["k_codes"], st["v_codes"], st["k_scales"], st["v_scales"])
