@@ -37,6 +37,8 @@
  *     the kernel returns.
  *   - Query heads map to KV heads in consecutive groups: h -> h / (Hq / Hkv).
  *   - LSE is the natural-log log-sum-exp, fp32, laid out [query][head].
+ *   - The attention calls take q and k as they are; the rotary calls below apply the head norms and
+ *     the positions before them, in training with gradients and in serving on the way into the cache.
  */
 #ifndef PADOC_ATTN_H
 #define PADOC_ATTN_H
@@ -54,7 +56,8 @@ extern "C" {
  * the bounded-wait self-test, the in-place plan advance and the one-call decode step. 4 adds the
  * merge key list to the decode plan (padoc_decode_plan.off_merge_keys, num_merge_keys). 5 adds the
  * loop's step runner (padoc_mpd_runner_*). 6 adds padoc_mpd_step.off_first_blocks and stores the
- * split-K partials in bf16 (the decode workspace's size changes with it). */
+ * split-K partials in bf16 (the decode workspace's size changes with it). The rotary calls, the block
+ * copies and padoc_mpd_fork_stream .. padoc_mpd_resize only add symbols and leave the number. */
 #define PADOC_ATTN_VERSION 6
 
 /* A CUDA stream handle; identical to cudaStream_t. */
@@ -659,6 +662,192 @@ padoc_status padoc_mpd_status(const padoc_mpd *mpd, int32_t *live_pages, int32_t
 padoc_status padoc_append_inputs(const padoc_kv_pool *pool, const void *k_src, const void *v_src, const void *q_src,
                                  int64_t src_total, int32_t num_q_heads, void *q_dst, const int32_t *src_rows,
                                  const int32_t *slots, int32_t count, padoc_stream_t stream);
+
+/* ============================================================================================
+ * Rotary positions with several axes, and the head norms before them
+ * ========================================================================================== */
+
+/* What a model does to its query and key heads between the projections and the attention. Per head of
+ * d = head_dim values x:
+ *   y = x r w,  r = 1 / sqrt(mean_j x_j^2 + eps)   (q_weight / k_weight given; else y = x)
+ *   z = y with each pair (u, v) of its first R = rotary_dim values turned by the pair's angle t:
+ *       (A (u cos t - v sin t), A (v cos t + u sin t)),   A = amplitude.
+ * Pair i < R / 2 is the dims (i, i + R / 2), or with adjacent = 1 the dims (2 i, 2 i + 1); its angle is
+ * inv_freq[i] x the row's position on the pair's axis (time, height and width of images and video, or one
+ * axis for text). Everything is computed in fp32 from the stored values and rounded once; the angle is
+ * reduced modulo a turn in integers, so far positions are as exact as near ones.
+ *   freq: (device) uint64 [R / 2], the table padoc_build_rotary_table makes.
+ *   q_weight, k_weight: (device) [head_dim] in the rows' dtype, 16-byte aligned; both or neither.
+ * head_dim a multiple of 8 up to 256, rotary_dim a multiple of 8 up to head_dim, 1 to 4 axes. */
+typedef struct {
+    const uint64_t *freq;
+    const void *q_weight;
+    const void *k_weight;
+    int32_t head_dim;
+    int32_t rotary_dim;
+    int32_t num_axes;
+    int32_t adjacent;
+    float eps;
+    float amplitude;
+} padoc_rotary;
+
+/* Rows of query, key and value heads, e.g. slices of a fused projection's output (device). Row r's query
+ * heads start at q + r x q_stride and lie behind one another, key and value heads likewise.
+ *   q: [rows][num_q_heads][head_dim], k, v: [rows][num_kv_heads][head_dim], in dtype, 16-byte aligned;
+ *   strides in elements, at least the heads' width, a multiple of 16 bytes.
+ *   pos: int32 [rows][num_axes]; any value, negative ones too. */
+typedef struct {
+    const void *q;
+    const void *k;
+    const void *v;
+    int64_t q_stride;
+    int64_t k_stride;
+    int64_t v_stride;
+    const int32_t *pos;
+    int64_t rows;
+    int32_t num_q_heads;
+    int32_t num_kv_heads;
+    padoc_dtype dtype;
+} padoc_qkv_rows;
+
+/* The device table of a padoc_rotary (host): entry i is inv_freq[i] / 2 pi modulo 1 as a 62-bit fraction
+ * above the pair's axis (axis_of[i], 0 .. num_axes - 1; NULL with one axis). Copy it to the device unchanged.
+ * Errors: INVALID_ARGUMENT (also a frequency that is not finite, an axis out of range). */
+padoc_status padoc_build_rotary_table(const double *inv_freq, const int32_t *axis_of, int32_t num_freqs,
+                                      int32_t num_axes, uint64_t *table);
+
+/* A grid of image or video patches among a page's prefix tokens: tokens [begin, begin + t h w) of page
+ * `page`, frame by frame, row by row. */
+typedef struct {
+    int32_t page;
+    int32_t begin;
+    int32_t t, h, w;   /* >= 1 each */
+} padoc_grid;
+
+/* Positions on three axes (time, height, width) of the packed tokens (host). Within a page a text token
+ * takes the next position p on all axes; a grid that starts at p gives its token (i, j, l) the positions
+ * (p + i, p + j, p + l), and the token behind it takes p + max(t, h, w). Layout tokens go on from the
+ * prefix's end, and token i of branch k takes end + f_k + i: what it would have if the page's visible
+ * tokens were one sequence (App. E.2 serves a branch as a request whose prompt they are).
+ *   grids: (host) [num_grids], by page and begin, not overlapping, inside the prefix.
+ *   pos: (host) int32 [capacity_tokens][3]. prefix_end: (host) int32 [num_pages] (NULL allowed), the
+ *   position of the token behind each prefix: in a decoding loop the layout stream's token j takes
+ *   prefix_end + j, a branch's as above. Errors: INVALID_ARGUMENT; CAPACITY when capacity_tokens < T. */
+padoc_status padoc_build_rotary_positions(const padoc_page *pages, int32_t num_pages, const padoc_grid *grids,
+                                          int32_t num_grids, int32_t *pos, int64_t capacity_tokens, int32_t *prefix_end);
+
+/* Norm and rotation of packed rows, the step before padoc_ancestor_prefill_attn: q_out [rows][Hq][d] and
+ * k_out [rows][Hkv][d] with row strides in elements (as in->q_stride), in dtype, 16-byte aligned. An output
+ * may be its input (same address and stride); other overlaps are not allowed. in->v is not used.
+ * bf16 and f32. Errors: INVALID_ARGUMENT, UNSUPPORTED, CUDA. */
+padoc_status padoc_qk_rotary(const padoc_rotary *rot, const padoc_qkv_rows *in, void *q_out, int64_t q_out_stride,
+                             void *k_out, int64_t k_out_stride, padoc_stream_t stream);
+
+/* Workspace (device) bytes of padoc_qk_rotary_bwd: partial sums of the weights' gradients (0 without the
+ * norm). */
+padoc_status padoc_qk_rotary_bwd_workspace_size(const padoc_rotary *rot, int64_t rows, size_t *bytes);
+
+/* Gradients of padoc_qk_rotary for upstream gradients dq_out, dk_out (e.g. what padoc_ancestor_prefill_bwd
+ * gives for the rotated q and k). With g the upstream gradient turned back (by the opposite angles, times A):
+ *   without the norm   dx = g;
+ *   with it, h = x r:  dx = r (w g - h mean_j(w_j g_j h_j)),  dw = sum over rows and heads of g h.
+ *   in: the forward's rows; without the norm only pos, rows, the head counts and dtype are used.
+ *   dq, dk: strides as above; each may be its upstream gradient (same address and stride).
+ *   dq_weight, dk_weight: (device) fp32 [head_dim], written (zero for no rows); NULL without the norm.
+ *   workspace: (device) >= padoc_qk_rotary_bwd_workspace_size bytes, 256-byte aligned.
+ * Sums in fp32 in a fixed order: the same call gives the same bits.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, CUDA. */
+padoc_status padoc_qk_rotary_bwd(const padoc_rotary *rot, const padoc_qkv_rows *in, const void *dq_out,
+                                 int64_t dq_out_stride, const void *dk_out, int64_t dk_out_stride, void *dq,
+                                 int64_t dq_stride, void *dk, int64_t dk_stride, float *dq_weight, float *dk_weight,
+                                 void *workspace, size_t workspace_bytes, padoc_stream_t stream);
+
+/* padoc_append_inputs with the norm and the rotation on the way: for i < count, row src_rows[i] (row i with
+ * src_rows NULL) of `in` gives its K heads, normed and rotated, and its V heads to pool slot slots[i], and,
+ * when in->q is not NULL, its query heads, normed and rotated, to row i of q_dst ([count][Hq][d], contiguous).
+ * The pool has the rows' dtype, KV heads and head_dim; its results are those of padoc_qk_rotary followed by
+ * padoc_append_inputs. A slot or source row out of range sets the device error word (code 1) and that input
+ * is skipped. Errors: INVALID_ARGUMENT, UNSUPPORTED, CUDA. */
+padoc_status padoc_append_rotary_inputs(const padoc_kv_pool *pool, const padoc_rotary *rot, const padoc_qkv_rows *in,
+                                        void *q_dst, const int32_t *src_rows, const int32_t *slots, int32_t count,
+                                        padoc_stream_t stream);
+
+/* padoc_append_rotary_inputs into an E4M3 pool (bf16 rows). The rotated K is encoded from fp32, without a
+ * rounding to bf16 between. Inputs that follow one another into consecutive rows of one block
+ * (slots[i + 1] = slots[i] + 1) are one run and may be a whole prefix: a run at rows r0 .. of a block sets its
+ * scale to max(old scale, amax over the run / 448), the old one taken as 0 when r0 = 0; when the scale grows
+ * from a nonzero old one, rows 0 .. r0-1 are encoded again as in padoc_append_inputs_e4m3; the run's codes are
+ * those of value / new scale. Rows past the run are left as they are. Inputs of one call in one block that are
+ * not one run race. Errors: INVALID_ARGUMENT, UNSUPPORTED (block_size 16, head_dim 128), CUDA. */
+padoc_status padoc_append_rotary_inputs_e4m3(const padoc_kv_pool_e4m3 *pool, const padoc_rotary *rot,
+                                             const padoc_qkv_rows *in, void *q_dst, const int32_t *src_rows,
+                                             const int32_t *slots, int32_t count, padoc_stream_t stream);
+
+/* ============================================================================================
+ * Copies of cache blocks, and what the loop's scheduler does with them
+ * ========================================================================================== */
+
+/* Copies whole blocks (K and V) by pairs, in every pool of a list at once (one pool a layer; layers share
+ * their block tables): block src_blocks[i] of src[j] to block dst_blocks[i] of dst[j], for i < count,
+ * j < num_pools. dst may be src (copies within the pools). All pools have one block size, KV head count,
+ * head_dim and dtype; the pools of a side have one num_blocks.
+ *   src_blocks, dst_blocks: (device) int32 [count]. An id out of range sets the device error word (code 1) and
+ *   that pair is skipped. A block must not be the destination of two pairs, nor, within the same pools,
+ *   source of one pair and destination of another: such pairs race.
+ * One launch for each 32 pools. Errors: INVALID_ARGUMENT, UNSUPPORTED, CUDA. */
+padoc_status padoc_copy_kv_blocks(const padoc_kv_pool *dst, const padoc_kv_pool *src, int32_t num_pools,
+                                  const int32_t *src_blocks, const int32_t *dst_blocks, int32_t count,
+                                  padoc_stream_t stream);
+
+/* The same for E4M3 pools: codes and scales. */
+padoc_status padoc_copy_kv_blocks_e4m3(const padoc_kv_pool_e4m3 *dst, const padoc_kv_pool_e4m3 *src, int32_t num_pools,
+                                       const int32_t *src_blocks, const int32_t *dst_blocks, int32_t count,
+                                       padoc_stream_t stream);
+
+/* Forks a live branch into num_copies more branches with the same history (several candidates of a
+ * region's content): same page and cutoff, the same private rows. Complete private blocks are shared (they
+ * are freed with their last owner); a partly filled last block, which the branches go on writing, is
+ * copied: src_blocks[j], dst_blocks[j] (host, [num_copies]) receive the num_pairs pairs (num_copies, or 0
+ * when the last block is full) that the caller passes to padoc_copy_kv_blocks before the next step.
+ * new_streams: (host) int32 [num_copies]; the copies come behind the page's live branches. Between steps.
+ * Errors: INVALID_ARGUMENT (also during a step, a layout stream, a stream that is not live); CAPACITY when the
+ * pool has too few free blocks (nothing changes). */
+padoc_status padoc_mpd_fork_stream(padoc_mpd *mpd, int32_t stream, int32_t num_copies, int32_t *new_streams,
+                                   int32_t *src_blocks, int32_t *dst_blocks, int32_t *num_pairs);
+
+/* Retires a live stream between steps (a candidate that lost), or every stream of a live page (a request
+ * that was cancelled); blocks return to the pool as at an EOS. Errors: INVALID_ARGUMENT (also during a step, a
+ * stream or page that is not live). */
+padoc_status padoc_mpd_drop_stream(padoc_mpd *mpd, int32_t stream);
+padoc_status padoc_mpd_drop_page(padoc_mpd *mpd, int32_t page);
+
+/* Moves the live blocks to the lowest ids, so that with B live blocks every block from B on is free: live
+ * blocks at B and above go to the free ids below B, both in ascending order. src_blocks, dst_blocks: (host)
+ * int32 [capacity] receive the moves for padoc_copy_kv_blocks, which the caller runs before the next step (no
+ * block is both source and destination); num_pairs: their count. Free blocks are handed out in ascending
+ * order afterwards. Between steps. Errors: INVALID_ARGUMENT; CAPACITY when capacity is below the moves
+ * (num_pairs is set, nothing changes). */
+padoc_status padoc_mpd_compact(padoc_mpd *mpd, int32_t *src_blocks, int32_t *dst_blocks, int32_t capacity,
+                               int32_t *num_pairs);
+
+/* Changes the number of pool blocks, between steps: new blocks are handed out behind the free ones; blocks
+ * given up must be free (padoc_mpd_compact first). The caller moves the live blocks into a pool of the new
+ * size. Errors: INVALID_ARGUMENT (also a negative or too large number); CAPACITY when a live block would be given up. */
+padoc_status padoc_mpd_resize(padoc_mpd *mpd, int32_t num_blocks);
+
+/* padoc_mpd_launch_step with padoc_append_rotary_inputs as its append: `in` holds the inputs' rows (in->q
+ * required) and their positions; dtype, heads and head_dim are the pool's. Errors: as padoc_mpd_launch_step. */
+padoc_status padoc_mpd_launch_step_rotary(const padoc_mpd_step *step, const int32_t *stage, int32_t *dev_ints,
+                                          int64_t dev_capacity_words, const padoc_kv_pool *pool, const padoc_rotary *rot,
+                                          const padoc_qkv_rows *in, void *q_dst, float scale, void *out, float *lse,
+                                          void *workspace, size_t workspace_bytes, padoc_stream_t stream);
+
+/* Makes the runner's steps from now on append with the norm and the rotation (rot NULL: as they are): the
+ * struct is copied, its device arrays and pos ((device) int32 [pos_rows][num_axes], a position for each source
+ * row of the steps) must live on. A step whose src_total exceeds pos_rows is INVALID_ARGUMENT.
+ * Errors: INVALID_ARGUMENT (also a head_dim that is not the pool's), UNSUPPORTED. */
+padoc_status padoc_mpd_runner_set_rotary(padoc_mpd_runner *runner, const padoc_rotary *rot, const int32_t *pos,
+                                         int64_t pos_rows);
 
 /* ============================================================================================
  * C3: packed variable-length ancestor prefill (training forward / branch prefill)

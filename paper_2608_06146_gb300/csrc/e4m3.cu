@@ -6,6 +6,7 @@
 // finite value. All arithmetic that decides a code is fp32 with round-to-nearest-even (division and
 // product rounded once each), so the codes are a function of the inputs alone.
 #include "common.cuh"
+#include "rotary.cuh"
 #include "tc.cuh"
 
 namespace {
@@ -195,6 +196,148 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_e4m3_kernel(
     }
 }
 
+// The rotary form of the append (padoc_append_rotary_inputs_e4m3): K rows are normed and rotated in fp32 and
+// encoded from there. The inputs of a call that follow one another into consecutive rows of a block are one
+// run, which the CTA of its first input writes: the scale becomes max(old, amax over the run / 448) (the old
+// one taken as 0 when the run starts the block), rows before the run are encoded again when it grows, and the
+// run's codes are those of x / new scale. A warp takes a (K or V, head) at a time with the run's rows in
+// registers, a lane two pairs of rotated dims (or four dims) of each; every CTA also lays out its own
+// input's query heads. Rows past the run are left as they are.
+struct RotaryAppendArgs {
+    padoc_rotary_dev::Spec sp;
+    const __nv_bfloat16 *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t *pos;
+    int64_t src_total;
+    __nv_bfloat16 *q_dst;
+    const int32_t *src_rows, *slots;
+    uint8_t *k_codes, *v_codes;
+    float *k_scales, *v_scales;
+    int64_t pool_slots;
+    int32_t hq, hkv, count;
+    int *err;
+};
+
+template <bool kAdjacent, bool kNorm>
+__global__ void __launch_bounds__(32 * kAppendWarps) append_rotary_e4m3_kernel(const RotaryAppendArgs p)
+{
+    using namespace padoc_rotary_dev;
+    pdl_wait_prerequisite();
+    pdl_launch_dependents();
+    const int i = blockIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t own = p.src_rows ? (int64_t)p.src_rows[i] : i;
+    const int64_t slot = p.slots[i];
+    const bool slot_ok = slot >= 0 && slot < p.pool_slots, row_ok = own >= 0 && own < p.src_total;
+    if (!slot_ok || !row_ok) {
+        if (threadIdx.x == 0) padoc_record_error(p.err, PADOC_DEVERR_BLOCK_ID, slot_ok ? (int)own : (int)slot);
+        if (!slot_ok) return;
+    }
+    if (p.q && row_ok) {   // the query heads: 16 lanes each
+        const Place pl = lane_place<4, kAdjacent>(lane & 15, kD, p.sp.rot);
+        float c[4], s[4];
+        if (pl.turned) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                cos_sin(p.sp.freq[(lane & 15) * 4 + j], p.pos + own * p.sp.axes, p.sp.amplitude, c[j], s[j]);
+        }
+        for (int h0 = 2 * warp; h0 < p.hq; h0 += 2 * kAppendWarps) {
+            const int h = h0 + (lane >> 4);
+            Place ph = pl;
+            ph.active = h < p.hq;
+            float a[4], b[4];
+            if (ph.active) {
+                load_vec<4>(p.q + own * p.q_stride + (int64_t)h * kD + pl.a, a);
+                load_vec<4>(p.q + own * p.q_stride + (int64_t)h * kD + pl.b, b);
+            }
+            if constexpr (kNorm) norm_head<__nv_bfloat16, 4>(a, b, static_cast<const __nv_bfloat16 *>(p.sp.q_weight), ph, p.sp, 16);
+            if (ph.active) {
+                if (pl.turned) turn_pairs<4, kAdjacent, false>(a, b, c, s);
+                __nv_bfloat16 *dst = p.q_dst + ((int64_t)i * p.hq + h) * kD;
+                store_vec<4>(dst + pl.a, a);
+                store_vec<4>(dst + pl.b, b);
+            }
+        }
+    }
+    const int r0 = (int)(slot % kBlk);
+    if (i > 0 && r0 > 0 && (int64_t)p.slots[i - 1] + 1 == slot) return;   // a run's later input
+    // the run: lane j looks at input i + j
+    int64_t row = -1;
+    bool in_run = false;
+    if (lane < kBlk - r0 && i + lane < p.count) {
+        in_run = (int64_t)p.slots[i + lane] == slot + lane;
+        if (in_run) row = p.src_rows ? (int64_t)p.src_rows[i + lane] : i + lane;
+    }
+    const uint32_t run_bits = __ballot_sync(0xffffffffu, in_run);
+    const int n = __ffs((int)~run_bits) - 1;   // (at most 16 lanes look)
+    const uint32_t good = __ballot_sync(0xffffffffu, lane < n && row >= 0 && row < p.src_total);
+    if (!good) return;
+    const int64_t blk = slot / kBlk;
+    const Place pl = lane_place<2, kAdjacent>(lane, kD, p.sp.rot);
+    for (int u = warp; u < 2 * p.hkv; u += kAppendWarps) {
+        const bool is_v = u >= p.hkv;
+        const int g = is_v ? u - p.hkv : u;
+        float *scp = (is_v ? p.v_scales : p.k_scales) + blk * p.hkv + g;
+        uint8_t *codes = (is_v ? p.v_codes : p.k_codes) + (blk * p.hkv + g) * kBlk * kD;
+        const float s_old = r0 == 0 ? 0.f : *scp;
+        uint32_t old[kBlk - 1];
+#pragma unroll
+        for (int rr = 0; rr < kBlk - 1; ++rr)
+            old[rr] = rr < r0 ? *reinterpret_cast<const uint16_t *>(codes + rr * kD + pl.a) |
+                                    (uint32_t) * reinterpret_cast<const uint16_t *>(codes + rr * kD + pl.b) << 16
+                              : 0u;
+        float a[kBlk][2], b[kBlk][2];
+        float amax = 0.f;
+#pragma unroll
+        for (int j = 0; j < kBlk; ++j) {
+            if (j >= n) break;
+            const int64_t src = __shfl_sync(0xffffffffu, row, j);
+            if (!(good >> j & 1u)) {
+                a[j][0] = a[j][1] = b[j][0] = b[j][1] = 0.f;
+                continue;
+            }
+            const __nv_bfloat16 *x = (is_v ? p.v + src * p.v_stride : p.k + src * p.k_stride) + (int64_t)g * kD;
+            load_vec<2>(x + pl.a, a[j]);
+            load_vec<2>(x + pl.b, b[j]);
+            if (!is_v) {
+                if constexpr (kNorm)
+                    norm_head<__nv_bfloat16, 2>(a[j], b[j], static_cast<const __nv_bfloat16 *>(p.sp.k_weight), pl, p.sp, 32);
+                if (pl.turned) {
+                    float c[2], s[2];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        cos_sin(p.sp.freq[lane * 2 + t], p.pos + src * p.sp.axes, p.sp.amplitude, c[t], s[t]);
+                    turn_pairs<2, kAdjacent, false>(a[j], b[j], c, s);
+                }
+            }
+            amax = fmaxf(amax, fmaxf(fmaxf(fabsf(a[j][0]), fabsf(a[j][1])), fmaxf(fabsf(b[j][0]), fabsf(b[j][1]))));
+        }
+        const float cand = __fdiv_rn(warp_max(amax), 448.f);
+        const Scale sc = make_scale(cand > s_old ? cand : s_old);
+        if (sc.s > s_old && s_old > 0.f) {
+#pragma unroll
+            for (int rr = 0; rr < kBlk - 1; ++rr) {
+                if (rr >= r0) break;
+                float y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = __fmul_rn(e4m3_to_f32((uint8_t)(old[rr] >> (8 * j))), s_old);
+                *reinterpret_cast<uint16_t *>(codes + rr * kD + pl.a) = (uint16_t)sc.codes(y[0], y[1]);
+                *reinterpret_cast<uint16_t *>(codes + rr * kD + pl.b) = (uint16_t)sc.codes(y[2], y[3]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kBlk; ++j) {
+            if (j >= n) break;
+            if (!(good >> j & 1u)) continue;
+            uint8_t *dst = codes + (r0 + j) * kD;
+            *reinterpret_cast<uint16_t *>(dst + pl.a) = sc.s > 0.f ? (uint16_t)sc.codes(a[j][0], a[j][1]) : (uint16_t)0;
+            *reinterpret_cast<uint16_t *>(dst + pl.b) = sc.s > 0.f ? (uint16_t)sc.codes(b[j][0], b[j][1]) : (uint16_t)0;
+        }
+        __syncwarp();   // every lane has read the old scale before it is replaced
+        if (lane == 0) *scp = sc.s;
+    }
+}
+
 bool e4m3_pool_ok(const padoc_kv_pool_e4m3 *pool)
 {
     return pool && pool->k_codes && pool->v_codes && pool->k_scales && pool->v_scales && pool->num_blocks >= 1 &&
@@ -259,5 +402,52 @@ extern "C" padoc_status padoc_append_inputs_e4m3(const padoc_kv_pool_e4m3 *pool,
                                       (uint8_t *)pool->k_codes, (uint8_t *)pool->v_codes, (float *)pool->k_scales,
                                       (float *)pool->v_scales, (int64_t)pool->num_blocks * kBlk, pool->num_kv_heads,
                                       q_src ? num_q_heads : 0, err));
+    return padoc_launch_status();
+}
+
+extern "C" padoc_status padoc_append_rotary_inputs_e4m3(const padoc_kv_pool_e4m3 *pool, const padoc_rotary *rot,
+                                                        const padoc_qkv_rows *in, void *q_dst, const int32_t *src_rows,
+                                                        const int32_t *slots, int32_t count, padoc_stream_t stream)
+{
+    using namespace padoc_rotary_dev;
+    if (!e4m3_pool_ok(pool) || count < 0) return PADOC_ERR_INVALID_ARGUMENT;
+    padoc_status st = check_spec(rot);
+    if (st != PADOC_OK) return st;
+    st = check_rows(in, rot, true);
+    if (st != PADOC_OK) return st;
+    if (in->dtype != PADOC_DTYPE_BF16 || pool->head_dim != rot->head_dim || pool->num_kv_heads != in->num_kv_heads)
+        return PADOC_ERR_INVALID_ARGUMENT;
+    if (pool->block_size != kBlk || pool->head_dim != kD) return PADOC_ERR_UNSUPPORTED;
+    if (count == 0) return PADOC_OK;
+    if (in->rows == 0 || !slots || (in->q && !q_dst)) return PADOC_ERR_INVALID_ARGUMENT;
+    const uintptr_t align = (uintptr_t)pool->k_codes | (uintptr_t)pool->v_codes | (uintptr_t)q_dst;
+    if ((align & 15) || (((uintptr_t)pool->k_scales | (uintptr_t)pool->v_scales) & 3)) return PADOC_ERR_INVALID_ARGUMENT;
+    RotaryAppendArgs p = {};
+    p.err = padoc_device_error_word();
+    if (!p.err) return PADOC_ERR_CUDA;
+    p.sp = make_spec(rot);
+    p.q = (const __nv_bfloat16 *)in->q, p.k = (const __nv_bfloat16 *)in->k, p.v = (const __nv_bfloat16 *)in->v;
+    p.q_stride = in->q_stride, p.k_stride = in->k_stride, p.v_stride = in->v_stride;
+    p.pos = in->pos;
+    p.src_total = in->rows;
+    p.q_dst = (__nv_bfloat16 *)q_dst;
+    p.src_rows = src_rows, p.slots = slots;
+    p.k_codes = (uint8_t *)pool->k_codes, p.v_codes = (uint8_t *)pool->v_codes;
+    p.k_scales = (float *)pool->k_scales, p.v_scales = (float *)pool->v_scales;
+    p.pool_slots = (int64_t)pool->num_blocks * kBlk;
+    p.hq = in->num_q_heads, p.hkv = in->num_kv_heads, p.count = count;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)count);
+    lc.blockDim = dim3(32 * kAppendWarps);
+    lc.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see the kernel's wait
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    const bool norm = rot->q_weight != nullptr;
+    auto *kernel = rot->adjacent ? (norm ? append_rotary_e4m3_kernel<true, true> : append_rotary_e4m3_kernel<true, false>)
+                                 : (norm ? append_rotary_e4m3_kernel<false, true> : append_rotary_e4m3_kernel<false, false>);
+    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, p));
     return padoc_launch_status();
 }

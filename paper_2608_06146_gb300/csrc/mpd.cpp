@@ -8,7 +8,9 @@
 // shared stream, so every later fork sees it; a branch's input extends its own private rows, which
 // no other stream can reach. A fork copies the layout stream's row before its boundary output is
 // appended, which is the shared stream's current length. Retiring removes the row and returns the
-// stream's private blocks; a page's shared blocks return once its last stream has retired.
+// stream's private blocks; a page's shared blocks return once its last stream has retired. A branch can
+// also be forked with its history (candidates of one region): the copies share its complete private
+// blocks, which return with their last owner, and own a copy of the partly filled one.
 #include <algorithm>
 #include <climits>
 #include <cstdint>
@@ -21,6 +23,7 @@
 
 #include "padoc_attn.h"
 #include "plan_build.h"
+#include "rotary.cuh"
 
 namespace {
 
@@ -46,6 +49,7 @@ struct padoc_mpd {
     int32_t bs = 16;
     int32_t num_blocks = 0;
     std::deque<int32_t> free_blocks;
+    std::vector<int32_t> more_owners;  // per block: streams that share it besides its first owner
     std::vector<MpdPage> pages;        // by page id
     std::vector<int32_t> live_pages;   // page ids in admission order
     std::vector<MpdStream> streams;    // by stream id
@@ -67,7 +71,10 @@ int32_t take_block(padoc_mpd *m)
 
 void give_blocks(padoc_mpd *m, std::vector<int32_t> &blocks)
 {
-    for (int32_t b : blocks) m->free_blocks.push_back(b);
+    for (int32_t b : blocks) {
+        if (m->more_owners[(size_t)b] > 0) --m->more_owners[(size_t)b];
+        else m->free_blocks.push_back(b);
+    }
     std::vector<int32_t>().swap(blocks);
 }
 
@@ -83,7 +90,35 @@ int32_t new_stream(padoc_mpd *m, int32_t page, bool layout, int32_t cutoff)
     return (int32_t)m->streams.size() - 1;
 }
 
+// Takes a live stream out; a branch's private blocks return to the pool.
+void retire(padoc_mpd *m, int32_t id)
+{
+    MpdStream &s = m->streams[(size_t)id];
+    MpdPage &pg = m->pages[(size_t)s.page];
+    s.live = false;
+    if (s.layout) {
+        pg.layout_stream = -1;
+    } else {
+        give_blocks(m, s.blocks);
+        pg.branches.erase(std::find(pg.branches.begin(), pg.branches.end(), id));
+    }
+}
+
 int32_t page_streams(const MpdPage &pg) { return (int32_t)pg.branches.size() + (pg.layout_stream >= 0 ? 1 : 0); }
+
+// Takes the pages without a live stream out; their shared blocks return to the pool.
+void sweep_pages(padoc_mpd *m)
+{
+    size_t w = 0;
+    for (size_t r = 0; r < m->live_pages.size(); ++r) {
+        MpdPage &pg = m->pages[(size_t)m->live_pages[r]];
+        if (page_streams(pg) > 0)
+            m->live_pages[w++] = m->live_pages[r];
+        else
+            give_blocks(m, pg.blocks);
+    }
+    m->live_pages.resize(w);
+}
 
 }  // namespace
 
@@ -104,6 +139,7 @@ extern "C" padoc_status padoc_mpd_create(int32_t num_blocks, int32_t block_size,
     if (!m) return PADOC_ERR_INVALID_ARGUMENT;
     m->bs = block_size;
     m->num_blocks = num_blocks;
+    m->more_owners.assign((size_t)num_blocks, 0);
     for (int32_t i = 0; i < num_blocks; ++i) m->free_blocks.push_back(block_order ? block_order[i] : i);
     *mpd = m;
     return PADOC_OK;
@@ -263,27 +299,9 @@ extern "C" padoc_status padoc_mpd_end_step(padoc_mpd *m, const int32_t *num_fork
             m->pages[pid].branches.push_back(nid);
             new_streams[k++] = nid;
         }
-        if (eos && eos[i]) {
-            MpdStream &s = m->streams[id];
-            MpdPage &pg = m->pages[pid];
-            s.live = false;
-            if (s.layout) {
-                pg.layout_stream = -1;
-            } else {
-                give_blocks(m, s.blocks);
-                pg.branches.erase(std::find(pg.branches.begin(), pg.branches.end(), id));
-            }
-        }
+        if (eos && eos[i]) retire(m, id);
     }
-    size_t w = 0;
-    for (size_t r = 0; r < m->live_pages.size(); ++r) {
-        MpdPage &pg = m->pages[m->live_pages[r]];
-        if (page_streams(pg) > 0)
-            m->live_pages[w++] = m->live_pages[r];
-        else
-            give_blocks(m, pg.blocks);
-    }
-    m->live_pages.resize(w);
+    sweep_pages(m);
     m->step_streams.clear();
     m->in_step = false;
     *num_new = k;
@@ -392,11 +410,12 @@ extern "C" padoc_status padoc_mpd_prepare_step(padoc_mpd *m, const padoc_decode_
     return PADOC_OK;
 }
 
-extern "C" padoc_status padoc_mpd_launch_step(const padoc_mpd_step *step, const int32_t *stage, int32_t *dev_ints,
-                                              int64_t dev_capacity_words, const padoc_kv_pool *pool,
-                                              const void *k_src, const void *v_src, const void *q_src,
-                                              int64_t src_total, void *q_dst, float scale, void *out, float *lse,
-                                              void *workspace, size_t workspace_bytes, padoc_stream_t stream)
+namespace {
+
+// The step's copy, append (with rot: normed and rotated) and decode, after the caller's own checks.
+padoc_status launch_step(const padoc_mpd_step *step, const int32_t *stage, int32_t *dev_ints, int64_t dev_capacity_words,
+                         const padoc_kv_pool *pool, const padoc_rotary *rot, const padoc_qkv_rows &in, void *q_dst,
+                         float scale, void *out, float *lse, void *workspace, size_t workspace_bytes, padoc_stream_t stream)
 {
     if (!step || !dev_ints || !pool) return PADOC_ERR_INVALID_ARGUMENT;
     const int32_t C = step->num_streams;
@@ -410,13 +429,168 @@ extern "C" padoc_status padoc_mpd_launch_step(const padoc_mpd_step *step, const 
     if (stage && cudaMemcpyAsync(dev_ints, stage, (size_t)step->upload_words * sizeof(int32_t), cudaMemcpyHostToDevice,
                                  (cudaStream_t)stream) != cudaSuccess)
         return PADOC_ERR_CUDA;
-    padoc_status st = padoc_append_inputs(pool, k_src, v_src, q_src, src_total, info.cfg.num_q_heads, q_dst,
-                                          dev_ints + step->off_rows, dev_ints + step->off_slots, C, stream);
+    const int32_t *rows = dev_ints + step->off_rows, *slots = dev_ints + step->off_slots;
+    const padoc_status st = rot ? padoc_append_rotary_inputs(pool, rot, &in, q_dst, rows, slots, C, stream)
+                                : padoc_append_inputs(pool, in.k, in.v, in.q, in.rows, info.cfg.num_q_heads, q_dst, rows,
+                                                      slots, C, stream);
     if (st != PADOC_OK) return st;
     return padoc_branch_decode_attn_after_append(pool, &info, dev_ints + step->off_plan, dev_ints + step->off_page_table,
                                     step->page_stride, dev_ints + step->off_stream_table, step->stream_stride, q_dst,
                                     scale, out, lse, workspace, workspace_bytes, stream,
                                                  step->plan.num_warps > 0 ? dev_ints + step->off_first_blocks : nullptr);
+}
+
+}  // namespace
+
+extern "C" padoc_status padoc_mpd_launch_step(const padoc_mpd_step *step, const int32_t *stage, int32_t *dev_ints,
+                                              int64_t dev_capacity_words, const padoc_kv_pool *pool,
+                                              const void *k_src, const void *v_src, const void *q_src,
+                                              int64_t src_total, void *q_dst, float scale, void *out, float *lse,
+                                              void *workspace, size_t workspace_bytes, padoc_stream_t stream)
+{
+    padoc_qkv_rows in = {};
+    in.q = q_src, in.k = k_src, in.v = v_src;
+    in.rows = src_total;
+    return launch_step(step, stage, dev_ints, dev_capacity_words, pool, nullptr, in, q_dst, scale, out, lse, workspace,
+                       workspace_bytes, stream);
+}
+
+extern "C" padoc_status padoc_mpd_launch_step_rotary(const padoc_mpd_step *step, const int32_t *stage, int32_t *dev_ints,
+                                                     int64_t dev_capacity_words, const padoc_kv_pool *pool,
+                                                     const padoc_rotary *rot, const padoc_qkv_rows *in, void *q_dst,
+                                                     float scale, void *out, float *lse, void *workspace,
+                                                     size_t workspace_bytes, padoc_stream_t stream)
+{
+    if (!step || !rot || !in) return PADOC_ERR_INVALID_ARGUMENT;
+    if (step->num_streams > 0 && (!in->q || in->num_q_heads != step->plan.cfg.num_q_heads)) return PADOC_ERR_INVALID_ARGUMENT;
+    return launch_step(step, stage, dev_ints, dev_capacity_words, pool, rot, *in, q_dst, scale, out, lse, workspace,
+                       workspace_bytes, stream);
+}
+
+// ---- forking, dropping and compacting between steps -------------------------------------------------
+
+extern "C" padoc_status padoc_mpd_fork_stream(padoc_mpd *m, int32_t stream, int32_t num_copies, int32_t *new_streams,
+                                              int32_t *src_blocks, int32_t *dst_blocks, int32_t *num_pairs)
+{
+    if (!m || m->in_step || stream < 0 || (size_t)stream >= m->streams.size() || num_copies < 0 || !num_pairs)
+        return PADOC_ERR_INVALID_ARGUMENT;
+    if (!m->streams[(size_t)stream].live || m->streams[(size_t)stream].layout) return PADOC_ERR_INVALID_ARGUMENT;
+    if (num_copies > 0 && (!new_streams || !src_blocks || !dst_blocks)) return PADOC_ERR_INVALID_ARGUMENT;
+    *num_pairs = 0;
+    const bool tail = m->streams[(size_t)stream].priv_len % m->bs != 0;
+    if (tail && (size_t)num_copies > m->free_blocks.size()) return PADOC_ERR_CAPACITY;
+    if ((size_t)num_copies > (size_t)INT32_MAX - m->streams.size()) return PADOC_ERR_CAPACITY;
+    try {   // everything that can run out of memory comes before the first change
+        std::vector<MpdStream> copies((size_t)num_copies, m->streams[(size_t)stream]);
+        MpdPage &pg = m->pages[(size_t)m->streams[(size_t)stream].page];
+        const auto room = [&](auto &v) {
+            if (v.size() + copies.size() > v.capacity()) v.reserve(std::max(v.size() + copies.size(), 2 * v.capacity()));
+        };
+        room(m->streams);
+        room(pg.branches);
+        for (int32_t j = 0; j < num_copies; ++j) {
+            MpdStream &s = copies[(size_t)j];
+            const size_t full = s.blocks.size() - (tail ? 1 : 0);
+            for (size_t b = 0; b < full; ++b) ++m->more_owners[(size_t)s.blocks[b]];
+            if (tail) {
+                src_blocks[j] = s.blocks.back();
+                dst_blocks[j] = s.blocks.back() = take_block(m);
+            }
+            new_streams[j] = (int32_t)m->streams.size();
+            pg.branches.push_back(new_streams[j]);
+            m->streams.push_back(std::move(s));
+        }
+    } catch (const std::bad_alloc &) {
+        return PADOC_ERR_CAPACITY;
+    }
+    *num_pairs = tail ? num_copies : 0;
+    return PADOC_OK;
+}
+
+extern "C" padoc_status padoc_mpd_drop_stream(padoc_mpd *m, int32_t stream)
+{
+    if (!m || m->in_step || stream < 0 || (size_t)stream >= m->streams.size() || !m->streams[(size_t)stream].live)
+        return PADOC_ERR_INVALID_ARGUMENT;
+    try {
+        retire(m, stream);
+        sweep_pages(m);
+    } catch (const std::bad_alloc &) {
+        return PADOC_ERR_CAPACITY;
+    }
+    return PADOC_OK;
+}
+
+extern "C" padoc_status padoc_mpd_drop_page(padoc_mpd *m, int32_t page)
+{
+    if (!m || m->in_step || std::find(m->live_pages.begin(), m->live_pages.end(), page) == m->live_pages.end())
+        return PADOC_ERR_INVALID_ARGUMENT;
+    try {
+        MpdPage &pg = m->pages[(size_t)page];
+        while (!pg.branches.empty()) retire(m, pg.branches.back());
+        if (pg.layout_stream >= 0) retire(m, pg.layout_stream);
+        sweep_pages(m);
+    } catch (const std::bad_alloc &) {
+        return PADOC_ERR_CAPACITY;
+    }
+    return PADOC_OK;
+}
+
+extern "C" padoc_status padoc_mpd_compact(padoc_mpd *m, int32_t *src_blocks, int32_t *dst_blocks, int32_t capacity,
+                                          int32_t *num_pairs)
+{
+    if (!m || m->in_step || capacity < 0 || !num_pairs || (capacity > 0 && (!src_blocks || !dst_blocks)))
+        return PADOC_ERR_INVALID_ARGUMENT;
+    try {
+        const int32_t live = m->num_blocks - (int32_t)m->free_blocks.size();
+        std::vector<uint8_t> is_free((size_t)m->num_blocks, 0);
+        for (int32_t b : m->free_blocks) is_free[(size_t)b] = 1;
+        int32_t n = 0;   // as many free ids below `live` as live ids from there on
+        for (int32_t b = live; b < m->num_blocks; ++b) n += !is_free[(size_t)b];
+        *num_pairs = n;
+        if (n > capacity) return PADOC_ERR_CAPACITY;
+        std::vector<int32_t> to((size_t)m->num_blocks);
+        std::deque<int32_t> free_after;
+        for (int32_t b = live; b < m->num_blocks; ++b) free_after.push_back(b);
+        for (int32_t b = 0; b < m->num_blocks; ++b) to[(size_t)b] = b;
+        for (int32_t b = live, d = 0, i = 0; b < m->num_blocks; ++b) {
+            if (is_free[(size_t)b]) continue;
+            while (!is_free[(size_t)d]) ++d;
+            src_blocks[i] = b;
+            dst_blocks[i++] = to[(size_t)b] = d;
+            m->more_owners[(size_t)d] = m->more_owners[(size_t)b];
+            m->more_owners[(size_t)b] = 0;
+            ++d;
+        }
+        for (int32_t pid : m->live_pages) {
+            MpdPage &pg = m->pages[(size_t)pid];
+            for (int32_t &b : pg.blocks) b = to[(size_t)b];
+            for (int32_t id : pg.branches)
+                for (int32_t &b : m->streams[(size_t)id].blocks) b = to[(size_t)b];
+        }
+        m->free_blocks.swap(free_after);
+    } catch (const std::bad_alloc &) {
+        return PADOC_ERR_CAPACITY;
+    }
+    return PADOC_OK;
+}
+
+extern "C" padoc_status padoc_mpd_resize(padoc_mpd *m, int32_t num_blocks)
+{
+    if (!m || m->in_step || num_blocks < 0 || (int64_t)num_blocks * m->bs >= ((int64_t)1 << 31)) return PADOC_ERR_INVALID_ARGUMENT;
+    try {
+        std::deque<int32_t> kept;
+        for (int32_t b : m->free_blocks)
+            if (b < num_blocks) kept.push_back(b);
+        const int32_t gone = (int32_t)(m->free_blocks.size() - kept.size());
+        if (num_blocks < m->num_blocks && gone != m->num_blocks - num_blocks) return PADOC_ERR_CAPACITY;
+        for (int32_t b = m->num_blocks; b < num_blocks; ++b) kept.push_back(b);
+        m->more_owners.resize((size_t)num_blocks, 0);
+        m->free_blocks.swap(kept);
+        m->num_blocks = num_blocks;
+    } catch (const std::bad_alloc &) {
+        return PADOC_ERR_CAPACITY;
+    }
+    return PADOC_OK;
 }
 
 // ---- the step loop's host side in one call per step (padoc_mpd_runner_*) ----------------------
@@ -436,6 +610,10 @@ struct padoc_mpd_runner {
     void *workspace = nullptr;
     size_t workspace_bytes = 0;
     int64_t turn = 0;
+    bool rotate = false;           // the steps append with rot at positions pos [pos_rows]
+    padoc_rotary rot{};
+    const int32_t *pos = nullptr;
+    int64_t pos_rows = 0;
     int last = -1;                 // stage of the last prepared step
     padoc_mpd_step last_step{};
 };
@@ -508,6 +686,25 @@ extern "C" void padoc_mpd_runner_destroy(padoc_mpd_runner *r)
     delete r;
 }
 
+extern "C" padoc_status padoc_mpd_runner_set_rotary(padoc_mpd_runner *r, const padoc_rotary *rot, const int32_t *pos,
+                                                    int64_t pos_rows)
+{
+    if (!r) return PADOC_ERR_INVALID_ARGUMENT;
+    if (!rot) {
+        r->rotate = false;
+        return PADOC_OK;
+    }
+    const padoc_status st = padoc_rotary_dev::check_spec(rot);
+    if (st != PADOC_OK) return st;
+    if (rot->head_dim != r->cfg.head_dim || pos_rows < 0 || (pos_rows > 0 && !pos) || (((uintptr_t)pos) & 3))
+        return PADOC_ERR_INVALID_ARGUMENT;
+    r->rotate = true;
+    r->rot = *rot;
+    r->pos = pos;
+    r->pos_rows = pos_rows;
+    return PADOC_OK;
+}
+
 extern "C" padoc_status padoc_mpd_runner_step(padoc_mpd_runner *r, const padoc_mpd_run_args *a, int32_t *num_streams,
                                               int64_t *upload_bytes)
 {
@@ -523,6 +720,8 @@ extern "C" padoc_status padoc_mpd_runner_step(padoc_mpd_runner *r, const padoc_m
                   !a->lse))
         return PADOC_ERR_INVALID_ARGUMENT;
     if (C > 0 && (int64_t)a->num_stream_ids < (int64_t)m->streams.size()) return PADOC_ERR_INVALID_ARGUMENT;
+    if (r->pool.num_blocks < m->num_blocks) return PADOC_ERR_INVALID_ARGUMENT;   // (the scheduler was resized)
+    if (C > 0 && r->rotate && a->src_total > r->pos_rows) return PADOC_ERR_INVALID_ARGUMENT;
     const cudaStream_t stream = (cudaStream_t)a->stream;
     const int b = (int)(r->turn & 1);
     if (r->recorded[b]) {   // the copy that read this stage two steps ago (usually done: ask first)
@@ -569,9 +768,16 @@ extern "C" padoc_status padoc_mpd_runner_step(padoc_mpd_runner *r, const padoc_m
         st = grow_device(&r->q_step, &r->q_bytes, (size_t)n * r->cfg.num_q_heads * r->cfg.head_dim * elt, stream);
     if (st == PADOC_OK) st = grow_device(&r->workspace, &r->workspace_bytes, std::max<size_t>(ws, 256), stream);
     if (st != PADOC_OK) return st;
-    st = padoc_mpd_launch_step(&step, stage, r->dev_ints, r->dev_words, &r->pool, a->k_src, a->v_src, a->q_src,
-                               a->src_total, r->q_step, a->scale, a->out, a->lse, r->workspace, r->workspace_bytes,
-                               a->stream);
+    padoc_qkv_rows in = {};
+    in.q = a->q_src, in.k = a->k_src, in.v = a->v_src;
+    in.num_q_heads = r->cfg.num_q_heads, in.num_kv_heads = r->cfg.num_kv_heads;
+    in.q_stride = (int64_t)in.num_q_heads * r->cfg.head_dim;
+    in.k_stride = in.v_stride = (int64_t)in.num_kv_heads * r->cfg.head_dim;
+    in.pos = r->pos;
+    in.rows = a->src_total;
+    in.dtype = r->pool.dtype;
+    st = launch_step(&step, stage, r->dev_ints, r->dev_words, &r->pool, r->rotate ? &r->rot : nullptr, in, r->q_step,
+                     a->scale, a->out, a->lse, r->workspace, r->workspace_bytes, a->stream);
     if (st != PADOC_OK) return st;
     if (cudaEventRecord(r->copied[b], stream) != cudaSuccess) return PADOC_ERR_CUDA;
     r->recorded[b] = true;

@@ -175,6 +175,54 @@ extern "C" padoc_status padoc_build_tile_map(const padoc_page *pages, int32_t nu
     return PADOC_OK;
 }
 
+extern "C" padoc_status padoc_build_rotary_positions(const padoc_page *pages, int32_t num_pages, const padoc_grid *grids,
+                                                     int32_t num_grids, int32_t *pos, int64_t capacity_tokens,
+                                                     int32_t *prefix_end)
+{
+    int64_t T = 0;
+    const padoc_status st = validate_pages(pages, num_pages, &T);
+    if (st != PADOC_OK) return st;
+    if (num_grids < 0 || (num_grids > 0 && !grids) || (T > 0 && !pos)) return PADOC_ERR_INVALID_ARGUMENT;
+    int64_t end = 0;
+    for (int32_t i = 0; i < num_grids; ++i) {
+        const padoc_grid &g = grids[i];
+        if (g.page < 0 || g.page >= num_pages || g.begin < 0 || g.t < 1 || g.h < 1 || g.w < 1) return PADOC_ERR_INVALID_ARGUMENT;
+        if (i > 0 && (g.page < grids[i - 1].page || (g.page == grids[i - 1].page && g.begin < end))) return PADOC_ERR_INVALID_ARGUMENT;
+        const int64_t plane = (int64_t)g.h * g.w, most = pages[g.page].prefix_len - g.begin;
+        if (most < 0 || plane > most || g.t > most / plane) return PADOC_ERR_INVALID_ARGUMENT;
+        end = g.begin + g.t * plane;
+    }
+    if (capacity_tokens < T) return PADOC_ERR_CAPACITY;
+    int32_t *o = pos;
+    const auto text = [&](int32_t p) {
+        o[0] = o[1] = o[2] = p;
+        o += 3;
+    };
+    int32_t gi = 0;
+    for (int32_t i = 0; i < num_pages; ++i) {
+        const padoc_page &pg = pages[i];
+        int32_t p = 0;   // (a grid's largest side is at most its tokens: p stays below the page's length)
+        for (int32_t q = 0; q < pg.prefix_len;) {
+            if (gi < num_grids && grids[gi].page == i && grids[gi].begin == q) {
+                const padoc_grid &g = grids[gi++];
+                for (int32_t a = 0; a < g.t; ++a)
+                    for (int32_t b = 0; b < g.h; ++b)
+                        for (int32_t c = 0; c < g.w; ++c, o += 3) o[0] = p + a, o[1] = p + b, o[2] = p + c;
+                p += std::max(g.t, std::max(g.h, g.w));
+                q += g.t * g.h * g.w;
+            } else {
+                text(p++);
+                ++q;
+            }
+        }
+        if (prefix_end) prefix_end[i] = p;
+        for (int32_t j = 0; j < pg.layout_len; ++j) text(p + j);
+        for (int32_t k = 0; k < pg.num_branches; ++k)
+            for (int32_t j = 0; j < pg.branch_len[k]; ++j) text(p + pg.fork_offset[k] + j);
+    }
+    return PADOC_OK;
+}
+
 extern "C" padoc_status padoc_build_key_tile_map(const padoc_page *pages, int32_t num_pages, int32_t q_tile,
                                                  int32_t k_tile, int32_t *col_ptr, int32_t *q_tiles, int8_t *kinds,
                                                  int32_t *k_order, int64_t capacity_nnz)

@@ -82,6 +82,41 @@ class PrefillBwdPlan:
                                       self.workspace, stream)
 
 
+class RotaryPrefill:
+    """One attention layer of the packed prefill from the projections on: the head norms and rotary
+    positions of ``rotary`` (pa.Rotary), then the ancestor attention; with training also the gradients of
+    both. grids: (page, begin, t, h, w) of the image patches among the prefix tokens, whose positions are
+    padoc_build_rotary_positions'; with one axis every token has its place in the page's visible sequence."""
+
+    def __init__(self, pages, rotary, num_q_heads: int, num_kv_heads: int, dtype: torch.dtype, device, grids=(),
+                 training: bool = False):
+        d = rotary.head_dim
+        self.rotary = rotary
+        self.fwd = PrefillPlan(pages, dtype, d, device)
+        self.T = self.fwd.T
+        pos, self.prefix_end = pa.padoc_build_rotary_positions(pages, grids)
+        if rotary.num_axes > 3 or (rotary.num_axes < 3 and len(grids)):
+            raise ValueError("a page's grids need the three axes, a page without them at most three")
+        self.pos = torch.from_numpy(np.ascontiguousarray(pos[:, :rotary.num_axes])).to(device)
+        new = lambda h, n=None: torch.empty((self.T, h, d), dtype=dtype, device=device)
+        self.q, self.k = new(num_q_heads), new(num_kv_heads)   # normed and rotated
+        self.bwd = None
+        if training:
+            self.bwd = PrefillBwdPlan(pages, dtype, d, num_q_heads, device)
+            self.workspace = torch.empty(max(pa.padoc_qk_rotary_bwd_workspace_size(rotary, self.T), 256),
+                                         dtype=torch.uint8, device=device)
+
+    def run(self, q, k, v, scale, out, lse, stream=None):
+        """q / k: [T][heads][d] as the projections give them (rows may lie apart); v contiguous."""
+        pa.padoc_qk_rotary(self.rotary, q, k, self.pos, self.q, self.k, stream)
+        self.fwd.run(self.q, self.k, v, scale, out, lse, stream)
+
+    def run_bwd(self, q, k, v, out, dout, lse, scale, dq, dk, dv, dq_weight=None, dk_weight=None, stream=None):
+        """Gradients of the last run's q, k, v (dq, dk, dv contiguous) and, with norm weights, of these."""
+        self.bwd.run(self.q, self.k, v, out, dout, lse, scale, dq, dk, dv, stream)
+        pa.padoc_qk_rotary_bwd(self.rotary, dq, dk, self.pos, dq, dk, q, k, dq_weight, dk_weight, self.workspace, stream)
+
+
 class ChunkPrefillPlan:
     """Plan (C1) of a chunked prefill over the paged cache, uploaded: chunks of consecutive query
     tokens per stream (padoc_prefill_chunk rows), run by the decode kernels with the chunks' tokens
@@ -117,11 +152,15 @@ class MaskedParallelLoop:
     step's decode plan from the stream list, and sends slots, source rows, block tables and plan to
     the device in one copy from pinned memory (two staging buffers, so the host fills one while
     the previous step's copy may still read the other). The device then appends every input's K/V
-    into the pool, lays out the queries and decodes every stream, all on one CUDA stream."""
+    into the pool, lays out the queries and decodes every stream, all on one CUDA stream. With rotary
+    (pa.Rotary) the inputs are appended normed and rotated, at positions given by source row.
+
+    Between steps a branch can be forked with its history (fork_stream), streams and pages dropped, and the
+    pool compacted or replaced by one of another size (compact, resize)."""
 
     def __init__(self, num_blocks: int, num_q_heads: int, num_kv_heads: int, head_dim: int, dtype: torch.dtype,
                  device, block_order=None, block_size: int = 16, tc_ctas: int = 0, warp_ctas: int = 0,
-                 split_tokens: int = 0):
+                 split_tokens: int = 0, rotary=None):
         self.mpd = pa.Mpd(num_blocks, block_size, block_order)
         self.k_pool = torch.zeros((num_blocks, num_kv_heads, block_size, head_dim), dtype=dtype, device=device)
         self.v_pool = torch.zeros_like(self.k_pool)
@@ -129,6 +168,8 @@ class MaskedParallelLoop:
         self.cfg = pa.make_decode_config(num_q_heads, num_kv_heads, head_dim, block_size, False, split_tokens,
                                          tc_ctas, warp_ctas)
         self.device, self.dtype = device, dtype
+        self.rotary = rotary
+        self._rotary_pos = None
         self.num_q_heads, self.head_dim = num_q_heads, head_dim
         self._stage = [None, None]
         self._stage_free = [torch.cuda.Event(), torch.cuda.Event()]
@@ -166,20 +207,26 @@ class MaskedParallelLoop:
         self.h2d_bytes = 4 * n
         return [self._ints[o:o + a.size] for a, o in zip(parts, offs)]
 
-    def add_page(self, prefix_len: int, num_forks: int, layout_eos: bool, k_src, v_src, src_rows, stream=None):
+    def add_page(self, prefix_len: int, num_forks: int, layout_eos: bool, k_src, v_src, src_rows, stream=None,
+                 pos_src=None):
         """Admits a page: its prefix K/V (rows src_rows of k_src / v_src, device tensors [rows][Hkv][d])
-        go into the blocks the scheduler gives it. Returns (page id, new stream ids)."""
+        go into the blocks the scheduler gives it. pos_src: int32 [rows][axes], with rotary. Returns (page
+        id, new stream ids)."""
         stream = stream or torch.cuda.current_stream()
         pid, slots, new = self.mpd.add_page(prefix_len, num_forks, layout_eos)
         if prefix_len > 0:
             slots_d, rows_d = self._upload([slots, np.asarray(src_rows, np.int32)], stream)
-            pa.padoc_append_inputs(self.k_pool, self.v_pool, k_src, v_src, slots_d, src_rows=rows_d, count=prefix_len,
-                                   stream=stream)
+            if self.rotary is not None:
+                pa.padoc_append_rotary_inputs(self.rotary, self.k_pool, self.v_pool, k_src, v_src, pos_src, slots_d,
+                                              src_rows=rows_d, count=prefix_len, stream=stream)
+            else:
+                pa.padoc_append_inputs(self.k_pool, self.v_pool, k_src, v_src, slots_d, src_rows=rows_d, count=prefix_len,
+                                       stream=stream)
         return pid, new
 
-    def step(self, k_src, v_src, q_src, rows_of, scale: float, out=None, lse=None, stream=None):
+    def step(self, k_src, v_src, q_src, rows_of, scale: float, out=None, lse=None, stream=None, pos_src=None):
         """One iteration: every live stream appends its next input (rows_of(stream ids) gives the rows
-        of k_src / v_src / q_src that hold them) and is decoded. Returns (stream ids, out [C][Hq][d],
+        of k_src / v_src / q_src, and with rotary of pos_src, that hold them) and is decoded. Returns (stream ids, out [C][Hq][d],
         lse fp32 [C][Hq]); the caller ends the step with end_step. The host work is two library calls:
         padoc_mpd_prepare_step into a pinned staging buffer, and padoc_mpd_launch_step, which copies it
         to the device and launches the append and the decode."""
@@ -225,18 +272,25 @@ class MaskedParallelLoop:
         if lse is None:
             lse = torch.empty((C, self.num_q_heads), dtype=torch.float32, device=self.device)
         # one library call: the stage's copy to the device, the append and the decode
-        pa.padoc_mpd_launch_step(st, self._stage[b], self._ints, self._pool, k_src, v_src, q_src, self.q_step, scale,
-                                 out, lse, self.workspace, stream)
+        if self.rotary is not None:
+            pa.padoc_mpd_launch_step_rotary(st, self._stage[b], self._ints, self._pool, self.rotary, k_src, v_src, q_src,
+                                            pos_src, self.q_step, scale, out, lse, self.workspace, stream)
+        else:
+            pa.padoc_mpd_launch_step(st, self._stage[b], self._ints, self._pool, k_src, v_src, q_src, self.q_step, scale,
+                                     out, lse, self.workspace, stream)
         self._stage_free[b].record(stream)
         return ids, out, lse
 
-    def run_step(self, k_src, v_src, q_src, row_of_stream, scale: float, out, lse, stream=None):
+    def run_step(self, k_src, v_src, q_src, row_of_stream, scale: float, out, lse, stream=None, pos_src=None):
         """step() as one library call (padoc_mpd_runner_step): row_of_stream is an int32 numpy table
         of each live stream's source row indexed by stream id; out [rows][Hq][d] and lse [rows][Hq]
         (rows at least the live streams) receive the outputs in step order. Returns (C, stream ids
         int32 [C], valid until the next step); end the step with end_step."""
         if self._runner is None:
             self._runner = pa.MpdRunner(self.mpd, self.cfg, self._pool)
+        if self.rotary is not None and self._rotary_pos is not pos_src:
+            self._runner.set_rotary(self.rotary, pos_src)
+            self._rotary_pos = pos_src
         n, ids = self._runner.step(k_src, v_src, q_src, row_of_stream, scale, out, lse, stream)
         self.h2d_bytes = self._runner.upload_bytes
         return n, ids
@@ -248,6 +302,56 @@ class MaskedParallelLoop:
     def end_step(self, num_forks=None, eos=None, num_streams=None):
         """Each stream's output event (forks, EOS) in step order; returns the new branches' ids."""
         return self.mpd.end_step(num_forks, eos, num_streams)
+
+    def _copy_blocks(self, src, dst, stream, pool=None):
+        """Blocks src to dst of the pool (or of ``pool``, (k_pool, v_pool))."""
+        if len(src):
+            stream = stream or torch.cuda.current_stream()
+            src_d, dst_d = self._upload([np.asarray(src, np.int32), np.asarray(dst, np.int32)], stream)
+            own = pa.KvPools([(self.k_pool, self.v_pool)])
+            pa.padoc_copy_kv_blocks(own if pool is None else pa.KvPools([pool]), src_d, dst_d, own, len(src), stream)
+
+    def fork_stream(self, stream_id: int, num_copies: int = 1, stream=None):
+        """Forks a live branch into num_copies more with the same history, between steps: they share its
+        complete blocks and get copies of the partly filled one. Returns the new stream ids."""
+        new, src, dst = self.mpd.fork_stream(stream_id, num_copies)
+        self._copy_blocks(src, dst, stream)
+        return new
+
+    def drop_stream(self, stream_id: int):
+        """Retires a live stream between steps."""
+        self.mpd.drop_stream(stream_id)
+
+    def drop_page(self, page_id: int):
+        """Retires every stream of a live page between steps."""
+        self.mpd.drop_page(page_id)
+
+    def compact(self, stream=None) -> int:
+        """Moves the live blocks to the pool's lowest ids, between steps. Returns their number."""
+        src, dst = self.mpd.compact()
+        self._copy_blocks(src, dst, stream)
+        return self.k_pool.shape[0] - self.status()[2]
+
+    def resize(self, num_blocks: int, stream=None):
+        """Replaces the pool by one of num_blocks blocks (at least the live ones), between steps."""
+        stream = stream or torch.cuda.current_stream()
+        if num_blocks < self.k_pool.shape[0] - self.status()[2]:
+            raise pa.PadocError("padoc_mpd_resize", 6)
+        live = self.compact(stream)
+        shape = (num_blocks,) + tuple(self.k_pool.shape[1:])
+        with torch.cuda.stream(stream):
+            k_pool = torch.zeros(shape, dtype=self.dtype, device=self.device)
+            v_pool = torch.zeros(shape, dtype=self.dtype, device=self.device)
+        ids = np.arange(live, dtype=np.int32)
+        self._copy_blocks(ids, ids, stream, (k_pool, v_pool))
+        self.mpd.resize(num_blocks)
+        if self._runner is not None:
+            self._runner.close()
+            self._runner = self._rotary_pos = None
+        for t in (self.k_pool, self.v_pool):
+            t.record_stream(stream)
+        self.k_pool, self.v_pool = k_pool, v_pool
+        self._pool = pa.make_kv_pool(self.k_pool, self.v_pool)
 
     def status(self):
         return self.mpd.status()

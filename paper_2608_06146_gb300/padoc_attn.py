@@ -99,6 +99,24 @@ class padoc_mpd_run_args(ctypes.Structure):
                 ("stream_ids", ctypes.c_void_p), ("stream", ctypes.c_void_p)]
 
 
+class padoc_rotary(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32),
+                ("adjacent", ctypes.c_int32), ("eps", ctypes.c_float), ("amplitude", ctypes.c_float)]
+
+
+class padoc_qkv_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("pos", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("dtype", ctypes.c_int)]
+
+
+class padoc_grid(ctypes.Structure):
+    _fields_ = [("page", ctypes.c_int32), ("begin", ctypes.c_int32), ("t", ctypes.c_int32), ("h", ctypes.c_int32),
+                ("w", ctypes.c_int32)]
+
+
 _lib = None
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _i64p = ctypes.POINTER(ctypes.c_int64)
@@ -190,6 +208,25 @@ def load_library(path: Optional[str] = None):
         "padoc_branch_decode_attn_e4m3": [ctypes.POINTER(padoc_kv_pool_e4m3), ctypes.POINTER(padoc_decode_plan), _vp,
                                           _vp, ctypes.c_int32, _vp, ctypes.c_int32, _vp, ctypes.c_float, _vp, _vp,
                                           _vp, ctypes.c_size_t, _vp],
+        "padoc_build_rotary_table": [_vp, _vp, ctypes.c_int32, ctypes.c_int32, _vp],
+        "padoc_build_rotary_positions": [P, ctypes.c_int32, _vp, ctypes.c_int32, _vp, ctypes.c_int64, _vp],
+        "padoc_qk_rotary": [_vp, _vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp],
+        "padoc_qk_rotary_bwd_workspace_size": [_vp, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)],
+        "padoc_qk_rotary_bwd": [_vp, _vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp,
+                                ctypes.c_int64, _vp, _vp, _vp, ctypes.c_size_t, _vp],
+        "padoc_append_rotary_inputs": [_vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_int32, _vp],
+        "padoc_append_rotary_inputs_e4m3": [_vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_int32, _vp],
+        "padoc_copy_kv_blocks": [_vp, _vp, ctypes.c_int32, _vp, _vp, ctypes.c_int32, _vp],
+        "padoc_copy_kv_blocks_e4m3": [_vp, _vp, ctypes.c_int32, _vp, _vp, ctypes.c_int32, _vp],
+        "padoc_mpd_fork_stream": [_vp, ctypes.c_int32, ctypes.c_int32, _i32p, _i32p, _i32p, _i32p],
+        "padoc_mpd_drop_stream": [_vp, ctypes.c_int32],
+        "padoc_mpd_drop_page": [_vp, ctypes.c_int32],
+        "padoc_mpd_compact": [_vp, _i32p, _i32p, ctypes.c_int32, _i32p],
+        "padoc_mpd_resize": [_vp, ctypes.c_int32],
+        "padoc_mpd_launch_step_rotary": [ctypes.POINTER(padoc_mpd_step), _vp, _vp, ctypes.c_int64,
+                                         ctypes.POINTER(padoc_kv_pool), _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp,
+                                         ctypes.c_size_t, _vp],
+        "padoc_mpd_runner_set_rotary": [_vp, _vp, _vp, ctypes.c_int64],
         "padoc_check_device_errors": [_vp],
         "padoc_last_device_error": [_i32p, _i32p],
         "padoc_status_string": [ctypes.c_int],
@@ -226,6 +263,11 @@ def exported_symbols() -> Sequence[str]:
                         "padoc_selftest_tcgen05", "padoc_selftest_wait_timeout",
                         "padoc_quantize_kv_blocks", "padoc_append_inputs_e4m3", "padoc_branch_decode_attn_e4m3",
                         "padoc_advance_decode_plan", "padoc_launch_decode_step",
+                        "padoc_build_rotary_table", "padoc_build_rotary_positions", "padoc_qk_rotary",
+                        "padoc_qk_rotary_bwd_workspace_size", "padoc_qk_rotary_bwd", "padoc_append_rotary_inputs",
+                        "padoc_append_rotary_inputs_e4m3", "padoc_copy_kv_blocks", "padoc_copy_kv_blocks_e4m3",
+                        "padoc_mpd_fork_stream", "padoc_mpd_drop_stream", "padoc_mpd_drop_page", "padoc_mpd_compact",
+                        "padoc_mpd_resize", "padoc_mpd_launch_step_rotary", "padoc_mpd_runner_set_rotary",
                         "padoc_check_device_errors",
                         "padoc_last_device_error", "padoc_status_string", "padoc_version")]
 
@@ -747,6 +789,40 @@ class Mpd:
         _check("padoc_mpd_end_step", st)
         return self._new[:self._k.value].copy()
 
+    def fork_stream(self, stream: int, num_copies: int = 1):
+        """Forks a live branch with its history: returns (new stream ids int32 [num_copies], source blocks,
+        destination blocks: the pairs to copy before the next step)."""
+        n = max(num_copies, 1)
+        new, src, dst, k = np.zeros(n, np.int32), np.zeros(n, np.int32), np.zeros(n, np.int32), ctypes.c_int32()
+        _check("padoc_mpd_fork_stream",
+               self._lib.padoc_mpd_fork_stream(self._h, int(stream), int(num_copies), new.ctypes.data_as(_i32p),
+                                               src.ctypes.data_as(_i32p), dst.ctypes.data_as(_i32p), ctypes.byref(k)))
+        return new[:num_copies], src[:k.value], dst[:k.value]
+
+    def drop_stream(self, stream: int):
+        """Retires a live stream between steps."""
+        _check("padoc_mpd_drop_stream", self._lib.padoc_mpd_drop_stream(self._h, int(stream)))
+
+    def drop_page(self, page: int):
+        """Retires every stream of a live page between steps."""
+        _check("padoc_mpd_drop_page", self._lib.padoc_mpd_drop_page(self._h, int(page)))
+
+    def compact(self):
+        """Moves the live blocks to the lowest ids: returns the (source, destination) blocks to copy before
+        the next step."""
+        k = ctypes.c_int32()
+        st = self._lib.padoc_mpd_compact(self._h, None, None, 0, ctypes.byref(k))
+        src, dst = np.zeros(max(k.value, 1), np.int32), np.zeros(max(k.value, 1), np.int32)
+        if st == 6:
+            st = self._lib.padoc_mpd_compact(self._h, src.ctypes.data_as(_i32p), dst.ctypes.data_as(_i32p), k.value,
+                                             ctypes.byref(k))
+        _check("padoc_mpd_compact", st)
+        return src[:k.value], dst[:k.value]
+
+    def resize(self, num_blocks: int):
+        """Changes the number of pool blocks; blocks given up must be free."""
+        _check("padoc_mpd_resize", self._lib.padoc_mpd_resize(self._h, int(num_blocks)))
+
     def prepare_step(self, cfg: padoc_decode_config, stage: np.ndarray) -> padoc_mpd_step:
         """padoc_mpd_prepare_step into ``stage`` (int32 numpy array, e.g. a view of pinned memory).
         Raises PadocError (status 6) when the stage is too small; step.total_words is then set on
@@ -780,6 +856,20 @@ def padoc_mpd_launch_step(step: padoc_mpd_step, stage, dev_ints, pool: padoc_kv_
                                    _dev(lse, "lse"), _dev(workspace, "workspace"),
                                    workspace.numel() * workspace.element_size(), _stream_ptr(stream))
     _check("padoc_mpd_launch_step", st)
+
+
+def padoc_mpd_launch_step_rotary(step: padoc_mpd_step, stage, dev_ints, pool: padoc_kv_pool, rotary: "Rotary", k_src,
+                                 v_src, q_src, pos, q_dst, scale, out, lse, workspace, stream=None):
+    """padoc_mpd_launch_step with padoc_append_rotary_inputs as its append: k_src / v_src / q_src as there
+    (row strides allowed), pos int32 [rows][axes]."""
+    lib = load_library()
+    rows = rotary.rows(pos, k_src, q_src, v_src)
+    st = lib.padoc_mpd_launch_step_rotary(ctypes.byref(step), None if stage is None else stage.data_ptr(),
+                                          _dev(dev_ints, "dev_ints"), dev_ints.numel(), ctypes.byref(pool), rotary.ref,
+                                          ctypes.byref(rows), _dev(q_dst, "q_dst"), float(scale), _dev(out, "out"),
+                                          _dev(lse, "lse"), _dev(workspace, "workspace"),
+                                          workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    _check("padoc_mpd_launch_step_rotary", st)
 
 
 class MpdRunner:
@@ -840,6 +930,20 @@ class MpdRunner:
                                                                         self._up_ref))
         n = self._n.value
         return n, self._ids[:n]
+
+    def set_rotary(self, rotary: Optional["Rotary"], pos=None):
+        """The steps from now on append with the norm and the rotation of ``rotary`` at pos (int32 CUDA tensor
+        [source rows][axes]); None: as they are."""
+        if rotary is None:
+            _check("padoc_mpd_runner_set_rotary", self._lib.padoc_mpd_runner_set_rotary(self._h, None, None, 0))
+            self._rotary = None
+            return
+        if self._elt is not rotary.dtype and rotary.dtype is not None:
+            raise TypeError("the norm weights must have the pool's dtype")
+        p = rotary.positions(pos)
+        _check("padoc_mpd_runner_set_rotary",
+               self._lib.padoc_mpd_runner_set_rotary(self._h, rotary.ref, p, pos.shape[0]))
+        self._rotary = (rotary, pos)   # kept alive
 
     @property
     def upload_bytes(self) -> int:
@@ -922,6 +1026,21 @@ class E4M3Pool:
                                     _dev(self.k_scales, "k_scales"), _dev(self.v_scales, "v_scales"), num_blocks,
                                     block_size, num_kv_heads, head_dim)
 
+    @classmethod
+    def over(cls, k_codes, v_codes, k_scales, v_scales):
+        """The pool over codes and scales that the caller holds already."""
+        import torch
+        nb, hkv, bs, d = k_codes.shape
+        for t, shape, dt in ((k_codes, (nb, hkv, bs, d), torch.uint8), (v_codes, (nb, hkv, bs, d), torch.uint8),
+                             (k_scales, (nb, hkv), torch.float32), (v_scales, (nb, hkv), torch.float32)):
+            if tuple(t.shape) != shape or t.dtype != dt:
+                raise ValueError("codes uint8 [num_blocks][Hkv][16][d], scales float32 [num_blocks][Hkv]")
+        p = cls.__new__(cls)
+        p.k_codes, p.v_codes, p.k_scales, p.v_scales = k_codes, v_codes, k_scales, v_scales
+        p.c = padoc_kv_pool_e4m3(_dev(k_codes, "k_codes"), _dev(v_codes, "v_codes"), _dev(k_scales, "k_scales"),
+                                 _dev(v_scales, "v_scales"), nb, bs, hkv, d)
+        return p
+
     @property
     def num_blocks(self) -> int:
         return self.c.num_blocks
@@ -973,6 +1092,236 @@ def padoc_append_inputs(k_pool, v_pool, k_src, v_src, slots, q_src=None, q_dst=N
                                  k_src.shape[0], hq, _dev(q_dst, "q_dst"), _dev(src_rows, "src_rows"),
                                  _dev(slots, "slots"), n, _stream_ptr(stream))
     _check("padoc_append_inputs", st)
+
+
+# ------------------------------------------------------------------------------------------------
+# Rotary positions and head norms
+# ------------------------------------------------------------------------------------------------
+
+def padoc_build_rotary_table(inv_freq, axis_of=None, num_axes: int = 1) -> np.ndarray:
+    """The uint64 table [pairs] of a rotary spec: inv_freq (float64) and each pair's axis."""
+    lib = load_library()
+    f = np.ascontiguousarray(inv_freq, np.float64).reshape(-1)
+    a = None if axis_of is None else np.ascontiguousarray(axis_of, np.int32).reshape(-1)
+    if a is not None and a.size != f.size:
+        raise ValueError("axis_of must name an axis for each frequency")
+    table = np.zeros(max(f.size, 1), np.uint64)
+    _check("padoc_build_rotary_table",
+           lib.padoc_build_rotary_table(f.ctypes.data, None if a is None else a.ctypes.data, f.size, num_axes,
+                                        table.ctypes.data))
+    return table[:f.size]
+
+
+def padoc_build_rotary_positions(pages, grids=()):
+    """Positions on (time, height, width) of the packed tokens: (pos int32 [T][3], the position behind each
+    page's prefix int32 [pages]). grids: (page, begin, t, h, w) of the image or video patches among the
+    prefix tokens, by page and begin."""
+    lib, P = load_library(), _as_pages(pages)
+    g = np.ascontiguousarray(np.asarray(grids, np.int32).reshape(-1, 5))
+    T = padoc_packed_size(pages)
+    pos = np.zeros((max(T, 1), 3), np.int32)
+    end = np.zeros(max(P.n, 1), np.int32)
+    _check("padoc_build_rotary_positions",
+           lib.padoc_build_rotary_positions(P.arr, P.n, g.ctypes.data, g.shape[0], pos.ctypes.data, T, end.ctypes.data))
+    return pos[:T], end[:P.n]
+
+
+class Rotary:
+    """A padoc_rotary with its device table and weights (owned or kept alive here): inv_freq [pairs] and
+    axis_of [pairs] as in padoc_build_rotary_table; pairs (i, i + pairs), or (2 i, 2 i + 1) with adjacent; q_weight and
+    k_weight (CUDA tensors [head_dim] in the rows' dtype) give the heads an RMS norm before the rotation."""
+
+    def __init__(self, inv_freq, axis_of=None, num_axes: int = 1, head_dim: int = 128, adjacent: bool = False,
+                 q_weight=None, k_weight=None, eps: float = 1e-6, amplitude: float = 1.0, device="cuda"):
+        import torch
+        table = padoc_build_rotary_table(inv_freq, axis_of, num_axes)
+        self.table = torch.from_numpy(table.view(np.int64).copy()).to(device)
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.dtype = None
+        self._codes = {torch.bfloat16: PADOC_DTYPE_BF16, torch.float32: PADOC_DTYPE_F32}
+        self._int32 = torch.int32
+        for w in (q_weight, k_weight):
+            if w is None:
+                continue
+            _dtype_code(w)
+            if tuple(w.shape) != (head_dim,) or (self.dtype is not None and w.dtype is not self.dtype):
+                raise ValueError("q_weight and k_weight must be [head_dim] of one dtype")
+            self.dtype = w.dtype
+        self.head_dim, self.num_axes = head_dim, num_axes
+        self.c = padoc_rotary(_dev(self.table, "table"), _dev(q_weight, "q_weight"), _dev(k_weight, "k_weight"),
+                              head_dim, 2 * table.size, num_axes, int(bool(adjacent)), eps, amplitude)
+        self.ref = ctypes.byref(self.c)
+
+    def positions(self, pos):
+        if pos.dtype is not self._int32 or pos.dim() != 2 or pos.shape[1] != self.num_axes:
+            raise ValueError("pos must be int32 [rows][axes]")
+        return _dev(pos, "pos")
+
+    def heads(self, t, name, rows=None, dtype=None):
+        """(address, row stride, heads) of a CUDA tensor [rows][heads][head_dim] whose rows may lie apart."""
+        sh, st = t.shape, t.stride()
+        if not t.is_cuda or len(sh) != 3 or sh[2] != self.head_dim or st[2] != 1 or (st[1] != sh[2] and sh[1] > 1):
+            raise ValueError(f"{name} must be a CUDA tensor [rows][heads][head_dim] with contiguous rows")
+        if (rows is not None and sh[0] != rows) or (dtype is not None and t.dtype is not dtype):
+            raise ValueError(f"{name} must have the other tensors' rows and dtype")
+        width = sh[1] * sh[2]
+        return t.data_ptr(), (st[0] if sh[0] > 1 else width), sh[1]
+
+    def rows(self, pos, k, q=None, v=None) -> padoc_qkv_rows:
+        """padoc_qkv_rows over q / k / v [rows][heads][head_dim] and pos int32 [rows][axes]."""
+        n, dt = k.shape[0], k.dtype
+        code = self._codes.get(dt)
+        if code is None or (self.dtype is not None and dt is not self.dtype):
+            raise TypeError("rows must be bfloat16 or float32, of the norm weights' dtype")
+        if pos.shape[0] != n:
+            raise ValueError("pos must have a position for each row")
+        kp, ks, hkv = self.heads(k, "k", n, dt)
+        qp, qs, hq = self.heads(q, "q", n, dt) if q is not None else (None, 0, 0)
+        vp, vs, hv = self.heads(v, "v", n, dt) if v is not None else (None, 0, hkv)
+        if hv != hkv:
+            raise ValueError("v must have k's heads")
+        return padoc_qkv_rows(qp, kp, vp, qs, ks, vs, self.positions(pos), n, hq, hkv, code)
+
+
+def padoc_qk_rotary(rotary: Rotary, q, k, pos, q_out, k_out, stream=None):
+    """Norm and rotation of packed rows: q [rows][Hq][d], k [rows][Hkv][d] (rows may lie apart, as slices of a
+    fused projection do), pos int32 [rows][axes] into q_out, k_out (the inputs themselves are allowed)."""
+    lib = load_library()
+    rows = rotary.rows(pos, k, q)
+    qp, qs, hq = rotary.heads(q_out, "q_out", rows.rows, k.dtype)
+    kp, ks, hkv = rotary.heads(k_out, "k_out", rows.rows, k.dtype)
+    if hq != rows.num_q_heads or hkv != rows.num_kv_heads:
+        raise ValueError("q_out and k_out must have q's and k's heads")
+    _check("padoc_qk_rotary", lib.padoc_qk_rotary(rotary.ref, ctypes.byref(rows), qp, qs, kp, ks, _stream_ptr(stream)))
+
+
+def padoc_qk_rotary_bwd_workspace_size(rotary: Rotary, rows: int) -> int:
+    lib = load_library()
+    n = ctypes.c_size_t()
+    _check("padoc_qk_rotary_bwd_workspace_size",
+           lib.padoc_qk_rotary_bwd_workspace_size(rotary.ref, rows, ctypes.byref(n)))
+    return n.value
+
+
+def padoc_qk_rotary_bwd(rotary: Rotary, dq_out, dk_out, pos, dq, dk, q=None, k=None, dq_weight=None, dk_weight=None,
+                        workspace=None, stream=None):
+    """Gradients of padoc_qk_rotary: dq_out / dk_out into dq / dk (which may be the same tensors); with norm
+    weights the forward's q and k, dq_weight and dk_weight (float32 [d], written) and a workspace (uint8 CUDA
+    tensor of padoc_qk_rotary_bwd_workspace_size bytes) are needed."""
+    lib = load_library()
+    norm = rotary.q_weight is not None
+    up = rotary.rows(pos, dk_out, dq_out)
+    rows = up
+    if norm:
+        if q is None or k is None or dq_weight is None or dk_weight is None:
+            raise ValueError("the norm's backward needs q, k, dq_weight and dk_weight")
+        rows = rotary.rows(pos, k, q)
+        if rows.num_q_heads != up.num_q_heads or rows.num_kv_heads != up.num_kv_heads or rows.dtype != up.dtype:
+            raise ValueError("dq_out and dk_out must be like q and k")
+        for w in (dq_weight, dk_weight):
+            if tuple(w.shape) != (rotary.head_dim,) or w.element_size() != 4 or not w.is_floating_point():
+                raise ValueError("dq_weight and dk_weight must be float32 [head_dim]")
+    qp, qs, hq = rotary.heads(dq, "dq", up.rows, dk_out.dtype)
+    kp, ks, hkv = rotary.heads(dk, "dk", up.rows, dk_out.dtype)
+    if hq != up.num_q_heads or hkv != up.num_kv_heads:
+        raise ValueError("dq and dk must have the gradients' heads")
+    ws, wsb = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel() * workspace.element_size())
+    st = lib.padoc_qk_rotary_bwd(rotary.ref, ctypes.byref(rows), up.q, up.q_stride, up.k, up.k_stride, qp, qs, kp, ks,
+                                 _dev(dq_weight, "dq_weight"), _dev(dk_weight, "dk_weight"), ws, wsb, _stream_ptr(stream))
+    _check("padoc_qk_rotary_bwd", st)
+
+
+def _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count):
+    rows = rotary.rows(pos, k_src, q_src, v_src)
+    n = slots.shape[0] if count is None else count
+    for t, nm in ((slots, "slots"), (src_rows, "src_rows")):
+        if t is not None and (t.dtype is not rotary._int32 or t.numel() < n):
+            raise ValueError(f"{nm} must be int32 [count]")
+    if src_rows is None and n > rows.rows:
+        raise ValueError("more slots than rows")
+    dst = None
+    if q_src is not None:
+        if q_dst is None or q_dst.dtype is not k_src.dtype or tuple(q_dst.shape[1:]) != tuple(q_src.shape[1:]) or \
+                q_dst.shape[0] < n:
+            raise ValueError("q_dst must be [count][Hq][d] in the rows' dtype")
+        dst = _dev(q_dst, "q_dst")
+    return rows, dst, _dev(src_rows, "src_rows"), _dev(slots, "slots"), n
+
+
+def padoc_append_rotary_inputs(rotary: Rotary, k_pool, v_pool, k_src, v_src, pos, slots, q_src=None, q_dst=None,
+                               src_rows=None, count=None, stream=None):
+    """padoc_append_inputs with the norm and the rotation on the way (sources' rows may lie apart; pos int32
+    [rows][axes] by source row)."""
+    lib = load_library()
+    pool = make_kv_pool(k_pool, v_pool)
+    rows, dst, sr, sl, n = _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count)
+    _check("padoc_append_rotary_inputs",
+           lib.padoc_append_rotary_inputs(ctypes.byref(pool), rotary.ref, ctypes.byref(rows), dst, sr, sl, n,
+                                          _stream_ptr(stream)))
+
+
+def padoc_append_rotary_inputs_e4m3(rotary: Rotary, pool: E4M3Pool, k_src, v_src, pos, slots, q_src=None, q_dst=None,
+                                    src_rows=None, count=None, stream=None):
+    """padoc_append_rotary_inputs into an E4M3 pool (bf16 sources); inputs of one block must follow one
+    another into consecutive rows."""
+    lib = load_library()
+    rows, dst, sr, sl, n = _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count)
+    _check("padoc_append_rotary_inputs_e4m3",
+           lib.padoc_append_rotary_inputs_e4m3(ctypes.byref(pool.c), rotary.ref, ctypes.byref(rows), dst, sr, sl, n,
+                                               _stream_ptr(stream)))
+
+
+# ------------------------------------------------------------------------------------------------
+# Copies of cache blocks
+# ------------------------------------------------------------------------------------------------
+
+class KvPools:
+    """The layers' pools of a cache, marshalled once: (k_pool, v_pool) tensors [num_blocks][Hkv][16][d] each."""
+
+    def __init__(self, pools):
+        self.tensors = [tuple(p) for p in pools]
+        self.c = (padoc_kv_pool * max(len(self.tensors), 1))(*[make_kv_pool(k, v) for k, v in self.tensors])
+        for k, v in self.tensors:
+            if k.shape != v.shape or k.dtype != v.dtype:
+                raise ValueError("k_pool and v_pool must be alike")
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+class KvPoolsE4M3:
+    """The layers' E4M3 pools: E4M3Pool objects or (k_codes, v_codes, k_scales, v_scales) tensors."""
+
+    def __init__(self, pools):
+        self.pools = [p if isinstance(p, E4M3Pool) else E4M3Pool.over(*p) for p in pools]
+        self.c = (padoc_kv_pool_e4m3 * max(len(self.pools), 1))(*[p.c for p in self.pools])
+
+    def __len__(self):
+        return len(self.pools)
+
+
+def _copy_blocks(name, pools, src_blocks, dst_blocks, src_pools, count, stream):
+    src = pools if src_pools is None else src_pools
+    if len(src) != len(pools):
+        raise ValueError("as many source pools as destination pools")
+    n = src_blocks.shape[0] if count is None else count
+    for t in (src_blocks, dst_blocks):
+        if t.element_size() != 4 or t.is_floating_point() or t.numel() < n:
+            raise ValueError("src_blocks and dst_blocks must be int32 [count]")
+    _check(name, getattr(load_library(), name)(pools.c, src.c, len(pools), _dev(src_blocks, "src_blocks"),
+                                               _dev(dst_blocks, "dst_blocks"), n, _stream_ptr(stream)))
+
+
+def padoc_copy_kv_blocks(pools: KvPools, src_blocks, dst_blocks, src_pools: Optional[KvPools] = None, count=None,
+                         stream=None):
+    """Blocks src_blocks[i] to dst_blocks[i] (int32 CUDA tensors) in every pool, from src_pools where given."""
+    _copy_blocks("padoc_copy_kv_blocks", pools, src_blocks, dst_blocks, src_pools, count, stream)
+
+
+def padoc_copy_kv_blocks_e4m3(pools: KvPoolsE4M3, src_blocks, dst_blocks, src_pools: Optional[KvPoolsE4M3] = None,
+                              count=None, stream=None):
+    """padoc_copy_kv_blocks for E4M3 pools (codes and scales)."""
+    _copy_blocks("padoc_copy_kv_blocks_e4m3", pools, src_blocks, dst_blocks, src_pools, count, stream)
 
 
 # ------------------------------------------------------------------------------------------------

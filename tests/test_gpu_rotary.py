@@ -1,0 +1,691 @@
+"""GPU parity of the head norms and rotary positions: the packed forward and backward, the append into the
+paged pool and into the FP8 pool, against the 64-bit definition (oracle/rotary.py).
+
+Tolerances, derived. The angle's fraction of a turn is cut at 2^-32 and rounded to 24 bits: 2e-7 rad; its
+sine and cosine are off by at most 2^-20.9 from a fast evaluation: in all under 8e-7 on each of c, s. A
+rotated value u c - v s is so off by 1e-6 (|u| + |v|) with the two products' roundings. The norm's scale:
+a sum of 256 squares in at most 21 additions (1.3e-6, halved by the root), the root's 2 units of the last place
+and three roundings: 1.1e-6 relative, on both u and v. So FWD = 3e-6 x amplitude x (|u| + |v|), and one
+rounding to the stored type, eps / 2 of the value. Backward: g has 1e-6, h = x r 1.2e-6, the mean of w g h 1.3e-6 for
+its sum and those of its terms, and the product's three roundings: BWD = 6e-6 x the sum of the magnitudes the
+formula adds. The weights' gradient sums (rows x heads) products, each off by 2.2e-6 of its magnitude, in chains of
+at most 512 fp32 additions here: DW = 2.2e-6 + 512 x 2^-24 of the sum of the magnitudes.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import rotary as orot
+from paper_2608_06146_gb300 import build as pbuild
+from paper_2608_06146_gb300 import inputs
+from paper_2608_06146_gb300 import padoc_attn as pa
+from paper_2608_06146_gb300.engine import MaskedParallelLoop, RotaryPrefill
+from paper_2608_06146_gb300.inputs import LoopTokenSource, PageSpec, Workload
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BS = 16
+FWD, BWD, DW = 3e-6, 6e-6, 2.2e-6 + 512 * 2.0 ** -24
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _build():
+    pbuild.build()
+    pa.load_library()
+
+
+def up(a, dtype=None):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV, dtype)
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+class Spec:
+    """A rotary spec on both sides."""
+
+    def __init__(self, seed, d, rot, axes, adjacent, norm, dtype, amplitude=1.0, eps=1e-6, base=5e6):
+        g = np.random.default_rng(seed)
+        n = rot // 2
+        self.inv = base ** (-np.arange(n) / n)
+        self.axis = g.integers(0, axes, n)
+        self.adjacent, self.amplitude, self.eps, self.d, self.axes = adjacent, amplitude, eps, d, axes
+        self.qw = self.kw = None
+        if norm:
+            self.qw, self.kw = (up(1 + 0.3 * g.standard_normal(d)).to(dtype) for _ in range(2))
+        self.dev = pa.Rotary(self.inv, self.axis, axes, d, adjacent=adjacent, q_weight=self.qw, k_weight=self.kw, eps=eps,
+                             amplitude=amplitude, device=DEV)
+
+    def w64(self, w):
+        return None if w is None else f64(w)
+
+    def angle(self, pos):
+        return orot.angles(pos.cpu().numpy(), self.inv, self.axis)
+
+    def forward(self, x, w, pos):
+        return orot.forward(f64(x), self.w64(w), self.eps, self.angle(pos), self.adjacent, self.amplitude)
+
+    def backward(self, dz, x, w, pos):
+        return orot.backward(f64(dz), None if x is None else f64(x), self.w64(w), self.eps, self.angle(pos), self.adjacent,
+                             self.amplitude)
+
+
+def check(got, want, size, rel, name):
+    """|got - want| within the stored type's rounding and rel x size."""
+    got_, eps = f64(got), torch.finfo(got.dtype).eps / 2
+    tol = eps * np.abs(want) + (1 + eps) * rel * size + 1e-37
+    bad = ~(np.abs(got_ - want) <= tol)
+    assert not bad.any(), f"{name}: {bad.sum()} of {bad.size} off, worst {np.nanmax(np.abs(got_ - want) / tol):.2f} x the bound"
+
+
+def positions(rng, rows, axes, far=0):
+    return up((far + rng.integers(-50, 3000, (rows, axes))).astype(np.int32))
+
+
+def qkv(rng, rows, hq, hkv, d, dtype, scale=1.0):
+    x = up(scale * rng.standard_normal((rows, hq + 2 * hkv, d))).to(dtype)
+    return x, x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:]
+
+
+# (dtype, rows, hq, hkv, d, rot, axes, adjacent, norm, far)
+SHAPES = [
+    (BF16, 1, 16, 2, 128, 128, 3, False, True, 0),
+    (BF16, 77, 16, 2, 128, 128, 3, False, True, 10 ** 6),
+    (BF16, 500, 16, 2, 128, 128, 1, True, False, 0),
+    (BF16, 33, 7, 1, 128, 64, 2, False, True, 0),
+    (BF16, 19, 5, 3, 64, 64, 2, True, True, 0),
+    (BF16, 40, 6, 6, 80, 32, 3, False, True, 0),
+    (BF16, 21, 3, 1, 72, 72, 2, False, True, 0),
+    (BF16, 21, 3, 1, 72, 24, 2, True, True, 0),
+    (BF16, 9, 4, 1, 256, 256, 4, False, True, 0),
+    (BF16, 9, 4, 1, 256, 248, 4, False, False, 0),
+    (BF16, 5, 1, 1, 8, 8, 1, False, True, 0),
+    (BF16, 1000, 33, 1, 96, 96, 1, False, False, 0),
+    (F32, 1, 4, 1, 64, 64, 1, False, False, 0),
+    (F32, 368, 4, 1, 64, 64, 3, False, True, 10 ** 6),
+    (F32, 50, 16, 2, 128, 128, 3, True, True, 0),
+    (F32, 23, 2, 2, 256, 128, 2, False, True, 0),
+    (F32, 23, 3, 1, 40, 24, 2, True, False, 0),
+    (F32, 2500, 1, 1, 8, 8, 1, False, True, 0),
+]
+ids = lambda s: f"{'bf16' if s[0] is BF16 else 'f32'}-{s[1]}x{s[2]}+{s[3]}x{s[4]}-r{s[5]}-a{s[6]}{'-adj' if s[7] else ''}{'-norm' if s[8] else ''}"
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=ids)
+def test_forward_and_backward(shape):
+    dtype, rows, hq, hkv, d, rot, axes, adjacent, norm, far = shape
+    rng = np.random.default_rng(rows + d)
+    sp = Spec(rows, d, rot, axes, adjacent, norm, dtype, amplitude=1.0 if rows % 2 else 1.2)
+    pos = positions(rng, rows, axes, far)
+    _, q, k, _ = qkv(rng, rows, hq, hkv, d, dtype)
+    new = lambda h: torch.full((rows, h, d), float("nan"), dtype=dtype, device=DEV)
+    qo, ko = new(hq), new(hkv)
+    pa.padoc_qk_rotary(sp.dev, q, k, pos, qo, ko)
+    pa.padoc_check_device_errors()
+    for got, x, w, name in ((qo, q, sp.qw, "q"), (ko, k, sp.kw, "k")):
+        check(got, *sp.forward(x, w, pos), FWD, name)
+    # backward: the upstream gradients in a buffer of their own, the results in slices of one
+    _, dqo, dko, _ = qkv(rng, rows, hq, hkv, d, dtype)
+    dqkv = torch.full((rows, hq + 2 * hkv, d), 7.0, dtype=dtype, device=DEV)
+    dq, dk = dqkv[:, :hq], dqkv[:, hq:hq + hkv]
+    dqw, dkw = (torch.full((d,), float("nan"), device=DEV) for _ in range(2))
+    ws = torch.empty(max(pa.padoc_qk_rotary_bwd_workspace_size(sp.dev, rows), 256), dtype=torch.uint8, device=DEV)
+    args = (q, k, dqw, dkw, ws) if norm else ()
+    pa.padoc_qk_rotary_bwd(sp.dev, dqo, dko, pos, dq, dk, *args)
+    pa.padoc_check_device_errors()
+    for got, dz, x, w, gw, name in ((dq, dqo, q, sp.qw, dqw, "dq"), (dk, dko, k, sp.kw, dkw, "dk")):
+        dx, size, dw, terms = sp.backward(dz, x, w, pos)
+        check(got, dx, size, BWD if norm else FWD, name)
+        if norm:
+            check(gw, dw, terms, DW, name + "_weight")
+    assert bool((dqkv[:, hq + hkv:] == 7).all()), "the rows' other heads are left as they were"
+    # a second call gives the same bits, also in place
+    first = (dq.clone(), dk.clone(), dqw.clone(), dkw.clone())
+    dq2, dk2 = dqo.contiguous(), dko.contiguous()
+    pa.padoc_qk_rotary_bwd(sp.dev, dq2, dk2, pos, dq2, dk2, *args)
+    assert torch.equal(dq2, first[0]) and torch.equal(dk2, first[1])
+    if norm:
+        assert torch.equal(dqw, first[2]) and torch.equal(dkw, first[3])
+    q2, k2 = q.clone().contiguous(), k.clone().contiguous()
+    pa.padoc_qk_rotary(sp.dev, q2, k2, pos, q2, k2)
+    assert torch.equal(q2, qo) and torch.equal(k2, ko)
+    pa.padoc_check_device_errors()
+
+
+def test_gradients_against_differences_of_the_forward():
+    # fp32 forward: differences with step 2^-6 of values of size 1: truncation 2^-12 x a third derivative of
+    # the norm (a few units), rounding 2^-24 x sum of 512 terms / 2^-6: together below 1e-2 of the gradients' size
+    rng = np.random.default_rng(3)
+    sp = Spec(3, 64, 64, 2, False, True, F32)
+    rows, pos = 4, positions(rng, 4, 2)
+    _, q, k, _ = qkv(rng, rows, 2, 1, 64, F32)
+    _, gq, gk, _ = qkv(rng, rows, 2, 1, 64, F32)
+    q, k, gq, gk = (x.contiguous() for x in (q, k, gq, gk))
+
+    def loss(q, k):
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        pa.padoc_qk_rotary(sp.dev, q, k, pos, qo, ko)
+        return float((qo.double() * gq.double()).sum() + (ko.double() * gk.double()).sum())
+    dq, dk = torch.empty_like(q), torch.empty_like(k)
+    dqw, dkw = torch.empty(64, device=DEV), torch.empty(64, device=DEV)
+    ws = torch.empty(pa.padoc_qk_rotary_bwd_workspace_size(sp.dev, rows), dtype=torch.uint8, device=DEV)
+    pa.padoc_qk_rotary_bwd(sp.dev, gq, gk, pos, dq, dk, q, k, dqw, dkw, ws)
+    h = 2.0 ** -6
+    for t, g, other in ((q, dq, k), (k, dk, q)):
+        for at in [(0, 0, 0), (1, 0, 31), (2, 0, 32), (3, 0, 63)]:
+            e = torch.zeros_like(t)
+            e[at] = h
+            two = [(loss(t + s * e, other) if t is q else loss(other, t + s * e)) for s in (1, -1)]
+            assert abs((two[0] - two[1]) / (2 * h) - float(g[at])) < 1e-2
+    for w, g in ((sp.qw, dqw), (sp.kw, dkw)):
+        for j in (0, 17, 63):
+            two = []
+            for s in (1, -1):
+                w[j] += s * h
+                two.append(loss(q, k))
+                w[j] -= s * h
+            assert abs((two[0] - two[1]) / (2 * h) - float(g[j])) < 1e-2 * max(1, abs(float(g[j])))
+
+
+def test_no_rows():
+    sp = Spec(0, 128, 128, 3, False, True, BF16)
+    e = lambda h: torch.empty((0, h, 128), dtype=BF16, device=DEV)
+    pos = torch.empty((0, 3), dtype=torch.int32, device=DEV)
+    pa.padoc_qk_rotary(sp.dev, e(16), e(2), pos, e(16), e(2))
+    dqw, dkw = (torch.full((128,), float("nan"), device=DEV) for _ in range(2))
+    ws = torch.empty(256, dtype=torch.uint8, device=DEV)
+    pa.padoc_qk_rotary_bwd(sp.dev, e(16), e(2), pos, e(16), e(2), e(16), e(2), dqw, dkw, ws)
+    pa.padoc_check_device_errors()
+    assert bool((dqw == 0).all()) and bool((dkw == 0).all())
+
+
+def test_zero_and_infinite_heads():
+    # a head of zeros norms to zero (eps above 0), its gradient is w g / sqrt(eps); an infinity gives NaN in its own head only
+    sp = Spec(1, 128, 128, 1, False, True, BF16, eps=2.0 ** -12)
+    rows, pos = 4, torch.arange(4, dtype=torch.int32, device=DEV)[:, None].contiguous()
+    q = torch.randn((rows, 2, 128), device=DEV).to(BF16)
+    q[0, 0] = 0
+    q[1, 0, 5] = float("inf")
+    k = q[:, :1].contiguous()
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    pa.padoc_qk_rotary(sp.dev, q, k, pos, qo, ko)
+    assert bool((qo[0, 0] == 0).all())
+    assert bool(torch.isnan(qo[1, 0]).any()) and bool(torch.isfinite(qo[1, 1]).all())
+    assert bool(torch.isfinite(qo[2:]).all()) and bool(torch.isfinite(qo[0]).all())
+    g = torch.randn_like(q)
+    gk = g[:, :1].contiguous()
+    dq, dk = torch.empty_like(q), torch.empty_like(k)
+    dqw, dkw = torch.empty(128, device=DEV), torch.empty(128, device=DEV)
+    ws = torch.empty(pa.padoc_qk_rotary_bwd_workspace_size(sp.dev, rows), dtype=torch.uint8, device=DEV)
+    pa.padoc_qk_rotary_bwd(sp.dev, g, gk, pos, dq, dk, q, k, dqw, dkw, ws)
+    dx, size, _, _ = orot.backward(f64(g)[:1, :1], f64(q)[:1, :1], f64(sp.qw), sp.eps, sp.angle(pos)[:1])
+    check(dq[:1, :1], dx, size, BWD, "a zero head's gradient")
+    pa.padoc_check_device_errors()
+
+
+def test_positions_past_24_bits():
+    # the angle is reduced in integers: positions of 2^30 turn as exactly as their table's entries (fp64
+    # frequencies: 2 x 2^-53 x 0.16 x 2^30 turns = 2.4e-7 rad at frequency 1, and as much from the checker's own product)
+    sp = Spec(2, 64, 64, 2, False, False, F32)
+    rng = np.random.default_rng(5)
+    pos = up(rng.integers(-2 ** 31, 2 ** 31, (300, 2)).astype(np.int32))
+    _, q, k, _ = qkv(rng, 300, 2, 1, 64, F32)
+    qo, ko = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
+    pa.padoc_qk_rotary(sp.dev, q, k, pos, qo, ko)
+    want, size = sp.forward(q, None, pos)
+    check(qo, want, size, FWD + 1e-6, "q")
+
+
+def test_on_a_side_stream_and_in_a_graph():
+    sp = Spec(6, 128, 128, 3, False, True, BF16)
+    rng = np.random.default_rng(6)
+    rows, pos = 200, positions(rng, 200, 3)
+    x, q, k, _ = qkv(rng, rows, 16, 2, 128, BF16)
+    e = lambda h: torch.empty((rows, h, 128), dtype=BF16, device=DEV)
+    qo, ko, dq, dk = e(16), e(2), e(16), e(2)
+    dqw, dkw = torch.empty(128, device=DEV), torch.empty(128, device=DEV)
+    ws = torch.empty(pa.padoc_qk_rotary_bwd_workspace_size(sp.dev, rows), dtype=torch.uint8, device=DEV)
+
+    def both(stream=None):
+        pa.padoc_qk_rotary(sp.dev, q, k, pos, qo, ko, stream)
+        pa.padoc_qk_rotary_bwd(sp.dev, qo, ko, pos, dq, dk, q, k, dqw, dkw, ws, stream)
+    both()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (qo, ko, dq, dk, dqw, dkw)]
+    side = torch.cuda.Stream()
+    for t in (qo, ko, dq, dk, dqw, dkw):
+        t.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    both(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((qo, ko, dq, dk, dqw, dkw), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    x.copy_(torch.randn_like(x))
+    both()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (qo, ko, dq, dk, dqw, dkw)]
+    for t in (qo, ko, dq, dk, dqw, dkw):
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((qo, ko, dq, dk, dqw, dkw), want))
+
+
+# ------------------------------------------------------------------------------------------------
+# Append
+# ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("shape", [s for s in SHAPES if s[4] in (64, 80, 128)], ids=ids)
+def test_append_equals_rotation_then_append(shape):
+    dtype, rows, hq, hkv, d, rot, axes, adjacent, norm, far = shape
+    rng = np.random.default_rng(rows)
+    sp = Spec(rows, d, rot, axes, adjacent, norm, dtype)
+    pos = positions(rng, rows, axes, far)
+    _, q, k, v = qkv(rng, rows, hq, hkv, d, dtype)
+    nb = rows // BS + 9
+    src = rng.permutation(rows)[:max(1, rows - 3)].astype(np.int32)
+    slots = up(rng.permutation(nb * BS)[:len(src)].astype(np.int32))
+    pools = [torch.full((nb, hkv, BS, d), 3.0, dtype=dtype, device=DEV) for _ in range(4)]
+    qd, qr = (torch.full((len(src) + 2, hq, d), 5.0, dtype=dtype, device=DEV) for _ in range(2))
+    pa.padoc_append_rotary_inputs(sp.dev, pools[0], pools[1], k, v, pos, slots, q, qd, up(src))
+    qo, ko = torch.empty((rows, hq, d), dtype=dtype, device=DEV), torch.empty((rows, hkv, d), dtype=dtype, device=DEV)
+    pa.padoc_qk_rotary(sp.dev, q, k, pos, qo, ko)
+    pa.padoc_append_inputs(pools[2], pools[3], ko, v.contiguous(), slots, qo, qr, up(src))
+    pa.padoc_check_device_errors()
+    assert torch.equal(qd, qr) and torch.equal(pools[0], pools[2]) and torch.equal(pools[1], pools[3])
+    # without queries and without a row list
+    n = len(src)
+    for p in pools:
+        p.fill_(3.0)
+    pa.padoc_append_rotary_inputs(sp.dev, pools[0], pools[1], k, v, pos, slots, count=n)
+    pa.padoc_append_inputs(pools[2], pools[3], ko, v.contiguous(), slots, count=n)
+    pa.padoc_check_device_errors()
+    assert torch.equal(pools[0], pools[2]) and torch.equal(pools[1], pools[3])
+
+
+def test_append_past_32_bits():
+    # a pool whose byte offsets pass 2^32, and sources whose rows lie far apart
+    rng = np.random.default_rng(8)
+    sp = Spec(8, 128, 128, 1, False, True, BF16)
+    nb = (9 << 30) // (2 * BS * 128 * 2) // 2
+    k_pool, v_pool = (torch.zeros((nb, 2, BS, 128), dtype=BF16, device=DEV) for _ in range(2))
+    rows, stride = 5, 1 << 28
+    buf = torch.zeros(rows * stride, dtype=BF16, device=DEV)
+    view = lambda off, h: torch.as_strided(buf, (rows, h, 128), (stride, 128, 1), off)
+    q, k, v = view(0, 16), view(16 * 128, 2), view(18 * 128, 2)
+    for t in (q, k, v):
+        t.copy_(torch.randn(t.shape, device=DEV))
+    pos = positions(rng, rows, 1)
+    slots = up(np.array([nb * BS - 1, 0, nb * BS - 17, 5, (nb // 2) * BS + 3], np.int32))
+    qd = torch.empty((rows, 16, 128), dtype=BF16, device=DEV)
+    pa.padoc_append_rotary_inputs(sp.dev, k_pool, v_pool, k, v, pos, slots, q, qd)
+    pa.padoc_check_device_errors()
+    sl = slots.cpu().numpy()
+    check(qd, *sp.forward(q, sp.qw, pos), FWD, "q")
+    got_k = torch.stack([k_pool[int(s) // BS, :, int(s) % BS] for s in sl])
+    got_v = torch.stack([v_pool[int(s) // BS, :, int(s) % BS] for s in sl])
+    check(got_k, *sp.forward(k, sp.kw, pos), FWD, "k")
+    assert torch.equal(got_v, v)
+    assert int((k_pool != 0).any(-1).sum()) == rows * 2
+
+
+def _bad_slots_case(e4m3):
+    sp = Spec(9, 128, 128, 1, False, False, BF16)
+    rng = np.random.default_rng(9)
+    _, q, k, v = qkv(rng, 6, 16, 2, 128, BF16)
+    pos = positions(rng, 6, 1)
+    nb = 4
+    return sp, q, k, v, pos, nb
+
+
+@pytest.mark.parametrize("bad", ["slot_high", "slot_low", "row_high", "row_low"])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_append_bad_ids_are_reported_and_skipped(bad, e4m3):
+    sp, q, k, v, pos, nb = _bad_slots_case(e4m3)
+    slots, src = np.array([3, 20, 40], np.int32), np.array([1, 4, 0], np.int32)
+    (slots if bad.startswith("slot") else src)[1] = {"slot_high": nb * BS, "slot_low": -1, "row_high": 6, "row_low": -7}[bad]
+    qd = torch.full((3, 16, 128), 5.0, dtype=BF16, device=DEV)
+    if e4m3:
+        pool = pa.E4M3Pool(nb, 2, 128, DEV)
+        pool.k_scales.fill_(1e-9)   # (a former owner's scale)
+        pa.padoc_append_rotary_inputs_e4m3(sp.dev, pool, k, v, pos, up(slots), q, qd, up(src))
+        written = lambda b, r: bool((pool.k_codes[b, :, r] != 0).any())
+    else:
+        kp, vp = (torch.zeros((nb, 2, BS, 128), dtype=BF16, device=DEV) for _ in range(2))
+        pa.padoc_append_rotary_inputs(sp.dev, kp, vp, k, v, pos, up(slots), q, qd, up(src))
+        written = lambda b, r: bool((kp[b, :, r] != 0).any())
+    with pytest.raises(pa.PadocError) as e:
+        pa.padoc_check_device_errors()
+    assert e.value.device_code == 1 and e.value.device_detail == int((slots if bad.startswith("slot") else src)[1])
+    assert written(0, 3) and written(2, 8) and not written(1, 4)
+    assert bool((qd[1] == 5).all()) and bool((qd[0] != 5).any()) and bool((qd[2] != 5).any())
+    pa.padoc_check_device_errors()
+
+
+# ------------------------------------------------------------------------------------------------
+# Append into the FP8 pool
+# ------------------------------------------------------------------------------------------------
+
+def e4m3_model(codes, scales, slots, x):
+    """The append's rule for rows x [count][Hkv][d] in fp32: (codes, scales), exact for exact inputs."""
+    codes, scales = codes.copy(), scales.copy()
+    i = 0
+    while i < len(slots):
+        n = 1
+        while i + n < len(slots) and slots[i + n] == slots[i] + n and slots[i + n] % BS:
+            n += 1
+        b, r0 = slots[i] // BS, slots[i] % BS
+        for g in range(scales.shape[1]):
+            old = np.float32(0) if r0 == 0 else scales[b, g]
+            new = max(old, np.abs(x[i:i + n, g]).max() / np.float32(448))
+            if new > old > 0:
+                codes[b, g, :r0] = oracle.e4m3_encode(oracle.e4m3_decode(codes[b, g, :r0]).astype(np.float32) * old / new)
+            codes[b, g, r0:r0 + n] = oracle.e4m3_encode(x[i:i + n, g] / new) if new > 0 else 0
+            scales[b, g] = new
+        i += n
+    return codes, scales
+
+
+def stale_pool(rng, nb, hkv):
+    pool = pa.E4M3Pool(nb, hkv, 128, DEV)
+    for c in (pool.k_codes, pool.v_codes):
+        c.copy_(up(rng.integers(0, 0x7E, tuple(c.shape)).astype(np.uint8)))
+    for s in (pool.k_scales, pool.v_scales):
+        s.copy_(up(rng.uniform(0.001, 0.02, tuple(s.shape)).astype(np.float32)))
+    return pool
+
+
+def runs(rng, kind, nb):
+    """Slots of a call: one input a block, whole prefixes of odd length, chunks that start inside a block."""
+    blocks = rng.permutation(nb)
+    if kind == "step":
+        return np.array([b * BS + rng.integers(0, BS) for b in blocks[:nb - 2]], np.int32)
+    if kind == "prefix":
+        return np.array([blocks[t // BS] * BS + t % BS for t in range(BS * (nb - 2) - 5)], np.int32)
+    out, b = [], 0
+    while b < nb - 4:
+        first, n = int(rng.integers(0, BS)), int(rng.integers(1, 40))
+        out += [blocks[b + (first + j) // BS] * BS + (first + j) % BS for j in range(n)]
+        b += (first + n - 1) // BS + 1
+    return np.array(out, np.int32)
+
+
+@pytest.mark.parametrize("kind", ["step", "prefix", "chunks"])
+@pytest.mark.parametrize("hq,hkv,rot,axes,adjacent,norm", [(16, 2, 128, 3, False, True), (8, 1, 64, 1, False, False),
+                                                             (10, 5, 128, 2, True, True), (16, 2, 24, 3, True, False)])
+def test_append_e4m3(kind, hq, hkv, rot, axes, adjacent, norm):
+    rng = np.random.default_rng(hq + rot)
+    sp = Spec(rot, 128, rot, axes, adjacent, norm, BF16)
+    nb = 23
+    slots = runs(rng, kind, nb)
+    n = len(slots)
+    rows = n + 4
+    x, q, k, v = qkv(rng, rows, hq, hkv, 128, BF16, 3.0)
+    x[:3] = 0                                   # rows of zeros
+    pos = positions(rng, rows, axes)
+    src = rng.permutation(rows)[:n].astype(np.int32)
+    if kind == "step":
+        src[:2] = [0, 1]
+        slots[0] = slots[0] // BS * BS          # a block that starts with a row of zeros
+    pool = stale_pool(rng, nb, hkv)
+    before = [t.cpu().numpy() for t in (pool.k_codes, pool.k_scales, pool.v_codes, pool.v_scales)]
+    qd = torch.empty((n, hq, 128), dtype=BF16, device=DEV)
+    pa.padoc_append_rotary_inputs_e4m3(sp.dev, pool, k, v, pos, up(slots), q, qd, up(src))
+    pa.padoc_check_device_errors()
+    kc, ks, vc, vs = (t.cpu().numpy() for t in (pool.k_codes, pool.k_scales, pool.v_codes, pool.v_scales))
+    at = torch.from_numpy(src.astype(np.int64)).to(DEV)
+    check(qd, *sp.forward(q[at], sp.qw, pos[at]), FWD, "q")
+    # V is not rotated: the rule bit for bit
+    want_c, want_s = e4m3_model(before[2], before[3], slots, f64(v[at]).astype(np.float32))
+    np.testing.assert_array_equal(vs, want_s)
+    np.testing.assert_array_equal(vc, want_c)
+    # K: the scale within the values' bound; with the GPU's scale, earlier rows bit for bit, new rows' codes
+    # within half a step of the format (2^-4 of the value, 2^-10 of the scale where codes are subnormal)
+    want, size = sp.forward(k[at], sp.kw, pos[at])
+    touched = {}
+    for i, s in enumerate(slots.tolist()):
+        touched.setdefault(s // BS, []).append((s % BS, i))
+    for b in range(nb):
+        rows_in = [r for r, _ in touched.get(b, [])]
+        r0 = min(rows_in, default=BS)
+        for g in range(hkv):
+            if b in touched:
+                old = np.float32(0) if r0 == 0 else before[1][b, g]
+                z = np.abs(np.stack([want[i, g] for _, i in touched[b]]))
+                e = np.stack([size[i, g] for _, i in touched[b]]).max() * FWD
+                assert abs(ks[b, g] - max(old, z.max() / 448)) <= (e / 448) + ks[b, g] * 2.0 ** -23
+                if ks[b, g] == old or old == 0:
+                    keep = before[0][b, g, :r0]
+                else:
+                    keep = oracle.e4m3_encode(oracle.e4m3_decode(before[0][b, g, :r0]).astype(np.float32) * old / ks[b, g])
+                np.testing.assert_array_equal(kc[b, g, :r0], keep)
+                for r, i in touched[b]:
+                    got = oracle.e4m3_decode(kc[b, g, r]).astype(np.float64) * ks[b, g]
+                    tol = np.maximum(2.0 ** -4 * np.abs(want[i, g]), 2.0 ** -10 * ks[b, g]) * (1 + 1e-5) + 2 * FWD * size[i, g]
+                    assert (np.abs(got - want[i, g]) <= tol).all()
+            rest = [r for r in range(r0, BS) if r not in rows_in]
+            np.testing.assert_array_equal(kc[b, g, rest], before[0][b, g, rest])
+
+
+def test_append_e4m3_without_angles_equals_the_plain_append():
+    # all positions 0, no norm: K goes in as it is, so single rows give the plain append's bits
+    rng = np.random.default_rng(14)
+    sp = Spec(14, 128, 128, 3, False, False, BF16)
+    nb = 40
+    slots = runs(rng, "step", nb)
+    _, q, k, v = qkv(rng, len(slots), 16, 2, 128, BF16, 2.0)
+    pos = torch.zeros((len(slots), 3), dtype=torch.int32, device=DEV)
+    a = stale_pool(rng, nb, 2)
+    b = pa.E4M3Pool.over(*(t.clone() for t in (a.k_codes, a.v_codes, a.k_scales, a.v_scales)))
+    qa, qb = (torch.empty((len(slots), 16, 128), dtype=BF16, device=DEV) for _ in range(2))
+    pa.padoc_append_rotary_inputs_e4m3(sp.dev, a, k, v, pos, up(slots), q, qa)
+    pa.padoc_append_inputs_e4m3(b, k.contiguous(), v.contiguous(), up(slots), q.contiguous(), qb)
+    pa.padoc_check_device_errors()
+    for x, y in ((a.k_codes, b.k_codes), (a.v_codes, b.v_codes), (a.k_scales, b.k_scales), (a.v_scales, b.v_scales), (qa, qb)):
+        assert torch.equal(x, y)
+
+
+# ------------------------------------------------------------------------------------------------
+# Together: a training layer, and the decoding loop
+# ------------------------------------------------------------------------------------------------
+
+GRIDS = [(0, 3, 1, 6, 8), (1, 0, 2, 3, 4)]
+PAGES = [PageSpec(60, 12, [0, 5, 12, 5], [17, 3, 30, 1]), PageSpec(26, 6, [6, 2], [9, 20])]
+
+
+def test_training_layer_fp32_against_fp64():
+    # projections -> norm, rotation -> ancestor attention -> its backward -> the rotation's and norm's
+    # backward, against the chain in 64 bits. fp32 attention is held to 1e-4 forward, and backward to 1e-4 of the
+    # row's largest plus 1e-5 of the root mean square (the fp32 path's own bounds). Rotated rows that are off by 3e-6
+    # shift scores of up to 10 by 3e-5, which changes probabilities and gradients by as much relative to their
+    # size: twice the bounds before the last step; the norm's Jacobian adds two such errors per value: four times.
+    hq, hkv, d = 4, 1, 64
+    sp = Spec(21, d, d, 3, False, True, F32)
+    layer = RotaryPrefill(PAGES, sp.dev, hq, hkv, F32, DEV, GRIDS, training=True)
+    T = layer.T
+    rng = np.random.default_rng(21)
+    _, q, k, v = qkv(rng, T, hq, hkv, d, F32)
+    v = v.contiguous()
+    scale = 1 / math.sqrt(d)
+    out, lse = torch.empty((T, hq, d), device=DEV), torch.empty((T, hq), device=DEV)
+    layer.run(q, k, v, scale, out, lse)
+    dout = up(rng.standard_normal((T, hq, d)).astype(np.float32))
+    dq, dk, dv = (torch.empty((T, h, d), device=DEV) for h in (hq, hkv, hkv))
+    dqw, dkw = torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+    layer.run_bwd(q, k, v, out, dout, lse, scale, dq, dk, dv, dqw, dkw)
+    pa.padoc_check_device_errors()
+    pos = layer.pos
+    np.testing.assert_array_equal(pos.cpu().numpy(), pa.padoc_build_rotary_positions(PAGES, GRIDS)[0])
+    zq, zk = sp.forward(q, sp.qw, pos)[0], sp.forward(k, sp.kw, pos)[0]
+    tq, tk = (torch.from_numpy(z.astype(np.float32)) for z in (zq, zk))
+    ro, rl = oracle.prefill_dense(PAGES, tq, tk, v.cpu(), scale)
+    assert np.abs(f64(out) - ro).max() <= 2e-4 and np.abs(f64(lse) - rl).max() <= 2e-4
+    gq, gk, gv = oracle.prefill_bwd(PAGES, tq, tk, v.cpu(), dout.cpu(), scale)
+    want_q, want_k = orot.backward(gq, f64(q), f64(sp.qw), sp.eps, sp.angle(pos)), orot.backward(gk, f64(k), f64(sp.kw), sp.eps, sp.angle(pos))
+    for got, want in ((dq, want_q[0]), (dk, want_k[0]), (dv, gv)):
+        rms = math.sqrt((want ** 2).mean())
+        err = np.abs(f64(got) - want).reshape(T, -1).max(1)
+        assert (err <= 4e-4 * np.abs(want).reshape(T, -1).max(1) + 4e-5 * rms).all()
+    # the weights' gradients sum the rows': their bounds add up in the same way
+    for got, want in ((dqw, want_q), (dkw, want_k)):
+        assert (np.abs(f64(got) - want[2]) <= 4e-4 * want[3]).all()
+
+
+def test_training_layer_bf16_runs_on_its_own_rotated_rows():
+    hq, hkv, d = 16, 2, 128
+    sp = Spec(22, d, d, 3, False, True, BF16)
+    layer = RotaryPrefill(PAGES, sp.dev, hq, hkv, BF16, DEV, GRIDS, training=True)
+    T = layer.T
+    rng = np.random.default_rng(22)
+    _, q, k, v = qkv(rng, T, hq, hkv, d, BF16)
+    v = v.contiguous()
+    scale = 1 / math.sqrt(d)
+    out, lse = torch.empty((T, hq, d), dtype=BF16, device=DEV), torch.empty((T, hq), device=DEV)
+    layer.run(q, k, v, scale, out, lse)
+    pa.padoc_check_device_errors()
+    check(layer.q, *sp.forward(q, sp.qw, layer.pos), FWD, "q")
+    ro, rl = oracle.prefill_dense(PAGES, layer.q.cpu(), layer.k.cpu(), v.cpu(), scale)
+    assert np.abs(f64(out) - ro).max() <= 1.5e-2 and np.abs(f64(lse) - rl).max() <= 1e-3
+    dout = up(rng.standard_normal((T, hq, d))).to(BF16)
+    new = lambda h: torch.empty((T, h, d), dtype=BF16, device=DEV)
+    dq, dk, dv, zq, zk = new(hq), new(hkv), new(hkv), new(hq), new(hkv)
+    dqw, dkw = torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+    layer.run_bwd(q, k, v, out, dout, lse, scale, dq, dk, dv, dqw, dkw)
+    layer.bwd.run(layer.q, layer.k, v, out, dout, lse, scale, zq, zk, dv)
+    pa.padoc_check_device_errors()
+    for got, dz, x, w, gw, name in ((dq, zq, q, sp.qw, dqw, "dq"), (dk, zk, k, sp.kw, dkw, "dk")):
+        dx, size, dw, terms = sp.backward(dz, x, w, layer.pos)
+        check(got, dx, size, BWD, name)
+        check(gw, dw, terms, DW, name + "_weight")
+
+
+LOOP_PAGES = [PageSpec(60, 10, [0, 10, 3, 7], [17, 5, 33, 16]), PageSpec(130, 24, [24, 12, 8, 20, 4], [2, 40, 12, 30, 18])]
+
+
+def loop(rows_q, rows_k, rows_v, rotary, pos, mode, act=None, dtype=BF16, num_blocks=64, events=None):
+    """Runs Algorithm 1 over LOOP_PAGES; act(loop, step) after each step. Returns {packed row: (out, lse)}."""
+    src = LoopTokenSource(LOOP_PAGES)
+    hq, hkv, d = rows_q.shape[1], rows_k.shape[1], rows_k.shape[2]
+    lp = MaskedParallelLoop(num_blocks, hq, hkv, d, dtype, DEV, block_order=np.random.default_rng(1).permutation(num_blocks),
+                            rotary=rotary)
+    for p in range(len(LOOP_PAGES)):
+        P, nf, leos, prow = src.admission(p)
+        _, new = lp.add_page(P, nf, leos, rows_k, rows_v, prow, pos_src=pos)
+        src.admitted(p, new)
+    cap = sum(1 + pg.num_branches for pg in LOOP_PAGES)   # every stream id the loop can create
+    out = torch.empty((cap, hq, d), dtype=dtype, device=DEV)
+    lse = torch.empty((cap, hq), dtype=torch.float32, device=DEV)
+    row_of, got, step = np.zeros(cap, np.int32), {}, 0
+    while lp.status()[1]:
+        if mode == "runner":
+            row_of[:] = src.peek_rows(np.arange(cap))
+            n, ids = lp.run_step(rows_k, rows_v, rows_q, row_of, 1 / math.sqrt(d), out, lse, pos_src=pos)
+            ids = ids.copy()
+            src.rows(ids)
+            o, l = out[:n], lse[:n]
+        else:
+            ids, o, l = lp.step(rows_k, rows_v, rows_q, src.rows, 1 / math.sqrt(d), pos_src=pos)
+        for r, a, b in zip(src.token_rows(ids).tolist(), o.clone(), l.clone()):
+            got[r] = (a, b)
+        nf, eos = src.events(ids)
+        src.forked(ids, nf, lp.end_step(nf, eos))
+        step += 1
+        if act is not None:
+            act(lp, step)
+    pa.padoc_check_device_errors()
+    assert lp.status()[2] == lp.k_pool.shape[0]
+    return got
+
+
+@pytest.mark.parametrize("mode", ["step", "runner"])
+def test_loop_with_rotary_equals_the_loop_over_rotated_rows(mode):
+    # also with the pool compacted after every fifth step and replaced by larger and smaller ones
+    sp = Spec(23, 128, 128, 3, False, True, BF16)
+    T = sum(pg.packed_len for pg in LOOP_PAGES)
+    pos = up(pa.padoc_build_rotary_positions(LOOP_PAGES, [(0, 3, 1, 6, 8), (1, 10, 1, 10, 10)])[0])
+    _, q, k, v = qkv(np.random.default_rng(23), T, 16, 2, 128, BF16)
+    q, k, v = (t.contiguous() for t in (q, k, v))
+    qr, kr = torch.empty_like(q), torch.empty_like(k)
+    pa.padoc_qk_rotary(sp.dev, q, k, pos, qr, kr)
+    want = loop(qr, kr, v, None, None, mode)
+    got = loop(q, k, v, sp.dev, pos, mode)
+
+    def act(lp, step):
+        if step % 5 == 0:
+            live = lp.compact()
+            assert lp.status()[2] == lp.k_pool.shape[0] - live
+        if step % 9 == 0:
+            lp.resize({0: 64, 1: 41, 2: 77}[step // 9 % 3])
+    moved = loop(q, k, v, sp.dev, pos, mode, act)
+    assert set(want) == set(got) == set(moved)
+    for r in want:
+        for other in (got, moved):
+            assert torch.equal(want[r][0], other[r][0]) and torch.equal(want[r][1], other[r][1])
+
+
+@pytest.mark.parametrize("mode", ["step", "runner"])
+def test_forked_candidates_decode_like_their_origin_and_then_apart(mode):
+    # a branch with 21 rows is forked in three; every candidate goes on with its own inputs, and each equals
+    # a branch that had that history from the start (oracle over the packed page)
+    sp = Spec(24, 128, 128, 1, False, True, BF16)
+    n, more = 21, 14
+    first = PageSpec(50, 4, [2], [n])
+    rng = np.random.default_rng(24)
+    hist = 50 + 4 + n
+    rows = hist + 3 * more
+    _, q, k, v = qkv(rng, rows, 16, 2, 128, BF16)
+    q, k, v = (t.contiguous() for t in (q, k, v))
+    place = np.concatenate([np.arange(54), 52 + np.arange(n)] + [52 + n + np.arange(more)] * 3).astype(np.int32)
+    pos = up(place[:, None])
+    lp = MaskedParallelLoop(40, 16, 2, 128, BF16, DEV, rotary=sp.dev)
+    _, new = lp.add_page(50, 0, False, k, v, np.arange(50), pos_src=pos)
+    layout = int(new[0])
+    out, lse = torch.empty((8, 16, 128), dtype=BF16, device=DEV), torch.empty((8, 16), device=DEV)
+    row_of = np.zeros(16, np.int32)
+
+    def step(rows_by_id, forks=None, eos=()):
+        for s, r in rows_by_id.items():
+            row_of[s] = r
+        if mode == "runner":
+            c, ids = lp.run_step(k, v, q, row_of, 128 ** -0.5, out, lse, pos_src=pos)
+            ids, o = ids.copy(), out[:c].clone()
+        else:
+            ids, o, _ = lp.step(k, v, q, lambda i: row_of[i], 128 ** -0.5, pos_src=pos)
+        res = dict(zip(ids.tolist(), o))
+        made = lp.end_step(np.array([(forks or {}).get(int(i), 0) for i in ids], np.int32),
+                           np.array([int(i) in eos for i in ids], np.uint8))
+        return res, made.tolist()
+    step({layout: 50})
+    _, (a,) = step({layout: 51}, forks={layout: 1})
+    step({layout: 52, a: 54})
+    step({layout: 53, a: 55}, eos=(layout,))
+    for j in range(2, n):
+        step({a: 54 + j})
+    b, c = (int(x) for x in lp.fork_stream(a, 2))
+    assert lp.status()[1] == 3
+    got = {a: [], b: [], c: []}
+    for j in range(more):
+        if j == 6:
+            lp.compact()
+        res, _ = step({s: hist + i * more + j for i, s in enumerate((a, b, c))})
+        for s in got:
+            got[s].append(res[s])
+    lp.drop_stream(b)
+    assert lp.status()[1] == 2
+    lp.drop_page(0)
+    assert lp.status() == (0, 0, 40)
+    pa.padoc_check_device_errors()
+    qr, kr = torch.empty_like(q), torch.empty_like(k)
+    pa.padoc_qk_rotary(sp.dev, q, k, pos, qr, kr)
+    page = PageSpec(50, 4, [2], [n + more])
+    for i, s in enumerate((a, b, c)):
+        at = torch.cat([torch.arange(hist), hist + i * more + torch.arange(more)])
+        ro, _ = oracle.prefill_dense([page], qr.cpu()[at], kr.cpu()[at], v.cpu()[at], 128 ** -0.5)
+        assert np.abs(f64(torch.stack(got[s])) - ro[hist:]).max() <= 1.5e-2
