@@ -5,7 +5,8 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
+constexpr int kPiece = 8;    // 16-byte pieces a lane
 constexpr int kPools = 32;   // pools of one launch (their addresses travel as kernel arguments)
 
 struct CopyArgs {
@@ -15,36 +16,55 @@ struct CopyArgs {
     float *dst_scales[2 * kPools];
     const int32_t *src_blocks, *dst_blocks;
     int32_t src_num, dst_num, vecs, scales;   // 16-byte pieces and fp32 scales of a block
+    int32_t parts, count;                     // warps a block, pairs
     int *err;
 };
 
-// A CTA per (pair, pool's K or V array). Bound by HBM: a block is read once and written once.
+// A warp takes kPiece 16-byte pieces a lane of one array (a pool's K or V, blockIdx.y) of one pair; the loads of a
+// piece are all in flight together. Bound by HBM: a block is read once and written once. 6001 FP8 blocks (98.5 MB
+// both ways) took 20.8 us with a CTA per (pair, array), one load a thread.
 __global__ void __launch_bounds__(kThreads) copy_blocks_kernel(const __grid_constant__ CopyArgs p)
 {
     pdl_wait_prerequisite();
     pdl_launch_dependents();
-    const int32_t s = p.src_blocks[blockIdx.x], d = p.dst_blocks[blockIdx.x];
+    const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const int64_t pair = p.parts == 1 ? w : w / p.parts;
+    if (pair >= p.count) return;
+    const int part = (int)(w - pair * p.parts), lane = threadIdx.x & 31;
+    const int32_t s = p.src_blocks[pair], d = p.dst_blocks[pair];
     const bool s_ok = s >= 0 && s < p.src_num;
     if (!s_ok || d < 0 || d >= p.dst_num) {
-        if (threadIdx.x == 0) padoc_record_error(p.err, PADOC_DEVERR_BLOCK_ID, s_ok ? d : s);
+        if (lane == 0) padoc_record_error(p.err, PADOC_DEVERR_BLOCK_ID, s_ok ? d : s);
         return;
     }
-    const uint4 *src = p.src[blockIdx.y] + (int64_t)s * p.vecs;
-    uint4 *dst = p.dst[blockIdx.y] + (int64_t)d * p.vecs;
-    for (int i = threadIdx.x; i < p.vecs; i += kThreads) dst[i] = src[i];
-    for (int i = threadIdx.x; i < p.scales; i += kThreads)
-        p.dst_scales[blockIdx.y][(int64_t)d * p.scales + i] = p.src_scales[blockIdx.y][(int64_t)s * p.scales + i];
+    const int first = part * 32 * kPiece + lane;
+    const uint4 *src = p.src[blockIdx.y] + (int64_t)s * p.vecs + first;
+    uint4 *dst = p.dst[blockIdx.y] + (int64_t)d * p.vecs + first;
+    uint4 x[kPiece];
+#pragma unroll
+    for (int j = 0; j < kPiece; ++j)
+        if (first + 32 * j < p.vecs) x[j] = __ldcs(src + 32 * j);
+    if (part == 0)
+        for (int i = lane; i < p.scales; i += 32)
+            p.dst_scales[blockIdx.y][(int64_t)d * p.scales + i] = p.src_scales[blockIdx.y][(int64_t)s * p.scales + i];
+#pragma unroll
+    for (int j = 0; j < kPiece; ++j)
+        if (first + 32 * j < p.vecs) dst[32 * j] = x[j];
 }
 
 // Launches the copies of all pools, kPools at a time; fill(j, a, i) puts pool j's addresses at entry i.
 template <typename Fill>
 padoc_status copy_pools(CopyArgs &p, int32_t num_pools, int32_t count, padoc_stream_t stream, Fill fill)
 {
+    p.count = count;
+    p.parts = (p.vecs + 32 * kPiece - 1) / (32 * kPiece);
+    const int64_t ctas = ((int64_t)count * p.parts + kThreads / 32 - 1) / (kThreads / 32);
+    if (ctas > INT32_MAX) return PADOC_ERR_UNSUPPORTED;
     for (int32_t first = 0; first < num_pools; first += kPools) {
         const int32_t n = num_pools - first < kPools ? num_pools - first : kPools;
         for (int32_t i = 0; i < n; ++i) fill(first + i, p, i);
         cudaLaunchConfig_t lc = {};
-        lc.gridDim = dim3((unsigned)count, (unsigned)(2 * n));
+        lc.gridDim = dim3((unsigned)ctas, (unsigned)(2 * n));
         lc.blockDim = dim3(kThreads);
         lc.stream = (cudaStream_t)stream;
         cudaLaunchAttribute attr[1];

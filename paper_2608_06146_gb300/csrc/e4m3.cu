@@ -196,146 +196,207 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_e4m3_kernel(
     }
 }
 
+template <bool kFirst, typename A, typename B>
+struct Pick {
+    using type = A;
+};
+template <typename A, typename B>
+struct Pick<false, A, B> {
+    using type = B;
+};
+// The codes of a lane's vector under a scale (0 for a block of zeros).
+__device__ __forceinline__ uint2 encode(const float (&x)[8], const Scale &sc)
+{
+    if (!(sc.s > 0.f)) return make_uint2(0u, 0u);
+    return make_uint2(sc.codes(x[0], x[1]) | sc.codes(x[2], x[3]) << 16, sc.codes(x[4], x[5]) | sc.codes(x[6], x[7]) << 16);
+}
+__device__ __forceinline__ uint32_t encode(const float (&x)[4], const Scale &sc)
+{
+    return sc.s > 0.f ? sc.codes(x[0], x[1]) | sc.codes(x[2], x[3]) << 16 : 0u;
+}
+// Codes of an old scale under a larger one: code value x old scale, each step rounded to fp32.
+__device__ __forceinline__ uint32_t encode_again(uint32_t c, float s_old, const Scale &sc)
+{
+    float y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = __fmul_rn(e4m3_to_f32((uint8_t)(c >> (8 * j))), s_old);
+    return encode(y, sc);
+}
+__device__ __forceinline__ uint2 encode_again(uint2 c, float s_old, const Scale &sc)
+{
+    return make_uint2(encode_again(c.x, s_old, sc), encode_again(c.y, s_old, sc));
+}
+
 // The rotary form of the append (padoc_append_rotary_inputs_e4m3): K rows are normed and rotated in fp32 and
 // encoded from there. The inputs of a call that follow one another into consecutive rows of a block are one
-// run, which the CTA of its first input writes: the scale becomes max(old, amax over the run / 448) (the old
-// one taken as 0 when the run starts the block), rows before the run are encoded again when it grows, and the
-// run's codes are those of x / new scale. A warp takes a (K or V, head) at a time with the run's rows in
-// registers, a lane two pairs of rotated dims (or four dims) of each; every CTA also lays out its own
-// input's query heads. Rows past the run are left as they are.
+// run: the scale becomes max(old, amax over the run / 448) (the old one taken as 0 when the run starts the
+// block), rows before the run are encoded again when it grows, and the run's codes are those of x / new scale.
+// Rows past the run are left as they are.
+// A warp takes one (K or V, head) of `inputs` inputs, the runs that start among them; a row is spread over the
+// 8 (V = 8) or 16 lanes that share a head in the packed kernel, so a run's 16 rows are 4 (8) passes whose loads are
+// all in flight before the first is used, and stay in registers until the scale is known. Further CTAs lay out the
+// queries. Bound by latency in a step; a 4001-token prefix: 51 us with a row a warp at a time, its runs written by
+// one CTA in 16.
 struct RotaryAppendArgs {
-    padoc_rotary_dev::Spec sp;
-    const __nv_bfloat16 *q, *k, *v;
-    int64_t q_stride, k_stride, v_stride;
-    const int32_t *pos;
-    int64_t src_total;
-    __nv_bfloat16 *q_dst;
-    const int32_t *src_rows, *slots;
-    uint8_t *k_codes, *v_codes;
+    padoc_rotary_dev::Args rows;   // its k_out and v_out are the codes
     float *k_scales, *v_scales;
-    int64_t pool_slots;
-    int32_t hq, hkv, count;
-    int *err;
+    int32_t inputs, kv_ctas, q_parts;
 };
 
-template <bool kAdjacent, bool kNorm>
-__global__ void __launch_bounds__(32 * kAppendWarps) append_rotary_e4m3_kernel(const RotaryAppendArgs p)
+template <int V, bool kAdjacent, bool kNorm>
+__device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int i, int unit)
 {
     using namespace padoc_rotary_dev;
-    pdl_wait_prerequisite();
-    pdl_launch_dependents();
-    const int i = blockIdx.x;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t own = p.src_rows ? (int64_t)p.src_rows[i] : i;
-    const int64_t slot = p.slots[i];
-    const bool slot_ok = slot >= 0 && slot < p.pool_slots, row_ok = own >= 0 && own < p.src_total;
-    if (!slot_ok || !row_ok) {
-        if (threadIdx.x == 0) padoc_record_error(p.err, PADOC_DEVERR_BLOCK_ID, slot_ok ? (int)own : (int)slot);
-        if (!slot_ok) return;
-    }
-    if (p.q && row_ok) {   // the query heads: 16 lanes each
-        const Place pl = lane_place<4, kAdjacent>(lane & 15, kD, p.sp.rot);
-        float c[4], s[4];
-        if (pl.turned) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                cos_sin(p.sp.freq[(lane & 15) * 4 + j], p.pos + own * p.sp.axes, p.sp.amplitude, c[j], s[j]);
-        }
-        for (int h0 = 2 * warp; h0 < p.hq; h0 += 2 * kAppendWarps) {
-            const int h = h0 + (lane >> 4);
-            Place ph = pl;
-            ph.active = h < p.hq;
-            float a[4], b[4];
-            if (ph.active) {
-                load_vec<4>(p.q + own * p.q_stride + (int64_t)h * kD + pl.a, a);
-                load_vec<4>(p.q + own * p.q_stride + (int64_t)h * kD + pl.b, b);
-            }
-            if constexpr (kNorm) norm_head<__nv_bfloat16, 4>(a, b, static_cast<const __nv_bfloat16 *>(p.sp.q_weight), ph, p.sp, 16);
-            if (ph.active) {
-                if (pl.turned) turn_pairs<4, kAdjacent, false>(a, b, c, s);
-                __nv_bfloat16 *dst = p.q_dst + ((int64_t)i * p.hq + h) * kD;
-                store_vec<4>(dst + pl.a, a);
-                store_vec<4>(dst + pl.b, b);
-            }
-        }
-    }
-    const int r0 = (int)(slot % kBlk);
-    if (i > 0 && r0 > 0 && (int64_t)p.slots[i - 1] + 1 == slot) return;   // a run's later input
-    // the run: lane j looks at input i + j
+    const Args &p = a.rows;
+    constexpr int kGroup = kD / (2 * V), kPassRows = 32 / kGroup, kPasses = kBlk / kPassRows;
+    const int lane = threadIdx.x & 31, sub = lane / kGroup, chunk = lane & (kGroup - 1);
+    const int32_t slot = p.slots[i];
+    const int r0 = slot & (kBlk - 1);
+    // lane j looks at input i + j
     int64_t row = -1;
     bool in_run = false;
     if (lane < kBlk - r0 && i + lane < p.count) {
-        in_run = (int64_t)p.slots[i + lane] == slot + lane;
+        in_run = p.slots[i + lane] == slot + lane;
         if (in_run) row = p.src_rows ? (int64_t)p.src_rows[i + lane] : i + lane;
     }
     const uint32_t run_bits = __ballot_sync(0xffffffffu, in_run);
     const int n = __ffs((int)~run_bits) - 1;   // (at most 16 lanes look)
-    const uint32_t good = __ballot_sync(0xffffffffu, lane < n && row >= 0 && row < p.src_total);
+    const uint32_t good = __ballot_sync(0xffffffffu, lane < n && row >= 0 && row < p.rows);
     if (!good) return;
-    const int64_t blk = slot / kBlk;
-    const Place pl = lane_place<2, kAdjacent>(lane, kD, p.sp.rot);
-    for (int u = warp; u < 2 * p.hkv; u += kAppendWarps) {
-        const bool is_v = u >= p.hkv;
-        const int g = is_v ? u - p.hkv : u;
-        float *scp = (is_v ? p.v_scales : p.k_scales) + blk * p.hkv + g;
-        uint8_t *codes = (is_v ? p.v_codes : p.k_codes) + (blk * p.hkv + g) * kBlk * kD;
-        const float s_old = r0 == 0 ? 0.f : *scp;
-        uint32_t old[kBlk - 1];
+    const bool is_v = unit >= p.hkv;
+    const int g = is_v ? unit - p.hkv : unit;
+    const Place pl = lane_place<V, kAdjacent>(chunk, kD, p.sp.rot);
+    const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(is_v ? p.v : p.k) + g * kD;
+    const int64_t stride = is_v ? p.v_stride : p.k_stride;
+    Raw<__nv_bfloat16, V> ra[kPasses], rb[kPasses];
 #pragma unroll
-        for (int rr = 0; rr < kBlk - 1; ++rr)
-            old[rr] = rr < r0 ? *reinterpret_cast<const uint16_t *>(codes + rr * kD + pl.a) |
-                                    (uint32_t) * reinterpret_cast<const uint16_t *>(codes + rr * kD + pl.b) << 16
-                              : 0u;
-        float a[kBlk][2], b[kBlk][2];
-        float amax = 0.f;
-#pragma unroll
-        for (int j = 0; j < kBlk; ++j) {
-            if (j >= n) break;
-            const int64_t src = __shfl_sync(0xffffffffu, row, j);
-            if (!(good >> j & 1u)) {
-                a[j][0] = a[j][1] = b[j][0] = b[j][1] = 0.f;
-                continue;
-            }
-            const __nv_bfloat16 *x = (is_v ? p.v + src * p.v_stride : p.k + src * p.k_stride) + (int64_t)g * kD;
-            load_vec<2>(x + pl.a, a[j]);
-            load_vec<2>(x + pl.b, b[j]);
-            if (!is_v) {
-                if constexpr (kNorm)
-                    norm_head<__nv_bfloat16, 2>(a[j], b[j], static_cast<const __nv_bfloat16 *>(p.sp.k_weight), pl, p.sp, 32);
-                if (pl.turned) {
-                    float c[2], s[2];
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        cos_sin(p.sp.freq[lane * 2 + t], p.pos + src * p.sp.axes, p.sp.amplitude, c[t], s[t]);
-                    turn_pairs<2, kAdjacent, false>(a[j], b[j], c, s);
-                }
-            }
-            amax = fmaxf(amax, fmaxf(fmaxf(fabsf(a[j][0]), fabsf(a[j][1])), fmaxf(fabsf(b[j][0]), fabsf(b[j][1]))));
+    for (int t = 0; t < kPasses; ++t) {
+        if (t * kPassRows >= n) break;
+        const int j = t * kPassRows + sub;
+        const int64_t at = __shfl_sync(0xffffffffu, row, j);
+        if (good >> j & 1u) {
+            ra[t] = load_raw<__nv_bfloat16, V>(src + at * stride + pl.a);
+            rb[t] = load_raw<__nv_bfloat16, V>(src + at * stride + pl.b);
         }
-        const float cand = __fdiv_rn(warp_max(amax), 448.f);
-        const Scale sc = make_scale(cand > s_old ? cand : s_old);
-        if (sc.s > s_old && s_old > 0.f) {
-#pragma unroll
-            for (int rr = 0; rr < kBlk - 1; ++rr) {
-                if (rr >= r0) break;
-                float y[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = __fmul_rn(e4m3_to_f32((uint8_t)(old[rr] >> (8 * j))), s_old);
-                *reinterpret_cast<uint16_t *>(codes + rr * kD + pl.a) = (uint16_t)sc.codes(y[0], y[1]);
-                *reinterpret_cast<uint16_t *>(codes + rr * kD + pl.b) = (uint16_t)sc.codes(y[2], y[3]);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kBlk; ++j) {
-            if (j >= n) break;
-            if (!(good >> j & 1u)) continue;
-            uint8_t *dst = codes + (r0 + j) * kD;
-            *reinterpret_cast<uint16_t *>(dst + pl.a) = sc.s > 0.f ? (uint16_t)sc.codes(a[j][0], a[j][1]) : (uint16_t)0;
-            *reinterpret_cast<uint16_t *>(dst + pl.b) = sc.s > 0.f ? (uint16_t)sc.codes(b[j][0], b[j][1]) : (uint16_t)0;
-        }
-        __syncwarp();   // every lane has read the old scale before it is replaced
-        if (lane == 0) *scp = sc.s;
     }
+    const int64_t blk = slot / kBlk;
+    float *scp = (is_v ? a.v_scales : a.k_scales) + blk * p.hkv + g;
+    uint8_t *codes = static_cast<uint8_t *>(is_v ? p.v_out : p.k_out) + (blk * p.hkv + g) * kBlk * kD;
+    using Codes = typename Pick<V == 8, uint2, uint32_t>::type;
+    Codes oa[kPasses], ob[kPasses];
+#pragma unroll
+    for (int t = 0; t < kPasses; ++t) {
+        const int j = t * kPassRows + sub;
+        if (j < r0) {
+            oa[t] = *reinterpret_cast<const Codes *>(codes + j * kD + pl.a);
+            ob[t] = *reinterpret_cast<const Codes *>(codes + j * kD + pl.b);
+        }
+    }
+    const float s_old = r0 == 0 ? 0.f : *scp;
+    float xa[kPasses][V], xb[kPasses][V];
+    float amax = 0.f;
+#pragma unroll
+    for (int t = 0; t < kPasses; ++t) {
+        if (t * kPassRows >= n) break;
+        const int j = t * kPassRows + sub;
+        const bool here = good >> j & 1u;
+        const int64_t at = __shfl_sync(0xffffffffu, row, j);
+        unpack(ra[t], xa[t]);
+        unpack(rb[t], xb[t]);
+        if (!is_v) {
+            if constexpr (kNorm) {
+                Place pn = pl;
+                pn.active = here;
+                const float r = norm_scale<V>(xa[t], xb[t], pn, p.sp, kGroup);
+                if (here) scale_head<V>(xa[t], xb[t], r, static_cast<const __nv_bfloat16 *>(p.sp.k_weight), pl);
+            }
+            if (here && pl.turned) {
+                float c[V], s[V];
+#pragma unroll
+                for (int f = 0; f < V; ++f)
+                    cos_sin<true>(p.sp.freq[chunk * V + f], p.pos + at * p.sp.axes, p.sp, c[f], s[f]);
+                turn_pairs<V, kAdjacent>(xa[t], xb[t], c, s);
+            }
+        }
+        if (here) {
+#pragma unroll
+            for (int f = 0; f < V; ++f) amax = fmaxf(amax, fmaxf(fabsf(xa[t][f]), fabsf(xb[t][f])));
+        }
+    }
+    const float cand = __fdiv_rn(warp_max(amax), 448.f);
+    const Scale sc = make_scale(cand > s_old ? cand : s_old);
+    if (sc.s > s_old && s_old > 0.f) {
+#pragma unroll
+        for (int t = 0; t < kPasses; ++t)
+            if (t * kPassRows + sub < r0) {
+                uint8_t *dst = codes + (t * kPassRows + sub) * kD;
+                *reinterpret_cast<Codes *>(dst + pl.a) = encode_again(oa[t], s_old, sc);
+                *reinterpret_cast<Codes *>(dst + pl.b) = encode_again(ob[t], s_old, sc);
+            }
+    }
+#pragma unroll
+    for (int t = 0; t < kPasses; ++t) {
+        if (t * kPassRows >= n) break;
+        const int j = t * kPassRows + sub;
+        if (good >> j & 1u) {
+            uint8_t *dst = codes + (r0 + j) * kD;
+            *reinterpret_cast<Codes *>(dst + pl.a) = encode(xa[t], sc);
+            *reinterpret_cast<Codes *>(dst + pl.b) = encode(xb[t], sc);
+        }
+    }
+    __syncwarp();   // every lane has read the old scale before it is replaced
+    if (lane == 0) *scp = sc.s;
+}
+
+template <int V, bool kAdjacent, bool kNorm>
+__global__ void __launch_bounds__(32 * kAppendWarps) append_rotary_e4m3_kernel(const __grid_constant__ RotaryAppendArgs a)
+{
+    using namespace padoc_rotary_dev;
+    const Args &p = a.rows;
+    // a programmatic dependent of the previous kernel in the stream, as the plain append
+    pdl_wait_prerequisite();
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if ((int)blockIdx.x >= a.kv_ctas) {
+        const uint32_t w = (blockIdx.x - a.kv_ctas) * kAppendWarps + warp, i = w / (uint32_t)a.q_parts;
+        if (i < p.count) row_part<__nv_bfloat16, V, kAdjacent, kNorm, kQueries>(p, i, w % (uint32_t)a.q_parts);
+        return;
+    }
+    const uint32_t w = blockIdx.x * kAppendWarps + warp, units = 2u * p.hkv;
+    const int unit = (int)(w % units);
+    const int64_t first = (int64_t)(w / units) * a.inputs;
+    if (first >= p.count) return;
+    // lane j looks at input first + j: a run starts where the slot does not continue the one before
+    const int64_t i = first + lane;
+    const bool mine = lane < a.inputs && i < p.count;
+    const int32_t slot = mine ? p.slots[i] : -1;
+    int32_t before = __shfl_up_sync(0xffffffffu, slot, 1);
+    if (lane == 0) before = first > 0 ? p.slots[first - 1] : -1;
+    const bool slot_ok = slot >= 0 && slot < p.pool_slots;
+    if (mine && unit == 0) {
+        const int32_t row = p.src_rows ? p.src_rows[i] : 0;
+        if (!slot_ok || row < 0 || row >= p.rows) padoc_record_error(p.err, PADOC_DEVERR_BLOCK_ID, slot_ok ? row : slot);
+    }
+    uint32_t starts = __ballot_sync(0xffffffffu, mine && slot_ok && ((slot & (kBlk - 1)) == 0 || (int64_t)before + 1 != slot));
+    for (; starts; starts &= starts - 1) append_run<V, kAdjacent, kNorm>(a, (int)first + __ffs((int)starts) - 1, unit);
+}
+
+template <int V>
+padoc_status launch_append_rotary(const RotaryAppendArgs &a, bool adjacent, bool norm, unsigned grid, padoc_stream_t stream)
+{
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(grid);
+    lc.blockDim = dim3(32 * kAppendWarps);
+    lc.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see the kernel's wait
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    auto *kernel = adjacent ? (norm ? append_rotary_e4m3_kernel<V, true, true> : append_rotary_e4m3_kernel<V, true, false>)
+                            : (norm ? append_rotary_e4m3_kernel<V, false, true> : append_rotary_e4m3_kernel<V, false, false>);
+    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, a));
+    return padoc_launch_status();
 }
 
 bool e4m3_pool_ok(const padoc_kv_pool_e4m3 *pool)
@@ -422,32 +483,33 @@ extern "C" padoc_status padoc_append_rotary_inputs_e4m3(const padoc_kv_pool_e4m3
     if (in->rows == 0 || !slots || (in->q && !q_dst)) return PADOC_ERR_INVALID_ARGUMENT;
     const uintptr_t align = (uintptr_t)pool->k_codes | (uintptr_t)pool->v_codes | (uintptr_t)q_dst;
     if ((align & 15) || (((uintptr_t)pool->k_scales | (uintptr_t)pool->v_scales) & 3)) return PADOC_ERR_INVALID_ARGUMENT;
-    RotaryAppendArgs p = {};
+    RotaryAppendArgs a = {};
+    Args &p = a.rows;
     p.err = padoc_device_error_word();
     if (!p.err) return PADOC_ERR_CUDA;
     p.sp = make_spec(rot);
-    p.q = (const __nv_bfloat16 *)in->q, p.k = (const __nv_bfloat16 *)in->k, p.v = (const __nv_bfloat16 *)in->v;
+    p.q = in->q, p.k = in->k, p.v = in->v;
     p.q_stride = in->q_stride, p.k_stride = in->k_stride, p.v_stride = in->v_stride;
     p.pos = in->pos;
-    p.src_total = in->rows;
-    p.q_dst = (__nv_bfloat16 *)q_dst;
+    p.rows = in->rows;
+    p.hq = in->num_q_heads, p.hkv = in->num_kv_heads;
+    p.q_out = q_dst, p.q_out_stride = (int64_t)in->num_q_heads * kD;
+    p.k_out = const_cast<void *>(pool->k_codes), p.v_out = const_cast<void *>(pool->v_codes);
     p.src_rows = src_rows, p.slots = slots;
-    p.k_codes = (uint8_t *)pool->k_codes, p.v_codes = (uint8_t *)pool->v_codes;
-    p.k_scales = (float *)pool->k_scales, p.v_scales = (float *)pool->v_scales;
+    p.count = count;
     p.pool_slots = (int64_t)pool->num_blocks * kBlk;
-    p.hq = in->num_q_heads, p.hkv = in->num_kv_heads, p.count = count;
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)count);
-    lc.blockDim = dim3(32 * kAppendWarps);
-    lc.stream = (cudaStream_t)stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see the kernel's wait
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = attr;
-    lc.numAttrs = 1;
-    const bool norm = rot->q_weight != nullptr;
-    auto *kernel = rot->adjacent ? (norm ? append_rotary_e4m3_kernel<true, true> : append_rotary_e4m3_kernel<true, false>)
-                                 : (norm ? append_rotary_e4m3_kernel<false, true> : append_rotary_e4m3_kernel<false, false>);
-    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, p));
-    return padoc_launch_status();
+    a.k_scales = (float *)pool->k_scales, a.v_scales = (float *)pool->v_scales;
+    const int vec = vec_of(rot, in->dtype);
+    // inputs a warp looks through for runs: one in small calls; up to 16 (a block's rows, so a prefix's warps find one
+    // run each) once there are more than 16 warps an SM
+    const int64_t units = 2 * (int64_t)p.hkv, many = count * units / ((int64_t)padoc_num_sms() * 16);
+    a.inputs = (int)(many < 1 ? 1 : many > kBlk ? kBlk : many);
+    const int64_t kv_ctas = ((count + a.inputs - 1) / a.inputs * units + kAppendWarps - 1) / kAppendWarps;
+    a.q_parts = p.q ? split_rows(p, vec, p.hq) : 0;
+    const int64_t q_ctas = ((int64_t)count * a.q_parts + kAppendWarps - 1) / kAppendWarps;
+    if (kv_ctas > (INT32_MAX >> 2) || q_ctas > (INT32_MAX >> 3)) return PADOC_ERR_UNSUPPORTED;   // (32-bit warp numbers)
+    a.kv_ctas = (int32_t)kv_ctas;
+    const unsigned grid = (unsigned)(kv_ctas + q_ctas);
+    const bool adj = rot->adjacent != 0, norm = rot->q_weight != nullptr;
+    return vec == 8 ? launch_append_rotary<8>(a, adj, norm, grid, stream) : launch_append_rotary<4>(a, adj, norm, grid, stream);
 }

@@ -12,111 +12,28 @@ namespace padoc_rotary_dev {
 
 namespace {
 
-constexpr int kWarps = 8;   // warps per CTA
+constexpr int kWarps = 4;   // warps per CTA
 
-struct Args {
-    Spec sp;
-    const void *q, *k, *v;
-    int64_t q_stride, k_stride, v_stride;   // elements
-    const int32_t *pos;
-    int64_t rows;                           // source rows
-    int32_t hq, hkv;
-    void *q_out, *k_out;
-    int64_t q_out_stride, k_out_stride;
-    int32_t group, splits;                  // lanes per head; warps per row
-    // append
-    void *v_out;                            // with k_out: the pool's arrays
-    const int32_t *src_rows, *slots;
-    int64_t count, pool_slots;
-    int32_t block_size;
-    int *err;
-};
-
-// A warp per row (or `splits` warps), 32 / group heads at a time. Bound by HBM in large calls: every
-// element is read once and written once. kAppend: row i of the call is source row src_rows[i]; its K and V
-// heads go to pool slot slots[i], its query heads to row i of q_out.
-template <typename T, int V, bool kAdjacent, bool kNorm, bool kAppend>
-__global__ void __launch_bounds__(32 * kWarps) rotary_kernel(const Args p)
+// See row_part.
+template <typename T, int V, bool kAdjacent, bool kNorm, int kMode>
+__global__ void __launch_bounds__(32 * kWarps) rotary_kernel(const __grid_constant__ Args p)
 {
     pdl_wait_prerequisite();
     pdl_launch_dependents();
-    const int64_t wid = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int64_t i = wid / p.splits;
-    const int split = (int)(wid - i * p.splits);
-    if (i >= p.count) return;
-    const int lane = threadIdx.x & 31;
-    int64_t row = i, slot = 0;
-    if constexpr (kAppend) {
-        if (p.src_rows) row = p.src_rows[i];
-        slot = p.slots[i];
-        if (slot < 0 || slot >= p.pool_slots || row < 0 || row >= p.rows) {
-            if (lane == 0 && split == 0)
-                padoc_record_error(p.err, PADOC_DEVERR_BLOCK_ID,
-                                   (slot < 0 || slot >= p.pool_slots) ? (int)slot : (int)row);
-            return;
-        }
-    }
-    const int group = p.group, heads = 32 / group;
-    const int sub = lane / group, chunk = lane & (group - 1);
-    const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
-    float c[V], s[V];
-    if (pl.turned) {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            cos_sin(p.sp.freq[chunk * V + j], p.pos + row * p.sp.axes, p.sp.amplitude, c[j], s[j]);
-    }
-    const T *q = static_cast<const T *>(p.q) + row * p.q_stride, *k = static_cast<const T *>(p.k) + row * p.k_stride;
-    const int nq = p.q ? p.hq : 0, turned = nq + p.hkv, total = kAppend ? turned + p.hkv : turned;
-    for (int h0 = split * heads; h0 < total; h0 += p.splits * heads) {
-        const int h = h0 + sub;
-        const bool here = h < total && pl.active;
-        const bool is_q = h < nq, is_v = kAppend && h >= turned;
-        const int hk = is_v ? h - turned : h - nq;
-        const T *src;
-        T *dst;
-        if (is_q) {
-            src = q + (int64_t)h * p.sp.d;
-            dst = static_cast<T *>(p.q_out) + i * p.q_out_stride + (int64_t)h * p.sp.d;
-        } else if constexpr (kAppend) {
-            src = is_v ? static_cast<const T *>(p.v) + row * p.v_stride + (int64_t)hk * p.sp.d : k + (int64_t)hk * p.sp.d;
-            dst = static_cast<T *>(is_v ? p.v_out : p.k_out) +
-                  ((slot / p.block_size * p.hkv + hk) * p.block_size + slot % p.block_size) * p.sp.d;
-        } else {
-            src = k + (int64_t)hk * p.sp.d;
-            dst = static_cast<T *>(p.k_out) + i * p.k_out_stride + (int64_t)hk * p.sp.d;
-        }
-        float a[V], b[V];
-        if (here) {
-            load_vec<V>(src + pl.a, a);
-            load_vec<V>(src + pl.b, b);
-        }
-        if constexpr (kNorm) {
-            float na[V], nb[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) na[j] = a[j], nb[j] = b[j];
-            Place pn = pl;
-            pn.active = here;
-            norm_head<T, V>(na, nb, static_cast<const T *>(is_q ? p.sp.q_weight : p.sp.k_weight), pn, p.sp, group);
-            if (!is_v) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) a[j] = na[j], b[j] = nb[j];
-            }
-        }
-        if (here) {
-            if (pl.turned && !is_v) turn_pairs<V, kAdjacent, false>(a, b, c, s);
-            store_vec<V>(dst + pl.a, a);
-            store_vec<V>(dst + pl.b, b);
-        }
-    }
+    const int64_t i = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    if (i < p.count) row_part<T, V, kAdjacent, kNorm, kMode>(p, i, blockIdx.y);
 }
 
+constexpr int kBwdWarps = 8;    // warps per CTA of the backward with the norm
+constexpr int kBwdStages = 4;   // steps of a warp whose loads are in flight
+
 struct BwdArgs {
-    Spec sp;
-    const void *q, *k;                      // the forward's inputs (with the norm)
+    Spec sp;                                // turns back
+    const void *q, *k;                      // the forward's inputs
     int64_t q_stride, k_stride;
     const int32_t *pos;
     int64_t rows;
-    int32_t hq, hkv, group;
+    int32_t hq, hkv, group_log;
     const void *dq_out, *dk_out;
     int64_t dq_out_stride, dk_out_stride;
     void *dq, *dk;
@@ -124,109 +41,142 @@ struct BwdArgs {
     float *part;                            // [CTAs][2][d]
 };
 
-// The gradient of one kind's heads (the queries or the keys) of a row; acc: the lane's sums of g x r.
-template <typename T, int V, bool kAdjacent, bool kNorm>
-__device__ __forceinline__ void bwd_heads(const BwdArgs &p, const T *x, const T *dy, T *dx, int n, const T *w, const Place &pl,
-                                          int sub, const float (&c)[V], const float (&s)[V], float (&acc)[2 * V])
+template <int kBytes>
+__device__ __forceinline__ void cp_async_vec(uint32_t dst, const void *src)
 {
-    const int group = p.group, heads = 32 / group;
-    for (int h0 = 0; h0 < n; h0 += heads) {
-        const int h = h0 + sub;
-        const bool here = h < n && pl.active;
-        const int64_t at = (int64_t)h * p.sp.d;
-        float a[V], b[V];
-        if (here) {
-            load_vec<V>(dy + at + pl.a, a);
-            load_vec<V>(dy + at + pl.b, b);
-            if (pl.turned) turn_pairs<V, kAdjacent, true>(a, b, c, s);
-        }
-        if constexpr (kNorm) {
-            float xa[V], xb[V], wa[V], wb[V];
-            float ss = 0.f, dot = 0.f;
-            if (here) {
-                load_vec<V>(x + at + pl.a, xa);
-                load_vec<V>(x + at + pl.b, xb);
-                load_vec<V>(w + pl.a, wa);
-                load_vec<V>(w + pl.b, wb);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    ss = fmaf(xa[j], xa[j], fmaf(xb[j], xb[j], ss));
-                    dot = fmaf(a[j] * wa[j], xa[j], fmaf(b[j] * wb[j], xb[j], dot));
-                }
-            }
-            const float r = rsqrtf(group_sum(ss, group) / (float)p.sp.d + p.sp.eps);
-            const float m = group_sum(dot, group) * r / (float)p.sp.d;   // mean of w g x r
-            if (here) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float ha = xa[j] * r, hb = xb[j] * r;
-                    acc[j] = fmaf(a[j], ha, acc[j]);
-                    acc[V + j] = fmaf(b[j], hb, acc[V + j]);
-                    a[j] = r * fmaf(-ha, m, wa[j] * a[j]);
-                    b[j] = r * fmaf(-hb, m, wb[j] * b[j]);
-                }
-            }
-        }
-        if (here) {
-            store_vec<V>(dx + at + pl.a, a);
-            store_vec<V>(dx + at + pl.b, b);
-        }
-    }
+    if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// A warp per row, rows in a grid-wide stride. With the norm every lane keeps fp32 sums of the weights'
-// gradient for its dims; a CTA joins them in a fixed order and writes one partial row, which
-// rotary_weight_grad_kernel adds up (no atomics: the same call gives the same bits).
-template <typename T, int V, bool kAdjacent, bool kNorm>
-__global__ void __launch_bounds__(32 * kWarps) rotary_bwd_kernel(const BwdArgs p)
+// The backward with the norm. A warp per row, rows in a grid-wide stride, 32 / group heads a step. Registers hold
+// the weights' gradient sums and the angles, so the rows' values come through shared memory: every lane copies its
+// own vectors kBwdStages steps ahead (cp.async) and reads them back itself, without a barrier. A CTA joins its
+// warps' sums in a fixed order and writes one partial row, which rotary_weight_grad_kernel adds up (no atomics:
+// the same call gives the same bits). The packed batch of 32768 rows (453 MB) took 276 us with plain loads, one
+// step at a time, at 178 registers.
+template <typename T, int V, bool kAdjacent>
+__global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(const __grid_constant__ BwdArgs p)
 {
-    extern __shared__ float sums[];   // [kWarps][2][d]
+    using Vec = Raw<T, V>;
+    extern __shared__ uint4 smem_raw[];   // [kBwdWarps][kBwdStages][4][32] vectors; at the end [kBwdWarps][2][d] sums
     pdl_wait_prerequisite();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int sub = lane / p.group, chunk = lane & (p.group - 1);
+    const int group = 1 << p.group_log, heads = 32 >> p.group_log;
+    const int sub = lane >> p.group_log, chunk = lane & (group - 1);
     const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
-    float acc_q[2 * V], acc_k[2 * V];
+    const int d = p.sp.d, q_steps = (p.hq + heads - 1) >> (5 - p.group_log), steps = q_steps + ((p.hkv + heads - 1) >> (5 - p.group_log));
+    Vec *ring = reinterpret_cast<Vec *>(smem_raw) + (size_t)warp * kBwdStages * 4 * 32 + lane;
+    const int64_t first = (int64_t)blockIdx.x * kBwdWarps + warp, stride = (int64_t)gridDim.x * kBwdWarps;
+
+    int64_t ahead_row = first;   // the next step to be copied, and the stage it goes to
+    int ahead_step = 0, ahead_stage = 0;
+    auto copy_ahead = [&]() {
+        if (ahead_row < p.rows) {
+            const bool is_q = ahead_step < q_steps;
+            const int h = (is_q ? ahead_step : ahead_step - q_steps) * heads + sub;
+            if (pl.active && h < (is_q ? p.hq : p.hkv)) {
+                const T *x = static_cast<const T *>(is_q ? p.q : p.k) + ahead_row * (is_q ? p.q_stride : p.k_stride) + h * d;
+                const T *g = static_cast<const T *>(is_q ? p.dq_out : p.dk_out) +
+                             ahead_row * (is_q ? p.dq_out_stride : p.dk_out_stride) + h * d;
+                const uint32_t dst = smem_u32(ring + ahead_stage * 4 * 32);
+                constexpr uint32_t kNext = 32 * sizeof(Vec);
+                cp_async_vec<sizeof(Vec)>(dst, x + pl.a);
+                cp_async_vec<sizeof(Vec)>(dst + kNext, x + pl.b);
+                cp_async_vec<sizeof(Vec)>(dst + 2 * kNext, g + pl.a);
+                cp_async_vec<sizeof(Vec)>(dst + 3 * kNext, g + pl.b);
+            }
+        }
+        cp_async_commit();
+        ahead_stage = ahead_stage + 1 == kBwdStages ? 0 : ahead_stage + 1;
+        if (++ahead_step == steps) {
+            ahead_step = 0;
+            ahead_row += stride;
+        }
+    };
 #pragma unroll
-    for (int j = 0; j < 2 * V; ++j) acc_q[j] = acc_k[j] = 0.f;
-    for (int64_t row = (int64_t)blockIdx.x * kWarps + warp; row < p.rows; row += (int64_t)gridDim.x * kWarps) {
+    for (int j = 0; j < kBwdStages; ++j) copy_ahead();
+
+    const float inv_d = 1.f / (float)d;
+    float acc[2][2 * V];
+#pragma unroll
+    for (int j = 0; j < 2 * V; ++j) acc[0][j] = acc[1][j] = 0.f;
+    int stage = 0;
+    for (int64_t row = first; row < p.rows; row += stride) {
         float c[V], s[V];
         if (pl.turned) {
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                cos_sin(p.sp.freq[chunk * V + j], p.pos + row * p.sp.axes, p.sp.amplitude, c[j], s[j]);
+                cos_sin<sizeof(T) == 2>(p.sp.freq[chunk * V + j], p.pos + row * p.sp.axes, p.sp, c[j], s[j]);
         }
-        const T *xq = nullptr, *xk = nullptr;
-        if constexpr (kNorm) {
-            xq = static_cast<const T *>(p.q) + row * p.q_stride;
-            xk = static_cast<const T *>(p.k) + row * p.k_stride;
-        }
-        bwd_heads<T, V, kAdjacent, kNorm>(p, xq, static_cast<const T *>(p.dq_out) + row * p.dq_out_stride,
-                                          static_cast<T *>(p.dq) + row * p.dq_stride, p.hq,
-                                          static_cast<const T *>(p.sp.q_weight), pl, sub, c, s, acc_q);
-        bwd_heads<T, V, kAdjacent, kNorm>(p, xk, static_cast<const T *>(p.dk_out) + row * p.dk_out_stride,
-                                          static_cast<T *>(p.dk) + row * p.dk_stride, p.hkv,
-                                          static_cast<const T *>(p.sp.k_weight), pl, sub, c, s, acc_k);
-    }
-    if constexpr (kNorm) {
-        const int d = p.sp.d;
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
-            float(&acc)[2 * V] = kind ? acc_k : acc_q;
+            const int n = kind ? p.hkv : p.hq;
+            const T *w = static_cast<const T *>(kind ? p.sp.k_weight : p.sp.q_weight);
+            T *out = static_cast<T *>(kind ? p.dk : p.dq) + row * (kind ? p.dk_stride : p.dq_stride);
+            Vec rwa, rwb;
+            if (pl.active) {
+                rwa = load_raw<T, V>(w + pl.a);
+                rwb = load_raw<T, V>(w + pl.b);
+            }
+#pragma unroll 1
+            for (int h = sub; h < n + sub; h += heads) {   // (the same steps for every lane)
+                cp_async_wait<kBwdStages - 1>();
+                const bool here = h < n && pl.active;
+                const Vec *in = ring + stage * 4 * 32;
+                float xa[V], xb[V], a[V], b[V], wa[V], wb[V];
+                float ss = 0.f, dot = 0.f;
+                if (here) {
+                    unpack(in[0], xa);
+                    unpack(in[32], xb);
+                    unpack(in[64], a);
+                    unpack(in[96], b);
+                    if (pl.turned) turn_pairs<V, kAdjacent>(a, b, c, s);
+                    unpack(rwa, wa);
+                    unpack(rwb, wb);
 #pragma unroll
-            for (int j = 0; j < 2 * V; ++j) {
-                float v = acc[j];
-                for (int m = p.group; m < 32; m <<= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
-                if (sub == 0 && pl.active) sums[(warp * 2 + kind) * d + (j < V ? pl.a + j : pl.b + j - V)] = v;
+                    for (int j = 0; j < V; ++j) {
+                        ss = fmaf(xa[j], xa[j], fmaf(xb[j], xb[j], ss));
+                        dot = fmaf(a[j] * wa[j], xa[j], fmaf(b[j] * wb[j], xb[j], dot));
+                    }
+                }
+                const float r = rsqrtf(group_sum(ss, group) * inv_d + p.sp.eps);
+                const float m = group_sum(dot, group) * r * inv_d;   // the mean of w g h
+                if (here) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float ha = xa[j] * r, hb = xb[j] * r;
+                        acc[kind][j] = fmaf(a[j], ha, acc[kind][j]);
+                        acc[kind][V + j] = fmaf(b[j], hb, acc[kind][V + j]);
+                        a[j] = r * fmaf(-ha, m, wa[j] * a[j]);
+                        b[j] = r * fmaf(-hb, m, wb[j] * b[j]);
+                    }
+                    store_vec<V>(out + h * d + pl.a, a);
+                    store_vec<V>(out + h * d + pl.b, b);
+                }
+                copy_ahead();   // into the stage just read
+                stage = stage + 1 == kBwdStages ? 0 : stage + 1;
             }
         }
-        __syncthreads();
-        for (int e = threadIdx.x; e < 2 * d; e += 32 * kWarps) {
-            float v = 0.f;
+    }
+    cp_async_wait<0>();
+    __syncthreads();   // every warp is done with its stages
+    float *sums = reinterpret_cast<float *>(smem_raw);
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) v += sums[w * 2 * d + e];
-            p.part[(int64_t)blockIdx.x * 2 * d + e] = v;
+    for (int kind = 0; kind < 2; ++kind) {
+#pragma unroll
+        for (int j = 0; j < 2 * V; ++j) {
+            float v = acc[kind][j];
+            for (int m = group; m < 32; m <<= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+            if (sub == 0 && pl.active) sums[(warp * 2 + kind) * d + (j < V ? pl.a + j : pl.b + j - V)] = v;
         }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * d; e += 32 * kBwdWarps) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kBwdWarps; ++w) v += sums[w * 2 * d + e];
+        p.part[(int64_t)blockIdx.x * 2 * d + e] = v;
     }
 }
 
@@ -252,19 +202,6 @@ __global__ void __launch_bounds__(256) rotary_weight_grad_kernel(const float *__
 
 size_t elt_size(padoc_dtype t) { return t == PADOC_DTYPE_BF16 ? 2 : 4; }
 
-// Elements of a lane's vectors: 16 bytes where the rotated and the other dims come in whole chunks of
-// them, else 8 bytes (bf16 heads whose dims are an odd multiple of 8).
-int vec_of(const padoc_rotary *r, padoc_dtype t)
-{
-    return t == PADOC_DTYPE_BF16 && r->head_dim % 16 == 0 && r->rotary_dim % 16 == 0 ? 8 : 4;
-}
-int group_of(const padoc_rotary *r, int vec)
-{
-    int g = 1;
-    while (g * 2 * vec < r->head_dim) g *= 2;
-    return g;
-}
-
 padoc_status check_ptr(const void *p, int64_t stride, int64_t rows, int64_t least, size_t esz)
 {
     if (!p) return PADOC_ERR_INVALID_ARGUMENT;
@@ -275,10 +212,10 @@ padoc_status check_ptr(const void *p, int64_t stride, int64_t rows, int64_t leas
 }
 
 template <typename K>
-padoc_status launch(K kernel, unsigned grid, int block, size_t smem, padoc_stream_t stream, const void *args)
+padoc_status launch(K kernel, dim3 grid, int block, size_t smem, padoc_stream_t stream, void **argv)
 {
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(grid);
+    lc.gridDim = grid;
     lc.blockDim = dim3(block);
     lc.dynamicSmemBytes = smem;
     lc.stream = (cudaStream_t)stream;
@@ -287,57 +224,73 @@ padoc_status launch(K kernel, unsigned grid, int block, size_t smem, padoc_strea
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = attr;
     lc.numAttrs = 1;
-    void *argv[1] = {const_cast<void *>(args)};
     PADOC_CUDA_TRY(cudaLaunchKernelExC(&lc, (const void *)kernel, argv));
     return padoc_launch_status();
 }
 
-template <typename T, int V, bool kAppend>
-padoc_status launch_rows(const Args &p, bool adjacent, bool norm, unsigned grid, padoc_stream_t stream)
+template <typename T, int V, int kMode>
+padoc_status launch_rows(const Args &p, bool adjacent, bool norm, dim3 grid, padoc_stream_t stream)
 {
-    auto *k = adjacent ? (norm ? rotary_kernel<T, V, true, true, kAppend> : rotary_kernel<T, V, true, false, kAppend>)
-                       : (norm ? rotary_kernel<T, V, false, true, kAppend> : rotary_kernel<T, V, false, false, kAppend>);
-    return launch(k, grid, 32 * kWarps, 0, stream, &p);
+    auto *k = adjacent ? (norm ? rotary_kernel<T, V, true, true, kMode> : rotary_kernel<T, V, true, false, kMode>)
+                       : (norm ? rotary_kernel<T, V, false, true, kMode> : rotary_kernel<T, V, false, false, kMode>);
+    void *argv[1] = {const_cast<Args *>(&p)};
+    return launch(k, grid, 32 * kWarps, 0, stream, argv);
 }
 
-// Warps per row: one when the rows fill the GPU by themselves, else as many as the heads can use.
-int splits_of(int64_t rows, int heads_total, int group)
-{
-    const int steps = (heads_total + 32 / group - 1) / (32 / group);
-    const int64_t want = (int64_t)padoc_num_sms() * 32 / (rows > 0 ? rows : 1);
-    return (int)(want < 1 ? 1 : want > steps ? steps : want);
-}
-
-template <bool kAppend>
+template <int kMode>
 padoc_status launch_any(Args &p, const padoc_rotary *rot, padoc_dtype dtype, padoc_stream_t stream)
 {
     const int vec = vec_of(rot, dtype);
-    p.group = group_of(rot, vec);
-    p.splits = splits_of(p.count, (p.q ? p.hq : 0) + (kAppend ? 2 : 1) * p.hkv, p.group);
-    const int64_t ctas = (p.count * p.splits + kWarps - 1) / kWarps;
-    if (ctas > INT32_MAX) return PADOC_ERR_UNSUPPORTED;
+    const int parts = split_rows(p, vec, (p.q ? p.hq : 0) + (kMode == kAppend ? 2 : 1) * p.hkv);
+    const dim3 grid((unsigned)((p.count + kWarps - 1) / kWarps), (unsigned)parts);
     const bool adj = rot->adjacent != 0, norm = rot->q_weight != nullptr;
-    if (dtype == PADOC_DTYPE_F32) return launch_rows<float, 4, kAppend>(p, adj, norm, (unsigned)ctas, stream);
-    return vec == 8 ? launch_rows<__nv_bfloat16, 8, kAppend>(p, adj, norm, (unsigned)ctas, stream)
-                    : launch_rows<__nv_bfloat16, 4, kAppend>(p, adj, norm, (unsigned)ctas, stream);
+    if (dtype == PADOC_DTYPE_F32) return launch_rows<float, 4, kMode>(p, adj, norm, grid, stream);
+    return vec == 8 ? launch_rows<__nv_bfloat16, 8, kMode>(p, adj, norm, grid, stream)
+                    : launch_rows<__nv_bfloat16, 4, kMode>(p, adj, norm, grid, stream);
 }
 
-// CTAs of the backward: with the norm each leaves a partial row of weight gradients.
+// CTAs of the backward with the norm, two an SM; each leaves a partial row of weight gradients.
 int bwd_ctas(int64_t rows)
 {
-    const int64_t need = (rows + kWarps - 1) / kWarps, most = 4 * (int64_t)padoc_default_ctas();
+    const int64_t need = (rows + kBwdWarps - 1) / kBwdWarps, most = 2 * (int64_t)padoc_default_ctas();
     return (int)(need < most ? need : most);
 }
 
 template <typename T, int V>
-padoc_status launch_bwd(const BwdArgs &p, bool adjacent, bool norm, int ctas, padoc_stream_t stream)
+padoc_status launch_bwd(const BwdArgs &p, bool adjacent, int ctas, padoc_stream_t stream)
 {
-    auto *k = adjacent ? (norm ? rotary_bwd_kernel<T, V, true, true> : rotary_bwd_kernel<T, V, true, false>)
-                       : (norm ? rotary_bwd_kernel<T, V, false, true> : rotary_bwd_kernel<T, V, false, false>);
-    return launch(k, (unsigned)ctas, 32 * kWarps, norm ? (size_t)kWarps * 2 * p.sp.d * sizeof(float) : 0, stream, &p);
+    auto *k = adjacent ? rotary_norm_bwd_kernel<T, V, true> : rotary_norm_bwd_kernel<T, V, false>;
+    const size_t ring = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>), sums = (size_t)kBwdWarps * 2 * p.sp.d * sizeof(float);
+    const int smem = (int)(ring > sums ? ring : sums);
+    const padoc_status st = padoc_set_max_smem((const void *)k, smem);
+    void *argv[1] = {const_cast<BwdArgs *>(&p)};
+    return st != PADOC_OK ? st : launch(k, dim3((unsigned)ctas), 32 * kBwdWarps, smem, stream, argv);
 }
 
 }  // namespace
+
+int vec_of(const padoc_rotary *r, padoc_dtype t)
+{
+    return t == PADOC_DTYPE_BF16 && r->head_dim % 16 == 0 && r->rotary_dim % 16 == 0 ? 8 : 4;
+}
+
+int group_log_of(int head_dim, int vec)
+{
+    int g = 0;
+    while ((2 * vec << g) < head_dim) ++g;
+    return g;
+}
+
+int split_rows(Args &p, int vec, int heads_total)
+{
+    p.group_log = group_log_of(p.sp.d, vec);
+    const int heads = 32 >> p.group_log;
+    const int steps = (heads_total + heads - 1) / heads, least = (steps + kSteps - 1) / kSteps;
+    const int64_t want = (int64_t)padoc_num_sms() * 16 / p.count;
+    const int parts = want < least ? least : want > steps ? steps : (int)want;
+    p.steps = (steps + parts - 1) / parts;
+    return (steps + p.steps - 1) / p.steps;
+}
 
 padoc_status check_spec(const padoc_rotary *r)
 {
@@ -413,7 +366,7 @@ extern "C" padoc_status padoc_qk_rotary(const padoc_rotary *rot, const padoc_qkv
     p.hq = in->num_q_heads, p.hkv = in->num_kv_heads;
     p.q_out = q_out, p.k_out = k_out;
     p.q_out_stride = q_out_stride, p.k_out_stride = k_out_stride;
-    return launch_any<false>(p, rot, in->dtype, stream);
+    return launch_any<kPacked>(p, rot, in->dtype, stream);
 }
 
 extern "C" padoc_status padoc_append_rotary_inputs(const padoc_kv_pool *pool, const padoc_rotary *rot, const padoc_qkv_rows *in,
@@ -447,7 +400,7 @@ extern "C" padoc_status padoc_append_rotary_inputs(const padoc_kv_pool *pool, co
     p.pool_slots = (int64_t)pool->num_blocks * pool->block_size;
     p.block_size = pool->block_size;
     p.err = err;
-    return launch_any<true>(p, rot, in->dtype, stream);
+    return launch_any<kAppend>(p, rot, in->dtype, stream);
 }
 
 extern "C" padoc_status padoc_qk_rotary_bwd_workspace_size(const padoc_rotary *rot, int64_t rows, size_t *bytes)
@@ -490,14 +443,27 @@ extern "C" padoc_status padoc_qk_rotary_bwd(const padoc_rotary *rot, const padoc
         if (st == PADOC_OK) st = check_ptr(dk, dk_stride, in->rows, nk, e);
         if (st != PADOC_OK) return st;
     }
-    const int ctas = bwd_ctas(in->rows);
-    if (norm && ctas > 0) {
-        if (!workspace || (((uintptr_t)workspace) & 255)) return PADOC_ERR_INVALID_ARGUMENT;
-        if (workspace_bytes < (size_t)ctas * 2 * rot->head_dim * sizeof(float)) return PADOC_ERR_WORKSPACE_TOO_SMALL;
+    Spec back = make_spec(rot);
+    back.sin_amplitude = -back.sin_amplitude;
+    if (!norm) {   // the rotation back is the forward's kernel
+        if (in->rows == 0) return PADOC_OK;
+        Args p = {};
+        p.sp = back;
+        p.q = dq_out, p.k = dk_out;
+        p.q_stride = dq_out_stride, p.k_stride = dk_out_stride;
+        p.pos = in->pos;
+        p.rows = p.count = in->rows;
+        p.hq = in->num_q_heads, p.hkv = in->num_kv_heads;
+        p.q_out = dq, p.k_out = dk;
+        p.q_out_stride = dq_stride, p.k_out_stride = dk_stride;
+        return launch_any<kPacked>(p, rot, in->dtype, stream);
     }
+    const int ctas = bwd_ctas(in->rows), d = rot->head_dim;
     if (ctas > 0) {
+        if (!workspace || (((uintptr_t)workspace) & 255)) return PADOC_ERR_INVALID_ARGUMENT;
+        if (workspace_bytes < (size_t)ctas * 2 * d * sizeof(float)) return PADOC_ERR_WORKSPACE_TOO_SMALL;
         BwdArgs p = {};
-        p.sp = make_spec(rot);
+        p.sp = back;
         p.q = in->q, p.k = in->k;
         p.q_stride = in->q_stride, p.k_stride = in->k_stride;
         p.pos = in->pos;
@@ -509,25 +475,16 @@ extern "C" padoc_status padoc_qk_rotary_bwd(const padoc_rotary *rot, const padoc
         p.dq_stride = dq_stride, p.dk_stride = dk_stride;
         p.part = (float *)workspace;
         const int vec = vec_of(rot, in->dtype);
-        p.group = group_of(rot, vec);
+        p.group_log = group_log_of(d, vec);
         const bool adj = rot->adjacent != 0;
-        st = in->dtype == PADOC_DTYPE_F32 ? launch_bwd<float, 4>(p, adj, norm, ctas, stream)
-             : vec == 8                   ? launch_bwd<__nv_bfloat16, 8>(p, adj, norm, ctas, stream)
-                                          : launch_bwd<__nv_bfloat16, 4>(p, adj, norm, ctas, stream);
+        st = in->dtype == PADOC_DTYPE_F32 ? launch_bwd<float, 4>(p, adj, ctas, stream)
+             : vec == 8                   ? launch_bwd<__nv_bfloat16, 8>(p, adj, ctas, stream)
+                                          : launch_bwd<__nv_bfloat16, 4>(p, adj, ctas, stream);
         if (st != PADOC_OK) return st;
     }
-    if (!norm) return PADOC_OK;
-    // no rows: the weights' gradients are zero
-    const int d = rot->head_dim;
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)((2 * d + 31) / 32));
-    lc.blockDim = dim3(256);
-    lc.stream = (cudaStream_t)stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = attr;
-    lc.numAttrs = 1;
-    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, rotary_weight_grad_kernel, (const float *)workspace, ctas, d, dq_weight, dk_weight));
-    return padoc_launch_status();
+    // (with no rows there are no partial sums: zeros)
+    const float *part = (const float *)workspace;
+    int n = ctas, dim = d;
+    void *argv[5] = {&part, &n, &dim, &dq_weight, &dk_weight};
+    return launch(rotary_weight_grad_kernel, dim3((unsigned)((2 * d + 31) / 32)), 256, 0, stream, argv);
 }

@@ -15,11 +15,11 @@ namespace padoc_rotary_dev {
 struct Spec {
     const uint64_t *freq;        // [rot / 2]
     const void *q_weight, *k_weight;
-    float eps, amplitude;
+    float eps, cos_amplitude, sin_amplitude;   // (the sine's negated: the rotation back)
     int32_t d, rot, axes;
 };
 
-// The cosine and sine of one pair's angle, times the amplitude. A table entry holds the fraction of a
+// The cosine and sine of one pair's angle, times their amplitudes. A table entry holds the fraction of a
 // turn per position unit as a 64-bit integer, its axis in the two lowest bits; times a 32-bit position it
 // wraps modulo a whole turn, so the angle of a position a million tokens away is as exact as that of the
 // first ones (its fraction is cut at 2^-32 of a turn; a product in fp32 would be off by 0.06 rad at 10^6).
@@ -29,40 +29,62 @@ __device__ __forceinline__ float half_turns(uint64_t f, const int32_t *__restric
     const int32_t t = (int32_t)(((f & ~(uint64_t)3) * (uint64_t)(int64_t)p) >> 32);
     return (float)t * 0x1p-31f;   // in [-1, 1): the angle is pi times this
 }
-__device__ __forceinline__ void cos_sin(uint64_t f, const int32_t *__restrict__ pos, float amplitude, float &c, float &s)
+// kFast (outputs of 16 bits): the hardware's sine and cosine, 2^-20.5 off at most on [-pi, pi], 2^-12 of
+// the half step that the output is rounded by; else CUDA's sincospif, within 2 units of the last place, which takes
+// some 40 instructions more a pair: a quarter of the packed forward's time when bf16 rows took it too.
+template <bool kFast>
+__device__ __forceinline__ void cos_sin(uint64_t f, const int32_t *__restrict__ pos, const Spec &sp, float &c, float &s)
 {
-    sincospif(half_turns(f, pos), &s, &c);
-    c *= amplitude;
-    s *= amplitude;
+    const float t = half_turns(f, pos);
+    if constexpr (kFast) __sincosf(t * 3.14159265358979f, &s, &c);
+    else sincospif(t, &s, &c);
+    c *= sp.cos_amplitude;
+    s *= sp.sin_amplitude;
 }
 
-// V consecutive elements as fp32.
-template <int V>
-__device__ __forceinline__ void load_vec(const __nv_bfloat16 *p, float (&x)[V])
+// V consecutive elements, as they are stored and as fp32.
+template <typename T, int V>
+struct Raw;
+template <>
+struct Raw<__nv_bfloat16, 8> {
+    uint4 w;
+};
+template <>
+struct Raw<__nv_bfloat16, 4> {
+    uint2 w;
+};
+template <>
+struct Raw<float, 4> {
+    float4 w;
+};
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> load_raw(const T *p)
 {
-    static_assert(V == 8 || V == 4 || V == 2, "8, 4 or 2 elements");
-    uint32_t w[V / 2];
-    if constexpr (V == 8) {
-        const uint4 u = *reinterpret_cast<const uint4 *>(p);
-        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-    } else if constexpr (V == 4) {
-        const uint2 u = *reinterpret_cast<const uint2 *>(p);
-        w[0] = u.x, w[1] = u.y;
-    } else {
-        w[0] = *reinterpret_cast<const uint32_t *>(p);
-    }
-#pragma unroll
-    for (int j = 0; j < V / 2; ++j) {
-        x[2 * j] = __uint_as_float(w[j] << 16);
-        x[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-    }
+    Raw<T, V> r;
+    r.w = *reinterpret_cast<const decltype(r.w) *>(p);
+    return r;
 }
-template <int V>
-__device__ __forceinline__ void load_vec(const float *p, float (&x)[V])
+__device__ __forceinline__ void widen(uint32_t w, float &lo, float &hi)
 {
-    static_assert(V == 4, "4 elements");
-    const float4 u = *reinterpret_cast<const float4 *>(p);
-    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xFFFF0000u);
+}
+__device__ __forceinline__ void unpack(const Raw<__nv_bfloat16, 8> &r, float (&x)[8])
+{
+    widen(r.w.x, x[0], x[1]), widen(r.w.y, x[2], x[3]), widen(r.w.z, x[4], x[5]), widen(r.w.w, x[6], x[7]);
+}
+__device__ __forceinline__ void unpack(const Raw<__nv_bfloat16, 4> &r, float (&x)[4])
+{
+    widen(r.w.x, x[0], x[1]), widen(r.w.y, x[2], x[3]);
+}
+__device__ __forceinline__ void unpack(const Raw<float, 4> &r, float (&x)[4])
+{
+    x[0] = r.w.x, x[1] = r.w.y, x[2] = r.w.z, x[3] = r.w.w;
+}
+template <int V, typename T>
+__device__ __forceinline__ void load_vec(const T *p, float (&x)[V])
+{
+    unpack(load_raw<T, V>(p), x);
 }
 template <int V>
 __device__ __forceinline__ void store_vec(__nv_bfloat16 *p, const float (&x)[V])
@@ -71,8 +93,7 @@ __device__ __forceinline__ void store_vec(__nv_bfloat16 *p, const float (&x)[V])
 #pragma unroll
     for (int j = 0; j < V / 2; ++j) w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
     if constexpr (V == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    else if constexpr (V == 4) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint32_t *>(p) = w[0];
+    else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
 }
 template <int V>
 __device__ __forceinline__ void store_vec(float *p, const float (&x)[V])
@@ -104,14 +125,14 @@ __device__ __forceinline__ Place lane_place(int chunk, int d, int rot)
     return p;
 }
 
-// The rotation of a lane's V pairs by its angles (kBack: by the opposite ones, the gradient's).
-template <int V, bool kAdjacent, bool kBack>
+// The rotation of a lane's V pairs by its angles.
+template <int V, bool kAdjacent>
 __device__ __forceinline__ void turn_pairs(float (&a)[V], float (&b)[V], const float (&c)[V], const float (&s)[V])
 {
     auto turn = [](float &x, float &y, float cc, float ss) {
         const float x0 = x, y0 = y;
-        x = kBack ? fmaf(x0, cc, y0 * ss) : fmaf(x0, cc, -(y0 * ss));
-        y = kBack ? fmaf(y0, cc, -(x0 * ss)) : fmaf(y0, cc, x0 * ss);
+        x = fmaf(x0, cc, -(y0 * ss));
+        y = fmaf(y0, cc, x0 * ss);
     };
     if constexpr (!kAdjacent) {
 #pragma unroll
@@ -125,32 +146,145 @@ __device__ __forceinline__ void turn_pairs(float (&a)[V], float (&b)[V], const f
 }
 
 // RMS norm of a head spread over `group` lanes: x r w with r = 1 / sqrt(mean x^2 + eps), sums in fp32.
-template <typename T, int V>
-__device__ __forceinline__ void norm_head(float (&a)[V], float (&b)[V], const T *w, const Place &pl, const Spec &sp, int group)
+template <int V>
+__device__ __forceinline__ float norm_scale(const float (&a)[V], const float (&b)[V], const Place &pl, const Spec &sp, int group)
 {
     float ss = 0.f;
     if (pl.active) {
 #pragma unroll
         for (int j = 0; j < V; ++j) ss = fmaf(a[j], a[j], fmaf(b[j], b[j], ss));
     }
-    const float r = rsqrtf(group_sum(ss, group) / (float)sp.d + sp.eps);
-    if (pl.active) {
-        float wa[V], wb[V];
-        load_vec<V>(w + pl.a, wa);
-        load_vec<V>(w + pl.b, wb);
+    return rsqrtf(group_sum(ss, group) / (float)sp.d + sp.eps);
+}
+template <int V, typename T>
+__device__ __forceinline__ void scale_head(float (&a)[V], float (&b)[V], float r, const T *w, const Place &pl)
+{
+    float wa[V], wb[V];
+    load_vec<V>(w + pl.a, wa);
+    load_vec<V>(w + pl.b, wb);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            a[j] *= r * wa[j];
-            b[j] *= r * wb[j];
+    for (int j = 0; j < V; ++j) {
+        a[j] *= r * wa[j];
+        b[j] *= r * wb[j];
+    }
+}
+
+// Arguments of a call's rows.
+struct Args {
+    Spec sp;
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;   // elements
+    const int32_t *pos;
+    int64_t rows;                           // source rows
+    int32_t hq, hkv;
+    void *q_out, *k_out;
+    int64_t q_out_stride, k_out_stride;
+    int32_t group_log, steps;               // log2 of the lanes per head; steps of a part
+    // append
+    void *v_out;                            // with k_out: the pool's arrays
+    const int32_t *src_rows, *slots;
+    int64_t count, pool_slots;
+    int32_t block_size;
+    int *err;
+};
+
+// What a call does with its rows: writes the query and key heads to rows of their own; appends to the paged
+// pool (row i of the call is source row src_rows[i]; its K and V heads go to pool slot slots[i], its query heads
+// to row i of q_out); or writes an append's query heads only.
+enum { kPacked = 0, kAppend = 1, kQueries = 2 };
+
+constexpr int kSteps = 5;   // most steps of a part: the 16 + 2 heads of 128 dims in bf16, four at a time
+
+// One warp's work: part `part` of row i, p.steps steps of 32 / group heads, at most kSteps. All of the part's loads
+// are issued before its angles are computed. Bound by HBM in large calls: every element is read once and written
+// once.
+template <typename T, int V, bool kAdjacent, bool kNorm, int kMode>
+__device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
+{
+    const int lane = threadIdx.x & 31;
+    int64_t row = i;
+    uint32_t slot = 0;
+    if constexpr (kMode != kPacked) {
+        if (p.src_rows) row = p.src_rows[i];
+        const int32_t at = p.slots[i];
+        if (at < 0 || at >= p.pool_slots || row < 0 || row >= p.rows) {
+            if (kMode == kAppend && lane == 0 && part == 0)
+                padoc_record_error(p.err, PADOC_DEVERR_BLOCK_ID, (at < 0 || at >= p.pool_slots) ? at : (int)row);
+            return;
+        }
+        slot = (uint32_t)at;
+    }
+    const int group = 1 << p.group_log, heads = 32 >> p.group_log;
+    const int sub = lane >> p.group_log, chunk = lane & (group - 1);
+    const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
+    const T *q = static_cast<const T *>(p.q) + row * p.q_stride, *k = static_cast<const T *>(p.k) + row * p.k_stride;
+    const int nq = p.q ? p.hq : 0, turned = kMode == kQueries ? nq : nq + p.hkv, total = kMode == kAppend ? turned + p.hkv : turned;
+    const int first = part * p.steps * heads + sub;
+    Raw<T, V> ra[kSteps], rb[kSteps];
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+        const int h = first + u * heads;
+        if (u < p.steps && h < total && pl.active) {
+            const T *src = h < nq ? q + h * p.sp.d : k + (h - nq) * p.sp.d;
+            if (kMode == kAppend && h >= turned) src = static_cast<const T *>(p.v) + row * p.v_stride + (h - turned) * p.sp.d;
+            ra[u] = load_raw<T, V>(src + pl.a);
+            rb[u] = load_raw<T, V>(src + pl.b);
+        }
+    }
+    float c[V], s[V];
+    if (pl.turned) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            cos_sin<sizeof(T) == 2>(p.sp.freq[chunk * V + j], p.pos + row * p.sp.axes, p.sp, c[j], s[j]);
+    }
+    T *q_out = static_cast<T *>(p.q_out) + i * p.q_out_stride;
+    // where the row's KV heads go, and the distance from one to the next
+    int64_t k_at = 0, k_step = p.sp.d;
+    if constexpr (kMode == kAppend) {
+        const uint32_t bs = (uint32_t)p.block_size;
+        k_at = ((int64_t)(slot / bs) * p.hkv * bs + slot % bs) * p.sp.d;
+        k_step = (int64_t)bs * p.sp.d;
+    } else if constexpr (kMode == kPacked) {
+        k_at = i * p.k_out_stride;
+    }
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+        if (u >= p.steps) break;
+        const int h = first + u * heads;
+        const bool here = h < total && pl.active, is_q = h < nq, is_v = kMode == kAppend && h >= turned;
+        float a[V], b[V];
+        unpack(ra[u], a);
+        unpack(rb[u], b);
+        if constexpr (kNorm) {
+            Place pn = pl;
+            pn.active = here;
+            const float r = norm_scale<V>(a, b, pn, p.sp, group);
+            if (here && !is_v) scale_head<V>(a, b, r, static_cast<const T *>(is_q ? p.sp.q_weight : p.sp.k_weight), pl);
+        }
+        if (here) {
+            if (pl.turned && !is_v) turn_pairs<V, kAdjacent>(a, b, c, s);
+            T *dst = is_q ? q_out + h * p.sp.d : static_cast<T *>(p.k_out) + k_at + (h - nq) * k_step;
+            if (is_v) dst = static_cast<T *>(p.v_out) + k_at + (h - turned) * k_step;
+            store_vec<V>(dst + pl.a, a);
+            store_vec<V>(dst + pl.b, b);
         }
     }
 }
+
+// Elements of a lane's vectors: 16 bytes where the rotated and the other dims come in whole chunks of
+// them, else 8 bytes (bf16 heads whose dims are an odd multiple of 8).
+int vec_of(const padoc_rotary *rot, padoc_dtype dtype);
+// log2 of the lanes that share a head.
+int group_log_of(int head_dim, int vec);
+// Sets group_log and steps; returns the parts of a row: as few as kSteps allows when the rows fill the GPU by
+// themselves, else as many as the heads can use, up to 16 warps an SM.
+int split_rows(Args &p, int vec, int heads_total);
 
 // Host checks of a padoc_rotary (defined in rotary.cu), and its device form.
 padoc_status check_spec(const padoc_rotary *rot);
 inline Spec make_spec(const padoc_rotary *r)
 {
-    return Spec{r->freq, r->q_weight, r->k_weight, r->eps, r->amplitude, r->head_dim, r->rotary_dim, r->num_axes};
+    return Spec{r->freq, r->q_weight, r->k_weight, r->eps, r->amplitude, r->amplitude, r->head_dim, r->rotary_dim, r->num_axes};
 }
 // Host checks of a call's source rows: strides and alignment of q (when given), k and, with_v, v.
 padoc_status check_rows(const padoc_qkv_rows *in, const padoc_rotary *rot, bool with_v);
