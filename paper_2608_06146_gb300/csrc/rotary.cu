@@ -52,107 +52,147 @@ __device__ __forceinline__ void cp_async_vec(uint32_t dst, const void *src)
 // the weights' gradient sums and the angles, so the rows' values come through shared memory: every lane copies its
 // own vectors kBwdStages steps ahead (cp.async) and reads them back itself, without a barrier. A CTA joins its
 // warps' sums in a fixed order and writes one partial row, which rotary_weight_grad_kernel adds up (no atomics:
-// the same call gives the same bits). The packed batch of 32768 rows (453 MB) took 276 us with plain loads, one
-// step at a time, at 178 registers.
-template <typename T, int V, bool kAdjacent>
+// the same call gives the same bits). Arithmetic is on packed pairs, weights come from shared memory in fp32: the
+// kernel is bound by issued instructions as much as by HBM. The packed batch of 32768 rows (453 MB): 276 us with
+// plain loads, one step at a time, at 178 registers; 115 us through the ring with scalar arithmetic (2620
+// instructions a row).
+// kGroup: the lanes that share a head where known at compile time (0: group_log says).
+template <typename T, int V, bool kAdjacent, int kGroup>
 __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(const __grid_constant__ BwdArgs p)
 {
     using Vec = Raw<T, V>;
-    extern __shared__ uint4 smem_raw[];   // [kBwdWarps][kBwdStages][4][32] vectors; at the end [kBwdWarps][2][d] sums
+    constexpr int kPairs = V / 2;
+    // [2][kPairs][group] weights in fp32, four to a piece, the pieces of a lane's two vectors; then
+    // [kBwdWarps][kBwdStages][4][32] vectors; at the end [kBwdWarps][2][d] sums
+    extern __shared__ uint4 smem_raw[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int group = kGroup ? kGroup : 1 << p.group_log, heads = 32 / group;
+    const int sub = lane / group, chunk = lane & (group - 1);
+    const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
+    const int d = p.sp.d, q_steps = (p.hq + heads - 1) / heads, steps = q_steps + (p.hkv + heads - 1) / heads;
+    Vec *ring = reinterpret_cast<Vec *>(smem_raw + 2 * kPairs * group) + (size_t)warp * kBwdStages * 4 * 32 + lane;
     pdl_wait_prerequisite();
     pdl_launch_dependents();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int group = 1 << p.group_log, heads = 32 >> p.group_log;
-    const int sub = lane >> p.group_log, chunk = lane & (group - 1);
-    const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
-    const int d = p.sp.d, q_steps = (p.hq + heads - 1) >> (5 - p.group_log), steps = q_steps + ((p.hkv + heads - 1) >> (5 - p.group_log));
-    Vec *ring = reinterpret_cast<Vec *>(smem_raw) + (size_t)warp * kBwdStages * 4 * 32 + lane;
+    for (int e = threadIdx.x; e < 2 * kPairs * group; e += 32 * kBwdWarps) {
+        const int kind = e >= kPairs * group, piece = e / group - kind * kPairs;
+        const Place at = lane_place<V, kAdjacent>(e & (group - 1), d, p.sp.rot);
+        if (!at.active) continue;
+        const T *w = static_cast<const T *>(kind ? p.sp.k_weight : p.sp.q_weight) +
+                     (piece < kPairs / 2 ? at.a + 4 * piece : at.b + 4 * (piece - kPairs / 2));
+        reinterpret_cast<float4 *>(smem_raw)[e] = make_float4((float)w[0], (float)w[1], (float)w[2], (float)w[3]);
+    }
+    __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * kBwdWarps + warp, stride = (int64_t)gridDim.x * kBwdWarps;
 
-    int64_t ahead_row = first;   // the next step to be copied, and the stage it goes to
-    int ahead_step = 0, ahead_stage = 0;
+    // the next step to be copied: its row, step and addresses (of the lane's first vectors), and its stage
+    int64_t ahead_row = first;
+    int ahead_step = 0;
+    uint32_t ahead_at = smem_u32(ring);
+    const uint32_t ring_end = ahead_at + kBwdStages * 4 * 32 * (uint32_t)sizeof(Vec);
+    const int lane_at = sub * d + pl.a, to_b = pl.b - pl.a;
+    const T *ax = nullptr, *ag = nullptr;
     auto copy_ahead = [&]() {
         if (ahead_row < p.rows) {
-            const bool is_q = ahead_step < q_steps;
-            const int h = (is_q ? ahead_step : ahead_step - q_steps) * heads + sub;
-            if (pl.active && h < (is_q ? p.hq : p.hkv)) {
-                const T *x = static_cast<const T *>(is_q ? p.q : p.k) + ahead_row * (is_q ? p.q_stride : p.k_stride) + h * d;
-                const T *g = static_cast<const T *>(is_q ? p.dq_out : p.dk_out) +
-                             ahead_row * (is_q ? p.dq_out_stride : p.dk_out_stride) + h * d;
-                const uint32_t dst = smem_u32(ring + ahead_stage * 4 * 32);
+            if (ahead_step == 0) {
+                ax = static_cast<const T *>(p.q) + ahead_row * p.q_stride + lane_at;
+                ag = static_cast<const T *>(p.dq_out) + ahead_row * p.dq_out_stride + lane_at;
+            } else if (ahead_step == q_steps) {
+                ax = static_cast<const T *>(p.k) + ahead_row * p.k_stride + lane_at;
+                ag = static_cast<const T *>(p.dk_out) + ahead_row * p.dk_out_stride + lane_at;
+            }
+            const int left = ahead_step < q_steps ? p.hq - ahead_step * heads : p.hkv - (ahead_step - q_steps) * heads;
+            if (pl.active && sub < left) {
                 constexpr uint32_t kNext = 32 * sizeof(Vec);
-                cp_async_vec<sizeof(Vec)>(dst, x + pl.a);
-                cp_async_vec<sizeof(Vec)>(dst + kNext, x + pl.b);
-                cp_async_vec<sizeof(Vec)>(dst + 2 * kNext, g + pl.a);
-                cp_async_vec<sizeof(Vec)>(dst + 3 * kNext, g + pl.b);
+                cp_async_vec<sizeof(Vec)>(ahead_at, ax);
+                cp_async_vec<sizeof(Vec)>(ahead_at + kNext, ax + to_b);
+                cp_async_vec<sizeof(Vec)>(ahead_at + 2 * kNext, ag);
+                cp_async_vec<sizeof(Vec)>(ahead_at + 3 * kNext, ag + to_b);
+            }
+            ax += heads * d;
+            ag += heads * d;
+            if (++ahead_step == steps) {
+                ahead_step = 0;
+                ahead_row += stride;
             }
         }
         cp_async_commit();
-        ahead_stage = ahead_stage + 1 == kBwdStages ? 0 : ahead_stage + 1;
-        if (++ahead_step == steps) {
-            ahead_step = 0;
-            ahead_row += stride;
-        }
+        ahead_at += 4 * 32 * (uint32_t)sizeof(Vec);
+        if (ahead_at == ring_end) ahead_at -= kBwdStages * 4 * 32 * (uint32_t)sizeof(Vec);
     };
 #pragma unroll
     for (int j = 0; j < kBwdStages; ++j) copy_ahead();
 
     const float inv_d = 1.f / (float)d;
-    float acc[2][2 * V];
+    uint64_t acc[2][V];   // sums of g h: the pairs of the lane's first, then of its second vector
 #pragma unroll
-    for (int j = 0; j < 2 * V; ++j) acc[0][j] = acc[1][j] = 0.f;
+    for (int j = 0; j < V; ++j) acc[0][j] = acc[1][j] = 0;
     int stage = 0;
     for (int64_t row = first; row < p.rows; row += stride) {
-        float c[V], s[V];
+        uint64_t c[kPairs], s[kPairs];
         if (pl.turned) {
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                cos_sin<sizeof(T) == 2>(p.sp.freq[chunk * V + j], p.pos + row * p.sp.axes, p.sp, c[j], s[j]);
+            for (int j = 0; j < kPairs; ++j) {
+                float c0, c1, s0, s1;
+                cos_sin<sizeof(T) == 2>(p.sp.freq[chunk * V + 2 * j], p.pos + row * p.sp.axes, p.sp, c0, s0);
+                cos_sin<sizeof(T) == 2>(p.sp.freq[chunk * V + 2 * j + 1], p.pos + row * p.sp.axes, p.sp, c1, s1);
+                c[j] = f2_pack(c0, c1);
+                s[j] = f2_pack(s0, s1);
+            }
         }
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
-            const int n = kind ? p.hkv : p.hq;
-            const T *w = static_cast<const T *>(kind ? p.sp.k_weight : p.sp.q_weight);
-            T *out = static_cast<T *>(kind ? p.dk : p.dq) + row * (kind ? p.dk_stride : p.dq_stride);
-            Vec rwa, rwb;
-            if (pl.active) {
-                rwa = load_raw<T, V>(w + pl.a);
-                rwb = load_raw<T, V>(w + pl.b);
-            }
+            const ulonglong2 *w = reinterpret_cast<const ulonglong2 *>(smem_raw) + kind * kPairs * group + chunk;
+            auto read_weights = [&](uint64_t(&wa)[kPairs], uint64_t(&wb)[kPairs]) {
+#pragma unroll
+                for (int j = 0; j < kPairs / 2; ++j) {
+                    const ulonglong2 a = w[j * group], b = w[(kPairs / 2 + j) * group];
+                    wa[2 * j] = a.x, wa[2 * j + 1] = a.y;
+                    wb[2 * j] = b.x, wb[2 * j + 1] = b.y;
+                }
+            };
+            T *out = kind ? static_cast<T *>(p.dk) + row * p.dk_stride : static_cast<T *>(p.dq) + row * p.dq_stride;
+            out += lane_at;
 #pragma unroll 1
-            for (int h = sub; h < n + sub; h += heads) {   // (the same steps for every lane)
+            for (int left = kind ? p.hkv : p.hq; left > 0; left -= heads, out += heads * d) {
                 cp_async_wait<kBwdStages - 1>();
-                const bool here = h < n && pl.active;
+                const bool here = sub < left && pl.active;
                 const Vec *in = ring + stage * 4 * 32;
-                float xa[V], xb[V], a[V], b[V], wa[V], wb[V];
+                uint64_t xa[kPairs], xb[kPairs], a[kPairs], b[kPairs];
                 float ss = 0.f, dot = 0.f;
                 if (here) {
-                    unpack(in[0], xa);
-                    unpack(in[32], xb);
-                    unpack(in[64], a);
-                    unpack(in[96], b);
-                    if (pl.turned) turn_pairs<V, kAdjacent>(a, b, c, s);
-                    unpack(rwa, wa);
-                    unpack(rwb, wb);
+                    unpack2(in[0], xa);
+                    unpack2(in[32], xb);
+                    unpack2(in[64], a);
+                    unpack2(in[96], b);
+                    if (pl.turned) turn_pairs2<V, kAdjacent>(a, b, c, s);
+                    uint64_t wa[kPairs], wb[kPairs];
+                    read_weights(wa, wb);
+                    uint64_t s2 = 0, d2 = 0;
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        ss = fmaf(xa[j], xa[j], fmaf(xb[j], xb[j], ss));
-                        dot = fmaf(a[j] * wa[j], xa[j], fmaf(b[j] * wb[j], xb[j], dot));
+                    for (int j = 0; j < kPairs; ++j) {
+                        s2 = f2_fma(xa[j], xa[j], f2_fma(xb[j], xb[j], s2));
+                        d2 = f2_fma(f2_mul(a[j], wa[j]), xa[j], f2_fma(f2_mul(b[j], wb[j]), xb[j], d2));
                     }
+                    ss = f2_sum(s2);
+                    dot = f2_sum(d2);
                 }
                 const float r = rsqrtf(group_sum(ss, group) * inv_d + p.sp.eps);
                 const float m = group_sum(dot, group) * r * inv_d;   // the mean of w g h
                 if (here) {
+                    // dx = r (w g - h m) with h = x r
+                    const uint64_t r2 = f2_pack(r, r), m2 = f2_pack(-m, -m);
+                    uint64_t wa[kPairs], wb[kPairs];
+                    read_weights(wa, wb);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float ha = xa[j] * r, hb = xb[j] * r;
-                        acc[kind][j] = fmaf(a[j], ha, acc[kind][j]);
-                        acc[kind][V + j] = fmaf(b[j], hb, acc[kind][V + j]);
-                        a[j] = r * fmaf(-ha, m, wa[j] * a[j]);
-                        b[j] = r * fmaf(-hb, m, wb[j] * b[j]);
+                    for (int j = 0; j < kPairs; ++j) {
+                        const uint64_t ha = f2_mul(xa[j], r2), hb = f2_mul(xb[j], r2);
+                        acc[kind][j] = f2_fma(a[j], ha, acc[kind][j]);
+                        acc[kind][kPairs + j] = f2_fma(b[j], hb, acc[kind][kPairs + j]);
+                        a[j] = f2_mul(r2, f2_fma(ha, m2, f2_mul(a[j], wa[j])));
+                        b[j] = f2_mul(r2, f2_fma(hb, m2, f2_mul(b[j], wb[j])));
                     }
-                    store_vec<V>(out + h * d + pl.a, a);
-                    store_vec<V>(out + h * d + pl.b, b);
+                    store_vec2<V>(out, a);
+                    store_vec2<V>(out + to_b, b);
                 }
                 copy_ahead();   // into the stage just read
                 stage = stage + 1 == kBwdStages ? 0 : stage + 1;
@@ -165,10 +205,15 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind) {
 #pragma unroll
-        for (int j = 0; j < 2 * V; ++j) {
-            float v = acc[kind][j];
-            for (int m = group; m < 32; m <<= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
-            if (sub == 0 && pl.active) sums[(warp * 2 + kind) * d + (j < V ? pl.a + j : pl.b + j - V)] = v;
+        for (int j = 0; j < V; ++j) {
+            float lo, hi;
+            f2_unpack(acc[kind][j], lo, hi);
+            for (int m = group; m < 32; m <<= 1) {
+                lo += __shfl_xor_sync(0xffffffffu, lo, m);
+                hi += __shfl_xor_sync(0xffffffffu, hi, m);
+            }
+            if (sub == 0 && pl.active)
+                *reinterpret_cast<float2 *>(sums + (warp * 2 + kind) * d + (j < kPairs ? pl.a + 2 * j : pl.b + 2 * (j - kPairs))) = make_float2(lo, hi);
         }
     }
     __syncthreads();
@@ -259,9 +304,12 @@ int bwd_ctas(int64_t rows)
 template <typename T, int V>
 padoc_status launch_bwd(const BwdArgs &p, bool adjacent, int ctas, padoc_stream_t stream)
 {
-    auto *k = adjacent ? rotary_norm_bwd_kernel<T, V, true> : rotary_norm_bwd_kernel<T, V, false>;
-    const size_t ring = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>), sums = (size_t)kBwdWarps * 2 * p.sp.d * sizeof(float);
-    const int smem = (int)(ring > sums ? ring : sums);
+    // (8 lanes a head: 128 dims in bf16, 64 in fp32)
+    auto *k = p.group_log == 3 ? (adjacent ? rotary_norm_bwd_kernel<T, V, true, 8> : rotary_norm_bwd_kernel<T, V, false, 8>)
+                               : (adjacent ? rotary_norm_bwd_kernel<T, V, true, 0> : rotary_norm_bwd_kernel<T, V, false, 0>);
+    const size_t weights = (size_t)V << p.group_log << 4, ring = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>);
+    const size_t sums = (size_t)kBwdWarps * 2 * p.sp.d * sizeof(float);
+    const int smem = (int)(weights + ring > sums ? weights + ring : sums);
     const padoc_status st = padoc_set_max_smem((const void *)k, smem);
     void *argv[1] = {const_cast<BwdArgs *>(&p)};
     return st != PADOC_OK ? st : launch(k, dim3((unsigned)ctas), 32 * kBwdWarps, smem, stream, argv);

@@ -8,6 +8,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "tc.cuh"
 
 namespace padoc_rotary_dev {
 
@@ -81,6 +82,15 @@ __device__ __forceinline__ void unpack(const Raw<float, 4> &r, float (&x)[4])
 {
     x[0] = r.w.x, x[1] = r.w.y, x[2] = r.w.z, x[3] = r.w.w;
 }
+// The same as packed pairs of fp32 (f2_*: one instruction for two values).
+template <typename T, int V>
+__device__ __forceinline__ void unpack2(const Raw<T, V> &r, uint64_t (&x)[V / 2])
+{
+    float f[V];
+    unpack(r, f);
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) x[j] = f2_pack(f[2 * j], f[2 * j + 1]);
+}
 template <int V, typename T>
 __device__ __forceinline__ void load_vec(const T *p, float (&x)[V])
 {
@@ -100,11 +110,21 @@ __device__ __forceinline__ void store_vec(float *p, const float (&x)[V])
 {
     *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
 }
+template <int V, typename T>
+__device__ __forceinline__ void store_vec2(T *p, const uint64_t (&x)[V / 2])
+{
+    float f[V];
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) f2_unpack(x[j], f[2 * j], f[2 * j + 1]);
+    store_vec<V>(p, f);
+}
 
 // Sum over the `group` lanes (a power of two) that share a head.
 __device__ __forceinline__ float group_sum(float v, int group)
 {
-    for (int m = group >> 1; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1)
+        if (m < group) v += __shfl_xor_sync(0xffffffffu, v, m);
     return v;
 }
 
@@ -143,6 +163,41 @@ __device__ __forceinline__ void turn_pairs(float (&a)[V], float (&b)[V], const f
 #pragma unroll
         for (int j = 0; j < V / 2; ++j) turn(b[2 * j], b[2 * j + 1], c[V / 2 + j], s[V / 2 + j]);
     }
+}
+
+// The same on packed pairs.
+template <int V, bool kAdjacent>
+__device__ __forceinline__ void turn_pairs2(uint64_t (&a)[V / 2], uint64_t (&b)[V / 2], const uint64_t (&c)[V / 2], const uint64_t (&s)[V / 2])
+{
+    if constexpr (!kAdjacent) {
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+            const uint64_t x = f2_sub(f2_mul(a[j], c[j]), f2_mul(b[j], s[j]));
+            b[j] = f2_fma(b[j], c[j], f2_mul(a[j], s[j]));
+            a[j] = x;
+        }
+    } else {
+        float fa[V], fb[V], fc[V], fs[V];
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+            f2_unpack(a[j], fa[2 * j], fa[2 * j + 1]);
+            f2_unpack(b[j], fb[2 * j], fb[2 * j + 1]);
+            f2_unpack(c[j], fc[2 * j], fc[2 * j + 1]);
+            f2_unpack(s[j], fs[2 * j], fs[2 * j + 1]);
+        }
+        turn_pairs<V, true>(fa, fb, fc, fs);
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+            a[j] = f2_pack(fa[2 * j], fa[2 * j + 1]);
+            b[j] = f2_pack(fb[2 * j], fb[2 * j + 1]);
+        }
+    }
+}
+__device__ __forceinline__ float f2_sum(uint64_t v)
+{
+    float lo, hi;
+    f2_unpack(v, lo, hi);
+    return lo + hi;
 }
 
 // RMS norm of a head spread over `group` lanes: x r w with r = 1 / sqrt(mean x^2 + eps), sums in fp32.
