@@ -301,21 +301,27 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int i, int
         const int j = t * kPassRows + sub;
         const bool here = good >> j & 1u;
         const int64_t at = __shfl_sync(0xffffffffu, row, j);
-        unpack(ra[t], xa[t]);
-        unpack(rb[t], xb[t]);
-        if (!is_v) {
+        if (is_v) {
+            unpack(ra[t], xa[t]);
+            unpack(rb[t], xb[t]);
+        } else {
+            uint64_t za[V / 2], zb[V / 2];
+            unpack2(ra[t], za);
+            unpack2(rb[t], zb);
             if constexpr (kNorm) {
-                Place pn = pl;
-                pn.active = here;
-                const float r = norm_scale<V>(xa[t], xb[t], pn, p.sp, kGroup);
-                if (here) scale_head<V>(xa[t], xb[t], r, static_cast<const __nv_bfloat16 *>(p.sp.k_weight), pl);
+                const float r = norm_scale<V>(za, zb, here, p.sp, kGroup);
+                const __nv_bfloat16 *w = static_cast<const __nv_bfloat16 *>(p.sp.k_weight);
+                scale_head<V, __nv_bfloat16>(za, zb, r, load_raw<__nv_bfloat16, V>(w + pl.a), load_raw<__nv_bfloat16, V>(w + pl.b));
             }
             if (here && pl.turned) {
-                float c[V], s[V];
+                uint64_t c[V / 2], s[V / 2];
+                lane_angles<V, true>(p.sp, p.pos, at, chunk, c, s);
+                turn_pairs<V, kAdjacent>(za, zb, c, s);
+            }
 #pragma unroll
-                for (int f = 0; f < V; ++f)
-                    cos_sin<true>(p.sp.freq[chunk * V + f], p.pos + at * p.sp.axes, p.sp, c[f], s[f]);
-                turn_pairs<V, kAdjacent>(xa[t], xb[t], c, s);
+            for (int f = 0; f < V / 2; ++f) {
+                f2_unpack(za[f], xa[t][2 * f], xa[t][2 * f + 1]);
+                f2_unpack(zb[f], xb[t][2 * f], xb[t][2 * f + 1]);
             }
         }
         if (here) {
@@ -359,7 +365,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_rotary_e4m3_kernel(c
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x >= a.kv_ctas) {
         const uint32_t w = (blockIdx.x - a.kv_ctas) * kAppendWarps + warp, i = w / (uint32_t)a.q_parts;
-        if (i < p.count) row_part<__nv_bfloat16, V, kAdjacent, kNorm, kQueries>(p, i, w % (uint32_t)a.q_parts);
+        if (i < p.count) row_part<__nv_bfloat16, V, kAdjacent, kNorm, kQueries, kD / (2 * V)>(p, i, w % (uint32_t)a.q_parts);
         return;
     }
     const uint32_t w = blockIdx.x * kAppendWarps + warp, units = 2u * p.hkv;

@@ -15,13 +15,13 @@ namespace {
 constexpr int kWarps = 4;   // warps per CTA
 
 // See row_part.
-template <typename T, int V, bool kAdjacent, bool kNorm, int kMode>
+template <typename T, int V, bool kAdjacent, bool kNorm, int kMode, int kGroup>
 __global__ void __launch_bounds__(32 * kWarps) rotary_kernel(const __grid_constant__ Args p)
 {
     pdl_wait_prerequisite();
     pdl_launch_dependents();
     const int64_t i = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    if (i < p.count) row_part<T, V, kAdjacent, kNorm, kMode>(p, i, blockIdx.y);
+    if (i < p.count) row_part<T, V, kAdjacent, kNorm, kMode, kGroup>(p, i, blockIdx.y);
 }
 
 constexpr int kBwdWarps = 8;    // warps per CTA of the backward with the norm
@@ -129,16 +129,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     int stage = 0;
     for (int64_t row = first; row < p.rows; row += stride) {
         uint64_t c[kPairs], s[kPairs];
-        if (pl.turned) {
-#pragma unroll
-            for (int j = 0; j < kPairs; ++j) {
-                float c0, c1, s0, s1;
-                cos_sin<sizeof(T) == 2>(p.sp.freq[chunk * V + 2 * j], p.pos + row * p.sp.axes, p.sp, c0, s0);
-                cos_sin<sizeof(T) == 2>(p.sp.freq[chunk * V + 2 * j + 1], p.pos + row * p.sp.axes, p.sp, c1, s1);
-                c[j] = f2_pack(c0, c1);
-                s[j] = f2_pack(s0, s1);
-            }
-        }
+        if (pl.turned) lane_angles<V, sizeof(T) == 2>(p.sp, p.pos, row, chunk, c, s);
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
             const ulonglong2 *w = reinterpret_cast<const ulonglong2 *>(smem_raw) + kind * kPairs * group + chunk;
@@ -164,7 +155,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
                     unpack2(in[32], xb);
                     unpack2(in[64], a);
                     unpack2(in[96], b);
-                    if (pl.turned) turn_pairs2<V, kAdjacent>(a, b, c, s);
+                    if (pl.turned) turn_pairs<V, kAdjacent>(a, b, c, s);
                     uint64_t wa[kPairs], wb[kPairs];
                     read_weights(wa, wb);
                     uint64_t s2 = 0, d2 = 0;
@@ -273,13 +264,20 @@ padoc_status launch(K kernel, dim3 grid, int block, size_t smem, padoc_stream_t 
     return padoc_launch_status();
 }
 
+template <typename T, int V, int kMode, int kGroup>
+padoc_status launch_group(const Args &p, bool adjacent, bool norm, dim3 grid, padoc_stream_t stream)
+{
+    auto *k = adjacent ? (norm ? rotary_kernel<T, V, true, true, kMode, kGroup> : rotary_kernel<T, V, true, false, kMode, kGroup>)
+                       : (norm ? rotary_kernel<T, V, false, true, kMode, kGroup> : rotary_kernel<T, V, false, false, kMode, kGroup>);
+    void *argv[1] = {const_cast<Args *>(&p)};
+    return launch(k, grid, 32 * kWarps, 0, stream, argv);
+}
 template <typename T, int V, int kMode>
 padoc_status launch_rows(const Args &p, bool adjacent, bool norm, dim3 grid, padoc_stream_t stream)
 {
-    auto *k = adjacent ? (norm ? rotary_kernel<T, V, true, true, kMode> : rotary_kernel<T, V, true, false, kMode>)
-                       : (norm ? rotary_kernel<T, V, false, true, kMode> : rotary_kernel<T, V, false, false, kMode>);
-    void *argv[1] = {const_cast<Args *>(&p)};
-    return launch(k, grid, 32 * kWarps, 0, stream, argv);
+    // (8 lanes a head: 128 dims in bf16, 64 in fp32)
+    return p.group_log == 3 ? launch_group<T, V, kMode, 8>(p, adjacent, norm, grid, stream)
+                            : launch_group<T, V, kMode, 0>(p, adjacent, norm, grid, stream);
 }
 
 template <int kMode>

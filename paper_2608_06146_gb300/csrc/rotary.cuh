@@ -145,29 +145,9 @@ __device__ __forceinline__ Place lane_place(int chunk, int d, int rot)
     return p;
 }
 
-// The rotation of a lane's V pairs by its angles.
+// The rotation of a lane's V pairs by its angles; pairs (i, i + R / 2) on packed values, adjacent ones one by one.
 template <int V, bool kAdjacent>
-__device__ __forceinline__ void turn_pairs(float (&a)[V], float (&b)[V], const float (&c)[V], const float (&s)[V])
-{
-    auto turn = [](float &x, float &y, float cc, float ss) {
-        const float x0 = x, y0 = y;
-        x = fmaf(x0, cc, -(y0 * ss));
-        y = fmaf(y0, cc, x0 * ss);
-    };
-    if constexpr (!kAdjacent) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) turn(a[j], b[j], c[j], s[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < V / 2; ++j) turn(a[2 * j], a[2 * j + 1], c[j], s[j]);
-#pragma unroll
-        for (int j = 0; j < V / 2; ++j) turn(b[2 * j], b[2 * j + 1], c[V / 2 + j], s[V / 2 + j]);
-    }
-}
-
-// The same on packed pairs.
-template <int V, bool kAdjacent>
-__device__ __forceinline__ void turn_pairs2(uint64_t (&a)[V / 2], uint64_t (&b)[V / 2], const uint64_t (&c)[V / 2], const uint64_t (&s)[V / 2])
+__device__ __forceinline__ void turn_pairs(uint64_t (&a)[V / 2], uint64_t (&b)[V / 2], const uint64_t (&c)[V / 2], const uint64_t (&s)[V / 2])
 {
     if constexpr (!kAdjacent) {
 #pragma unroll
@@ -185,7 +165,16 @@ __device__ __forceinline__ void turn_pairs2(uint64_t (&a)[V / 2], uint64_t (&b)[
             f2_unpack(c[j], fc[2 * j], fc[2 * j + 1]);
             f2_unpack(s[j], fs[2 * j], fs[2 * j + 1]);
         }
-        turn_pairs<V, true>(fa, fb, fc, fs);
+        auto turn = [](float &x, float &y, float cc, float ss) {
+            const float x0 = x, y0 = y;
+            x = fmaf(x0, cc, -(y0 * ss));
+            y = fmaf(y0, cc, x0 * ss);
+        };
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+            turn(fa[2 * j], fa[2 * j + 1], fc[j], fs[j]);
+            turn(fb[2 * j], fb[2 * j + 1], fc[V / 2 + j], fs[V / 2 + j]);
+        }
 #pragma unroll
         for (int j = 0; j < V / 2; ++j) {
             a[j] = f2_pack(fa[2 * j], fa[2 * j + 1]);
@@ -200,27 +189,42 @@ __device__ __forceinline__ float f2_sum(uint64_t v)
     return lo + hi;
 }
 
-// RMS norm of a head spread over `group` lanes: x r w with r = 1 / sqrt(mean x^2 + eps), sums in fp32.
+// RMS norm of a head spread over `group` lanes: x r w with r = 1 / sqrt(mean x^2 + eps), sums in fp32. `here`:
+// the lane holds dims of a head.
 template <int V>
-__device__ __forceinline__ float norm_scale(const float (&a)[V], const float (&b)[V], const Place &pl, const Spec &sp, int group)
+__device__ __forceinline__ float norm_scale(const uint64_t (&a)[V / 2], const uint64_t (&b)[V / 2], bool here, const Spec &sp, int group)
 {
-    float ss = 0.f;
-    if (pl.active) {
+    uint64_t ss = 0;
 #pragma unroll
-        for (int j = 0; j < V; ++j) ss = fmaf(a[j], a[j], fmaf(b[j], b[j], ss));
-    }
-    return rsqrtf(group_sum(ss, group) / (float)sp.d + sp.eps);
+    for (int j = 0; j < V / 2; ++j) ss = f2_fma(a[j], a[j], f2_fma(b[j], b[j], ss));
+    return rsqrtf(group_sum(here ? f2_sum(ss) : 0.f, group) * (1.f / (float)sp.d) + sp.eps);
 }
 template <int V, typename T>
-__device__ __forceinline__ void scale_head(float (&a)[V], float (&b)[V], float r, const T *w, const Place &pl)
+__device__ __forceinline__ void scale_head(uint64_t (&a)[V / 2], uint64_t (&b)[V / 2], float r, const Raw<T, V> &rwa, const Raw<T, V> &rwb)
 {
-    float wa[V], wb[V];
-    load_vec<V>(w + pl.a, wa);
-    load_vec<V>(w + pl.b, wb);
+    uint64_t wa[V / 2], wb[V / 2];
+    unpack2(rwa, wa);
+    unpack2(rwb, wb);
+    const uint64_t r2 = f2_pack(r, r);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        a[j] *= r * wa[j];
-        b[j] *= r * wb[j];
+    for (int j = 0; j < V / 2; ++j) {
+        a[j] = f2_mul(a[j], f2_mul(r2, wa[j]));
+        b[j] = f2_mul(b[j], f2_mul(r2, wb[j]));
+    }
+}
+
+// The cosines and sines of a lane's V pairs at row `row`, as packed pairs.
+template <int V, bool kFast>
+__device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__restrict__ pos, int64_t row, int chunk, uint64_t (&c)[V / 2], uint64_t (&s)[V / 2])
+{
+    pos += row * sp.axes;
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+        float c0, c1, s0, s1;
+        cos_sin<kFast>(sp.freq[chunk * V + 2 * j], pos, sp, c0, s0);
+        cos_sin<kFast>(sp.freq[chunk * V + 2 * j + 1], pos, sp, c1, s1);
+        c[j] = f2_pack(c0, c1);
+        s[j] = f2_pack(s0, s1);
     }
 }
 
@@ -253,7 +257,8 @@ constexpr int kSteps = 5;   // most steps of a part: the 16 + 2 heads of 128 dim
 // One warp's work: part `part` of row i, p.steps steps of 32 / group heads, at most kSteps. All of the part's loads
 // are issued before its angles are computed. Bound by HBM in large calls: every element is read once and written
 // once.
-template <typename T, int V, bool kAdjacent, bool kNorm, int kMode>
+// kGroup: the lanes that share a head where known at compile time (0: group_log says).
+template <typename T, int V, bool kAdjacent, bool kNorm, int kMode, int kGroup>
 __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
 {
     const int lane = threadIdx.x & 31;
@@ -269,8 +274,8 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
         }
         slot = (uint32_t)at;
     }
-    const int group = 1 << p.group_log, heads = 32 >> p.group_log;
-    const int sub = lane >> p.group_log, chunk = lane & (group - 1);
+    const int group = kGroup ? kGroup : 1 << p.group_log, heads = 32 / group;
+    const int sub = lane / group, chunk = lane & (group - 1);
     const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
     const T *q = static_cast<const T *>(p.q) + row * p.q_stride, *k = static_cast<const T *>(p.k) + row * p.k_stride;
     const int nq = p.q ? p.hq : 0, turned = kMode == kQueries ? nq : nq + p.hkv, total = kMode == kAppend ? turned + p.hkv : turned;
@@ -286,12 +291,8 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
             rb[u] = load_raw<T, V>(src + pl.b);
         }
     }
-    float c[V], s[V];
-    if (pl.turned) {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            cos_sin<sizeof(T) == 2>(p.sp.freq[chunk * V + j], p.pos + row * p.sp.axes, p.sp, c[j], s[j]);
-    }
+    uint64_t c[V / 2], s[V / 2];
+    if (pl.turned) lane_angles<V, sizeof(T) == 2>(p.sp, p.pos, row, chunk, c, s);
     T *q_out = static_cast<T *>(p.q_out) + i * p.q_out_stride;
     // where the row's KV heads go, and the distance from one to the next
     int64_t k_at = 0, k_step = p.sp.d;
@@ -307,21 +308,22 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
         if (u >= p.steps) break;
         const int h = first + u * heads;
         const bool here = h < total && pl.active, is_q = h < nq, is_v = kMode == kAppend && h >= turned;
-        float a[V], b[V];
-        unpack(ra[u], a);
-        unpack(rb[u], b);
+        uint64_t a[V / 2], b[V / 2];
+        unpack2(ra[u], a);
+        unpack2(rb[u], b);
         if constexpr (kNorm) {
-            Place pn = pl;
-            pn.active = here;
-            const float r = norm_scale<V>(a, b, pn, p.sp, group);
-            if (here && !is_v) scale_head<V>(a, b, r, static_cast<const T *>(is_q ? p.sp.q_weight : p.sp.k_weight), pl);
+            const float r = norm_scale<V>(a, b, here, p.sp, group);
+            if (here && !is_v) {
+                const T *w = static_cast<const T *>(is_q ? p.sp.q_weight : p.sp.k_weight);
+                scale_head<V, T>(a, b, r, load_raw<T, V>(w + pl.a), load_raw<T, V>(w + pl.b));
+            }
         }
         if (here) {
             if (pl.turned && !is_v) turn_pairs<V, kAdjacent>(a, b, c, s);
             T *dst = is_q ? q_out + h * p.sp.d : static_cast<T *>(p.k_out) + k_at + (h - nq) * k_step;
             if (is_v) dst = static_cast<T *>(p.v_out) + k_at + (h - turned) * k_step;
-            store_vec<V>(dst + pl.a, a);
-            store_vec<V>(dst + pl.b, b);
+            store_vec2<V>(dst + pl.a, a);
+            store_vec2<V>(dst + pl.b, b);
         }
     }
 }
