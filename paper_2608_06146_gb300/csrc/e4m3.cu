@@ -234,8 +234,8 @@ __device__ __forceinline__ uint2 encode_again(uint2 c, float s_old, const Scale 
 // Rows past the run are left as they are.
 // A warp takes one (K or V, head) of `inputs` inputs, the runs that start among them; a row is spread over the
 // 8 (V = 8) or 16 lanes that share a head in the packed kernel, so a run's 16 rows are 4 (8) passes whose loads are
-// all in flight before the first is used, and stay in registers until the scale is known. Further CTAs lay out the
-// queries. Bound by latency in a step; a 4001-token prefix: 51 us with a row a warp at a time, its runs written by
+// all in flight before the first is used; their values wait in shared memory until the scale is known. Further
+// CTAs lay out the queries. Bound by latency in a step; a 4001-token prefix: 51 us with a row a warp at a time, its runs written by
 // one CTA in 16.
 struct RotaryAppendArgs {
     padoc_rotary_dev::Args rows;   // its k_out and v_out are the codes
@@ -243,25 +243,20 @@ struct RotaryAppendArgs {
     int32_t inputs, kv_ctas, q_parts;
 };
 
+// The run that starts at lane `from`'s input: lane j holds the slot and source row of input first + j (slot -1 past
+// the call's end). z: the warp's staging of 16 rows in fp32, each lane reads back what it wrote.
 template <int V, bool kAdjacent, bool kNorm>
-__device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int i, int unit)
+__device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int32_t slot, int32_t row, int from, int unit, float4 *z)
 {
     using namespace padoc_rotary_dev;
     const Args &p = a.rows;
     constexpr int kGroup = kD / (2 * V), kPassRows = 32 / kGroup, kPasses = kBlk / kPassRows;
     const int lane = threadIdx.x & 31, sub = lane / kGroup, chunk = lane & (kGroup - 1);
-    const int32_t slot = p.slots[i];
-    const int r0 = slot & (kBlk - 1);
-    // lane j looks at input i + j
-    int64_t row = -1;
-    bool in_run = false;
-    if (lane < kBlk - r0 && i + lane < p.count) {
-        in_run = p.slots[i + lane] == slot + lane;
-        if (in_run) row = p.src_rows ? (int64_t)p.src_rows[i + lane] : i + lane;
-    }
-    const uint32_t run_bits = __ballot_sync(0xffffffffu, in_run);
-    const int n = __ffs((int)~run_bits) - 1;   // (at most 16 lanes look)
-    const uint32_t good = __ballot_sync(0xffffffffu, lane < n && row >= 0 && row < p.rows);
+    const int32_t slot0 = __shfl_sync(0xffffffffu, slot, from);
+    const int r0 = slot0 & (kBlk - 1);
+    const uint32_t run = __ballot_sync(0xffffffffu, lane >= from && lane < from + kBlk - r0 && slot == slot0 + (lane - from)) >> from;
+    const int n = __ffs((int)~run) - 1;   // (at most 16)
+    const uint32_t good = __ballot_sync(0xffffffffu, row >= 0 && row < p.rows) >> from & ((1u << n) - 1);
     if (!good) return;
     const bool is_v = unit >= p.hkv;
     const int g = is_v ? unit - p.hkv : unit;
@@ -273,13 +268,13 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int i, int
     for (int t = 0; t < kPasses; ++t) {
         if (t * kPassRows >= n) break;
         const int j = t * kPassRows + sub;
-        const int64_t at = __shfl_sync(0xffffffffu, row, j);
+        const int64_t at = __shfl_sync(0xffffffffu, row, from + j);
         if (good >> j & 1u) {
             ra[t] = load_raw<__nv_bfloat16, V>(src + at * stride + pl.a);
             rb[t] = load_raw<__nv_bfloat16, V>(src + at * stride + pl.b);
         }
     }
-    const int64_t blk = slot / kBlk;
+    const int64_t blk = slot0 / kBlk;
     float *scp = (is_v ? a.v_scales : a.k_scales) + blk * p.hkv + g;
     uint8_t *codes = static_cast<uint8_t *>(is_v ? p.v_out : p.k_out) + (blk * p.hkv + g) * kBlk * kD;
     using Codes = typename Pick<V == 8, uint2, uint32_t>::type;
@@ -293,21 +288,17 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int i, int
         }
     }
     const float s_old = r0 == 0 ? 0.f : *scp;
-    float xa[kPasses][V], xb[kPasses][V];
     float amax = 0.f;
 #pragma unroll
     for (int t = 0; t < kPasses; ++t) {
         if (t * kPassRows >= n) break;
         const int j = t * kPassRows + sub;
         const bool here = good >> j & 1u;
-        const int64_t at = __shfl_sync(0xffffffffu, row, j);
-        if (is_v) {
-            unpack(ra[t], xa[t]);
-            unpack(rb[t], xb[t]);
-        } else {
-            uint64_t za[V / 2], zb[V / 2];
-            unpack2(ra[t], za);
-            unpack2(rb[t], zb);
+        uint64_t za[V / 2], zb[V / 2];
+        unpack2(ra[t], za);
+        unpack2(rb[t], zb);
+        if (!is_v) {
+            const int64_t at = __shfl_sync(0xffffffffu, row, from + j);
             if constexpr (kNorm) {
                 const float r = norm_scale<V>(za, zb, here, p.sp, kGroup);
                 const __nv_bfloat16 *w = static_cast<const __nv_bfloat16 *>(p.sp.k_weight);
@@ -318,15 +309,21 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int i, int
                 lane_angles<V, true>(p.sp, p.pos, at, chunk, c, s);
                 turn_pairs<V, kAdjacent>(za, zb, c, s);
             }
-#pragma unroll
-            for (int f = 0; f < V / 2; ++f) {
-                f2_unpack(za[f], xa[t][2 * f], xa[t][2 * f + 1]);
-                f2_unpack(zb[f], xb[t][2 * f], xb[t][2 * f + 1]);
-            }
         }
         if (here) {
+            float xa[V], xb[V];
 #pragma unroll
-            for (int f = 0; f < V; ++f) amax = fmaxf(amax, fmaxf(fabsf(xa[t][f]), fabsf(xb[t][f])));
+            for (int f = 0; f < V / 2; ++f) {
+                f2_unpack(za[f], xa[2 * f], xa[2 * f + 1]);
+                f2_unpack(zb[f], xb[2 * f], xb[2 * f + 1]);
+            }
+#pragma unroll
+            for (int f = 0; f < V; ++f) amax = fmaxf(amax, fmaxf(fabsf(xa[f]), fabsf(xb[f])));
+#pragma unroll
+            for (int f = 0; f < V / 4; ++f) {
+                z[(t * V / 2 + f) * 32] = make_float4(xa[4 * f], xa[4 * f + 1], xa[4 * f + 2], xa[4 * f + 3]);
+                z[(t * V / 2 + V / 4 + f) * 32] = make_float4(xb[4 * f], xb[4 * f + 1], xb[4 * f + 2], xb[4 * f + 3]);
+            }
         }
     }
     const float cand = __fdiv_rn(warp_max(amax), 448.f);
@@ -340,14 +337,19 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int i, int
                 *reinterpret_cast<Codes *>(dst + pl.b) = encode_again(ob[t], s_old, sc);
             }
     }
-#pragma unroll
-    for (int t = 0; t < kPasses; ++t) {
-        if (t * kPassRows >= n) break;
+#pragma unroll 1
+    for (int t = 0; t * kPassRows < n; ++t) {
         const int j = t * kPassRows + sub;
         if (good >> j & 1u) {
             uint8_t *dst = codes + (r0 + j) * kD;
-            *reinterpret_cast<Codes *>(dst + pl.a) = encode(xa[t], sc);
-            *reinterpret_cast<Codes *>(dst + pl.b) = encode(xb[t], sc);
+            float x[V];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                for (int f = 0; f < V / 4; ++f)
+                    *reinterpret_cast<float4 *>(x + 4 * f) = z[(t * V / 2 + half * (V / 4) + f) * 32];
+                *reinterpret_cast<Codes *>(dst + (half ? pl.b : pl.a)) = encode(x, sc);
+            }
         }
     }
     __syncwarp();   // every lane has read the old scale before it is replaced
@@ -355,10 +357,11 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int i, int
 }
 
 template <int V, bool kAdjacent, bool kNorm>
-__global__ void __launch_bounds__(32 * kAppendWarps) append_rotary_e4m3_kernel(const __grid_constant__ RotaryAppendArgs a)
+__global__ void __launch_bounds__(32 * kAppendWarps, 5) append_rotary_e4m3_kernel(const __grid_constant__ RotaryAppendArgs a)
 {
     using namespace padoc_rotary_dev;
     const Args &p = a.rows;
+    __shared__ float4 staging[kAppendWarps][kBlk * kD / 4];
     // a programmatic dependent of the previous kernel in the stream, as the plain append
     pdl_wait_prerequisite();
     pdl_launch_dependents();
@@ -372,19 +375,19 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_rotary_e4m3_kernel(c
     const int unit = (int)(w % units);
     const int64_t first = (int64_t)(w / units) * a.inputs;
     if (first >= p.count) return;
-    // lane j looks at input first + j: a run starts where the slot does not continue the one before
+    // lane j looks at input first + j, as far as a run of the warp's inputs can reach; a run starts where the slot
+    // does not continue the one before
     const int64_t i = first + lane;
-    const bool mine = lane < a.inputs && i < p.count;
-    const int32_t slot = mine ? p.slots[i] : -1;
+    const bool looks = lane < a.inputs + kBlk - 1 && i < p.count;
+    const int32_t slot = looks ? p.slots[i] : -1, row = !looks ? -1 : p.src_rows ? p.src_rows[i] : (int32_t)i;
     int32_t before = __shfl_up_sync(0xffffffffu, slot, 1);
     if (lane == 0) before = first > 0 ? p.slots[first - 1] : -1;
-    const bool slot_ok = slot >= 0 && slot < p.pool_slots;
-    if (mine && unit == 0) {
-        const int32_t row = p.src_rows ? p.src_rows[i] : 0;
-        if (!slot_ok || row < 0 || row >= p.rows) padoc_record_error(p.err, PADOC_DEVERR_BLOCK_ID, slot_ok ? row : slot);
-    }
+    const bool mine = looks && lane < a.inputs, slot_ok = slot >= 0 && slot < p.pool_slots;
+    if (mine && unit == 0 && (!slot_ok || row < 0 || row >= p.rows))
+        padoc_record_error(p.err, PADOC_DEVERR_BLOCK_ID, slot_ok ? row : slot);
     uint32_t starts = __ballot_sync(0xffffffffu, mine && slot_ok && ((slot & (kBlk - 1)) == 0 || (int64_t)before + 1 != slot));
-    for (; starts; starts &= starts - 1) append_run<V, kAdjacent, kNorm>(a, (int)first + __ffs((int)starts) - 1, unit);
+    for (; starts; starts &= starts - 1)
+        append_run<V, kAdjacent, kNorm>(a, slot, row, __ffs((int)starts) - 1, unit, staging[warp] + lane);
 }
 
 template <int V>
@@ -508,7 +511,7 @@ extern "C" padoc_status padoc_append_rotary_inputs_e4m3(const padoc_kv_pool_e4m3
     const int vec = vec_of(rot, in->dtype);
     // inputs a warp looks through for runs: one in small calls; up to 16 (a block's rows, so a prefix's warps find one
     // run each) once there are more than 16 warps an SM
-    const int64_t units = 2 * (int64_t)p.hkv, many = count * units / ((int64_t)padoc_num_sms() * 16);
+    const int64_t units = 2 * (int64_t)p.hkv, many = count * units / ((int64_t)padoc_default_ctas() * 16);
     a.inputs = (int)(many < 1 ? 1 : many > kBlk ? kBlk : many);
     const int64_t kv_ctas = ((count + a.inputs - 1) / a.inputs * units + kAppendWarps - 1) / kAppendWarps;
     a.q_parts = p.q ? split_rows(p, vec, p.hq) : 0;

@@ -332,7 +332,7 @@ int split_rows(Args &p, int vec, int heads_total)
     p.group_log = group_log_of(p.sp.d, vec);
     const int heads = 32 >> p.group_log;
     const int steps = (heads_total + heads - 1) / heads, least = (steps + kSteps - 1) / kSteps;
-    const int64_t want = (int64_t)padoc_num_sms() * 16 / p.count;
+    const int64_t want = ((int64_t)padoc_default_ctas() * 8 + p.count - 1) / p.count;
     const int parts = want < least ? least : want > steps ? steps : (int)want;
     p.steps = (steps + parts - 1) / parts;
     return (steps + p.steps - 1) / p.steps;

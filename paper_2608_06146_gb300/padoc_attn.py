@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -110,6 +111,11 @@ class padoc_qkv_rows(ctypes.Structure):
                 ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("pos", ctypes.c_void_p),
                 ("rows", ctypes.c_int64), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("dtype", ctypes.c_int)]
+
+
+# packed in one call: a third of what building the ctypes structure field by field takes
+_QKV_ROWS = struct.Struct("@3P3qPq3i4x")
+assert _QKV_ROWS.size == ctypes.sizeof(padoc_qkv_rows)
 
 
 class padoc_grid(ctypes.Structure):
@@ -863,10 +869,10 @@ def padoc_mpd_launch_step_rotary(step: padoc_mpd_step, stage, dev_ints, pool: pa
     """padoc_mpd_launch_step with padoc_append_rotary_inputs as its append: k_src / v_src / q_src as there
     (row strides allowed), pos int32 [rows][axes]."""
     lib = load_library()
-    rows = rotary.rows(pos, k_src, q_src, v_src)
+    rows = rotary.rows(pos, k_src, q_src, v_src)[0]
     st = lib.padoc_mpd_launch_step_rotary(ctypes.byref(step), None if stage is None else stage.data_ptr(),
                                           _dev(dev_ints, "dev_ints"), dev_ints.numel(), ctypes.byref(pool), rotary.ref,
-                                          ctypes.byref(rows), _dev(q_dst, "q_dst"), float(scale), _dev(out, "out"),
+                                          rows, _dev(q_dst, "q_dst"), float(scale), _dev(out, "out"),
                                           _dev(lse, "lse"), _dev(workspace, "workspace"),
                                           workspace.numel() * workspace.element_size(), _stream_ptr(stream))
     _check("padoc_mpd_launch_step_rotary", st)
@@ -1007,8 +1013,8 @@ class MpdRunner:
 
 def make_kv_pool(k_pool, v_pool) -> padoc_kv_pool:
     """padoc_kv_pool over pool tensors [num_blocks][Hkv][16][d] (the caller keeps them alive)."""
-    return padoc_kv_pool(_dev(k_pool, "k_pool"), _dev(v_pool, "v_pool"), k_pool.shape[0], k_pool.shape[2],
-                         k_pool.shape[1], k_pool.shape[3], _dtype_code(k_pool))
+    nb, hkv, bs, d = k_pool.shape
+    return padoc_kv_pool(_dev(k_pool, "k_pool"), _dev(v_pool, "v_pool"), nb, bs, hkv, d, _dtype_code(k_pool))
 
 
 class E4M3Pool:
@@ -1139,7 +1145,7 @@ class Rotary:
         self.q_weight, self.k_weight = q_weight, k_weight
         self.dtype = None
         self._codes = {torch.bfloat16: PADOC_DTYPE_BF16, torch.float32: PADOC_DTYPE_F32}
-        self._int32 = torch.int32
+        self._int32, self._f32 = torch.int32, torch.float32
         for w in (q_weight, k_weight):
             if w is None:
                 continue
@@ -1152,47 +1158,49 @@ class Rotary:
                               head_dim, 2 * table.size, num_axes, int(bool(adjacent)), eps, amplitude)
         self.ref = ctypes.byref(self.c)
 
-    def positions(self, pos):
-        if pos.dtype is not self._int32 or pos.dim() != 2 or pos.shape[1] != self.num_axes:
-            raise ValueError("pos must be int32 [rows][axes]")
+    def positions(self, pos, rows=None):
+        """Address of pos int32 [rows][axes]."""
+        n, axes = pos.shape
+        if pos.dtype is not self._int32 or axes != self.num_axes or (rows is not None and n != rows):
+            raise ValueError("pos must be int32 [rows][axes], a position for each row")
         return _dev(pos, "pos")
 
-    def heads(self, t, name, rows=None, dtype=None):
+    def heads(self, t, name, rows, dtype):
         """(address, row stride, heads) of a CUDA tensor [rows][heads][head_dim] whose rows may lie apart."""
-        sh, st = t.shape, t.stride()
-        if not t.is_cuda or len(sh) != 3 or sh[2] != self.head_dim or st[2] != 1 or (st[1] != sh[2] and sh[1] > 1):
+        n, h, d = t.shape
+        s0, s1, s2 = t.stride()
+        if d != self.head_dim or s2 != 1 or (s1 != d and h > 1) or not t.is_cuda:
             raise ValueError(f"{name} must be a CUDA tensor [rows][heads][head_dim] with contiguous rows")
-        if (rows is not None and sh[0] != rows) or (dtype is not None and t.dtype is not dtype):
+        if n != rows or t.dtype is not dtype:
             raise ValueError(f"{name} must have the other tensors' rows and dtype")
-        width = sh[1] * sh[2]
-        return t.data_ptr(), (st[0] if sh[0] > 1 else width), sh[1]
+        return t.data_ptr(), (s0 if n > 1 else h * d), h
 
-    def rows(self, pos, k, q=None, v=None) -> padoc_qkv_rows:
-        """padoc_qkv_rows over q / k / v [rows][heads][head_dim] and pos int32 [rows][axes]."""
+    def rows(self, pos, k, q=None, v=None):
+        """(a padoc_qkv_rows over q / k / v [rows][heads][head_dim] and pos int32 [rows][axes], as bytes; rows;
+        query heads; KV heads)."""
         n, dt = k.shape[0], k.dtype
         code = self._codes.get(dt)
         if code is None or (self.dtype is not None and dt is not self.dtype):
             raise TypeError("rows must be bfloat16 or float32, of the norm weights' dtype")
-        if pos.shape[0] != n:
-            raise ValueError("pos must have a position for each row")
         kp, ks, hkv = self.heads(k, "k", n, dt)
-        qp, qs, hq = self.heads(q, "q", n, dt) if q is not None else (None, 0, 0)
-        vp, vs, hv = self.heads(v, "v", n, dt) if v is not None else (None, 0, hkv)
+        qp, qs, hq = self.heads(q, "q", n, dt) if q is not None else (0, 0, 0)
+        vp, vs, hv = self.heads(v, "v", n, dt) if v is not None else (0, 0, hkv)
         if hv != hkv:
             raise ValueError("v must have k's heads")
-        return padoc_qkv_rows(qp, kp, vp, qs, ks, vs, self.positions(pos), n, hq, hkv, code)
+        return _QKV_ROWS.pack(qp, kp, vp, qs, ks, vs, self.positions(pos, n), n, hq, hkv, code), n, hq, hkv
 
 
 def padoc_qk_rotary(rotary: Rotary, q, k, pos, q_out, k_out, stream=None):
     """Norm and rotation of packed rows: q [rows][Hq][d], k [rows][Hkv][d] (rows may lie apart, as slices of a
     fused projection do), pos int32 [rows][axes] into q_out, k_out (the inputs themselves are allowed)."""
     lib = load_library()
-    rows = rotary.rows(pos, k, q)
-    qp, qs, hq = rotary.heads(q_out, "q_out", rows.rows, k.dtype)
-    kp, ks, hkv = rotary.heads(k_out, "k_out", rows.rows, k.dtype)
-    if hq != rows.num_q_heads or hkv != rows.num_kv_heads:
+    rows, n, hq, hkv = rotary.rows(pos, k, q)
+    dt = k.dtype
+    qp, qs, qh = rotary.heads(q_out, "q_out", n, dt)
+    kp, ks, kh = rotary.heads(k_out, "k_out", n, dt)
+    if qh != hq or kh != hkv:
         raise ValueError("q_out and k_out must have q's and k's heads")
-    _check("padoc_qk_rotary", lib.padoc_qk_rotary(rotary.ref, ctypes.byref(rows), qp, qs, kp, ks, _stream_ptr(stream)))
+    _check("padoc_qk_rotary", lib.padoc_qk_rotary(rotary.ref, rows, qp, qs, kp, ks, _stream_ptr(stream)))
 
 
 def padoc_qk_rotary_bwd_workspace_size(rotary: Rotary, rows: int) -> int:
@@ -1210,39 +1218,47 @@ def padoc_qk_rotary_bwd(rotary: Rotary, dq_out, dk_out, pos, dq, dk, q=None, k=N
     tensor of padoc_qk_rotary_bwd_workspace_size bytes) are needed."""
     lib = load_library()
     norm = rotary.q_weight is not None
-    up = rotary.rows(pos, dk_out, dq_out)
-    rows = up
+    n, dt = dk_out.shape[0], dk_out.dtype
+    uq, uqs, hq = rotary.heads(dq_out, "dq_out", n, dt)
+    uk, uks, hkv = rotary.heads(dk_out, "dk_out", n, dt)
     if norm:
         if q is None or k is None or dq_weight is None or dk_weight is None:
             raise ValueError("the norm's backward needs q, k, dq_weight and dk_weight")
-        rows = rotary.rows(pos, k, q)
-        if rows.num_q_heads != up.num_q_heads or rows.num_kv_heads != up.num_kv_heads or rows.dtype != up.dtype:
+        rows, xn, xq, xk = rotary.rows(pos, k, q)
+        if xn != n or xq != hq or xk != hkv or k.dtype is not dt:
             raise ValueError("dq_out and dk_out must be like q and k")
         for w in (dq_weight, dk_weight):
-            if tuple(w.shape) != (rotary.head_dim,) or w.element_size() != 4 or not w.is_floating_point():
+            if w.dtype is not rotary._f32 or w.shape != (rotary.head_dim,):
                 raise ValueError("dq_weight and dk_weight must be float32 [head_dim]")
-    qp, qs, hq = rotary.heads(dq, "dq", up.rows, dk_out.dtype)
-    kp, ks, hkv = rotary.heads(dk, "dk", up.rows, dk_out.dtype)
-    if hq != up.num_q_heads or hkv != up.num_kv_heads:
+    else:
+        rows = rotary.rows(pos, dk_out, dq_out)[0]
+    qp, qs, qh = rotary.heads(dq, "dq", n, dt)
+    kp, ks, kh = rotary.heads(dk, "dk", n, dt)
+    if qh != hq or kh != hkv:
         raise ValueError("dq and dk must have the gradients' heads")
     ws, wsb = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel() * workspace.element_size())
-    st = lib.padoc_qk_rotary_bwd(rotary.ref, ctypes.byref(rows), up.q, up.q_stride, up.k, up.k_stride, qp, qs, kp, ks,
-                                 _dev(dq_weight, "dq_weight"), _dev(dk_weight, "dk_weight"), ws, wsb, _stream_ptr(stream))
+    st = lib.padoc_qk_rotary_bwd(rotary.ref, rows, uq, uqs, uk, uks, qp, qs, kp, ks, _dev(dq_weight, "dq_weight"),
+                                 _dev(dk_weight, "dk_weight"), ws, wsb, _stream_ptr(stream))
     _check("padoc_qk_rotary_bwd", st)
 
 
 def _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count):
-    rows = rotary.rows(pos, k_src, q_src, v_src)
+    rows, n_rows, hq, _ = rotary.rows(pos, k_src, q_src, v_src)
     n = slots.shape[0] if count is None else count
-    for t, nm in ((slots, "slots"), (src_rows, "src_rows")):
-        if t is not None and (t.dtype is not rotary._int32 or t.numel() < n):
-            raise ValueError(f"{nm} must be int32 [count]")
-    if src_rows is None and n > rows.rows:
-        raise ValueError("more slots than rows")
+    i32 = rotary._int32
+    if slots.dtype is not i32 or slots.numel() < n:
+        raise ValueError("slots must be int32 [count]")
+    if src_rows is None:
+        if n > n_rows:
+            raise ValueError("more slots than rows")
+    elif src_rows.dtype is not i32 or src_rows.numel() < n:
+        raise ValueError("src_rows must be int32 [count]")
     dst = None
     if q_src is not None:
-        if q_dst is None or q_dst.dtype is not k_src.dtype or tuple(q_dst.shape[1:]) != tuple(q_src.shape[1:]) or \
-                q_dst.shape[0] < n:
+        if q_dst is None:
+            raise ValueError("queries need q_dst")
+        dn, dh, dd = q_dst.shape
+        if dn < n or dh != hq or dd != rotary.head_dim or q_dst.dtype is not k_src.dtype:
             raise ValueError("q_dst must be [count][Hq][d] in the rows' dtype")
         dst = _dev(q_dst, "q_dst")
     return rows, dst, _dev(src_rows, "src_rows"), _dev(slots, "slots"), n
@@ -1253,10 +1269,12 @@ def padoc_append_rotary_inputs(rotary: Rotary, k_pool, v_pool, k_src, v_src, pos
     """padoc_append_inputs with the norm and the rotation on the way (sources' rows may lie apart; pos int32
     [rows][axes] by source row)."""
     lib = load_library()
+    if v_pool.shape != k_pool.shape or v_pool.dtype is not k_pool.dtype:
+        raise ValueError("k_pool and v_pool must be alike")
     pool = make_kv_pool(k_pool, v_pool)
     rows, dst, sr, sl, n = _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count)
     _check("padoc_append_rotary_inputs",
-           lib.padoc_append_rotary_inputs(ctypes.byref(pool), rotary.ref, ctypes.byref(rows), dst, sr, sl, n,
+           lib.padoc_append_rotary_inputs(ctypes.byref(pool), rotary.ref, rows, dst, sr, sl, n,
                                           _stream_ptr(stream)))
 
 
@@ -1267,7 +1285,7 @@ def padoc_append_rotary_inputs_e4m3(rotary: Rotary, pool: E4M3Pool, k_src, v_src
     lib = load_library()
     rows, dst, sr, sl, n = _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count)
     _check("padoc_append_rotary_inputs_e4m3",
-           lib.padoc_append_rotary_inputs_e4m3(ctypes.byref(pool.c), rotary.ref, ctypes.byref(rows), dst, sr, sl, n,
+           lib.padoc_append_rotary_inputs_e4m3(ctypes.byref(pool.c), rotary.ref, rows, dst, sr, sl, n,
                                                _stream_ptr(stream)))
 
 
@@ -1279,6 +1297,8 @@ class KvPools:
     """The layers' pools of a cache, marshalled once: (k_pool, v_pool) tensors [num_blocks][Hkv][16][d] each."""
 
     def __init__(self, pools):
+        import torch
+        self._int32 = torch.int32
         self.tensors = [tuple(p) for p in pools]
         self.c = (padoc_kv_pool * max(len(self.tensors), 1))(*[make_kv_pool(k, v) for k, v in self.tensors])
         for k, v in self.tensors:
@@ -1293,6 +1313,8 @@ class KvPoolsE4M3:
     """The layers' E4M3 pools: E4M3Pool objects or (k_codes, v_codes, k_scales, v_scales) tensors."""
 
     def __init__(self, pools):
+        import torch
+        self._int32 = torch.int32
         self.pools = [p if isinstance(p, E4M3Pool) else E4M3Pool.over(*p) for p in pools]
         self.c = (padoc_kv_pool_e4m3 * max(len(self.pools), 1))(*[p.c for p in self.pools])
 
@@ -1300,28 +1322,30 @@ class KvPoolsE4M3:
         return len(self.pools)
 
 
-def _copy_blocks(name, pools, src_blocks, dst_blocks, src_pools, count, stream):
+def _copy_blocks(f, name, pools, src_blocks, dst_blocks, src_pools, count, stream):
     src = pools if src_pools is None else src_pools
-    if len(src) != len(pools):
+    layers = len(pools)
+    if len(src) != layers:
         raise ValueError("as many source pools as destination pools")
     n = src_blocks.shape[0] if count is None else count
-    for t in (src_blocks, dst_blocks):
-        if t.element_size() != 4 or t.is_floating_point() or t.numel() < n:
-            raise ValueError("src_blocks and dst_blocks must be int32 [count]")
-    _check(name, getattr(load_library(), name)(pools.c, src.c, len(pools), _dev(src_blocks, "src_blocks"),
-                                               _dev(dst_blocks, "dst_blocks"), n, _stream_ptr(stream)))
+    i32 = pools._int32
+    if src_blocks.dtype is not i32 or dst_blocks.dtype is not i32 or src_blocks.numel() < n or dst_blocks.numel() < n:
+        raise ValueError("src_blocks and dst_blocks must be int32 [count]")
+    _check(name, f(pools.c, src.c, layers, _dev(src_blocks, "src_blocks"), _dev(dst_blocks, "dst_blocks"), n,
+                   _stream_ptr(stream)))
 
 
 def padoc_copy_kv_blocks(pools: KvPools, src_blocks, dst_blocks, src_pools: Optional[KvPools] = None, count=None,
                          stream=None):
     """Blocks src_blocks[i] to dst_blocks[i] (int32 CUDA tensors) in every pool, from src_pools where given."""
-    _copy_blocks("padoc_copy_kv_blocks", pools, src_blocks, dst_blocks, src_pools, count, stream)
+    _copy_blocks(load_library().padoc_copy_kv_blocks, "padoc_copy_kv_blocks", pools, src_blocks, dst_blocks, src_pools, count, stream)
 
 
 def padoc_copy_kv_blocks_e4m3(pools: KvPoolsE4M3, src_blocks, dst_blocks, src_pools: Optional[KvPoolsE4M3] = None,
                               count=None, stream=None):
     """padoc_copy_kv_blocks for E4M3 pools (codes and scales)."""
-    _copy_blocks("padoc_copy_kv_blocks_e4m3", pools, src_blocks, dst_blocks, src_pools, count, stream)
+    _copy_blocks(load_library().padoc_copy_kv_blocks_e4m3, "padoc_copy_kv_blocks_e4m3", pools, src_blocks, dst_blocks,
+                 src_pools, count, stream)
 
 
 # ------------------------------------------------------------------------------------------------
