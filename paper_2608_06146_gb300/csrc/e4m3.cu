@@ -306,7 +306,7 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int32_t sl
             }
             if (here && pl.turned) {
                 uint64_t c[V / 2], s[V / 2];
-                lane_angles<V, true>(p.sp, p.pos, at, chunk, c, s);
+                lane_angles<V, true, 0>(p.sp, p.pos, at, chunk, true, c, s);   // (a row a group: nothing to share)
                 turn_pairs<V, kAdjacent>(za, zb, c, s);
             }
         }

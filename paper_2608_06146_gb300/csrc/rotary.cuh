@@ -128,7 +128,8 @@ __device__ __forceinline__ float group_sum(float v, int group)
     return v;
 }
 
-// A lane's place in a head: its chunk, the element offsets of its two vectors, whether its dims are rotated.
+// A lane's place in a head: the element offsets of its two vectors, whether they exist (else the offsets are 0) and
+// are rotated.
 struct Place {
     int a, b;
     bool active, turned;
@@ -142,6 +143,7 @@ __device__ __forceinline__ Place lane_place(int chunk, int d, int rot)
     const bool split = !kAdjacent && p.turned;
     p.a = split ? chunk * V : chunk * 2 * V;
     p.b = split ? rot / 2 + chunk * V : chunk * 2 * V + V;
+    if (!p.active) p.a = p.b = 0;
     return p;
 }
 
@@ -213,18 +215,38 @@ __device__ __forceinline__ void scale_head(uint64_t (&a)[V / 2], uint64_t (&b)[V
     }
 }
 
-// The cosines and sines of a lane's V pairs at row `row`, as packed pairs.
-template <int V, bool kFast>
-__device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__restrict__ pos, int64_t row, int chunk, uint64_t (&c)[V / 2], uint64_t (&s)[V / 2])
+// The cosines and sines of a lane's V pairs at row `row`, as packed pairs; for the whole warp. The lanes that hold
+// the same chunk of different heads share the work (kGroup lanes a head, where known at compile time): each
+// computes V kGroup / 32 of the pairs and hands them to the others.
+template <int V, bool kFast, int kGroup>
+__device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__restrict__ pos, int64_t row, int chunk, bool turned,
+                                            uint64_t (&c)[V / 2], uint64_t (&s)[V / 2])
 {
     pos += row * sp.axes;
+    float cj[V], sj[V];
+    if constexpr (kGroup != 0 && kGroup * V >= 32) {
+        constexpr int kOwn = kGroup * V / 32;
+        const int lane = threadIdx.x & 31;
+        float co[kOwn], so[kOwn];
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) {
+            co[j] = so[j] = 0.f;
+            if (turned) cos_sin<kFast>(sp.freq[chunk * V + lane / kGroup * kOwn + j], pos, sp, co[j], so[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int from = j / kOwn * kGroup + chunk;
+            cj[j] = __shfl_sync(0xffffffffu, co[j % kOwn], from);
+            sj[j] = __shfl_sync(0xffffffffu, so[j % kOwn], from);
+        }
+    } else if (turned) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) cos_sin<kFast>(sp.freq[chunk * V + j], pos, sp, cj[j], sj[j]);
+    }
 #pragma unroll
     for (int j = 0; j < V / 2; ++j) {
-        float c0, c1, s0, s1;
-        cos_sin<kFast>(sp.freq[chunk * V + 2 * j], pos, sp, c0, s0);
-        cos_sin<kFast>(sp.freq[chunk * V + 2 * j + 1], pos, sp, c1, s1);
-        c[j] = f2_pack(c0, c1);
-        s[j] = f2_pack(s0, s1);
+        c[j] = f2_pack(cj[2 * j], cj[2 * j + 1]);
+        s[j] = f2_pack(sj[2 * j], sj[2 * j + 1]);
     }
 }
 
@@ -279,20 +301,21 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
     const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
     const T *q = static_cast<const T *>(p.q) + row * p.q_stride, *k = static_cast<const T *>(p.k) + row * p.k_stride;
     const int nq = p.q ? p.hq : 0, turned = kMode == kQueries ? nq : nq + p.hkv, total = kMode == kAppend ? turned + p.hkv : turned;
-    const int first = part * p.steps * heads + sub;
+    const int first = part * p.steps * heads;
+    // Lanes past the last head or the head's dims load what another lane does and store nothing: the loop has no
+    // divergent branch but the stores'.
     Raw<T, V> ra[kSteps], rb[kSteps];
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
-        const int h = first + u * heads;
-        if (u < p.steps && h < total && pl.active) {
-            const T *src = h < nq ? q + h * p.sp.d : k + (h - nq) * p.sp.d;
-            if (kMode == kAppend && h >= turned) src = static_cast<const T *>(p.v) + row * p.v_stride + (h - turned) * p.sp.d;
-            ra[u] = load_raw<T, V>(src + pl.a);
-            rb[u] = load_raw<T, V>(src + pl.b);
-        }
+        if (u >= p.steps) break;
+        const int h = min(first + u * heads + sub, total - 1);
+        const T *src = h < nq ? q + h * p.sp.d : k + (h - nq) * p.sp.d;
+        if (kMode == kAppend && h >= turned) src = static_cast<const T *>(p.v) + row * p.v_stride + (h - turned) * p.sp.d;
+        ra[u] = load_raw<T, V>(src + pl.a);
+        rb[u] = load_raw<T, V>(src + pl.b);
     }
     uint64_t c[V / 2], s[V / 2];
-    if (pl.turned) lane_angles<V, sizeof(T) == 2>(p.sp, p.pos, row, chunk, c, s);
+    lane_angles<V, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, chunk, pl.turned, c, s);
     T *q_out = static_cast<T *>(p.q_out) + i * p.q_out_stride;
     // where the row's KV heads go, and the distance from one to the next
     int64_t k_at = 0, k_step = p.sp.d;
@@ -303,25 +326,32 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
     } else if constexpr (kMode == kPacked) {
         k_at = i * p.k_out_stride;
     }
+    const bool whole = p.sp.rot == p.sp.d;
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
         if (u >= p.steps) break;
-        const int h = first + u * heads;
-        const bool here = h < total && pl.active, is_q = h < nq, is_v = kMode == kAppend && h >= turned;
+        const int h = first + u * heads + sub;
+        const bool here = h < total && pl.active, is_q = h < nq;
+        if (kMode == kAppend && h >= turned) {   // a value head: as it is
+            if (here) {
+                T *dst = static_cast<T *>(p.v_out) + k_at + (h - turned) * k_step;
+                *reinterpret_cast<Raw<T, V> *>(dst + pl.a) = ra[u];
+                *reinterpret_cast<Raw<T, V> *>(dst + pl.b) = rb[u];
+            }
+        }
+        if (kMode == kAppend && first + u * heads >= turned) continue;   // (the whole step)
         uint64_t a[V / 2], b[V / 2];
         unpack2(ra[u], a);
         unpack2(rb[u], b);
         if constexpr (kNorm) {
-            const float r = norm_scale<V>(a, b, here, p.sp, group);
-            if (here && !is_v) {
-                const T *w = static_cast<const T *>(is_q ? p.sp.q_weight : p.sp.k_weight);
-                scale_head<V, T>(a, b, r, load_raw<T, V>(w + pl.a), load_raw<T, V>(w + pl.b));
-            }
+            const float r = norm_scale<V>(a, b, pl.active, p.sp, group);
+            const T *w = static_cast<const T *>(is_q ? p.sp.q_weight : p.sp.k_weight);
+            scale_head<V, T>(a, b, r, load_raw<T, V>(w + pl.a), load_raw<T, V>(w + pl.b));
         }
-        if (here) {
-            if (pl.turned && !is_v) turn_pairs<V, kAdjacent>(a, b, c, s);
+        if (whole) turn_pairs<V, kAdjacent>(a, b, c, s);
+        else if (pl.turned) turn_pairs<V, kAdjacent>(a, b, c, s);
+        if (here && h < turned) {
             T *dst = is_q ? q_out + h * p.sp.d : static_cast<T *>(p.k_out) + k_at + (h - nq) * k_step;
-            if (is_v) dst = static_cast<T *>(p.v_out) + k_at + (h - turned) * k_step;
             store_vec2<V>(dst + pl.a, a);
             store_vec2<V>(dst + pl.b, b);
         }
