@@ -41,11 +41,12 @@ struct BwdArgs {
     float *part;                            // [CTAs][2][d]
 };
 
+// A vector of 16 or 8 bytes; bytes 0 writes zeros and reads nothing.
 template <int kBytes>
-__device__ __forceinline__ void cp_async_vec(uint32_t dst, const void *src)
+__device__ __forceinline__ void cp_async_vec(uint32_t dst, const void *src, uint32_t bytes)
 {
-    if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+    if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
 // The backward with the norm. A warp per row, rows in a grid-wide stride, 32 / group heads a step. Registers hold
@@ -69,50 +70,52 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     const int group = kGroup ? kGroup : 1 << p.group_log, heads = 32 / group;
     const int sub = lane / group, chunk = lane & (group - 1);
     const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
-    const int d = p.sp.d, q_steps = (p.hq + heads - 1) / heads, steps = q_steps + (p.hkv + heads - 1) / heads;
+    const int d = p.sp.d;
     Vec *ring = reinterpret_cast<Vec *>(smem_raw + 2 * kPairs * group) + (size_t)warp * kBwdStages * 4 * 32 + lane;
     pdl_wait_prerequisite();
     pdl_launch_dependents();
     for (int e = threadIdx.x; e < 2 * kPairs * group; e += 32 * kBwdWarps) {
         const int kind = e >= kPairs * group, piece = e / group - kind * kPairs;
         const Place at = lane_place<V, kAdjacent>(e & (group - 1), d, p.sp.rot);
-        if (!at.active) continue;
-        const T *w = static_cast<const T *>(kind ? p.sp.k_weight : p.sp.q_weight) +
-                     (piece < kPairs / 2 ? at.a + 4 * piece : at.b + 4 * (piece - kPairs / 2));
-        reinterpret_cast<float4 *>(smem_raw)[e] = make_float4((float)w[0], (float)w[1], (float)w[2], (float)w[3]);
+        float4 w4 = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at.active) {
+            const T *w = static_cast<const T *>(kind ? p.sp.k_weight : p.sp.q_weight) +
+                         (piece < kPairs / 2 ? at.a + 4 * piece : at.b + 4 * (piece - kPairs / 2));
+            w4 = make_float4((float)w[0], (float)w[1], (float)w[2], (float)w[3]);
+        }
+        reinterpret_cast<float4 *>(smem_raw)[e] = w4;
     }
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * kBwdWarps + warp, stride = (int64_t)gridDim.x * kBwdWarps;
 
-    // the next step to be copied: its row, step and addresses (of the lane's first vectors), and its stage
+    // the next step to be copied: its row, its kind's heads from it on, its addresses (of the lane's first vectors),
+    // and its stage; lanes without a head there get zeros
     int64_t ahead_row = first;
-    int ahead_step = 0;
+    bool ahead_k = false;
+    int ahead_left = p.hq;
     uint32_t ahead_at = smem_u32(ring);
     const uint32_t ring_end = ahead_at + kBwdStages * 4 * 32 * (uint32_t)sizeof(Vec);
-    const int lane_at = sub * d + pl.a, to_b = pl.b - pl.a;
-    const T *ax = nullptr, *ag = nullptr;
+    const int lane_at = sub * d + pl.a, to_b = pl.b - pl.a, step_at = heads * d;
+    const T *ax = static_cast<const T *>(p.q) + first * p.q_stride + lane_at;
+    const T *ag = static_cast<const T *>(p.dq_out) + first * p.dq_out_stride + lane_at;
     auto copy_ahead = [&]() {
         if (ahead_row < p.rows) {
-            if (ahead_step == 0) {
-                ax = static_cast<const T *>(p.q) + ahead_row * p.q_stride + lane_at;
-                ag = static_cast<const T *>(p.dq_out) + ahead_row * p.dq_out_stride + lane_at;
-            } else if (ahead_step == q_steps) {
-                ax = static_cast<const T *>(p.k) + ahead_row * p.k_stride + lane_at;
-                ag = static_cast<const T *>(p.dk_out) + ahead_row * p.dk_out_stride + lane_at;
-            }
-            const int left = ahead_step < q_steps ? p.hq - ahead_step * heads : p.hkv - (ahead_step - q_steps) * heads;
-            if (pl.active && sub < left) {
-                constexpr uint32_t kNext = 32 * sizeof(Vec);
-                cp_async_vec<sizeof(Vec)>(ahead_at, ax);
-                cp_async_vec<sizeof(Vec)>(ahead_at + kNext, ax + to_b);
-                cp_async_vec<sizeof(Vec)>(ahead_at + 2 * kNext, ag);
-                cp_async_vec<sizeof(Vec)>(ahead_at + 3 * kNext, ag + to_b);
-            }
-            ax += heads * d;
-            ag += heads * d;
-            if (++ahead_step == steps) {
-                ahead_step = 0;
-                ahead_row += stride;
+            constexpr uint32_t kNext = 32 * sizeof(Vec);
+            const uint32_t bytes = pl.active && sub < ahead_left ? (uint32_t)sizeof(Vec) : 0u;
+            cp_async_vec<sizeof(Vec)>(ahead_at, ax, bytes);
+            cp_async_vec<sizeof(Vec)>(ahead_at + kNext, ax + to_b, bytes);
+            cp_async_vec<sizeof(Vec)>(ahead_at + 2 * kNext, ag, bytes);
+            cp_async_vec<sizeof(Vec)>(ahead_at + 3 * kNext, ag + to_b, bytes);
+            ax += step_at;
+            ag += step_at;
+            ahead_left -= heads;
+            if (ahead_left <= 0) {   // on to the row's key heads, or to the next row's query heads
+                ahead_k = !ahead_k;
+                ahead_row += ahead_k ? 0 : stride;
+                ahead_left = ahead_k ? p.hkv : p.hq;
+                ax = (ahead_k ? static_cast<const T *>(p.k) + ahead_row * p.k_stride : static_cast<const T *>(p.q) + ahead_row * p.q_stride) + lane_at;
+                ag = (ahead_k ? static_cast<const T *>(p.dk_out) + ahead_row * p.dk_out_stride
+                              : static_cast<const T *>(p.dq_out) + ahead_row * p.dq_out_stride) + lane_at;
             }
         }
         cp_async_commit();
@@ -123,6 +126,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     for (int j = 0; j < kBwdStages; ++j) copy_ahead();
 
     const float inv_d = 1.f / (float)d;
+    const bool whole = p.sp.rot == d;
     uint64_t acc[2][V];   // sums of g h: the pairs of the lane's first, then of its second vector
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[0][j] = acc[1][j] = 0;
@@ -148,40 +152,35 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
                 cp_async_wait<kBwdStages - 1>();
                 const bool here = sub < left && pl.active;
                 const Vec *in = ring + stage * 4 * 32;
-                uint64_t xa[kPairs], xb[kPairs], a[kPairs], b[kPairs];
-                float ss = 0.f, dot = 0.f;
-                if (here) {
-                    unpack2(in[0], xa);
-                    unpack2(in[32], xb);
-                    unpack2(in[64], a);
-                    unpack2(in[96], b);
-                    if (pl.turned) turn_pairs<V, kAdjacent>(a, b, c, s);
-                    uint64_t wa[kPairs], wb[kPairs];
-                    read_weights(wa, wb);
-                    uint64_t s2 = 0, d2 = 0;
+                uint64_t xa[kPairs], xb[kPairs], a[kPairs], b[kPairs], wa[kPairs], wb[kPairs];
+                unpack2(in[0], xa);
+                unpack2(in[32], xb);
+                unpack2(in[64], a);
+                unpack2(in[96], b);
+                if (whole) turn_pairs<V, kAdjacent>(a, b, c, s);
+                else if (pl.turned) turn_pairs<V, kAdjacent>(a, b, c, s);
+                read_weights(wa, wb);
+                uint64_t s2 = 0, d2 = 0;
 #pragma unroll
-                    for (int j = 0; j < kPairs; ++j) {
-                        s2 = f2_fma(xa[j], xa[j], f2_fma(xb[j], xb[j], s2));
-                        d2 = f2_fma(f2_mul(a[j], wa[j]), xa[j], f2_fma(f2_mul(b[j], wb[j]), xb[j], d2));
-                    }
-                    ss = f2_sum(s2);
-                    dot = f2_sum(d2);
+                for (int j = 0; j < kPairs; ++j) {
+                    s2 = f2_fma(xa[j], xa[j], f2_fma(xb[j], xb[j], s2));
+                    d2 = f2_fma(f2_mul(a[j], wa[j]), xa[j], f2_fma(f2_mul(b[j], wb[j]), xb[j], d2));
                 }
-                const float r = rsqrtf(group_sum(ss, group) * inv_d + p.sp.eps);
-                const float m = group_sum(dot, group) * r * inv_d;   // the mean of w g h
-                if (here) {
-                    // dx = r (w g - h m) with h = x r
-                    const uint64_t r2 = f2_pack(r, r), m2 = f2_pack(-m, -m);
-                    uint64_t wa[kPairs], wb[kPairs];
-                    read_weights(wa, wb);
+                float r = rsqrtf(group_sum(f2_sum(s2), group) * inv_d + p.sp.eps);
+                if (sub >= left) r = 0.f;   // no head: its zeros must not meet an infinite scale
+                const float m = group_sum(f2_sum(d2), group) * r * inv_d;   // the mean of w g h
+                // dx = r (w g - h m) with h = x r
+                const uint64_t r2 = f2_pack(r, r), m2 = f2_pack(-m, -m);
+                read_weights(wa, wb);
 #pragma unroll
-                    for (int j = 0; j < kPairs; ++j) {
-                        const uint64_t ha = f2_mul(xa[j], r2), hb = f2_mul(xb[j], r2);
-                        acc[kind][j] = f2_fma(a[j], ha, acc[kind][j]);
-                        acc[kind][kPairs + j] = f2_fma(b[j], hb, acc[kind][kPairs + j]);
-                        a[j] = f2_mul(r2, f2_fma(ha, m2, f2_mul(a[j], wa[j])));
-                        b[j] = f2_mul(r2, f2_fma(hb, m2, f2_mul(b[j], wb[j])));
-                    }
+                for (int j = 0; j < kPairs; ++j) {
+                    const uint64_t ha = f2_mul(xa[j], r2), hb = f2_mul(xb[j], r2);
+                    acc[kind][j] = f2_fma(a[j], ha, acc[kind][j]);
+                    acc[kind][kPairs + j] = f2_fma(b[j], hb, acc[kind][kPairs + j]);
+                    a[j] = f2_mul(r2, f2_fma(ha, m2, f2_mul(a[j], wa[j])));
+                    b[j] = f2_mul(r2, f2_fma(hb, m2, f2_mul(b[j], wb[j])));
+                }
+                if (here) {
                     store_vec2<V>(out, a);
                     store_vec2<V>(out + to_b, b);
                 }
