@@ -14,9 +14,12 @@ namespace {
 
 constexpr int kWarps = 4;   // warps per CTA
 
-// See row_part.
-template <typename T, int V, bool kAdjacent, bool kNorm, int kMode, int kGroup>
-__global__ void __launch_bounds__(32 * kWarps) rotary_kernel(const __grid_constant__ Args p)
+// See row_part. kCtas: CTAs an SM that the registers have to allow. With the norm a row's steps take longer than its
+// loads, so many rows want more warps on an SM than the compiler's own choice gives (92 registers, 5 CTAs), even at a
+// few spilled values; few rows want the loads first. 16 + 2 heads of 128 dims in bf16, own choice / 7 CTAs: 2500
+// rows 5.3 / 7.0 us, 5000 12.0 / 12.6, 10000 19.6 / 19.4, 32768 51.5 / 49.5. Without the norm 46.0 / 51.7.
+template <typename T, int V, bool kAdjacent, bool kNorm, int kMode, int kGroup, int kCtas>
+__global__ void __launch_bounds__(32 * kWarps, kCtas) rotary_kernel(const __grid_constant__ Args p)
 {
     pdl_wait_prerequisite();
     pdl_launch_dependents();
@@ -25,7 +28,7 @@ __global__ void __launch_bounds__(32 * kWarps) rotary_kernel(const __grid_consta
 }
 
 constexpr int kBwdWarps = 8;    // warps per CTA of the backward with the norm
-constexpr int kBwdStages = 4;   // steps of a warp whose loads are in flight
+constexpr int kBwdStages = 3;   // steps of a warp whose loads are in flight (2: 80.9, 3: 79.3, 4: 79.9, 6: 84.9 us for 32768 rows)
 
 struct BwdArgs {
     Spec sp;                                // turns back
@@ -215,22 +218,31 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     }
 }
 
-// Column sums of the CTAs' partial rows: 32 columns a CTA, eight warps that take the rows in turn.
-__global__ void __launch_bounds__(256) rotary_weight_grad_kernel(const float *__restrict__ part, int n, int d, float *dqw, float *dkw)
+// Column sums of the CTAs' partial rows: 32 columns a CTA, a warp takes every 32nd row and has eight of them in
+// flight (with 8 warps and a load at a time the 304 rows of the largest grid took 6 us).
+constexpr int kSumWarps = 32;
+__global__ void __launch_bounds__(32 * kSumWarps) rotary_weight_grad_kernel(const float *__restrict__ part, int n, int d, float *dqw, float *dkw)
 {
-    __shared__ float sums[8][32];
+    __shared__ float sums[kSumWarps][32];
     pdl_wait_prerequisite();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     float v = 0.f;
-    if (col < 2 * d)
-        for (int r = warp; r < n; r += 8) v += part[(int64_t)r * 2 * d + col];
+    for (int r0 = warp; r0 < n; r0 += 8 * kSumWarps) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = r0 + j * kSumWarps;
+            x[j] = r < n && col < 2 * d ? part[(int64_t)r * 2 * d + col] : 0.f;
+        }
+        v += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    }
     sums[warp][lane] = v;
     __syncthreads();
     if (warp == 0 && col < 2 * d) {
         float t = 0.f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) t += sums[w][lane];
+        for (int w = 0; w < kSumWarps; ++w) t += sums[w][lane];
         (col < d ? dqw[col] : dkw[col - d]) = t;
     }
 }
@@ -266,8 +278,11 @@ padoc_status launch(K kernel, dim3 grid, int block, size_t smem, padoc_stream_t 
 template <typename T, int V, int kMode, int kGroup>
 padoc_status launch_group(const Args &p, bool adjacent, bool norm, dim3 grid, padoc_stream_t stream)
 {
-    auto *k = adjacent ? (norm ? rotary_kernel<T, V, true, true, kMode, kGroup> : rotary_kernel<T, V, true, false, kMode, kGroup>)
-                       : (norm ? rotary_kernel<T, V, false, true, kMode, kGroup> : rotary_kernel<T, V, false, false, kMode, kGroup>);
+    auto *k = adjacent ? (norm ? rotary_kernel<T, V, true, true, kMode, kGroup, 1> : rotary_kernel<T, V, true, false, kMode, kGroup, 1>)
+                       : (norm ? rotary_kernel<T, V, false, true, kMode, kGroup, 1> : rotary_kernel<T, V, false, false, kMode, kGroup, 1>);
+    if constexpr (kMode == kPacked && V == 8)
+        if (norm && (int64_t)grid.x * grid.y * kWarps >= 64 * (int64_t)padoc_default_ctas())   // 64 warps an SM
+            k = adjacent ? rotary_kernel<T, V, true, true, kMode, kGroup, 7> : rotary_kernel<T, V, false, true, kMode, kGroup, 7>;
     void *argv[1] = {const_cast<Args *>(&p)};
     return launch(k, grid, 32 * kWarps, 0, stream, argv);
 }
@@ -531,5 +546,5 @@ extern "C" padoc_status padoc_qk_rotary_bwd(const padoc_rotary *rot, const padoc
     const float *part = (const float *)workspace;
     int n = ctas, dim = d;
     void *argv[5] = {&part, &n, &dim, &dq_weight, &dk_weight};
-    return launch(rotary_weight_grad_kernel, dim3((unsigned)((2 * d + 31) / 32)), 256, 0, stream, argv);
+    return launch(rotary_weight_grad_kernel, dim3((unsigned)((2 * d + 31) / 32)), 32 * kSumWarps, 0, stream, argv);
 }
