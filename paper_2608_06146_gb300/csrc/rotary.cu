@@ -172,16 +172,16 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
                 float r = rsqrtf(group_sum(f2_sum(s2), group) * inv_d + p.sp.eps);
                 if (sub >= left) r = 0.f;   // no head: its zeros must not meet an infinite scale
                 const float m = group_sum(f2_sum(d2), group) * r * inv_d;   // the mean of w g h
-                // dx = r (w g - h m) with h = x r
-                const uint64_t r2 = f2_pack(r, r), m2 = f2_pack(-m, -m);
+                // with t = r g: dw += t x, dx = r (w g - h m) = w t - (r r m) x
+                const uint64_t r2 = f2_pack(r, r), c2 = f2_pack(-(r * r) * m, -(r * r) * m);
                 read_weights(wa, wb);
 #pragma unroll
                 for (int j = 0; j < kPairs; ++j) {
-                    const uint64_t ha = f2_mul(xa[j], r2), hb = f2_mul(xb[j], r2);
-                    acc[kind][j] = f2_fma(a[j], ha, acc[kind][j]);
-                    acc[kind][kPairs + j] = f2_fma(b[j], hb, acc[kind][kPairs + j]);
-                    a[j] = f2_mul(r2, f2_fma(ha, m2, f2_mul(a[j], wa[j])));
-                    b[j] = f2_mul(r2, f2_fma(hb, m2, f2_mul(b[j], wb[j])));
+                    const uint64_t ta = f2_mul(a[j], r2), tb = f2_mul(b[j], r2);
+                    acc[kind][j] = f2_fma(ta, xa[j], acc[kind][j]);
+                    acc[kind][kPairs + j] = f2_fma(tb, xb[j], acc[kind][kPairs + j]);
+                    a[j] = f2_fma(ta, wa[j], f2_mul(xa[j], c2));
+                    b[j] = f2_fma(tb, wb[j], f2_mul(xb[j], c2));
                 }
                 if (here) {
                     store_vec2<V>(out, a);

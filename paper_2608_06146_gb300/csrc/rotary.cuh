@@ -239,9 +239,12 @@ __device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__res
             cj[j] = __shfl_sync(0xffffffffu, co[j % kOwn], from);
             sj[j] = __shfl_sync(0xffffffffu, so[j % kOwn], from);
         }
-    } else if (turned) {
+    } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) cos_sin<kFast>(sp.freq[chunk * V + j], pos, sp, cj[j], sj[j]);
+        for (int j = 0; j < V; ++j) {
+            cj[j] = sj[j] = 0.f;   // (lanes past the head's dims take part in the arithmetic: their values must be finite)
+            if (turned) cos_sin<kFast>(sp.freq[chunk * V + j], pos, sp, cj[j], sj[j]);
+        }
     }
 #pragma unroll
     for (int j = 0; j < V / 2; ++j) {
