@@ -52,14 +52,14 @@ __device__ __forceinline__ void cp_async_vec(uint32_t dst, const void *src, uint
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-// The backward with the norm. A warp per row, rows in a grid-wide stride, 32 / group heads a step. Registers hold
+// The backward with the norm. Persistent CTAs, a warp per row, 32 / group heads a step. Registers hold
 // the weights' gradient sums and the angles, so the rows' values come through shared memory: every lane copies its
 // own vectors kBwdStages steps ahead (cp.async) and reads them back itself, without a barrier. A CTA joins its
 // warps' sums in a fixed order and writes one partial row, which rotary_weight_grad_kernel adds up (no atomics:
-// the same call gives the same bits). Arithmetic is on packed pairs, weights come from shared memory in fp32: the
-// kernel is bound by issued instructions as much as by HBM. The packed batch of 32768 rows (453 MB): 276 us with
-// plain loads, one step at a time, at 178 registers; 115 us through the ring with scalar arithmetic (2620
-// instructions a row).
+// the same call gives the same bits). Arithmetic is on packed pairs, weights come from shared memory in fp32.
+// The packed batch of 32768 rows (453 MB): 276 us with plain loads, one step at a time, at 178 registers; 115 us
+// through the ring with scalar arithmetic (2620 instructions a row); 76.8 us now (1390; 87% of the copy rate), bound
+// by the latency of a step's chain (two sums over the head) at the 16 warps an SM that the sums' registers leave.
 // kGroup: the lanes that share a head where known at compile time (0: group_log says).
 template <typename T, int V, bool kAdjacent, int kGroup>
 __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(const __grid_constant__ BwdArgs p)
@@ -89,7 +89,8 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
         reinterpret_cast<float4 *>(smem_raw)[e] = w4;
     }
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kBwdWarps + warp, stride = (int64_t)gridDim.x * kBwdWarps;
+    // a CTA's rows lie behind one another (a grid apart they take 79.4 us instead of 76.8 for 32768 rows)
+    const int64_t first = p.rows * blockIdx.x / gridDim.x + warp, row_end = p.rows * (blockIdx.x + 1) / gridDim.x;
 
     // the next step to be copied: its row, its kind's heads from it on, its addresses (of the lane's first vectors),
     // and its stage; lanes without a head there get zeros
@@ -102,7 +103,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     const T *ax = static_cast<const T *>(p.q) + first * p.q_stride + lane_at;
     const T *ag = static_cast<const T *>(p.dq_out) + first * p.dq_out_stride + lane_at;
     auto copy_ahead = [&]() {
-        if (ahead_row < p.rows) {
+        if (ahead_row < row_end) {
             constexpr uint32_t kNext = 32 * sizeof(Vec);
             const uint32_t bytes = pl.active && sub < ahead_left ? (uint32_t)sizeof(Vec) : 0u;
             cp_async_vec<sizeof(Vec)>(ahead_at, ax, bytes);
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
             ahead_left -= heads;
             if (ahead_left <= 0) {   // on to the row's key heads, or to the next row's query heads
                 ahead_k = !ahead_k;
-                ahead_row += ahead_k ? 0 : stride;
+                ahead_row += ahead_k ? 0 : kBwdWarps;
                 ahead_left = ahead_k ? p.hkv : p.hq;
                 ax = (ahead_k ? static_cast<const T *>(p.k) + ahead_row * p.k_stride : static_cast<const T *>(p.q) + ahead_row * p.q_stride) + lane_at;
                 ag = (ahead_k ? static_cast<const T *>(p.dk_out) + ahead_row * p.dk_out_stride
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[0][j] = acc[1][j] = 0;
     int stage = 0;
-    for (int64_t row = first; row < p.rows; row += stride) {
+    for (int64_t row = first; row < row_end; row += kBwdWarps) {
         uint64_t c[kPairs], s[kPairs];
         lane_angles<V, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, chunk, pl.turned, c, s);
 #pragma unroll

@@ -1160,6 +1160,8 @@ class Rotary:
 
     def positions(self, pos, rows=None):
         """Address of pos int32 [rows][axes]."""
+        if pos is None:
+            raise ValueError("rotary needs pos")
         n, axes = pos.shape
         if pos.dtype is not self._int32 or axes != self.num_axes or (rows is not None and n != rows):
             raise ValueError("pos must be int32 [rows][axes], a position for each row")

@@ -112,6 +112,9 @@ SHAPES = [
     (F32, 23, 2, 2, 256, 128, 2, False, True, 0),
     (F32, 23, 3, 1, 40, 24, 2, True, False, 0),
     (F32, 2500, 1, 1, 8, 8, 1, False, True, 0),
+    (BF16, 10001, 16, 2, 128, 128, 3, False, True, 0),
+    (BF16, 9990, 7, 1, 128, 64, 2, True, True, 0),
+    (F32, 70001, 1, 1, 64, 64, 2, False, True, 0),
 ]
 ids = lambda s: f"{'bf16' if s[0] is BF16 else 'f32'}-{s[1]}x{s[2]}+{s[3]}x{s[4]}-r{s[5]}-a{s[6]}{'-adj' if s[7] else ''}{'-norm' if s[8] else ''}"
 
@@ -417,13 +420,13 @@ def runs(rng, kind, nb):
     return np.array(out, np.int32)
 
 
+@pytest.mark.parametrize("nb", [23, 260])     # (from some 1200 inputs on a warp looks through several)
 @pytest.mark.parametrize("kind", ["step", "prefix", "chunks"])
 @pytest.mark.parametrize("hq,hkv,rot,axes,adjacent,norm", [(16, 2, 128, 3, False, True), (8, 1, 64, 1, False, False),
                                                              (10, 5, 128, 2, True, True), (16, 2, 24, 3, True, False)])
-def test_append_e4m3(kind, hq, hkv, rot, axes, adjacent, norm):
+def test_append_e4m3(kind, hq, hkv, rot, axes, adjacent, norm, nb):
     rng = np.random.default_rng(hq + rot)
     sp = Spec(rot, 128, rot, axes, adjacent, norm, BF16)
-    nb = 23
     slots = runs(rng, kind, nb)
     n = len(slots)
     rows = n + 4
@@ -474,13 +477,19 @@ def test_append_e4m3(kind, hq, hkv, rot, axes, adjacent, norm):
             np.testing.assert_array_equal(kc[b, g, rest], before[0][b, g, rest])
 
 
-def test_append_e4m3_without_angles_equals_the_plain_append():
-    # all positions 0, no norm: K goes in as it is, so single rows give the plain append's bits
+@pytest.mark.parametrize("special", [False, True])
+def test_append_e4m3_without_angles_equals_the_plain_append(special):
+    # all positions 0, no norm: K goes in as it is, so single rows give the plain append's bits. special: infinities, NaN and
+    # subnormals in V
     rng = np.random.default_rng(14)
     sp = Spec(14, 128, 128, 3, False, False, BF16)
     nb = 40
     slots = runs(rng, "step", nb)
-    _, q, k, v = qkv(rng, len(slots), 16, 2, 128, BF16, 2.0)
+    x, q, k, v = qkv(rng, len(slots), 16, 2, 128, BF16, 2.0)
+    if special:
+        v[3, 0, 7], v[4, 1, 100], v[5, 0, 0] = float("inf"), float("nan"), -float("inf")
+        v[6] = float("nan")
+        v[7, 1, 3:9] = 1e-40
     pos = torch.zeros((len(slots), 3), dtype=torch.int32, device=DEV)
     a = stale_pool(rng, nb, 2)
     b = pa.E4M3Pool.over(*(t.clone() for t in (a.k_codes, a.v_codes, a.k_scales, a.v_scales)))
