@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kThreads) copy_blocks_kernel(const __grid_cons
     uint4 x[kPiece];
 #pragma unroll
     for (int j = 0; j < kPiece; ++j)
-        if (first + 32 * j < p.vecs) x[j] = __ldcs(src + 32 * j);
+        if (first + 32 * j < p.vecs) x[j] = src[32 * j];
     if (part == 0)
         for (int i = lane; i < p.scales; i += 32)
             p.dst_scales[blockIdx.y][(int64_t)d * p.scales + i] = p.src_scales[blockIdx.y][(int64_t)s * p.scales + i];
