@@ -514,7 +514,7 @@ extern "C" padoc_status padoc_append_rotary_inputs_e4m3(const padoc_kv_pool_e4m3
     const int64_t units = 2 * (int64_t)p.hkv, many = count * units / ((int64_t)padoc_default_ctas() * 16);
     a.inputs = (int)(many < 1 ? 1 : many > kBlk ? kBlk : many);
     const int64_t kv_ctas = ((count + a.inputs - 1) / a.inputs * units + kAppendWarps - 1) / kAppendWarps;
-    a.q_parts = p.q ? split_rows(p, vec, p.hq) : 0;
+    a.q_parts = p.q ? split_rows(p, vec, p.hq, steps_of(kQueries)) : 0;
     const int64_t q_ctas = ((int64_t)count * a.q_parts + kAppendWarps - 1) / kAppendWarps;
     if (kv_ctas > (INT32_MAX >> 2) || q_ctas > (INT32_MAX >> 3)) return PADOC_ERR_UNSUPPORTED;   // (32-bit warp numbers)
     a.kv_ctas = (int32_t)kv_ctas;

@@ -279,8 +279,8 @@ padoc_status launch(K kernel, dim3 grid, int block, size_t smem, padoc_stream_t 
 template <typename T, int V, int kMode, int kGroup>
 padoc_status launch_group(const Args &p, bool adjacent, bool norm, dim3 grid, padoc_stream_t stream)
 {
-    auto *k = adjacent ? (norm ? rotary_kernel<T, V, true, true, kMode, kGroup, 1> : rotary_kernel<T, V, true, false, kMode, kGroup, 1>)
-                       : (norm ? rotary_kernel<T, V, false, true, kMode, kGroup, 1> : rotary_kernel<T, V, false, false, kMode, kGroup, 1>);
+    auto *k = adjacent ? (norm ? rotary_kernel<T, V, true, true, kMode, kGroup, kMode == kAppend ? 7 : 1> : rotary_kernel<T, V, true, false, kMode, kGroup, kMode == kAppend ? 7 : 1>)
+                       : (norm ? rotary_kernel<T, V, false, true, kMode, kGroup, kMode == kAppend ? 7 : 1> : rotary_kernel<T, V, false, false, kMode, kGroup, kMode == kAppend ? 7 : 1>);
     if constexpr (kMode == kPacked && V == 8)
         if (norm && (int64_t)grid.x * grid.y * kWarps >= 64 * (int64_t)padoc_default_ctas())   // 64 warps an SM
             k = adjacent ? rotary_kernel<T, V, true, true, kMode, kGroup, 7> : rotary_kernel<T, V, false, true, kMode, kGroup, 7>;
@@ -299,7 +299,7 @@ template <int kMode>
 padoc_status launch_any(Args &p, const padoc_rotary *rot, padoc_dtype dtype, padoc_stream_t stream)
 {
     const int vec = vec_of(rot, dtype);
-    const int parts = split_rows(p, vec, (p.q ? p.hq : 0) + (kMode == kAppend ? 2 : 1) * p.hkv);
+    const int parts = split_rows(p, vec, (p.q ? p.hq : 0) + (kMode == kAppend ? 2 : 1) * p.hkv, steps_of(kMode));
     const dim3 grid((unsigned)((p.count + kWarps - 1) / kWarps), (unsigned)parts);
     const bool adj = rot->adjacent != 0, norm = rot->q_weight != nullptr;
     if (dtype == PADOC_DTYPE_F32) return launch_rows<float, 4, kMode>(p, adj, norm, grid, stream);
@@ -342,11 +342,11 @@ int group_log_of(int head_dim, int vec)
     return g;
 }
 
-int split_rows(Args &p, int vec, int heads_total)
+int split_rows(Args &p, int vec, int heads_total, int most_steps)
 {
     p.group_log = group_log_of(p.sp.d, vec);
     const int heads = 32 >> p.group_log;
-    const int steps = (heads_total + heads - 1) / heads, least = (steps + kSteps - 1) / kSteps;
+    const int steps = (heads_total + heads - 1) / heads, least = (steps + most_steps - 1) / most_steps;
     const int64_t want = ((int64_t)padoc_default_ctas() * 8 + p.count - 1) / p.count;
     const int parts = want < least ? least : want > steps ? steps : (int)want;
     p.steps = (steps + parts - 1) / parts;

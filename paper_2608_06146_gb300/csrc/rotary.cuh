@@ -24,19 +24,19 @@ struct Spec {
 // turn per position unit as a 64-bit integer, its axis in the two lowest bits; times a 32-bit position it
 // wraps modulo a whole turn, so the angle of a position a million tokens away is as exact as that of the
 // first ones (its fraction is cut at 2^-32 of a turn; a product in fp32 would be off by 0.06 rad at 10^6).
-__device__ __forceinline__ float half_turns(uint64_t f, const int32_t *__restrict__ pos)
+__device__ __forceinline__ float half_turns(uint64_t f, const int32_t *__restrict__ pos, int32_t axes)
 {
-    const int32_t p = pos[f & 3u];
+    const int32_t p = pos[min((int32_t)(f & 3u), axes - 1)];   // (a table of more axes than the rows have stays in the row)
     const int32_t t = (int32_t)(((f & ~(uint64_t)3) * (uint64_t)(int64_t)p) >> 32);
     return (float)t * 0x1p-31f;   // in [-1, 1): the angle is pi times this
 }
-// kFast (outputs of 16 bits): the hardware's sine and cosine, 2^-20.5 off at most on [-pi, pi], 2^-12 of
-// the half step that the output is rounded by; else CUDA's sincospif, within 2 units of the last place, which takes
-// some 40 instructions more a pair: a quarter of the packed forward's time when bf16 rows took it too.
+// kFast (outputs of 16 bits or fewer): the hardware's sine and cosine, 2^-20.5 off at most on [-pi, pi], 2^-12 of
+// the half step that a bf16 output is rounded by; else CUDA's sincospif, within 2 units of the last place, which takes
+// some 40 instructions more a pair.
 template <bool kFast>
 __device__ __forceinline__ void cos_sin(uint64_t f, const int32_t *__restrict__ pos, const Spec &sp, float &c, float &s)
 {
-    const float t = half_turns(f, pos);
+    const float t = half_turns(f, pos, sp.axes);
     if constexpr (kFast) __sincosf(t * 3.14159265358979f, &s, &c);
     else sincospif(t, &s, &c);
     c *= sp.cos_amplitude;
@@ -277,7 +277,11 @@ struct Args {
 // to row i of q_out); or writes an append's query heads only.
 enum { kPacked = 0, kAppend = 1, kQueries = 2 };
 
-constexpr int kSteps = 5;   // most steps of a part: the 16 + 2 heads of 128 dims in bf16, four at a time
+// Most steps of a part. 5: the 16 + 2 heads of 128 dims in bf16, four at a time, in one part. An append's rows are
+// few and its loads wait for their row number: two parts on more warps an SM hide more of it. Own choice of registers
+// and 5 steps / 7 CTAs an SM and 3 steps, with the norm: one row 2.2 / 2.4 us, 672 rows 3.9 / 3.7, 2000 5.2 / 5.6, 4001
+// 12.7 / 11.5; without it 672 3.3 / 2.8, 4001 10.6 / 9.4.
+constexpr int steps_of(int mode) { return mode == kAppend ? 3 : 5; }
 
 // One warp's work: part `part` of row i, p.steps steps of 32 / group heads, at most kSteps. All of the part's loads
 // are issued before its angles are computed. Bound by HBM in large calls: every element is read once and written
@@ -286,6 +290,7 @@ constexpr int kSteps = 5;   // most steps of a part: the 16 + 2 heads of 128 dim
 template <typename T, int V, bool kAdjacent, bool kNorm, int kMode, int kGroup>
 __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
 {
+    constexpr int kSteps = steps_of(kMode);
     const int lane = threadIdx.x & 31;
     int64_t row = i;
     uint32_t slot = 0;
@@ -366,10 +371,10 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
 int vec_of(const padoc_rotary *rot, padoc_dtype dtype);
 // log2 of the lanes that share a head.
 int group_log_of(int head_dim, int vec);
-// Sets group_log and steps; returns the parts of a row: as few as kSteps allows when the rows give every SM 8 warps,
-// else as many as it takes to have them (672 rows of 20 heads: 3.9 us in two parts, 4.6 in one, 4.3 in three; 2617
-// rows: 5.4 in one, 5.6 in two; one row: 2.3 in five, 3.9 in one).
-int split_rows(Args &p, int vec, int heads_total);
+// Sets group_log and steps; returns the parts of a row: as few as most_steps allows when the rows give every SM 8 warps,
+// else as many as it takes to have them (at 5 steps a part, 672 rows of 20 heads: 3.9 us in two parts, 4.6 in one,
+// 4.3 in three; 2617 rows: 5.4 in one, 5.6 in two; one row: 2.3 in five, 3.9 in one).
+int split_rows(Args &p, int vec, int heads_total, int most_steps);
 
 // Host checks of a padoc_rotary (defined in rotary.cu), and its device form.
 padoc_status check_spec(const padoc_rotary *rot);

@@ -244,6 +244,79 @@ def test_positions_past_24_bits():
     check(qo, want, size, FWD + 1e-6, "q")
 
 
+def test_a_table_of_more_axes_reads_the_last_one():
+    # three axes in the table, one in the rows: every pair takes that one, nothing past a row is read
+    sp = Spec(7, 64, 64, 3, False, False, BF16)
+    rng = np.random.default_rng(7)
+    pos = positions(rng, 5, 1)
+    _, q, k, _ = qkv(rng, 5, 2, 1, 64, BF16)
+    sp.dev.c.num_axes = sp.dev.num_axes = 1
+    qo, ko = torch.empty((5, 2, 64), dtype=BF16, device=DEV), torch.empty((5, 1, 64), dtype=BF16, device=DEV)
+    pa.padoc_qk_rotary(sp.dev, q, k, pos, qo, ko)
+    sp.axis = 0 * sp.axis
+    check(qo, *sp.forward(q, None, pos), FWD, "q")
+    check(ko, *sp.forward(k, None, pos), FWD, "k")
+
+
+@pytest.mark.parametrize("what", ["dtype", "pos", "heads", "strides", "cpu", "weights", "slots", "expand", "align"])
+def test_python_refusals(what):
+    sp = Spec(1, 64, 64, 1, False, True, BF16)
+    q, k = torch.zeros((4, 2, 64), dtype=BF16, device=DEV), torch.zeros((4, 1, 64), dtype=BF16, device=DEV)
+    pos = torch.zeros((4, 1), dtype=torch.int32, device=DEV)
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    run = lambda q=q, k=k, pos=pos, qo=qo, ko=ko: pa.padoc_qk_rotary(sp.dev, q, k, pos, qo, ko)
+    run()
+    if what == "dtype":
+        for bad in (dict(q=q.float(), k=k.float()), dict(q=q.half(), k=k.half()), dict(qo=qo.float()), dict(k=k.float())):
+            with pytest.raises((TypeError, ValueError)):
+                run(**bad)
+    elif what == "pos":
+        for bad in (pos.long(), pos[:3], torch.zeros((4, 2), dtype=torch.int32, device=DEV), pos[:, 0], pos.cpu(), None):
+            with pytest.raises(ValueError):
+                run(pos=bad)
+    elif what == "heads":
+        for bad in (dict(qo=qo[:, :1]), dict(ko=qo), dict(q=q[..., :32]), dict(q=q.reshape(4, 128))):
+            with pytest.raises(ValueError):
+                run(**bad)
+    elif what == "strides":
+        wide = torch.zeros((4, 2, 128), dtype=BF16, device=DEV)
+        for bad in (wide[..., :64], wide[..., ::2]):
+            with pytest.raises(ValueError):
+                run(q=bad)
+    elif what == "cpu":
+        with pytest.raises(ValueError):
+            run(q=q.cpu())
+    elif what == "weights":
+        with pytest.raises(ValueError):
+            pa.padoc_qk_rotary_bwd(sp.dev, q, k, pos, qo, ko)
+        w = torch.empty(64, dtype=BF16, device=DEV)
+        ws = torch.empty(1 << 16, dtype=torch.uint8, device=DEV)
+        with pytest.raises(ValueError):
+            pa.padoc_qk_rotary_bwd(sp.dev, q, k, pos, qo, ko, q, k, w, w, ws)
+        with pytest.raises(pa.PadocError) as e:
+            pa.padoc_qk_rotary_bwd(sp.dev, q, k, pos, qo, ko, q, k, w.float(), w.float(), ws[:256])
+        assert e.value.status == 3
+    elif what == "slots":
+        pool = torch.zeros((2, 1, BS, 64), dtype=BF16, device=DEV)
+        slots = torch.arange(4, dtype=torch.int32, device=DEV)
+        for bad in (dict(slots=slots.long()), dict(slots=slots, count=5), dict(slots=slots, src_rows=slots[:2]),
+                    dict(slots=slots, q_src=q), dict(slots=slots, q_src=q, q_dst=qo[:2]),
+                    dict(slots=torch.arange(5, dtype=torch.int32, device=DEV))):
+            with pytest.raises(ValueError):
+                pa.padoc_append_rotary_inputs(sp.dev, pool, pool, k, k, pos, **bad)
+        with pytest.raises(ValueError):
+            pa.padoc_append_rotary_inputs(sp.dev, pool, pool[:1], k, k, pos, slots)
+    elif what == "expand":
+        with pytest.raises(pa.PadocError) as e:      # rows that lie on one another
+            run(q=q[:1].expand(4, 2, 64))
+        assert e.value.status == 1
+    else:
+        flat = torch.zeros(4 * 128 + 4, dtype=BF16, device=DEV)[4:].view(4, 2, 64)
+        with pytest.raises(pa.PadocError) as e:      # 8 bytes off a 16-byte boundary
+            run(q=flat)
+        assert e.value.status == 1
+
+
 def test_on_a_side_stream_and_in_a_graph():
     sp = Spec(6, 128, 128, 3, False, True, BF16)
     rng = np.random.default_rng(6)
