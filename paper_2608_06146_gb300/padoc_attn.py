@@ -360,6 +360,26 @@ def _dev(t, name):
     return t.data_ptr()
 
 
+_get_device = None
+
+
+def _current_device() -> int:
+    global _get_device
+    if _get_device is None:
+        import torch
+        _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _get_device()
+
+
+def _on(t, name, device):
+    """Address of a contiguous tensor on the given CUDA device (index)."""
+    if t is None:
+        return None
+    if t.get_device() != device or not t.is_contiguous():   # (-1: a CPU tensor)
+        raise ValueError(f"{name} must be a contiguous CUDA tensor on device {device}")
+    return t.data_ptr()
+
+
 # ------------------------------------------------------------------------------------------------
 # C1: descriptors
 # ------------------------------------------------------------------------------------------------
@@ -1135,13 +1155,15 @@ def padoc_build_rotary_positions(pages, grids=()):
 class Rotary:
     """A padoc_rotary with its device table and weights (owned or kept alive here): inv_freq [pairs] and
     axis_of [pairs] as in padoc_build_rotary_table; pairs (i, i + pairs), or (2 i, 2 i + 1) with adjacent; q_weight and
-    k_weight (CUDA tensors [head_dim] in the rows' dtype) give the heads an RMS norm before the rotation."""
+    k_weight (CUDA tensors [head_dim] in the rows' dtype) give the heads an RMS norm before the rotation. Calls take
+    tensors on its device, which must be the current one."""
 
     def __init__(self, inv_freq, axis_of=None, num_axes: int = 1, head_dim: int = 128, adjacent: bool = False,
                  q_weight=None, k_weight=None, eps: float = 1e-6, amplitude: float = 1.0, device="cuda"):
         import torch
         table = padoc_build_rotary_table(inv_freq, axis_of, num_axes)
-        self.table = torch.from_numpy(table.view(np.int64).copy()).to(device)
+        self.table = torch.from_numpy(table.view(np.int64)).to(device)
+        self._device = self.table.get_device()
         self.q_weight, self.k_weight = q_weight, k_weight
         self.dtype = None
         self._codes = {torch.bfloat16: PADOC_DTYPE_BF16, torch.float32: PADOC_DTYPE_F32}
@@ -1154,8 +1176,8 @@ class Rotary:
                 raise ValueError("q_weight and k_weight must be [head_dim] of one dtype")
             self.dtype = w.dtype
         self.head_dim, self.num_axes = head_dim, num_axes
-        self.c = padoc_rotary(_dev(self.table, "table"), _dev(q_weight, "q_weight"), _dev(k_weight, "k_weight"),
-                              head_dim, 2 * table.size, num_axes, int(bool(adjacent)), eps, amplitude)
+        dev = self._device
+        self.c = padoc_rotary(_dev(self.table, "table"), _on(q_weight, "q_weight", dev), _on(k_weight, "k_weight", dev), head_dim, 2 * table.size, num_axes, int(bool(adjacent)), eps, amplitude)
         self.ref = ctypes.byref(self.c)
 
     def positions(self, pos, rows=None):
@@ -1165,14 +1187,15 @@ class Rotary:
         n, axes = pos.shape
         if pos.dtype is not self._int32 or axes != self.num_axes or (rows is not None and n != rows):
             raise ValueError("pos must be int32 [rows][axes], a position for each row")
-        return _dev(pos, "pos")
+        return _on(pos, "pos", self._device)
 
     def heads(self, t, name, rows, dtype):
         """(address, row stride, heads) of a CUDA tensor [rows][heads][head_dim] whose rows may lie apart."""
         n, h, d = t.shape
         s0, s1, s2 = t.stride()
-        if d != self.head_dim or s2 != 1 or (s1 != d and h > 1) or not t.is_cuda:
-            raise ValueError(f"{name} must be a CUDA tensor [rows][heads][head_dim] with contiguous rows")
+        if d != self.head_dim or s2 != 1 or (s1 != d and h > 1) or t.get_device() != self._device:
+            raise ValueError(f"{name} must be a CUDA tensor [rows][heads][head_dim] with contiguous rows on device "
+                             f"{self._device}")
         if n != rows or t.dtype is not dtype:
             raise ValueError(f"{name} must have the other tensors' rows and dtype")
         return t.data_ptr(), (s0 if n > 1 else h * d), h
@@ -1180,6 +1203,8 @@ class Rotary:
     def rows(self, pos, k, q=None, v=None):
         """(a padoc_qkv_rows over q / k / v [rows][heads][head_dim] and pos int32 [rows][axes], as bytes; rows;
         query heads; KV heads)."""
+        if _current_device() != self._device:
+            raise ValueError(f"the current device must be the rotary's, {self._device}")
         n, dt = k.shape[0], k.dtype
         code = self._codes.get(dt)
         if code is None or (self.dtype is not None and dt is not self.dtype):
@@ -1238,9 +1263,10 @@ def padoc_qk_rotary_bwd(rotary: Rotary, dq_out, dk_out, pos, dq, dk, q=None, k=N
     kp, ks, kh = rotary.heads(dk, "dk", n, dt)
     if qh != hq or kh != hkv:
         raise ValueError("dq and dk must have the gradients' heads")
-    ws, wsb = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel() * workspace.element_size())
-    st = lib.padoc_qk_rotary_bwd(rotary.ref, rows, uq, uqs, uk, uks, qp, qs, kp, ks, _dev(dq_weight, "dq_weight"),
-                                 _dev(dk_weight, "dk_weight"), ws, wsb, _stream_ptr(stream))
+    dev = rotary._device
+    ws, wsb = (None, 0) if workspace is None else (_on(workspace, "workspace", dev), workspace.numel() * workspace.element_size())
+    st = lib.padoc_qk_rotary_bwd(rotary.ref, rows, uq, uqs, uk, uks, qp, qs, kp, ks, _on(dq_weight, "dq_weight", dev),
+                                 _on(dk_weight, "dk_weight", dev), ws, wsb, _stream_ptr(stream))
     _check("padoc_qk_rotary_bwd", st)
 
 
@@ -1262,8 +1288,8 @@ def _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count
         dn, dh, dd = q_dst.shape
         if dn < n or dh != hq or dd != rotary.head_dim or q_dst.dtype is not k_src.dtype:
             raise ValueError("q_dst must be [count][Hq][d] in the rows' dtype")
-        dst = _dev(q_dst, "q_dst")
-    return rows, dst, _dev(src_rows, "src_rows"), _dev(slots, "slots"), n
+        dst = _on(q_dst, "q_dst", rotary._device)
+    return rows, dst, _on(src_rows, "src_rows", rotary._device), _on(slots, "slots", rotary._device), n
 
 
 def padoc_append_rotary_inputs(rotary: Rotary, k_pool, v_pool, k_src, v_src, pos, slots, q_src=None, q_dst=None,
@@ -1271,8 +1297,9 @@ def padoc_append_rotary_inputs(rotary: Rotary, k_pool, v_pool, k_src, v_src, pos
     """padoc_append_inputs with the norm and the rotation on the way (sources' rows may lie apart; pos int32
     [rows][axes] by source row)."""
     lib = load_library()
-    if v_pool.shape != k_pool.shape or v_pool.dtype is not k_pool.dtype:
-        raise ValueError("k_pool and v_pool must be alike")
+    if v_pool.shape != k_pool.shape or v_pool.dtype is not k_pool.dtype or k_pool.get_device() != rotary._device or \
+            v_pool.get_device() != rotary._device:
+        raise ValueError("k_pool and v_pool must be alike, on the rotary's device")
     pool = make_kv_pool(k_pool, v_pool)
     rows, dst, sr, sl, n = _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count)
     _check("padoc_append_rotary_inputs",
@@ -1285,6 +1312,8 @@ def padoc_append_rotary_inputs_e4m3(rotary: Rotary, pool: E4M3Pool, k_src, v_src
     """padoc_append_rotary_inputs into an E4M3 pool (bf16 sources); inputs of one block must follow one
     another into consecutive rows."""
     lib = load_library()
+    if pool.k_codes.get_device() != rotary._device:
+        raise ValueError("the pool must be on the rotary's device")
     rows, dst, sr, sl, n = _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count)
     _check("padoc_append_rotary_inputs_e4m3",
            lib.padoc_append_rotary_inputs_e4m3(ctypes.byref(pool.c), rotary.ref, rows, dst, sr, sl, n,
@@ -1303,9 +1332,10 @@ class KvPools:
         self._int32 = torch.int32
         self.tensors = [tuple(p) for p in pools]
         self.c = (padoc_kv_pool * max(len(self.tensors), 1))(*[make_kv_pool(k, v) for k, v in self.tensors])
+        self._device = self.tensors[0][0].get_device() if self.tensors else _current_device()
         for k, v in self.tensors:
-            if k.shape != v.shape or k.dtype != v.dtype:
-                raise ValueError("k_pool and v_pool must be alike")
+            if k.shape != v.shape or k.dtype != v.dtype or k.get_device() != self._device or v.get_device() != self._device:
+                raise ValueError("k_pool and v_pool must be alike, all on one device")
 
     def __len__(self):
         return len(self.tensors)
@@ -1319,6 +1349,9 @@ class KvPoolsE4M3:
         self._int32 = torch.int32
         self.pools = [p if isinstance(p, E4M3Pool) else E4M3Pool.over(*p) for p in pools]
         self.c = (padoc_kv_pool_e4m3 * max(len(self.pools), 1))(*[p.c for p in self.pools])
+        self._device = self.pools[0].k_codes.get_device() if self.pools else _current_device()
+        if any(t.get_device() != self._device for p in self.pools for t in (p.k_codes, p.v_codes, p.k_scales, p.v_scales)):
+            raise ValueError("the pools must be on one device")
 
     def __len__(self):
         return len(self.pools)
@@ -1329,11 +1362,14 @@ def _copy_blocks(f, name, pools, src_blocks, dst_blocks, src_pools, count, strea
     layers = len(pools)
     if len(src) != layers:
         raise ValueError("as many source pools as destination pools")
+    dev = pools._device
+    if src._device != dev or _current_device() != dev:
+        raise ValueError("the pools must be on the current device")
     n = src_blocks.shape[0] if count is None else count
     i32 = pools._int32
     if src_blocks.dtype is not i32 or dst_blocks.dtype is not i32 or src_blocks.numel() < n or dst_blocks.numel() < n:
         raise ValueError("src_blocks and dst_blocks must be int32 [count]")
-    _check(name, f(pools.c, src.c, layers, _dev(src_blocks, "src_blocks"), _dev(dst_blocks, "dst_blocks"), n,
+    _check(name, f(pools.c, src.c, layers, _on(src_blocks, "src_blocks", dev), _on(dst_blocks, "dst_blocks", dev), n,
                    _stream_ptr(stream)))
 
 

@@ -258,7 +258,7 @@ def test_a_table_of_more_axes_reads_the_last_one():
     check(ko, *sp.forward(k, None, pos), FWD, "k")
 
 
-@pytest.mark.parametrize("what", ["dtype", "pos", "heads", "strides", "cpu", "weights", "slots", "expand", "align"])
+@pytest.mark.parametrize("what", ["dtype", "pos", "heads", "strides", "cpu", "weights", "slots", "expand", "align", "device"])
 def test_python_refusals(what):
     sp = Spec(1, 64, 64, 1, False, True, BF16)
     q, k = torch.zeros((4, 2, 64), dtype=BF16, device=DEV), torch.zeros((4, 1, 64), dtype=BF16, device=DEV)
@@ -306,6 +306,15 @@ def test_python_refusals(what):
                 pa.padoc_append_rotary_inputs(sp.dev, pool, pool, k, k, pos, **bad)
         with pytest.raises(ValueError):
             pa.padoc_append_rotary_inputs(sp.dev, pool, pool[:1], k, k, pos, slots)
+    elif what == "device":
+        sp.dev._device = 1                           # (as if it were on a second GPU)
+        with pytest.raises(ValueError, match="device"):
+            run()
+        pools = pa.KvPools([(torch.zeros((2, 1, BS, 64), device=DEV),) * 2])
+        pools._device = 1
+        i = torch.zeros(1, dtype=torch.int32, device=DEV)
+        with pytest.raises(ValueError, match="device"):
+            pa.padoc_copy_kv_blocks(pools, i, i)
     elif what == "expand":
         with pytest.raises(pa.PadocError) as e:      # rows that lie on one another
             run(q=q[:1].expand(4, 2, 64))
