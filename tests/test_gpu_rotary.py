@@ -1,15 +1,14 @@
 """GPU parity of the head norms and rotary positions: the packed forward and backward, the append into the
 paged pool and into the FP8 pool, against the 64-bit definition (oracle/rotary.py).
 
-Tolerances, derived. The angle's fraction of a turn is cut at 2^-32 and rounded to 24 bits: 2e-7 rad; its
-sine and cosine are off by at most 2^-20.9 from a fast evaluation: in all under 8e-7 on each of c, s. A
-rotated value u c - v s is so off by 1e-6 (|u| + |v|) with the two products' roundings. The norm's scale:
-a sum of 256 squares in at most 21 additions (1.3e-6, halved by the root), the root's 2 units of the last place
-and three roundings: 1.1e-6 relative, on both u and v. So FWD = 3e-6 x amplitude x (|u| + |v|), and one
-rounding to the stored type, eps / 2 of the value. Backward: g has 1e-6, h = x r 1.2e-6, the mean of w g h 1.3e-6 for
-its sum and those of its terms, and the product's three roundings: BWD = 6e-6 x the sum of the magnitudes the
-formula adds. The weights' gradient sums (rows x heads) products, each off by 2.2e-6 of its magnitude, in chains of
-at most 512 fp32 additions here: DW = 2.2e-6 + 512 x 2^-24 of the sum of the magnitudes.
+Tolerances, derived (worst cases, relative, in units of 1e-6; 2^-24 = 0.06). The angle's fraction of a turn is cut
+at 2^-32 and rounded to 24 bits: 0.2 rad; the hardware's sine and cosine are 2^-20.5 = 0.67 off at most: in all 0.9 on
+each of c and s, and u c - v s is 1.1 (|u| + |v|) off with its roundings. The norm's scale: a sum of 256 squares in at
+most 21 additions (1.25, halved by the root), the root's 2 units of the last place and the roundings: 0.95, on both u
+and v. So FWD = 3 x amplitude x (|u| + |v|), and one rounding to the stored type, eps / 2 of the value. Backward: g has
+1.1; r g x w 2.4; the mean of w g h: 1.25 for its sum, 1.3 for its terms' w g, 0.95 for r; times r r x: 5.9. BWD = 6 x
+the sum of the magnitudes that the formula adds. The weights' gradient sums (rows x heads) products r g x, each 2.2
+off, in chains of fewer than 500 fp32 additions: DW = 2.2 + 512 x 0.06 of the sum of the magnitudes.
 """
 import math
 
@@ -581,6 +580,101 @@ def test_append_e4m3_without_angles_equals_the_plain_append(special):
     pa.padoc_check_device_errors()
     for x, y in ((a.k_codes, b.k_codes), (a.v_codes, b.v_codes), (a.k_scales, b.k_scales), (a.v_scales, b.v_scales), (qa, qb)):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_append_captured_replayed_and_on_two_streams(e4m3):
+    # a captured append reads the buffers' contents at each replay; two streams append to pools of their own at once
+    sp = Spec(31, 128, 128, 3, False, True, BF16)
+    rng = np.random.default_rng(31)
+    n, nb = 40, 60
+    _, q, k, v = qkv(rng, n, 16, 2, 128, BF16)
+    pos = positions(rng, n, 3)
+    slots = up(runs(rng, "step", nb)[:n])
+    src = torch.arange(n, dtype=torch.int32, device=DEV)
+
+    def new_pool():
+        if e4m3:
+            return stale_pool(np.random.default_rng(5), nb, 2)
+        return tuple(torch.full((nb, 2, BS, 128), 2.0, dtype=BF16, device=DEV) for _ in range(2))
+
+    def tensors(p):
+        return (p.k_codes, p.v_codes, p.k_scales, p.v_scales) if e4m3 else p
+
+    def append(p, qd, stream=None):
+        if e4m3:
+            pa.padoc_append_rotary_inputs_e4m3(sp.dev, p, k, v, pos, slots, q, qd, src, stream=stream)
+        else:
+            pa.padoc_append_rotary_inputs(sp.dev, *p, k, v, pos, slots, q, qd, src, stream=stream)
+    qd = [torch.zeros((n, 16, 128), dtype=BF16, device=DEV) for _ in range(4)]
+    want = new_pool()
+    append(want, qd[0])
+    streams, pools = [torch.cuda.Stream() for _ in range(2)], [new_pool() for _ in range(2)]
+    torch.cuda.synchronize()
+    for s, p, d in zip(streams, pools, qd[1:]):
+        append(p, d, s)
+    torch.cuda.synchronize()
+    for p, d in zip(pools, qd[1:]):
+        assert all(torch.equal(a, b) for a, b in zip(tensors(p), tensors(want))) and torch.equal(d, qd[0])
+    graph, held = torch.cuda.CUDAGraph(), new_pool()
+    with torch.cuda.graph(graph):
+        append(held, qd[3])
+    src.copy_(src.flip(0))
+    pos.add_(7)
+    append(want, qd[0])
+    for t, x in zip(tensors(held), tensors(pools[0])):
+        t.copy_(x)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(tensors(held), tensors(want))) and torch.equal(qd[3], qd[0])
+    # nothing to append
+    none = torch.empty(0, dtype=torch.int32, device=DEV)
+    if e4m3:
+        pa.padoc_append_rotary_inputs_e4m3(sp.dev, held, k, v, pos, none)
+    else:
+        pa.padoc_append_rotary_inputs(sp.dev, *held, k, v, pos, none)
+    pa.padoc_check_device_errors()
+    assert all(torch.equal(a, b) for a, b in zip(tensors(held), tensors(want)))
+
+
+def test_runner_rotary_is_set_replaced_and_taken_off():
+    sp = Spec(32, 128, 128, 1, False, True, BF16)
+    mpd = pa.Mpd(8)
+    pool = tuple(torch.zeros((8, 2, BS, 128), dtype=BF16, device=DEV) for _ in range(2))
+    cfg = pa.make_decode_config(16, 2, 128)
+    runner = pa.MpdRunner(mpd, cfg, pa.make_kv_pool(*pool))
+    _, q, k, v = qkv(np.random.default_rng(32), 4, 16, 2, 128, BF16)
+    q, k, v = (t.contiguous() for t in (q, k, v))
+    pos = torch.arange(4, dtype=torch.int32, device=DEV)[:, None].contiguous()
+    out, lse = torch.empty((4, 16, 128), dtype=BF16, device=DEV), torch.empty((4, 16), device=DEV)
+    mpd.add_page(0, 0)
+    row = np.zeros(4, np.int32)
+    kr, qr = torch.empty_like(k), torch.empty_like(q)
+    pa.padoc_qk_rotary(sp.dev, q, k, pos, qr, kr)
+
+    def step(r):
+        row[:] = r
+        runner.step(k, v, q, row, 0.1, out, lse)
+        mpd.end_step(num_streams=1)
+        torch.cuda.synchronize()
+    step(1)
+    runner.set_rotary(sp.dev, pos)
+    step(2)
+    runner.set_rotary(sp.dev, pos[:3])
+    row[:] = 1
+    with pytest.raises(pa.PadocError) as e:              # four source rows, three positions
+        runner.step(k, v, q, row, 0.1, out, lse)
+    assert e.value.status == 1 and mpd.status()[1] == 1
+    runner.set_rotary(None)
+    step(3)
+    pa.padoc_check_device_errors()
+    got = pool[0][0, :, :3]
+    assert torch.equal(got[:, 0], k[1]) and torch.equal(got[:, 1], kr[2]) and torch.equal(got[:, 2], k[3])
+    small = Spec(32, 64, 64, 1, False, False, BF16)
+    with pytest.raises(pa.PadocError):
+        runner.set_rotary(small.dev, pos)                # another head_dim
+    with pytest.raises(TypeError):
+        runner.set_rotary(Spec(32, 128, 128, 1, False, True, F32).dev, pos)
 
 
 # ------------------------------------------------------------------------------------------------
