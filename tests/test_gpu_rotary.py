@@ -19,10 +19,9 @@ import torch
 import oracle
 from oracle import rotary as orot
 from paper_2608_06146_gb300 import build as pbuild
-from paper_2608_06146_gb300 import inputs
 from paper_2608_06146_gb300 import padoc_attn as pa
-from paper_2608_06146_gb300.engine import MaskedParallelLoop, RotaryPrefill
-from paper_2608_06146_gb300.inputs import LoopTokenSource, PageSpec, Workload
+from paper_2608_06146_gb300.engine import ChunkPrefillPlan, DecodePlan, MaskedParallelLoop, RotaryPrefill
+from paper_2608_06146_gb300.inputs import LoopTokenSource, PageSpec
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -749,6 +748,60 @@ def test_training_layer_bf16_runs_on_its_own_rotated_rows():
         dx, size, dw, terms = sp.backward(dz, x, w, layer.pos)
         check(got, dx, size, BWD, name)
         check(gw, dw, terms, DW, name + "_weight")
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_prefix_and_chunk_appended_then_attended(e4m3):
+    # a page's prefix and layout tokens go into the cache in one call, a branch's 21 tokens in another, which also
+    # lays out their queries; then the chunk is prefilled (bf16), or its newest token decoded (FP8), against the oracle
+    # over the rotated rows, resp. over what the codes stand for (the decode's own tolerances)
+    P, L, f, n = 70, 10, 4, 21
+    page = PageSpec(P, L, [f], [n])
+    sp = Spec(33, 128, 128, 3, False, True, BF16)
+    rng = np.random.default_rng(33)
+    T, scale = P + L + n, 128 ** -0.5
+    x, q, k, v = qkv(rng, T, 16, 2, 128, BF16)
+    pos = up(pa.padoc_build_rotary_positions([page], [(0, 2, 1, 8, 8)])[0])
+    blocks = rng.permutation(12).astype(np.int32)
+    shared, private = blocks[:5], blocks[5:7]
+    slots = np.concatenate([shared[np.arange(P + L) // BS] * BS + np.arange(P + L) % BS,
+                            private[np.arange(n) // BS] * BS + np.arange(n) % BS]).astype(np.int32)
+    rows = np.arange(T, dtype=np.int32)
+    qd = torch.empty((n, 16, 128), dtype=BF16, device=DEV)
+    if e4m3:
+        pool = stale_pool(rng, 12, 2)
+        append = lambda *a, **kw: pa.padoc_append_rotary_inputs_e4m3(sp.dev, pool, k, v, pos, *a, **kw)
+    else:
+        kp, vp = (torch.zeros((12, 2, BS, 128), dtype=BF16, device=DEV) for _ in range(2))
+        append = lambda *a, **kw: pa.padoc_append_rotary_inputs(sp.dev, kp, vp, k, v, pos, *a, **kw)
+    append(up(slots[:P + L]))
+    append(up(slots[P + L:]), q, qd, up(rows[P + L:]))
+    page_table, table = up(shared[None]), private[None]
+    if e4m3:
+        plan = DecodePlan([page], 16, 2, 128, DEV)
+        out, lse = torch.empty((1, 16, 128), dtype=BF16, device=DEV), torch.empty((1, 16), device=DEV)
+        newest = qd[n - 1:].contiguous()
+        pa.padoc_branch_decode_attn_e4m3(pool, plan.info, plan.plan_dev, page_table, up(table), newest, scale, out, lse,
+                                         plan.workspace)
+        pa.padoc_check_device_errors()
+        deq = [oracle.dequantize_kv_blocks(c.cpu().numpy(), s.cpu().numpy())
+               for c, s in ((pool.k_codes, pool.k_scales), (pool.v_codes, pool.v_scales))]
+        ro, rl = oracle.decode_paged([page], *deq, shared[None], table, newest.cpu(), scale)
+        # and the codes stand for the rotated rows: half a step of the format at the block's largest magnitude
+        want = sp.forward(k, sp.kw, pos)[0]
+        held = np.stack([deq[0][s // BS, :, s % BS] for s in slots])
+        step = np.stack([pool.k_scales.cpu().numpy()[s // BS] for s in slots])[..., None]
+        assert (np.abs(held - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * step) * 1.001 + 1e-4).all()
+    else:
+        plan = ChunkPrefillPlan([P + L], [(0, P + f, 0, n)], table, 16, 2, 128, DEV)
+        out, lse = torch.empty((n, 16, 128), dtype=BF16, device=DEV), torch.empty((n, 16), device=DEV)
+        plan.run(kp, vp, page_table, qd, scale, out, lse)
+        pa.padoc_check_device_errors()
+        qr, kr = torch.empty((T, 16, 128), dtype=BF16, device=DEV), torch.empty((T, 2, 128), dtype=BF16, device=DEV)
+        pa.padoc_qk_rotary(sp.dev, q, k, pos, qr, kr)
+        ro, rl = oracle.prefill_dense([page], qr.cpu(), kr.cpu(), v.cpu(), scale)
+        ro, rl = ro[P + L:], rl[P + L:]
+    assert np.abs(f64(out) - ro).max() <= 1.5e-2 and np.abs(f64(lse) - rl).max() <= 1e-3
 
 
 LOOP_PAGES = [PageSpec(60, 10, [0, 10, 3, 7], [17, 5, 33, 16]), PageSpec(130, 24, [24, 12, 8, 20, 4], [2, 40, 12, 30, 18])]
