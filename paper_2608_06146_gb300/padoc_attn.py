@@ -118,6 +118,10 @@ _QKV_ROWS = struct.Struct("@3P3qPq3i4x")
 assert _QKV_ROWS.size == ctypes.sizeof(padoc_qkv_rows)
 
 
+_KV_POOL = struct.Struct("@2P5i4x")
+assert _KV_POOL.size == ctypes.sizeof(padoc_kv_pool)
+
+
 class padoc_grid(ctypes.Structure):
     _fields_ = [("page", ctypes.c_int32), ("begin", ctypes.c_int32), ("t", ctypes.c_int32), ("h", ctypes.c_int32),
                 ("w", ctypes.c_int32)]
@@ -1297,14 +1301,14 @@ def padoc_append_rotary_inputs(rotary: Rotary, k_pool, v_pool, k_src, v_src, pos
     """padoc_append_inputs with the norm and the rotation on the way (sources' rows may lie apart; pos int32
     [rows][axes] by source row)."""
     lib = load_library()
-    if v_pool.shape != k_pool.shape or v_pool.dtype is not k_pool.dtype or k_pool.get_device() != rotary._device or \
-            v_pool.get_device() != rotary._device:
-        raise ValueError("k_pool and v_pool must be alike, on the rotary's device")
-    pool = make_kv_pool(k_pool, v_pool)
+    shape, dt, dev = k_pool.shape, k_pool.dtype, rotary._device
+    if v_pool.shape != shape or v_pool.dtype is not dt or dt is not k_src.dtype:
+        raise ValueError("k_pool and v_pool must be alike, in the rows' dtype")
+    nb, hkv, bs, d = shape
+    pool = _KV_POOL.pack(_on(k_pool, "k_pool", dev), _on(v_pool, "v_pool", dev), nb, bs, hkv, d, rotary._codes.get(dt, -1))
     rows, dst, sr, sl, n = _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count)
     _check("padoc_append_rotary_inputs",
-           lib.padoc_append_rotary_inputs(ctypes.byref(pool), rotary.ref, rows, dst, sr, sl, n,
-                                          _stream_ptr(stream)))
+           lib.padoc_append_rotary_inputs(pool, rotary.ref, rows, dst, sr, sl, n, _stream_ptr(stream)))
 
 
 def padoc_append_rotary_inputs_e4m3(rotary: Rotary, pool: E4M3Pool, k_src, v_src, pos, slots, q_src=None, q_dst=None,
