@@ -131,9 +131,14 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
 
     const float inv_d = 1.f / (float)d;
     const bool whole = p.sp.rot == d;
-    uint64_t acc[2][V];   // sums of g h: the pairs of the lane's first, then of its second vector
+    // sums of g h, the pairs of the lane's first, then of its second vector: the queries' in registers, the keys' (a
+    // step in five at 16 + 2 heads) in shared memory
+    uint64_t acc[V];
+    ulonglong2 *acc_k = reinterpret_cast<ulonglong2 *>(smem_raw + 2 * kPairs * group + kBwdWarps * kBwdStages * 4 * 32 * sizeof(Vec) / 16) + warp * kPairs * 32 + lane;
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[0][j] = acc[1][j] = 0;
+    for (int j = 0; j < V; ++j) acc[j] = 0;
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) acc_k[j * 32] = make_ulonglong2(0, 0);
     int stage = 0;
     for (int64_t row = first; row < row_end; row += kBwdWarps) {
         uint64_t c[kPairs], s[kPairs];
@@ -179,8 +184,15 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
 #pragma unroll
                 for (int j = 0; j < kPairs; ++j) {
                     const uint64_t ta = f2_mul(a[j], r2), tb = f2_mul(b[j], r2);
-                    acc[kind][j] = f2_fma(ta, xa[j], acc[kind][j]);
-                    acc[kind][kPairs + j] = f2_fma(tb, xb[j], acc[kind][kPairs + j]);
+                    if (kind == 0) {
+                        acc[j] = f2_fma(ta, xa[j], acc[j]);
+                        acc[kPairs + j] = f2_fma(tb, xb[j], acc[kPairs + j]);
+                    } else {
+                        ulonglong2 v = acc_k[j * 32];
+                        v.x = f2_fma(ta, xa[j], v.x);
+                        v.y = f2_fma(tb, xb[j], v.y);
+                        acc_k[j * 32] = v;
+                    }
                     a[j] = f2_fma(ta, wa[j], f2_mul(xa[j], c2));
                     b[j] = f2_fma(tb, wb[j], f2_mul(xb[j], c2));
                 }
@@ -194,6 +206,13 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
         }
     }
     cp_async_wait<0>();
+    uint64_t acc_all[2][V];
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) {
+        const ulonglong2 v = acc_k[j * 32];
+        acc_all[0][j] = acc[j], acc_all[0][kPairs + j] = acc[kPairs + j];
+        acc_all[1][j] = v.x, acc_all[1][kPairs + j] = v.y;
+    }
     __syncthreads();   // every warp is done with its stages
     float *sums = reinterpret_cast<float *>(smem_raw);
 #pragma unroll
@@ -201,7 +220,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             float lo, hi;
-            f2_unpack(acc[kind][j], lo, hi);
+            f2_unpack(acc_all[kind][j], lo, hi);
             for (int m = group; m < 32; m <<= 1) {
                 lo += __shfl_xor_sync(0xffffffffu, lo, m);
                 hi += __shfl_xor_sync(0xffffffffu, hi, m);
@@ -320,7 +339,7 @@ padoc_status launch_bwd(const BwdArgs &p, bool adjacent, int ctas, padoc_stream_
     // (8 lanes a head: 128 dims in bf16, 64 in fp32)
     auto *k = p.group_log == 3 ? (adjacent ? rotary_norm_bwd_kernel<T, V, true, 8> : rotary_norm_bwd_kernel<T, V, false, 8>)
                                : (adjacent ? rotary_norm_bwd_kernel<T, V, true, 0> : rotary_norm_bwd_kernel<T, V, false, 0>);
-    const size_t weights = (size_t)V << p.group_log << 4, ring = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>);
+    const size_t weights = (size_t)V << p.group_log << 4, ring = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>) + (size_t)kBwdWarps * (V / 2) * 32 * 16;
     const size_t sums = (size_t)kBwdWarps * 2 * p.sp.d * sizeof(float);
     const int smem = (int)(weights + ring > sums ? weights + ring : sums);
     const padoc_status st = padoc_set_max_smem((const void *)k, smem);
