@@ -261,7 +261,7 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int32_t sl
     if (!good) return;
     const bool is_v = unit >= p.hkv;
     const int g = is_v ? unit - p.hkv : unit;
-    const Place pl = lane_place<V, kAdjacent>(chunk, kD, p.sp.rot);
+    const Place pl = lane_place<V>(chunk, kD, p.sp.rot);
     const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(is_v ? p.v : p.k) + g * kD;
     const int64_t stride = is_v ? p.v_stride : p.k_stride;
     Raw<__nv_bfloat16, V> ra[kPasses], rb[kPasses];
@@ -298,7 +298,7 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int32_t sl
             }
             if (here && pl.turned) {
                 uint64_t c[V / 2], s[V / 2];
-                lane_angles<V, true, 0>(p.sp, p.pos, at, chunk, true, c, s);   // (a row a group: nothing to share)
+                lane_angles<V, kAdjacent, true, 0>(p.sp, p.pos, at, chunk, true, c, s);   // (a row a group: nothing to share)
                 turn_pairs<V, kAdjacent>(za, zb, c, s);
             }
         }

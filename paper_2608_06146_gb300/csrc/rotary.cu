@@ -15,9 +15,10 @@ namespace {
 constexpr int kWarps = 4;   // warps per CTA
 
 // See row_part. kCtas: CTAs an SM that the registers have to allow. With the norm a row's steps take longer than its
-// loads, so many rows want more warps on an SM than the compiler's own choice gives (92 registers, 5 CTAs), even at a
-// few spilled values; few rows want the loads first. 16 + 2 heads of 128 dims in bf16, own choice / 7 CTAs: 2500
-// rows 5.3 / 7.0 us, 5000 12.0 / 12.6, 10000 19.6 / 19.4, 32768 51.5 / 49.5. Without the norm 46.0 / 51.7.
+// loads, so many rows want one more CTA on an SM than the compiler's own choice gives (96 registers, 5 CTAs), even at a
+// few spilled values; few rows want the loads first. 16 + 2 heads of 128 dims in bf16, own choice / 6 / 7 CTAs: 10001
+// rows 19.3 / 19.5 / 20.7 us, 32768 50.3 / 49.2 / 53.2; 64 dims, 52083 rows 49.9 / 48.4 / 53.3. Adjacent pairs, which
+// are turned one by one, lose by it: 26041 rows 43.3 / 46.9 / 49.1.
 template <typename T, int V, bool kAdjacent, bool kNorm, int kMode, int kGroup, int kCtas>
 __global__ void __launch_bounds__(32 * kWarps, kCtas) rotary_kernel(const __grid_constant__ Args p)
 {
@@ -72,14 +73,14 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int group = kGroup ? kGroup : 1 << p.group_log, heads = 32 / group;
     const int sub = lane / group, chunk = lane & (group - 1);
-    const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
+    const Place pl = lane_place<V>(chunk, p.sp.d, p.sp.rot);
     const int d = p.sp.d;
     Vec *ring = reinterpret_cast<Vec *>(smem_raw + 2 * kPairs * group) + (size_t)warp * kBwdStages * 4 * 32 + lane;
     pdl_wait_prerequisite();
     pdl_launch_dependents();
     for (int e = threadIdx.x; e < 2 * kPairs * group; e += 32 * kBwdWarps) {
         const int kind = e >= kPairs * group, piece = e / group - kind * kPairs;
-        const Place at = lane_place<V, kAdjacent>(e & (group - 1), d, p.sp.rot);
+        const Place at = lane_place<V>(e & (group - 1), d, p.sp.rot);
         float4 w4 = make_float4(0.f, 0.f, 0.f, 0.f);
         if (at.active) {
             const T *w = static_cast<const T *>(kind ? p.sp.k_weight : p.sp.q_weight) +
@@ -142,7 +143,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     int stage = 0;
     for (int64_t row = first; row < row_end; row += kBwdWarps) {
         uint64_t c[kPairs], s[kPairs];
-        lane_angles<V, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, chunk, pl.turned, c, s);
+        lane_angles<V, kAdjacent, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, chunk, pl.turned, c, s);
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
             const ulonglong2 *w = reinterpret_cast<const ulonglong2 *>(smem_raw) + kind * kPairs * group + chunk;
@@ -301,17 +302,22 @@ padoc_status launch_group(const Args &p, bool adjacent, bool norm, dim3 grid, pa
     auto *k = adjacent ? (norm ? rotary_kernel<T, V, true, true, kMode, kGroup, kMode == kAppend ? 7 : 1> : rotary_kernel<T, V, true, false, kMode, kGroup, kMode == kAppend ? 7 : 1>)
                        : (norm ? rotary_kernel<T, V, false, true, kMode, kGroup, kMode == kAppend ? 7 : 1> : rotary_kernel<T, V, false, false, kMode, kGroup, kMode == kAppend ? 7 : 1>);
     if constexpr (kMode == kPacked && V == 8)
-        if (norm && (int64_t)grid.x * grid.y * kWarps >= 64 * (int64_t)padoc_default_ctas())   // 64 warps an SM
-            k = adjacent ? rotary_kernel<T, V, true, true, kMode, kGroup, 7> : rotary_kernel<T, V, false, true, kMode, kGroup, 7>;
+        if (norm && !adjacent && (int64_t)grid.x * grid.y * kWarps >= 64 * (int64_t)padoc_default_ctas())   // 64 warps an SM
+            k = rotary_kernel<T, V, false, true, kMode, kGroup, 6>;
     void *argv[1] = {const_cast<Args *>(&p)};
     return launch(k, grid, 32 * kWarps, 0, stream, argv);
 }
 template <typename T, int V, int kMode>
 padoc_status launch_rows(const Args &p, bool adjacent, bool norm, dim3 grid, padoc_stream_t stream)
 {
-    // (8 lanes a head: 128 dims in bf16, 64 in fp32)
-    return p.group_log == 3 ? launch_group<T, V, kMode, 8>(p, adjacent, norm, grid, stream)
-                            : launch_group<T, V, kMode, 0>(p, adjacent, norm, grid, stream);
+    // (64, 128 and 256 dims in bf16, 64 and 128 in fp32; other heads, and bf16 ones in 8-byte vectors, take the general form)
+    if constexpr (V == 8)
+        if (p.group_log == 2) return launch_group<T, V, kMode, 4>(p, adjacent, norm, grid, stream);
+    if constexpr (V == 8 || sizeof(T) == 4) {
+        if (p.group_log == 3) return launch_group<T, V, kMode, 8>(p, adjacent, norm, grid, stream);
+        if (p.group_log == 4) return launch_group<T, V, kMode, 16>(p, adjacent, norm, grid, stream);
+    }
+    return launch_group<T, V, kMode, 0>(p, adjacent, norm, grid, stream);
 }
 
 template <int kMode>
@@ -333,18 +339,27 @@ int bwd_ctas(int64_t rows)
     return (int)(need < most ? need : most);
 }
 
-template <typename T, int V>
-padoc_status launch_bwd(const BwdArgs &p, bool adjacent, int ctas, padoc_stream_t stream)
+template <typename T, int V, int kGroup>
+padoc_status launch_bwd_group(const BwdArgs &p, bool adjacent, int ctas, padoc_stream_t stream)
 {
-    // (8 lanes a head: 128 dims in bf16, 64 in fp32)
-    auto *k = p.group_log == 3 ? (adjacent ? rotary_norm_bwd_kernel<T, V, true, 8> : rotary_norm_bwd_kernel<T, V, false, 8>)
-                               : (adjacent ? rotary_norm_bwd_kernel<T, V, true, 0> : rotary_norm_bwd_kernel<T, V, false, 0>);
+    auto *k = adjacent ? rotary_norm_bwd_kernel<T, V, true, kGroup> : rotary_norm_bwd_kernel<T, V, false, kGroup>;
     const size_t weights = (size_t)V << p.group_log << 4, ring = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>) + (size_t)kBwdWarps * (V / 2) * 32 * 16;
     const size_t sums = (size_t)kBwdWarps * 2 * p.sp.d * sizeof(float);
     const int smem = (int)(weights + ring > sums ? weights + ring : sums);
     const padoc_status st = padoc_set_max_smem((const void *)k, smem);
     void *argv[1] = {const_cast<BwdArgs *>(&p)};
     return st != PADOC_OK ? st : launch(k, dim3((unsigned)ctas), 32 * kBwdWarps, smem, stream, argv);
+}
+template <typename T, int V>
+padoc_status launch_bwd(const BwdArgs &p, bool adjacent, int ctas, padoc_stream_t stream)
+{
+    if constexpr (V == 8)
+        if (p.group_log == 2) return launch_bwd_group<T, V, 4>(p, adjacent, ctas, stream);
+    if constexpr (V == 8 || sizeof(T) == 4) {
+        if (p.group_log == 3) return launch_bwd_group<T, V, 8>(p, adjacent, ctas, stream);
+        if (p.group_log == 4) return launch_bwd_group<T, V, 16>(p, adjacent, ctas, stream);
+    }
+    return launch_bwd_group<T, V, 0>(p, adjacent, ctas, stream);
 }
 
 }  // namespace

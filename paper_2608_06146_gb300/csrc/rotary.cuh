@@ -1,10 +1,12 @@
 // rotary.cuh -- rotary positions with several axes and the per-head RMS norm before them, as device
 // helpers shared by the packed forward and backward, the append into the paged pool and the E4M3 append.
 //
-// A head of d dims is taken in chunks of 2 V dims, one lane each: V pairs of the rotated part, or 2 V
-// consecutive dims behind it. Lane chunk c holds two vectors of V elements: of pairs (i, i + R/2) the
-// dims c V and R/2 + c V, of adjacent pairs and of dims past R the dims 2 c V and 2 c V + V. In both
-// layouts its pairs are c V .. c V + V - 1, so a lane's V angles serve every head of its row.
+// A head of d dims is taken in chunks of 2 V dims, one lane each, as two vectors of V: chunk c holds the dims from
+// c V and from R/2 + c V on (R rotated dims), or, behind the rotated ones, the same of the remaining d - R. So the
+// lanes' vectors lie behind one another (side by side in a lane, each access would touch every sector for half of
+// it: the packed backward with norms 96 us instead of 62 for 26041 rows). Of pairs (i, i + R/2) a lane holds both
+// members, V pairs from c V on; of adjacent pairs V/2 from c V/2 and V/2 from R/4 + c V/2 on. A lane's V angles serve
+// every head of its row.
 #pragma once
 
 #include "common.cuh"
@@ -134,17 +136,23 @@ struct Place {
     int a, b;
     bool active, turned;
 };
-template <int V, bool kAdjacent>
+template <int V>
 __device__ __forceinline__ Place lane_place(int chunk, int d, int rot)
 {
     Place p;
     p.active = chunk * 2 * V < d;
     p.turned = chunk * 2 * V < rot;
-    const bool split = !kAdjacent && p.turned;
-    p.a = split ? chunk * V : chunk * 2 * V;
-    p.b = split ? rot / 2 + chunk * V : chunk * 2 * V + V;
+    p.a = p.turned ? chunk * V : rot / 2 + chunk * V;   // (R + (c - R / 2V) V)
+    p.b = p.a + (p.turned ? rot : d - rot) / 2;
     if (!p.active) p.a = p.b = 0;
     return p;
+}
+// The pair that a lane's angle j belongs to.
+template <int V, bool kAdjacent>
+__device__ __forceinline__ int lane_pair(int chunk, int j, int rot)
+{
+    if constexpr (!kAdjacent) return chunk * V + j;
+    else return chunk * (V / 2) + (j < V / 2 ? j : rot / 4 + j - V / 2);
 }
 
 // The rotation of a lane's V pairs by its angles; pairs (i, i + R / 2) on packed values, adjacent ones one by one.
@@ -218,7 +226,7 @@ __device__ __forceinline__ void scale_head(uint64_t (&a)[V / 2], uint64_t (&b)[V
 // The cosines and sines of a lane's V pairs at row `row`, as packed pairs; for the whole warp. The lanes that hold
 // the same chunk of different heads share the work (kGroup lanes a head, where known at compile time): each
 // computes V kGroup / 32 of the pairs and hands them to the others.
-template <int V, bool kFast, int kGroup>
+template <int V, bool kAdjacent, bool kFast, int kGroup>
 __device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__restrict__ pos, int64_t row, int chunk, bool turned,
                                             uint64_t (&c)[V / 2], uint64_t (&s)[V / 2])
 {
@@ -231,7 +239,7 @@ __device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__res
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) {
             co[j] = so[j] = 0.f;
-            if (turned) cos_sin<kFast>(sp.freq[chunk * V + lane / kGroup * kOwn + j], pos, sp, co[j], so[j]);
+            if (turned) cos_sin<kFast>(sp.freq[lane_pair<V, kAdjacent>(chunk, lane / kGroup * kOwn + j, sp.rot)], pos, sp, co[j], so[j]);
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -243,7 +251,7 @@ __device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__res
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             cj[j] = sj[j] = 0.f;   // (lanes past the head's dims take part in the arithmetic: their values must be finite)
-            if (turned) cos_sin<kFast>(sp.freq[chunk * V + j], pos, sp, cj[j], sj[j]);
+            if (turned) cos_sin<kFast>(sp.freq[lane_pair<V, kAdjacent>(chunk, j, sp.rot)], pos, sp, cj[j], sj[j]);
         }
     }
 #pragma unroll
@@ -306,25 +314,31 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
     }
     const int group = kGroup ? kGroup : 1 << p.group_log, heads = 32 / group;
     const int sub = lane / group, chunk = lane & (group - 1);
-    const Place pl = lane_place<V, kAdjacent>(chunk, p.sp.d, p.sp.rot);
-    const T *q = static_cast<const T *>(p.q) + row * p.q_stride, *k = static_cast<const T *>(p.k) + row * p.k_stride;
+    const Place pl = lane_place<V>(chunk, p.sp.d, p.sp.rot);
     const int nq = p.q ? p.hq : 0, turned = kMode == kQueries ? nq : nq + p.hkv, total = kMode == kAppend ? turned + p.hkv : turned;
-    const int first = part * p.steps * heads;
-    // Lanes past the last head or the head's dims load what another lane does and store nothing: the loop has no
-    // divergent branch but the stores'.
+    const int first = part * p.steps * heads, lane_at = sub * p.sp.d + pl.a, to_b = pl.b - pl.a;
+    // heads first + u heads + sub; a step of query heads alone has one address for the warp and the lane's place in it
+    const T *q = static_cast<const T *>(p.q) + row * p.q_stride + lane_at;
     Raw<T, V> ra[kSteps], rb[kSteps];
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
         if (u >= p.steps) break;
-        const int h = min(first + u * heads + sub, total - 1);
-        const T *src = h < nq ? q + h * p.sp.d : k + (h - nq) * p.sp.d;
-        if (kMode == kAppend && h >= turned) src = static_cast<const T *>(p.v) + row * p.v_stride + (h - turned) * p.sp.d;
-        ra[u] = load_raw<T, V>(src + pl.a);
-        rb[u] = load_raw<T, V>(src + pl.b);
+        const int h0 = first + u * heads;
+        const T *src = q + h0 * p.sp.d;
+        if (h0 + heads > nq) {
+            // Lanes past the last head or the head's dims load what another lane does and store nothing: the steps have no
+            // divergent branch but the stores'.
+            const int h = min(h0 + sub, total - 1) - sub;
+            if (h + sub < nq) src = q + h * p.sp.d;
+            else if (kMode != kAppend || h + sub < turned) src = static_cast<const T *>(p.k) + row * p.k_stride + lane_at + (h - nq) * p.sp.d;
+            else src = static_cast<const T *>(p.v) + row * p.v_stride + lane_at + (h - turned) * p.sp.d;
+        }
+        ra[u] = load_raw<T, V>(src);
+        rb[u] = load_raw<T, V>(src + to_b);
     }
     uint64_t c[V / 2], s[V / 2];
-    lane_angles<V, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, chunk, pl.turned, c, s);
-    T *q_out = static_cast<T *>(p.q_out) + i * p.q_out_stride;
+    lane_angles<V, kAdjacent, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, chunk, pl.turned, c, s);
+    T *q_out = static_cast<T *>(p.q_out) + i * p.q_out_stride + lane_at;
     // where the row's KV heads go, and the distance from one to the next
     int64_t k_at = 0, k_step = p.sp.d;
     if constexpr (kMode == kAppend) {
@@ -338,30 +352,34 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
         if (u >= p.steps) break;
-        const int h = first + u * heads + sub;
-        const bool here = h < total && pl.active, is_q = h < nq;
-        if (kMode == kAppend && h >= turned) {   // a value head: as it is
-            if (here) {
-                T *dst = static_cast<T *>(p.v_out) + k_at + (h - turned) * k_step;
-                *reinterpret_cast<Raw<T, V> *>(dst + pl.a) = ra[u];
-                *reinterpret_cast<Raw<T, V> *>(dst + pl.b) = rb[u];
+        const int h0 = first + u * heads, h = h0 + sub;
+        if (kMode == kAppend && h0 + heads > turned) {   // value heads: as they are
+            if (h >= turned && h < total && pl.active) {
+                T *dst = static_cast<T *>(p.v_out) + k_at + (h - turned) * k_step + pl.a;
+                *reinterpret_cast<Raw<T, V> *>(dst) = ra[u];
+                *reinterpret_cast<Raw<T, V> *>(dst + to_b) = rb[u];
             }
+            if (h0 >= turned) continue;
         }
-        if (kMode == kAppend && first + u * heads >= turned) continue;   // (the whole step)
         uint64_t a[V / 2], b[V / 2];
         unpack2(ra[u], a);
         unpack2(rb[u], b);
         if constexpr (kNorm) {
             const float r = norm_scale<V>(a, b, pl.active, p.sp, group);
-            const T *w = static_cast<const T *>(is_q ? p.sp.q_weight : p.sp.k_weight);
-            scale_head<V, T>(a, b, r, load_raw<T, V>(w + pl.a), load_raw<T, V>(w + pl.b));
+            const T *w = static_cast<const T *>(h < nq ? p.sp.q_weight : p.sp.k_weight) + pl.a;
+            scale_head<V, T>(a, b, r, load_raw<T, V>(w), load_raw<T, V>(w + to_b));
         }
         if (whole) turn_pairs<V, kAdjacent>(a, b, c, s);
         else if (pl.turned) turn_pairs<V, kAdjacent>(a, b, c, s);
-        if (here && h < turned) {
-            T *dst = is_q ? q_out + h * p.sp.d : static_cast<T *>(p.k_out) + k_at + (h - nq) * k_step;
-            store_vec2<V>(dst + pl.a, a);
-            store_vec2<V>(dst + pl.b, b);
+        T *dst = q_out + h0 * p.sp.d;
+        bool here = pl.active;
+        if (h0 + heads > nq) {
+            here = here && h < turned;
+            if (h >= nq) dst = static_cast<T *>(p.k_out) + k_at + (h - nq) * k_step + pl.a;
+        }
+        if (here) {
+            store_vec2<V>(dst, a);
+            store_vec2<V>(dst + to_b, b);
         }
     }
 }
