@@ -252,7 +252,9 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int32_t sl
     using namespace padoc_rotary_dev;
     const Args &p = a.rows;
     constexpr int kGroup = kD / (2 * V), kPassRows = 32 / kGroup, kPasses = kBlk / kPassRows;
-    const int lane = threadIdx.x & 31, sub = lane / kGroup, chunk = lane & (kGroup - 1);
+    const int lane = threadIdx.x & 31;
+    const Lane l = warp_lane<kGroup>(kGroup);
+    const int sub = l.sub, chunk = l.chunk;
     const int32_t slot0 = __shfl_sync(0xffffffffu, slot, from);
     const int r0 = slot0 & (kBlk - 1);
     const uint32_t run = __ballot_sync(0xffffffffu, lane >= from && lane < from + kBlk - r0 && slot == slot0 + (lane - from)) >> from;
@@ -261,7 +263,7 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int32_t sl
     if (!good) return;
     const bool is_v = unit >= p.hkv;
     const int g = is_v ? unit - p.hkv : unit;
-    const Place pl = lane_place<V>(chunk, kD, p.sp.rot);
+    const Place pl = lane_place<V>(chunk, true, kD, p.sp.rot);
     const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(is_v ? p.v : p.k) + g * kD;
     const int64_t stride = is_v ? p.v_stride : p.k_stride;
     Raw<__nv_bfloat16, V> ra[kPasses], rb[kPasses];
@@ -292,7 +294,7 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int32_t sl
         if (!is_v) {
             const int64_t at = __shfl_sync(0xffffffffu, row, from + j);
             if constexpr (kNorm) {
-                const float r = norm_scale<V>(za, zb, here, p.sp, kGroup);
+                const float r = norm_scale<V, kGroup>(za, zb, here, p.sp, l);
                 const __nv_bfloat16 *w = static_cast<const __nv_bfloat16 *>(p.sp.k_weight);
                 scale_head<V, __nv_bfloat16>(za, zb, r, load_raw<__nv_bfloat16, V>(w + pl.a), load_raw<__nv_bfloat16, V>(w + pl.b));
             }

@@ -37,7 +37,7 @@ struct BwdArgs {
     int64_t q_stride, k_stride;
     const int32_t *pos;
     int64_t rows;
-    int32_t hq, hkv, group_log;
+    int32_t hq, hkv, group;
     const void *dq_out, *dk_out;
     int64_t dq_out_stride, dk_out_stride;
     void *dq, *dk;
@@ -53,7 +53,7 @@ __device__ __forceinline__ void cp_async_vec(uint32_t dst, const void *src, uint
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-// The backward with the norm. Persistent CTAs, a warp per row, 32 / group heads a step. Registers hold
+// The backward with the norm. Persistent CTAs, a warp per row, as many heads a step as fit. Registers hold
 // the weights' gradient sums and the angles, so the rows' values come through shared memory: every lane copies its
 // own vectors kBwdStages steps ahead (cp.async) and reads them back itself, without a barrier. A CTA joins its
 // warps' sums in a fixed order and writes one partial row, which rotary_weight_grad_kernel adds up (no atomics:
@@ -61,7 +61,7 @@ __device__ __forceinline__ void cp_async_vec(uint32_t dst, const void *src, uint
 // The packed batch of 32768 rows (453 MB): 276 us with plain loads, one step at a time, at 178 registers; 115 us
 // through the ring with scalar arithmetic (2620 instructions a row); 76.8 us now (1390; 87% of the copy rate), bound
 // by the latency of a step's chain (two sums over the head) at the 16 warps an SM that the sums' registers leave.
-// kGroup: the lanes that share a head where known at compile time (0: group_log says).
+// kGroup: see Lane.
 template <typename T, int V, bool kAdjacent, int kGroup>
 __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(const __grid_constant__ BwdArgs p)
 {
@@ -71,23 +71,19 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     // [kBwdWarps][kBwdStages][4][32] vectors; at the end [kBwdWarps][2][d] sums
     extern __shared__ uint4 smem_raw[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int group = kGroup ? kGroup : 1 << p.group_log, heads = 32 / group;
-    const int sub = lane / group, chunk = lane & (group - 1);
-    const Place pl = lane_place<V>(chunk, p.sp.d, p.sp.rot);
+    const Lane l = warp_lane<kGroup>(p.group);
+    const int group = l.group, heads = l.heads, sub = l.sub, chunk = l.chunk;
+    const Place pl = lane_place<V>(chunk, l.used, p.sp.d, p.sp.rot);
     const int d = p.sp.d;
     Vec *ring = reinterpret_cast<Vec *>(smem_raw + 2 * kPairs * group) + (size_t)warp * kBwdStages * 4 * 32 + lane;
     pdl_wait_prerequisite();
     pdl_launch_dependents();
     for (int e = threadIdx.x; e < 2 * kPairs * group; e += 32 * kBwdWarps) {
         const int kind = e >= kPairs * group, piece = e / group - kind * kPairs;
-        const Place at = lane_place<V>(e & (group - 1), d, p.sp.rot);
-        float4 w4 = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (at.active) {
-            const T *w = static_cast<const T *>(kind ? p.sp.k_weight : p.sp.q_weight) +
-                         (piece < kPairs / 2 ? at.a + 4 * piece : at.b + 4 * (piece - kPairs / 2));
-            w4 = make_float4((float)w[0], (float)w[1], (float)w[2], (float)w[3]);
-        }
-        reinterpret_cast<float4 *>(smem_raw)[e] = w4;
+        const Place at = lane_place<V>(e % group, true, d, p.sp.rot);
+        const T *w = static_cast<const T *>(kind ? p.sp.k_weight : p.sp.q_weight) +
+                     (piece < kPairs / 2 ? at.a + 4 * piece : at.b + 4 * (piece - kPairs / 2));
+        reinterpret_cast<float4 *>(smem_raw)[e] = make_float4((float)w[0], (float)w[1], (float)w[2], (float)w[3]);
     }
     __syncthreads();
     // a CTA's rows lie behind one another (a grid apart they take 79.4 us instead of 76.8 for 32768 rows)
@@ -176,9 +172,9 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
                     s2 = f2_fma(xa[j], xa[j], f2_fma(xb[j], xb[j], s2));
                     d2 = f2_fma(f2_mul(a[j], wa[j]), xa[j], f2_fma(f2_mul(b[j], wb[j]), xb[j], d2));
                 }
-                float r = rsqrtf(group_sum(f2_sum(s2), group) * inv_d + p.sp.eps);
+                float r = rsqrtf(group_sum<kGroup>(f2_sum(s2), l) * inv_d + p.sp.eps);
                 if (sub >= left) r = 0.f;   // no head: its zeros must not meet an infinite scale
-                const float m = group_sum(f2_sum(d2), group) * r * inv_d;   // the mean of w g h
+                const float m = group_sum<kGroup>(f2_sum(d2), l) * r * inv_d;   // the mean of w g h
                 // with t = r g: dw += t x, dx = r (w g - h m) = w t - (r r m) x
                 const uint64_t r2 = f2_pack(r, r), c2 = f2_pack(-(r * r) * m, -(r * r) * m);
                 read_weights(wa, wb);
@@ -222,9 +218,18 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
         for (int j = 0; j < V; ++j) {
             float lo, hi;
             f2_unpack(acc_all[kind][j], lo, hi);
-            for (int m = group; m < 32; m <<= 1) {
-                lo += __shfl_xor_sync(0xffffffffu, lo, m);
-                hi += __shfl_xor_sync(0xffffffffu, hi, m);
+            if constexpr (kGroup != 0) {
+#pragma unroll
+                for (int m = kGroup; m < 32; m <<= 1) {
+                    lo += __shfl_xor_sync(0xffffffffu, lo, m);
+                    hi += __shfl_xor_sync(0xffffffffu, hi, m);
+                }
+            } else {   // the first head's lanes collect the others'
+                const float own_lo = lo, own_hi = hi;
+                for (int g = 1; g < heads; ++g) {
+                    lo += __shfl_sync(0xffffffffu, own_lo, chunk + g * group);
+                    hi += __shfl_sync(0xffffffffu, own_hi, chunk + g * group);
+                }
             }
             if (sub == 0 && pl.active)
                 *reinterpret_cast<float2 *>(sums + (warp * 2 + kind) * d + (j < kPairs ? pl.a + 2 * j : pl.b + 2 * (j - kPairs))) = make_float2(lo, hi);
@@ -312,10 +317,10 @@ padoc_status launch_rows(const Args &p, bool adjacent, bool norm, dim3 grid, pad
 {
     // (64, 128 and 256 dims in bf16, 64 and 128 in fp32; other heads, and bf16 ones in 8-byte vectors, take the general form)
     if constexpr (V == 8)
-        if (p.group_log == 2) return launch_group<T, V, kMode, 4>(p, adjacent, norm, grid, stream);
+        if (p.group == 4) return launch_group<T, V, kMode, 4>(p, adjacent, norm, grid, stream);
     if constexpr (V == 8 || sizeof(T) == 4) {
-        if (p.group_log == 3) return launch_group<T, V, kMode, 8>(p, adjacent, norm, grid, stream);
-        if (p.group_log == 4) return launch_group<T, V, kMode, 16>(p, adjacent, norm, grid, stream);
+        if (p.group == 8) return launch_group<T, V, kMode, 8>(p, adjacent, norm, grid, stream);
+        if (p.group == 16) return launch_group<T, V, kMode, 16>(p, adjacent, norm, grid, stream);
     }
     return launch_group<T, V, kMode, 0>(p, adjacent, norm, grid, stream);
 }
@@ -343,7 +348,7 @@ template <typename T, int V, int kGroup>
 padoc_status launch_bwd_group(const BwdArgs &p, bool adjacent, int ctas, padoc_stream_t stream)
 {
     auto *k = adjacent ? rotary_norm_bwd_kernel<T, V, true, kGroup> : rotary_norm_bwd_kernel<T, V, false, kGroup>;
-    const size_t weights = (size_t)V << p.group_log << 4, ring = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>) + (size_t)kBwdWarps * (V / 2) * 32 * 16;
+    const size_t weights = (size_t)V * p.group * 16, ring = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>) + (size_t)kBwdWarps * (V / 2) * 32 * 16;
     const size_t sums = (size_t)kBwdWarps * 2 * p.sp.d * sizeof(float);
     const int smem = (int)(weights + ring > sums ? weights + ring : sums);
     const padoc_status st = padoc_set_max_smem((const void *)k, smem);
@@ -354,10 +359,10 @@ template <typename T, int V>
 padoc_status launch_bwd(const BwdArgs &p, bool adjacent, int ctas, padoc_stream_t stream)
 {
     if constexpr (V == 8)
-        if (p.group_log == 2) return launch_bwd_group<T, V, 4>(p, adjacent, ctas, stream);
+        if (p.group == 4) return launch_bwd_group<T, V, 4>(p, adjacent, ctas, stream);
     if constexpr (V == 8 || sizeof(T) == 4) {
-        if (p.group_log == 3) return launch_bwd_group<T, V, 8>(p, adjacent, ctas, stream);
-        if (p.group_log == 4) return launch_bwd_group<T, V, 16>(p, adjacent, ctas, stream);
+        if (p.group == 8) return launch_bwd_group<T, V, 8>(p, adjacent, ctas, stream);
+        if (p.group == 16) return launch_bwd_group<T, V, 16>(p, adjacent, ctas, stream);
     }
     return launch_bwd_group<T, V, 0>(p, adjacent, ctas, stream);
 }
@@ -369,17 +374,10 @@ int vec_of(const padoc_rotary *r, padoc_dtype t)
     return t == PADOC_DTYPE_BF16 && r->head_dim % 16 == 0 && r->rotary_dim % 16 == 0 ? 8 : 4;
 }
 
-int group_log_of(int head_dim, int vec)
-{
-    int g = 0;
-    while ((2 * vec << g) < head_dim) ++g;
-    return g;
-}
-
 int split_rows(Args &p, int vec, int heads_total, int most_steps)
 {
-    p.group_log = group_log_of(p.sp.d, vec);
-    const int heads = 32 >> p.group_log;
+    p.group = group_of(p.sp.d, vec);
+    const int heads = 32 / p.group;
     const int steps = (heads_total + heads - 1) / heads, least = (steps + most_steps - 1) / most_steps;
     const int64_t want = ((int64_t)padoc_default_ctas() * 8 + p.count - 1) / p.count;
     const int parts = want < least ? least : want > steps ? steps : (int)want;
@@ -570,7 +568,7 @@ extern "C" padoc_status padoc_qk_rotary_bwd(const padoc_rotary *rot, const padoc
         p.dq_stride = dq_stride, p.dk_stride = dk_stride;
         p.part = (float *)workspace;
         const int vec = vec_of(rot, in->dtype);
-        p.group_log = group_log_of(d, vec);
+        p.group = group_of(d, vec);
         const bool adj = rot->adjacent != 0;
         st = in->dtype == PADOC_DTYPE_F32 ? launch_bwd<float, 4>(p, adj, ctas, stream)
              : vec == 8                   ? launch_bwd<__nv_bfloat16, 8>(p, adj, ctas, stream)

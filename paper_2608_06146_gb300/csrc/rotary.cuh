@@ -121,30 +121,58 @@ __device__ __forceinline__ void store_vec2(T *p, const uint64_t (&x)[V / 2])
     store_vec<V>(p, f);
 }
 
-// Sum over the `group` lanes (a power of two) that share a head.
-__device__ __forceinline__ float group_sum(float v, int group)
+// The lanes of a warp: `group` lanes share a head (kGroup of them where known at compile time, a power of two), as many
+// heads as fit side by side; lanes behind the last one hold no dims.
+struct Lane {
+    int group, heads, sub, chunk;
+    bool used;
+};
+template <int kGroup>
+__device__ __forceinline__ Lane warp_lane(int group)
 {
+    const int lane = threadIdx.x & 31;
+    Lane l;
+    l.group = kGroup ? kGroup : group;
+    l.heads = 32 / l.group;
+    l.sub = lane / l.group;
+    l.used = kGroup || l.sub < l.heads;
+    if (!l.used) l.sub = 0;
+    l.chunk = l.used ? lane - l.sub * l.group : 0;
+    return l;
+}
+// Sum over the lanes that share a head, the same bits in each of them.
+template <int kGroup>
+__device__ __forceinline__ float group_sum(float v, const Lane &l)
+{
+    if constexpr (kGroup != 0) {
 #pragma unroll
-    for (int m = 16; m > 0; m >>= 1)
-        if (m < group) v += __shfl_xor_sync(0xffffffffu, v, m);
+        for (int m = kGroup / 2; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    } else {   // after step m a lane has the sum of its own and the 2 m - 1 lanes behind it in the head
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1)
+            if (m < l.group) {
+                const float t = __shfl_down_sync(0xffffffffu, v, m);
+                if (l.chunk + m < l.group) v += t;
+            }
+        v = __shfl_sync(0xffffffffu, v, (threadIdx.x & 31) - l.chunk);
+    }
     return v;
 }
 
-// A lane's place in a head: the element offsets of its two vectors, whether they exist (else the offsets are 0) and
-// are rotated.
+// A lane's place in a head: the element offsets of its two vectors (lanes without dims: the first lane's), whether
+// they are its own and are rotated.
 struct Place {
     int a, b;
     bool active, turned;
 };
 template <int V>
-__device__ __forceinline__ Place lane_place(int chunk, int d, int rot)
+__device__ __forceinline__ Place lane_place(int chunk, bool used, int d, int rot)
 {
     Place p;
-    p.active = chunk * 2 * V < d;
+    p.active = used;
     p.turned = chunk * 2 * V < rot;
     p.a = p.turned ? chunk * V : rot / 2 + chunk * V;   // (R + (c - R / 2V) V)
     p.b = p.a + (p.turned ? rot : d - rot) / 2;
-    if (!p.active) p.a = p.b = 0;
     return p;
 }
 // The pair that a lane's angle j belongs to.
@@ -201,13 +229,13 @@ __device__ __forceinline__ float f2_sum(uint64_t v)
 
 // RMS norm of a head spread over `group` lanes: x r w with r = 1 / sqrt(mean x^2 + eps), sums in fp32. `here`:
 // the lane holds dims of a head.
-template <int V>
-__device__ __forceinline__ float norm_scale(const uint64_t (&a)[V / 2], const uint64_t (&b)[V / 2], bool here, const Spec &sp, int group)
+template <int V, int kGroup>
+__device__ __forceinline__ float norm_scale(const uint64_t (&a)[V / 2], const uint64_t (&b)[V / 2], bool here, const Spec &sp, const Lane &l)
 {
     uint64_t ss = 0;
 #pragma unroll
     for (int j = 0; j < V / 2; ++j) ss = f2_fma(a[j], a[j], f2_fma(b[j], b[j], ss));
-    return rsqrtf(group_sum(here ? f2_sum(ss) : 0.f, group) * (1.f / (float)sp.d) + sp.eps);
+    return rsqrtf(group_sum<kGroup>(here ? f2_sum(ss) : 0.f, l) * (1.f / (float)sp.d) + sp.eps);
 }
 template <int V, typename T>
 __device__ __forceinline__ void scale_head(uint64_t (&a)[V / 2], uint64_t (&b)[V / 2], float r, const Raw<T, V> &rwa, const Raw<T, V> &rwb)
@@ -250,7 +278,7 @@ __device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__res
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            cj[j] = sj[j] = 0.f;   // (lanes past the head's dims take part in the arithmetic: their values must be finite)
+            cj[j] = sj[j] = 0.f;
             if (turned) cos_sin<kFast>(sp.freq[lane_pair<V, kAdjacent>(chunk, j, sp.rot)], pos, sp, cj[j], sj[j]);
         }
     }
@@ -271,7 +299,7 @@ struct Args {
     int32_t hq, hkv;
     void *q_out, *k_out;
     int64_t q_out_stride, k_out_stride;
-    int32_t group_log, steps;               // log2 of the lanes per head; steps of a part
+    int32_t group, steps;                   // lanes per head; steps of a part
     // append
     void *v_out;                            // with k_out: the pool's arrays
     const int32_t *src_rows, *slots;
@@ -291,10 +319,10 @@ enum { kPacked = 0, kAppend = 1, kQueries = 2 };
 // 12.7 / 11.5; without it 672 3.3 / 2.8, 4001 10.6 / 9.4.
 constexpr int steps_of(int mode) { return mode == kAppend ? 3 : 5; }
 
-// One warp's work: part `part` of row i, p.steps steps of 32 / group heads, at most kSteps. All of the part's loads
+// One warp's work: part `part` of row i, p.steps steps of as many heads as fit a warp, at most kSteps. All of the part's loads
 // are issued before its angles are computed. Bound by HBM in large calls: every element is read once and written
 // once.
-// kGroup: the lanes that share a head where known at compile time (0: group_log says).
+// kGroup: see Lane.
 template <typename T, int V, bool kAdjacent, bool kNorm, int kMode, int kGroup>
 __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
 {
@@ -312,9 +340,9 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
         }
         slot = (uint32_t)at;
     }
-    const int group = kGroup ? kGroup : 1 << p.group_log, heads = 32 / group;
-    const int sub = lane / group, chunk = lane & (group - 1);
-    const Place pl = lane_place<V>(chunk, p.sp.d, p.sp.rot);
+    const Lane l = warp_lane<kGroup>(p.group);
+    const int heads = l.heads, sub = l.sub;
+    const Place pl = lane_place<V>(l.chunk, l.used, p.sp.d, p.sp.rot);
     const int nq = p.q ? p.hq : 0, turned = kMode == kQueries ? nq : nq + p.hkv, total = kMode == kAppend ? turned + p.hkv : turned;
     const int first = part * p.steps * heads, lane_at = sub * p.sp.d + pl.a, to_b = pl.b - pl.a;
     // heads first + u heads + sub; a step of query heads alone has one address for the warp and the lane's place in it
@@ -326,8 +354,8 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
         const int h0 = first + u * heads;
         const T *src = q + h0 * p.sp.d;
         if (h0 + heads > nq) {
-            // Lanes past the last head or the head's dims load what another lane does and store nothing: the steps have no
-            // divergent branch but the stores'.
+            // Lanes past the last head load what another lane does and store nothing: the steps have no divergent
+            // branch but the stores'.
             const int h = min(h0 + sub, total - 1) - sub;
             if (h + sub < nq) src = q + h * p.sp.d;
             else if (kMode != kAppend || h + sub < turned) src = static_cast<const T *>(p.k) + row * p.k_stride + lane_at + (h - nq) * p.sp.d;
@@ -337,7 +365,7 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
         rb[u] = load_raw<T, V>(src + to_b);
     }
     uint64_t c[V / 2], s[V / 2];
-    lane_angles<V, kAdjacent, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, chunk, pl.turned, c, s);
+    lane_angles<V, kAdjacent, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, l.chunk, pl.turned, c, s);
     T *q_out = static_cast<T *>(p.q_out) + i * p.q_out_stride + lane_at;
     // where the row's KV heads go, and the distance from one to the next
     int64_t k_at = 0, k_step = p.sp.d;
@@ -365,7 +393,7 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
         unpack2(ra[u], a);
         unpack2(rb[u], b);
         if constexpr (kNorm) {
-            const float r = norm_scale<V>(a, b, pl.active, p.sp, group);
+            const float r = norm_scale<V, kGroup>(a, b, pl.active, p.sp, l);
             const T *w = static_cast<const T *>(h < nq ? p.sp.q_weight : p.sp.k_weight) + pl.a;
             scale_head<V, T>(a, b, r, load_raw<T, V>(w), load_raw<T, V>(w + to_b));
         }
@@ -387,9 +415,9 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
 // Elements of a lane's vectors: 16 bytes where the rotated and the other dims come in whole chunks of
 // them, else 8 bytes (bf16 heads whose dims are an odd multiple of 8).
 int vec_of(const padoc_rotary *rot, padoc_dtype dtype);
-// log2 of the lanes that share a head.
-int group_log_of(int head_dim, int vec);
-// Sets group_log and steps; returns the parts of a row: as few as most_steps allows when the rows give every SM 8 warps,
+// Lanes that share a head.
+inline int group_of(int head_dim, int vec) { return head_dim / (2 * vec); }
+// Sets group and steps; returns the parts of a row: as few as most_steps allows when the rows give every SM 8 warps,
 // else as many as it takes to have them (at 5 steps a part, 672 rows of 20 heads: 3.9 us in two parts, 4.6 in one,
 // 4.3 in three; 2617 rows: 5.4 in one, 5.6 in two; one row: 2.3 in five, 3.9 in one).
 int split_rows(Args &p, int vec, int heads_total, int most_steps);
