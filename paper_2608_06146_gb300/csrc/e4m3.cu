@@ -300,7 +300,7 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int32_t sl
             }
             if (here && pl.turned) {
                 uint64_t c[V / 2], s[V / 2];
-                lane_angles<V, kAdjacent, true, 0>(p.sp, p.pos, at, chunk, true, c, s);   // (a row a group: nothing to share)
+                own_angles<V, kAdjacent, true>(p.sp, p.pos, at, chunk, c, s);
                 turn_pairs<V, kAdjacent>(za, zb, c, s);
             }
         }

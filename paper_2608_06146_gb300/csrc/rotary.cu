@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     int stage = 0;
     for (int64_t row = first; row < row_end; row += kBwdWarps) {
         uint64_t c[kPairs], s[kPairs];
-        lane_angles<V, kAdjacent, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, chunk, pl.turned, c, s);
+        lane_angles<V, kAdjacent, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, l, pl.turned, c, s);
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
             const ulonglong2 *w = reinterpret_cast<const ulonglong2 *>(smem_raw) + kind * kPairs * group + chunk;

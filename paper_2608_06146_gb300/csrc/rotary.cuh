@@ -252,40 +252,59 @@ __device__ __forceinline__ void scale_head(uint64_t (&a)[V / 2], uint64_t (&b)[V
 }
 
 // The cosines and sines of a lane's V pairs at row `row`, as packed pairs; for the whole warp. The lanes that hold
-// the same chunk of different heads share the work (kGroup lanes a head, where known at compile time): each
-// computes V kGroup / 32 of the pairs and hands them to the others.
+// the same chunk of different heads share the work where there are enough of them: each computes kOwn pairs and
+// hands them to the others.
+template <int V, bool kAdjacent, bool kFast, int kOwn>
+__device__ __forceinline__ void shared_angles(const Spec &sp, const int32_t *__restrict__ pos, const Lane &l, bool turned, float (&cj)[V], float (&sj)[V])
+{
+    float co[kOwn], so[kOwn];
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+        co[j] = so[j] = 0.f;
+        if (turned && l.sub * kOwn < V) cos_sin<kFast>(sp.freq[lane_pair<V, kAdjacent>(l.chunk, l.sub * kOwn + j, sp.rot)], pos, sp, co[j], so[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int from = j / kOwn * l.group + l.chunk;
+        cj[j] = __shfl_sync(0xffffffffu, co[j % kOwn], from);
+        sj[j] = __shfl_sync(0xffffffffu, so[j % kOwn], from);
+    }
+}
 template <int V, bool kAdjacent, bool kFast, int kGroup>
-__device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__restrict__ pos, int64_t row, int chunk, bool turned,
+__device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__restrict__ pos, int64_t row, const Lane &l, bool turned,
                                             uint64_t (&c)[V / 2], uint64_t (&s)[V / 2])
 {
     pos += row * sp.axes;
     float cj[V], sj[V];
-    if constexpr (kGroup != 0 && kGroup * V >= 32) {
-        constexpr int kOwn = kGroup * V / 32;
-        const int lane = threadIdx.x & 31;
-        float co[kOwn], so[kOwn];
-#pragma unroll
-        for (int j = 0; j < kOwn; ++j) {
-            co[j] = so[j] = 0.f;
-            if (turned) cos_sin<kFast>(sp.freq[lane_pair<V, kAdjacent>(chunk, lane / kGroup * kOwn + j, sp.rot)], pos, sp, co[j], so[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int from = j / kOwn * kGroup + chunk;
-            cj[j] = __shfl_sync(0xffffffffu, co[j % kOwn], from);
-            sj[j] = __shfl_sync(0xffffffffu, so[j % kOwn], from);
-        }
+    if constexpr (kGroup * V >= 32) {
+        shared_angles<V, kAdjacent, kFast, kGroup * V / 32>(sp, pos, l, turned, cj, sj);
+    } else if (kGroup == 0 && l.heads * 2 >= V) {
+        shared_angles<V, kAdjacent, kFast, 2>(sp, pos, l, turned, cj, sj);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             cj[j] = sj[j] = 0.f;
-            if (turned) cos_sin<kFast>(sp.freq[lane_pair<V, kAdjacent>(chunk, j, sp.rot)], pos, sp, cj[j], sj[j]);
+            if (turned) cos_sin<kFast>(sp.freq[lane_pair<V, kAdjacent>(l.chunk, j, sp.rot)], pos, sp, cj[j], sj[j]);
         }
     }
 #pragma unroll
     for (int j = 0; j < V / 2; ++j) {
         c[j] = f2_pack(cj[2 * j], cj[2 * j + 1]);
         s[j] = f2_pack(sj[2 * j], sj[2 * j + 1]);
+    }
+}
+// The same where every head of the warp has a row of its own.
+template <int V, bool kAdjacent, bool kFast>
+__device__ __forceinline__ void own_angles(const Spec &sp, const int32_t *__restrict__ pos, int64_t row, int chunk, uint64_t (&c)[V / 2], uint64_t (&s)[V / 2])
+{
+    pos += row * sp.axes;
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+        float c0, c1, s0, s1;
+        cos_sin<kFast>(sp.freq[lane_pair<V, kAdjacent>(chunk, 2 * j, sp.rot)], pos, sp, c0, s0);
+        cos_sin<kFast>(sp.freq[lane_pair<V, kAdjacent>(chunk, 2 * j + 1, sp.rot)], pos, sp, c1, s1);
+        c[j] = f2_pack(c0, c1);
+        s[j] = f2_pack(s0, s1);
     }
 }
 
@@ -365,7 +384,7 @@ __device__ __forceinline__ void row_part(const Args &p, int64_t i, int part)
         rb[u] = load_raw<T, V>(src + to_b);
     }
     uint64_t c[V / 2], s[V / 2];
-    lane_angles<V, kAdjacent, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, l.chunk, pl.turned, c, s);
+    lane_angles<V, kAdjacent, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, l, pl.turned, c, s);
     T *q_out = static_cast<T *>(p.q_out) + i * p.q_out_stride + lane_at;
     // where the row's KV heads go, and the distance from one to the next
     int64_t k_at = 0, k_step = p.sp.d;
