@@ -59,8 +59,10 @@ __device__ __forceinline__ void cp_async_vec(uint32_t dst, const void *src, uint
 // warps' sums in a fixed order and writes one partial row, which rotary_weight_grad_kernel adds up (no atomics:
 // the same call gives the same bits). Arithmetic is on packed pairs, weights come from shared memory in fp32.
 // The packed batch of 32768 rows (453 MB): 276 us with plain loads, one step at a time, at 178 registers; 115 us
-// through the ring with scalar arithmetic (2620 instructions a row); 76.8 us now (1390; 87% of the copy rate), bound
-// by the latency of a step's chain (two sums over the head) at the 16 warps an SM that the sums' registers leave.
+// through the ring with scalar arithmetic (2620 instructions a row); 76.3 us now (87% of the copy rate), bound by the
+// latency of a step's chain (two sums over the head) at the 16 warps an SM that the sums' registers leave. Steps of
+// query and of key heads apart take 74.4 us there, but 79.9 instead of 69.7 at 7 + 1 heads and 95 instead of 87 at
+// 80 dims, where they leave lanes without a head.
 // kGroup: see Lane.
 template <typename T, int V, bool kAdjacent, int kGroup>
 __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(const __grid_constant__ BwdArgs p)
@@ -86,14 +88,14 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
         reinterpret_cast<float4 *>(smem_raw)[e] = make_float4((float)w[0], (float)w[1], (float)w[2], (float)w[3]);
     }
     __syncthreads();
-    // a CTA's rows lie behind one another (a grid apart they take 79.4 us instead of 76.8 for 32768 rows)
+    // a CTA's rows lie behind one another (a grid apart: 3% slower)
     const int64_t first = p.rows * blockIdx.x / gridDim.x + warp, row_end = p.rows * (blockIdx.x + 1) / gridDim.x;
 
-    // the next step to be copied: its row, its kind's heads from it on, its addresses (of the lane's first vectors),
-    // and its stage; lanes without a head there get zeros
+    // the next step to be copied: its row and first head (the queries', then the keys'), the addresses of the lane's
+    // first vectors there (of a query head), and its stage; lanes without a head there get zeros
+    const int total = p.hq + p.hkv;
     int64_t ahead_row = first;
-    bool ahead_k = false;
-    int ahead_left = p.hq;
+    int ahead_head = 0;
     uint32_t ahead_at = smem_u32(ring);
     const uint32_t ring_end = ahead_at + kBwdStages * 4 * 32 * (uint32_t)sizeof(Vec);
     const int lane_at = sub * d + pl.a, to_b = pl.b - pl.a, step_at = heads * d;
@@ -102,21 +104,25 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     auto copy_ahead = [&]() {
         if (ahead_row < row_end) {
             constexpr uint32_t kNext = 32 * sizeof(Vec);
-            const uint32_t bytes = pl.active && sub < ahead_left ? (uint32_t)sizeof(Vec) : 0u;
-            cp_async_vec<sizeof(Vec)>(ahead_at, ax, bytes);
-            cp_async_vec<sizeof(Vec)>(ahead_at + kNext, ax + to_b, bytes);
-            cp_async_vec<sizeof(Vec)>(ahead_at + 2 * kNext, ag, bytes);
-            cp_async_vec<sizeof(Vec)>(ahead_at + 3 * kNext, ag + to_b, bytes);
+            const uint32_t bytes = pl.active && ahead_head + sub < total ? (uint32_t)sizeof(Vec) : 0u;
+            const T *x = ax, *g = ag;
+            if (ahead_head + heads > p.hq && ahead_head + sub >= p.hq) {
+                const int at = (ahead_head - p.hq) * d + lane_at;
+                x = static_cast<const T *>(p.k) + ahead_row * p.k_stride + at;
+                g = static_cast<const T *>(p.dk_out) + ahead_row * p.dk_out_stride + at;
+            }
+            cp_async_vec<sizeof(Vec)>(ahead_at, x, bytes);
+            cp_async_vec<sizeof(Vec)>(ahead_at + kNext, x + to_b, bytes);
+            cp_async_vec<sizeof(Vec)>(ahead_at + 2 * kNext, g, bytes);
+            cp_async_vec<sizeof(Vec)>(ahead_at + 3 * kNext, g + to_b, bytes);
             ax += step_at;
             ag += step_at;
-            ahead_left -= heads;
-            if (ahead_left <= 0) {   // on to the row's key heads, or to the next row's query heads
-                ahead_k = !ahead_k;
-                ahead_row += ahead_k ? 0 : kBwdWarps;
-                ahead_left = ahead_k ? p.hkv : p.hq;
-                ax = (ahead_k ? static_cast<const T *>(p.k) + ahead_row * p.k_stride : static_cast<const T *>(p.q) + ahead_row * p.q_stride) + lane_at;
-                ag = (ahead_k ? static_cast<const T *>(p.dk_out) + ahead_row * p.dk_out_stride
-                              : static_cast<const T *>(p.dq_out) + ahead_row * p.dq_out_stride) + lane_at;
+            ahead_head += heads;
+            if (ahead_head >= total) {
+                ahead_head = 0;
+                ahead_row += kBwdWarps;
+                ax = static_cast<const T *>(p.q) + ahead_row * p.q_stride + lane_at;
+                ag = static_cast<const T *>(p.dq_out) + ahead_row * p.dq_out_stride + lane_at;
             }
         }
         cp_async_commit();
@@ -140,9 +146,12 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
     for (int64_t row = first; row < row_end; row += kBwdWarps) {
         uint64_t c[kPairs], s[kPairs];
         lane_angles<V, kAdjacent, sizeof(T) == 2, kGroup>(p.sp, p.pos, row, l, pl.turned, c, s);
-#pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {
-            const ulonglong2 *w = reinterpret_cast<const ulonglong2 *>(smem_raw) + kind * kPairs * group + chunk;
+        T *out_q = static_cast<T *>(p.dq) + row * p.dq_stride + lane_at;
+#pragma unroll 1
+        for (int h0 = 0; h0 < total; h0 += heads, out_q += step_at) {
+            cp_async_wait<kBwdStages - 1>();
+            const bool is_q = h0 + sub < p.hq;
+            const ulonglong2 *w = reinterpret_cast<const ulonglong2 *>(smem_raw) + (is_q ? 0 : kPairs * group) + chunk;
             auto read_weights = [&](uint64_t(&wa)[kPairs], uint64_t(&wb)[kPairs]) {
 #pragma unroll
                 for (int j = 0; j < kPairs / 2; ++j) {
@@ -151,55 +160,59 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(cons
                     wb[2 * j] = b.x, wb[2 * j + 1] = b.y;
                 }
             };
-            T *out = kind ? static_cast<T *>(p.dk) + row * p.dk_stride : static_cast<T *>(p.dq) + row * p.dq_stride;
-            out += lane_at;
-#pragma unroll 1
-            for (int left = kind ? p.hkv : p.hq; left > 0; left -= heads, out += heads * d) {
-                cp_async_wait<kBwdStages - 1>();
-                const bool here = sub < left && pl.active;
-                const Vec *in = ring + stage * 4 * 32;
-                uint64_t xa[kPairs], xb[kPairs], a[kPairs], b[kPairs], wa[kPairs], wb[kPairs];
-                unpack2(in[0], xa);
-                unpack2(in[32], xb);
-                unpack2(in[64], a);
-                unpack2(in[96], b);
-                if (whole) turn_pairs<V, kAdjacent>(a, b, c, s);
-                else if (pl.turned) turn_pairs<V, kAdjacent>(a, b, c, s);
-                read_weights(wa, wb);
-                uint64_t s2 = 0, d2 = 0;
+            const Vec *in = ring + stage * 4 * 32;
+            uint64_t xa[kPairs], xb[kPairs], a[kPairs], b[kPairs], wa[kPairs], wb[kPairs];
+            unpack2(in[0], xa);
+            unpack2(in[32], xb);
+            unpack2(in[64], a);
+            unpack2(in[96], b);
+            if (whole) turn_pairs<V, kAdjacent>(a, b, c, s);
+            else if (pl.turned) turn_pairs<V, kAdjacent>(a, b, c, s);
+            read_weights(wa, wb);
+            uint64_t s2 = 0, d2 = 0;
 #pragma unroll
-                for (int j = 0; j < kPairs; ++j) {
-                    s2 = f2_fma(xa[j], xa[j], f2_fma(xb[j], xb[j], s2));
-                    d2 = f2_fma(f2_mul(a[j], wa[j]), xa[j], f2_fma(f2_mul(b[j], wb[j]), xb[j], d2));
-                }
-                float r = rsqrtf(group_sum<kGroup>(f2_sum(s2), l) * inv_d + p.sp.eps);
-                if (sub >= left) r = 0.f;   // no head: its zeros must not meet an infinite scale
-                const float m = group_sum<kGroup>(f2_sum(d2), l) * r * inv_d;   // the mean of w g h
-                // with t = r g: dw += t x, dx = r (w g - h m) = w t - (r r m) x
-                const uint64_t r2 = f2_pack(r, r), c2 = f2_pack(-(r * r) * m, -(r * r) * m);
-                read_weights(wa, wb);
-#pragma unroll
-                for (int j = 0; j < kPairs; ++j) {
-                    const uint64_t ta = f2_mul(a[j], r2), tb = f2_mul(b[j], r2);
-                    if (kind == 0) {
-                        acc[j] = f2_fma(ta, xa[j], acc[j]);
-                        acc[kPairs + j] = f2_fma(tb, xb[j], acc[kPairs + j]);
-                    } else {
-                        ulonglong2 v = acc_k[j * 32];
-                        v.x = f2_fma(ta, xa[j], v.x);
-                        v.y = f2_fma(tb, xb[j], v.y);
-                        acc_k[j * 32] = v;
-                    }
-                    a[j] = f2_fma(ta, wa[j], f2_mul(xa[j], c2));
-                    b[j] = f2_fma(tb, wb[j], f2_mul(xb[j], c2));
-                }
-                if (here) {
-                    store_vec2<V>(out, a);
-                    store_vec2<V>(out + to_b, b);
-                }
-                copy_ahead();   // into the stage just read
-                stage = stage + 1 == kBwdStages ? 0 : stage + 1;
+            for (int j = 0; j < kPairs; ++j) {
+                s2 = f2_fma(xa[j], xa[j], f2_fma(xb[j], xb[j], s2));
+                d2 = f2_fma(f2_mul(a[j], wa[j]), xa[j], f2_fma(f2_mul(b[j], wb[j]), xb[j], d2));
             }
+            float r = rsqrtf(group_sum<kGroup>(f2_sum(s2), l) * inv_d + p.sp.eps);
+            if (h0 + sub >= total) r = 0.f;   // no head: its zeros must not meet an infinite scale
+            const float m = group_sum<kGroup>(f2_sum(d2), l) * r * inv_d;   // the mean of w g h
+            // with t = r g: dw += t x, dx = r (w g - h m) = w t - (r r m) x
+            const uint64_t r2 = f2_pack(r, r), c2 = f2_pack(-(r * r) * m, -(r * r) * m);
+            read_weights(wa, wb);
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                a[j] = f2_mul(a[j], r2);
+                b[j] = f2_mul(b[j], r2);
+            }
+            if (is_q) {
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) {
+                    acc[j] = f2_fma(a[j], xa[j], acc[j]);
+                    acc[kPairs + j] = f2_fma(b[j], xb[j], acc[kPairs + j]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) {
+                    ulonglong2 v = acc_k[j * 32];
+                    v.x = f2_fma(a[j], xa[j], v.x);
+                    v.y = f2_fma(b[j], xb[j], v.y);
+                    acc_k[j * 32] = v;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                a[j] = f2_fma(a[j], wa[j], f2_mul(xa[j], c2));
+                b[j] = f2_fma(b[j], wb[j], f2_mul(xb[j], c2));
+            }
+            if (pl.active && h0 + sub < total) {
+                T *out = is_q ? out_q : static_cast<T *>(p.dk) + row * p.dk_stride + (h0 - p.hq) * d + lane_at;
+                store_vec2<V>(out, a);
+                store_vec2<V>(out + to_b, b);
+            }
+            copy_ahead();   // into the stage just read
+            stage = stage + 1 == kBwdStages ? 0 : stage + 1;
         }
     }
     cp_async_wait<0>();
