@@ -361,10 +361,11 @@ template <typename T, int V, int kGroup>
 padoc_status launch_bwd_group(const BwdArgs &p, bool adjacent, int ctas, padoc_stream_t stream)
 {
     auto *k = adjacent ? rotary_norm_bwd_kernel<T, V, true, kGroup> : rotary_norm_bwd_kernel<T, V, false, kGroup>;
-    const size_t weights = (size_t)V * p.group * 16, ring = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>) + (size_t)kBwdWarps * (V / 2) * 32 * 16;
-    const size_t sums = (size_t)kBwdWarps * 2 * p.sp.d * sizeof(float);
-    const int smem = (int)(weights + ring > sums ? weights + ring : sums);
-    const padoc_status st = padoc_set_max_smem((const void *)k, smem);
+    constexpr size_t kRing = (size_t)kBwdWarps * kBwdStages * 4 * 32 * sizeof(Raw<T, V>), kSums = (size_t)kBwdWarps * (V / 2) * 32 * 16;
+    static_assert(kRing >= (size_t)kBwdWarps * 2 * 256 * sizeof(float), "the joined sums fit where the ring was");
+    const int smem = (int)((size_t)V * p.group * 16 + kRing + kSums);
+    // the limit for the longest heads, whatever this call's: it stays with the kernel, and a later call may need more
+    const padoc_status st = padoc_set_max_smem((const void *)k, (int)((size_t)V * 32 * 16 + kRing + kSums));
     void *argv[1] = {const_cast<BwdArgs *>(&p)};
     return st != PADOC_OK ? st : launch(k, dim3((unsigned)ctas), 32 * kBwdWarps, smem, stream, argv);
 }

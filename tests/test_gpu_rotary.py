@@ -193,6 +193,23 @@ def test_gradients_against_differences_of_the_forward():
             assert abs((two[0] - two[1]) / (2 * h) - float(g[j])) < 1e-2 * max(1, abs(float(g[j])))
 
 
+def test_backward_of_short_heads_between_long_ones():
+    # heads of several sizes share a kernel, whose shared memory differs: the limit set for one serves the others
+    for d in (200, 40, 200, 248, 24, 248):
+        sp = Spec(d, d, 8, 1, False, True, BF16)
+        rng = np.random.default_rng(d)
+        pos = positions(rng, 3, 1)
+        _, q, k, _ = qkv(rng, 3, 2, 1, d, BF16)
+        _, dqo, dko, _ = qkv(rng, 3, 2, 1, d, BF16)
+        dq, dk = (torch.empty((3, h, d), dtype=BF16, device=DEV) for h in (2, 1))
+        dqw, dkw = torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+        ws = torch.empty(pa.padoc_qk_rotary_bwd_workspace_size(sp.dev, 3), dtype=torch.uint8, device=DEV)
+        pa.padoc_qk_rotary_bwd(sp.dev, dqo, dko, pos, dq, dk, q, k, dqw, dkw, ws)
+        dx, size, dw, terms = sp.backward(dqo, q, sp.qw, pos)
+        check(dq, dx, size, BWD, "dq")
+        check(dqw, dw, terms, DW, "dq_weight")
+
+
 def test_no_rows():
     sp = Spec(0, 128, 128, 3, False, True, BF16)
     e = lambda h: torch.empty((0, h, 128), dtype=BF16, device=DEV)
