@@ -169,7 +169,6 @@ class MaskedParallelLoop:
                                          tc_ctas, warp_ctas)
         self.device, self.dtype = device, dtype
         self.rotary = rotary
-        self._rotary_pos = None
         self.num_q_heads, self.head_dim = num_q_heads, head_dim
         self._stage = [None, None]
         self._stage_free = [torch.cuda.Event(), torch.cuda.Event()]
@@ -285,12 +284,11 @@ class MaskedParallelLoop:
         """step() as one library call (padoc_mpd_runner_step): row_of_stream is an int32 numpy table
         of each live stream's source row indexed by stream id; out [rows][Hq][d] and lse [rows][Hq]
         (rows at least the live streams) receive the outputs in step order. Returns (C, stream ids
-        int32 [C], valid until the next step); end the step with end_step."""
+        int32 [C], valid until the next step); end the step with end_step. With rotary, pos_src as in step."""
         if self._runner is None:
             self._runner = pa.MpdRunner(self.mpd, self.cfg, self._pool)
-        if self.rotary is not None and self._rotary_pos is not pos_src:
+        if self.rotary is not None:   # every step: the same tensor object may have other memory by now
             self._runner.set_rotary(self.rotary, pos_src)
-            self._rotary_pos = pos_src
         n, ids = self._runner.step(k_src, v_src, q_src, row_of_stream, scale, out, lse, stream)
         self.h2d_bytes = self._runner.upload_bytes
         return n, ids
@@ -347,7 +345,7 @@ class MaskedParallelLoop:
         self.mpd.resize(num_blocks)
         if self._runner is not None:
             self._runner.close()
-            self._runner = self._rotary_pos = None
+            self._runner = None
         for t in (self.k_pool, self.v_pool):
             t.record_stream(stream)
         self.k_pool, self.v_pool = k_pool, v_pool

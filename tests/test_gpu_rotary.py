@@ -944,3 +944,29 @@ def test_forked_candidates_decode_like_their_origin_and_then_apart(mode):
         at = torch.cat([torch.arange(hist), hist + i * more + torch.arange(more)])
         ro, _ = oracle.prefill_dense([page], qr.cpu()[at], kr.cpu()[at], v.cpu()[at], 128 ** -0.5)
         assert np.abs(f64(torch.stack(got[s])) - ro[hist:]).max() <= 1.5e-2
+
+
+def test_loop_without_positions_is_refused_and_positions_may_change_their_memory():
+    sp = Spec(33, 128, 128, 1, False, True, BF16)
+    _, q, k, v = qkv(np.random.default_rng(33), 4, 16, 2, 128, BF16)
+    q, k, v = (t.contiguous() for t in (q, k, v))
+    lp = MaskedParallelLoop(8, 16, 2, 128, BF16, DEV, rotary=sp.dev)
+    lp.add_page(0, 0, False, k, v, np.zeros(0, np.int32))
+    out, lse = torch.empty((4, 16, 128), dtype=BF16, device=DEV), torch.empty((4, 16), device=DEV)
+    row = np.zeros(4, np.int32)
+    with pytest.raises(ValueError):
+        lp.run_step(k, v, q, row, 0.1, out, lse)
+    pos = torch.arange(4, dtype=torch.int32, device=DEV)[:, None].contiguous()
+    later = pos + 1000
+    lp.run_step(k, v, q, row, 0.1, out, lse, pos_src=pos)
+    lp.end_step(num_streams=1)
+    kr, qr = [torch.empty_like(k) for _ in range(2)], torch.empty_like(q)
+    pa.padoc_qk_rotary(sp.dev, q, k, pos, qr, kr[0])
+    pa.padoc_qk_rotary(sp.dev, q, k, later, qr, kr[1])
+    before = pos.data_ptr()
+    pos.set_(later)                                       # the same object over other memory
+    assert pos.data_ptr() != before
+    lp.run_step(k, v, q, row, 0.1, out, lse, pos_src=pos)
+    lp.end_step(num_streams=1)
+    pa.padoc_check_device_errors()
+    assert torch.equal(lp.k_pool[0, :, 0], kr[0][0]) and torch.equal(lp.k_pool[0, :, 1], kr[1][0])
