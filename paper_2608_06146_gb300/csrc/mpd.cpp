@@ -721,7 +721,19 @@ extern "C" padoc_status padoc_mpd_runner_step(padoc_mpd_runner *r, const padoc_m
         return PADOC_ERR_INVALID_ARGUMENT;
     if (C > 0 && (int64_t)a->num_stream_ids < (int64_t)m->streams.size()) return PADOC_ERR_INVALID_ARGUMENT;
     if (r->pool.num_blocks < m->num_blocks) return PADOC_ERR_INVALID_ARGUMENT;   // (the scheduler was resized)
-    if (C > 0 && r->rotate && a->src_total > r->pos_rows) return PADOC_ERR_INVALID_ARGUMENT;
+    padoc_qkv_rows in = {};
+    in.q = a->q_src, in.k = a->k_src, in.v = a->v_src;
+    in.num_q_heads = r->cfg.num_q_heads, in.num_kv_heads = r->cfg.num_kv_heads;
+    in.q_stride = (int64_t)in.num_q_heads * r->cfg.head_dim;
+    in.k_stride = in.v_stride = (int64_t)in.num_kv_heads * r->cfg.head_dim;
+    in.pos = r->pos;
+    in.rows = a->src_total;
+    in.dtype = r->pool.dtype;
+    if (C > 0 && r->rotate) {
+        if (in.rows == 0 || in.rows > r->pos_rows) return PADOC_ERR_INVALID_ARGUMENT;
+        const padoc_status rows_ok = padoc_rotary_dev::check_rows(&in, &r->rot, true);
+        if (rows_ok != PADOC_OK) return rows_ok;
+    }
     const cudaStream_t stream = (cudaStream_t)a->stream;
     const int b = (int)(r->turn & 1);
     if (r->recorded[b]) {   // the copy that read this stage two steps ago (usually done: ask first)
@@ -768,14 +780,6 @@ extern "C" padoc_status padoc_mpd_runner_step(padoc_mpd_runner *r, const padoc_m
         st = grow_device(&r->q_step, &r->q_bytes, (size_t)n * r->cfg.num_q_heads * r->cfg.head_dim * elt, stream);
     if (st == PADOC_OK) st = grow_device(&r->workspace, &r->workspace_bytes, std::max<size_t>(ws, 256), stream);
     if (st != PADOC_OK) return st;
-    padoc_qkv_rows in = {};
-    in.q = a->q_src, in.k = a->k_src, in.v = a->v_src;
-    in.num_q_heads = r->cfg.num_q_heads, in.num_kv_heads = r->cfg.num_kv_heads;
-    in.q_stride = (int64_t)in.num_q_heads * r->cfg.head_dim;
-    in.k_stride = in.v_stride = (int64_t)in.num_kv_heads * r->cfg.head_dim;
-    in.pos = r->pos;
-    in.rows = a->src_total;
-    in.dtype = r->pool.dtype;
     st = launch_step(&step, stage, r->dev_ints, r->dev_words, &r->pool, r->rotate ? &r->rot : nullptr, in, r->q_step,
                      a->scale, a->out, a->lse, r->workspace, r->workspace_bytes, a->stream);
     if (st != PADOC_OK) return st;

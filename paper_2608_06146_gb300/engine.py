@@ -206,12 +206,23 @@ class MaskedParallelLoop:
         self.h2d_bytes = 4 * n
         return [self._ints[o:o + a.size] for a, o in zip(parts, offs)]
 
+    def _check_rows(self, k_src, q_src, v_src, pos_src):
+        """Refuses source rows that the append with rotary would refuse (by an append of none of them)."""
+        if k_src.shape[0] < 1:
+            raise ValueError("sources must have a row")
+        pa.padoc_append_rotary_inputs(self.rotary, self.k_pool, self.v_pool, k_src, v_src, pos_src, self._ints,
+                                      q_src=q_src, q_dst=self.q_step, count=0)
+
     def add_page(self, prefix_len: int, num_forks: int, layout_eos: bool, k_src, v_src, src_rows, stream=None,
                  pos_src=None):
         """Admits a page: its prefix K/V (rows src_rows of k_src / v_src, device tensors [rows][Hkv][d])
         go into the blocks the scheduler gives it. pos_src: int32 [rows][axes], with rotary. Returns (page
         id, new stream ids)."""
         stream = stream or torch.cuda.current_stream()
+        if self.rotary is not None and prefix_len > 0:   # before the scheduler admits the page
+            self._check_rows(k_src, None, v_src, pos_src)
+            if len(src_rows) != prefix_len:
+                raise ValueError("src_rows must name a row for each prefix token")
         pid, slots, new = self.mpd.add_page(prefix_len, num_forks, layout_eos)
         if prefix_len > 0:
             slots_d, rows_d = self._upload([slots, np.asarray(src_rows, np.int32)], stream)
@@ -230,6 +241,10 @@ class MaskedParallelLoop:
         padoc_mpd_prepare_step into a pinned staging buffer, and padoc_mpd_launch_step, which copies it
         to the device and launches the append and the decode."""
         stream = stream or torch.cuda.current_stream()
+        if self.rotary is not None and self.status()[1]:   # before the scheduler begins the step
+            if q_src is None:
+                raise ValueError("a step needs q_src")
+            self._check_rows(k_src, q_src, v_src, pos_src)
         b = self._turn & 1
         self._turn += 1
         self._stage_free[b].synchronize()

@@ -970,3 +970,42 @@ def test_loop_without_positions_is_refused_and_positions_may_change_their_memory
     lp.end_step(num_streams=1)
     pa.padoc_check_device_errors()
     assert torch.equal(lp.k_pool[0, :, 0], kr[0][0]) and torch.equal(lp.k_pool[0, :, 1], kr[1][0])
+
+
+@pytest.mark.parametrize("what", ["no positions", "positions short", "another dtype", "heads", "unaligned", "no rows"])
+def test_loop_refuses_bad_sources_before_it_begins(what):
+    # the refused call leaves the scheduler as it was, so the next one goes through
+    sp = Spec(34, 128, 128, 1, False, False, BF16)
+    _, q, k, v = qkv(np.random.default_rng(34), 6, 16, 2, 128, BF16)
+    q, k, v = (t.contiguous() for t in (q, k, v))
+    pos = torch.arange(6, dtype=torch.int32, device=DEV)[:, None].contiguous()
+    bad = {"no positions": (k, v, q, None), "positions short": (k, v, q, pos[:5]),
+           "another dtype": (k.float(), v.float(), q.float(), pos),
+           "heads": (k[:, :1].contiguous(), v[:, :1].contiguous(), q, pos),
+           "unaligned": (torch.zeros(6 * 256 + 4, dtype=BF16, device=DEV)[4:].view(6, 2, 128), v, q, pos),
+           "no rows": (k[:0], v[:0], q[:0], pos[:0])}[what]
+    lp = MaskedParallelLoop(8, 16, 2, 128, BF16, DEV, rotary=sp.dev)
+    errors = (ValueError, TypeError, pa.PadocError)
+    with pytest.raises(errors):
+        lp.add_page(3, 0, False, bad[0], bad[1], np.arange(3), pos_src=bad[3])
+    with pytest.raises(errors):
+        lp.add_page(3, 0, False, k, v, np.arange(2), pos_src=pos)
+    assert lp.status() == (0, 0, 8)
+    lp.add_page(3, 0, False, k, v, np.arange(3), pos_src=pos)
+    free = lp.status()
+    out, lse = torch.empty((4, 16, 128), dtype=BF16, device=DEV), torch.empty((4, 16), device=DEV)
+    row = np.full(4, 3, np.int32)
+    with pytest.raises(errors):
+        lp.step(*bad[:3], lambda i: row[i], 0.1, pos_src=bad[3])
+    with pytest.raises(errors):
+        lp.step(k, v, None, lambda i: row[i], 0.1, pos_src=pos)
+    with pytest.raises(errors):
+        lp.run_step(*bad[:3], row, 0.1, out, lse, pos_src=bad[3])
+    assert lp.status() == free
+    _, o, l = lp.step(k, v, q, lambda i: row[i], 0.1, pos_src=pos)
+    lp.end_step(num_streams=1)
+    row[:] = 4
+    assert lp.run_step(k, v, q, row, 0.1, out, lse, pos_src=pos)[0] == 1
+    lp.end_step(num_streams=1)
+    pa.padoc_check_device_errors()
+    assert torch.isfinite(o).all() and torch.isfinite(out[0]).all()
