@@ -113,6 +113,8 @@ class RotaryPrefill:
 
     def run_bwd(self, q, k, v, out, dout, lse, scale, dq, dk, dv, dq_weight=None, dk_weight=None, stream=None):
         """Gradients of the last run's q, k, v (dq, dk, dv contiguous) and, with norm weights, of these."""
+        if self.bwd is None:
+            raise ValueError("gradients need training=True")
         self.bwd.run(self.q, self.k, v, out, dout, lse, scale, dq, dk, dv, stream)
         pa.padoc_qk_rotary_bwd(self.rotary, dq, dk, self.pos, dq, dk, q, k, dq_weight, dk_weight, self.workspace, stream)
 

@@ -1009,3 +1009,9 @@ def test_loop_refuses_bad_sources_before_it_begins(what):
     lp.end_step(num_streams=1)
     pa.padoc_check_device_errors()
     assert torch.isfinite(o).all() and torch.isfinite(out[0]).all()
+
+
+def test_gradients_of_a_layer_that_is_not_trained_are_refused():
+    layer = RotaryPrefill(PAGES, Spec(35, 128, 128, 3, False, False, BF16).dev, 16, 2, BF16, DEV)
+    with pytest.raises(ValueError):
+        layer.run_bwd(*[None] * 6, 0.1, None, None, None)
