@@ -93,11 +93,6 @@ __device__ __forceinline__ void unpack2(const Raw<T, V> &r, uint64_t (&x)[V / 2]
 #pragma unroll
     for (int j = 0; j < V / 2; ++j) x[j] = f2_pack(f[2 * j], f[2 * j + 1]);
 }
-template <int V, typename T>
-__device__ __forceinline__ void load_vec(const T *p, float (&x)[V])
-{
-    unpack(load_raw<T, V>(p), x);
-}
 template <int V>
 __device__ __forceinline__ void store_vec(__nv_bfloat16 *p, const float (&x)[V])
 {

@@ -1065,6 +1065,8 @@ class E4M3Pool:
                              (k_scales, (nb, hkv), torch.float32), (v_scales, (nb, hkv), torch.float32)):
             if tuple(t.shape) != shape or t.dtype != dt:
                 raise ValueError("codes uint8 [num_blocks][Hkv][16][d], scales float32 [num_blocks][Hkv]")
+            if t.get_device() != k_codes.get_device():
+                raise ValueError("codes and scales must be on one device")
         p = cls.__new__(cls)
         p.k_codes, p.v_codes, p.k_scales, p.v_scales = k_codes, v_codes, k_scales, v_scales
         p.c = padoc_kv_pool_e4m3(_dev(k_codes, "k_codes"), _dev(v_codes, "v_codes"), _dev(k_scales, "k_scales"),
