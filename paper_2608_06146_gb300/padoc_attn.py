@@ -924,6 +924,7 @@ class MpdRunner:
         self._args.ids_capacity, self._args.stream_ids = self._ids.size, self._ids.ctypes.data
         self._src = None
         self._outs = {}
+        self._rotary = None
         import torch
         self._elt = torch.bfloat16 if pool.dtype == PADOC_DTYPE_BF16 else torch.float32
         self._f32 = torch.float32
@@ -945,6 +946,8 @@ class MpdRunner:
         next step). out [rows >= C][Hq][d] and lse fp32 [rows][Hq] receive the outputs in step order;
         row_of_stream: int32 [ids] (host), the source row of each live stream's input. Arrays are
         checked the first time they are seen (the runner keeps the last few)."""
+        if self._rotary is not None:   # the weights and positions where they are now
+            self.set_rotary(*self._rotary)
         a = self._args
         src = self._src
         if src is None or src[0] is not k_src or src[1] is not v_src or src[2] is not q_src or \
@@ -963,17 +966,23 @@ class MpdRunner:
 
     def set_rotary(self, rotary: Optional["Rotary"], pos=None):
         """The steps from now on append with the norm and the rotation of ``rotary`` at pos (int32 CUDA tensor
-        [source rows][axes]); None: as they are."""
+        [source rows][axes], read where it is at each step); None: as they are."""
         if rotary is None:
             _check("padoc_mpd_runner_set_rotary", self._lib.padoc_mpd_runner_set_rotary(self._h, None, None, 0))
             self._rotary = None
             return
+        rotary.weights()
         if self._elt is not rotary.dtype and rotary.dtype is not None:
             raise TypeError("the norm weights must have the pool's dtype")
         p = rotary.positions(pos)
         _check("padoc_mpd_runner_set_rotary",
                self._lib.padoc_mpd_runner_set_rotary(self._h, rotary.ref, p, pos.shape[0]))
         self._rotary = (rotary, pos)   # kept alive
+
+    def rotates(self, rotary: "Rotary", pos) -> bool:
+        """Whether set_rotary was called last with these two objects."""
+        r = self._rotary
+        return r is not None and r[0] is rotary and r[1] is pos
 
     @property
     def upload_bytes(self) -> int:
@@ -1161,8 +1170,9 @@ def padoc_build_rotary_positions(pages, grids=()):
 class Rotary:
     """A padoc_rotary with its device table and weights (owned or kept alive here): inv_freq [pairs] and
     axis_of [pairs] as in padoc_build_rotary_table; pairs (i, i + pairs), or (2 i, 2 i + 1) with adjacent; q_weight and
-    k_weight (CUDA tensors [head_dim] in the rows' dtype) give the heads an RMS norm before the rotation. Calls take
-    tensors on its device, which must be the current one."""
+    k_weight (CUDA tensors [head_dim] in the rows' dtype) give the heads an RMS norm before the rotation. Every call reads
+    the weights where they are then (a parameter may be given other memory or another dtype between calls). Calls
+    take tensors on its device, which must be the current one."""
 
     def __init__(self, inv_freq, axis_of=None, num_axes: int = 1, head_dim: int = 128, adjacent: bool = False,
                  q_weight=None, k_weight=None, eps: float = 1e-6, amplitude: float = 1.0, device="cuda"):
@@ -1171,20 +1181,35 @@ class Rotary:
         self.table = torch.from_numpy(table.view(np.int64)).to(device)
         self._device = self.table.get_device()
         self.q_weight, self.k_weight = q_weight, k_weight
-        self.dtype = None
         self._codes = {torch.bfloat16: PADOC_DTYPE_BF16, torch.float32: PADOC_DTYPE_F32}
         self._int32, self._f32 = torch.int32, torch.float32
-        for w in (q_weight, k_weight):
+        self.head_dim, self.num_axes = head_dim, num_axes
+        self.c = padoc_rotary(_dev(self.table, "table"), None, None, head_dim, 2 * table.size, num_axes, int(bool(adjacent)), eps, amplitude)
+        self._shape = torch.Size((head_dim,))
+        self._seen = None
+        self.weights()
+        self.ref = ctypes.byref(self.c)
+
+    def weights(self):
+        """Brings the struct in line with the weights' memory and dtype as they are now."""
+        q, k, seen, shape = self.q_weight, self.k_weight, self._seen, self._shape
+        if q is not None and k is not None:
+            if seen == (q.data_ptr(), k.data_ptr()) and q.dtype is self.dtype and k.dtype is self.dtype and \
+                    q.shape == shape and k.shape == shape and q.is_contiguous() and k.is_contiguous():
+                return
+        elif q is k and seen == (None, None):
+            return
+        dtype = None
+        for w in (q, k):
             if w is None:
                 continue
             _dtype_code(w)
-            if tuple(w.shape) != (head_dim,) or (self.dtype is not None and w.dtype is not self.dtype):
+            if w.shape != shape or (dtype is not None and w.dtype is not dtype):
                 raise ValueError("q_weight and k_weight must be [head_dim] of one dtype")
-            self.dtype = w.dtype
-        self.head_dim, self.num_axes = head_dim, num_axes
-        dev = self._device
-        self.c = padoc_rotary(_dev(self.table, "table"), _on(q_weight, "q_weight", dev), _on(k_weight, "k_weight", dev), head_dim, 2 * table.size, num_axes, int(bool(adjacent)), eps, amplitude)
-        self.ref = ctypes.byref(self.c)
+            dtype = w.dtype
+        seen = (_on(q, "q_weight", self._device), _on(k, "k_weight", self._device))
+        self.c.q_weight, self.c.k_weight = seen
+        self.dtype, self._seen = dtype, seen
 
     def positions(self, pos, rows=None):
         """Address of pos int32 [rows][axes]."""
@@ -1211,6 +1236,7 @@ class Rotary:
         query heads; KV heads)."""
         if _current_device() != self._device:
             raise ValueError(f"the current device must be the rotary's, {self._device}")
+        self.weights()
         n, dt = k.shape[0], k.dtype
         code = self._codes.get(dt)
         if code is None or (self.dtype is not None and dt is not self.dtype):
@@ -1239,6 +1265,7 @@ def padoc_qk_rotary(rotary: Rotary, q, k, pos, q_out, k_out, stream=None):
 def padoc_qk_rotary_bwd_workspace_size(rotary: Rotary, rows: int) -> int:
     lib = load_library()
     n = ctypes.c_size_t()
+    rotary.weights()
     _check("padoc_qk_rotary_bwd_workspace_size",
            lib.padoc_qk_rotary_bwd_workspace_size(rotary.ref, rows, ctypes.byref(n)))
     return n.value
