@@ -148,3 +148,37 @@ def test_runner_reads_weights_and_positions_at_every_step(lib):
     r.set_rotary(None)
     step()
     assert not r.rotates(rot, pos)
+
+
+def test_runner_reads_sources_and_outputs_where_they_are(lib, monkeypatch):
+    r = runner()
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))   # (as if on the GPU)
+    new = lambda h, n=4: torch.zeros((n, h, D), dtype=BF16)
+    k, v, q, row = new(1), new(1), new(2), np.zeros(4, np.int32)
+    out, lse = new(2), torch.zeros((4, 2))
+    step = lambda: r.step(k, v, q, row, 1.0, out, lse)
+    step()
+    held = [t.clone().set_(t) for t in (k, v, q, out, lse)]   # (their memory is not given out again)
+    for name, t, h in (("k", k, 1), ("v", v, 1), ("q", q, 2), ("out", out, 2)):
+        before = t.data_ptr()
+        t.set_(new(h))
+        step()
+        assert lib.seen[name] == t.data_ptr() != before
+    lse.set_(torch.zeros((4, 2)))
+    step()
+    assert lib.seen["lse"] == lse.data_ptr() != held[4].data_ptr()
+    for t, h in ((k, 1), (v, 1), (q, 2)):
+        t.set_(new(h, 3))                                     # fewer rows
+    step()
+    assert lib.seen["rows"] == 3
+    for t, bad in ((k, new(2)), (q, new(2).float()), (out, new(3)), (lse, torch.zeros((4, 3)))):
+        good = t.clone().set_(t)
+        t.data = bad
+        for _ in range(2):
+            with pytest.raises((ValueError, TypeError)):
+                step()
+        t.data = good
+        step()
+    out.resize_(2, 2, D)                                      # fewer rows at the same address
+    step()
+    assert r._args.out_rows == 2
