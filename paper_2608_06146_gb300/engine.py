@@ -158,7 +158,10 @@ class MaskedParallelLoop:
     (pa.Rotary) the inputs are appended normed and rotated, at positions given by source row.
 
     Between steps a branch can be forked with its history (fork_stream), streams and pages dropped, and the
-    pool compacted or replaced by one of another size (compact, resize)."""
+    pool compacted or replaced by one of another size (compact, resize).
+
+    Memory that a call needs more of is allocated on that call's stream. Calls on different streams are ordered by
+    the caller, the first one behind the stream that was current when the loop was made (its pool is zeroed there)."""
 
     def __init__(self, num_blocks: int, num_q_heads: int, num_kv_heads: int, head_dim: int, dtype: torch.dtype,
                  device, block_order=None, block_size: int = 16, tc_ctas: int = 0, warp_ctas: int = 0,
@@ -184,6 +187,15 @@ class MaskedParallelLoop:
         self.h2d_bytes = 0
         self._runner = None
 
+    def _grow(self, name, rows, stream):
+        """Makes the array ``name`` at least rows long for use on ``stream``, where the old one may still be in use."""
+        old = getattr(self, name)
+        if old.shape[0] < rows:
+            old.record_stream(stream)
+            with torch.cuda.stream(stream):
+                new = torch.empty((max(rows, 2 * old.shape[0]),) + tuple(old.shape[1:]), dtype=old.dtype, device=self.device)
+            setattr(self, name, new)
+
     def _upload(self, parts, stream):
         """Copies int32 host arrays to the device in one transfer, each starting on a 128-byte
         boundary; returns device views."""
@@ -200,8 +212,7 @@ class MaskedParallelLoop:
         host = self._stage[b].numpy()
         for a, o in zip(parts, offs):
             host[o:o + a.size] = a.reshape(-1)
-        if self._ints.numel() < n:
-            self._ints = torch.empty(max(n, 2 * self._ints.numel()), dtype=torch.int32, device=self.device)
+        self._grow("_ints", n, stream)
         with torch.cuda.stream(stream):
             self._ints[:n].copy_(self._stage[b][:n], non_blocking=True)
         self._stage_free[b].record(stream)
@@ -266,8 +277,7 @@ class MaskedParallelLoop:
         ids = host[st.off_stream_ids:st.off_stream_ids + C].copy()
         host[st.off_rows:st.off_rows + C] = rows_of(ids)
         n = int(st.upload_words)
-        if self._ints.numel() < n:
-            self._ints = torch.empty(max(n, 2 * self._ints.numel()), dtype=torch.int32, device=self.device)
+        self._grow("_ints", n, stream)
         self.h2d_bytes = 4 * n
         info = st.plan
         self.last_info = info
@@ -277,16 +287,14 @@ class MaskedParallelLoop:
             self._stage_free[b].record(stream)
             empty = torch.empty((0, self.num_q_heads), dtype=torch.float32, device=self.device)
             return ids, torch.empty((0, self.num_q_heads, self.head_dim), dtype=self.dtype, device=self.device), empty
-        if self.q_step.shape[0] < C:
-            self.q_step = torch.empty((max(C, 2 * self.q_step.shape[0]), self.num_q_heads, self.head_dim),
-                                      dtype=self.dtype, device=self.device)
-        ws = pa.padoc_decode_workspace_size(info)
-        if self.workspace.numel() < ws:
-            self.workspace = torch.empty(max(ws, 2 * self.workspace.numel()), dtype=torch.uint8, device=self.device)
-        if out is None:
-            out = torch.empty((C, self.num_q_heads, self.head_dim), dtype=self.dtype, device=self.device)
-        if lse is None:
-            lse = torch.empty((C, self.num_q_heads), dtype=torch.float32, device=self.device)
+        self._grow("q_step", C, stream)
+        self._grow("workspace", pa.padoc_decode_workspace_size(info), stream)
+        if out is None or lse is None:
+            with torch.cuda.stream(stream):
+                if out is None:
+                    out = torch.empty((C, self.num_q_heads, self.head_dim), dtype=self.dtype, device=self.device)
+                if lse is None:
+                    lse = torch.empty((C, self.num_q_heads), dtype=torch.float32, device=self.device)
         # one library call: the stage's copy to the device, the append and the decode
         if self.rotary is not None:
             pa.padoc_mpd_launch_step_rotary(st, self._stage[b], self._ints, self._pool, self.rotary, k_src, v_src, q_src,
