@@ -196,23 +196,30 @@ class MaskedParallelLoop:
                 new = torch.empty((max(rows, 2 * old.shape[0]),) + tuple(old.shape[1:]), dtype=old.dtype, device=self.device)
             setattr(self, name, new)
 
+    def _room(self, sizes, stream):
+        """Room for an upload of arrays of these sizes on ``stream``; returns their places and the words."""
+        offs, n = [], 0
+        for size in sizes:
+            offs.append(n)
+            n += (int(size) + 31) // 32 * 32
+        b = self._turn & 1
+        if self._stage[b] is None or self._stage[b].numel() < n:
+            self._stage_free[b].synchronize()
+            self._stage[b] = torch.empty(max(n, 2 * (0 if self._stage[b] is None else self._stage[b].numel()), 4096),
+                                         dtype=torch.int32).pin_memory()
+        self._grow("_ints", n, stream)
+        return offs, n
+
     def _upload(self, parts, stream):
         """Copies int32 host arrays to the device in one transfer, each starting on a 128-byte
         boundary; returns device views."""
-        offs, n = [], 0
-        for a in parts:
-            offs.append(n)
-            n += (int(a.size) + 31) // 32 * 32
+        offs, n = self._room([a.size for a in parts], stream)
         b = self._turn & 1
         self._turn += 1
         self._stage_free[b].synchronize()
-        if self._stage[b] is None or self._stage[b].numel() < n:
-            self._stage[b] = torch.empty(max(n, 2 * (0 if self._stage[b] is None else self._stage[b].numel()), 4096),
-                                         dtype=torch.int32).pin_memory()
         host = self._stage[b].numpy()
         for a, o in zip(parts, offs):
             host[o:o + a.size] = a.reshape(-1)
-        self._grow("_ints", n, stream)
         with torch.cuda.stream(stream):
             self._ints[:n].copy_(self._stage[b][:n], non_blocking=True)
         self._stage_free[b].record(stream)
@@ -236,9 +243,13 @@ class MaskedParallelLoop:
             self._check_rows(k_src, None, v_src, pos_src)
             if len(src_rows) != prefix_len:
                 raise ValueError("src_rows must name a row for each prefix token")
+        if prefix_len > 0:
+            rows = np.asarray(src_rows, np.int32)
+            if prefix_len <= self.status()[2] * self.cfg.block_size:   # (a page that does not fit is refused below)
+                self._room((prefix_len, rows.size), stream)
         pid, slots, new = self.mpd.add_page(prefix_len, num_forks, layout_eos)
         if prefix_len > 0:
-            slots_d, rows_d = self._upload([slots, np.asarray(src_rows, np.int32)], stream)
+            slots_d, rows_d = self._upload([slots, rows], stream)
             if self.rotary is not None:
                 pa.padoc_append_rotary_inputs(self.rotary, self.k_pool, self.v_pool, k_src, v_src, pos_src, slots_d,
                                               src_rows=rows_d, count=prefix_len, stream=stream)
@@ -326,10 +337,18 @@ class MaskedParallelLoop:
         """Each stream's output event (forks, EOS) in step order; returns the new branches' ids."""
         return self.mpd.end_step(num_forks, eos, num_streams)
 
+    def _before_copies(self, pairs, stream):
+        """Refuses what a copy of up to ``pairs`` blocks within the pool would refuse, and makes its room: the
+        scheduler changes only after this."""
+        if pairs == 0:
+            return
+        own = pa.KvPools([(self.k_pool, self.v_pool)])
+        pa.padoc_copy_kv_blocks(own, self._ints, self._ints, own, 0, stream)
+        self._room((pairs, pairs), stream)
+
     def _copy_blocks(self, src, dst, stream, pool=None):
         """Blocks src to dst of the pool (or of ``pool``, (k_pool, v_pool))."""
         if len(src):
-            stream = stream or torch.cuda.current_stream()
             src_d, dst_d = self._upload([np.asarray(src, np.int32), np.asarray(dst, np.int32)], stream)
             own = pa.KvPools([(self.k_pool, self.v_pool)])
             pa.padoc_copy_kv_blocks(own if pool is None else pa.KvPools([pool]), src_d, dst_d, own, len(src), stream)
@@ -337,6 +356,8 @@ class MaskedParallelLoop:
     def fork_stream(self, stream_id: int, num_copies: int = 1, stream=None):
         """Forks a live branch into num_copies more with the same history, between steps: they share its
         complete blocks and get copies of the partly filled one. Returns the new stream ids."""
+        stream = stream or torch.cuda.current_stream()
+        self._before_copies(max(0, min(num_copies, self.status()[2])), stream)   # (a copy takes a free block)
         new, src, dst = self.mpd.fork_stream(stream_id, num_copies)
         self._copy_blocks(src, dst, stream)
         return new
@@ -351,9 +372,12 @@ class MaskedParallelLoop:
 
     def compact(self, stream=None) -> int:
         """Moves the live blocks to the pool's lowest ids, between steps. Returns their number."""
+        stream = stream or torch.cuda.current_stream()
+        free = self.status()[2]
+        self._before_copies(min(free, self.k_pool.shape[0] - free), stream)      # (a move takes a live block to a free one)
         src, dst = self.mpd.compact()
         self._copy_blocks(src, dst, stream)
-        return self.k_pool.shape[0] - self.status()[2]
+        return self.k_pool.shape[0] - free
 
     def resize(self, num_blocks: int, stream=None):
         """Replaces the pool by one of num_blocks blocks (at least the live ones), between steps."""

@@ -73,3 +73,33 @@ def test_steps_on_a_side_stream_that_need_more_room():
     pa.padoc_check_device_errors()
     for a, b in zip(*results):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_moves_refused_on_another_device_leave_the_loop_as_it_was(monkeypatch):
+    results = []
+    for refused in (False, True):
+        loop, src = make()
+        row = np.arange(512, dtype=np.int32) % 400
+        step = lambda: loop.step(src[1], src[2], src[0], lambda i: row[i], 0.1)
+        ids, _, _ = step()
+        loop.end_step(num_streams=len(ids))
+        loop.drop_page(3)
+        branch = int(loop.step(src[1], src[2], src[0], lambda i: row[i], 0.1)[0][0])
+        loop.end_step(num_streams=118)
+        if refused:
+            before = loop.status()
+            with monkeypatch.context() as m:
+                m.setattr(pa, "_current_device", lambda: 1)   # (as if another GPU were current)
+                for call in (lambda: loop.fork_stream(branch, 2), loop.compact, lambda: loop.resize(2000)):
+                    with pytest.raises(ValueError, match="device"):
+                        call()
+            assert loop.status() == before and loop.k_pool.shape[0] == 3000
+        new = loop.fork_stream(branch, 2)
+        loop.compact()
+        loop.resize(1800)
+        ids, out, lse = step()
+        results.append((new, ids, out, lse))
+    pa.padoc_check_device_errors()
+    a, b = results
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1]) and len(a[1]) == 120
+    assert torch.equal(a[2], b[2]) and torch.equal(a[3], b[3])

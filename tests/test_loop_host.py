@@ -108,3 +108,85 @@ def test_room_that_a_step_needs_is_made_on_its_stream(cuda):
     loop.end_step(num_streams=len(ids))
     loop.step(rows[1], rows[2], rows[0], lambda i: np.zeros(len(i), np.int32), 0.1, out, lse, stream=cuda.side)
     assert not cuda.kept and loop._ints is new[0] and loop.q_step is new[1] and loop.workspace is new[2]
+
+
+def used(num_blocks=64):
+    """A loop whose pool has free blocks below live ones, and whose branches have a row each; the copies it asks for."""
+    loop, rows = make(num_blocks, prefix=40)
+    pid, _ = loop.add_page(40, 3, False, rows[1], rows[2], np.zeros(40, np.int32))
+    ids, _, _ = loop.step(rows[1], rows[2], rows[0], lambda i: np.zeros(len(i), np.int32), 0.1)
+    loop.end_step(num_streams=len(ids))
+    loop.drop_page(0)
+    return loop, [int(i) for i in ids if int(i) > 2], rows
+
+
+def pairs(loop, monkeypatch):
+    """The (source, destination) lists of the copies from now on."""
+    got = []
+    monkeypatch.setattr(loop, "_copy_blocks", lambda src, dst, stream, pool=None: got.append((list(src), list(dst))))
+    return got
+
+
+def refusal(what, monkeypatch):
+    """Something that makes a copy fail, until the context ends."""
+    m = monkeypatch.context()
+    p = m.__enter__()
+    if what == "device":
+        p.setattr(pa, "_current_device", lambda: 1)
+    else:                       # no pinned memory for longer lists
+        def none(t):
+            raise MemoryError
+        p.setattr(torch.Tensor, "pin_memory", none)
+    return m
+
+
+@pytest.mark.parametrize("what", ["device", "memory"])
+@pytest.mark.parametrize("act", ["fork", "compact", "resize"])
+def test_a_move_that_cannot_be_made_leaves_the_scheduler_as_it_was(cuda, monkeypatch, act, what):
+    twin, live, _ = used()
+    loop, same, _ = used()
+    assert live == same
+    branch = live[1]
+    call = {"fork": lambda lp: lp.fork_stream(branch, 2), "compact": lambda lp: lp.compact(),
+            "resize": lambda lp: lp.resize(30)}[act]
+    before = loop.status()
+    if what == "memory":
+        loop._stage = [None, None]
+    m = refusal(what, monkeypatch)
+    with pytest.raises((ValueError, MemoryError)):
+        call(loop)
+    m.__exit__(None, None, None)
+    assert loop.status() == before and loop.k_pool.shape[0] == 64
+    want, got = pairs(twin, monkeypatch), pairs(loop, monkeypatch)
+    a, b = call(twin), call(loop)
+    assert np.array_equal(a, b) and got == want and len(want[0][0]) > 0
+
+
+def test_a_page_whose_rows_cannot_be_sent_is_not_admitted(cuda, monkeypatch):
+    loop, _, rows = used()
+    before = loop.status()
+    loop._stage = [None, None]
+    m = refusal("memory", monkeypatch)
+    with pytest.raises(MemoryError):
+        loop.add_page(40, 1, False, rows[1], rows[2], np.zeros(40, np.int32))
+    m.__exit__(None, None, None)
+    assert loop.status() == before
+    with pytest.raises((TypeError, ValueError)):
+        loop.add_page(2, 1, False, rows[1], rows[2], [0, None])
+    assert loop.status() == before
+    with pytest.raises(pa.PadocError) as e:          # a page that does not fit
+        loop.add_page(10 ** 6, 1, False, rows[1], rows[2], np.zeros(1, np.int32))
+    assert e.value.status == 6 and loop.status() == before
+    loop.add_page(40, 1, False, rows[1], rows[2], np.zeros(40, np.int32))
+    loop.add_page(0, 1, False, rows[1], rows[2], None)
+    assert loop.status()[0] == before[0] + 2
+
+
+def test_moves_of_an_empty_pool(cuda):
+    loop, _, _ = used()
+    loop.drop_page(1)
+    assert loop.compact() == 0
+    loop.resize(0)
+    assert loop.status() == (0, 0, 0) and loop.compact() == 0
+    loop.resize(12)
+    assert loop.status() == (0, 0, 12) and loop.k_pool.shape[0] == 12
