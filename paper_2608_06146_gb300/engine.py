@@ -323,7 +323,7 @@ class MaskedParallelLoop:
         int32 [C], valid until the next step); end the step with end_step. With rotary, pos_src as in step."""
         if self._runner is None:
             self._runner = pa.MpdRunner(self.mpd, self.cfg, self._pool)
-        if self.rotary is not None and not self._runner.rotates(self.rotary, pos_src):
+        if self.rotary is not None and not self._runner.rotates(self.rotary, pos_src) and self.status()[1]:
             self._runner.set_rotary(self.rotary, pos_src)
         n, ids = self._runner.step(k_src, v_src, q_src, row_of_stream, scale, out, lse, stream)
         self.h2d_bytes = self._runner.upload_bytes

@@ -58,7 +58,7 @@ def cuda(monkeypatch):
 
     class Lib:
         def __getattr__(self, name):
-            if name.startswith(("padoc_mpd_launch", "padoc_copy", "padoc_append")):
+            if name.startswith(("padoc_mpd_launch", "padoc_mpd_runner", "padoc_copy", "padoc_append")):
                 return lambda *a: c.launches.append(name) or 0
             return getattr(real, name)
     monkeypatch.setattr(torch.cuda, "Event", Event)
@@ -190,3 +190,18 @@ def test_moves_of_an_empty_pool(cuda):
     assert loop.status() == (0, 0, 0) and loop.compact() == 0
     loop.resize(12)
     assert loop.status() == (0, 0, 12) and loop.k_pool.shape[0] == 12
+
+
+def test_a_step_of_a_loop_without_streams_needs_no_positions(cuda, monkeypatch):
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))   # (as if on the GPU)
+    loop, _, rows = used()
+    loop.drop_page(1)
+    loop.rotary = pa.Rotary(np.ones(D // 2), head_dim=D, device="cpu")
+    out, lse = torch.zeros((4, HQ, D), dtype=BF16), torch.zeros((4, HQ))
+    assert loop.step(rows[1], rows[2], rows[0], lambda i: i, 0.1)[0].size == 0
+    loop.end_step(num_streams=0)
+    n, ids = loop.run_step(rows[1], rows[2], rows[0], np.zeros(8, np.int32), 0.1, out, lse)
+    assert n == 0 and len(ids) == 0
+    loop.add_page(0, 1, False, rows[1], rows[2], None)
+    with pytest.raises(ValueError, match="pos"):
+        loop.run_step(rows[1], rows[2], rows[0], np.zeros(8, np.int32), 0.1, out, lse)
