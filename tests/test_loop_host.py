@@ -69,6 +69,7 @@ def cuda(monkeypatch):
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: c.kept.append((t.data_ptr(), s.name)))
     monkeypatch.setattr(pa, "_dev", lambda t, name: None if t is None else t.data_ptr())
     monkeypatch.setattr(pa, "_current_device", lambda: -1)
+    monkeypatch.setattr(pa, "_stream_ptr", lambda stream: None)
     monkeypatch.setattr(pa, "load_library", lambda *a: Lib())
     return c
 
