@@ -115,6 +115,13 @@ class RotaryPrefill:
         """Gradients of the last run's q, k, v (dq, dk, dv contiguous) and, with norm weights, of these."""
         if self.bwd is None:
             raise ValueError("gradients need training=True")
+        # what either step would refuse, before the first writes dq and dk
+        if dq.shape != self.q.shape or dk.shape != self.k.shape or dq.dtype is not self.q.dtype or dk.dtype is not self.q.dtype:
+            raise ValueError("dq and dk must be like the layer's q and k")
+        pa._rotary_bwd_args(self.rotary, dq, dk, self.pos, dq, dk, q, k, dq_weight, dk_weight, self.workspace)
+        rows = (q, k) if self.rotary.q_weight is not None else ()
+        if any(t.data_ptr() % 16 or (self.T > 1 and t.stride(0) * t.element_size() % 16) for t in rows + (dq, dk)):
+            raise ValueError("rows must start on 16-byte boundaries")
         self.bwd.run(self.q, self.k, v, out, dout, lse, scale, dq, dk, dv, stream)
         pa.padoc_qk_rotary_bwd(self.rotary, dq, dk, self.pos, dq, dk, q, k, dq_weight, dk_weight, self.workspace, stream)
 

@@ -1275,12 +1275,7 @@ def padoc_qk_rotary_bwd_workspace_size(rotary: Rotary, rows: int) -> int:
     return n.value
 
 
-def padoc_qk_rotary_bwd(rotary: Rotary, dq_out, dk_out, pos, dq, dk, q=None, k=None, dq_weight=None, dk_weight=None,
-                        workspace=None, stream=None):
-    """Gradients of padoc_qk_rotary: dq_out / dk_out into dq / dk (which may be the same tensors); with norm
-    weights the forward's q and k, dq_weight and dk_weight (float32 [d], written) and a workspace (uint8 CUDA
-    tensor of padoc_qk_rotary_bwd_workspace_size bytes) are needed."""
-    lib = load_library()
+def _rotary_bwd_args(rotary, dq_out, dk_out, pos, dq, dk, q, k, dq_weight, dk_weight, workspace):
     norm = rotary.q_weight is not None
     n, dt = dk_out.shape[0], dk_out.dtype
     uq, uqs, hq = rotary.heads(dq_out, "dq_out", n, dt)
@@ -1302,9 +1297,18 @@ def padoc_qk_rotary_bwd(rotary: Rotary, dq_out, dk_out, pos, dq, dk, q=None, k=N
         raise ValueError("dq and dk must have the gradients' heads")
     dev = rotary._device
     ws, wsb = (None, 0) if workspace is None else (_on(workspace, "workspace", dev), workspace.numel() * workspace.element_size())
-    st = lib.padoc_qk_rotary_bwd(rotary.ref, rows, uq, uqs, uk, uks, qp, qs, kp, ks, _on(dq_weight, "dq_weight", dev),
-                                 _on(dk_weight, "dk_weight", dev), ws, wsb, _stream_ptr(stream))
-    _check("padoc_qk_rotary_bwd", st)
+    return (rotary.ref, rows, uq, uqs, uk, uks, qp, qs, kp, ks, _on(dq_weight, "dq_weight", dev),
+            _on(dk_weight, "dk_weight", dev), ws, wsb)
+
+
+def padoc_qk_rotary_bwd(rotary: Rotary, dq_out, dk_out, pos, dq, dk, q=None, k=None, dq_weight=None, dk_weight=None,
+                        workspace=None, stream=None):
+    """Gradients of padoc_qk_rotary: dq_out / dk_out into dq / dk (which may be the same tensors); with norm
+    weights the forward's q and k, dq_weight and dk_weight (float32 [d], written) and a workspace (uint8 CUDA
+    tensor of padoc_qk_rotary_bwd_workspace_size bytes) are needed."""
+    lib = load_library()
+    args = _rotary_bwd_args(rotary, dq_out, dk_out, pos, dq, dk, q, k, dq_weight, dk_weight, workspace)
+    _check("padoc_qk_rotary_bwd", lib.padoc_qk_rotary_bwd(*args, _stream_ptr(stream)))
 
 
 def _append_args(rotary, k_src, v_src, pos, slots, q_src, q_dst, src_rows, count):

@@ -1,0 +1,92 @@
+"""CPU tests of what the training layer refuses before it launches anything. Tensors are on the CPU; the library's plans
+and positions are its own, its launches are replaced by a note of their names."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_06146_gb300 import build as pbuild
+from paper_2608_06146_gb300 import padoc_attn as pa
+from paper_2608_06146_gb300.engine import RotaryPrefill
+from paper_2608_06146_gb300.inputs import PageSpec
+
+HQ, HKV, D, BF16 = 4, 2, 128, torch.bfloat16
+PAGES = [PageSpec(20, 4, [0, 2], [7, 3])]
+
+
+@pytest.fixture
+def launched(monkeypatch):
+    pbuild.build()
+    real, names = pa.load_library(), []
+
+    class Lib:
+        def __getattr__(self, name):
+            if name in ("padoc_qk_rotary", "padoc_qk_rotary_bwd", "padoc_ancestor_prefill_attn", "padoc_ancestor_prefill_bwd"):
+                return lambda *a: names.append(name) or 0
+            return getattr(real, name)
+    # (the workspace's size asks for the number of SMs)
+    monkeypatch.setattr(pa, "padoc_qk_rotary_bwd_workspace_size", lambda rotary, rows: 4096)
+    monkeypatch.setattr(pa, "_dev", lambda t, name: None if t is None else t.data_ptr())
+    monkeypatch.setattr(pa, "_current_device", lambda: -1)
+    monkeypatch.setattr(pa, "_stream_ptr", lambda stream: None)
+    monkeypatch.setattr(pa, "load_library", lambda *a: Lib())
+    return names
+
+
+def layer(norm=True):
+    w = [torch.ones(D, dtype=BF16) for _ in range(2)] if norm else (None, None)
+    rot = pa.Rotary(np.ones(D // 2), head_dim=D, q_weight=w[0], k_weight=w[1], device="cpu")
+    return RotaryPrefill(PAGES, rot, HQ, HKV, BF16, "cpu", training=True)
+
+
+def tensors(T):
+    z = lambda h, dt=BF16: torch.zeros((T, h, D), dtype=dt)
+    return dict(q=z(HQ), k=z(HKV), v=z(HKV), out=z(HQ), dout=z(HQ), lse=torch.zeros((T, HQ)), scale=0.1, dq=z(HQ), dk=z(HKV),
+                dv=z(HKV), dq_weight=torch.zeros(D), dk_weight=torch.zeros(D))
+
+
+def off(t):
+    """The same tensor 8 bytes past a 16-byte boundary."""
+    flat = torch.zeros(t.numel() + 16, dtype=t.dtype)
+    at = (16 - flat.data_ptr() % 16) % 16 // 2 + 4
+    return flat[at:at + t.numel()].view(t.shape)
+
+
+BWD = ["padoc_ancestor_prefill_bwd", "padoc_qk_rotary_bwd"]
+
+
+def test_backward_of_a_layer_runs_both_steps(launched):
+    for norm in (True, False):
+        lay = layer(norm)
+        launched.clear()
+        lay.run_bwd(**tensors(lay.T))
+        assert launched == BWD
+    launched.clear()
+    t = tensors(lay.T)
+    del t["dq_weight"], t["dk_weight"]                   # not needed without a norm
+    lay.run_bwd(**t)
+    assert launched == BWD
+
+
+@pytest.mark.parametrize("name, bad", [
+    ("dq_weight", lambda t: None), ("dk_weight", lambda t: None), ("dq_weight", lambda t: t.to(BF16)),
+    ("dk_weight", lambda t: t[:64]), ("q", lambda t: t[:-1]), ("q", lambda t: t[:, :2]), ("k", lambda t: t.float()),
+    ("q", lambda t: None), ("q", off), ("k", off), ("dq", off), ("dk", off), ("dq", lambda t: t[:, :2].contiguous()),
+    ("dq", lambda t: t.float()), ("dk", lambda t: t[:-1]), ("k", lambda t: torch.zeros((t.shape[0], HKV * D + 4), dtype=BF16)[:, :HKV * D].view(-1, HKV, D)),
+])
+def test_backward_of_a_layer_is_refused_before_it_writes(launched, name, bad):
+    lay = layer()
+    t = tensors(lay.T)
+    t[name] = bad(t[name])
+    launched.clear()
+    with pytest.raises((ValueError, TypeError)):
+        lay.run_bwd(**t)
+    assert launched == []
+
+
+def test_backward_of_a_layer_on_another_device_is_refused_before_it_writes(launched, monkeypatch):
+    lay = layer()
+    launched.clear()
+    monkeypatch.setattr(pa, "_current_device", lambda: 1)
+    with pytest.raises(ValueError, match="device"):
+        lay.run_bwd(**tensors(lay.T))
+    assert launched == []
