@@ -106,8 +106,17 @@ class RotaryPrefill:
             self.workspace = torch.empty(max(pa.padoc_qk_rotary_bwd_workspace_size(rotary, self.T), 256),
                                          dtype=torch.uint8, device=device)
 
+    def _like(self, queries, keys, lse):
+        """Refuses tensors that are not [T] rows of the layer's query or key heads, and an lse that is not [T][Hq]."""
+        for like, ts in ((self.q, queries), (self.k, keys)):
+            if any(t.shape != like.shape or t.dtype is not like.dtype for t in ts):
+                raise ValueError("out, dout and dq must be like the layer's q, v, dk and dv like its k")
+        if lse.shape != self.q.shape[:2] or lse.dtype is not torch.float32:
+            raise ValueError("lse must be float32 [T][Hq]")
+
     def run(self, q, k, v, scale, out, lse, stream=None):
         """q / k: [T][heads][d] as the projections give them (rows may lie apart); v contiguous."""
+        self._like((out,), (v,), lse)
         pa.padoc_qk_rotary(self.rotary, q, k, self.pos, self.q, self.k, stream)
         self.fwd.run(self.q, self.k, v, scale, out, lse, stream)
 
@@ -116,8 +125,7 @@ class RotaryPrefill:
         if self.bwd is None:
             raise ValueError("gradients need training=True")
         # what either step would refuse, before the first writes dq and dk
-        if dq.shape != self.q.shape or dk.shape != self.k.shape or dq.dtype is not self.q.dtype or dk.dtype is not self.q.dtype:
-            raise ValueError("dq and dk must be like the layer's q and k")
+        self._like((out, dout, dq), (v, dk, dv), lse)
         pa._rotary_bwd_args(self.rotary, dq, dk, self.pos, dq, dk, q, k, dq_weight, dk_weight, self.workspace)
         rows = (q, k) if self.rotary.q_weight is not None else ()
         if any(t.data_ptr() % 16 or (self.T > 1 and t.stride(0) * t.element_size() % 16) for t in rows + (dq, dk)):

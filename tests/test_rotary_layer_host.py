@@ -90,3 +90,25 @@ def test_backward_of_a_layer_on_another_device_is_refused_before_it_writes(launc
     with pytest.raises(ValueError, match="device"):
         lay.run_bwd(**tensors(lay.T))
     assert launched == []
+
+
+SHORT = [(name, bad) for name in ("v", "out", "lse", "dout", "dv") for bad in ("rows", "heads", "dtype")]
+
+
+@pytest.mark.parametrize("name, bad", SHORT)
+def test_tensors_that_are_not_the_layers_are_refused(launched, name, bad):
+    # (the attention calls take addresses: a tensor with fewer rows or heads would be read or written past its end)
+    lay = layer()
+    t = tensors(lay.T)
+    t[name] = {"rows": lambda x: x[:-1], "heads": lambda x: x[:, :1].contiguous(),
+               "dtype": lambda x: x.half()}[bad](t[name])
+    launched.clear()
+    with pytest.raises(ValueError):
+        lay.run_bwd(**t)
+    if name in ("v", "out", "lse"):
+        with pytest.raises(ValueError):
+            lay.run(**{n: t[n] for n in ("q", "k", "v", "scale", "out", "lse")})
+    assert launched == []
+    good = tensors(lay.T)
+    lay.run(**{n: good[n] for n in ("q", "k", "v", "scale", "out", "lse")})
+    assert launched == ["padoc_qk_rotary", "padoc_ancestor_prefill_attn"]
