@@ -891,9 +891,16 @@ def padoc_mpd_launch_step(step: padoc_mpd_step, stage, dev_ints, pool: padoc_kv_
 def padoc_mpd_launch_step_rotary(step: padoc_mpd_step, stage, dev_ints, pool: padoc_kv_pool, rotary: "Rotary", k_src,
                                  v_src, q_src, pos, q_dst, scale, out, lse, workspace, stream=None):
     """padoc_mpd_launch_step with padoc_append_rotary_inputs as its append: k_src / v_src / q_src as there
-    (row strides allowed), pos int32 [rows][axes]."""
+    (row strides allowed), pos int32 [rows][axes]; q_dst, out [rows >= streams][Hq][d] and lse fp32 [rows][Hq]."""
     lib = load_library()
-    rows = rotary.rows(pos, k_src, q_src, v_src)[0]
+    rows, _, hq, _ = rotary.rows(pos, k_src, q_src, v_src)
+    n = step.num_streams
+    if n:
+        for t, name in ((q_dst, "q_dst"), (out, "out")):
+            if t.shape[0] < n or t.shape[1:] != (hq, rotary.head_dim) or t.dtype is not k_src.dtype:
+                raise ValueError(f"{name} must be [streams][Hq][d] in the rows' dtype")
+        if lse.shape[0] < n or lse.shape[1:] != (hq,) or lse.dtype is not rotary._f32:
+            raise ValueError("lse must be float32 [streams][Hq]")
     st = lib.padoc_mpd_launch_step_rotary(ctypes.byref(step), None if stage is None else stage.data_ptr(),
                                           _dev(dev_ints, "dev_ints"), dev_ints.numel(), ctypes.byref(pool), rotary.ref,
                                           rows, _dev(q_dst, "q_dst"), float(scale), _dev(out, "out"),

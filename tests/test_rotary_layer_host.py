@@ -112,3 +112,26 @@ def test_tensors_that_are_not_the_layers_are_refused(launched, name, bad):
     good = tensors(lay.T)
     lay.run(**{n: good[n] for n in ("q", "k", "v", "scale", "out", "lse")})
     assert launched == ["padoc_qk_rotary", "padoc_ancestor_prefill_attn"]
+
+
+@pytest.mark.parametrize("name", ["q_dst", "out", "lse"])
+def test_step_outputs_that_are_too_small_are_refused(launched, monkeypatch, name):
+    monkeypatch.setattr(pa.load_library().__class__, "padoc_mpd_launch_step_rotary", lambda *a: launched.append("step") or 0,
+                        raising=False)
+    rot = pa.Rotary(np.ones(D // 2), head_dim=D, device="cpu")
+    z = lambda h, n=5, dt=BF16: torch.zeros((n, h, D), dtype=dt)
+    step, pos, ints = pa.padoc_mpd_step(), torch.zeros((5, 1), dtype=torch.int32), torch.zeros(64, dtype=torch.int32)
+    step.num_streams = 4
+
+    def call(**kw):
+        t = dict(q_dst=z(HQ), out=z(HQ, 4), lse=torch.zeros((4, HQ)))
+        t.update(kw)
+        pa.padoc_mpd_launch_step_rotary(step, None, ints, pa.padoc_kv_pool(), rot, z(HKV), z(HKV), z(HQ), pos, t["q_dst"], 0.1,
+                                        t["out"], t["lse"], ints)
+    call()
+    bad = [torch.zeros((3, HQ)), torch.zeros((4, HQ - 1)), torch.zeros((4, HQ)).half()] if name == "lse" else \
+        [z(HQ, 3), z(HQ - 1), z(HQ, dt=torch.float32), torch.zeros((5, HQ, D // 2), dtype=BF16)]
+    for b in bad:
+        with pytest.raises(ValueError):
+            call(**{name: b})
+    assert launched == ["step"]
