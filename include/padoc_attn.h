@@ -754,7 +754,8 @@ padoc_status padoc_qk_rotary_bwd_workspace_size(const padoc_rotary *rot, int64_t
  *   with it, h = x r:  dx = r (w g - h mean_j(w_j g_j h_j)),  dw = sum over rows and heads of g h.
  *   in: the forward's rows; without the norm only pos, rows, the head counts and dtype are used.
  *   dq, dk: strides as above; each may be its upstream gradient (same address and stride).
- *   dq_weight, dk_weight: (device) fp32 [head_dim], written (zero for no rows); NULL without the norm.
+ *   dq_weight, dk_weight: (device) fp32 [head_dim] each, not overlapping, written (zero for no rows); NULL
+ *   without the norm.
  *   workspace: (device) >= padoc_qk_rotary_bwd_workspace_size bytes, 256-byte aligned.
  * Sums in fp32 in a fixed order: the same call gives the same bits.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, CUDA. */

@@ -569,6 +569,11 @@ extern "C" padoc_status padoc_qk_rotary_bwd(const padoc_rotary *rot, const padoc
     if (ctas > 0) {
         if (!workspace || (((uintptr_t)workspace) & 255)) return PADOC_ERR_INVALID_ARGUMENT;
         if (workspace_bytes < (size_t)ctas * 2 * d * sizeof(float)) return PADOC_ERR_WORKSPACE_TOO_SMALL;
+    }
+    // both are written, by threads without an order between them
+    if ((uintptr_t)dq_weight < (uintptr_t)(dk_weight + d) && (uintptr_t)dk_weight < (uintptr_t)(dq_weight + d))
+        return PADOC_ERR_INVALID_ARGUMENT;
+    if (ctas > 0) {
         BwdArgs p = {};
         p.sp = back;
         p.q = in->q, p.k = in->k;
