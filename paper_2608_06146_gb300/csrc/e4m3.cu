@@ -493,7 +493,8 @@ extern "C" padoc_status padoc_append_rotary_inputs_e4m3(const padoc_kv_pool_e4m3
     if (count == 0) return PADOC_OK;
     if (in->rows == 0 || !slots || (in->q && !q_dst)) return PADOC_ERR_INVALID_ARGUMENT;
     const uintptr_t align = (uintptr_t)pool->k_codes | (uintptr_t)pool->v_codes | (uintptr_t)q_dst;
-    if ((align & 15) || (((uintptr_t)pool->k_scales | (uintptr_t)pool->v_scales) & 3)) return PADOC_ERR_INVALID_ARGUMENT;
+    const uintptr_t words = (uintptr_t)pool->k_scales | (uintptr_t)pool->v_scales | (uintptr_t)src_rows | (uintptr_t)slots;
+    if ((align & 15) || (words & 3)) return PADOC_ERR_INVALID_ARGUMENT;
     RotaryAppendArgs a = {};
     Args &p = a.rows;
     p.err = padoc_device_error_word();

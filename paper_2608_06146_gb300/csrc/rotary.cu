@@ -491,6 +491,7 @@ extern "C" padoc_status padoc_append_rotary_inputs(const padoc_kv_pool *pool, co
     if (count == 0) return PADOC_OK;
     if (in->rows == 0 || !slots || !pool->k_pool || !pool->v_pool || (in->q && !q_dst)) return PADOC_ERR_INVALID_ARGUMENT;
     if ((((uintptr_t)pool->k_pool) | ((uintptr_t)pool->v_pool) | ((uintptr_t)q_dst)) & 15) return PADOC_ERR_INVALID_ARGUMENT;
+    if ((((uintptr_t)src_rows) | ((uintptr_t)slots)) & 3) return PADOC_ERR_INVALID_ARGUMENT;
     int *err = padoc_device_error_word();
     if (!err) return PADOC_ERR_CUDA;
     Args p = {};

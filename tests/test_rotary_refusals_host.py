@@ -36,3 +36,15 @@ def test_weight_gradients_that_overlap(lib, n):
     for off in (0, 4, 127 * 4):
         assert call(A, A + off) == 1 and call(A + off, A) == 1
     assert call(A, A + 512) not in (0, 1) and call(A + 512, A) not in (0, 1)   # (the launch, that finds no GPU)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_append_lists_off_a_4_byte_boundary(lib, e4m3):
+    if e4m3:
+        pool, f = pa.padoc_kv_pool_e4m3(A, A, A, A, 64, 16, 2, 128), lib.padoc_append_rotary_inputs_e4m3
+    else:
+        pool, f = pa.padoc_kv_pool(A, A, 64, 16, 2, 128, BF16), lib.padoc_append_rotary_inputs
+    call = lambda src, slots: f(ctypes.byref(pool), ctypes.byref(rot()), ctypes.byref(rows()), A, src, slots, 4, None)
+    for off in (1, 2, 3):
+        assert call(None, A + off) == 1 and call(A + off, A) == 1
+    assert call(None, A + 4) not in (0, 1) and call(A + 4, A) not in (0, 1)    # (no GPU to launch on)
