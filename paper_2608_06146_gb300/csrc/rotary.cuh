@@ -24,17 +24,20 @@ struct Spec {
 
 // The cosine and sine of one pair's angle, times their amplitudes. A table entry holds the fraction of a
 // turn per position unit as a 64-bit integer, its axis in the two lowest bits; times a 32-bit position it
-// wraps modulo a whole turn, so the angle of a position a million tokens away is as exact as that of the
-// first ones (its fraction is cut at 2^-32 of a turn; a product in fp32 would be off by 0.06 rad at 10^6).
+// wraps modulo a whole turn. The product is cut at 2^-32 of a turn, and the entry is at most 2^-54 of a turn off
+// (frequencies from 0 to 1 radian a position: two fp64 roundings, then 62 bits), so an angle a million tokens away is
+// 2^-31.7 of a turn off, one at 2^31 2^-23 (a product in fp32 would be off by 0.06 rad at 10^6).
 __device__ __forceinline__ float half_turns(uint64_t f, const int32_t *__restrict__ pos, int32_t axes)
 {
     const int32_t p = pos[min((int32_t)(f & 3u), axes - 1)];   // (a table of more axes than the rows have stays in the row)
     const int32_t t = (int32_t)(((f & ~(uint64_t)3) * (uint64_t)(int64_t)p) >> 32);
-    return (float)t * 0x1p-31f;   // in [-1, 1): the angle is pi times this
+    return (float)t * 0x1p-31f;   // in [-1, 1], 24 bits (the last 64 values of t round up to 1): the angle is pi times this
 }
-// kFast (outputs of 16 bits or fewer): the hardware's sine and cosine, 2^-20.5 off at most on [-pi, pi], 2^-12 of
-// the half step that a bf16 output is rounded by; else CUDA's sincospif, within 2 units of the last place, which takes
-// some 40 instructions more a pair.
+// kFast (outputs of 16 bits or fewer): the hardware's sine and cosine, each 2^-20.5 off at most (absolute, on [-pi, pi]; at
+// half a turn the fp32 pi lies 2^-23.5 past it, where a test holds the same bound). A turned value u c - v s is off by
+// that times |u| + |v|: 2^-11.5 or less of the half step by which a bf16 value of that size is rounded, and more than a
+// half step where the two terms cancel to less than 2^-11.5 of it. Else CUDA's sincospif, within 2 units of the last place, which
+// takes some 40 instructions more a pair.
 template <bool kFast>
 __device__ __forceinline__ void cos_sin(uint64_t f, const int32_t *__restrict__ pos, const Spec &sp, float &c, float &s)
 {
@@ -246,9 +249,9 @@ __device__ __forceinline__ void scale_head(uint64_t (&a)[V / 2], uint64_t (&b)[V
     }
 }
 
-// The cosines and sines of a lane's V pairs at row `row`, as packed pairs; for the whole warp. The lanes that hold
-// the same chunk of different heads share the work where there are enough of them: each computes kOwn pairs and
-// hands them to the others.
+// The cosines and sines of a lane's V pairs at a row's positions; for the whole warp. The lanes that hold the same chunk
+// of different heads share the work where there are enough of them: each computes kOwn pairs and hands them to the
+// others.
 template <int V, bool kAdjacent, bool kFast, int kOwn>
 __device__ __forceinline__ void shared_angles(const Spec &sp, const int32_t *__restrict__ pos, const Lane &l, bool turned, float (&cj)[V], float (&sj)[V])
 {
@@ -265,6 +268,7 @@ __device__ __forceinline__ void shared_angles(const Spec &sp, const int32_t *__r
         sj[j] = __shfl_sync(0xffffffffu, so[j % kOwn], from);
     }
 }
+// The same at row `row`, as packed pairs, shared or not.
 template <int V, bool kAdjacent, bool kFast, int kGroup>
 __device__ __forceinline__ void lane_angles(const Spec &sp, const int32_t *__restrict__ pos, int64_t row, const Lane &l, bool turned,
                                             uint64_t (&c)[V / 2], uint64_t (&s)[V / 2])
