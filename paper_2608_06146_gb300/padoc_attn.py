@@ -952,19 +952,17 @@ class MpdRunner:
         """One step: returns (C, stream ids int32 [C], a view of the runner's array valid until the
         next step). out [rows >= C][Hq][d] and lse fp32 [rows][Hq] receive the outputs in step order;
         row_of_stream: int32 [ids] (host), the source row of each live stream's input. Arrays are
-        checked the first time they are seen (the runner keeps the last few), and again when their
-        memory or shape has changed."""
+        checked the first time they are seen (the runner keeps the last few and their memory), and again
+        when their memory has changed."""
         if self._rotary is not None:   # the weights and positions where they are now
             self.set_rotary(*self._rotary)
         a = self._args
         src = self._src
         if src is None or src[0] is not k_src or src[1] is not v_src or src[2] is not q_src or \
-                src[3] is not row_of_stream or src[4] != (k_src.data_ptr(), v_src.data_ptr(), q_src.data_ptr()) or \
-                src[5] != (k_src.shape, v_src.shape, q_src.shape):
+                src[3] is not row_of_stream or src[4]() != src[7] or src[5]() != src[8] or src[6]() != src[9]:
             self._set_sources(k_src, v_src, q_src, row_of_stream)
         o = self._outs.get((id(out), id(lse)))
-        if o is None or o[0] is not out or o[1] is not lse or o[2] != out.data_ptr() or o[3] != lse.data_ptr() or \
-                o[5] != (out.shape, lse.shape):
+        if o is None or o[0] is not out or o[1] is not lse or o[5]() != o[2] or o[6]() != o[3]:
             o = self._set_outputs(out, lse)
         a.out, a.lse, a.out_rows = o[2], o[3], o[4]
         a.scale = scale
@@ -1017,8 +1015,9 @@ class MpdRunner:
         a.src_total = k_src.shape[0]
         a.src_row_of_stream = row_of_stream.ctypes.data
         a.num_stream_ids = row_of_stream.size
-        self._src = (k_src, v_src, q_src, row_of_stream, (a.k_src, a.v_src, a.q_src),
-                     (k_src.shape, v_src.shape, q_src.shape))
+        # (the detached tensors hold the memory, so that another at the same address is still this one)
+        self._src = (k_src, v_src, q_src, row_of_stream, k_src.data_ptr, v_src.data_ptr, q_src.data_ptr, k_src.data_ptr(),
+                     v_src.data_ptr(), q_src.data_ptr(), k_src.detach(), v_src.detach(), q_src.detach())
 
     def _set_outputs(self, out, lse):
         # plain attribute reads: a caller that passes new slices of a longer buffer comes here on every step
@@ -1033,7 +1032,7 @@ class MpdRunner:
             self._args.ids_capacity, self._args.stream_ids = self._ids.size, self._ids.ctypes.data
         if len(self._outs) >= 8:
             self._outs.clear()
-        o = (out, lse, out.data_ptr(), lse.data_ptr(), cap, (osh, lsh))
+        o = (out, lse, out.data_ptr(), lse.data_ptr(), cap, out.data_ptr, lse.data_ptr, out.detach(), lse.detach())
         self._outs[(id(out), id(lse))] = o
         return o
 

@@ -129,8 +129,8 @@ def test_runner_reads_weights_and_positions_at_every_step(lib):
     r, rot = runner(), spec()
     src = [torch.zeros((4, h, D), dtype=BF16) for h in (1, 1, 2)]
     row, pos = np.zeros(4, np.int32), torch.zeros((4, 1), dtype=torch.int32)
-    o = types.SimpleNamespace(shape=(4, 2, D), dtype=BF16, is_cuda=True, is_contiguous=lambda: True, data_ptr=lambda: 64)
-    l = types.SimpleNamespace(shape=(4, 2), dtype=F32, is_cuda=True, is_contiguous=lambda: True, data_ptr=lambda: 128)
+    o = types.SimpleNamespace(shape=(4, 2, D), dtype=BF16, is_cuda=True, is_contiguous=lambda: True, data_ptr=lambda: 64, detach=lambda: None)
+    l = types.SimpleNamespace(shape=(4, 2), dtype=F32, is_cuda=True, is_contiguous=lambda: True, data_ptr=lambda: 128, detach=lambda: None)
     step = lambda: r.step(*src, row, 1.0, o, l)
     r.set_rotary(rot, pos)
     step()
@@ -179,6 +179,9 @@ def test_runner_reads_sources_and_outputs_where_they_are(lib, monkeypatch):
                 step()
         t.data = good
         step()
-    out.resize_(2, 2, D)                                      # fewer rows at the same address
+    # memory that the runner has seen is not given out again while it may take it for the same tensor's
+    seen = k.data_ptr()
+    k.data = new(1, 3)
+    assert all(new(1, n).data_ptr() != seen for n in range(1, 4) for _ in range(8))
     step()
-    assert r._args.out_rows == 2
+    assert lib.seen["k"] == k.data_ptr()
