@@ -5,6 +5,8 @@
 // over the rows the block holds, so that a block's largest magnitude maps to the format's largest
 // finite value. All arithmetic that decides a code is fp32 with round-to-nearest-even (division and
 // product rounded once each), so the codes are a function of the inputs alone.
+#include <type_traits>
+
 #include "common.cuh"
 #include "rotary.cuh"
 #include "tc.cuh"
@@ -196,14 +198,6 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_e4m3_kernel(
     }
 }
 
-template <bool kFirst, typename A, typename B>
-struct Pick {
-    using type = A;
-};
-template <typename A, typename B>
-struct Pick<false, A, B> {
-    using type = B;
-};
 // The codes of a lane's vector under a scale (0 for a block of zeros).
 __device__ __forceinline__ uint2 encode(const float (&x)[8], const Scale &sc)
 {
@@ -280,7 +274,7 @@ __device__ __forceinline__ void append_run(const RotaryAppendArgs &a, int32_t sl
     const int64_t blk = slot0 / kBlk;
     float *scp = (is_v ? a.v_scales : a.k_scales) + blk * p.hkv + g;
     uint8_t *codes = static_cast<uint8_t *>(is_v ? p.v_out : p.k_out) + (blk * p.hkv + g) * kBlk * kD;
-    using Codes = typename Pick<V == 8, uint2, uint32_t>::type;
+    using Codes = std::conditional_t<V == 8, uint2, uint32_t>;
     const float s_old = r0 == 0 ? 0.f : *scp;
     float amax = 0.f;
 #pragma unroll
