@@ -16,9 +16,11 @@ constexpr int kWarps = 4;   // warps per CTA
 
 // See row_part. kCtas: CTAs an SM that the registers have to allow. With the norm a row's steps take longer than its
 // loads, so many rows want one more CTA on an SM than the compiler's own choice gives (96 registers, 5 CTAs), even at a
-// few spilled values; few rows want the loads first. 16 + 2 heads of 128 dims in bf16, own choice / 6 / 7 CTAs: 10001
-// rows 19.3 / 19.5 / 20.7 us, 32768 50.3 / 49.2 / 53.2; 64 dims, 52083 rows 49.9 / 48.4 / 53.3. Adjacent pairs, which
-// are turned one by one, lose by it: 26041 rows 43.3 / 46.9 / 49.1.
+// few spilled values (8 bytes, 24 in the general form); few rows want the loads first. 16 + 2 heads of 128 dims in bf16,
+// own choice / 6 / 7 CTAs: 10001 rows 18.7 / 19.0 / 20.8 us, 32768 49.4 / 48.0 / 53.3; 64 dims, 65536 rows 59.9 / 57.1 /
+// 55.7; 256 dims, 16384 rows 51.8 / 50.1 / 53.7; 80 dims (the general form), 10001 rows 17.3 / 16.0 / 15.8, 52428 70.3 /
+// 62.2 / 59.9. Adjacent pairs, which are turned one by one, lose by it: 26041 rows 43.3 / 46.9 / 49.1. Appends: see
+// steps_of.
 template <typename T, int V, bool kAdjacent, bool kNorm, int kMode, int kGroup, int kCtas>
 __global__ void __launch_bounds__(32 * kWarps, kCtas) rotary_kernel(const __grid_constant__ Args p)
 {
@@ -62,7 +64,7 @@ __device__ __forceinline__ void cp_async_vec(uint32_t dst, const void *src, uint
 // through the ring with scalar arithmetic (2620 instructions a row); 76.3 us now (87% of the copy rate), bound by the
 // latency of a step's chain (two sums over the head) at the 16 warps an SM that the sums' registers leave. Steps of
 // query and of key heads apart take 74.4 us there, but 79.9 instead of 69.7 at 7 + 1 heads and 95 instead of 87 at
-// 80 dims, where they leave lanes without a head.
+// 80 dims, where they leave lanes without a head. The general form (kGroup 0) in bf16 spills 4 to 8 bytes.
 // kGroup: see Lane.
 template <typename T, int V, bool kAdjacent, int kGroup>
 __global__ void __launch_bounds__(32 * kBwdWarps, 2) rotary_norm_bwd_kernel(const __grid_constant__ BwdArgs p)

@@ -333,8 +333,11 @@ enum { kPacked = 0, kAppend = 1, kQueries = 2 };
 
 // Most steps of a part. 5: the 16 + 2 heads of 128 dims in bf16, four at a time, in one part. An append's rows are
 // few and its loads wait for their row number: two parts on more warps an SM hide more of it. Own choice of registers
-// and 5 steps / 7 CTAs an SM and 3 steps, with the norm: one row 2.2 / 2.4 us, 672 rows 3.9 / 3.7, 2000 5.2 / 5.6, 4001
-// 12.7 / 11.5; without it 672 3.3 / 2.8, 4001 10.6 / 9.4.
+// and 5 steps / 7 CTAs an SM and 3 steps, with the norm: one row 2.2 / 2.5 us, 672 rows 3.7 / 3.6, 2000 5.1 / 5.2, 4001
+// 12.3 / 11.1; without it 672 3.2 / 2.7, 4001 10.3 / 9.0. Adjacent pairs, at 28 spilled bytes: 672 3.9 / 3.7, 2000 5.4 /
+// 5.4, 4001 12.7 / 11.3; 64 dims 672 3.1 / 3.0, 4001 6.6 / 5.3; 80 dims (the general form) 672 3.6 / 3.6, 4001 8.7 /
+// 8.2. (3 steps at the compiler's own registers are faster while the grid is one round, 672 rows 3.3, and slower behind
+// it, 2000 6.2.) fp32 rows and 8-byte vectors need fewer registers: no difference.
 constexpr int steps_of(int mode) { return mode == kAppend ? 3 : 5; }
 
 // One warp's work: part `part` of row i, p.steps steps of as many heads as fit a warp, at most kSteps. All of the part's loads

@@ -1077,7 +1077,7 @@ class E4M3Pool:
 
     @classmethod
     def over(cls, k_codes, v_codes, k_scales, v_scales):
-        """The pool over codes and scales that the caller holds already."""
+        """The pool over codes and scales that the caller holds already (they keep their memory while it is used)."""
         import torch
         nb, hkv, bs, d = k_codes.shape
         for t, shape, dt in ((k_codes, (nb, hkv, bs, d), torch.uint8), (v_codes, (nb, hkv, bs, d), torch.uint8),
@@ -1372,7 +1372,8 @@ def padoc_append_rotary_inputs_e4m3(rotary: Rotary, pool: E4M3Pool, k_src, v_src
 # ------------------------------------------------------------------------------------------------
 
 class KvPools:
-    """The layers' pools of a cache, marshalled once: (k_pool, v_pool) tensors [num_blocks][Hkv][16][d] each."""
+    """The layers' pools of a cache, marshalled once: (k_pool, v_pool) tensors [num_blocks][Hkv][16][d] each, which keep
+    their memory while this object is used."""
 
     def __init__(self, pools):
         import torch
@@ -1389,7 +1390,8 @@ class KvPools:
 
 
 class KvPoolsE4M3:
-    """The layers' E4M3 pools: E4M3Pool objects or (k_codes, v_codes, k_scales, v_scales) tensors."""
+    """The layers' E4M3 pools: E4M3Pool objects or (k_codes, v_codes, k_scales, v_scales) tensors, which keep their
+    memory while this object is used."""
 
     def __init__(self, pools):
         import torch
