@@ -188,6 +188,8 @@ class MaskedParallelLoop:
         self.cfg = pa.make_decode_config(num_q_heads, num_kv_heads, head_dim, block_size, False, split_tokens,
                                          tc_ctas, warp_ctas)
         self.device, self.dtype = device, dtype
+        if rotary is not None and rotary.table.device != self.k_pool.device:
+            raise ValueError("the rotary must be on the pool's device")
         self.rotary = rotary
         self.num_q_heads, self.head_dim = num_q_heads, head_dim
         self._stage = [None, None]

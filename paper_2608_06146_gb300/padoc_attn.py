@@ -979,6 +979,8 @@ class MpdRunner:
             _check("padoc_mpd_runner_set_rotary", self._lib.padoc_mpd_runner_set_rotary(self._h, None, None, 0))
             self._rotary = None
             return
+        if _current_device() != rotary._device:
+            raise ValueError(f"the current device must be the rotary's, {rotary._device}")
         rotary.weights()
         if self._elt is not rotary.dtype and rotary.dtype is not None:
             raise TypeError("the norm weights must have the pool's dtype")

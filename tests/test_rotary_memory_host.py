@@ -145,6 +145,8 @@ def test_runner_reads_weights_and_positions_at_every_step(lib):
     with pytest.raises(ValueError):
         step()
     assert r.rotates(rot, pos) and not r.rotates(rot, pos.clone())
+    rot.k_weight.data = rot.k_weight.data.to(BF16)
+    step()
     r.set_rotary(None)
     step()
     assert not r.rotates(rot, pos)
@@ -185,3 +187,29 @@ def test_runner_reads_sources_and_outputs_where_they_are(lib, monkeypatch):
     assert all(new(1, n).data_ptr() != seen for n in range(1, 4) for _ in range(8))
     step()
     assert lib.seen["k"] == k.data_ptr()
+
+
+def test_runner_with_rotary_on_another_device_is_refused(lib, monkeypatch):
+    r, rot = runner(), spec()
+    row, pos = np.zeros(4, np.int32), torch.zeros((4, 1), dtype=torch.int32)
+    k, v, q = (torch.zeros((4, h, D), dtype=BF16) for h in (1, 1, 2))
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))   # (as if on the GPU)
+    out, lse = torch.zeros((4, 2, D), dtype=BF16), torch.zeros((4, 2))
+    r.set_rotary(rot, pos)
+    r.step(k, v, q, row, 1.0, out, lse)
+    lib.seen.clear()
+    monkeypatch.setattr(pa, "_current_device", lambda: 1)
+    with pytest.raises(ValueError, match="device"):
+        r.step(k, v, q, row, 1.0, out, lse)
+    with pytest.raises(ValueError, match="device"):
+        r.set_rotary(rot, pos)
+    assert not lib.seen
+
+
+def test_loop_over_a_pool_on_another_device_than_its_rotary(lib, monkeypatch):
+    from paper_2608_06146_gb300 import engine
+    rot = spec(norm=False)
+    monkeypatch.setattr(torch.cuda, "Event", lambda: None)
+    with pytest.raises(ValueError, match="device"):
+        engine.MaskedParallelLoop(2, 2, 1, D, BF16, "meta", rotary=rot)
+    engine.MaskedParallelLoop(2, 2, 1, D, BF16, "cpu", rotary=rot)
