@@ -770,8 +770,9 @@ padoc_status padoc_qk_rotary_bwd(const padoc_rotary *rot, const padoc_qkv_rows *
  * src_rows NULL) of `in` gives its K heads, normed and rotated, and its V heads to pool slot slots[i], and,
  * when in->q is not NULL, its query heads, normed and rotated, to row i of q_dst ([count][Hq][d], contiguous).
  * The pool has the rows' dtype, KV heads and head_dim; its results are those of padoc_qk_rotary followed by
- * padoc_append_inputs. A call's slots are distinct (two inputs of one slot race). A slot or source row out of range
- * sets the device error word (code 1) and that input is skipped. Errors: INVALID_ARGUMENT, UNSUPPORTED, CUDA. */
+ * padoc_append_inputs. A call's slots are distinct (two inputs of one slot race), and q_dst and the pool do not
+ * overlap the sources. A slot or source row out of range sets the device error word (code 1) and that input is
+ * skipped. Errors: INVALID_ARGUMENT, UNSUPPORTED, CUDA. */
 padoc_status padoc_append_rotary_inputs(const padoc_kv_pool *pool, const padoc_rotary *rot, const padoc_qkv_rows *in,
                                         void *q_dst, const int32_t *src_rows, const int32_t *slots, int32_t count,
                                         padoc_stream_t stream);
