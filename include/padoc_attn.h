@@ -920,6 +920,121 @@ padoc_status padoc_ancestor_prefill_bwd(const void *q, const void *k, const void
                                         void *workspace, size_t workspace_bytes, padoc_stream_t stream);
 
 /* ============================================================================================
+ * Cross attention: query rows over an encoder's states of another length
+ * ========================================================================================== */
+
+/* One segment (host): query rows [q_begin, q_begin + q_len) see key rows [k_begin, k_begin + k_len), all of them
+ * and no others (e.g. a page's tokens or live streams over the states of its image, a branch's over its region's
+ * crop). Segments come in ascending order of q_begin and share no query row; their key ranges may overlap or
+ * coincide. k_len 0: the rows see nothing (out 0, lse -inf, dq 0, and they add nothing to dk and dv). q_len 0: no
+ * rows. */
+typedef struct {
+    int32_t q_begin;
+    int32_t q_len;
+    int32_t k_begin;
+    int32_t k_len;
+} padoc_cross_segment;
+
+typedef struct {
+    int32_t num_q_heads;
+    int32_t num_kv_heads;   /* num_q_heads / num_kv_heads <= 64 */
+    int32_t head_dim;       /* 64 or 128 */
+    padoc_dtype dtype;
+    int32_t backward;       /* 1: the plan also serves padoc_cross_attn_bwd */
+    int32_t ctas;           /* CTAs the work is balanced over; 0: the current device's multiprocessor count */
+} padoc_cross_config;
+
+/* Host summary of a cross-attention plan, filled by padoc_build_cross_plan. The int32 plan blob it describes must be
+ * copied to the device unchanged (16-byte aligned) and passed as plan_dev. */
+typedef struct {
+    padoc_cross_config cfg;
+    int32_t num_segments;
+    int32_t query_rows;      /* query rows the segments reach to (their largest q_begin + q_len) */
+    int32_t key_rows;        /* key rows they reach to */
+    int32_t pair;            /* 1: the forward's units are 512 rows for a pair of CTAs, else 256 for one */
+    int32_t num_units;       /* forward: work items, each for every KV head */
+    int32_t num_merges;      /* row blocks whose key range is split over several items (or empty) */
+    int32_t num_slots;       /* partial results, each for every KV head */
+    int32_t num_dq_units;    /* the same of the backward's dq pass */
+    int32_t num_dq_merges;
+    int32_t num_dq_slots;
+    int32_t num_subs;        /* blocks of 64 rows whose statistics the backward keeps */
+    int32_t num_key_tiles;   /* backward: key tiles of at most 128 rows, seen by the same segments as a whole */
+    int32_t num_covers;      /* (key interval, segment) pairs */
+    int32_t max_steps;       /* most blocks of 64 rows that see one key tile */
+    int32_t reserved;
+    int64_t pairs;           /* visible (query row, key row) pairs */
+    int64_t plan_ints;       /* int32 words in the plan blob */
+    int64_t off_units;       /* offsets (int32 words) of the blob's arrays */
+    int64_t off_merges;
+    int64_t off_dq_units;
+    int64_t off_dq_merges;
+    int64_t off_key_tiles;
+    int64_t off_covers;
+} padoc_cross_plan;
+
+/* Size in int32 words of the plan blob. Errors as padoc_build_cross_plan. */
+padoc_status padoc_cross_plan_size(const padoc_cross_segment *segments, int32_t num_segments,
+                                   const padoc_cross_config *cfg, int64_t *plan_ints);
+
+/* Builds the plan (host): the forward's items, heavier ones first, with key ranges split over the chip where there
+ * are few rows, and for training the backward's. plan: (host) int32 [capacity_ints]; info: (host) summary.
+ * Errors: INVALID_ARGUMENT (also segments out of order or sharing query rows, rows past 2^31 - 1024); UNSUPPORTED;
+ * CAPACITY when capacity_ints is too small. */
+padoc_status padoc_build_cross_plan(const padoc_cross_segment *segments, int32_t num_segments,
+                                    const padoc_cross_config *cfg, int32_t *plan, int64_t capacity_ints,
+                                    padoc_cross_plan *info);
+
+/* Workspace (device) bytes of padoc_cross_attn and of padoc_cross_attn_bwd for this plan (0 or more). */
+padoc_status padoc_cross_workspace_size(const padoc_cross_plan *info, size_t *bytes);
+padoc_status padoc_cross_bwd_workspace_size(const padoc_cross_plan *info, size_t *bytes);
+
+/* Query, key and value rows (device), e.g. slices of a projection's output: row r's query heads start at
+ * q + r * q_stride elements, [Hq][head_dim], its key and value heads at k + r * k_stride and v + r * v_stride,
+ * [Hkv][head_dim]. Bases and strides are multiples of 16 bytes, a stride at least a row's heads. Rows that no
+ * segment names are not read, whatever they hold. */
+typedef struct {
+    const void *q;
+    const void *k;
+    const void *v;
+    int64_t q_stride;
+    int64_t k_stride;
+    int64_t v_stride;
+    int64_t query_rows;   /* >= the plan's query_rows */
+    int64_t key_rows;     /* >= the plan's key_rows */
+} padoc_cross_rows;
+
+/* Cross attention of every segment: out [query_rows][Hq][head_dim] (device) in the rows' dtype, lse fp32
+ * [query_rows][Hq] (device). Query rows in no segment are neither read nor written. The serving form for single
+ * tokens is the same call with a plan of the live streams' rows (few rows, long key ranges: split and joined).
+ * bf16: head_dim 64 or 128 on the tensor cores, P rounded to bf16 before its product, fp32 sums; f32: fp32 throughout.
+ * workspace: (device) >= padoc_cross_workspace_size bytes, 256-byte aligned (NULL when that is 0); calls that may run
+ * at the same time need one each. Outputs overlap no input. Errors: INVALID_ARGUMENT, UNSUPPORTED,
+ * WORKSPACE_TOO_SMALL, CUDA. */
+padoc_status padoc_cross_attn(const padoc_cross_plan *info, const int32_t *plan_dev, const padoc_cross_rows *rows,
+                              float scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                              padoc_stream_t stream);
+
+/* Gradients (device) in the rows' dtype, rows laid out as padoc_cross_rows' (dk and dv may lie side by side). */
+typedef struct {
+    void *dq;
+    void *dk;
+    void *dv;
+    int64_t dq_stride;
+    int64_t dk_stride;
+    int64_t dv_stride;
+} padoc_cross_grads;
+
+/* Gradients of padoc_cross_attn for an upstream gradient dout [query_rows][Hq][head_dim], with the forward's out and
+ * lse: dq of the segments' rows (others are not written), dk and dv of every key row, summed in a fixed order over all
+ * segments and query heads that see it (0 where none does). The plan must have been built with cfg.backward. No
+ * output overlaps an input or another output. workspace and errors as above. */
+padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const int32_t *plan_dev, const padoc_cross_rows *rows,
+                                  const void *out, const void *dout, const float *lse, float scale,
+                                  const padoc_cross_grads *grads, void *workspace, size_t workspace_bytes,
+                                  padoc_stream_t stream);
+
+/* ============================================================================================
  * Status
  * ========================================================================================== */
 

@@ -1,0 +1,651 @@
+// cross.cu -- cross attention (query rows over an encoder's states of another length): the host entry points, their
+// validation, the kernels that join split rows, and the fp32 kernels. The bf16 kernels run on the tensor cores
+// (cross_tc.cu, cross_bwd_tc.cu).
+//
+// Per segment, query head h of KV head g:  S = scale Q K^T,  lse = ln sum_j exp S_j,  O = sum_j exp(S_j - lse) V_j;
+//   P = exp(S - lse),  D = rowsum(dO * O),  dS = P (dO V^T - D),  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.
+#include <math.h>
+
+#include "cross.cuh"
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------
+// Joining split rows
+// ------------------------------------------------------------------------------------------------
+
+template <typename T>
+__device__ __forceinline__ void store4(T *p, float4 x)
+{
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4 *>(p) = x;
+    } else {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
+    }
+}
+
+// A warp per packed row. Parts hold O / l and lse * log2(e), so O = sum_i w_i O_i with w_i = 2^(lse2_i - lse2); dq's
+// are plain sums. Parts are added in their order. Rows without parts (segments without keys) get O = 0, lse = -inf.
+template <typename T, int D, bool kDq>
+__global__ void __launch_bounds__(256) cross_merge_kernel(const padoc_cross_args a)
+{
+    constexpr int kRows = (kDq ? PADOC_CROSS_DQ_BLOCKS : PADOC_CROSS_UNIT_BLOCKS) * PADOC_CROSS_BLOCK;
+    constexpr int kPer = kRows / 8, E = D / 32;
+    const int unit = blockIdx.x / kPer, row = (blockIdx.x % kPer) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const padoc_cross_merge m = a.merges[unit / a.hkv];
+    const int g = unit % a.hkv;
+    int token, head;
+    const bool in = cross_row(a, m.tok, m.ntok, row, token, head);
+    pdl_wait_prerequisite();
+    if (!in) return;
+    const size_t h = (size_t)token * a.hq + g * a.group + head;
+    float acc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    float top = -INFINITY, sum = 0.f;
+    if (!kDq)
+        for (int i = 0; i < m.parts; ++i) top = fmaxf(top, a.part_lse[((size_t)(m.slot + i) * a.hkv + g) * kRows + row]);
+    for (int i = 0; i < m.parts; ++i) {
+        const size_t r = ((size_t)(m.slot + i) * a.hkv + g) * kRows + row;
+        float w = 1.f;
+        if (!kDq) {
+            const float l = a.part_lse[r];
+            w = l == -INFINITY ? 0.f : exp2f(l - top);
+            sum += w;
+        }
+        const float *p = a.part + r * D + lane * E;
+        float x[E];
+        if constexpr (E == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(p);
+        else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(p);
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(w, x[e], acc[e]);
+    }
+    float mul = kDq ? a.scale : sum > 0.f ? 1.f / sum : 0.f;
+    if (!kDq && isnan(sum)) mul = sum;
+    T *dst = kDq ? (T *)a.dq + (size_t)token * a.dq_stride + (size_t)(g * a.group + head) * D + lane * E
+                 : (T *)a.o + h * D + lane * E;
+    if constexpr (E == 4) {
+        store4(dst, make_float4(acc[0] * mul, acc[1] * mul, acc[2] * mul, acc[3] * mul));
+    } else {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float2 *>(dst) = make_float2(acc[0] * mul, acc[1] * mul);
+        else *reinterpret_cast<uint32_t *>(dst) = pack_bf16x2(acc[0] * mul, acc[1] * mul);
+    }
+    if (!kDq && lane == 0) a.lse[h] = sum > 0.f ? (top + log2f(sum)) * PADOC_LN2 : isnan(sum) ? sum : -INFINITY;
+}
+
+template <typename T, int D, bool kDq>
+padoc_status launch_merge(const padoc_cross_args &a, bool pdl, cudaStream_t stream)
+{
+    constexpr int kPer = (kDq ? PADOC_CROSS_DQ_BLOCKS : PADOC_CROSS_UNIT_BLOCKS) * PADOC_CROSS_BLOCK / 8;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)(a.num_merges * a.hkv * kPer));
+    lc.blockDim = dim3(256);
+    lc.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = pdl ? 1 : 0;
+    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, cross_merge_kernel<T, D, kDq>, a));
+    return padoc_launch_status();
+}
+
+// ------------------------------------------------------------------------------------------------
+// fp32: 64 packed rows a CTA of 256 threads, in steps of 64 keys. Tiles lie in shared memory, rows four
+// floats further apart than their length (a quarter warp's 16-byte reads of eight rows then meet no bank twice); a
+// thread keeps four rows by four columns of a 64 x 64 product, or four rows by D / 16 columns of a 64 x D one.
+// ------------------------------------------------------------------------------------------------
+
+constexpr int kB = PADOC_CROSS_BLOCK;
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T *p)
+{
+    if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float4 *>(p);
+    const uint2 w = *reinterpret_cast<const uint2 *>(p);
+    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                       __uint_as_float(w.y & 0xffff0000u));
+}
+
+template <int D>
+struct Simt {
+    static constexpr int P = D + 4;          // pitch of a tile's rows
+    static constexpr int PS = kB + 4;        // ... of a 64 x 64 product's
+    static constexpr int kTile = kB * P;
+
+    // 64 rows of D values; row r at base(r), or zeros where that is null
+    template <typename T, typename F>
+    static __device__ __forceinline__ void load(float *dst, F base)
+    {
+        for (int i = threadIdx.x; i < kB * (D / 4); i += 256) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4;
+            const T *p = base(r);
+            *reinterpret_cast<float4 *>(dst + r * P + c) = p ? load4(p + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
+    // acc[i][j] = x[4 ty + i] . y[tx + 16 j]
+    static __device__ __forceinline__ void dots(const float *x, const float *y, float (&acc)[4][4])
+    {
+        const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+#pragma unroll 4
+        for (int d = 0; d < D; d += 4) {
+            float4 a[4], b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                a[i] = *reinterpret_cast<const float4 *>(x + (4 * ty + i) * P + d);
+                b[i] = *reinterpret_cast<const float4 *>(y + (tx + 16 * i) * P + d);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    acc[i][j] = fmaf(a[i].x, b[j].x, acc[i][j]);
+                    acc[i][j] = fmaf(a[i].y, b[j].y, acc[i][j]);
+                    acc[i][j] = fmaf(a[i].z, b[j].z, acc[i][j]);
+                    acc[i][j] = fmaf(a[i].w, b[j].w, acc[i][j]);
+                }
+        }
+    }
+    // acc[i][4 j + e] += sum_k s[4 ty + i][k] y[k][64 j + 4 tx + e]
+    static __device__ __forceinline__ void add_product(const float *s, const float *y, float (&acc)[4][D / 16])
+    {
+        const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+#pragma unroll 4
+        for (int k = 0; k < kB; ++k) {
+            float w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = s[(4 * ty + i) * PS + k];
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) {
+                const float4 b = *reinterpret_cast<const float4 *>(y + k * P + 64 * j + 4 * tx);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    acc[i][4 * j] = fmaf(w[i], b.x, acc[i][4 * j]);
+                    acc[i][4 * j + 1] = fmaf(w[i], b.y, acc[i][4 * j + 1]);
+                    acc[i][4 * j + 2] = fmaf(w[i], b.z, acc[i][4 * j + 2]);
+                    acc[i][4 * j + 3] = fmaf(w[i], b.w, acc[i][4 * j + 3]);
+                }
+            }
+        }
+    }
+    static __device__ __forceinline__ void zero(float (&acc)[4][D / 16])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) acc[i][c] = 0.f;
+    }
+};
+
+// over the 16 threads that share rows 4 ty .. 4 ty + 3
+__device__ __forceinline__ float max16(float x)
+{
+#pragma unroll
+    for (int s = 8; s; s >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, s));
+    return x;
+}
+__device__ __forceinline__ float sum16(float x)
+{
+#pragma unroll
+    for (int s = 8; s; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
+    return x;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) cross_fwd_simt_kernel(const padoc_cross_args a)
+{
+    using S = Simt<D>;
+    extern __shared__ __align__(16) float sm[];
+    float *sq = sm, *sk = sq + S::kTile, *sv = sk + S::kTile, *sp = sv + S::kTile;
+    const int unit = blockIdx.x / PADOC_CROSS_UNIT_BLOCKS, blk = blockIdx.x % PADOC_CROSS_UNIT_BLOCKS;
+    const padoc_cross_unit u = a.units[unit / a.hkv];
+    const int g = unit % a.hkv, ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    pdl_launch_dependents();
+    if (blk * a.block_tokens >= u.ntok) return;
+    auto heads_row = [&](const void *base, int64_t stride, int r) -> const T * {
+        int token, head;
+        if (!cross_row(a, u.tok, u.ntok, blk * kB + r, token, head)) return nullptr;
+        return (const T *)base + (size_t)token * stride + (size_t)(g * a.group + head) * D;
+    };
+    S::template load<T>(sq, [&](int r) { return heads_row(a.q, a.q_stride, r); });
+    float acc[4][D / 16], m[4], l[4];
+    S::zero(acc);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+    for (int j0 = 0; j0 < u.nk; j0 += kB) {
+        __syncthreads();
+        auto key_row = [&](const void *base, int64_t stride, int r) -> const T * {
+            return j0 + r < u.nk ? (const T *)base + (size_t)(u.k0 + j0 + r) * stride + (size_t)g * D : nullptr;
+        };
+        S::template load<T>(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
+        S::template load<T>(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
+        __syncthreads();
+        float s[4][4];
+        S::dots(sq, sk, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float mx = m[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[i][j] = j0 + tx + 16 * j < u.nk ? s[i][j] * a.scale_log2 : -INFINITY;
+                mx = fmaxf(mx, s[i][j]);
+            }
+            mx = max16(mx);
+            const float ref = mx == -INFINITY ? 0.f : mx, alpha = exp2f(m[i] - ref);
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = exp2f(s[i][j] - ref);
+                sum += p;
+                sp[(4 * ty + i) * S::PS + tx + 16 * j] = p;
+            }
+            l[i] = l[i] * alpha + sum16(sum);
+            m[i] = mx;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) acc[i][c] *= alpha;
+        }
+        __syncwarp();   // (a product's rows are written and read by the same half warp)
+        S::add_product(sp, sv, acc);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = blk * kB + 4 * ty + i;
+        int token, head;
+        if (!cross_row(a, u.tok, u.ntok, r, token, head)) continue;
+        const float inv = l[i] == 0.f ? 0.f : 1.f / l[i], lse2 = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
+        const size_t h = (size_t)token * a.hq + g * a.group + head;
+        const size_t pr = ((size_t)max(u.slot, 0) * a.hkv + g) * (PADOC_CROSS_UNIT_BLOCKS * kB) + r;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+            const float4 x = make_float4(acc[i][4 * j] * inv, acc[i][4 * j + 1] * inv, acc[i][4 * j + 2] * inv, acc[i][4 * j + 3] * inv);
+            if (u.slot < 0) store4((T *)a.o + h * D + 64 * j + 4 * tx, x);
+            else store4(a.part + pr * D + 64 * j + 4 * tx, x);
+        }
+        if (tx == 0) {
+            if (u.slot < 0) a.lse[h] = lse2 * PADOC_LN2;
+            else a.part_lse[pr] = lse2;
+        }
+    }
+}
+
+// dQ, and the rows' statistics for the dK/dV pass.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) cross_dq_simt_kernel(const padoc_cross_args a)
+{
+    using S = Simt<D>;
+    extern __shared__ __align__(16) float sm[];
+    float *sq = sm, *sg = sq + S::kTile, *sk = sg + S::kTile, *sv = sk + S::kTile, *sp = sv + S::kTile;
+    float *st = sp + kB * S::PS;   // -lse2 and D
+    const int unit = blockIdx.x / PADOC_CROSS_DQ_BLOCKS, blk = blockIdx.x % PADOC_CROSS_DQ_BLOCKS;
+    const padoc_cross_unit u = a.units[unit / a.hkv];
+    const int g = unit % a.hkv, ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    if (blk * a.block_tokens >= u.ntok) return;
+    auto heads_row = [&](const void *base, int64_t stride, int r) -> const T * {
+        int token, head;
+        if (!cross_row(a, u.tok, u.ntok, blk * kB + r, token, head)) return nullptr;
+        return (const T *)base + (size_t)token * stride + (size_t)(g * a.group + head) * D;
+    };
+    S::template load<T>(sq, [&](int r) { return heads_row(a.q, a.q_stride, r); });
+    S::template load<T>(sg, [&](int r) { return heads_row(a.dout, (int64_t)a.hq * D, r); });
+    for (int r = threadIdx.x >> 5; r < kB; r += 8) {   // a warp per row
+        const T *o = heads_row(a.out, (int64_t)a.hq * D, r), *d = heads_row(a.dout, (int64_t)a.hq * D, r);
+        const int c = threadIdx.x & 31;
+        float x = 0.f;
+        if (o && c < D / 4) {
+            const float4 u4 = load4(o + 4 * c), v4 = load4(d + 4 * c);
+            x = fmaf(u4.x, v4.x, fmaf(u4.y, v4.y, fmaf(u4.z, v4.z, u4.w * v4.w)));
+        }
+#pragma unroll
+        for (int s = 16; s; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
+        if (c == 0) {
+            int token, head;
+            const bool in = cross_row(a, u.tok, u.ntok, blk * kB + r, token, head);
+            const float l = in ? a.lse_in[(size_t)token * a.hq + g * a.group + head] : -INFINITY;
+            st[r] = l == -INFINITY ? -INFINITY : -l * PADOC_LOG2E;
+            st[kB + r] = in ? x : 0.f;
+            if (u.sub >= 0) {
+                const size_t at = ((size_t)g * a.num_subs + u.sub + blk) * kB + r;
+                a.neg_lse2[at] = st[r];
+                a.dsum[at] = st[kB + r];
+            }
+        }
+    }
+    float acc[4][D / 16];
+    S::zero(acc);
+    for (int j0 = 0; j0 < u.nk; j0 += kB) {
+        __syncthreads();
+        auto key_row = [&](const void *base, int64_t stride, int r) -> const T * {
+            return j0 + r < u.nk ? (const T *)base + (size_t)(u.k0 + j0 + r) * stride + (size_t)g * D : nullptr;
+        };
+        S::template load<T>(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
+        S::template load<T>(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
+        __syncthreads();
+        float s[4][4], dp[4][4];
+        S::dots(sq, sk, s);
+        S::dots(sg, sv, dp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = exp2f(fmaf(s[i][j], a.scale_log2, st[4 * ty + i]));
+                sp[(4 * ty + i) * S::PS + tx + 16 * j] = j0 + tx + 16 * j < u.nk ? p * (dp[i][j] - st[kB + 4 * ty + i]) : 0.f;
+            }
+        __syncwarp();
+        S::add_product(sp, sk, acc);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = blk * kB + 4 * ty + i;
+        int token, head;
+        if (!cross_row(a, u.tok, u.ntok, r, token, head)) continue;
+        const float mul = u.slot < 0 ? a.scale : 1.f;
+        const size_t pr = ((size_t)max(u.slot, 0) * a.hkv + g) * (PADOC_CROSS_DQ_BLOCKS * kB) + r;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+            const float4 x = make_float4(acc[i][4 * j] * mul, acc[i][4 * j + 1] * mul, acc[i][4 * j + 2] * mul, acc[i][4 * j + 3] * mul);
+            if (u.slot < 0) store4((T *)a.dq + (size_t)token * a.dq_stride + (size_t)(g * a.group + head) * D + 64 * j + 4 * tx, x);
+            else store4(a.part + pr * D + 64 * j + 4 * tx, x);
+        }
+    }
+}
+
+// dK and dV of 64 keys: the sums over every block of rows that sees them, in the covers' order.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_args a)
+{
+    using S = Simt<D>;
+    extern __shared__ __align__(16) float sm[];
+    float *sq = sm, *sg = sq + S::kTile, *sk = sg + S::kTile, *sv = sk + S::kTile, *sp = sv + S::kTile, *sd = sp + kB * S::PS;
+    const int half = blockIdx.x & 1, unit = blockIdx.x >> 1, g = unit % a.hkv, i0 = unit / a.hkv;
+    padoc_cross_key_tile t;
+    if (i0 < a.num_tiles) t = a.tiles[i0];
+    else {
+        t.k0 = a.tail_begin + (i0 - a.num_tiles) * PADOC_CROSS_KEY_TILE;
+        t.nk = (int)min((int64_t)PADOC_CROSS_KEY_TILE, a.key_rows - t.k0);
+        t.cover = t.ncover = t.steps = 0;
+    }
+    const int k0 = t.k0 + half * kB, nk = min(kB, t.nk - half * kB), ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    if (nk <= 0) return;
+    float ak[4][D / 16], av[4][D / 16];
+    S::zero(ak);
+    S::zero(av);
+    if (t.steps > 0) {
+        auto key_row = [&](const void *base, int64_t stride, int r) -> const T * {
+            return r < nk ? (const T *)base + (size_t)(k0 + r) * stride + (size_t)g * D : nullptr;
+        };
+        S::template load<T>(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
+        S::template load<T>(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
+    }
+    for (int ci = 0; ci < t.ncover; ++ci) {
+        const padoc_cross_cover c = a.covers[t.cover + ci];
+        for (int b = 0; b < c.nsub; ++b) {
+            auto heads_row = [&](const void *base, int64_t stride, int r) -> const T * {
+                int token, head;
+                if (!cross_row(a, c.tok, c.ntok, b * kB + r, token, head)) return nullptr;
+                return (const T *)base + (size_t)token * stride + (size_t)(g * a.group + head) * D;
+            };
+            __syncthreads();
+            S::template load<T>(sq, [&](int r) { return heads_row(a.q, a.q_stride, r); });
+            S::template load<T>(sg, [&](int r) { return heads_row(a.dout, (int64_t)a.hq * D, r); });
+            __syncthreads();
+            float s[4][4], dp[4][4];
+            S::dots(sk, sq, s);
+            S::dots(sv, sg, dp);
+            const size_t at = ((size_t)g * a.num_subs + c.sub + b) * kB;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = tx + 16 * j;
+                const float l = a.neg_lse2[at + r], d = a.dsum[at + r];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = exp2f(fmaf(s[i][j], a.scale_log2, l));   // (rows past the segment's: l = -inf)
+                    sp[(4 * ty + i) * S::PS + r] = p;
+                    sd[(4 * ty + i) * S::PS + r] = p * (dp[i][j] - d);
+                }
+            }
+            __syncwarp();
+            S::add_product(sp, sg, av);
+            S::add_product(sd, sq, ak);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 4 * ty + i;
+        if (r >= nk) continue;
+        T *dk = (T *)a.dk + (size_t)(k0 + r) * a.dk_stride + (size_t)g * D, *dv = (T *)a.dv + (size_t)(k0 + r) * a.dv_stride + (size_t)g * D;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+            store4(dk + 64 * j + 4 * tx, make_float4(ak[i][4 * j] * a.scale, ak[i][4 * j + 1] * a.scale, ak[i][4 * j + 2] * a.scale, ak[i][4 * j + 3] * a.scale));
+            store4(dv + 64 * j + 4 * tx, make_float4(av[i][4 * j], av[i][4 * j + 1], av[i][4 * j + 2], av[i][4 * j + 3]));
+        }
+    }
+}
+
+template <typename T, int D>
+padoc_status run_fwd_simt(const padoc_cross_args &a, cudaStream_t cs)
+{
+    constexpr int bytes = (3 * Simt<D>::kTile + kB * Simt<D>::PS) * 4;
+    auto kernel = cross_fwd_simt_kernel<T, D>;
+    if (const padoc_status st = padoc_set_max_smem((const void *)kernel, bytes)) return st;
+    kernel<<<(unsigned)(a.num_units * a.hkv * PADOC_CROSS_UNIT_BLOCKS), 256, bytes, cs>>>(a);
+    return padoc_launch_status();
+}
+
+template <typename T, int D>
+padoc_status run_bwd_simt(const padoc_cross_args &a, cudaStream_t cs)
+{
+    constexpr int dq_bytes = (4 * Simt<D>::kTile + kB * Simt<D>::PS + 2 * kB) * 4;
+    constexpr int dkv_bytes = (4 * Simt<D>::kTile + 2 * kB * Simt<D>::PS) * 4;
+    auto dq = cross_dq_simt_kernel<T, D>;
+    auto dkv = cross_dkv_simt_kernel<T, D>;
+    padoc_status st = padoc_set_max_smem((const void *)dq, dq_bytes);
+    if (st == PADOC_OK) st = padoc_set_max_smem((const void *)dkv, dkv_bytes);
+    if (st != PADOC_OK) return st;
+    if (a.num_units) {
+        dq<<<(unsigned)(a.num_units * a.hkv * PADOC_CROSS_DQ_BLOCKS), 256, dq_bytes, cs>>>(a);
+        if ((st = padoc_launch_status()) != PADOC_OK) return st;
+    }
+    if (a.num_tiles + a.tail_tiles) {
+        dkv<<<(unsigned)((a.num_tiles + a.tail_tiles) * a.hkv * 2), 256, dkv_bytes, cs>>>(a);
+        st = padoc_launch_status();
+    }
+    return st;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Validation
+// ------------------------------------------------------------------------------------------------
+
+// Bytes that rows of `width` bytes every `stride` bytes take.
+struct Span {
+    uintptr_t base;
+    int64_t stride, width, rows;
+};
+
+// Whether two arrays of rows share a byte. Rows that lie side by side (slices of one buffer, equal strides) do not.
+bool overlap(const Span &x, const Span &y)
+{
+    if (x.rows == 0 || y.rows == 0) return false;
+    const uintptr_t xe = x.base + (uintptr_t)((x.rows - 1) * x.stride + x.width), ye = y.base + (uintptr_t)((y.rows - 1) * y.stride + y.width);
+    if (xe <= y.base || ye <= x.base) return false;
+    if (x.stride != y.stride) return true;
+    const int64_t d = (int64_t)((y.base >= x.base ? y.base - x.base : x.base - y.base) % (uintptr_t)x.stride);
+    const int64_t first = y.base >= x.base ? x.width : y.width, second = y.base >= x.base ? y.width : x.width;
+    return d < first || d + second > x.stride;
+}
+
+padoc_status check_rows(const padoc_cross_plan *info, const int32_t *plan, const padoc_cross_rows *r, float scale)
+{
+    if (!info || !r) return PADOC_ERR_INVALID_ARGUMENT;
+    const padoc_cross_config &c = info->cfg;
+    if (c.num_q_heads < 1 || c.num_kv_heads < 1 || c.num_q_heads % c.num_kv_heads) return PADOC_ERR_INVALID_ARGUMENT;
+    if (c.dtype != PADOC_DTYPE_F32 && c.dtype != PADOC_DTYPE_BF16) return PADOC_ERR_UNSUPPORTED;
+    if ((c.head_dim != 64 && c.head_dim != 128) || c.num_q_heads / c.num_kv_heads > kB) return PADOC_ERR_UNSUPPORTED;
+    if (!(scale > 0.f) || !isfinite(scale)) return PADOC_ERR_INVALID_ARGUMENT;
+    if (r->query_rows < info->query_rows || r->key_rows < info->key_rows || r->query_rows < 0 || r->key_rows < 0 ||
+        r->query_rows > INT32_MAX - 1024 || r->key_rows > INT32_MAX - 1024)
+        return PADOC_ERR_INVALID_ARGUMENT;
+    const int64_t e = c.dtype == PADOC_DTYPE_F32 ? 4 : 2;
+    const int64_t most = (int64_t)1 << 39;   // (a tensor map's strides have 40 bits)
+    for (const int64_t s : {r->q_stride, r->k_stride, r->v_stride})
+        if (s < 0 || s * e % 16 || s > most / e) return PADOC_ERR_INVALID_ARGUMENT;
+    if (r->q_stride < (int64_t)c.num_q_heads * c.head_dim || r->k_stride < (int64_t)c.num_kv_heads * c.head_dim ||
+        r->v_stride < (int64_t)c.num_kv_heads * c.head_dim)
+        return PADOC_ERR_INVALID_ARGUMENT;
+    if ((((uintptr_t)r->q) | ((uintptr_t)r->k) | ((uintptr_t)r->v) | ((uintptr_t)plan)) & 15) return PADOC_ERR_INVALID_ARGUMENT;
+    if (info->query_rows > 0 && (!r->q || !plan)) return PADOC_ERR_INVALID_ARGUMENT;
+    if (info->key_rows > 0 && (!r->k || !r->v)) return PADOC_ERR_INVALID_ARGUMENT;
+    return PADOC_OK;
+}
+
+void fill_args(padoc_cross_args &a, const padoc_cross_plan *info, const padoc_cross_rows *r, float scale)
+{
+    a = padoc_cross_args{};
+    a.q = r->q;
+    a.k = r->k;
+    a.v = r->v;
+    a.q_stride = r->q_stride;
+    a.k_stride = r->k_stride;
+    a.v_stride = r->v_stride;
+    a.query_rows = r->query_rows;
+    a.key_rows = r->key_rows;
+    a.hq = info->cfg.num_q_heads;
+    a.hkv = info->cfg.num_kv_heads;
+    a.group = a.hq / a.hkv;
+    a.block_tokens = kB / a.group;
+    a.scale = scale;
+    a.scale_log2 = scale * PADOC_LOG2E;
+}
+
+}  // namespace
+
+padoc_status padoc_cross_launch_merge(const padoc_cross_args &a, padoc_dtype dtype, int head_dim, bool dq, bool pdl, cudaStream_t cs)
+{
+#define PADOC_CROSS_MERGE(T, D) (dq ? launch_merge<T, D, true>(a, pdl, cs) : launch_merge<T, D, false>(a, pdl, cs))
+    if (dtype == PADOC_DTYPE_F32) return head_dim == 64 ? PADOC_CROSS_MERGE(float, 64) : PADOC_CROSS_MERGE(float, 128);
+    return head_dim == 64 ? PADOC_CROSS_MERGE(__nv_bfloat16, 64) : PADOC_CROSS_MERGE(__nv_bfloat16, 128);
+#undef PADOC_CROSS_MERGE
+}
+
+extern "C" padoc_status padoc_cross_attn(const padoc_cross_plan *info, const int32_t *plan_dev, const padoc_cross_rows *rows,
+                                         float scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                                         padoc_stream_t stream)
+{
+    padoc_status st = check_rows(info, plan_dev, rows, scale);
+    if (st != PADOC_OK) return st;
+    if (info->query_rows == 0) return PADOC_OK;
+    if (!out || !lse || (((uintptr_t)out) & 15) || (((uintptr_t)lse) & 3)) return PADOC_ERR_INVALID_ARGUMENT;
+    size_t need = 0;
+    if ((st = padoc_cross_workspace_size(info, &need)) != PADOC_OK) return st;
+    if (need && (!workspace || (((uintptr_t)workspace) & 255))) return PADOC_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < need) return PADOC_ERR_WORKSPACE_TOO_SMALL;
+    const padoc_cross_config &c = info->cfg;
+    const int64_t e = c.dtype == PADOC_DTYPE_F32 ? 4 : 2, qw = (int64_t)c.num_q_heads * c.head_dim * e, kw = (int64_t)c.num_kv_heads * c.head_dim * e;
+    const Span in[] = {{(uintptr_t)rows->q, rows->q_stride * e, qw, info->query_rows},
+                       {(uintptr_t)rows->k, rows->k_stride * e, kw, info->key_rows},
+                       {(uintptr_t)rows->v, rows->v_stride * e, kw, info->key_rows}};
+    const Span to[] = {{(uintptr_t)out, qw, qw, info->query_rows},
+                       {(uintptr_t)lse, (int64_t)c.num_q_heads * 4, (int64_t)c.num_q_heads * 4, info->query_rows}};
+    if (overlap(to[0], to[1])) return PADOC_ERR_INVALID_ARGUMENT;
+    for (const Span &x : to)
+        for (const Span &y : in)
+            if (overlap(x, y)) return PADOC_ERR_INVALID_ARGUMENT;
+
+    padoc_cross_args a;
+    fill_args(a, info, rows, scale);
+    a.units = (const padoc_cross_unit *)(plan_dev + info->off_units);
+    a.merges = (const padoc_cross_merge *)(plan_dev + info->off_merges);
+    a.num_units = info->num_units;
+    a.num_merges = info->num_merges;
+    a.o = out;
+    a.lse = lse;
+    a.part = (float *)workspace;
+    a.part_lse = a.part + (size_t)info->num_slots * a.hkv * (PADOC_CROSS_UNIT_BLOCKS * kB) * c.head_dim;
+    cudaStream_t cs = (cudaStream_t)stream;
+    if (a.num_units) {
+        if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_fwd_simt<float, 64>(a, cs) : run_fwd_simt<float, 128>(a, cs);
+        else st = c.head_dim == 64 ? run_fwd_simt<__nv_bfloat16, 64>(a, cs) : run_fwd_simt<__nv_bfloat16, 128>(a, cs);
+        if (st != PADOC_OK) return st;
+    }
+    return a.num_merges ? padoc_cross_launch_merge(a, c.dtype, c.head_dim, false, a.num_units > 0, cs) : PADOC_OK;
+}
+
+extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const int32_t *plan_dev, const padoc_cross_rows *rows,
+                                             const void *out, const void *dout, const float *lse, float scale,
+                                             const padoc_cross_grads *grads, void *workspace, size_t workspace_bytes,
+                                             padoc_stream_t stream)
+{
+    padoc_status st = check_rows(info, plan_dev, rows, scale);
+    if (st != PADOC_OK) return st;
+    if (!grads || !info->cfg.backward) return PADOC_ERR_INVALID_ARGUMENT;
+    const padoc_cross_config &c = info->cfg;
+    const int64_t e = c.dtype == PADOC_DTYPE_F32 ? 4 : 2;
+    for (const int64_t s : {grads->dq_stride, grads->dk_stride, grads->dv_stride})
+        if (s < 0 || s * e % 16 || s > ((int64_t)1 << 39) / e) return PADOC_ERR_INVALID_ARGUMENT;
+    if (grads->dq_stride < (int64_t)c.num_q_heads * c.head_dim || grads->dk_stride < (int64_t)c.num_kv_heads * c.head_dim ||
+        grads->dv_stride < (int64_t)c.num_kv_heads * c.head_dim)
+        return PADOC_ERR_INVALID_ARGUMENT;
+    if (info->query_rows > 0 && (!out || !dout || !lse || !grads->dq)) return PADOC_ERR_INVALID_ARGUMENT;
+    if (rows->key_rows > 0 && (!grads->dk || !grads->dv)) return PADOC_ERR_INVALID_ARGUMENT;
+    if (((((uintptr_t)out) | ((uintptr_t)dout) | ((uintptr_t)grads->dq) | ((uintptr_t)grads->dk) | ((uintptr_t)grads->dv)) & 15) ||
+        (((uintptr_t)lse) & 3))
+        return PADOC_ERR_INVALID_ARGUMENT;
+    size_t need = 0;
+    if ((st = padoc_cross_bwd_workspace_size(info, &need)) != PADOC_OK) return st;
+    if (need && (!workspace || (((uintptr_t)workspace) & 255))) return PADOC_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < need) return PADOC_ERR_WORKSPACE_TOO_SMALL;
+    const int64_t qw = (int64_t)c.num_q_heads * c.head_dim * e, kw = (int64_t)c.num_kv_heads * c.head_dim * e, lw = (int64_t)c.num_q_heads * 4;
+    const Span in[] = {{(uintptr_t)rows->q, rows->q_stride * e, qw, info->query_rows},
+                       {(uintptr_t)rows->k, rows->k_stride * e, kw, info->key_rows},
+                       {(uintptr_t)rows->v, rows->v_stride * e, kw, info->key_rows},
+                       {(uintptr_t)out, qw, qw, info->query_rows},
+                       {(uintptr_t)dout, qw, qw, info->query_rows},
+                       {(uintptr_t)lse, lw, lw, info->query_rows}};
+    const Span to[] = {{(uintptr_t)grads->dq, grads->dq_stride * e, qw, info->query_rows},
+                       {(uintptr_t)grads->dk, grads->dk_stride * e, kw, rows->key_rows},
+                       {(uintptr_t)grads->dv, grads->dv_stride * e, kw, rows->key_rows}};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (overlap(to[i], to[j])) return PADOC_ERR_INVALID_ARGUMENT;
+        for (const Span &y : in)
+            if (overlap(to[i], y)) return PADOC_ERR_INVALID_ARGUMENT;
+    }
+
+    padoc_cross_args a;
+    fill_args(a, info, rows, scale);
+    a.units = (const padoc_cross_unit *)(plan_dev + info->off_dq_units);
+    a.merges = (const padoc_cross_merge *)(plan_dev + info->off_dq_merges);
+    a.tiles = (const padoc_cross_key_tile *)(plan_dev + info->off_key_tiles);
+    a.covers = (const padoc_cross_cover *)(plan_dev + info->off_covers);
+    a.num_units = info->num_dq_units;
+    a.num_merges = info->num_dq_merges;
+    a.num_tiles = info->num_key_tiles;
+    a.num_subs = info->num_subs;
+    // the key tiles reach to the last key that a row sees; behind it the gradients are zero
+    a.tail_begin = info->key_rows;
+    a.tail_tiles = (int32_t)((rows->key_rows - info->key_rows + PADOC_CROSS_KEY_TILE - 1) / PADOC_CROSS_KEY_TILE);
+    if ((int64_t)(a.num_tiles + (int64_t)a.tail_tiles) * a.hkv * 8 > INT32_MAX) return PADOC_ERR_UNSUPPORTED;
+    if (a.num_units + a.num_merges + a.num_tiles + a.tail_tiles == 0) return PADOC_OK;
+    a.out = out;
+    a.dout = dout;
+    a.lse_in = lse;
+    a.dq = grads->dq;
+    a.dk = grads->dk;
+    a.dv = grads->dv;
+    a.dq_stride = grads->dq_stride;
+    a.dk_stride = grads->dk_stride;
+    a.dv_stride = grads->dv_stride;
+    const size_t stats = (size_t)info->num_subs * a.hkv * kB;
+    a.neg_lse2 = (float *)workspace;
+    a.dsum = a.neg_lse2 + stats;
+    a.part = a.dsum + stats;
+    cudaStream_t cs = (cudaStream_t)stream;
+    if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_bwd_simt<float, 64>(a, cs) : run_bwd_simt<float, 128>(a, cs);
+    else st = c.head_dim == 64 ? run_bwd_simt<__nv_bfloat16, 64>(a, cs) : run_bwd_simt<__nv_bfloat16, 128>(a, cs);
+    if (st != PADOC_OK) return st;
+    return a.num_merges ? padoc_cross_launch_merge(a, c.dtype, c.head_dim, true, false, cs) : PADOC_OK;
+}

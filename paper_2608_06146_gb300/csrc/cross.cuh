@@ -1,0 +1,41 @@
+// cross.cuh -- what the cross-attention kernels share: the packed rows of a block, and the arguments.
+#pragma once
+
+#include "common.cuh"
+#include "cross_internal.h"
+
+// Arguments of the forward and of both backward passes.
+struct padoc_cross_args {
+    const padoc_cross_unit *units;             // forward or dq items
+    const padoc_cross_merge *merges;
+    const padoc_cross_key_tile *tiles;
+    const padoc_cross_cover *covers;
+    const void *q, *k, *v, *out, *dout;
+    const float *lse_in;
+    int64_t q_stride, k_stride, v_stride;      // elements
+    int64_t query_rows, key_rows;
+    int64_t dq_stride, dk_stride, dv_stride;
+    void *o, *dq, *dk, *dv;
+    float *lse;
+    float *part, *part_lse;                    // partial results
+    float *neg_lse2, *dsum;                    // -lse * log2(e) and rowsum(dO * O): [Hkv][subs][64]
+    int32_t num_units, num_merges, num_tiles, num_subs;
+    int32_t tail_begin, tail_tiles;            // key rows that the plan does not reach
+    int32_t hq, hkv, group, block_tokens;      // block_tokens: 64 / group
+    float scale, scale_log2;
+    int *err;
+};
+
+// The (token, head) of packed row r (of a run of blocks) of a unit whose first token is tok: false past its rows.
+__device__ __forceinline__ bool cross_row(const padoc_cross_args &a, int tok, int ntok, int r, int &token, int &head)
+{
+    const int rr = r % PADOC_CROSS_BLOCK, t = rr / a.group;
+    const int i = r / PADOC_CROSS_BLOCK * a.block_tokens + t;
+    token = tok + i;
+    head = rr - t * a.group;
+    return t < a.block_tokens && i < ntok;
+}
+
+// Rows joined from parts, a warp per row: the forward's outputs and log-sum-exps (kDq 0), or dq (1).
+padoc_status padoc_cross_launch_merge(const padoc_cross_args &a, padoc_dtype dtype, int head_dim, bool dq, bool pdl,
+                                      cudaStream_t stream);

@@ -1,0 +1,41 @@
+// cross_internal.h -- layouts shared by the cross-attention planner and its kernels.
+//
+// Rows are packed for the tensor cores as (token, query head of the KV head's group): 64-row blocks of
+// 64 / group tokens, so that every query head of a KV head reads a key tile together, whatever the group. A tile is
+// two blocks, the M = 128 of the MMAs; the forward's unit is two tiles (a CTA) or four (a pair of CTAs).
+#pragma once
+
+#include <stdint.h>
+
+#include "padoc_attn.h"
+
+#define PADOC_CROSS_BLOCK 64         // rows of a block
+#define PADOC_CROSS_UNIT_BLOCKS 4    // blocks of the forward's unit (8 for a pair)
+#define PADOC_CROSS_DQ_BLOCKS 2      // blocks of the dq pass's unit
+#define PADOC_CROSS_KEY_TILE 128     // keys of a tile: of the forward's steps and of the dk/dv pass's units
+#define PADOC_CROSS_DQ_STEP 64       // keys of a step of the dq pass
+
+// Forward and dq work item: tokens of one segment over a part of its keys. 32 bytes.
+struct padoc_cross_unit {
+    int32_t tok, ntok;    // query rows
+    int32_t k0, nk;       // key rows, nk >= 1
+    int32_t slot;         // partial result, -1: the rows' whole key range, written as the output
+    int32_t sub;          // dq: index of the first block in the statistics, -1: another part writes them
+    int32_t pad[2];
+};
+// Rows joined from parts slot .. slot + parts - 1 (none: a segment without keys).
+struct padoc_cross_merge {
+    int32_t tok, ntok, slot, parts;
+};
+// Key rows that the same segments see: covers cover .. cover + ncover - 1, of `steps` blocks together. 32 bytes.
+struct padoc_cross_key_tile {
+    int32_t k0, nk;
+    int32_t cover, ncover;
+    int32_t steps;
+    int32_t pad[3];
+};
+struct padoc_cross_cover {
+    int32_t tok, ntok, sub, nsub;
+};
+
+// Blocks of the statistics, lse and D: [Hkv][num_subs][64] floats each.

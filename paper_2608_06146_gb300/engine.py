@@ -134,6 +134,33 @@ class RotaryPrefill:
         pa.padoc_qk_rotary_bwd(self.rotary, dq, dk, self.pos, dq, dk, q, k, dq_weight, dk_weight, self.workspace, stream)
 
 
+class CrossPlan:
+    """Cross attention of query rows over an encoder's states: the plan of segments (q_begin, q_len, k_begin, k_len)
+    on the device, with its workspaces. Calls that may run at the same time (two streams, two captured graphs) need a
+    CrossPlan each."""
+
+    def __init__(self, segments, num_q_heads: int, num_kv_heads: int, head_dim: int, dtype: torch.dtype, device,
+                 training: bool = False, ctas: int = 0):
+        self.cfg = pa.make_cross_config(num_q_heads, num_kv_heads, head_dim, dtype, training, ctas)
+        plan, self.info = pa.padoc_build_cross_plan(segments, self.cfg)
+        self.plan_dev = torch.from_numpy(plan.copy() if plan.size else np.zeros(1, np.int32)).to(device)
+        new = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+        self.workspace = new(pa.padoc_cross_workspace_size(self.info))
+        self.bwd_workspace = new(pa.padoc_cross_bwd_workspace_size(self.info)) if training else None
+
+    def run(self, q, k, v, scale, out, lse, stream=None):
+        """q [rows][Hq][d]; k, v [key rows][Hkv][d] (rows may lie apart); out like q, lse fp32 [rows][Hq]. Rows in no
+        segment are left as they are."""
+        pa.padoc_cross_attn(self.info, self.plan_dev, q, k, v, scale, out, lse, self.workspace, stream)
+
+    def run_bwd(self, q, k, v, out, dout, lse, scale, dq, dk, dv, stream=None):
+        """Gradients of run for its out and lse: dq of the segments' rows, dk and dv of every key row."""
+        if self.bwd_workspace is None:
+            raise ValueError("gradients need training=True")
+        pa.padoc_cross_attn_bwd(self.info, self.plan_dev, q, k, v, out, dout, lse, scale, dq, dk, dv, self.bwd_workspace,
+                                stream)
+
+
 class ChunkPrefillPlan:
     """Plan (C1) of a chunked prefill over the paged cache, uploaded: chunks of consecutive query
     tokens per stream (padoc_prefill_chunk rows), run by the decode kernels with the chunks' tokens

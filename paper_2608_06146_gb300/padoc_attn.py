@@ -127,6 +127,44 @@ class padoc_grid(ctypes.Structure):
                 ("w", ctypes.c_int32)]
 
 
+class padoc_cross_segment(ctypes.Structure):
+    _fields_ = [("q_begin", ctypes.c_int32), ("q_len", ctypes.c_int32), ("k_begin", ctypes.c_int32),
+                ("k_len", ctypes.c_int32)]
+
+
+class padoc_cross_config(ctypes.Structure):
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int), ("backward", ctypes.c_int32), ("ctas", ctypes.c_int32)]
+
+
+class padoc_cross_plan(ctypes.Structure):
+    _fields_ = [("cfg", padoc_cross_config), ("num_segments", ctypes.c_int32), ("query_rows", ctypes.c_int32),
+                ("key_rows", ctypes.c_int32), ("pair", ctypes.c_int32), ("num_units", ctypes.c_int32),
+                ("num_merges", ctypes.c_int32), ("num_slots", ctypes.c_int32), ("num_dq_units", ctypes.c_int32),
+                ("num_dq_merges", ctypes.c_int32), ("num_dq_slots", ctypes.c_int32), ("num_subs", ctypes.c_int32),
+                ("num_key_tiles", ctypes.c_int32), ("num_covers", ctypes.c_int32), ("max_steps", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("pairs", ctypes.c_int64), ("plan_ints", ctypes.c_int64),
+                ("off_units", ctypes.c_int64), ("off_merges", ctypes.c_int64), ("off_dq_units", ctypes.c_int64),
+                ("off_dq_merges", ctypes.c_int64), ("off_key_tiles", ctypes.c_int64), ("off_covers", ctypes.c_int64)]
+
+
+class padoc_cross_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("query_rows", ctypes.c_int64),
+                ("key_rows", ctypes.c_int64)]
+
+
+class padoc_cross_grads(ctypes.Structure):
+    _fields_ = [("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p),
+                ("dq_stride", ctypes.c_int64), ("dk_stride", ctypes.c_int64), ("dv_stride", ctypes.c_int64)]
+
+
+_CROSS_ROWS = struct.Struct("@3P5q")
+assert _CROSS_ROWS.size == ctypes.sizeof(padoc_cross_rows)
+_CROSS_GRADS = struct.Struct("@3P3q")
+assert _CROSS_GRADS.size == ctypes.sizeof(padoc_cross_grads)
+
+
 _lib = None
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _i64p = ctypes.POINTER(ctypes.c_int64)
@@ -237,6 +275,13 @@ def load_library(path: Optional[str] = None):
                                          ctypes.POINTER(padoc_kv_pool), _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp,
                                          ctypes.c_size_t, _vp],
         "padoc_mpd_runner_set_rotary": [_vp, _vp, _vp, ctypes.c_int64],
+        "padoc_cross_plan_size": [_vp, ctypes.c_int32, ctypes.POINTER(padoc_cross_config), _i64p],
+        "padoc_build_cross_plan": [_vp, ctypes.c_int32, ctypes.POINTER(padoc_cross_config), _i32p, ctypes.c_int64,
+                                   ctypes.POINTER(padoc_cross_plan)],
+        "padoc_cross_workspace_size": [ctypes.POINTER(padoc_cross_plan), ctypes.POINTER(ctypes.c_size_t)],
+        "padoc_cross_bwd_workspace_size": [ctypes.POINTER(padoc_cross_plan), ctypes.POINTER(ctypes.c_size_t)],
+        "padoc_cross_attn": [_vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, ctypes.c_size_t, _vp],
+        "padoc_cross_attn_bwd": [_vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp],
         "padoc_check_device_errors": [_vp],
         "padoc_last_device_error": [_i32p, _i32p],
         "padoc_status_string": [ctypes.c_int],
@@ -278,6 +323,8 @@ def exported_symbols() -> Sequence[str]:
                         "padoc_append_rotary_inputs_e4m3", "padoc_copy_kv_blocks", "padoc_copy_kv_blocks_e4m3",
                         "padoc_mpd_fork_stream", "padoc_mpd_drop_stream", "padoc_mpd_drop_page", "padoc_mpd_compact",
                         "padoc_mpd_resize", "padoc_mpd_launch_step_rotary", "padoc_mpd_runner_set_rotary",
+                        "padoc_cross_plan_size", "padoc_build_cross_plan", "padoc_cross_workspace_size",
+                        "padoc_cross_bwd_workspace_size", "padoc_cross_attn", "padoc_cross_attn_bwd",
                         "padoc_check_device_errors",
                         "padoc_last_device_error", "padoc_status_string", "padoc_version")]
 
@@ -1482,6 +1529,138 @@ def padoc_ancestor_prefill_bwd(q, k, v, out, dout, lse, spans_dev, q_map: padoc_
                                         _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(),
                                         _stream_ptr(stream))
     _check("padoc_ancestor_prefill_bwd", st)
+
+
+# ------------------------------------------------------------------------------------------------
+# Cross attention over an encoder's states
+# ------------------------------------------------------------------------------------------------
+
+def make_cross_config(num_q_heads: int, num_kv_heads: int, head_dim: int, dtype, backward: bool = False,
+                      ctas: int = 0) -> padoc_cross_config:
+    """dtype: torch.bfloat16 or torch.float32 (or its PADOC_DTYPE_ code)."""
+    import torch
+    code = {torch.bfloat16: PADOC_DTYPE_BF16, torch.float32: PADOC_DTYPE_F32}.get(dtype, dtype)
+    if not isinstance(code, int):
+        raise TypeError(f"unsupported dtype {dtype}")
+    return padoc_cross_config(num_q_heads, num_kv_heads, head_dim, code, int(bool(backward)), ctas)
+
+
+def _cross_segments(segments):
+    a = np.asarray(segments, np.int64).reshape(-1, 4)
+    if a.size and (a.min() < 0 or a.max() > 0x7fffffff):
+        raise ValueError("segments: rows from 0 to 2^31 - 1")
+    return np.ascontiguousarray(a, np.int32)
+
+
+def padoc_cross_plan_size(segments, cfg: padoc_cross_config) -> int:
+    a, n = _cross_segments(segments), ctypes.c_int64()
+    _check("padoc_cross_plan_size",
+           load_library().padoc_cross_plan_size(a.ctypes.data, a.shape[0], ctypes.byref(cfg), ctypes.byref(n)))
+    return n.value
+
+
+def padoc_build_cross_plan(segments, cfg: padoc_cross_config, out=None):
+    """The plan of segments (q_begin, q_len, k_begin, k_len), in ascending order of q_begin. Returns (plan blob int32,
+    padoc_cross_plan); ``out`` as in padoc_build_decode_plan."""
+    lib, a, info = load_library(), _cross_segments(segments), padoc_cross_plan()
+    buf = np.zeros(64 + 24 * a.shape[0], np.int32) if out is None else out
+    for _ in range(2):
+        st = lib.padoc_build_cross_plan(a.ctypes.data, a.shape[0], ctypes.byref(cfg), buf.ctypes.data_as(_i32p), buf.size,
+                                        ctypes.byref(info))
+        if st != 6 or info.plan_ints <= buf.size:
+            break
+        buf = np.zeros(int(info.plan_ints), np.int32)
+    _check("padoc_build_cross_plan", st)
+    return buf[:info.plan_ints], info
+
+
+def padoc_cross_workspace_size(info: padoc_cross_plan) -> int:
+    n = ctypes.c_size_t()
+    _check("padoc_cross_workspace_size", load_library().padoc_cross_workspace_size(ctypes.byref(info), ctypes.byref(n)))
+    return n.value
+
+
+def padoc_cross_bwd_workspace_size(info: padoc_cross_plan) -> int:
+    n = ctypes.c_size_t()
+    _check("padoc_cross_bwd_workspace_size",
+           load_library().padoc_cross_bwd_workspace_size(ctypes.byref(info), ctypes.byref(n)))
+    return n.value
+
+
+def _cross_heads(t, name, heads, info, device):
+    """(address, elements between rows, rows) of rows of heads, which may lie apart."""
+    c = info.cfg
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be a CUDA tensor on the current device, {device}")
+    if _dtype_code(t) != c.dtype:
+        raise TypeError(f"{name} must have the plan's dtype")
+    sh = t.shape
+    if len(sh) != 3 or sh[1] != heads or sh[2] != c.head_dim:
+        raise ValueError(f"{name} must be [rows][{heads}][{c.head_dim}]")
+    s = t.stride()
+    if sh[0] and (s[2] != 1 or (heads > 1 and s[1] != c.head_dim)):
+        raise ValueError(f"{name}: a row's heads must lie behind one another")
+    return t.data_ptr(), s[0] if sh[0] > 1 else heads * c.head_dim, sh[0]
+
+
+def _cross_rows(info, plan_dev, q, k, v, device):
+    import torch
+    if plan_dev.get_device() != device or plan_dev.dtype is not torch.int32 or not plan_dev.is_contiguous() or \
+            plan_dev.numel() < info.plan_ints:
+        raise ValueError("plan_dev must hold the plan's int32 words on the current device")
+    c = info.cfg
+    qp, qs, qn = _cross_heads(q, "q", c.num_q_heads, info, device)
+    kp, ks, kn = _cross_heads(k, "k", c.num_kv_heads, info, device)
+    vp, vs, vn = _cross_heads(v, "v", c.num_kv_heads, info, device)
+    if kn != vn:
+        raise ValueError("k and v must have as many rows")
+    return _CROSS_ROWS.pack(qp, kp, vp, qs, ks, vs, qn, kn)
+
+
+def _cross_like(t, name, shape, dtype, device):
+    if tuple(t.shape) != tuple(shape) or t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype} {list(shape)}")
+    return _on(t, name, device)
+
+
+def _cross_workspace(t, device):
+    if t is None:
+        return None, 0
+    return _on(t, "workspace", device), t.numel() * t.element_size()
+
+
+def padoc_cross_attn(info: padoc_cross_plan, plan_dev, q, k, v, scale, out, lse, workspace=None, stream=None):
+    """q [rows][Hq][d], k / v [key rows][Hkv][d] (rows may lie apart); out [rows][Hq][d], lse fp32 [rows][Hq], both
+    contiguous; workspace: padoc_cross_workspace_size bytes (None when that is 0)."""
+    import torch
+    dev = _current_device()
+    rows = _cross_rows(info, plan_dev, q, k, v, dev)
+    o = _cross_like(out, "out", q.shape, q.dtype, dev)
+    l = _cross_like(lse, "lse", q.shape[:2], torch.float32, dev)
+    ws, n = _cross_workspace(workspace, dev)
+    _check("padoc_cross_attn", load_library().padoc_cross_attn(ctypes.byref(info), plan_dev.data_ptr(), rows, scale, o, l,
+                                                               ws, n, _stream_ptr(stream)))
+
+
+def padoc_cross_attn_bwd(info: padoc_cross_plan, plan_dev, q, k, v, out, dout, lse, scale, dq, dk, dv, workspace=None,
+                         stream=None):
+    """Gradients of padoc_cross_attn: q, k, v, dq, dk, dv rows that may lie apart; out, dout, lse contiguous."""
+    import torch
+    dev = _current_device()
+    rows = _cross_rows(info, plan_dev, q, k, v, dev)
+    o = _cross_like(out, "out", q.shape, q.dtype, dev)
+    g = _cross_like(dout, "dout", q.shape, q.dtype, dev)
+    l = _cross_like(lse, "lse", q.shape[:2], torch.float32, dev)
+    if dq.shape != q.shape or dk.shape != k.shape or dv.shape != v.shape:
+        raise ValueError("dq, dk and dv must have the shapes of q, k and v")
+    c = info.cfg
+    qp, qs, _ = _cross_heads(dq, "dq", c.num_q_heads, info, dev)
+    kp, ks, _ = _cross_heads(dk, "dk", c.num_kv_heads, info, dev)
+    vp, vs, _ = _cross_heads(dv, "dv", c.num_kv_heads, info, dev)
+    ws, n = _cross_workspace(workspace, dev)
+    _check("padoc_cross_attn_bwd",
+           load_library().padoc_cross_attn_bwd(ctypes.byref(info), plan_dev.data_ptr(), rows, o, g, l, scale,
+                                               _CROSS_GRADS.pack(qp, kp, vp, qs, ks, vs), ws, n, _stream_ptr(stream)))
 
 
 def padoc_selftest_tcgen05(a, bk, v, c1, c2, c3, stream=None):

@@ -1,0 +1,271 @@
+"""Cross attention on the GPU against its definition in 64 bits, at the sizes and segments where it can go wrong.
+
+Tolerances are oracle.cross's bounds (derived there), element by element."""
+import math
+
+import pytest
+import torch
+
+from oracle import cross as oc
+from paper_2608_06146_gb300 import build as pbuild
+from paper_2608_06146_gb300 import padoc_attn as pa
+from paper_2608_06146_gb300.engine import CrossPlan
+
+pytestmark = pytest.mark.gpu
+DEV, BF16, F32 = "cuda:0", torch.bfloat16, torch.float32
+NAN = math.nan
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _build():
+    pbuild.build()
+    pa.load_library()
+
+
+def rows_of(n, heads, d, dtype, g, stride_heads=0):
+    """[n][heads][d], a slice of a wider buffer (filled with NaN) when stride_heads is more than heads."""
+    wide = torch.full((n, max(stride_heads, heads), d), NAN, dtype=dtype, device=DEV)
+    at = (max(stride_heads, heads) - heads) // 2
+    wide[:, at:at + heads] = torch.randn((n, heads, d), generator=g, device=DEV).to(dtype)
+    return wide[:, at:at + heads]
+
+
+def inputs(segments, hq, hkv, d, dtype, seed=0, rows=None, keys=None, wide=0, poison=True):
+    """q, k, v, dout; rows that no segment names hold NaN and infinities."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    rows = rows or max([s[0] + s[1] for s in segments]) + 3
+    keys = keys or max([s[2] + s[3] for s in segments]) + 2
+    q, dout = rows_of(rows, hq, d, dtype, g, hq + wide), rows_of(rows, hq, d, dtype, g)
+    k, v = rows_of(keys, hkv, d, dtype, g, hkv + 2 * wide), rows_of(keys, hkv, d, dtype, g, hkv + wide)
+    if poison:
+        nq, nk = torch.ones(rows, dtype=torch.bool), torch.ones(keys, dtype=torch.bool)
+        for a, n, b, m in segments:
+            nq[a:a + n] = False
+            nk[b:b + (m if n else 0)] = False
+        for t, bad in ((q, nq), (dout, nq), (k, nk), (v, nk)):
+            t[bad.to(DEV)] = torch.tensor([NAN, math.inf], device=DEV, dtype=dtype).repeat(d // 2)
+    return q, k, v, dout
+
+
+def within(got, want, bound, rows=None):
+    got, want = got.double(), want.clone()
+    if rows is not None:
+        got, want, bound = got[rows], want[rows], bound[rows]
+    same = (got == want) | ((got - want).abs() <= bound)
+    assert same.all(), f"{(~same).sum().item()} of {same.numel()} off, worst {((got - want).abs() / bound.clamp_min(1e-30)).nan_to_num(9e9).max().item():.3g} of the bound"
+
+
+def check_forward(segments, hq, hkv, d, dtype, ctas=0, **kw):
+    q, k, v, _ = inputs(segments, hq, hkv, d, dtype, **kw)
+    plan = CrossPlan(segments, hq, hkv, d, dtype, DEV, ctas=ctas)
+    out = torch.full((q.shape[0], hq, d), 77.0, dtype=dtype, device=DEV)
+    lse = torch.full((q.shape[0], hq), 77.0, device=DEV)
+    scale = 1 / math.sqrt(d)
+    plan.workspace.fill_(255)     # NaN
+    plan.run(q, k, v, scale, out, lse)
+    pa.padoc_check_device_errors()
+    want, wl, rows = oc.forward(segments, q, k, v, scale)
+    bo, bl = oc.forward_bounds(segments, q, k, v, scale)
+    within(out, want, bo, rows)
+    within(lse, wl, bl, rows)
+    assert (out[~rows] == 77).all() and (lse[~rows] == 77).all()
+    first = out.clone()
+    plan.run(q, k, v, scale, out, lse)
+    assert torch.equal(first, out)
+    return plan
+
+
+def check_backward(segments, hq, hkv, d, dtype, ctas=0, **kw):
+    q, k, v, dout = inputs(segments, hq, hkv, d, dtype, **kw)
+    plan = CrossPlan(segments, hq, hkv, d, dtype, DEV, training=True, ctas=ctas)
+    scale = 1 / math.sqrt(d)
+    want, wl, rows = oc.forward(segments, q, k, v, scale)
+    out, lse = want.to(dtype), wl.float()
+    dq = torch.full_like(out, 77.0)
+    dkv = torch.full((k.shape[0], 3 * hkv, d), 77.0, dtype=dtype, device=DEV)
+    dk, dv = dkv[:, :hkv], dkv[:, 2 * hkv:]
+    plan.bwd_workspace.fill_(255)
+    plan.run_bwd(q, k, v, out, dout, lse, scale, dq, dk, dv)
+    pa.padoc_check_device_errors()
+    # NaN of unnamed rows does not reach the checker either: it reads the segments' rows alone
+    gq, gk, gv = oc.backward(segments, q, k, v, dout, scale)
+    bq, bk, bv = oc.backward_bounds(segments, q, k, v, out, dout, scale)
+    within(dq, gq, bq, rows)
+    within(dk, gk, bk)
+    within(dv, gv, bv)
+    assert (dq[~rows] == 77).all() and (dkv[:, hkv:2 * hkv] == 77).all()
+    first = [t.clone() for t in (dq, dk, dv)]
+    plan.run_bwd(q, k, v, out, dout, lse, scale, dq, dk, dv)
+    assert all(torch.equal(a, b) for a, b in zip(first, (dq, dk, dv)))
+    return plan
+
+
+HEADS = [(16, 2, 128), (16, 16, 64), (2, 2, 128), (7, 1, 64), (14, 2, 128), (64, 1, 128), (12, 4, 64), (33, 1, 64)]
+EDGES = [
+    [(0, 1, 0, 1)],
+    [(0, 1, 3, 129)],
+    [(2, 65, 5, 127)],
+    [(0, 16, 0, 128), (16, 17, 128, 128)],
+    [(0, 33, 1, 64), (33, 31, 66, 1), (70, 64, 70, 191)],
+    [(0, 5, 0, 0), (5, 3, 0, 200), (9, 0, 0, 50), (9, 40, 3, 0)],           # rows without keys, a segment without rows
+    [(0, 40, 10, 300), (40, 9, 20, 30), (49, 1, 309, 1), (50, 70, 10, 300), (120, 7, 250, 200)],   # shared key ranges
+    [(0, 130, 0, 1), (130, 1, 0, 513)],
+]
+
+
+@pytest.mark.parametrize("segments", EDGES)
+@pytest.mark.parametrize("hq,hkv,d", HEADS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_forward_edges(dtype, hq, hkv, d, segments):
+    check_forward(segments, hq, hkv, d, dtype)
+
+
+@pytest.mark.parametrize("segments", EDGES)
+@pytest.mark.parametrize("hq,hkv,d", HEADS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_backward_edges(dtype, hq, hkv, d, segments):
+    check_backward(segments, hq, hkv, d, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("ctas", [1, 7, 0])
+@pytest.mark.parametrize("keys", [2, 129, 1000, 4097])
+def test_few_rows_over_long_keys(dtype, ctas, keys):
+    # split over the chip and joined, or whole
+    segments = [(0, 3, 1, keys), (3, 1, 0, keys + 1)]
+    check_forward(segments, 16, 2, 128, dtype, ctas=ctas)
+    check_backward(segments, 4, 2, 64, dtype, ctas=ctas)
+
+
+def test_document_of_many_states():
+    check_forward([(0, 24, 7, 50_003)], 16, 2, 128, BF16)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_that_lie_apart(dtype):
+    segments = [(1, 70, 2, 140), (71, 5, 30, 40)]
+    check_forward(segments, 8, 2, 128, dtype, wide=4)
+    check_backward(segments, 8, 2, 128, dtype, wide=4)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(16, 2, 128), (16, 16, 64), (4, 4, 128)])
+def test_many_rows(hq, hkv, d):
+    # more units than SMs, several waves, every kind of launch
+    segments = [(0, 1500, 0, 400), (1500, 1111, 400, 700), (2611, 300, 350, 100)]
+    check_forward(segments, hq, hkv, d, BF16, poison=False)
+    check_backward(segments, hq, hkv, d, BF16, poison=False)
+
+
+def test_many_rows_f32():
+    segments = [(0, 700, 0, 400), (700, 311, 400, 300)]
+    check_forward(segments, 4, 1, 64, F32)
+    check_backward(segments, 4, 1, 64, F32)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_scores_of_far_apart_sizes(dtype):
+    # keys that grow by steps: the running maximum moves at every tile, and early weights vanish
+    segments, hq, hkv, d = [(0, 20, 0, 700)], 8, 2, 128
+    q, k, v, dout = inputs(segments, hq, hkv, d, dtype, rows=20, keys=700)
+    k *= torch.arange(700, device=DEV)[:, None, None] // 100 * 2 + 0.25
+    plan = CrossPlan(segments, hq, hkv, d, dtype, DEV, training=True, ctas=1)
+    out, lse = torch.empty_like(q.contiguous()), torch.empty((20, hq), device=DEV)
+    plan.run(q, k, v, 0.5, out, lse)
+    want, wl, _ = oc.forward(segments, q, k, v, 0.5)
+    bo, bl = oc.forward_bounds(segments, q, k, v, 0.5)
+    within(out, want, bo)
+    within(lse, wl, bl)
+    dq, dk, dv = torch.empty_like(out), torch.empty_like(k.contiguous()), torch.empty_like(k.contiguous())
+    plan.run_bwd(q, k, v, want.to(dtype), dout, wl.float(), 0.5, dq, dk, dv)
+    for got, ref, bound in zip((dq, dk, dv), oc.backward(segments, q, k, v, dout, 0.5),
+                               oc.backward_bounds(segments, q, k, v, want.to(dtype), dout, 0.5)):
+        within(got, ref, bound)
+
+
+def test_segments_without_keys_alone():
+    segments = [(0, 4, 0, 0), (6, 2, 9, 0)]
+    q, k, v, dout = inputs(segments, 16, 2, 128, BF16, keys=5)
+    plan = CrossPlan(segments, 16, 2, 128, BF16, DEV, training=True)
+    out, lse = torch.full_like(dout, 3.0), torch.full((q.shape[0], 16), 3.0, device=DEV)
+    plan.run(q, k, v, 0.1, out, lse)
+    assert (out[:4] == 0).all() and (out[6:8] == 0).all() and (out[4:6] == 3).all() and (out[8:] == 3).all()
+    assert (lse[:4] == -math.inf).all() and (lse[4:6] == 3).all()
+    dq, dk, dv = torch.full_like(dout, 3.0), torch.full_like(k.contiguous(), 3.0), torch.full_like(k.contiguous(), 3.0)
+    plan.run_bwd(q, k, v, out, dout, lse, 0.1, dq, dk, dv)
+    assert (dq[:4] == 0).all() and (dq[4:6] == 3).all() and (dk == 0).all() and (dv == 0).all()
+
+
+def test_key_rows_behind_the_last_segment_have_zero_gradients():
+    segments = [(0, 9, 3, 40)]
+    q, k, v, dout = inputs(segments, 4, 2, 64, BF16, keys=400)
+    plan = CrossPlan(segments, 4, 2, 64, BF16, DEV, training=True)
+    out, lse = torch.zeros_like(dout), torch.zeros((q.shape[0], 4), device=DEV)
+    plan.run(q, k, v, 0.125, out, lse)
+    dq, dk, dv = (torch.full_like(t, 9.0) for t in (out, k.contiguous(), k.contiguous()))
+    plan.run_bwd(q, k, v, out, dout, lse, 0.125, dq, dk, dv)
+    for t in (dk, dv):
+        assert (t[:3] == 0).all() and (t[43:] == 0).all() and (t[3:43] != 0).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_nan_and_infinity_stay_with_the_rows_that_see_them(dtype):
+    segments = [(0, 20, 0, 150), (20, 20, 150, 150)]
+    q, k, v, dout = inputs(segments, 8, 2, 64, dtype, rows=40, keys=300)
+    v[149] = math.inf
+    k[140, 1] = NAN
+    plan = CrossPlan(segments, 8, 2, 64, dtype, DEV, training=True)
+    out, lse = torch.empty_like(dout), torch.empty((40, 8), device=DEV)
+    plan.run(q, k, v, 0.125, out, lse)
+    assert not torch.isfinite(out[:20]).any() and torch.isnan(out[:20, 4:]).all() and torch.isnan(lse[:20, 4:]).all()
+    assert torch.isfinite(lse[:20, :4]).all()
+    want, wl, _ = oc.forward(segments[1:], q, k, v, 0.125)
+    bo, bl = oc.forward_bounds(segments[1:], q, k, v, 0.125)
+    within(out[20:], want[20:], bo[20:])
+    within(lse[20:], wl[20:], bl[20:])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gradients_against_differences(dtype):
+    # the forward's own change along a direction, in 64 bits' differences of the checker at the same inputs
+    segments, hq, hkv, d = [(0, 30, 0, 90), (30, 10, 50, 60)], 4, 2, 64
+    q, k, v, dout = inputs(segments, hq, hkv, d, dtype, rows=40, keys=110)
+    plan = CrossPlan(segments, hq, hkv, d, dtype, DEV, training=True)
+    out, lse = torch.empty_like(dout), torch.empty((40, hq), device=DEV)
+    plan.run(q, k, v, 0.125, out, lse)
+    dq, dk, dv = torch.empty_like(out), torch.empty_like(k.contiguous()), torch.empty_like(k.contiguous())
+    plan.run_bwd(q, k, v, out, dout, lse, 0.125, dq, dk, dv)
+    bounds = oc.backward_bounds(segments, q, k, v, out, dout, 0.125)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    for n, (got, bound) in enumerate(zip((dq, dk, dv), bounds)):
+        args = [t.double() for t in (q, k, v)]
+        way = torch.randn(args[n].shape, generator=g, device=DEV, dtype=torch.float64)
+        ends = []
+        for h in (1e-5, -1e-5):
+            at = list(args)
+            at[n] = args[n] + h * way
+            ends.append((oc.forward(segments, *at, 0.125)[0] * dout.double()).sum().item())
+        slope = (ends[0] - ends[1]) / 2e-5
+        assert abs((got.double() * way).sum().item() - slope) <= (bound * way.abs()).sum().item() + 1e-6 * abs(slope) + 1e-6
+
+
+def test_python_refusals():
+    segments = [(0, 4, 0, 9)]
+    plan = CrossPlan(segments, 4, 2, 64, BF16, DEV)
+    q, k, v, _ = inputs(segments, 4, 2, 64, BF16)
+    out, lse = torch.empty_like(q.contiguous()), torch.empty(q.shape[:2], device=DEV)
+    run = lambda **o: plan.run(**{**dict(q=q, k=k, v=v, scale=0.1, out=out, lse=lse), **o})
+    run()
+    with pytest.raises(ValueError):
+        plan.run_bwd(q, k, v, out, out, lse, 0.1, out, k, v)
+    for bad in (dict(q=q.cpu()), dict(q=q[:, :3]), dict(k=k[:, :1]), dict(v=v[:5]), dict(out=out[:3]), dict(out=out.float()),
+                dict(lse=lse.double()), dict(lse=lse[:, :3]), dict(q=q.transpose(0, 1)), dict(q=q[..., :32])):
+        with pytest.raises((ValueError, TypeError, pa.PadocError)):
+            run(**bad)
+    with pytest.raises(pa.PadocError):     # fewer rows than the plan names
+        plan.run(q[:3], k, v, 0.1, out[:3], lse[:3])
+    with pytest.raises(pa.PadocError):
+        run(k=k[:8], v=v[:8])
+    with pytest.raises(pa.PadocError):     # an output over an input
+        run(out=q)
+    with pytest.raises(TypeError):
+        run(q=q.half(), k=k.half(), v=v.half())
