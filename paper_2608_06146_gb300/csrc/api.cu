@@ -47,17 +47,19 @@ int *padoc_device_error_word()
 namespace {
 
 // The last few 2-D maps this thread encoded, by their arguments: a decoding loop encodes the same
-// pool's maps every step, and an encoding is a pure function of its arguments. A backward takes ten.
-constexpr int kTmaps = 16;
+// pool's maps every step, and an encoding is a pure function of its arguments. A backward takes ten, a cross attention and its
+// gradients as many.
+constexpr int kTmaps = 32;
 struct TmapKey {
     int dtype;
     const void *base;
     uint64_t cols, rows, stride;
     uint32_t box_cols, box_rows;
+    uint32_t heads, box_heads;   // (rows of heads; 0 else)
     bool operator==(const TmapKey &o) const
     {
         return dtype == o.dtype && base == o.base && cols == o.cols && rows == o.rows && stride == o.stride &&
-               box_cols == o.box_cols && box_rows == o.box_rows;
+               box_cols == o.box_cols && box_rows == o.box_rows && heads == o.heads && box_heads == o.box_heads;
     }
 };
 struct TmapCache {
@@ -138,6 +140,26 @@ bool padoc_make_tmap_u8(CUtensorMap *map, const void *base, uint64_t cols, uint6
     cuuint32_t box[2] = {box_cols, box_rows};
     cuuint32_t estr[2] = {1, 1};
     CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return false;
+    tmap_remember(key, *map);
+    return true;
+}
+
+bool padoc_make_tmap_bf16_heads(CUtensorMap *map, const void *base, uint32_t head_dim, uint32_t heads, uint64_t rows,
+                                uint64_t row_stride_bytes, uint32_t box_heads, uint32_t box_rows)
+{
+    const TmapKey key{2, base, head_dim, rows, row_stride_bytes, 64, box_rows, heads, box_heads};
+    if (tmap_cached(key, map)) return true;
+    PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+    if (!fn) return false;
+    if ((((uintptr_t)base) & 15) || (row_stride_bytes & 15) || rows == 0) return false;
+    cuuint64_t dims[3] = {head_dim, heads, rows};
+    cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, row_stride_bytes};
+    cuuint32_t box[3] = {64, box_heads, box_rows};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return false;

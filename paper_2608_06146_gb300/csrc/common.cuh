@@ -232,6 +232,22 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
         : "memory");
 }
 
+// 3-D tiles, as the two above.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+
 // 2-D tile from shared to global memory (parts past the tensor's end are not written). The issuing
 // thread's copies form bulk groups: tma_store_commit closes one, tma_store_wait_read<N> waits until at
 // most the N latest still read shared memory.
@@ -530,6 +546,10 @@ bool padoc_make_tmap_bf16(CUtensorMap *map, const void *base, uint64_t cols, uin
 // box_rows x box_cols bytes (box_cols <= 128), 128-byte swizzle.
 bool padoc_make_tmap_u8(CUtensorMap *map, const void *base, uint64_t cols, uint64_t rows, uint64_t row_stride_bytes,
                         uint32_t box_cols, uint32_t box_rows);
+// 3-D bf16 tensor map of rows of heads ([rows][heads][head_dim], a row's heads adjacent, rows row_stride_bytes apart),
+// box of box_rows x box_heads x 64 dims, 128-byte swizzle.
+bool padoc_make_tmap_bf16_heads(CUtensorMap *map, const void *base, uint32_t head_dim, uint32_t heads, uint64_t rows,
+                                uint64_t row_stride_bytes, uint32_t box_heads, uint32_t box_rows);
 // 4-D bf16 tensor map (dims[0] innermost, strides of dims 1..3 in bytes), 128-byte swizzle.
 bool padoc_make_tmap_bf16_4d(CUtensorMap *map, const void *base, const uint64_t dims[4], const uint64_t strides_bytes[3],
                              const uint32_t box[4]);

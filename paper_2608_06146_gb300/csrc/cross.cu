@@ -568,7 +568,7 @@ extern "C" padoc_status padoc_cross_attn(const padoc_cross_plan *info, const int
     cudaStream_t cs = (cudaStream_t)stream;
     if (a.num_units) {
         if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_fwd_simt<float, 64>(a, cs) : run_fwd_simt<float, 128>(a, cs);
-        else st = c.head_dim == 64 ? run_fwd_simt<__nv_bfloat16, 64>(a, cs) : run_fwd_simt<__nv_bfloat16, 128>(a, cs);
+        else st = padoc_cross_launch_tc(a, c.head_dim, info->pair != 0, cs);
         if (st != PADOC_OK) return st;
     }
     return a.num_merges ? padoc_cross_launch_merge(a, c.dtype, c.head_dim, false, a.num_units > 0, cs) : PADOC_OK;

@@ -39,3 +39,5 @@ __device__ __forceinline__ bool cross_row(const padoc_cross_args &a, int tok, in
 // Rows joined from parts, a warp per row: the forward's outputs and log-sum-exps (kDq 0), or dq (1).
 padoc_status padoc_cross_launch_merge(const padoc_cross_args &a, padoc_dtype dtype, int head_dim, bool dq, bool pdl,
                                       cudaStream_t stream);
+// The forward's units on the tensor cores (cross_tc.cu).
+padoc_status padoc_cross_launch_tc(const padoc_cross_args &args, int head_dim, bool pair, cudaStream_t stream);

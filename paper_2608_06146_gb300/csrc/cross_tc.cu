@@ -1,0 +1,609 @@
+// cross_tc.cu -- cross attention forward on the 5th-generation tensor cores: S = Q K^T, online softmax, O = P V.
+//
+// A unit is 256 packed rows of one KV head (two 128-row tiles of (token, head of the group) rows; 512 for a CTA
+// pair) over a segment's keys or a part of them. All rows of a unit see the same keys, so the only mask is the end of
+// the last 128-key tile: its scores past the end become -inf, and its V rows there zeros, because what lies behind a
+// segment's keys may be anything (0 x NaN would reach the output).
+//
+// Warp roles (384 threads): warps 0-3 / 4-7 softmax and epilogue of tile 0 / 1 (TMEM lane = row: row max and sum need
+// no shuffles); warp 8 TMA producer, which also announces the units; warps 9, 10 the MMA issuers of tile 0 / 1 (a
+// converged warp, one elected lane); warp 9 also allocates tensor memory. Tensor memory: tile i keeps S in two halves
+// of 64 keys at columns 128 i + 64 h, with P as packed bf16 over the first 32 columns of its half, and O at 256 + 128 i.
+// For a tile and half the MMAs run S(t) -> P(t) -> P V(t) -> S(t + 1). O is rescaled only when a row's maximum has
+// grown by more than 2^8 since the last time, which keeps P <= 256.
+//
+// The grid has one CTA (pair) per unit, most keys first; a running one takes over units not yet launched (cluster
+// launch control), and the next unit's queries and first scores come under the last one's output. A unit of at most
+// 128 rows is run by tile 0's warps alone.
+// Every wait is bounded; a wait that runs out records an error, all roles leave their loops, the issuers wait for
+// their MMAs, the producer for its copies, and tensor memory is released.
+#include <math.h>
+
+#include "cross.cuh"
+#include "tc.cuh"
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr uint32_t kTmemCols = 512;
+constexpr int kPanel = 128 * 128;      // [128 rows][64 bf16]
+constexpr int kBlk = PADOC_CROSS_BLOCK;
+constexpr int kKT = PADOC_CROSS_KEY_TILE;
+
+template <int D, int CG>
+struct Cfg {
+    static constexpr int kPanels = D / 64;
+    static constexpr int kTile = kPanels * kPanel;
+    static constexpr int kStages = D == 64 ? 4 : CG == 2 ? 3 : 2;
+    static constexpr int kHalf = kTile / CG;         // a CTA's part of a K or V tile
+    static constexpr int kKPanel = kPanel / 2 / CG;  // 64 dims of its keys of one half
+    static constexpr int kOutBytes = 8 * 4096;       // [32 rows][64 dims] a softmax warp
+    enum {
+        B_QFULL = 0,                    // [tile]
+        B_QEMPTY = 2,                   // [tile]
+        B_SFULL = 4,                    // [tile][half]
+        B_PFULL = 8,                    // [tile][half], one arrival per warp of the tile (both CTAs')
+        B_PVDONE = 12,                  // [tile][half]
+        B_OFREE = 16,                   // [tile], one arrival per warp of the tile (both CTAs')
+        B_UFULL = 18,                   // [slot]: the announced unit
+        B_UEMPTY = 20,                  // [slot], one arrival per reading warp (both CTAs')
+        B_NEXT = 22,                    // the launch control's answer
+        B_FINAL = 23,                   // [tile]
+        B_VTAIL = 25,                   // this CTA's part of a unit's last V tile, where keys end inside it
+        B_KFULL = 26,                   // [stage]
+        B_KEMPTY = B_KFULL + kStages,   // [stage], one arrival per tile
+        B_VFULL = B_KEMPTY + kStages,   // [stage]
+        B_VEMPTY = B_VFULL + kStages,   // [stage], one arrival per tile
+        B_COUNT = B_VEMPTY + kStages
+    };
+    static constexpr int kReaders = CG == 2 ? 19 : 10;   // softmax warps, MMA warps, the second CTA's producer
+    static constexpr size_t kSmemBytes = 1024 + 2 * (size_t)kTile + 2 * (size_t)kStages * kHalf + kOutBytes + 96 + B_COUNT * 8 + 16;
+    static_assert(kSmemBytes <= 227 * 1024 && (CG == 1 || D == 128), "");
+};
+
+// A unit as the producer announces it; tiles < 0 ends the CTA.
+struct Unit {
+    int32_t tok, ntok, k0, nk;
+    int32_t g, slot, tiles, two;   // tiles: 128-key tiles; two: whether the second tile has rows
+};
+
+template <bool kCluster>
+__device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, int *err, int site, volatile int *abort_flag)
+{
+    if (kCluster ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
+    if (kCluster ? mbar_wait_bounded_cluster(bar, parity, err, site) : mbar_wait_bounded(bar, parity, err, site)) return true;
+    *abort_flag = 1;
+    return false;
+}
+
+template <int D, int CG>
+__global__ void __launch_bounds__(kThreads, 1)
+cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
+{
+    using C = Cfg<D, CG>;
+    constexpr int kStages = C::kStages, kTile = C::kTile;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t *sq = smem;                       // [2 tiles][panel][128 rows]
+    uint8_t *sk = sq + 2 * kTile;             // [kStages][key half][panel] (CG 2: this CTA's half of the keys)
+    uint8_t *sv = sk + kStages * C::kHalf;    // [kStages][panel] (CG 2: this CTA's 64 dims)
+    uint8_t *so = sv + kStages * C::kHalf;    // [8 warps][32][128 bytes]
+    Unit *units = (Unit *)(so + C::kOutBytes);   // [2]
+    uint8_t *answer = (uint8_t *)(units + 2); // 16 bytes
+    uint64_t *bars = (uint64_t *)(so + C::kOutBytes + 96);
+    uint32_t *tmem_slot = (uint32_t *)(bars + C::B_COUNT);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (a value the compiler knows to be warp-uniform)
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const int tile_tokens = 2 * a.block_tokens;
+    pdl_launch_dependents();   // the joining of split rows, where there is one, may take the SMs that run out of work
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    // a barrier of the pair's first CTA, which issues the MMAs and announces the units
+    auto lead_bar = [&](int i) { return CG == 2 ? cluster_map(bar(i), 0) : bar(i); };
+    auto arrive_lead = [&](int i) {
+        if (CG == 2) mbar_arrive_cluster<false>(lead_bar(i));
+        else mbar_arrive(bar(i));
+    };
+
+    if (tid == 0) {
+        for (int i = 0; i < C::B_COUNT; ++i) {
+            int n = 1;
+            if (i >= C::B_PFULL && i < C::B_PFULL + 4) n = 4 * CG;
+            if (i == C::B_OFREE || i == C::B_OFREE + 1) n = 4 * CG;
+            if (i >= C::B_KEMPTY && i < C::B_KEMPTY + kStages) n = 2;
+            if (i >= C::B_VEMPTY && i < C::B_VEMPTY + kStages) n = 2;
+            if (i == C::B_UEMPTY || i == C::B_UEMPTY + 1) n = C::kReaders;
+            mbar_init(bar(i), n);
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    // rows of a block that hold no (token, head): no copy writes them
+    const int used = a.block_tokens * a.group;
+    if (used < kBlk) {
+        for (int i = tid; i < 4 * C::kPanels * (kBlk - used) * 8; i += kThreads) {
+            const int r = i / 8 % (kBlk - used) + used, b = i / 8 / (kBlk - used);
+            *reinterpret_cast<uint4 *>(sq + b * kBlk * 128 + r * 128 + i % 8 * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+    }
+    if (warp == 9) {
+        tmem_alloc<CG>(smem_u32(tmem_slot), kTmemCols);
+        tmem_relinquish<CG>();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync();   // no arrival or copy for the other CTA before its barriers are set up
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    // the n-th unit, as every lane of a reading warp sees it
+    auto read_unit = [&](int n, Unit &u, int site) {
+        const bool r = wait_or_abort<CG == 2>(bar(C::B_UFULL + (n & 1)), (n >> 1) & 1, a.err, site, abort_flag);
+        if (!__all_sync(0xffffffffu, r)) return false;
+        const Unit v = units[n & 1];
+        u.tok = __shfl_sync(0xffffffffu, v.tok, 0);
+        u.ntok = __shfl_sync(0xffffffffu, v.ntok, 0);
+        u.nk = __shfl_sync(0xffffffffu, v.nk, 0);
+        u.g = __shfl_sync(0xffffffffu, v.g, 0);
+        u.slot = __shfl_sync(0xffffffffu, v.slot, 0);
+        u.tiles = __shfl_sync(0xffffffffu, v.tiles, 0);
+        u.two = __shfl_sync(0xffffffffu, v.two, 0);
+        __syncwarp();   // (every lane's read has returned before the arrival lets the slot be written again)
+        if (lane == 0) arrive_lead(C::B_UEMPTY + (n & 1));
+        return true;
+    };
+    // the next unit that tile i takes part in; ring: K and V tiles so far, of all units
+    auto next_unit = [&](int i, int &n, Unit &u, int &ring, int site) {
+        for (;;) {
+            if (!read_unit(n++, u, site)) return false;
+            if (u.tiles < 0 || i == 0 || u.two) return true;
+            ring += u.tiles;
+        }
+    };
+
+    if (warp >= 8) {
+        if (warp == 8 && lane == 0) {
+            // ------------------------------------------------------------ TMA producer
+            tma_prefetch_desc(&qmap);
+            tma_prefetch_desc(&kmap);
+            tma_prefetch_desc(&vmap);
+            auto wait = [&](int b, uint32_t parity, int site) {
+                return wait_or_abort<false>(bar(b), parity, a.err, site, abort_flag);
+            };
+            // the first CTA's barrier counts both CTAs' bytes
+            auto expect = [&](int b, uint32_t bytes) {
+                if (rank == 0) mbar_arrive_expect_tx(bar(b), CG * bytes);
+            };
+            auto box = [&](uint8_t *dst, const CUtensorMap *map, int x, int y, int b) {
+                if (CG == 2) tma_load_2d_pair(smem_u32(dst), map, x, y, lead_bar(b));
+                else tma_load_2d(smem_u32(dst), map, x, y, bar(b));
+            };
+            int x = (int)blockIdx.x / CG;
+            int tk = 0, nq[2] = {0, 0}, tails = 0;   // K and V tiles, queries per tile, V tails issued so far
+            bool ok = true, more = true, asked = false;
+            // asked with the unit's last tile, a few tiles ahead of the MMAs: early enough for the answer,
+            // and late enough that no CTA holds a second unit while others run out of work
+            auto ask = [&]() {
+                if (rank != 0) return;
+                mbar_arrive_expect_tx(bar(C::B_NEXT), 16);
+                launch_control_ask(smem_u32(answer), bar(C::B_NEXT));
+                asked = true;
+            };
+            auto load_q = [&](int i, const Unit &u) {
+                if (nq[i] && !wait(C::B_QEMPTY + i, (nq[i] - 1) & 1, 120)) return false;
+                const int t0 = u.tok + (2 * (int)rank + i) * tile_tokens;
+                expect(C::B_QFULL + i, 2 * C::kPanels * used * 128);
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int p = 0; p < C::kPanels; ++p) {
+                        const uint32_t dst = smem_u32(sq + i * kTile + p * kPanel + b * kBlk * 128);
+                        const int y = u.g * a.group, z = t0 + b * a.block_tokens;
+                        if (CG == 2) tma_load_3d_pair(dst, &qmap, 64 * p, y, z, lead_bar(C::B_QFULL + i));
+                        else tma_load_3d(dst, &qmap, 64 * p, y, z, bar(C::B_QFULL + i));
+                    }
+                ++nq[i];
+                return true;
+            };
+            int n = 0, asks = 0;   // units announced, questions answered
+            for (;; ++n) {
+                Unit u = {0, 0, 0, 0, 0, 0, -1, 0};
+                if (rank == 0) {
+                    if (n >= 2 && !wait(C::B_UEMPTY + (n & 1), ((n >> 1) - 1) & 1, 124)) break;
+                    if (more) {
+                        const padoc_cross_unit w = a.units[x / a.hkv];
+                        u.tok = w.tok;
+                        u.ntok = w.ntok;
+                        u.k0 = w.k0;
+                        u.nk = w.nk;
+                        u.g = x % a.hkv;
+                        u.slot = w.slot;
+                        u.tiles = (w.nk + kKT - 1) / kKT;
+                        u.two = CG == 2 || w.ntok > tile_tokens;
+                    }
+                    units[n & 1] = u;
+                    mbar_arrive(bar(C::B_UFULL + (n & 1)));
+                    if (CG == 2) {
+                        const uint32_t to = cluster_map(smem_u32(&units[n & 1]), 1);
+                        st_cluster_v4(to, make_int4(u.tok, u.ntok, u.k0, u.nk));
+                        st_cluster_v4(to + 16, make_int4(u.g, u.slot, u.tiles, u.two));
+                        mbar_arrive_cluster<true>(cluster_map(bar(C::B_UFULL + (n & 1)), 1));
+                    }
+                } else {
+                    if (!wait_or_abort<true>(bar(C::B_UFULL + (n & 1)), (n >> 1) & 1, a.err, 125, abort_flag)) break;
+                    u = units[n & 1];
+                }
+                if (u.tiles < 0) break;
+                for (int j = 0; j < u.tiles; ++j, ++tk) {
+                    if (j + 1 == u.tiles) ask();
+                    // (the first K tile between the two tiles' queries: S_0 needs it first)
+                    if (j == 0 && !(ok = load_q(0, u))) break;
+                    const int s = tk % kStages, row = u.k0 + j * kKT;
+                    if (tk >= kStages && !(ok = wait(C::B_KEMPTY + s, (tk / kStages - 1) & 1, 121))) break;
+                    uint8_t *kb = sk + s * C::kHalf;
+                    expect(C::B_KFULL + s, C::kHalf);
+                    if (!u.two) mbar_arrive(bar(C::B_KEMPTY + s));   // (for the second tile, which has no part)
+#pragma unroll
+                    for (int b = 0; b < 2 * C::kPanels; ++b)   // [key half][panel]
+                        box(kb + b * C::kKPanel, &kmap, u.g * D + 64 * (b % C::kPanels),
+                            row + 64 * (b / C::kPanels) + 64 / CG * (int)rank, C::B_KFULL + s);
+                    if (j == 0 && u.two && !(ok = load_q(1, u))) { ++tk; break; }
+                    if (tk >= kStages && !(ok = wait(C::B_VEMPTY + s, (tk / kStages - 1) & 1, 123))) { ++tk; break; }
+                    uint8_t *vb = sv + s * C::kHalf;
+                    const bool tail = u.nk - j * kKT < kKT;
+                    if (tail) {   // completes on this CTA's own barrier: the softmax warps zero its rows past the end
+                        if (rank == 0) mbar_arrive(bar(C::B_VFULL + s));
+                        mbar_arrive_expect_tx(bar(C::B_VTAIL), C::kHalf);
+                        ++tails;
+                    } else {
+                        expect(C::B_VFULL + s, C::kHalf);
+                    }
+                    if (!u.two) mbar_arrive(bar(C::B_VEMPTY + s));
+#pragma unroll
+                    for (int p = 0; p < C::kPanels / CG; ++p) {
+                        const int col = u.g * D + 64 * (CG == 2 ? (int)rank : p);
+                        if (tail) tma_load_2d(smem_u32(vb + p * kPanel), &vmap, col, row, bar(C::B_VTAIL));
+                        else box(vb + p * kPanel, &vmap, col, row, C::B_VFULL + s);
+                    }
+                }
+                if (!ok) break;
+                if (rank != 0) {
+                    // Only now may the first CTA write this slot of ours again (it does two units on): with
+                    // cluster scope, so that its stores come after the reads above.
+                    mbar_arrive_cluster<true>(lead_bar(C::B_UEMPTY + (n & 1)));
+                } else {
+                    if (!wait(C::B_NEXT, asks & 1, 126)) break;
+                    ++asks;
+                    asked = false;
+                    int y;
+                    more = launch_control_answer(smem_u32(answer), x, y);
+                    x /= CG;
+                    fence_proxy_async_smem();   // the answer is read before the next one may be written
+                }
+            }
+            // copies still in flight must land before the CTA's shared memory is released (CG 2: the first
+            // CTA sees both CTAs' land, and both stay until the cluster barrier below; after a wait that
+            // ran out the other CTA may never issue its part, so the copies get a millisecond to land)
+            if (asked) mbar_wait_bounded(bar(C::B_NEXT), asks & 1, a.err, 127);
+            if (CG == 2 && *abort_flag) {
+                const uint64_t t0 = padoc_globaltimer();
+                while (padoc_globaltimer() - t0 < 1000000ull) {
+                }
+            } else {
+                if (tails) mbar_wait_bounded(bar(C::B_VTAIL), (tails - 1) & 1, a.err, 127);
+                if (rank == 0) {
+                    for (int i = 0; i < 2; ++i)
+                        if (nq[i]) mbar_wait_bounded(bar(C::B_QFULL + i), (nq[i] - 1) & 1, a.err, 127);
+                    for (int t = max(tk - kStages, 0); t < tk; ++t)
+                        mbar_wait_bounded(bar(C::B_KFULL + t % kStages), (t / kStages) & 1, a.err, 128);
+                    // (after a wait that ran out between a tile's K and its V the last phase was never opened)
+                    for (int t = max(tk - kStages, 0); t < tk && !*abort_flag; ++t)
+                        mbar_wait_bounded(bar(C::B_VFULL + t % kStages), (t / kStages) & 1, a.err, 129);
+                }
+                if (*abort_flag) {
+                    const uint64_t t0 = padoc_globaltimer();
+                    while (padoc_globaltimer() - t0 < 1000000ull) {
+                    }
+                }
+            }
+        } else if (warp >= 9 && warp < 11 && rank == 0) {
+            // ------------------------------------------------------------ MMA issuers (a whole warp per tile)
+            const int i = warp - 9;
+            constexpr uint32_t idS = umma_idesc_bf16(128 * CG, 64, false);
+            constexpr uint32_t idPV = umma_idesc_bf16(128 * CG, D, true);
+            const uint64_t dq = umma_desc_sw128(smem_u32(sq + i * kTile), 16, 1024);
+            const uint64_t dk = umma_desc_sw128(smem_u32(sk), 16, 1024), dv = umma_desc_sw128(smem_u32(sv), kPanel, 1024);
+            const uint32_t tS = tmem + 128 * i, tO = tmem + 256 + 128 * i;
+            auto wait = [&](int b, uint32_t parity, int site) {
+                return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
+            };
+            auto commit = [&](int b) {
+                if (CG == 2) umma_commit_pair_warp(bar(b));
+                else umma_commit_warp(bar(b));
+            };
+            // S_i over half h of the tile in the given stage; the last tile of a unit frees Q_i
+            auto issue_s = [&](int stage, int h, bool last) {
+                const uint64_t b = dk + ((stage * C::kHalf + h * C::kPanels * C::kKPanel) >> 4);
+                if constexpr (D == 128) umma_bf16_ss_k128_warp<CG, kPanel, C::kKPanel>(tS + 64 * h, dq, b, idS);
+                else umma_bf16_ss_k64_warp(tS + 64 * h, dq, b, idS);
+                commit(C::B_SFULL + 2 * i + h);
+                if (h == 1) {
+                    if (last) commit(C::B_QEMPTY + i);
+                    commit(C::B_KEMPTY + stage);
+                }
+            };
+            int n = 0, ring = 0, t = 0;   // units read; K and V tiles of all units, and of this tile's
+            Unit u;
+            bool ok = next_unit(i, n, u, ring, 130);
+            auto first_s = [&](int w) {
+                const int s = ring % kStages;
+                if (!wait(C::B_KFULL + s, (ring / kStages) & 1, 131) || !wait(C::B_QFULL + i, w & 1, 132)) return false;
+                tc_fence_after();
+                issue_s(s, 0, u.tiles == 1);
+                issue_s(s, 1, u.tiles == 1);
+                return true;
+            };
+            // O_i += P_i V over half h of the tile
+            auto issue_pv = [&](int s, int h, bool first, bool tail) {
+                if (!wait(C::B_PFULL + 2 * i + h, t & 1, 135)) return false;
+                if (CG == 2 && tail) asm volatile("fence.acq_rel.cluster;" ::: "memory");   // (V's zeros of both CTAs)
+                tc_fence_after();
+                umma_bf16_ts_k64_mn_warp<CG>(tO, tS + 64 * h, dv + ((s * C::kHalf + h * 8192) >> 4), idPV, !first);
+                commit(C::B_PVDONE + 2 * i + h);
+                if (h == 1) commit(C::B_VEMPTY + s);
+                return true;
+            };
+            if (ok && u.tiles > 0) ok = first_s(0);
+            for (int w = 0; ok && u.tiles > 0; ++w) {
+                if (w > 0) ok = wait(C::B_OFREE + i, (w - 1) & 1, 134);
+                const int ne = u.tiles;
+                const bool cut = u.nk % kKT != 0;
+                for (int j = 0; ok && j + 1 < ne; ++j, ++t, ++ring) {
+                    const int s = ring % kStages, sn = (ring + 1) % kStages;
+                    // (while the tensor cores still run the S of this tile)
+                    ok = wait(C::B_VFULL + s, (ring / kStages) & 1, 133) && wait(C::B_KFULL + sn, ((ring + 1) / kStages) & 1, 136);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if (ok && (ok = issue_pv(s, h, j == 0 && h == 0, false))) issue_s(sn, h, j + 2 == ne);
+                }
+                if (!ok) break;
+                // the unit's last tile, then the first S of the next unit, under this one's epilogue
+                const int s = ring % kStages;
+                ok = wait(C::B_VFULL + s, (ring / kStages) & 1, 133) && issue_pv(s, 0, ne == 1, cut) && issue_pv(s, 1, false, cut);
+                if (!ok) break;
+                ++t;
+                ++ring;
+                ok = next_unit(i, n, u, ring, 130);
+                if (!ok || u.tiles < 0) break;
+                ok = first_s(w + 1);
+            }
+            // every MMA issued above must complete before TMEM is released
+            if (CG == 2) umma_commit_pair_warp(bar(C::B_FINAL + i));
+            else umma_commit_warp(bar(C::B_FINAL + i));
+            mbar_wait_bounded(bar(C::B_FINAL + i), 0, a.err, 138);
+        }
+    } else {
+        // ---------------------------------------------------------------- softmax + epilogue
+        const int hi = warp / 4;                    // tile inside the unit
+        const int row = tid & 127;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem + lanes + 128 * hi, tO = tmem + lanes + 256 + 128 * hi;
+        const float c = a.scale_log2;
+        // every decision below is warp-uniform: the TMEM loads and stores are warp-collective
+        auto wait_all = [&](int b, uint32_t parity, int site) {
+            return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
+        };
+        int t_tile = 0, ring = 0, n = 0, tails = 0;   // this tile's K tiles, all units', units read, V tails passed
+        Unit next = {};
+        auto next_of_tile = [&]() {
+            for (;;) {
+                if (!read_unit(n++, next, 139)) return false;
+                if (next.tiles < 0 || hi == 0 || next.two) return true;
+                ring += next.tiles;
+                // (its V tail comes by the same barrier, whose phases are waited for one by one)
+                if (next.nk % kKT != 0 && !wait_all(C::B_VTAIL, tails++ & 1, 144)) return false;
+            }
+        };
+        bool ok = next_of_tile();
+        while (ok && next.tiles > 0) {
+            const Unit u = next;
+            int token, head;
+            const bool in = cross_row(a, u.tok, u.ntok, (2 * (int)rank + hi) * 128 + row, token, head);
+            float m_ref = -INFINITY, l = 0.f;   // m_ref in raw score units
+            for (int j = 0; j < u.tiles; ++j, ++t_tile, ++ring) {
+                const int left = u.nk - j * kKT;   // keys from this tile on
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t tB = tS + 64 * half;
+                    if (!wait_all(C::B_SFULL + 2 * hi + half, t_tile & 1, 140)) { ok = false; break; }
+                    tc_fence_after();
+                    // the row's scores are read from tensor memory once and stay in registers
+                    uint32_t sr[2][32];
+                    tmem_ld32(tB, sr[0]);
+                    tmem_ld32(tB + 32, sr[1]);
+                    tmem_ld_wait();
+                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int base = 64 * half + 32 * q;
+                        if (left < base + 32) {
+                            const uint32_t vis = interval_bits(0, left, base);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) sr[q][i] = (vis >> i) & 1u ? sr[q][i] : 0xff800000u;   // -inf
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            mx4[0] = fmax3f(mx4[0], __uint_as_float(sr[q][i]), __uint_as_float(sr[q][i + 1]));
+                            mx4[1] = fmax3f(mx4[1], __uint_as_float(sr[q][i + 2]), __uint_as_float(sr[q][i + 3]));
+                            mx4[2] = fmax3f(mx4[2], __uint_as_float(sr[q][i + 4]), __uint_as_float(sr[q][i + 5]));
+                            mx4[3] = fmax3f(mx4[3], __uint_as_float(sr[q][i + 6]), __uint_as_float(sr[q][i + 7]));
+                        }
+                    }
+                    const float mx = fmaxf(fmax3f(mx4[0], mx4[1], mx4[2]), mx4[3]);
+                    const float m_new = fmaxf(m_ref, mx);
+                    // a row with nothing accumulated yet (O holds zeros) adopts the new maximum directly;
+                    // otherwise the reference only moves when the maximum grew by more than 2^8
+                    const bool rescale = m_ref != -INFINITY && (m_new - m_ref) * c > 8.f;
+                    if (m_ref == -INFINITY) m_ref = m_new;
+                    if (__any_sync(0xffffffffu, rescale)) {
+                        // O_i is quiescent once the previous half's PV is done: the next one waits for this P
+                        // (the one before that was done before this half's S)
+                        if (!wait_all(C::B_PVDONE + 2 * hi + (half ^ 1), (half ? t_tile : t_tile - 1) & 1, 141)) { ok = false; break; }
+                        tc_fence_after();
+                        const float alpha = rescale ? fast_exp2((m_ref - m_new) * c) : 1.f;
+#pragma unroll 1   // (rare; unrolled it takes registers from every tile)
+                        for (int q = 0; q < D / 16; ++q) {
+                            uint32_t o[16];
+                            tmem_ld16(tO + q * 16, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                            tmem_st16(tO + q * 16, o);
+                        }
+                        if (rescale) { l *= alpha; m_ref = m_new; }
+                    }
+                    const float moff = m_ref == -INFINITY ? 0.f : m_ref * c;
+                    // P = exp2(S * c - m * c) as packed bf16 over the first 32 columns of this half's S: the MMA's
+                    // operand type, half a step (2^-9 of a weight on average), where l adds the unrounded weights
+                    const uint64_t c2 = f2_pack(c, c), moff2 = f2_pack(-moff, -moff);
+                    uint64_t rs[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            float x0, x1;
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[q][i]), __uint_as_float(sr[q][i + 1])), c2, moff2), x0, x1);
+                            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+                            rs[(i >> 1) & 3] = f2_add(rs[(i >> 1) & 3], f2_pack(p0, p1));
+                            pk[i >> 1] = pack_bf16x2(p0, p1);
+                        }
+                        tmem_st16(tB + q * 16, pk);
+                    }
+                    float r0, r1;
+                    f2_unpack(f2_add(f2_add(rs[0], rs[1]), f2_add(rs[2], rs[3])), r0, r1);
+                    l += r0 + r1;
+                    const bool tail = half == 0 && left < kKT;
+                    if (tail) {   // V's rows past the end (both tiles' warps write the same zeros)
+                        if (!wait_all(C::B_VTAIL, tails & 1, 142)) { ok = false; break; }
+                        ++tails;
+                        uint8_t *vb = sv + ring % kStages * C::kHalf + row * 128;
+                        if (row >= left)
+#pragma unroll
+                            for (int p = 0; p < C::kPanels / CG; ++p)
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(vb + p * kPanel + 16 * i) = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_smem();
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (CG == 2 && tail) mbar_arrive_cluster<true>(lead_bar(C::B_PFULL + 2 * hi + half));
+                        else arrive_lead(C::B_PFULL + 2 * hi + half);
+                    }
+                }
+                if (!ok) break;
+            }
+            const int last_tile = t_tile - 1;
+            if (!ok || !(ok = wait_all(C::B_PVDONE + 2 * hi + 1, last_tile & 1, 143))) break;
+            tc_fence_after();
+            // O / l: through shared memory, so that eight lanes write a row's 128 bytes, or, as a part of the row's
+            // keys, in fp32 with the part's log-sum-exp. O_i is free for the next unit's PV as soon as it is read.
+            const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m_ref * c + log2f(l);
+            const int64_t at = in ? ((int64_t)token * a.hq + u.g * a.group + head) * D : -1;
+            const size_t pr = ((size_t)max(u.slot, 0) * a.hkv + u.g) * (PADOC_CROSS_UNIT_BLOCKS * kBlk) + hi * 128 + row;
+            uint8_t *stage = so + warp * 4096;
+#pragma unroll
+            for (int half = 0; half < C::kPanels; ++half) {
+                uint32_t o[2][32];
+                tmem_ld32(tO + 64 * half, o[0]);
+                tmem_ld32(tO + 64 * half + 32, o[1]);
+                tmem_ld_wait();
+                if (half == C::kPanels - 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_lead(C::B_OFREE + hi);
+                }
+                auto v = [&](int i) { return __uint_as_float(o[i >> 5][i & 31]) * inv; };
+                if (u.slot >= 0) {
+                    if (in) {
+#pragma unroll
+                        for (int i = 0; i < 64; i += 8)
+                            st_global_v8(a.part + pr * D + 64 * half + i, v(i), v(i + 1), v(i + 2), v(i + 3), v(i + 4), v(i + 5),
+                                         v(i + 6), v(i + 7));
+                    }
+                    continue;
+                }
+#pragma unroll
+                for (int i = 0; i < 64; i += 8)
+                    *reinterpret_cast<uint4 *>(stage + lane * 128 + (((i / 8) ^ (lane & 7)) << 4)) =
+                        make_uint4(pack_bf16x2(v(i), v(i + 1)), pack_bf16x2(v(i + 2), v(i + 3)), pack_bf16x2(v(i + 4), v(i + 5)),
+                                   pack_bf16x2(v(i + 6), v(i + 7)));
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int r = 4 * i + (lane >> 3), k = lane & 7;
+                    const int64_t to = __shfl_sync(0xffffffffu, at, r);
+                    const uint4 w = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((k ^ (r & 7)) << 4));
+                    if (to >= 0) *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.o + to + 64 * half + 8 * k) = w;
+                }
+                __syncwarp();
+            }
+            if (in) {
+                if (u.slot < 0) a.lse[at / D] = lse2 * PADOC_LN2;
+                else a.part_lse[pr] = lse2;
+            }
+            ok = next_of_tile();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    // neither CTA leaves while the other may still reach its shared memory, barriers or tensor memory
+    if (CG == 2) cluster_sync();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc<CG>(tmem, kTmemCols);
+    }
+}
+
+template <int D, int CG>
+padoc_status launch(const padoc_cross_args &a, cudaStream_t stream)
+{
+    auto kernel = cross_tc_kernel<D, CG>;
+    constexpr size_t bytes = Cfg<D, CG>::kSmemBytes;
+    if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)bytes)) return st;
+    CUtensorMap qmap, kmap, vmap;
+    if (!padoc_make_tmap_bf16_heads(&qmap, a.q, D, a.hq, a.query_rows, a.q_stride * 2, a.group, a.block_tokens) ||
+        !padoc_make_tmap_bf16(&kmap, a.k, (uint64_t)a.hkv * D, a.key_rows, a.k_stride * 2, 64, 64 / CG) ||
+        !padoc_make_tmap_bf16(&vmap, a.v, (uint64_t)a.hkv * D, a.key_rows, a.v_stride * 2, 64, kKT))
+        return PADOC_ERR_CUDA;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)(a.num_units * a.hkv * CG));
+    lc.blockDim = dim3(kThreads);
+    lc.dynamicSmemBytes = bytes;
+    lc.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = CG == 1 ? 0 : 1;
+    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, qmap, kmap, vmap, a));
+    return padoc_launch_status();
+}
+
+}  // namespace
+
+padoc_status padoc_cross_launch_tc(const padoc_cross_args &args, int head_dim, bool pair, cudaStream_t stream)
+{
+    padoc_cross_args a = args;
+    a.err = padoc_device_error_word();
+    if (!a.err) return PADOC_ERR_CUDA;
+    if (head_dim == 64) return launch<64, 1>(a, stream);
+    return pair ? launch<128, 2>(a, stream) : launch<128, 1>(a, stream);
+}

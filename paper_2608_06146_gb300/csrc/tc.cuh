@@ -156,6 +156,18 @@ __device__ __forceinline__ void umma_bf16_ss_k128_warp(uint32_t d_tmem, uint64_t
             " add.s64 a, %1, %4+6;\n add.s64 b, %2, %5+6;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n}" ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "n"(PA >> 4), "n"(PB >> 4)
             : "memory");
 }
+// Four K-steps (64 elements, one panel) of a K-major product, D = A[smem] . B[smem]^T.
+__device__ __forceinline__ void umma_bf16_ss_k64_warp(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc)
+{
+    asm volatile(
+        "{\n .reg .pred e, t, f;\n .reg .b64 a, b;\n elect.sync _|e, 0xffffffff;\n"
+        " setp.eq.u32 t, 0, 0;\n setp.ne.u32 f, 0, 0;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, f;\n"
+        " add.s64 a, %1, 2;\n add.s64 b, %2, 2;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n"
+        " add.s64 a, %1, 4;\n add.s64 b, %2, 4;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n"
+        " add.s64 a, %1, 6;\n add.s64 b, %2, 6;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n}" ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc)
+        : "memory");
+}
 // Four K-steps (64 elements) of D (+)= A[tmem] . B[smem], B MN-major (a step adds 16 rows, 2048 bytes);
 // A's steps start at columns 0, A1, A2 and A3; `accumulate` 0: the first step overwrites D.
 template <int CG, int A1 = 8, int A2 = 16, int A3 = 24>
