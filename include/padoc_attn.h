@@ -962,7 +962,7 @@ typedef struct {
     int32_t num_key_tiles;   /* backward: key tiles of at most 128 rows, seen by the same segments as a whole */
     int32_t num_covers;      /* (key interval, segment) pairs */
     int32_t max_steps;       /* most blocks of 64 rows that see one key tile */
-    int32_t reserved;
+    int32_t cluster;         /* CTAs that share a key tile in the backward */
     int64_t pairs;           /* visible (query row, key row) pairs */
     int64_t plan_ints;       /* int32 words in the plan blob */
     int64_t off_units;       /* offsets (int32 words) of the blob's arrays */

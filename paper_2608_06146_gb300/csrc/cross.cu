@@ -645,7 +645,7 @@ extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const
     a.part = a.dsum + stats;
     cudaStream_t cs = (cudaStream_t)stream;
     if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_bwd_simt<float, 64>(a, cs) : run_bwd_simt<float, 128>(a, cs);
-    else st = c.head_dim == 64 ? run_bwd_simt<__nv_bfloat16, 64>(a, cs) : run_bwd_simt<__nv_bfloat16, 128>(a, cs);
+    else st = padoc_cross_launch_bwd_tc(a, c.head_dim, info->cluster, cs);
     if (st != PADOC_OK) return st;
     return a.num_merges ? padoc_cross_launch_merge(a, c.dtype, c.head_dim, true, false, cs) : PADOC_OK;
 }

@@ -41,3 +41,5 @@ padoc_status padoc_cross_launch_merge(const padoc_cross_args &a, padoc_dtype dty
                                       cudaStream_t stream);
 // The forward's units on the tensor cores (cross_tc.cu).
 padoc_status padoc_cross_launch_tc(const padoc_cross_args &args, int head_dim, bool pair, cudaStream_t stream);
+// The backward's passes on the tensor cores (cross_bwd_tc.cu); cluster: CTAs that share a dK/dV unit.
+padoc_status padoc_cross_launch_bwd_tc(const padoc_cross_args &args, int head_dim, int cluster, cudaStream_t stream);

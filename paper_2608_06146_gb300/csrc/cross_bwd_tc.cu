@@ -1,0 +1,946 @@
+// cross_bwd_tc.cu -- gradients of cross attention on the 5th-generation tensor cores, in two passes without atomics.
+//
+// With c = scale * log2(e), lse2 = lse * log2(e), D = rowsum(dO * O):
+//   P = exp2(S c - lse2),  dS = P (dP - D),  S = Q K^T,  dP = dO V^T.
+//
+// dQ pass: a unit is a 128-row tile of packed (token, head) rows of one KV head over a segment's keys, or a part of
+//   them (parts are joined by a later kernel). It walks 64-key steps: S = Q K^T (Q in tensor memory), dP = dO V^T (dO in
+//   shared memory), dS as bf16 over S, dQ += dS K. It also writes -lse2 and D of its rows for the other pass. A
+//   running CTA takes over units not yet launched (cluster launch control).
+// dK/dV pass: a unit is a tile of at most 128 keys that the same segments see and a KV head, run by a cluster of 1 to 8
+//   CTAs that share out its steps and add their fp32 sums through distributed shared memory, in rank order. A step is a
+//   block of 64 packed rows: S^T = K Q^T, dP^T = V dO^T (V in tensor memory), P^T and dS^T as bf16 over S^T, dV += P^T dO,
+//   dK += dS^T Q. Query heads of the group and the segments that share keys are thus summed in a fixed order.
+//
+// No step needs a mask but the last ones: where a segment's keys (dQ) or rows (dK/dV) end inside a step, the weights
+// past the end become 0 and the operand rows there zeros, because what lies behind may be anything.
+//
+// A step is bound by its chain S -> softmax -> accumulation -> S more than by its MMAs, so S, dP and the accumulating
+// MMAs are issued by a warp each; P and dS share S's columns, so dP's buffer is free as soon as it is read; waits and
+// roles are uniform per warp. A softmax warp owns 32 TMEM lanes (rows) and one 32-column half of a step; its bf16
+// results go to the first 16 columns of its own half of S (dS of the dK/dV pass to the other 16).
+// Warp roles (384 threads): warps 0-7 softmax and epilogue, warp 8 TMA producer, warp 9 TMEM allocation and S, warp 10
+// the accumulating MMAs, warp 11 dP (converged warps, one elected lane issues). Every wait is bounded; a wait that
+// runs out records an error and all roles leave their loops, the MMA warps wait for their MMAs, the producer for its
+// copies, and tensor memory is released.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "cross.cuh"
+#include "tc.cuh"
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr uint32_t kTmemCols = 512;
+constexpr int kBlk = PADOC_CROSS_BLOCK;
+
+__device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, int *err, int site, volatile int *abort_flag)
+{
+    if (*abort_flag) return false;
+    if (mbar_wait_bounded(bar, parity, err, site)) return true;
+    *abort_flag = 1;
+    return false;
+}
+
+// TMEM column of k-slice k (16 values) of a 64-wide bf16 operand written by the softmax warps: column half c packs its
+// 32 values into the first 16 columns of its own half.
+__host__ __device__ constexpr uint32_t slice_col(int k) { return (uint32_t)((k / 2) * 32 + (k % 2) * 8); }
+
+__device__ __forceinline__ void store_row_bf16(__nv_bfloat16 *dst, const float (&o)[16], float mul)
+{
+#pragma unroll
+    for (int i = 0; i < 16; i += 8) {
+        uint4 w;
+        w.x = pack_bf16x2(o[i] * mul, o[i + 1] * mul);
+        w.y = pack_bf16x2(o[i + 2] * mul, o[i + 3] * mul);
+        w.z = pack_bf16x2(o[i + 4] * mul, o[i + 5] * mul);
+        w.w = pack_bf16x2(o[i + 6] * mul, o[i + 7] * mul);
+        *reinterpret_cast<uint4 *>(dst + i) = w;
+    }
+}
+
+// A thread's 16-byte pieces of a row of D / 2 dims, its column half of the row (panels of 64 dims, 128-byte swizzle),
+// and the same as the A operand in tensor memory.
+template <int D>
+struct HalfRow {
+    static constexpr int kPieces = D / 16;
+    static __device__ __forceinline__ int offset(int ch, int row, int i, int panel_bytes)
+    {
+        if constexpr (D == 128) return ch * panel_bytes + row * 128 + ((i ^ (row & 7)) * 16);
+        return row * 128 + (((4 * ch + i) ^ (row & 7)) * 16);
+    }
+    static __device__ __forceinline__ void to_tmem(uint32_t taddr, const uint8_t *tile, int ch, int row, int panel_bytes)
+    {
+        uint32_t w[4 * kPieces];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(tile + offset(ch, row, i, panel_bytes));
+            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+        }
+        if constexpr (D == 128) tmem_st32(taddr + 32 * ch, w);
+        else tmem_st16(taddr + 16 * ch, w);
+    }
+};
+
+// ================================================================================================
+// dK/dV pass
+// ================================================================================================
+namespace dkv {
+constexpr int kKT = PADOC_CROSS_KEY_TILE;   // 128 keys: the M of every MMA
+constexpr int kStages = 4;
+constexpr uint32_t kColS = 0, kColDP = 128, kColV = 192, kColAcc = 256;   // kColS: two buffers; kColAcc: dV, then dK
+constexpr int kKPanel = kKT * 128;           // [128 rows][64 bf16]
+constexpr int kQPanel = kBlk * 128;          // [64 rows][64 bf16]
+constexpr int kAuxBytes = 2 * kBlk * 4;      // -lse2[64], D[64]
+enum {
+    B_KV = 0,
+    B_QFULL = 1,                  // [stage]
+    B_QEMPTY = 1 + kStages,       // [stage]
+    B_SFULL = 1 + 2 * kStages,    // [step parity]
+    B_PFULL = 3 + 2 * kStages,    // [step parity], an arrival per softmax warp
+    B_ACC = 5 + 2 * kStages,      // [step parity]: the step's accumulating MMAs are done
+    B_DPFREE = 7 + 2 * kStages,   // dP is read (an arrival per softmax warp)
+    B_VT = 8 + 2 * kStages,       // V is in tensor memory (an arrival per softmax warp)
+    B_FINAL = 9 + 2 * kStages,    // [issuing warp]
+    B_COUNT = 12 + 2 * kStages
+};
+template <int D>
+constexpr size_t smem_bytes() { return 1024 + 2 * (size_t)(D / 64) * kKPanel + 2 * (size_t)kStages * (D / 64) * kQPanel + (size_t)kStages * kAuxBytes + B_COUNT * 8 + 64; }
+}  // namespace dkv
+
+// The blocks of rows that a key tile's steps are, one after the other.
+struct Steps {
+    const padoc_cross_cover *covers;
+    padoc_cross_cover c;
+    int i, b;
+    __device__ __forceinline__ Steps(const padoc_cross_args &a, const padoc_cross_key_tile &t, int first) : covers(a.covers + t.cover), i(0), b(first)
+    {
+        c = covers[0];
+        while (b >= c.nsub) {
+            b -= c.nsub;
+            c = covers[++i];
+        }
+    }
+    __device__ __forceinline__ void next(bool more)
+    {
+        if (++b == c.nsub && more) {
+            b = 0;
+            c = covers[++i];
+        }
+    }
+    __device__ __forceinline__ int tokens(const padoc_cross_args &a) const { return min(a.block_tokens, c.ntok - b * a.block_tokens); }
+};
+
+// NC: the CTAs of a unit's cluster.
+template <int D, int NC>
+__global__ void __launch_bounds__(kThreads, 1)
+cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap gmap,
+                 const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
+{
+    using namespace dkv;
+    constexpr int kPanels = D / 64, kKTile = kPanels * kKPanel, kQTile = kPanels * kQPanel;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t *sk = smem;
+    uint8_t *sv = sk + kKTile;
+    uint8_t *sq = sv + kKTile;                 // [stage] Q step tiles
+    uint8_t *sg = sq + kStages * kQTile;       // [stage] dO step tiles
+    uint8_t *aux = sg + kStages * kQTile;      // [stage] -lse2, D
+    uint64_t *bars = (uint64_t *)(aux + kStages * kAuxBytes);
+    uint32_t *tmem_slot = (uint32_t *)(bars + B_COUNT);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (a value the compiler knows to be warp-uniform)
+    // the cluster's unit, and this CTA's steps of it: ub .. ub + nu - 1
+    const int unit = (int)blockIdx.x / NC, rank = (int)blockIdx.x % NC, g = unit % a.hkv, ti = unit / a.hkv;
+    padoc_cross_key_tile t;
+    if (ti < a.num_tiles) {
+        t = a.tiles[ti];
+    } else {   // key rows that the plan does not reach
+        t.k0 = a.tail_begin + (ti - a.num_tiles) * kKT;
+        t.nk = (int)min((int64_t)kKT, a.key_rows - t.k0);
+        t.cover = t.ncover = t.steps = 0;
+    }
+    if (t.steps == 0) {   // keys that no row sees
+        if (rank == 0)
+            for (int i = tid; i < t.nk * (D / 8); i += kThreads) {
+                const size_t r = (size_t)(t.k0 + i / (D / 8));
+                const int c = g * D + i % (D / 8) * 8;
+                *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.dk + r * a.dk_stride + c) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.dv + r * a.dv_stride + c) = make_uint4(0, 0, 0, 0);
+            }
+        pdl_wait_prerequisite();
+        return;
+    }
+    const int k0 = __shfl_sync(0xffffffffu, t.k0, 0), steps = __shfl_sync(0xffffffffu, t.steps, 0);
+    const int ub = (int)((int64_t)steps * rank / NC), nu = (int)((int64_t)steps * (rank + 1) / NC) - ub;
+    const int used = a.block_tokens * a.group;   // rows of a block that its copies write
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+
+    if (tid == 0) {
+        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), (i == B_PFULL || i == B_PFULL + 1 || i == B_DPFREE || i == B_VT) ? 8
+                                                                  : i == B_SFULL || i == B_SFULL + 1 ? 2 : 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (used < kBlk) {   // the others are zeros throughout: they are summed over
+        for (int i = tid; i < 2 * kStages * kPanels * (kBlk - used) * 8; i += kThreads) {
+            const int r = i / 8 % (kBlk - used) + used, b = i / 8 / (kBlk - used);
+            *reinterpret_cast<uint4 *>(sq + b * kQPanel + r * 128 + i % 8 * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+    }
+    if (warp == 9) {
+        tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    const int lq = warp & 3, ch = warp >> 2;          // softmax warps: TMEM lane quarter, column half
+    const uint32_t lanes = (uint32_t)(lq * 32) << 16;
+    bool sums = false;                                // softmax warps: this CTA's dV and dK are complete
+
+    if (warp == 8) {
+        // ---------------------------------------------------------------- TMA producer
+        if (lane == 0 && nu == 0) pdl_wait_prerequisite();
+        if (lane == 0 && nu > 0) {
+            tma_prefetch_desc(&qmap);
+            tma_prefetch_desc(&gmap);
+            tma_prefetch_desc(&kmap);
+            tma_prefetch_desc(&vmap);
+            pdl_wait_prerequisite();   // -lse2 and D are the dQ pass's
+            mbar_arrive_expect_tx(bar(B_KV), 2 * kKTile);
+#pragma unroll
+            for (int p = 0; p < kPanels; ++p) {
+                tma_load_2d(smem_u32(sk) + p * kKPanel, &kmap, g * D + 64 * p, k0, bar(B_KV));
+                tma_load_2d(smem_u32(sv) + p * kKPanel, &vmap, g * D + 64 * p, k0, bar(B_KV));
+            }
+            int issued = 0;
+            Steps st(a, t, ub);
+            for (int u = 0; u < nu; ++u) {
+                const int s = u % kStages;
+                if (u >= kStages && !wait_or_abort(bar(B_QEMPTY + s), (u / kStages - 1) & 1, a.err, 150, abort_flag)) break;
+                const int tok = st.c.tok + st.b * a.block_tokens;
+                const size_t at = ((size_t)g * a.num_subs + st.c.sub + st.b) * kBlk;
+                const uint32_t fb = bar(B_QFULL + s);
+                const uint32_t qb = smem_u32(sq + s * kQTile), gb = smem_u32(sg + s * kQTile);
+                const uint32_t ab = smem_u32(aux + s * kAuxBytes);
+                mbar_arrive_expect_tx(fb, 2 * kPanels * used * 128 + kAuxBytes);
+#pragma unroll
+                for (int p = 0; p < kPanels; ++p) {
+                    tma_load_3d(qb + p * kQPanel, &qmap, 64 * p, g * a.group, tok, fb);
+                    tma_load_3d(gb + p * kQPanel, &gmap, 64 * p, g * a.group, tok, fb);
+                }
+                bulk_load(ab, a.neg_lse2 + at, kBlk * 4, fb);
+                bulk_load(ab + kBlk * 4, a.dsum + at, kBlk * 4, fb);
+                issued = u + 1;
+                st.next(issued < nu);
+            }
+            // copies still in flight must land before the CTA's shared memory is released
+            mbar_wait_bounded(bar(B_KV), 0, a.err, 151);
+            for (int u = (issued > kStages ? issued - kStages : 0); u < issued; ++u)
+                mbar_wait_bounded(bar(B_QFULL + u % kStages), (u / kStages) & 1, a.err, 152);
+        }
+    } else if (warp >= 9) {
+        // ---------------------------------------------------------------- MMA issuers (whole warps)
+        if (nu > 0) {
+            auto wait_w = [&](int b, uint32_t parity, int site) {
+                return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
+            };
+            constexpr uint32_t idS = umma_idesc_bf16(128, kBlk, false), idAcc = umma_idesc_bf16(128, D, true);
+            if (warp == 9) {
+                const uint64_t dK = umma_desc_sw128(smem_u32(sk), 16, 1024);
+                bool ok = wait_w(B_KV, 0, 160);
+                for (int u = 0; ok && u < nu; ++u) {
+                    const int s = u % kStages;
+                    const uint32_t b = (uint32_t)(u & 1) * 64;
+                    ok = wait_w(B_QFULL + s, (u / kStages) & 1, 161) && (u < 2 || wait_w(B_ACC + (u & 1), ((u >> 1) - 1) & 1, 163));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t dq = umma_desc_sw128(smem_u32(sq + s * kQTile), 16, 1024);
+                    if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kKPanel, kQPanel>(tmem + kColS + b, dK, dq, idS);
+                    else umma_bf16_ss_k64_warp(tmem + kColS + b, dK, dq, idS);
+                    umma_commit_warp(bar(B_SFULL + (u & 1)));
+                }
+            } else if (warp == 11) {
+                bool ok = wait_w(B_VT, 0, 166);
+                for (int u = 0; ok && u < nu; ++u) {
+                    const int s = u % kStages;
+                    ok = wait_w(B_QFULL + s, (u / kStages) & 1, 167) && (u == 0 || wait_w(B_DPFREE, (u - 1) & 1, 165));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t dg = umma_desc_sw128(smem_u32(sg + s * kQTile), 16, 1024);
+                    if constexpr (D == 128) umma_bf16_ts_k128_warp<kQPanel>(tmem + kColDP, tmem + kColV, dg, idS);
+                    else umma_bf16_ts_k64_warp(tmem + kColDP, tmem + kColV, dg, idS);
+                    umma_commit_warp(bar(B_SFULL + (u & 1)));
+                }
+            } else {
+                bool ok = true;
+                for (int u = 0; ok && u < nu; ++u) {
+                    const int s = u % kStages;
+                    const uint32_t b = (uint32_t)(u & 1) * 64;
+                    if (!(ok = wait_w(B_PFULL + (u & 1), (u >> 1) & 1, 162))) break;
+                    tc_fence_after();
+                    // the step's Q and dO as MN-major B operands (N = head dim, K = the 64 rows)
+                    const uint64_t gmn = umma_desc_sw128(smem_u32(sg + s * kQTile), kQPanel, 1024);
+                    const uint64_t qmn = umma_desc_sw128(smem_u32(sq + s * kQTile), kQPanel, 1024);
+                    umma_bf16_ts_k64_mn_warp<1, slice_col(1), slice_col(2), slice_col(3)>(tmem + kColAcc, tmem + kColS + b, gmn, idAcc, u > 0);
+                    umma_bf16_ts_k64_mn_warp<1, slice_col(1), slice_col(2), slice_col(3)>(tmem + kColAcc + D, tmem + kColS + b + 16, qmn, idAcc, u > 0);
+                    umma_commit_warp(bar(B_ACC + (u & 1)));
+                    umma_commit_warp(bar(B_QEMPTY + s));
+                }
+            }
+            // every MMA issued above must complete before tensor memory is read or released
+            umma_commit_warp(bar(B_FINAL + warp - 9));
+            mbar_wait_bounded(bar(B_FINAL + warp - 9), 0, a.err, 164);
+        }
+    } else {
+        // ---------------------------------------------------------------- softmax + epilogue
+        const float c = a.scale_log2;
+        auto wait_all = [&](int b, uint32_t parity, int site) {
+            return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
+        };
+        bool ok = true;
+        if (nu > 0 && (ok = wait_all(B_KV, 0, 173))) {   // V's rows into tensor memory, half of the dims a thread
+            HalfRow<D>::to_tmem(tmem + lanes + kColV, sv, ch, lq * 32 + lane, kKPanel);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_warp(bar(B_VT));
+        }
+        Steps st(a, t, nu > 0 ? ub : 0);
+        for (int u = 0; ok && u < nu; ++u) {
+            const int s = u % kStages;
+            const uint32_t b = (uint32_t)(u & 1) * 64 + 32 * ch;
+            const int rows = __shfl_sync(0xffffffffu, st.tokens(a), 0) * a.group;
+            const bool partial = rows < used;
+            if (!wait_all(B_QFULL + s, (u / kStages) & 1, 171) || !wait_all(B_SFULL + (u & 1), (u >> 1) & 1, 170)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            st.next(u + 1 < nu);
+            uint32_t sr[32], dr[32];
+            tmem_ld32(tmem + lanes + kColS + b, sr);
+            tmem_ld32(tmem + lanes + kColDP + 32 * ch, dr);
+            const float4 *la = reinterpret_cast<const float4 *>(aux + s * kAuxBytes) + 8 * ch;
+            const float4 *da = reinterpret_cast<const float4 *>(aux + s * kAuxBytes + kBlk * 4) + 8 * ch;
+            uint32_t vis = 0xffffffffu;
+            if (partial) {
+                // the block's rows past the segment's, which the products below sum over: zeros (S and dP, which
+                // have read them, are done)
+                vis = interval_bits(0, rows, 32 * ch);
+                for (int i = tid; i < (kBlk - rows) * 8 * kPanels; i += 256) {
+                    const int r = rows + i / 8 % (kBlk - rows), p = i / 8 / (kBlk - rows), o = p * kQPanel + r * 128 + i % 8 * 16;
+                    *reinterpret_cast<uint4 *>(sq + s * kQTile + o) = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(sg + s * kQTile + o) = make_uint4(0, 0, 0, 0);
+                }
+                fence_proxy_async_smem();
+            }
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_warp(bar(B_DPFREE));
+            uint32_t pk[16], dk[16];
+            const uint64_t c2 = f2_pack(c, c);
+            // two row columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D), both rounded to the MMAs'
+            // operand type (half a step, 2^-9 of a value on average)
+            auto column_pairs = [&](auto masked) {
+#pragma unroll
+                for (int i4 = 0; i4 < 8; ++i4) {
+                    const float4 l4 = la[i4], d4 = da[i4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int i = 4 * i4 + 2 * j;
+                        float x0, x1;
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2,
+                                         j ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y)), x0, x1);
+                        float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+                        const uint64_t e = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])),
+                                                  j ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y));
+                        float d0, d1;
+                        f2_unpack(f2_mul(f2_pack(p0, p1), e), d0, d1);
+                        if (decltype(masked)::value) {
+                            p0 = (vis >> i) & 1u ? p0 : 0.f;
+                            p1 = (vis >> (i + 1)) & 1u ? p1 : 0.f;
+                            d0 = (vis >> i) & 1u ? d0 : 0.f;
+                            d1 = (vis >> (i + 1)) & 1u ? d1 : 0.f;
+                        }
+                        pk[i >> 1] = pack_bf16x2(p0, p1);
+                        dk[i >> 1] = pack_bf16x2(d0, d1);
+                    }
+                }
+            };
+            if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
+            tmem_st16(tmem + lanes + kColS + b, pk);
+            tmem_st16(tmem + lanes + kColS + b + 16, dk);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_warp(bar(B_PFULL + (u & 1)));
+        }
+        sums = ok && (nu == 0 || wait_all(B_FINAL + 1, 0, 172));
+        tc_fence_after();
+    }
+    // Epilogue. The 2 D columns of dV | dK are split over the cluster's CTAs: each one's softmax threads
+    // (a key row and half of the columns each) send the other CTAs' parts to their shared memory, which
+    // nothing else uses any more, add what they receive to their own part in rank order and write it.
+    constexpr int kPart = 2 * D / NC, kHalfPart = kPart / 2;   // columns of a CTA, of a thread
+    static_assert(kHalfPart % 16 == 0, "");
+    auto part = [&](int p, int c, uint32_t (&o)[16]) {       // 16 of this CTA's sums of part p
+        if (nu > 0) {
+            tmem_ld16(tmem + lanes + kColAcc + kPart * p + kHalfPart * ch + c, o);
+            tmem_ld_wait();
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = 0u;
+        }
+    };
+    // the place of a thread's 16 columns from CTA `from` in the receiver's shared memory
+    auto slot = [&](int from, int to, int c) {
+        const int n = from < to ? from : from - 1;
+        return (uint32_t)(n * kPart * kKT * 4 + (kHalfPart * ch + c) * kKT * 4 + (lq * 32 + lane) * 16);
+    };
+    static_assert((NC - 1) * kPart * kKT * 4 <= 2 * kKTile + 2 * kStages * kQTile, "");
+    if (NC > 1) {
+        tc_fence_before();
+        cluster_sync();
+        if (sums) {
+            tc_fence_after();
+#pragma unroll 1
+            for (int d = 1; d < NC; ++d) {
+                const int p = (rank + d) % NC;
+                const uint32_t dst = cluster_map(smem_u32(smem), p);
+#pragma unroll 1
+                for (int c = 0; c < kHalfPart; c += 16) {
+                    uint32_t o[16];
+                    part(p, c, o);
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        st_cluster_v4(dst + slot(rank, p, c + i), make_int4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+                }
+            }
+        }
+        cluster_sync();
+    }
+    if (sums) {
+#pragma unroll 1
+        for (int c = 0; c < kHalfPart; c += 16) {
+            uint32_t own[16];
+            part(rank, c, own);
+            float acc[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+#pragma unroll
+            for (int from = 0; from < NC; ++from)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const float4 x = from == rank ? make_float4(__uint_as_float(own[i]), __uint_as_float(own[i + 1]),
+                                                                __uint_as_float(own[i + 2]), __uint_as_float(own[i + 3]))
+                                                  : *reinterpret_cast<const float4 *>(smem + slot(from, rank, c + i));
+                    acc[i] += x.x;
+                    acc[i + 1] += x.y;
+                    acc[i + 2] += x.z;
+                    acc[i + 3] += x.w;
+                }
+            const int col = kPart * rank + kHalfPart * ch + c, r = lq * 32 + lane;
+            const bool isk = col >= D;                       // dV first, then dK (times scale)
+            if (r < t.nk)
+                store_row_bf16(isk ? (__nv_bfloat16 *)a.dk + (size_t)(k0 + r) * a.dk_stride + g * D + (col - D)
+                                   : (__nv_bfloat16 *)a.dv + (size_t)(k0 + r) * a.dv_stride + g * D + col,
+                               acc, isk ? a.scale : 1.f);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+// ================================================================================================
+// dQ pass
+// ================================================================================================
+namespace dqp {
+constexpr int kQT = PADOC_CROSS_DQ_BLOCKS * kBlk;   // 128 rows: the M of every MMA
+constexpr int kW = PADOC_CROSS_DQ_STEP;             // 64 keys per step
+constexpr int kStages = 4;
+constexpr int kQPanel = kQT * 128;           // [128 rows][64 bf16]
+constexpr int kKPanel = kW * 128;            // [64 rows][64 bf16]
+constexpr int kSlots = 3;                    // S buffers; a step's dS takes its S's place
+constexpr uint32_t kColQ = 0, kColS = 64, kColDP = 256, kColDQ = 384;   // Q (A operand), S x 3, dP x 2, dQ
+enum {
+    B_QROWS = 0,                   // the unit's Q has landed
+    B_GROWS = 1,                   // its dO and O have landed
+    B_QT = 2,                      // its Q is in tensor memory (an arrival per softmax warp)
+    B_D = 3,                       // its rows' halves of D are in shared memory (an arrival per softmax warp)
+    B_DREAD = 4,                   // ... and have been read, as dO and O (an arrival per softmax warp)
+    B_QFREE = 5,                   // Q's place is free for the next unit's (an arrival per softmax warp)
+    B_GFREE = 6,                   // the unit's last dP is done
+    B_DQFULL = 7,                  // the unit's dQ is complete
+    B_DQFREE = 8,                  // ... and read (an arrival per softmax warp)
+    B_NEXT = 9,                    // the launch control's answer
+    B_UFULL = 10,                  // [unit parity]
+    B_UEMPTY = 12,                 // [unit parity], an arrival per reading warp
+    B_KFULL = 14,                  // [stage]
+    B_KEMPTY = 14 + kStages,       // [stage]
+    B_SFULL = 14 + 2 * kStages,    // [slot]: S and dP (an arrival each)
+    B_PFULL = 17 + 2 * kStages,    // [slot]: dS (an arrival per softmax warp)
+    B_ACC = 20 + 2 * kStages,      // [slot]: the accumulating MMAs that read it are done
+    B_DPFREE = 23 + 2 * kStages,   // [step parity]: dP is read (an arrival per softmax warp)
+    B_FINAL = 25 + 2 * kStages,    // [issuing warp]
+    B_COUNT = 28 + 2 * kStages
+};
+struct Unit {   // steps < 0: no more units
+    int32_t tok, ntok, k0, nk;
+    int32_t g, slot, sub, steps;
+};
+constexpr int kReaders = 11;       // softmax and issuing warps
+template <int D>
+constexpr size_t smem_bytes()
+{
+    return 1024 + 3 * (size_t)(D / 64) * kQPanel + 2 * (size_t)kStages * (D / 64) * kKPanel + 2 * sizeof(Unit) + 16 + B_COUNT * 8 + 32 + 2 * kQT * 4;
+}
+static_assert(smem_bytes<128>() <= 232448, "shared memory per CTA");
+}  // namespace dqp
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap gmap,
+                const __grid_constant__ CUtensorMap omap, const __grid_constant__ CUtensorMap kmap,
+                const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
+{
+    using namespace dqp;
+    constexpr int kPanels = D / 64, kQTile = kPanels * kQPanel, kKTile = kPanels * kKPanel;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t *sq = smem;                        // Q, dO and O rows; dQ leaves by way of Q's place
+    uint8_t *sg = sq + kQTile;
+    uint8_t *so = sg + kQTile;
+    uint8_t *sk = so + kQTile;                 // [stage] K step tiles
+    uint8_t *sv = sk + kStages * kKTile;       // [stage] V step tiles
+    Unit *units = (Unit *)(sv + kStages * kKTile);   // [2]
+    uint8_t *answer = (uint8_t *)(units + 2);  // 16 bytes
+    uint64_t *bars = (uint64_t *)(answer + 16);
+    uint32_t *tmem_slot = (uint32_t *)(bars + B_COUNT);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    float *dsum = (float *)(tmem_slot + 8);    // [2][128]: the two column halves' parts of D
+
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (a value the compiler knows to be warp-uniform)
+    const int used = a.block_tokens * a.group;
+    pdl_launch_dependents();   // the dK/dV pass may take the SMs that run out of work here
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+
+    if (tid == 0) {
+        for (int i = 0; i < B_COUNT; ++i) {
+            const bool soft = i == B_QT || i == B_D || i == B_DREAD || i == B_QFREE || i == B_DQFREE ||
+                              (i >= B_PFULL && i < B_PFULL + kSlots) || i == B_DPFREE || i == B_DPFREE + 1;
+            mbar_init(bar(i), soft ? 8 : i == B_UEMPTY || i == B_UEMPTY + 1 ? kReaders : i >= B_SFULL && i < B_SFULL + kSlots ? 2 : 1);
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (used < kBlk) {   // rows that no copy writes (dQ's way out puts what it likes there)
+        for (int i = tid; i < 6 * kPanels * (kBlk - used) * 8; i += kThreads) {
+            const int r = i / 8 % (kBlk - used) + used, b = i / 8 / (kBlk - used);
+            *reinterpret_cast<uint4 *>(sq + b * kBlk * 128 + r * 128 + i % 8 * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+    }
+    if (warp == 9) {
+        tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    auto wait_w = [&](int b, uint32_t parity, int site) {
+        return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
+    };
+    // the n-th unit, as every lane of a reading warp sees it
+    auto read_unit = [&](int n, Unit &u, int site) {
+        if (!wait_w(B_UFULL + (n & 1), (n >> 1) & 1, site)) return false;
+        const Unit v = units[n & 1];
+        u.tok = __shfl_sync(0xffffffffu, v.tok, 0);
+        u.ntok = __shfl_sync(0xffffffffu, v.ntok, 0);
+        u.nk = __shfl_sync(0xffffffffu, v.nk, 0);
+        u.g = __shfl_sync(0xffffffffu, v.g, 0);
+        u.slot = __shfl_sync(0xffffffffu, v.slot, 0);
+        u.sub = __shfl_sync(0xffffffffu, v.sub, 0);
+        u.steps = __shfl_sync(0xffffffffu, v.steps, 0);
+        __syncwarp();   // (every lane's read has returned before the slot may be written again)
+        mbar_arrive_warp(bar(B_UEMPTY + (n & 1)));
+        return true;
+    };
+
+    if (warp == 8) {
+        // ---------------------------------------------------------------- TMA producer
+        if (lane == 0) {
+            auto wait = [&](int b, uint32_t parity, int site) {
+                return wait_or_abort(bar(b), parity, a.err, site, abort_flag);
+            };
+            int x = blockIdx.x, y = 0;
+            int tk = 0, nq = 0, ng = 0;   // K/V tiles, Q tiles, dO and O tiles issued so far
+            bool ok = true, more = true, asked = false;
+            // asked with the unit's last tile: early enough for the answer, and late enough that no CTA
+            // holds a second unit while others run out of work
+            auto ask = [&]() {
+                mbar_arrive_expect_tx(bar(B_NEXT), 16);
+                launch_control_ask(smem_u32(answer), bar(B_NEXT));
+                asked = true;
+            };
+            int n = 0;
+            for (;; ++n) {
+                if (n >= 2 && !wait(B_UEMPTY + (n & 1), ((n >> 1) - 1) & 1, 183)) break;
+                Unit u = {0, 0, 0, 0, 0, 0, 0, -1};
+                if (more) {
+                    const padoc_cross_unit w = a.units[x / a.hkv];
+                    u = {w.tok, w.ntok, w.k0, w.nk, x % a.hkv, w.slot, w.sub, (w.nk + kW - 1) / kW};
+                }
+                units[n & 1] = u;
+                mbar_arrive(bar(B_UFULL + (n & 1)));
+                if (u.steps < 0) break;
+                auto rows = [&](uint8_t *dst, const CUtensorMap *map, int b) {
+#pragma unroll
+                    for (int i = 0; i < 2 * kPanels; ++i)   // [panel][block]
+                        tma_load_3d(smem_u32(dst) + (i >> 1) * kQPanel + (i & 1) * kBlk * 128, map, 64 * (i >> 1), u.g * a.group,
+                                    u.tok + (i & 1) * a.block_tokens, bar(b));
+                };
+                if (n > 0 && !wait(B_QFREE, (n - 1) & 1, 184)) break;
+                mbar_arrive_expect_tx(bar(B_QROWS), 2 * kPanels * used * 128);
+                rows(sq, &qmap, B_QROWS);
+                ++nq;
+                for (int j = 0; j < u.steps; ++j, ++tk) {
+                    if (j + 1 == u.steps) ask();
+                    const int s = tk % kStages;
+                    if (tk >= kStages && !(ok = wait(B_KEMPTY + s, (tk / kStages - 1) & 1, 180))) break;
+                    const int row = u.k0 + j * kW;
+                    const uint32_t fb = bar(B_KFULL + s);
+                    mbar_arrive_expect_tx(fb, 2 * kKTile);
+#pragma unroll
+                    for (int p = 0; p < kPanels; ++p) {
+                        tma_load_2d(smem_u32(sk + s * kKTile) + p * kKPanel, &kmap, u.g * D + 64 * p, row, fb);
+                        tma_load_2d(smem_u32(sv + s * kKTile) + p * kKPanel, &vmap, u.g * D + 64 * p, row, fb);
+                    }
+                    if (j == 0) {   // the first K and V tiles go before dO, whose place is free later
+                        if (n > 0 && !(ok = wait(B_DREAD, (n - 1) & 1, 185) && wait(B_GFREE, (n - 1) & 1, 186))) { ++tk; break; }
+                        mbar_arrive_expect_tx(bar(B_GROWS), 4 * kPanels * used * 128);
+                        rows(sg, &gmap, B_GROWS);
+                        rows(so, &omap, B_GROWS);
+                        ++ng;
+                    }
+                }
+                if (!ok) break;
+                if (!wait(B_NEXT, n & 1, 187)) break;
+                asked = false;
+                more = launch_control_answer(smem_u32(answer), x, y);
+                fence_proxy_async_smem();   // the answer is read before the next one may be written
+            }
+            // copies still in flight must land before the CTA's shared memory is released
+            if (asked) mbar_wait_bounded(bar(B_NEXT), n & 1, a.err, 188);
+            if (nq) mbar_wait_bounded(bar(B_QROWS), (nq - 1) & 1, a.err, 181);
+            if (ng) mbar_wait_bounded(bar(B_GROWS), (ng - 1) & 1, a.err, 181);
+            for (int i = max(tk - kStages, 0); i < tk; ++i)
+                mbar_wait_bounded(bar(B_KFULL + i % kStages), (i / kStages) & 1, a.err, 182);
+        }
+    } else if (warp >= 9) {
+        // ---------------------------------------------------------------- MMA issuers (whole warps)
+        // warp 9 S, warp 11 dP, warp 10 dQ; c counts the steps of all units
+        int c = 0, slot = 0;
+        uint32_t ph = 0;   // parity of the slot's use
+        bool ok = true;
+        auto next_step = [&]() {
+            ++c;
+            if (++slot == kSlots) { slot = 0; ph ^= 1; }
+        };
+        constexpr uint32_t idS = umma_idesc_bf16(128, kW, false), idAcc = umma_idesc_bf16(128, D, true);
+        Unit un;
+        for (int n = 0; ok && (ok = read_unit(n, un, 201)) && un.steps >= 0; ++n) {
+            if (warp == 9) {
+                // S = Q K^T, A from tensor memory
+                ok = wait_w(B_QT, n & 1, 190);
+                for (int u = 0; ok && u < un.steps; ++u, next_step()) {
+                    const int s = c % kStages;
+                    ok = wait_w(B_KFULL + s, (c / kStages) & 1, 191) && (c < kSlots || wait_w(B_ACC + slot, ph ^ 1, 193));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t dk = umma_desc_sw128(smem_u32(sk + s * kKTile), 16, 1024);
+                    if constexpr (D == 128) umma_bf16_ts_k128_warp<kKPanel>(tmem + kColS + 64 * slot, tmem + kColQ, dk, idS);
+                    else umma_bf16_ts_k64_warp(tmem + kColS + 64 * slot, tmem + kColQ, dk, idS);
+                    umma_commit_warp(bar(B_SFULL + slot));
+                }
+            } else if (warp == 11) {
+                // dP = dO V^T, both from shared memory
+                const uint64_t dg = umma_desc_sw128(smem_u32(sg), 16, 1024);
+                ok = wait_w(B_GROWS, n & 1, 197);
+                for (int u = 0; ok && u < un.steps; ++u, next_step()) {
+                    const int s = c % kStages;
+                    ok = wait_w(B_KFULL + s, (c / kStages) & 1, 198) &&
+                         (c < 2 || wait_w(B_DPFREE + (c & 1), ((c >> 1) - 1) & 1, 199));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t dv = umma_desc_sw128(smem_u32(sv + s * kKTile), 16, 1024);
+                    if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kQPanel, kKPanel>(tmem + kColDP + 64 * (c & 1), dg, dv, idS);
+                    else umma_bf16_ss_k64_warp(tmem + kColDP + 64 * (c & 1), dg, dv, idS);
+                    umma_commit_warp(bar(B_SFULL + slot));
+                }
+                umma_commit_warp(bar(B_GFREE));
+            } else {
+                for (int u = 0; ok && u < un.steps; ++u, next_step()) {
+                    const int s = c % kStages;
+                    // (the dQ of the unit before is read before this one's first product overwrites it)
+                    ok = wait_w(B_PFULL + slot, ph, 192) && (u > 0 || n == 0 || wait_w(B_DQFREE, (n - 1) & 1, 202));
+                    if (!ok) break;
+                    tc_fence_after();
+                    // the step's K as an MN-major B operand (N = head dim, K = the 64 keys)
+                    const uint64_t kmn = umma_desc_sw128(smem_u32(sk + s * kKTile), kKPanel, 1024);
+                    umma_bf16_ts_k64_mn_warp<1, slice_col(1), slice_col(2), slice_col(3)>(tmem + kColDQ, tmem + kColS + 64 * slot, kmn,
+                                                                                         idAcc, u > 0);
+                    umma_commit_warp(bar(B_ACC + slot));
+                    umma_commit_warp(bar(B_KEMPTY + s));
+                }
+                umma_commit_warp(bar(B_DQFULL));
+            }
+        }
+        umma_commit_warp(bar(B_FINAL + warp - 9));
+        mbar_wait_bounded(bar(B_FINAL + warp - 9), 0, a.err, 194);
+    } else {
+        // ---------------------------------------------------------------- softmax + epilogue
+        const int lq = warp & 3, ch = warp >> 2;
+        const int row = lq * 32 + lane;
+        const uint32_t lanes = (uint32_t)(lq * 32) << 16;
+        const uint64_t c2 = f2_pack(a.scale_log2, a.scale_log2);
+        int c = 0, slot = 0;   // steps of all units
+        uint32_t ph = 0;
+        Unit un, last = {};
+        int64_t last_at = -1;  // where the last unit's row of dQ goes
+        bool ok = true;
+        for (int n = 0; ok && (ok = read_unit(n, un, 203)); ++n) {
+            int token = 0, head = 0;
+            const bool in = un.steps >= 0 && cross_row(a, un.tok, un.ntok, row, token, head);
+            float nlrow = -INFINITY;
+            if (un.steps >= 0) {
+                if (in) {
+                    const float l = a.lse_in[(size_t)token * a.hq + un.g * a.group + head];
+                    nlrow = l == -INFINITY ? -INFINITY : -l * PADOC_LOG2E;
+                }
+                // Q's row into tensor memory (half of its dims); the S of the unit before that read the last
+                // one are done, as their steps are
+                if (!(ok = wait_w(B_QROWS, n & 1, 200))) break;
+                HalfRow<D>::to_tmem(tmem + lanes + kColQ, sq, ch, row, kQPanel);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_warp(bar(B_QT));
+            }
+            // the unit before's dQ, half of its columns: times scale as bf16 by way of this warp's part of Q's place,
+            // so that neighbouring lanes write a row's bytes, or in fp32 as a part
+            if (n > 0) {
+                if (!(ok = wait_w(B_DQFULL, (n - 1) & 1, 196))) break;
+                tc_fence_after();
+                constexpr int kCols = D / 2;
+                uint32_t o[kCols / 32][32];
+#pragma unroll
+                for (int i = 0; i < kCols / 32; ++i) tmem_ld32(tmem + lanes + kColDQ + kCols * ch + 32 * i, o[i]);
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_warp(bar(B_DQFREE));
+                if (last.slot >= 0) {
+                    const size_t pr = ((size_t)last.slot * a.hkv + last.g) * kQT + row;
+                    auto v = [&](int i) { return __uint_as_float(o[i >> 5][i & 31]); };
+                    if (last_at >= 0)
+#pragma unroll
+                        for (int i = 0; i < kCols; i += 8)
+                            st_global_v8(a.part + pr * D + kCols * ch + i, v(i), v(i + 1), v(i + 2), v(i + 3), v(i + 4), v(i + 5),
+                                         v(i + 6), v(i + 7));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kCols; i += 8) {
+                        auto v = [&](int k) { return __uint_as_float(o[i >> 5][(i & 31) + k]) * a.scale; };
+                        *reinterpret_cast<uint4 *>(sq + HalfRow<D>::offset(ch, row, i / 8, kQPanel)) =
+                            make_uint4(pack_bf16x2(v(0), v(1)), pack_bf16x2(v(2), v(3)), pack_bf16x2(v(4), v(5)), pack_bf16x2(v(6), v(7)));
+                    }
+                    __syncwarp();
+                    constexpr int kPer = D / 16;   // lanes a row
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) {
+                        const int r = i * (32 / kPer) + lane / kPer, k = lane % kPer;
+                        const int64_t to = __shfl_sync(0xffffffffu, last_at, r);
+                        const uint4 w = *reinterpret_cast<const uint4 *>(sq + HalfRow<D>::offset(ch, lq * 32 + r, k, kQPanel));
+                        if (to >= 0) *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.dq + to + kCols * ch + 8 * k) = w;
+                    }
+                    fence_proxy_async_smem();   // (the next unit's Q is copied over what was read)
+                }
+                __syncwarp();
+            }
+            if (un.steps < 0) break;
+            mbar_arrive_warp(bar(B_QFREE));
+            last = un;
+            last_at = in ? (int64_t)token * a.dq_stride + (un.g * a.group + head) * D : -1;
+            // the row's statistics: D = dO . O (fp32, the two column halves added through shared memory) and -lse2;
+            // rows past the segment's get -lse2 = -inf and D = 0, so that the dK/dV pass adds nothing for them
+            if (!(ok = wait_w(B_GROWS, n & 1, 204) && (n == 0 || wait_w(B_DREAD, (n - 1) & 1, 205)))) break;
+            uint64_t acc2 = f2_pack(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < HalfRow<D>::kPieces; ++i) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(sg + HalfRow<D>::offset(ch, row, i, kQPanel));
+                const uint4 w = *reinterpret_cast<const uint4 *>(so + HalfRow<D>::offset(ch, row, i, kQPanel));
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc2 = f2_fma(f2_pack(__uint_as_float(xs[j] << 16), __uint_as_float(xs[j] & 0xffff0000u)),
+                                  f2_pack(__uint_as_float(ws[j] << 16), __uint_as_float(ws[j] & 0xffff0000u)), acc2);
+            }
+            float lo, hi;
+            f2_unpack(acc2, lo, hi);
+            dsum[ch * kQT + row] = lo + hi;
+            __syncwarp();
+            mbar_arrive_warp(bar(B_D));
+            if (!(ok = wait_w(B_D, n & 1, 206))) break;
+            const float drow = in ? dsum[row] + dsum[kQT + row] : 0.f;
+            __syncwarp();
+            mbar_arrive_warp(bar(B_DREAD));
+            if (ch == 0 && un.sub >= 0 && row / kBlk * a.block_tokens < un.ntok) {
+                const size_t at = ((size_t)un.g * a.num_subs + un.sub) * kBlk + row;
+                a.neg_lse2[at] = nlrow;
+                a.dsum[at] = drow;
+            }
+            const uint64_t nl2 = f2_pack(nlrow, nlrow), d2 = f2_pack(drow, drow);
+            for (int u = 0; ok && u < un.steps; ++u, ++c) {
+                const uint32_t b = tmem + lanes + kColS + 64 * slot + 32 * ch;
+                const int left = un.nk - u * kW;   // keys from this step on
+                const bool partial = left < kW;
+                if (!(ok = wait_w(B_SFULL + slot, ph, 195))) break;
+                tc_fence_after();
+                uint32_t sr[32], dr[32];
+                tmem_ld32(b, sr);
+                tmem_ld32(tmem + lanes + kColDP + 64 * (c & 1) + 32 * ch, dr);
+                uint32_t vis = 0xffffffffu;
+                if (partial) {
+                    // K's rows past the end, which dQ's product sums over: zeros (S, which has read them, is done)
+                    vis = interval_bits(0, left, 32 * ch);
+                    uint8_t *kb = sk + c % kStages * kKTile;
+                    for (int i = tid; i < (kW - left) * 8 * kPanels; i += 256)
+                        *reinterpret_cast<uint4 *>(kb + i / 8 / (kW - left) * kKPanel + (left + i / 8 % (kW - left)) * 128 + i % 8 * 16) =
+                            make_uint4(0, 0, 0, 0);
+                    fence_proxy_async_smem();
+                }
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_warp(bar(B_DPFREE + (c & 1)));
+                uint32_t dk[16];
+                // two key columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D)
+                auto column_pairs = [&](auto masked) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        float x0, x1;
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2, nl2), x0, x1);
+                        const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+                        const uint64_t t2 = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])), d2);
+                        float d0, d1;
+                        f2_unpack(f2_mul(f2_pack(p0, p1), t2), d0, d1);
+                        if (decltype(masked)::value) {
+                            d0 = (vis >> i) & 1u ? d0 : 0.f;
+                            d1 = (vis >> (i + 1)) & 1u ? d1 : 0.f;
+                        }
+                        dk[i >> 1] = pack_bf16x2(d0, d1);
+                    }
+                };
+                if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
+                tmem_st16(b, dk);   // over the first half of this thread's own S columns
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_warp(bar(B_PFULL + slot));
+                if (++slot == kSlots) { slot = 0; ph ^= 1; }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+template <int D, int NC>
+padoc_status launch_dkv(const CUtensorMap &qmap, const CUtensorMap &gmap, const padoc_cross_args &a, bool after, cudaStream_t stream)
+{
+    CUtensorMap kmap, vmap;
+    if (!padoc_make_tmap_bf16(&kmap, a.k, (uint64_t)a.hkv * D, a.key_rows, a.k_stride * 2, 64, dkv::kKT) ||
+        !padoc_make_tmap_bf16(&vmap, a.v, (uint64_t)a.hkv * D, a.key_rows, a.v_stride * 2, 64, dkv::kKT))
+        return PADOC_ERR_CUDA;
+    auto kernel = cross_dkv_kernel<D, NC>;
+    if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dkv::smem_bytes<D>())) return st;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)((a.num_tiles + a.tail_tiles) * a.hkv * NC));
+    lc.blockDim = dim3(kThreads);
+    lc.dynamicSmemBytes = dkv::smem_bytes<D>();
+    lc.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = NC;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see the producer's wait
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = after ? 2 : 1;
+    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, qmap, gmap, kmap, vmap, a));
+    return padoc_launch_status();
+}
+
+template <int D>
+padoc_status run(const padoc_cross_args &a, int cluster, cudaStream_t stream)
+{
+    const uint64_t row = (uint64_t)a.hq * D * 2;
+    CUtensorMap qmap, gmap, omap, kmap, vmap;
+    if (!a.num_units) {   // no row sees a key: the key rows' zeros alone, which read nothing
+        CUtensorMap none = {};
+        CUtensorMap kv = {};
+        auto kernel = cross_dkv_kernel<D, 1>;
+        if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dkv::smem_bytes<D>())) return st;
+        if (a.num_tiles + a.tail_tiles)
+            kernel<<<(unsigned)((a.num_tiles + a.tail_tiles) * a.hkv), kThreads, dkv::smem_bytes<D>(), stream>>>(none, none, kv, kv, a);
+        return padoc_launch_status();
+    }
+    if (!padoc_make_tmap_bf16_heads(&qmap, a.q, D, a.hq, a.query_rows, a.q_stride * 2, a.group, a.block_tokens) ||
+        !padoc_make_tmap_bf16_heads(&gmap, a.dout, D, a.hq, a.query_rows, row, a.group, a.block_tokens) ||
+        !padoc_make_tmap_bf16_heads(&omap, a.out, D, a.hq, a.query_rows, row, a.group, a.block_tokens) ||
+        !padoc_make_tmap_bf16(&kmap, a.k, (uint64_t)a.hkv * D, a.key_rows, a.k_stride * 2, 64, dqp::kW) ||
+        !padoc_make_tmap_bf16(&vmap, a.v, (uint64_t)a.hkv * D, a.key_rows, a.v_stride * 2, 64, dqp::kW))
+        return PADOC_ERR_CUDA;
+    auto kernel = cross_dq_kernel<D>;
+    if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dqp::smem_bytes<D>())) return st;
+    kernel<<<(unsigned)(a.num_units * a.hkv), kThreads, dqp::smem_bytes<D>(), stream>>>(qmap, gmap, omap, kmap, vmap, a);
+    const padoc_status st = padoc_launch_status();
+    if (st != PADOC_OK) return st;
+    switch (cluster) {
+        case 8:
+            if constexpr (D == 128) return launch_dkv<D, 8>(qmap, gmap, a, true, stream);
+        case 4: return launch_dkv<D, 4>(qmap, gmap, a, true, stream);
+        case 2: return launch_dkv<D, 2>(qmap, gmap, a, true, stream);
+        default: return launch_dkv<D, 1>(qmap, gmap, a, true, stream);
+    }
+}
+
+}  // namespace
+
+padoc_status padoc_cross_launch_bwd_tc(const padoc_cross_args &args, int head_dim, int cluster, cudaStream_t stream)
+{
+    padoc_cross_args a = args;
+    a.err = padoc_device_error_word();
+    if (!a.err) return PADOC_ERR_CUDA;
+    return head_dim == 64 ? run<64>(a, cluster, stream) : run<128>(a, cluster, stream);
+}

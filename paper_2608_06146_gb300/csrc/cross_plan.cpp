@@ -252,6 +252,22 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
         std::stable_sort(b.tiles.begin(), b.tiles.end(),
                          [](const padoc_cross_key_tile &x, const padoc_cross_key_tile &y) { return x.steps > y.steps; });
         info.num_subs = (int32_t)subs;
+
+        // The CTAs that share a key tile's steps: few tiles seen by many rows leave most of the chip idle, but each
+        // sharing costs its exchange (in steps of 0.8 us).
+        static const float start[] = {6.f, 12.f, 13.f, 16.f};
+        float best = 0.f;
+        for (int i = 0; i < (cfg->head_dim == 128 ? 4 : 3); ++i) {
+            const int nc = 1 << i;
+            std::vector<float> cost;
+            for (const padoc_cross_key_tile &t : b.tiles)
+                if (t.steps) cost.push_back((float)ceil_div(t.steps, nc) + start[i]);
+            const float time = makespan(cost, hkv, std::max(1, lanes / nc));
+            if (i == 0 || time < best) {
+                best = time;
+                info.cluster = nc;
+            }
+        }
     }
     if ((int64_t)std::max(b.units.size(), std::max(b.dq_units.size(), b.tiles.size())) * hkv * 8 > INT32_MAX ||
         (int64_t)std::max(b.merges.size(), b.dq_merges.size()) * hkv * 64 > INT32_MAX)

@@ -210,6 +210,18 @@ __device__ __forceinline__ void umma_bf16_ts_k128_warp(uint32_t d_tmem, uint32_t
         " add.s32 a, %1, 56;\n add.s64 b, %2, %4+6;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n}" ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "n"(PB >> 4)
         : "memory");
 }
+// Four K-steps (64 elements, one panel) of D = A[tmem] . B[smem]^T, B K-major.
+__device__ __forceinline__ void umma_bf16_ts_k64_warp(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc)
+{
+    asm volatile(
+        "{\n .reg .pred e, t, f;\n .reg .b64 b;\n .reg .b32 a;\n elect.sync _|e, 0xffffffff;\n"
+        " setp.eq.u32 t, 0, 0;\n setp.ne.u32 f, 0, 0;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, f;\n"
+        " add.s32 a, %1, 8;\n add.s64 b, %2, 2;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n"
+        " add.s32 a, %1, 16;\n add.s64 b, %2, 4;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n"
+        " add.s32 a, %1, 24;\n add.s64 b, %2, 6;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n}" ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc)
+        : "memory");
+}
 // As umma_commit_warp for MMAs over a CTA pair: arrives on the barrier at this offset in both CTAs.
 __device__ __forceinline__ void umma_commit_pair_warp(uint32_t mbar)
 {

@@ -143,7 +143,7 @@ class padoc_cross_plan(ctypes.Structure):
                 ("num_merges", ctypes.c_int32), ("num_slots", ctypes.c_int32), ("num_dq_units", ctypes.c_int32),
                 ("num_dq_merges", ctypes.c_int32), ("num_dq_slots", ctypes.c_int32), ("num_subs", ctypes.c_int32),
                 ("num_key_tiles", ctypes.c_int32), ("num_covers", ctypes.c_int32), ("max_steps", ctypes.c_int32),
-                ("reserved", ctypes.c_int32), ("pairs", ctypes.c_int64), ("plan_ints", ctypes.c_int64),
+                ("cluster", ctypes.c_int32), ("pairs", ctypes.c_int64), ("plan_ints", ctypes.c_int64),
                 ("off_units", ctypes.c_int64), ("off_merges", ctypes.c_int64), ("off_dq_units", ctypes.c_int64),
                 ("off_dq_merges", ctypes.c_int64), ("off_key_tiles", ctypes.c_int64), ("off_covers", ctypes.c_int64)]
 
