@@ -951,23 +951,28 @@ typedef struct {
     int32_t num_segments;
     int32_t query_rows;      /* query rows the segments reach to (their largest q_begin + q_len) */
     int32_t key_rows;        /* key rows they reach to */
-    int32_t pair;            /* 1: the forward's units are 512 rows for a pair of CTAs, else 256 for one */
-    int32_t num_units;       /* forward: work items, each for every KV head */
-    int32_t num_merges;      /* row blocks whose key range is split over several items (or empty) */
-    int32_t num_slots;       /* partial results, each for every KV head */
+    int32_t pair;            /* 1: the forward's items are 512 packed rows for a pair of CTAs, else 256 for one */
+    int32_t num_units;       /* forward: work items */
+    int32_t num_ctas;        /* CTAs (pairs) that have a list of items each; 0: a CTA an item, taken as SMs get free */
+    int32_t num_merges;      /* row blocks whose key range is split over several items, or empty */
+    int32_t num_slots;       /* partial results */
+    int32_t max_parts;       /* most partial results of one row */
     int32_t num_dq_units;    /* the same of the backward's dq pass */
+    int32_t num_dq_ctas;
     int32_t num_dq_merges;
     int32_t num_dq_slots;
-    int32_t num_subs;        /* blocks of 64 rows whose statistics the backward keeps */
-    int32_t num_key_tiles;   /* backward: key tiles of at most 128 rows, seen by the same segments as a whole */
-    int32_t num_covers;      /* (key interval, segment) pairs */
-    int32_t max_steps;       /* most blocks of 64 rows that see one key tile */
+    int32_t max_dq_parts;
+    int32_t num_subs;        /* blocks of 64 packed rows whose statistics the backward keeps, for each KV head */
+    int32_t num_key_tiles;   /* backward: key tiles of at most 128 rows */
+    int32_t num_covers;      /* (key tile, segment that sees some of it) pairs */
     int32_t cluster;         /* CTAs that share a key tile in the backward */
     int64_t pairs;           /* visible (query row, key row) pairs */
     int64_t plan_ints;       /* int32 words in the plan blob */
     int64_t off_units;       /* offsets (int32 words) of the blob's arrays */
+    int64_t off_ctas;
     int64_t off_merges;
     int64_t off_dq_units;
+    int64_t off_dq_ctas;
     int64_t off_dq_merges;
     int64_t off_key_tiles;
     int64_t off_covers;
@@ -1027,7 +1032,8 @@ typedef struct {
 
 /* Gradients of padoc_cross_attn for an upstream gradient dout [query_rows][Hq][head_dim], with the forward's out and
  * lse: dq of the segments' rows (others are not written), dk and dv of every key row, summed in a fixed order over all
- * segments and query heads that see it (0 where none does). The plan must have been built with cfg.backward. No
+ * segments and query heads that see it (0 where none does). The plan must have been built with cfg.backward. Where
+ * key ranges overlap, a dout that is not finite may reach the gradients of up to 127 keys next to those its row sees. No
  * output overlaps an input or another output. workspace and errors as above. */
 padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const int32_t *plan_dev, const padoc_cross_rows *rows,
                                   const void *out, const void *dout, const float *lse, float scale,

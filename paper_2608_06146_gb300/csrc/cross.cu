@@ -24,45 +24,78 @@ __device__ __forceinline__ void store4(T *p, float4 x)
     }
 }
 
-// A warp per packed row. Parts hold O / l and lse * log2(e), so O = sum_i w_i O_i with w_i = 2^(lse2_i - lse2); dq's
-// are plain sums. Parts are added in their order. Rows without parts (segments without keys) get O = 0, lse = -inf.
-template <typename T, int D, bool kDq>
+// A packed row by one warp, or by the eight of a CTA (W 8: a warp each eighth part) where there are many parts. Parts
+// hold O / l and lse * log2(e), so O = sum_i w_i O_i with w_i = 2^(lse2_i - lse2); dq's are plain sums. The order is
+// fixed. Rows without parts (segments without keys) get O = 0, lse = -inf.
+template <typename T, int D, bool kDq, int W>
 __global__ void __launch_bounds__(256) cross_merge_kernel(const padoc_cross_args a)
 {
     constexpr int kRows = (kDq ? PADOC_CROSS_DQ_BLOCKS : PADOC_CROSS_UNIT_BLOCKS) * PADOC_CROSS_BLOCK;
-    constexpr int kPer = kRows / 8, E = D / 32;
-    const int unit = blockIdx.x / kPer, row = (blockIdx.x % kPer) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const padoc_cross_merge m = a.merges[unit / a.hkv];
-    const int g = unit % a.hkv;
+    constexpr int kPer = kRows * W / 8, E = D / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w0 = W == 8 ? warp : 0;
+    const int row = W == 8 ? blockIdx.x % kPer : (blockIdx.x % kPer) * 8 + warp;
+    const padoc_cross_merge m = a.merges[blockIdx.x / kPer];
     int token, head;
     const bool in = cross_row(a, m.tok, m.ntok, row, token, head);
     pdl_wait_prerequisite();
     if (!in) return;
-    const size_t h = (size_t)token * a.hq + g * a.group + head;
-    float acc[E];
+    const int n = (m.parts - w0 + W - 1) / W;   // this warp's parts: w0, w0 + W, ..
+    auto at = [&](int i) { return (size_t)(m.slot + w0 + i * W) * kRows + row; };
+    float acc[E], top = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    float top = -INFINITY, sum = 0.f;
-    if (!kDq)
-        for (int i = 0; i < m.parts; ++i) top = fmaxf(top, a.part_lse[((size_t)(m.slot + i) * a.hkv + g) * kRows + row]);
-    for (int i = 0; i < m.parts; ++i) {
-        const size_t r = ((size_t)(m.slot + i) * a.hkv + g) * kRows + row;
+    if (!kDq) {
+        for (int i = lane; i < n; i += 32) top = fmaxf(top, a.part_lse[at(i)]);
+#pragma unroll
+        for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+    }
+    for (int i0 = 0; i0 < n; i0 += 32) {
         float w = 1.f;
         if (!kDq) {
-            const float l = a.part_lse[r];
+            const float l = i0 + lane < n ? a.part_lse[at(i0 + lane)] : -INFINITY;
             w = l == -INFINITY ? 0.f : exp2f(l - top);
-            sum += w;
         }
-        const float *p = a.part + r * D + lane * E;
-        float x[E];
-        if constexpr (E == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(p);
-        else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(p);
+        const int k = min(32, n - i0);
+#pragma unroll 4
+        for (int j = 0; j < k; ++j) {
+            const float *p = a.part + at(i0 + j) * D + lane * E;
+            const float wj = kDq ? 1.f : __shfl_sync(0xffffffffu, w, j);
+            float x[E];
+            if constexpr (E == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(p);
+            else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(p);
+            sum += wj;
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(w, x[e], acc[e]);
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(wj, x[e], acc[e]);
+        }
     }
-    float mul = kDq ? a.scale : sum > 0.f ? 1.f / sum : 0.f;
-    if (!kDq && isnan(sum)) mul = sum;
-    T *dst = kDq ? (T *)a.dq + (size_t)token * a.dq_stride + (size_t)(g * a.group + head) * D + lane * E
+    if constexpr (W == 8) {
+        __shared__ float parts[8][D + 2];
+#pragma unroll
+        for (int e = 0; e < E; ++e) parts[warp][lane * E + e] = acc[e];
+        if (lane == 0) {
+            parts[warp][D] = top;
+            parts[warp][D + 1] = sum;
+        }
+        __syncthreads();
+        if (warp) return;
+        float most = -INFINITY;
+        if (!kDq)
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, parts[i][D]);
+        sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float t = parts[i][D], w = kDq ? 1.f : t == -INFINITY ? 0.f : exp2f(t - most);
+            sum = fmaf(w, parts[i][D + 1], sum);
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(w, parts[i][lane * E + e], acc[e]);
+        }
+        top = most;
+    }
+    const float mul = kDq ? a.scale : sum == 0.f ? 0.f : 1.f / sum;
+    const size_t h = (size_t)token * a.hq + m.g * a.group + head;
+    T *dst = kDq ? (T *)a.dq + (size_t)token * a.dq_stride + (size_t)(m.g * a.group + head) * D + lane * E
                  : (T *)a.o + h * D + lane * E;
     if constexpr (E == 4) {
         store4(dst, make_float4(acc[0] * mul, acc[1] * mul, acc[2] * mul, acc[3] * mul));
@@ -70,15 +103,15 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const padoc_cross_args
         if constexpr (sizeof(T) == 4) *reinterpret_cast<float2 *>(dst) = make_float2(acc[0] * mul, acc[1] * mul);
         else *reinterpret_cast<uint32_t *>(dst) = pack_bf16x2(acc[0] * mul, acc[1] * mul);
     }
-    if (!kDq && lane == 0) a.lse[h] = sum > 0.f ? (top + log2f(sum)) * PADOC_LN2 : isnan(sum) ? sum : -INFINITY;
+    if (!kDq && lane == 0) a.lse[h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * PADOC_LN2;
 }
 
-template <typename T, int D, bool kDq>
+template <typename T, int D, bool kDq, int W>
 padoc_status launch_merge(const padoc_cross_args &a, bool pdl, cudaStream_t stream)
 {
-    constexpr int kPer = (kDq ? PADOC_CROSS_DQ_BLOCKS : PADOC_CROSS_UNIT_BLOCKS) * PADOC_CROSS_BLOCK / 8;
+    constexpr int kPer = (kDq ? PADOC_CROSS_DQ_BLOCKS : PADOC_CROSS_UNIT_BLOCKS) * PADOC_CROSS_BLOCK * W / 8;
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)(a.num_merges * a.hkv * kPer));
+    lc.gridDim = dim3((unsigned)(a.num_merges * kPer));
     lc.blockDim = dim3(256);
     lc.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -86,8 +119,15 @@ padoc_status launch_merge(const padoc_cross_args &a, bool pdl, cudaStream_t stre
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = attr;
     lc.numAttrs = pdl ? 1 : 0;
-    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, cross_merge_kernel<T, D, kDq>, a));
+    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, cross_merge_kernel<T, D, kDq, W>, a));
     return padoc_launch_status();
+}
+
+template <typename T, bool kDq>
+padoc_status merge_rows(const padoc_cross_args &a, int head_dim, bool pdl, cudaStream_t stream)
+{
+    if (head_dim == 64) return a.max_parts > 16 ? launch_merge<T, 64, kDq, 8>(a, pdl, stream) : launch_merge<T, 64, kDq, 1>(a, pdl, stream);
+    return a.max_parts > 16 ? launch_merge<T, 128, kDq, 8>(a, pdl, stream) : launch_merge<T, 128, kDq, 1>(a, pdl, stream);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -98,14 +138,7 @@ padoc_status launch_merge(const padoc_cross_args &a, bool pdl, cudaStream_t stre
 
 constexpr int kB = PADOC_CROSS_BLOCK;
 
-template <typename T>
-__device__ __forceinline__ float4 load4(const T *p)
-{
-    if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float4 *>(p);
-    const uint2 w = *reinterpret_cast<const uint2 *>(p);
-    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                       __uint_as_float(w.y & 0xffff0000u));
-}
+__device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 
 template <int D>
 struct Simt {
@@ -114,12 +147,12 @@ struct Simt {
     static constexpr int kTile = kB * P;
 
     // 64 rows of D values; row r at base(r), or zeros where that is null
-    template <typename T, typename F>
+    template <typename F>
     static __device__ __forceinline__ void load(float *dst, F base)
     {
         for (int i = threadIdx.x; i < kB * (D / 4); i += 256) {
             const int r = i / (D / 4), c = i % (D / 4) * 4;
-            const T *p = base(r);
+            const float *p = base(r);
             *reinterpret_cast<float4 *>(dst + r * P + c) = p ? load4(p + c) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
@@ -195,34 +228,34 @@ __device__ __forceinline__ float sum16(float x)
     return x;
 }
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(256) cross_fwd_simt_kernel(const padoc_cross_args a)
 {
     using S = Simt<D>;
     extern __shared__ __align__(16) float sm[];
     float *sq = sm, *sk = sq + S::kTile, *sv = sk + S::kTile, *sp = sv + S::kTile;
     const int unit = blockIdx.x / PADOC_CROSS_UNIT_BLOCKS, blk = blockIdx.x % PADOC_CROSS_UNIT_BLOCKS;
-    const padoc_cross_unit u = a.units[unit / a.hkv];
-    const int g = unit % a.hkv, ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    const padoc_cross_unit u = a.units[unit];
+    const int g = u.g, ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     pdl_launch_dependents();
     if (blk * a.block_tokens >= u.ntok) return;
-    auto heads_row = [&](const void *base, int64_t stride, int r) -> const T * {
+    auto heads_row = [&](const void *base, int64_t stride, int r) -> const float * {
         int token, head;
         if (!cross_row(a, u.tok, u.ntok, blk * kB + r, token, head)) return nullptr;
-        return (const T *)base + (size_t)token * stride + (size_t)(g * a.group + head) * D;
+        return (const float *)base + (size_t)token * stride + (size_t)(g * a.group + head) * D;
     };
-    S::template load<T>(sq, [&](int r) { return heads_row(a.q, a.q_stride, r); });
+    S::load(sq, [&](int r) { return heads_row(a.q, a.q_stride, r); });
     float acc[4][D / 16], m[4], l[4];
     S::zero(acc);
 #pragma unroll
     for (int i = 0; i < 4; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
     for (int j0 = 0; j0 < u.nk; j0 += kB) {
         __syncthreads();
-        auto key_row = [&](const void *base, int64_t stride, int r) -> const T * {
-            return j0 + r < u.nk ? (const T *)base + (size_t)(u.k0 + j0 + r) * stride + (size_t)g * D : nullptr;
+        auto key_row = [&](const void *base, int64_t stride, int r) -> const float * {
+            return j0 + r < u.nk ? (const float *)base + (size_t)(u.k0 + j0 + r) * stride + (size_t)g * D : nullptr;
         };
-        S::template load<T>(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
-        S::template load<T>(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
+        S::load(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
+        S::load(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
         __syncthreads();
         float s[4][4];
         S::dots(sq, sk, s);
@@ -258,11 +291,11 @@ __global__ void __launch_bounds__(256) cross_fwd_simt_kernel(const padoc_cross_a
         if (!cross_row(a, u.tok, u.ntok, r, token, head)) continue;
         const float inv = l[i] == 0.f ? 0.f : 1.f / l[i], lse2 = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
         const size_t h = (size_t)token * a.hq + g * a.group + head;
-        const size_t pr = ((size_t)max(u.slot, 0) * a.hkv + g) * (PADOC_CROSS_UNIT_BLOCKS * kB) + r;
+        const size_t pr = (size_t)max(u.slot, 0) * (PADOC_CROSS_UNIT_BLOCKS * kB) + r;
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) {
             const float4 x = make_float4(acc[i][4 * j] * inv, acc[i][4 * j + 1] * inv, acc[i][4 * j + 2] * inv, acc[i][4 * j + 3] * inv);
-            if (u.slot < 0) store4((T *)a.o + h * D + 64 * j + 4 * tx, x);
+            if (u.slot < 0) store4((float *)a.o + h * D + 64 * j + 4 * tx, x);
             else store4(a.part + pr * D + 64 * j + 4 * tx, x);
         }
         if (tx == 0) {
@@ -273,7 +306,7 @@ __global__ void __launch_bounds__(256) cross_fwd_simt_kernel(const padoc_cross_a
 }
 
 // dQ, and the rows' statistics for the dK/dV pass.
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(256) cross_dq_simt_kernel(const padoc_cross_args a)
 {
     using S = Simt<D>;
@@ -281,18 +314,18 @@ __global__ void __launch_bounds__(256) cross_dq_simt_kernel(const padoc_cross_ar
     float *sq = sm, *sg = sq + S::kTile, *sk = sg + S::kTile, *sv = sk + S::kTile, *sp = sv + S::kTile;
     float *st = sp + kB * S::PS;   // -lse2 and D
     const int unit = blockIdx.x / PADOC_CROSS_DQ_BLOCKS, blk = blockIdx.x % PADOC_CROSS_DQ_BLOCKS;
-    const padoc_cross_unit u = a.units[unit / a.hkv];
-    const int g = unit % a.hkv, ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    const padoc_cross_unit u = a.units[unit];
+    const int g = u.g, ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     if (blk * a.block_tokens >= u.ntok) return;
-    auto heads_row = [&](const void *base, int64_t stride, int r) -> const T * {
+    auto heads_row = [&](const void *base, int64_t stride, int r) -> const float * {
         int token, head;
         if (!cross_row(a, u.tok, u.ntok, blk * kB + r, token, head)) return nullptr;
-        return (const T *)base + (size_t)token * stride + (size_t)(g * a.group + head) * D;
+        return (const float *)base + (size_t)token * stride + (size_t)(g * a.group + head) * D;
     };
-    S::template load<T>(sq, [&](int r) { return heads_row(a.q, a.q_stride, r); });
-    S::template load<T>(sg, [&](int r) { return heads_row(a.dout, (int64_t)a.hq * D, r); });
+    S::load(sq, [&](int r) { return heads_row(a.q, a.q_stride, r); });
+    S::load(sg, [&](int r) { return heads_row(a.dout, (int64_t)a.hq * D, r); });
     for (int r = threadIdx.x >> 5; r < kB; r += 8) {   // a warp per row
-        const T *o = heads_row(a.out, (int64_t)a.hq * D, r), *d = heads_row(a.dout, (int64_t)a.hq * D, r);
+        const float *o = heads_row(a.out, (int64_t)a.hq * D, r), *d = heads_row(a.dout, (int64_t)a.hq * D, r);
         const int c = threadIdx.x & 31;
         float x = 0.f;
         if (o && c < D / 4) {
@@ -318,11 +351,11 @@ __global__ void __launch_bounds__(256) cross_dq_simt_kernel(const padoc_cross_ar
     S::zero(acc);
     for (int j0 = 0; j0 < u.nk; j0 += kB) {
         __syncthreads();
-        auto key_row = [&](const void *base, int64_t stride, int r) -> const T * {
-            return j0 + r < u.nk ? (const T *)base + (size_t)(u.k0 + j0 + r) * stride + (size_t)g * D : nullptr;
+        auto key_row = [&](const void *base, int64_t stride, int r) -> const float * {
+            return j0 + r < u.nk ? (const float *)base + (size_t)(u.k0 + j0 + r) * stride + (size_t)g * D : nullptr;
         };
-        S::template load<T>(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
-        S::template load<T>(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
+        S::load(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
+        S::load(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
         __syncthreads();
         float s[4][4], dp[4][4];
         S::dots(sq, sk, s);
@@ -343,18 +376,18 @@ __global__ void __launch_bounds__(256) cross_dq_simt_kernel(const padoc_cross_ar
         int token, head;
         if (!cross_row(a, u.tok, u.ntok, r, token, head)) continue;
         const float mul = u.slot < 0 ? a.scale : 1.f;
-        const size_t pr = ((size_t)max(u.slot, 0) * a.hkv + g) * (PADOC_CROSS_DQ_BLOCKS * kB) + r;
+        const size_t pr = (size_t)max(u.slot, 0) * (PADOC_CROSS_DQ_BLOCKS * kB) + r;
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) {
             const float4 x = make_float4(acc[i][4 * j] * mul, acc[i][4 * j + 1] * mul, acc[i][4 * j + 2] * mul, acc[i][4 * j + 3] * mul);
-            if (u.slot < 0) store4((T *)a.dq + (size_t)token * a.dq_stride + (size_t)(g * a.group + head) * D + 64 * j + 4 * tx, x);
+            if (u.slot < 0) store4((float *)a.dq + (size_t)token * a.dq_stride + (size_t)(g * a.group + head) * D + 64 * j + 4 * tx, x);
             else store4(a.part + pr * D + 64 * j + 4 * tx, x);
         }
     }
 }
 
 // dK and dV of 64 keys: the sums over every block of rows that sees them, in the covers' order.
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_args a)
 {
     using S = Simt<D>;
@@ -374,23 +407,24 @@ __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_a
     S::zero(ak);
     S::zero(av);
     if (t.steps > 0) {
-        auto key_row = [&](const void *base, int64_t stride, int r) -> const T * {
-            return r < nk ? (const T *)base + (size_t)(k0 + r) * stride + (size_t)g * D : nullptr;
+        auto key_row = [&](const void *base, int64_t stride, int r) -> const float * {
+            return r < nk ? (const float *)base + (size_t)(k0 + r) * stride + (size_t)g * D : nullptr;
         };
-        S::template load<T>(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
-        S::template load<T>(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
+        S::load(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
+        S::load(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
     }
     for (int ci = 0; ci < t.ncover; ++ci) {
         const padoc_cross_cover c = a.covers[t.cover + ci];
+        if (c.k0 >= k0 + nk || c.k0 + c.nk <= k0) continue;
         for (int b = 0; b < c.nsub; ++b) {
-            auto heads_row = [&](const void *base, int64_t stride, int r) -> const T * {
+            auto heads_row = [&](const void *base, int64_t stride, int r) -> const float * {
                 int token, head;
                 if (!cross_row(a, c.tok, c.ntok, b * kB + r, token, head)) return nullptr;
-                return (const T *)base + (size_t)token * stride + (size_t)(g * a.group + head) * D;
+                return (const float *)base + (size_t)token * stride + (size_t)(g * a.group + head) * D;
             };
             __syncthreads();
-            S::template load<T>(sq, [&](int r) { return heads_row(a.q, a.q_stride, r); });
-            S::template load<T>(sg, [&](int r) { return heads_row(a.dout, (int64_t)a.hq * D, r); });
+            S::load(sq, [&](int r) { return heads_row(a.q, a.q_stride, r); });
+            S::load(sg, [&](int r) { return heads_row(a.dout, (int64_t)a.hq * D, r); });
             __syncthreads();
             float s[4][4], dp[4][4];
             S::dots(sk, sq, s);
@@ -402,9 +436,10 @@ __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_a
                 const float l = a.neg_lse2[at + r], d = a.dsum[at + r];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float p = exp2f(fmaf(s[i][j], a.scale_log2, l));   // (rows past the segment's: l = -inf)
+                    const bool sees = k0 + 4 * ty + i >= c.k0 && k0 + 4 * ty + i < c.k0 + c.nk;
+                    const float p = sees ? exp2f(fmaf(s[i][j], a.scale_log2, l)) : 0.f;   // (rows past the segment's: l = -inf)
                     sp[(4 * ty + i) * S::PS + r] = p;
-                    sd[(4 * ty + i) * S::PS + r] = p * (dp[i][j] - d);
+                    sd[(4 * ty + i) * S::PS + r] = sees ? p * (dp[i][j] - d) : 0.f;
                 }
             }
             __syncwarp();
@@ -416,7 +451,7 @@ __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_a
     for (int i = 0; i < 4; ++i) {
         const int r = 4 * ty + i;
         if (r >= nk) continue;
-        T *dk = (T *)a.dk + (size_t)(k0 + r) * a.dk_stride + (size_t)g * D, *dv = (T *)a.dv + (size_t)(k0 + r) * a.dv_stride + (size_t)g * D;
+        float *dk = (float *)a.dk + (size_t)(k0 + r) * a.dk_stride + (size_t)g * D, *dv = (float *)a.dv + (size_t)(k0 + r) * a.dv_stride + (size_t)g * D;
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) {
             store4(dk + 64 * j + 4 * tx, make_float4(ak[i][4 * j] * a.scale, ak[i][4 * j + 1] * a.scale, ak[i][4 * j + 2] * a.scale, ak[i][4 * j + 3] * a.scale));
@@ -425,28 +460,28 @@ __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_a
     }
 }
 
-template <typename T, int D>
+template <int D>
 padoc_status run_fwd_simt(const padoc_cross_args &a, cudaStream_t cs)
 {
     constexpr int bytes = (3 * Simt<D>::kTile + kB * Simt<D>::PS) * 4;
-    auto kernel = cross_fwd_simt_kernel<T, D>;
+    auto kernel = cross_fwd_simt_kernel<D>;
     if (const padoc_status st = padoc_set_max_smem((const void *)kernel, bytes)) return st;
-    kernel<<<(unsigned)(a.num_units * a.hkv * PADOC_CROSS_UNIT_BLOCKS), 256, bytes, cs>>>(a);
+    kernel<<<(unsigned)(a.num_units * PADOC_CROSS_UNIT_BLOCKS), 256, bytes, cs>>>(a);
     return padoc_launch_status();
 }
 
-template <typename T, int D>
+template <int D>
 padoc_status run_bwd_simt(const padoc_cross_args &a, cudaStream_t cs)
 {
     constexpr int dq_bytes = (4 * Simt<D>::kTile + kB * Simt<D>::PS + 2 * kB) * 4;
     constexpr int dkv_bytes = (4 * Simt<D>::kTile + 2 * kB * Simt<D>::PS) * 4;
-    auto dq = cross_dq_simt_kernel<T, D>;
-    auto dkv = cross_dkv_simt_kernel<T, D>;
+    auto dq = cross_dq_simt_kernel<D>;
+    auto dkv = cross_dkv_simt_kernel<D>;
     padoc_status st = padoc_set_max_smem((const void *)dq, dq_bytes);
     if (st == PADOC_OK) st = padoc_set_max_smem((const void *)dkv, dkv_bytes);
     if (st != PADOC_OK) return st;
     if (a.num_units) {
-        dq<<<(unsigned)(a.num_units * a.hkv * PADOC_CROSS_DQ_BLOCKS), 256, dq_bytes, cs>>>(a);
+        dq<<<(unsigned)(a.num_units * PADOC_CROSS_DQ_BLOCKS), 256, dq_bytes, cs>>>(a);
         if ((st = padoc_launch_status()) != PADOC_OK) return st;
     }
     if (a.num_tiles + a.tail_tiles) {
@@ -523,14 +558,6 @@ void fill_args(padoc_cross_args &a, const padoc_cross_plan *info, const padoc_cr
 
 }  // namespace
 
-padoc_status padoc_cross_launch_merge(const padoc_cross_args &a, padoc_dtype dtype, int head_dim, bool dq, bool pdl, cudaStream_t cs)
-{
-#define PADOC_CROSS_MERGE(T, D) (dq ? launch_merge<T, D, true>(a, pdl, cs) : launch_merge<T, D, false>(a, pdl, cs))
-    if (dtype == PADOC_DTYPE_F32) return head_dim == 64 ? PADOC_CROSS_MERGE(float, 64) : PADOC_CROSS_MERGE(float, 128);
-    return head_dim == 64 ? PADOC_CROSS_MERGE(__nv_bfloat16, 64) : PADOC_CROSS_MERGE(__nv_bfloat16, 128);
-#undef PADOC_CROSS_MERGE
-}
-
 extern "C" padoc_status padoc_cross_attn(const padoc_cross_plan *info, const int32_t *plan_dev, const padoc_cross_rows *rows,
                                          float scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
                                          padoc_stream_t stream)
@@ -564,14 +591,19 @@ extern "C" padoc_status padoc_cross_attn(const padoc_cross_plan *info, const int
     a.o = out;
     a.lse = lse;
     a.part = (float *)workspace;
-    a.part_lse = a.part + (size_t)info->num_slots * a.hkv * (PADOC_CROSS_UNIT_BLOCKS * kB) * c.head_dim;
+    a.ctas = info->num_ctas ? plan_dev + info->off_ctas : nullptr;
+    a.num_ctas = info->num_ctas;
+    a.max_parts = info->max_parts;
+    a.part_lse = a.part + (size_t)info->num_slots * (PADOC_CROSS_UNIT_BLOCKS * kB) * c.head_dim;
     cudaStream_t cs = (cudaStream_t)stream;
     if (a.num_units) {
-        if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_fwd_simt<float, 64>(a, cs) : run_fwd_simt<float, 128>(a, cs);
+        if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_fwd_simt<64>(a, cs) : run_fwd_simt<128>(a, cs);
         else st = padoc_cross_launch_tc(a, c.head_dim, info->pair != 0, cs);
         if (st != PADOC_OK) return st;
     }
-    return a.num_merges ? padoc_cross_launch_merge(a, c.dtype, c.head_dim, false, a.num_units > 0, cs) : PADOC_OK;
+    if (!a.num_merges) return PADOC_OK;
+    return c.dtype == PADOC_DTYPE_F32 ? merge_rows<float, false>(a, c.head_dim, a.num_units > 0, cs)
+                                      : merge_rows<__nv_bfloat16, false>(a, c.head_dim, a.num_units > 0, cs);
 }
 
 extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const int32_t *plan_dev, const padoc_cross_rows *rows,
@@ -621,7 +653,10 @@ extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const
     a.merges = (const padoc_cross_merge *)(plan_dev + info->off_dq_merges);
     a.tiles = (const padoc_cross_key_tile *)(plan_dev + info->off_key_tiles);
     a.covers = (const padoc_cross_cover *)(plan_dev + info->off_covers);
+    a.ctas = info->num_dq_ctas ? plan_dev + info->off_dq_ctas : nullptr;
     a.num_units = info->num_dq_units;
+    a.num_ctas = info->num_dq_ctas;
+    a.max_parts = info->max_dq_parts;
     a.num_merges = info->num_dq_merges;
     a.num_tiles = info->num_key_tiles;
     a.num_subs = info->num_subs;
@@ -644,8 +679,10 @@ extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const
     a.dsum = a.neg_lse2 + stats;
     a.part = a.dsum + stats;
     cudaStream_t cs = (cudaStream_t)stream;
-    if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_bwd_simt<float, 64>(a, cs) : run_bwd_simt<float, 128>(a, cs);
+    if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_bwd_simt<64>(a, cs) : run_bwd_simt<128>(a, cs);
     else st = padoc_cross_launch_bwd_tc(a, c.head_dim, info->cluster, cs);
     if (st != PADOC_OK) return st;
-    return a.num_merges ? padoc_cross_launch_merge(a, c.dtype, c.head_dim, true, false, cs) : PADOC_OK;
+    if (!a.num_merges) return PADOC_OK;
+    return c.dtype == PADOC_DTYPE_F32 ? merge_rows<float, true>(a, c.head_dim, false, cs)
+                                      : merge_rows<__nv_bfloat16, true>(a, c.head_dim, false, cs);
 }

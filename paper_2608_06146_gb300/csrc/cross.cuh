@@ -7,6 +7,7 @@
 // Arguments of the forward and of both backward passes.
 struct padoc_cross_args {
     const padoc_cross_unit *units;             // forward or dq items
+    const int32_t *ctas;                       // first item of each CTA's list, and the end; null: an item a CTA
     const padoc_cross_merge *merges;
     const padoc_cross_key_tile *tiles;
     const padoc_cross_cover *covers;
@@ -19,7 +20,7 @@ struct padoc_cross_args {
     float *lse;
     float *part, *part_lse;                    // partial results
     float *neg_lse2, *dsum;                    // -lse * log2(e) and rowsum(dO * O): [Hkv][subs][64]
-    int32_t num_units, num_merges, num_tiles, num_subs;
+    int32_t num_units, num_ctas, num_merges, max_parts, num_tiles, num_subs;
     int32_t tail_begin, tail_tiles;            // key rows that the plan does not reach
     int32_t hq, hkv, group, block_tokens;      // block_tokens: 64 / group
     float scale, scale_log2;
@@ -36,9 +37,6 @@ __device__ __forceinline__ bool cross_row(const padoc_cross_args &a, int tok, in
     return t < a.block_tokens && i < ntok;
 }
 
-// Rows joined from parts, a warp per row: the forward's outputs and log-sum-exps (kDq 0), or dq (1).
-padoc_status padoc_cross_launch_merge(const padoc_cross_args &a, padoc_dtype dtype, int head_dim, bool dq, bool pdl,
-                                      cudaStream_t stream);
 // The forward's units on the tensor cores (cross_tc.cu).
 padoc_status padoc_cross_launch_tc(const padoc_cross_args &args, int head_dim, bool pair, cudaStream_t stream);
 // The backward's passes on the tensor cores (cross_bwd_tc.cu); cluster: CTAs that share a dK/dV unit.

@@ -7,13 +7,13 @@
 //   them (parts are joined by a later kernel). It walks 64-key steps: S = Q K^T (Q in tensor memory), dP = dO V^T (dO in
 //   shared memory), dS as bf16 over S, dQ += dS K. It also writes -lse2 and D of its rows for the other pass. A
 //   running CTA takes over units not yet launched (cluster launch control).
-// dK/dV pass: a unit is a tile of at most 128 keys that the same segments see and a KV head, run by a cluster of 1 to 8
-//   CTAs that share out its steps and add their fp32 sums through distributed shared memory, in rank order. A step is a
+// dK/dV pass: a unit is a tile of at most 128 keys and a KV head, run by a cluster of 1 to 8 CTAs that share out its steps and add their fp32 sums through distributed shared memory, in rank order. A step is a
 //   block of 64 packed rows: S^T = K Q^T, dP^T = V dO^T (V in tensor memory), P^T and dS^T as bf16 over S^T, dV += P^T dO,
 //   dK += dS^T Q. Query heads of the group and the segments that share keys are thus summed in a fixed order.
 //
-// No step needs a mask but the last ones: where a segment's keys (dQ) or rows (dK/dV) end inside a step, the weights
-// past the end become 0 and the operand rows there zeros, because what lies behind may be anything.
+// Masks are needed at ends only: where a segment's keys (dQ) or rows (dK/dV) end inside a step, the weights past the end
+// become 0 and the operand rows there zeros, because what lies behind may be anything; and keys of a tile that the
+// step's segment does not see (key ranges that overlap) get weights 0.
 //
 // A step is bound by its chain S -> softmax -> accumulation -> S more than by its MMAs, so S, dP and the accumulating
 // MMAs are issued by a warp each; P and dS share S's columns, so dP's buffer is free as soon as it is read; waits and
@@ -320,6 +320,9 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             const uint32_t b = (uint32_t)(u & 1) * 64 + 32 * ch;
             const int rows = __shfl_sync(0xffffffffu, st.tokens(a), 0) * a.group;
             const bool partial = rows < used;
+            // keys of the tile that the segment does not see
+            const int key = k0 + lq * 32 + lane;
+            const bool blind = key < st.c.k0 || key >= st.c.k0 + st.c.nk;
             if (!wait_all(B_QFULL + s, (u / kStages) & 1, 171) || !wait_all(B_SFULL + (u & 1), (u >> 1) & 1, 170)) {
                 ok = false;
                 break;
@@ -378,6 +381,13 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 }
             };
             if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
+            if (__any_sync(0xffffffffu, blind)) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    pk[i] = blind ? 0u : pk[i];
+                    dk[i] = blind ? 0u : dk[i];
+                }
+            }
             tmem_st16(tmem + lanes + kColS + b, pk);
             tmem_st16(tmem + lanes + kColS + b + 16, dk);
             tmem_st_wait();
@@ -588,12 +598,17 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             auto wait = [&](int b, uint32_t parity, int site) {
                 return wait_or_abort(bar(b), parity, a.err, site, abort_flag);
             };
-            int x = blockIdx.x, y = 0;
+            int x = blockIdx.x, y = 0, xe = 0;   // items: x and, of a list, those up to xe
+            if (a.ctas) {
+                xe = a.ctas[x + 1];
+                x = a.ctas[x];
+            }
             int tk = 0, nq = 0, ng = 0;   // K/V tiles, Q tiles, dO and O tiles issued so far
             bool ok = true, more = true, asked = false;
             // asked with the unit's last tile: early enough for the answer, and late enough that no CTA
             // holds a second unit while others run out of work
             auto ask = [&]() {
+                if (a.ctas) return;
                 mbar_arrive_expect_tx(bar(B_NEXT), 16);
                 launch_control_ask(smem_u32(answer), bar(B_NEXT));
                 asked = true;
@@ -603,8 +618,8 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 if (n >= 2 && !wait(B_UEMPTY + (n & 1), ((n >> 1) - 1) & 1, 183)) break;
                 Unit u = {0, 0, 0, 0, 0, 0, 0, -1};
                 if (more) {
-                    const padoc_cross_unit w = a.units[x / a.hkv];
-                    u = {w.tok, w.ntok, w.k0, w.nk, x % a.hkv, w.slot, w.sub, (w.nk + kW - 1) / kW};
+                    const padoc_cross_unit w = a.units[x];
+                    u = {w.tok, w.ntok, w.k0, w.nk, w.g, w.slot, w.sub, (w.nk + kW - 1) / kW};
                 }
                 units[n & 1] = u;
                 mbar_arrive(bar(B_UFULL + (n & 1)));
@@ -640,6 +655,10 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     }
                 }
                 if (!ok) break;
+                if (a.ctas) {
+                    more = ++x < xe;
+                    continue;
+                }
                 if (!wait(B_NEXT, n & 1, 187)) break;
                 asked = false;
                 more = launch_control_answer(smem_u32(answer), x, y);
@@ -756,7 +775,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 __syncwarp();
                 mbar_arrive_warp(bar(B_DQFREE));
                 if (last.slot >= 0) {
-                    const size_t pr = ((size_t)last.slot * a.hkv + last.g) * kQT + row;
+                    const size_t pr = (size_t)last.slot * kQT + row;
                     auto v = [&](int i) { return __uint_as_float(o[i >> 5][i & 31]); };
                     if (last_at >= 0)
 #pragma unroll
@@ -923,7 +942,7 @@ padoc_status run(const padoc_cross_args &a, int cluster, cudaStream_t stream)
         return PADOC_ERR_CUDA;
     auto kernel = cross_dq_kernel<D>;
     if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dqp::smem_bytes<D>())) return st;
-    kernel<<<(unsigned)(a.num_units * a.hkv), kThreads, dqp::smem_bytes<D>(), stream>>>(qmap, gmap, omap, kmap, vmap, a);
+    kernel<<<(unsigned)(a.ctas ? a.num_ctas : a.num_units), kThreads, dqp::smem_bytes<D>(), stream>>>(qmap, gmap, omap, kmap, vmap, a);
     const padoc_status st = padoc_launch_status();
     if (st != PADOC_OK) return st;
     switch (cluster) {

@@ -15,27 +15,32 @@
 #define PADOC_CROSS_KEY_TILE 128     // keys of a tile: of the forward's steps and of the dk/dv pass's units
 #define PADOC_CROSS_DQ_STEP 64       // keys of a step of the dq pass
 
-// Forward and dq work item: tokens of one segment over a part of its keys. 32 bytes.
+// Forward and dq work item: tokens of one segment, one KV head, a part of the segment's keys. 32 bytes.
 struct padoc_cross_unit {
     int32_t tok, ntok;    // query rows
     int32_t k0, nk;       // key rows, nk >= 1
+    int32_t g;            // KV head
     int32_t slot;         // partial result, -1: the rows' whole key range, written as the output
     int32_t sub;          // dq: index of the first block in the statistics, -1: another part writes them
-    int32_t pad[2];
+    int32_t pad;
 };
-// Rows joined from parts slot .. slot + parts - 1 (none: a segment without keys).
+// Rows joined from parts slot .. slot + parts - 1 (none: a segment without keys). 32 bytes.
 struct padoc_cross_merge {
-    int32_t tok, ntok, slot, parts;
+    int32_t tok, ntok, slot, parts, g;
+    int32_t pad[3];
 };
-// Key rows that the same segments see: covers cover .. cover + ncover - 1, of `steps` blocks together. 32 bytes.
+// Keys of one or more overlapping ranges, with covers cover .. cover + ncover - 1, of `steps` blocks together. 32 bytes.
 struct padoc_cross_key_tile {
     int32_t k0, nk;
     int32_t cover, ncover;
     int32_t steps;
     int32_t pad[3];
 };
+// A segment that sees keys k0 .. k0 + nk - 1 of the tile: its rows and blocks. 32 bytes.
 struct padoc_cross_cover {
     int32_t tok, ntok, sub, nsub;
+    int32_t k0, nk;
+    int32_t pad[2];
 };
 
 // Blocks of the statistics, lse and D: [Hkv][num_subs][64] floats each.

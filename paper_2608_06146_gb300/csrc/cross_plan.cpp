@@ -1,9 +1,9 @@
 // cross_plan.cpp -- the host planner of cross attention (integers only).
 //
-// Forward: every segment's rows are cut into units of 256 packed rows (512 for CTA pairs), each with the segment's
-// whole key range, or, where that leaves the chip idle, with parts of it whose results are joined. Backward: the dq
-// pass has units of 128 rows cut the same way; the dk/dv pass has key tiles. The key axis is cut at every
-// segment's ends, so that a tile's keys are all seen by the same segments and its steps need no mask.
+// Forward: every segment's rows are cut into chunks of 256 packed rows (512 for CTA pairs), each with the segment's
+// whole key range for every KV head. They are work items as they are, or, where that leaves the chip idle, the sequence
+// of all their steps is cut into runs of equal time, one for each SM, and the parts of a chunk are joined. Backward: the
+// dq pass has chunks of 128 rows cut the same way; the dk/dv pass has key tiles with the segments that see them.
 #include <string.h>
 
 #include <algorithm>
@@ -20,107 +20,151 @@ namespace {
 
 typedef padoc_cross_segment Segment;
 
-// Time of a set of pieces, each run once per KV head, heaviest first on `lanes` SMs (or pairs): the greedy schedule
-// that the hardware's launch order and the kernels' taking over of pending units come close to.
-float makespan(std::vector<float> cost, int hkv, int lanes)
-{
-    if (cost.empty()) return 0.f;
-    std::sort(cost.begin(), cost.end(), std::greater<float>());
-    double total = 0;
-    for (float c : cost) total += c;
-    total *= hkv;
-    if ((double)cost.size() * hkv > 16.0 * lanes) return (float)(total / lanes) + 0.5f * cost[0];
-    std::priority_queue<float, std::vector<float>, std::greater<float>> free;
-    for (int i = 0; i < lanes; ++i) free.push(0.f);
-    float end = 0.f;
-    for (float c : cost)
-        for (int g = 0; g < hkv; ++g) {
-            const float t = free.top() + c;
-            free.pop();
-            free.push(t);
-            end = std::max(end, t);
-        }
-    return end;
-}
-
-// Costs in units of one 128-key step of two 128-row tiles (forward) or one 64-key step of a tile (dq).
+// Costs of a pass, in units of one step of a full item.
 struct Costs {
-    float start;    // a unit's start and end
-    float part;     // ... and what a partial result's traffic adds
+    float start;    // an item's start and end
+    float part;     // what a partial result's traffic adds
     float merge;    // the launch that joins them
-    float half;     // a step of a unit whose second tile is empty (forward)
+    float half;     // a step of an item that is at most half full
+    int32_t step;   // keys of a step
+    int32_t least;  // fewest steps of a piece that is cut off
 };
 
+// Rows of one segment that are worked on together, for every KV head.
 struct Chunk {
-    int32_t tok, ntok, k0, nk, steps;
+    int32_t tok, ntok, k0, nk, steps, sub;
     float step_cost;
 };
 
-struct Cut {
-    int32_t longest;    // most steps of a piece; chunks are cut into equal pieces no longer than this
-    float time;
+struct Work {
+    std::vector<padoc_cross_unit> units;
+    std::vector<padoc_cross_merge> merges;
+    std::vector<int32_t> ctas;   // first item of each CTA's list, and the end; empty: no lists
+    int32_t slots = 0, max_parts = 0;
 };
 
-int32_t pieces_of(const Chunk &c, int32_t longest) { return (c.steps + longest - 1) / longest; }
-
-// The cut with the shortest estimated time: none, or pieces that give each SM one to eight of them.
-Cut choose_cut(const std::vector<Chunk> &chunks, int hkv, int lanes, const Costs &k)
+// Time of items, longest first on `lanes` SMs (or pairs): the greedy schedule that the launch order and the kernels'
+// taking over of pending items come close to.
+float makespan(std::vector<float> cost, int lanes)
 {
-    double work = 0;
-    int32_t most = 1;
-    for (const Chunk &c : chunks) {
-        work += c.steps;
-        most = std::max(most, c.steps);
+    if (cost.empty()) return 0.f;
+    std::sort(cost.begin(), cost.end(), std::greater<float>());
+    if (cost.size() > (size_t)16 * lanes) {
+        double total = 0;
+        for (float c : cost) total += c;
+        return (float)(total / lanes) + 0.5f * cost[0];
     }
-    std::vector<int32_t> tries = {most};
-    static const int waves[] = {1, 2, 3, 4, 6, 8};
-    for (int w : waves) {
-        const int32_t l = (int32_t)std::max(1.0, work * hkv / ((double)lanes * w) + 0.999);
-        if (l < most) tries.push_back(l);
+    std::priority_queue<float, std::vector<float>, std::greater<float>> free;
+    for (int i = 0; i < lanes; ++i) free.push(0.f);
+    float end = 0.f;
+    for (float c : cost) {
+        const float t = free.top() + c;
+        free.pop();
+        free.push(t);
+        end = std::max(end, t);
     }
-    Cut best = {most, 0.f};
-    bool first = true;
-    for (int32_t longest : tries) {
-        std::vector<float> cost;
-        bool split = false;
-        for (const Chunk &c : chunks) {
-            const int32_t n = pieces_of(c, longest);
-            split |= n > 1;
-            for (int32_t i = 0; i < n; ++i) {
-                const int32_t steps = (int32_t)((int64_t)c.steps * (i + 1) / n - (int64_t)c.steps * i / n);
-                cost.push_back((float)steps * c.step_cost + k.start + (n > 1 ? k.part : 0.f));
-            }
-        }
-        const float t = makespan(cost, hkv, lanes) + (split ? k.merge : 0.f);
-        if (first || t < best.time) best = {longest, t};
-        first = false;
-    }
-    return best;
+    return end;
 }
 
-// Units and merges of these chunks, heavier units first.
-void cut_units(const std::vector<Chunk> &chunks, int32_t longest, int32_t step, std::vector<padoc_cross_unit> &units,
-               std::vector<padoc_cross_merge> &merges, int32_t &slots, const std::function<int32_t(size_t)> &sub)
+struct Piece {
+    int32_t chunk, g, first, steps, cta;
+};
+
+// The (chunk, KV head, step) sequence cut into runs of equal time, one for each CTA; false when `lanes` do not suffice
+// for a time of `most` each.
+bool cut_runs(const std::vector<Chunk> &chunks, int hkv, int lanes, const Costs &k, float most, std::vector<Piece> *out)
 {
-    slots = 0;
-    for (size_t i = 0; i < chunks.size(); ++i) {
-        const Chunk &c = chunks[i];
-        const int32_t n = pieces_of(c, longest);
-        if (n > 1) merges.push_back({c.tok, c.ntok, slots, n});
-        for (int32_t p = 0; p < n; ++p) {
-            const int32_t a = (int32_t)((int64_t)c.steps * p / n) * step;
-            const int32_t b = std::min(c.nk, (int32_t)((int64_t)c.steps * (p + 1) / n) * step);
-            units.push_back({c.tok, c.ntok, c.k0 + a, b - a, n > 1 ? slots + p : -1, p == 0 ? sub(i) : -1, {0, 0}});
+    int cta = 0;
+    float used = 0.f;
+    for (size_t c = 0; c < chunks.size(); ++c)
+        for (int32_t g = 0; g < hkv; ++g)
+            for (int32_t at = 0; at < chunks[c].steps;) {
+                const Chunk &ch = chunks[c];
+                const int32_t rem = ch.steps - at;
+                const float whole = used + k.start + (at ? k.part : 0.f) + rem * ch.step_cost;
+                int32_t take = rem;
+                if (whole > most) {
+                    take = (int32_t)((most - used - k.start - k.part) / ch.step_cost);
+                    take = std::min(take, rem - std::min(rem, k.least));   // (what is left is a piece, too)
+                    if (take < std::min(k.least, rem)) {
+                        if (used == 0.f) return false;
+                        ++cta;
+                        used = 0.f;
+                        if (cta >= lanes) return false;
+                        continue;
+                    }
+                }
+                if (out) out->push_back({(int32_t)c, g, at, take, cta});
+                used += k.start + (take < ch.steps ? k.part : 0.f) + take * ch.step_cost;
+                at += take;
+            }
+    return true;
+}
+
+void make_work(const std::vector<Chunk> &chunks, const std::vector<Piece> &pieces, const Costs &k, Work &w)
+{
+    for (size_t i = 0; i < pieces.size();) {
+        size_t n = i + 1;
+        while (n < pieces.size() && pieces[n].chunk == pieces[i].chunk && pieces[n].g == pieces[i].g) ++n;
+        const Chunk &c = chunks[pieces[i].chunk];
+        const int32_t parts = (int32_t)(n - i);
+        if (parts > 1) w.merges.push_back({c.tok, c.ntok, w.slots, parts, pieces[i].g, {0, 0, 0}});
+        w.max_parts = std::max(w.max_parts, parts > 1 ? parts : 0);
+        for (size_t p = i; p < n; ++p) {
+            const int32_t a = pieces[p].first * k.step, b = std::min(c.nk, (pieces[p].first + pieces[p].steps) * k.step);
+            w.units.push_back({c.tok, c.ntok, c.k0 + a, b - a, pieces[p].g, parts > 1 ? w.slots + (int32_t)(p - i) : -1,
+                               p == i ? c.sub : -1, 0});
         }
-        if (n > 1) slots += n;
+        if (parts > 1) w.slots += parts;
+        i = n;
     }
-    std::stable_sort(units.begin(), units.end(),
+}
+
+// The items of a pass: whole chunks, taken as SMs get free, or, where that leaves the chip idle, equal runs of the
+// sequence of all steps, a list for each CTA, with chunks cut where a run ends. `lists` false (fp32, whose kernels
+// run a CTA per 64 rows): the runs' pieces without the lists.
+float plan_work(const std::vector<Chunk> &chunks, int hkv, int lanes, const Costs &k, bool lists, Work &w)
+{
+    std::vector<float> cost;
+    std::vector<Piece> whole;
+    double total = 0;
+    float longest = 0.f;
+    for (size_t c = 0; c < chunks.size(); ++c)
+        for (int32_t g = 0; g < hkv; ++g) {
+            cost.push_back(chunks[c].steps * chunks[c].step_cost + k.start);
+            whole.push_back({(int32_t)c, g, 0, chunks[c].steps, 0});
+            total += cost.back();
+            longest = std::max(longest, cost.back());
+        }
+    if (chunks.empty()) return 0.f;
+    const float plain = makespan(cost, lanes);
+    float lo = (float)(total / lanes), hi = std::max(longest, 2.f * lo) + 4.f * (k.start + k.part);
+    if (cut_runs(chunks, hkv, lanes, k, hi, nullptr) && lo + k.merge < 0.97f * plain) {
+        for (int i = 0; i < 16 && hi - lo > 0.01f * hi; ++i) {
+            const float mid = 0.5f * (lo + hi);
+            (cut_runs(chunks, hkv, lanes, k, mid, nullptr) ? hi : lo) = mid;
+        }
+        std::vector<Piece> pieces;
+        cut_runs(chunks, hkv, lanes, k, hi, &pieces);
+        const bool split = pieces.size() > whole.size();
+        if (hi + (split ? k.merge : 0.f) < 0.97f * plain) {
+            make_work(chunks, pieces, k, w);
+            if (lists) {
+                for (size_t i = 0; i < pieces.size(); ++i)
+                    while ((int32_t)w.ctas.size() <= pieces[i].cta) w.ctas.push_back((int32_t)i);
+                w.ctas.push_back((int32_t)pieces.size());
+            }
+            return hi + (split ? k.merge : 0.f);
+        }
+    }
+    make_work(chunks, whole, k, w);
+    std::stable_sort(w.units.begin(), w.units.end(),
                      [](const padoc_cross_unit &x, const padoc_cross_unit &y) { return x.nk > y.nk; });
+    return plain;
 }
 
 struct Built {
-    std::vector<padoc_cross_unit> units, dq_units;
-    std::vector<padoc_cross_merge> merges, dq_merges;
+    Work fwd, dq;
     std::vector<padoc_cross_key_tile> tiles;
     std::vector<padoc_cross_cover> covers;
     padoc_cross_plan info;
@@ -178,16 +222,15 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
     // blocks, and steps over them, are counted in 32 bits on the device
     if (blocks * hkv > (int64_t)1 << 24 || k_end > (int64_t)1 << 29) return PADOC_ERR_UNSUPPORTED;
 
-    auto chunks_of = [&](int32_t unit_blocks, int32_t step, float half, std::vector<int32_t> *sub) {
+    auto chunks_of = [&](int32_t unit_blocks, const Costs &k) {
         std::vector<Chunk> c;
         const int32_t per = unit_blocks * block;
         for (int32_t i = 0; i < n; ++i) {
             if (seg[i].q_len == 0 || seg[i].k_len == 0) continue;
             for (int32_t t = 0; t < seg[i].q_len; t += per) {
                 const int32_t m = std::min(per, seg[i].q_len - t);
-                c.push_back({seg[i].q_begin + t, m, seg[i].k_begin, seg[i].k_len, ceil_div(seg[i].k_len, step),
-                             m <= per / 2 ? half : 1.f});
-                if (sub) sub->push_back(first_sub[i] + t / block);
+                c.push_back({seg[i].q_begin + t, m, seg[i].k_begin, seg[i].k_len, ceil_div(seg[i].k_len, k.step),
+                             first_sub[i] + t / block, m <= per / 2 ? k.half : 1.f});
             }
         }
         return c;
@@ -197,57 +240,53 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
         for (int32_t i = 0; i < n; ++i)
             if (seg[i].k_len == 0)
                 for (int32_t t = 0; t < seg[i].q_len; t += per)
-                    merges.push_back({seg[i].q_begin + t, std::min(per, seg[i].q_len - t), 0, 0});
+                    for (int32_t g = 0; g < hkv; ++g)
+                        merges.push_back({seg[i].q_begin + t, std::min(per, seg[i].q_len - t), 0, 0, g, {0, 0, 0}});
     };
+    const bool lists = cfg->dtype == PADOC_DTYPE_BF16;
 
-    // forward (a step of two tiles lasts about 1.5 us)
-    const Costs fwd = {1.5f, 0.5f, 2.0f, 0.65f};
-    std::vector<Chunk> chunks = chunks_of(PADOC_CROSS_UNIT_BLOCKS, PADOC_CROSS_KEY_TILE, fwd.half, nullptr);
-    Cut cut = choose_cut(chunks, hkv, lanes, fwd);
-    b.info.pair = 0;
-    cut_units(chunks, cut.longest, PADOC_CROSS_KEY_TILE, b.units, b.merges, info.num_slots, [](size_t) { return -1; });
-    empty_rows(PADOC_CROSS_UNIT_BLOCKS, b.merges);
+    // forward (a step of two 128-row tiles lasts about 1.6 us)
+    const Costs fwd = {1.5f, 0.5f, 2.0f, 0.65f, PADOC_CROSS_KEY_TILE, 1};
+    plan_work(chunks_of(PADOC_CROSS_UNIT_BLOCKS, fwd), hkv, lanes, fwd, lists, b.fwd);
+    empty_rows(PADOC_CROSS_UNIT_BLOCKS, b.fwd.merges);
 
     if (cfg->backward) {
-        const Costs bwd = {6.f, 1.f, 4.f, 1.f};   // (a step of a tile lasts about 0.55 us)
-        std::vector<int32_t> sub;
-        chunks = chunks_of(PADOC_CROSS_DQ_BLOCKS, PADOC_CROSS_DQ_STEP, 1.f, &sub);
-        cut = choose_cut(chunks, hkv, lanes, bwd);
-        cut_units(chunks, cut.longest, PADOC_CROSS_DQ_STEP, b.dq_units, b.dq_merges, info.num_dq_slots,
-                  [&](size_t i) { return sub[i]; });
-        empty_rows(PADOC_CROSS_DQ_BLOCKS, b.dq_merges);
+        const Costs bwd = {6.f, 1.f, 4.f, 1.f, PADOC_CROSS_DQ_STEP, 4};   // (a step of a tile lasts about 0.55 us)
+        plan_work(chunks_of(PADOC_CROSS_DQ_BLOCKS, bwd), hkv, lanes, bwd, lists, b.dq);
+        empty_rows(PADOC_CROSS_DQ_BLOCKS, b.dq.merges);
 
-        // key intervals between neighbouring ends of the segments' key ranges
-        std::vector<int32_t> ends = {0};
+        // Key tiles: ranges that overlap are tiled together, from the first one's begin; between them lie keys that
+        // nobody sees.
         std::vector<int32_t> order;   // segments by their first key
         for (int32_t i = 0; i < n; ++i)
-            if (seg[i].q_len && seg[i].k_len) {
-                ends.push_back(seg[i].k_begin);
-                ends.push_back(seg[i].k_begin + seg[i].k_len);
-                order.push_back(i);
-            }
-        std::sort(ends.begin(), ends.end());
-        ends.erase(std::unique(ends.begin(), ends.end()), ends.end());
+            if (seg[i].q_len && seg[i].k_len) order.push_back(i);
         std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return seg[x].k_begin < seg[y].k_begin; });
-        std::vector<int32_t> live;   // segments that see the interval, in their own order
+        std::vector<int32_t> live;    // segments that may see the tile, in their own order
+        auto end_of = [&](int32_t i) { return seg[i].k_begin + seg[i].k_len; };
         size_t next = 0;
-        for (size_t e = 0; e + 1 < ends.size(); ++e) {
-            const int32_t k0 = ends[e], k1 = ends[e + 1];
-            live.erase(std::remove_if(live.begin(), live.end(), [&](int32_t i) { return seg[i].k_begin + seg[i].k_len <= k0; }),
-                       live.end());
-            for (; next < order.size() && seg[order[next]].k_begin <= k0; ++next)
+        auto add_tile = [&](int32_t k0, int32_t k1) {
+            live.erase(std::remove_if(live.begin(), live.end(), [&](int32_t i) { return end_of(i) <= k0; }), live.end());
+            for (; next < order.size() && seg[order[next]].k_begin < k1; ++next)
                 live.insert(std::lower_bound(live.begin(), live.end(), order[next]), order[next]);
-            const int32_t cover = (int32_t)b.covers.size();
             int64_t steps = 0;
+            const int32_t cover = (int32_t)b.covers.size();
             for (int32_t i : live) {
-                const int32_t m = ceil_div(seg[i].q_len, block);
-                b.covers.push_back({seg[i].q_begin, seg[i].q_len, first_sub[i], m});
+                const int32_t m = ceil_div(seg[i].q_len, block), c0 = std::max(k0, seg[i].k_begin);
+                b.covers.push_back({seg[i].q_begin, seg[i].q_len, first_sub[i], m, c0, std::min(k1, end_of(i)) - c0, {0, 0}});
                 steps += m;
             }
-            if (b.covers.size() > (size_t)1 << 24) return PADOC_ERR_UNSUPPORTED;
-            for (int32_t k = k0; k < k1; k += PADOC_CROSS_KEY_TILE)
-                b.tiles.push_back({k, std::min(PADOC_CROSS_KEY_TILE, k1 - k), cover, (int32_t)live.size(), (int32_t)steps, {0, 0, 0}});
-            info.max_steps = std::max(info.max_steps, (int32_t)steps);
+            b.tiles.push_back({k0, k1 - k0, cover, (int32_t)live.size(), (int32_t)steps, {0, 0, 0}});
+        };
+        int32_t at = 0;               // keys tiled so far
+        for (size_t i = 0; i < order.size();) {
+            const int32_t begin = seg[order[i]].k_begin;
+            int32_t end = end_of(order[i]);
+            for (++i; i < order.size() && seg[order[i]].k_begin < end; ++i) end = std::max(end, end_of(order[i]));
+            for (; at < begin; at = std::min(begin, at + PADOC_CROSS_KEY_TILE)) add_tile(at, std::min(begin, at + PADOC_CROSS_KEY_TILE));
+            for (; at < end; at = std::min(end, at + PADOC_CROSS_KEY_TILE)) {
+                add_tile(at, std::min(end, at + PADOC_CROSS_KEY_TILE));
+                if (b.covers.size() > (size_t)1 << 24) return PADOC_ERR_UNSUPPORTED;
+            }
         }
         std::stable_sort(b.tiles.begin(), b.tiles.end(),
                          [](const padoc_cross_key_tile &x, const padoc_cross_key_tile &y) { return x.steps > y.steps; });
@@ -261,16 +300,16 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
             const int nc = 1 << i;
             std::vector<float> cost;
             for (const padoc_cross_key_tile &t : b.tiles)
-                if (t.steps) cost.push_back((float)ceil_div(t.steps, nc) + start[i]);
-            const float time = makespan(cost, hkv, std::max(1, lanes / nc));
+                for (int32_t g = 0; g < hkv && t.steps; ++g) cost.push_back((float)ceil_div(t.steps, nc) + start[i]);
+            const float time = makespan(cost, std::max(1, lanes / nc));
             if (i == 0 || time < best) {
                 best = time;
                 info.cluster = nc;
             }
         }
     }
-    if ((int64_t)std::max(b.units.size(), std::max(b.dq_units.size(), b.tiles.size())) * hkv * 8 > INT32_MAX ||
-        (int64_t)std::max(b.merges.size(), b.dq_merges.size()) * hkv * 64 > INT32_MAX)
+    if ((int64_t)std::max(b.fwd.units.size(), b.dq.units.size()) * 4 > INT32_MAX || (int64_t)b.tiles.size() * hkv * 8 > INT32_MAX ||
+        (int64_t)std::max(b.fwd.merges.size(), b.dq.merges.size()) * 512 > INT32_MAX)
         return PADOC_ERR_UNSUPPORTED;   // (grid sizes)
 
     int64_t at = 0;
@@ -279,16 +318,24 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
         at += (int64_t)(items * bytes / 4 + 31) / 32 * 32;
         return off;
     };
-    info.num_units = (int32_t)b.units.size();
-    info.num_merges = (int32_t)b.merges.size();
-    info.num_dq_units = (int32_t)b.dq_units.size();
-    info.num_dq_merges = (int32_t)b.dq_merges.size();
+    info.num_units = (int32_t)b.fwd.units.size();
+    info.num_ctas = b.fwd.ctas.empty() ? 0 : (int32_t)b.fwd.ctas.size() - 1;
+    info.num_merges = (int32_t)b.fwd.merges.size();
+    info.num_slots = b.fwd.slots;
+    info.max_parts = b.fwd.max_parts;
+    info.num_dq_units = (int32_t)b.dq.units.size();
+    info.num_dq_ctas = b.dq.ctas.empty() ? 0 : (int32_t)b.dq.ctas.size() - 1;
+    info.num_dq_merges = (int32_t)b.dq.merges.size();
+    info.num_dq_slots = b.dq.slots;
+    info.max_dq_parts = b.dq.max_parts;
     info.num_key_tiles = (int32_t)b.tiles.size();
     info.num_covers = (int32_t)b.covers.size();
-    info.off_units = place(b.units.size(), sizeof(padoc_cross_unit));
-    info.off_merges = place(b.merges.size(), sizeof(padoc_cross_merge));
-    info.off_dq_units = place(b.dq_units.size(), sizeof(padoc_cross_unit));
-    info.off_dq_merges = place(b.dq_merges.size(), sizeof(padoc_cross_merge));
+    info.off_units = place(b.fwd.units.size(), sizeof(padoc_cross_unit));
+    info.off_ctas = place(b.fwd.ctas.size(), sizeof(int32_t));
+    info.off_merges = place(b.fwd.merges.size(), sizeof(padoc_cross_merge));
+    info.off_dq_units = place(b.dq.units.size(), sizeof(padoc_cross_unit));
+    info.off_dq_ctas = place(b.dq.ctas.size(), sizeof(int32_t));
+    info.off_dq_merges = place(b.dq.merges.size(), sizeof(padoc_cross_merge));
     info.off_key_tiles = place(b.tiles.size(), sizeof(padoc_cross_key_tile));
     info.off_covers = place(b.covers.size(), sizeof(padoc_cross_cover));
     info.plan_ints = at;
@@ -332,10 +379,12 @@ extern "C" padoc_status padoc_build_cross_plan(const padoc_cross_segment *segmen
     auto put = [&](int64_t off, const void *src, size_t bytes) {
         if (bytes) memcpy(plan + off, src, bytes);
     };
-    put(b.info.off_units, b.units.data(), b.units.size() * sizeof(padoc_cross_unit));
-    put(b.info.off_merges, b.merges.data(), b.merges.size() * sizeof(padoc_cross_merge));
-    put(b.info.off_dq_units, b.dq_units.data(), b.dq_units.size() * sizeof(padoc_cross_unit));
-    put(b.info.off_dq_merges, b.dq_merges.data(), b.dq_merges.size() * sizeof(padoc_cross_merge));
+    put(b.info.off_units, b.fwd.units.data(), b.fwd.units.size() * sizeof(padoc_cross_unit));
+    put(b.info.off_ctas, b.fwd.ctas.data(), b.fwd.ctas.size() * sizeof(int32_t));
+    put(b.info.off_merges, b.fwd.merges.data(), b.fwd.merges.size() * sizeof(padoc_cross_merge));
+    put(b.info.off_dq_units, b.dq.units.data(), b.dq.units.size() * sizeof(padoc_cross_unit));
+    put(b.info.off_dq_ctas, b.dq.ctas.data(), b.dq.ctas.size() * sizeof(int32_t));
+    put(b.info.off_dq_merges, b.dq.merges.data(), b.dq.merges.size() * sizeof(padoc_cross_merge));
     put(b.info.off_key_tiles, b.tiles.data(), b.tiles.size() * sizeof(padoc_cross_key_tile));
     put(b.info.off_covers, b.covers.data(), b.covers.size() * sizeof(padoc_cross_cover));
     *info = b.info;
@@ -345,8 +394,8 @@ extern "C" padoc_status padoc_build_cross_plan(const padoc_cross_segment *segmen
 extern "C" padoc_status padoc_cross_workspace_size(const padoc_cross_plan *info, size_t *bytes)
 {
     if (!info || !bytes || info->num_slots < 0) return PADOC_ERR_INVALID_ARGUMENT;
-    // partial outputs [slots][Hkv][256][d] and their log-sum-exps [slots][Hkv][256], fp32
-    const size_t rows = (size_t)info->num_slots * info->cfg.num_kv_heads * (PADOC_CROSS_UNIT_BLOCKS * PADOC_CROSS_BLOCK);
+    // partial outputs [slots][256][d] and their log-sum-exps [slots][256], fp32
+    const size_t rows = (size_t)info->num_slots * (PADOC_CROSS_UNIT_BLOCKS * PADOC_CROSS_BLOCK);
     *bytes = rows * (info->cfg.head_dim + 1) * sizeof(float);
     return PADOC_OK;
 }
@@ -354,9 +403,9 @@ extern "C" padoc_status padoc_cross_workspace_size(const padoc_cross_plan *info,
 extern "C" padoc_status padoc_cross_bwd_workspace_size(const padoc_cross_plan *info, size_t *bytes)
 {
     if (!info || !bytes || !info->cfg.backward || info->num_dq_slots < 0 || info->num_subs < 0) return PADOC_ERR_INVALID_ARGUMENT;
-    // -lse2 and D, [Hkv][subs][64] each, then partial dq [slots][Hkv][128][d], fp32
+    // -lse2 and D, [Hkv][subs][64] each, then partial dq [slots][128][d], fp32
     const size_t stats = (size_t)info->num_subs * info->cfg.num_kv_heads * PADOC_CROSS_BLOCK;
-    const size_t rows = (size_t)info->num_dq_slots * info->cfg.num_kv_heads * (PADOC_CROSS_DQ_BLOCKS * PADOC_CROSS_BLOCK);
+    const size_t rows = (size_t)info->num_dq_slots * (PADOC_CROSS_DQ_BLOCKS * PADOC_CROSS_BLOCK);
     *bytes = (2 * stats + rows * info->cfg.head_dim) * sizeof(float);
     return PADOC_OK;
 }

@@ -13,8 +13,8 @@
 // grown by more than 2^8 since the last time, which keeps P <= 256.
 //
 // The grid has one CTA (pair) per unit, most keys first; a running one takes over units not yet launched (cluster
-// launch control), and the next unit's queries and first scores come under the last one's output. A unit of at most
-// 128 rows is run by tile 0's warps alone.
+// launch control). Where the planner cut the steps into equal runs, each CTA has a list of units. The next unit's
+// queries and first scores come under the last one's output. A unit of at most 128 rows is run by tile 0's warps alone.
 // Every wait is bounded; a wait that runs out records an error, all roles leave their loops, the issuers wait for
 // their MMAs, the producer for its copies, and tensor memory is released.
 #include <math.h>
@@ -182,13 +182,18 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 if (CG == 2) tma_load_2d_pair(smem_u32(dst), map, x, y, lead_bar(b));
                 else tma_load_2d(smem_u32(dst), map, x, y, bar(b));
             };
-            int x = (int)blockIdx.x / CG;
+            // items: x and, of a list, those up to xe
+            int x = (int)blockIdx.x / CG, xe = 0;
+            if (a.ctas) {
+                xe = a.ctas[x + 1];
+                x = a.ctas[x];
+            }
             int tk = 0, nq[2] = {0, 0}, tails = 0;   // K and V tiles, queries per tile, V tails issued so far
             bool ok = true, more = true, asked = false;
             // asked with the unit's last tile, a few tiles ahead of the MMAs: early enough for the answer,
             // and late enough that no CTA holds a second unit while others run out of work
             auto ask = [&]() {
-                if (rank != 0) return;
+                if (rank != 0 || a.ctas) return;
                 mbar_arrive_expect_tx(bar(C::B_NEXT), 16);
                 launch_control_ask(smem_u32(answer), bar(C::B_NEXT));
                 asked = true;
@@ -215,12 +220,12 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 if (rank == 0) {
                     if (n >= 2 && !wait(C::B_UEMPTY + (n & 1), ((n >> 1) - 1) & 1, 124)) break;
                     if (more) {
-                        const padoc_cross_unit w = a.units[x / a.hkv];
+                        const padoc_cross_unit w = a.units[x];
                         u.tok = w.tok;
                         u.ntok = w.ntok;
                         u.k0 = w.k0;
                         u.nk = w.nk;
-                        u.g = x % a.hkv;
+                        u.g = w.g;
                         u.slot = w.slot;
                         u.tiles = (w.nk + kKT - 1) / kKT;
                         u.two = CG == 2 || w.ntok > tile_tokens;
@@ -275,6 +280,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     // Only now may the first CTA write this slot of ours again (it does two units on): with
                     // cluster scope, so that its stores come after the reads above.
                     mbar_arrive_cluster<true>(lead_bar(C::B_UEMPTY + (n & 1)));
+                } else if (a.ctas) {
+                    more = ++x < xe;
                 } else {
                     if (!wait(C::B_NEXT, asks & 1, 126)) break;
                     ++asks;
@@ -413,6 +420,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             const Unit u = next;
             int token, head;
             const bool in = cross_row(a, u.tok, u.ntok, (2 * (int)rank + hi) * 128 + row, token, head);
+            const bool idle = !__any_sync(0xffffffffu, in);   // a warp without rows only keeps the others' pace
             float m_ref = -INFINITY, l = 0.f;   // m_ref in raw score units
             for (int j = 0; j < u.tiles; ++j, ++t_tile, ++ring) {
                 const int left = u.nk - j * kKT;   // keys from this tile on
@@ -421,72 +429,74 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     const uint32_t tB = tS + 64 * half;
                     if (!wait_all(C::B_SFULL + 2 * hi + half, t_tile & 1, 140)) { ok = false; break; }
                     tc_fence_after();
-                    // the row's scores are read from tensor memory once and stay in registers
-                    uint32_t sr[2][32];
-                    tmem_ld32(tB, sr[0]);
-                    tmem_ld32(tB + 32, sr[1]);
-                    tmem_ld_wait();
-                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    if (!idle) {
+                        // the row's scores are read from tensor memory once and stay in registers
+                        uint32_t sr[2][32];
+                        tmem_ld32(tB, sr[0]);
+                        tmem_ld32(tB + 32, sr[1]);
+                        tmem_ld_wait();
+                        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int base = 64 * half + 32 * q;
-                        if (left < base + 32) {
-                            const uint32_t vis = interval_bits(0, left, base);
+                        for (int q = 0; q < 2; ++q) {
+                            const int base = 64 * half + 32 * q;
+                            if (left < base + 32) {
+                                const uint32_t vis = interval_bits(0, left, base);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) sr[q][i] = (vis >> i) & 1u ? sr[q][i] : 0xff800000u;   // -inf
+                                for (int i = 0; i < 32; ++i) sr[q][i] = (vis >> i) & 1u ? sr[q][i] : 0xff800000u;   // -inf
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; i += 8) {
+                                mx4[0] = fmax3f(mx4[0], __uint_as_float(sr[q][i]), __uint_as_float(sr[q][i + 1]));
+                                mx4[1] = fmax3f(mx4[1], __uint_as_float(sr[q][i + 2]), __uint_as_float(sr[q][i + 3]));
+                                mx4[2] = fmax3f(mx4[2], __uint_as_float(sr[q][i + 4]), __uint_as_float(sr[q][i + 5]));
+                                mx4[3] = fmax3f(mx4[3], __uint_as_float(sr[q][i + 6]), __uint_as_float(sr[q][i + 7]));
+                            }
                         }
-#pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            mx4[0] = fmax3f(mx4[0], __uint_as_float(sr[q][i]), __uint_as_float(sr[q][i + 1]));
-                            mx4[1] = fmax3f(mx4[1], __uint_as_float(sr[q][i + 2]), __uint_as_float(sr[q][i + 3]));
-                            mx4[2] = fmax3f(mx4[2], __uint_as_float(sr[q][i + 4]), __uint_as_float(sr[q][i + 5]));
-                            mx4[3] = fmax3f(mx4[3], __uint_as_float(sr[q][i + 6]), __uint_as_float(sr[q][i + 7]));
-                        }
-                    }
-                    const float mx = fmaxf(fmax3f(mx4[0], mx4[1], mx4[2]), mx4[3]);
-                    const float m_new = fmaxf(m_ref, mx);
-                    // a row with nothing accumulated yet (O holds zeros) adopts the new maximum directly;
-                    // otherwise the reference only moves when the maximum grew by more than 2^8
-                    const bool rescale = m_ref != -INFINITY && (m_new - m_ref) * c > 8.f;
-                    if (m_ref == -INFINITY) m_ref = m_new;
-                    if (__any_sync(0xffffffffu, rescale)) {
-                        // O_i is quiescent once the previous half's PV is done: the next one waits for this P
-                        // (the one before that was done before this half's S)
-                        if (!wait_all(C::B_PVDONE + 2 * hi + (half ^ 1), (half ? t_tile : t_tile - 1) & 1, 141)) { ok = false; break; }
-                        tc_fence_after();
-                        const float alpha = rescale ? fast_exp2((m_ref - m_new) * c) : 1.f;
+                        const float mx = fmaxf(fmax3f(mx4[0], mx4[1], mx4[2]), mx4[3]);
+                        const float m_new = fmaxf(m_ref, mx);
+                        // a row with nothing accumulated yet (O holds zeros) adopts the new maximum directly;
+                        // otherwise the reference only moves when the maximum grew by more than 2^8
+                        const bool rescale = m_ref != -INFINITY && (m_new - m_ref) * c > 8.f;
+                        if (m_ref == -INFINITY) m_ref = m_new;
+                        if (__any_sync(0xffffffffu, rescale)) {
+                            // O_i is quiescent once the previous half's PV is done: the next one waits for this P
+                            // (the one before that was done before this half's S)
+                            if (!wait_all(C::B_PVDONE + 2 * hi + (half ^ 1), (half ? t_tile : t_tile - 1) & 1, 141)) { ok = false; break; }
+                            tc_fence_after();
+                            const float alpha = rescale ? fast_exp2((m_ref - m_new) * c) : 1.f;
 #pragma unroll 1   // (rare; unrolled it takes registers from every tile)
-                        for (int q = 0; q < D / 16; ++q) {
-                            uint32_t o[16];
-                            tmem_ld16(tO + q * 16, o);
-                            tmem_ld_wait();
+                            for (int q = 0; q < D / 16; ++q) {
+                                uint32_t o[16];
+                                tmem_ld16(tO + q * 16, o);
+                                tmem_ld_wait();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                            tmem_st16(tO + q * 16, o);
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tmem_st16(tO + q * 16, o);
+                            }
+                            if (rescale) { l *= alpha; m_ref = m_new; }
                         }
-                        if (rescale) { l *= alpha; m_ref = m_new; }
-                    }
-                    const float moff = m_ref == -INFINITY ? 0.f : m_ref * c;
-                    // P = exp2(S * c - m * c) as packed bf16 over the first 32 columns of this half's S: the MMA's
-                    // operand type, half a step (2^-9 of a weight on average), where l adds the unrounded weights
-                    const uint64_t c2 = f2_pack(c, c), moff2 = f2_pack(-moff, -moff);
-                    uint64_t rs[4] = {0ull, 0ull, 0ull, 0ull};
+                        const float moff = m_ref == -INFINITY ? 0.f : m_ref * c;
+                        // P = exp2(S * c - m * c) as packed bf16 over the first 32 columns of this half's S: the MMA's
+                        // operand type, half a step (2^-9 of a weight on average), where l adds the unrounded weights
+                        const uint64_t c2 = f2_pack(c, c), moff2 = f2_pack(-moff, -moff);
+                        uint64_t rs[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        uint32_t pk[16];
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t pk[16];
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            float x0, x1;
-                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[q][i]), __uint_as_float(sr[q][i + 1])), c2, moff2), x0, x1);
-                            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-                            rs[(i >> 1) & 3] = f2_add(rs[(i >> 1) & 3], f2_pack(p0, p1));
-                            pk[i >> 1] = pack_bf16x2(p0, p1);
+                            for (int i = 0; i < 32; i += 2) {
+                                float x0, x1;
+                                f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[q][i]), __uint_as_float(sr[q][i + 1])), c2, moff2), x0, x1);
+                                const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+                                rs[(i >> 1) & 3] = f2_add(rs[(i >> 1) & 3], f2_pack(p0, p1));
+                                pk[i >> 1] = pack_bf16x2(p0, p1);
+                            }
+                            tmem_st16(tB + q * 16, pk);
                         }
-                        tmem_st16(tB + q * 16, pk);
+                        float r0, r1;
+                        f2_unpack(f2_add(f2_add(rs[0], rs[1]), f2_add(rs[2], rs[3])), r0, r1);
+                        l += r0 + r1;
                     }
-                    float r0, r1;
-                    f2_unpack(f2_add(f2_add(rs[0], rs[1]), f2_add(rs[2], rs[3])), r0, r1);
-                    l += r0 + r1;
                     const bool tail = half == 0 && left < kKT;
                     if (tail) {   // V's rows past the end (both tiles' warps write the same zeros)
                         if (!wait_all(C::B_VTAIL, tails & 1, 142)) { ok = false; break; }
@@ -516,7 +526,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             // keys, in fp32 with the part's log-sum-exp. O_i is free for the next unit's PV as soon as it is read.
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m_ref * c + log2f(l);
             const int64_t at = in ? ((int64_t)token * a.hq + u.g * a.group + head) * D : -1;
-            const size_t pr = ((size_t)max(u.slot, 0) * a.hkv + u.g) * (PADOC_CROSS_UNIT_BLOCKS * kBlk) + hi * 128 + row;
+            const size_t pr = (size_t)max(u.slot, 0) * (PADOC_CROSS_UNIT_BLOCKS * kBlk) + hi * 128 + row;
             uint8_t *stage = so + warp * 4096;
 #pragma unroll
             for (int half = 0; half < C::kPanels; ++half) {
@@ -583,7 +593,7 @@ padoc_status launch(const padoc_cross_args &a, cudaStream_t stream)
         !padoc_make_tmap_bf16(&vmap, a.v, (uint64_t)a.hkv * D, a.key_rows, a.v_stride * 2, 64, kKT))
         return PADOC_ERR_CUDA;
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)(a.num_units * a.hkv * CG));
+    lc.gridDim = dim3((unsigned)((a.ctas ? a.num_ctas : a.num_units) * CG));
     lc.blockDim = dim3(kThreads);
     lc.dynamicSmemBytes = bytes;
     lc.stream = stream;

@@ -138,14 +138,12 @@ class padoc_cross_config(ctypes.Structure):
 
 
 class padoc_cross_plan(ctypes.Structure):
-    _fields_ = [("cfg", padoc_cross_config), ("num_segments", ctypes.c_int32), ("query_rows", ctypes.c_int32),
-                ("key_rows", ctypes.c_int32), ("pair", ctypes.c_int32), ("num_units", ctypes.c_int32),
-                ("num_merges", ctypes.c_int32), ("num_slots", ctypes.c_int32), ("num_dq_units", ctypes.c_int32),
-                ("num_dq_merges", ctypes.c_int32), ("num_dq_slots", ctypes.c_int32), ("num_subs", ctypes.c_int32),
-                ("num_key_tiles", ctypes.c_int32), ("num_covers", ctypes.c_int32), ("max_steps", ctypes.c_int32),
-                ("cluster", ctypes.c_int32), ("pairs", ctypes.c_int64), ("plan_ints", ctypes.c_int64),
-                ("off_units", ctypes.c_int64), ("off_merges", ctypes.c_int64), ("off_dq_units", ctypes.c_int64),
-                ("off_dq_merges", ctypes.c_int64), ("off_key_tiles", ctypes.c_int64), ("off_covers", ctypes.c_int64)]
+    _fields_ = [("cfg", padoc_cross_config)] + [(n, ctypes.c_int32) for n in (
+        "num_segments", "query_rows", "key_rows", "pair", "num_units", "num_ctas", "num_merges", "num_slots", "max_parts",
+        "num_dq_units", "num_dq_ctas", "num_dq_merges", "num_dq_slots", "max_dq_parts", "num_subs", "num_key_tiles",
+        "num_covers", "cluster")] + [(n, ctypes.c_int64) for n in (
+            "pairs", "plan_ints", "off_units", "off_ctas", "off_merges", "off_dq_units", "off_dq_ctas", "off_dq_merges",
+            "off_key_tiles", "off_covers")]
 
 
 class padoc_cross_rows(ctypes.Structure):
