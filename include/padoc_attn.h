@@ -951,9 +951,10 @@ typedef struct {
     int32_t num_segments;
     int32_t query_rows;      /* query rows the segments reach to (their largest q_begin + q_len) */
     int32_t key_rows;        /* key rows they reach to */
-    int32_t pair;            /* 1: the forward's items are 512 packed rows for a pair of CTAs, else 256 for one */
+    int32_t few;             /* forward: > 0: items of few rows, each by a cluster of that many CTAs; 0: of 256 packed rows */
+    int32_t unit_rows;       /* packed (token, query head) rows of a forward item at most: 16, 32 or 256 */
     int32_t num_units;       /* forward: work items */
-    int32_t num_ctas;        /* CTAs (pairs) that have a list of items each; 0: a CTA an item, taken as SMs get free */
+    int32_t num_ctas;        /* CTAs that have a list of items each; 0: a CTA an item, taken as SMs get free */
     int32_t num_merges;      /* row blocks whose key range is split over several items, or empty */
     int32_t num_slots;       /* partial results */
     int32_t max_parts;       /* most partial results of one row */

@@ -14,7 +14,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libpadoc_attn.so")
 SOURCES = ["plan.cpp", "api.cu", "decode.cu", "prefill.cu", "prefill_tc.cu", "prefill_bwd.cu", "prefill_bwd_tc.cu",
            "decode_tc.cu", "tc_selftest.cu", "mpd.cpp", "append.cu", "e4m3.cu",
-           "rotary.cu", "blocks.cu", "cross_plan.cpp", "cross.cu", "cross_tc.cu",
+           "rotary.cu", "blocks.cu", "cross_plan.cpp", "cross.cu", "cross_tc.cu", "cross_few.cu",
            "cross_bwd_tc.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

@@ -30,17 +30,18 @@ __device__ __forceinline__ void store4(T *p, float4 x)
 template <typename T, int D, bool kDq, int W>
 __global__ void __launch_bounds__(256) cross_merge_kernel(const padoc_cross_args a)
 {
-    constexpr int kRows = (kDq ? PADOC_CROSS_DQ_BLOCKS : PADOC_CROSS_UNIT_BLOCKS) * PADOC_CROSS_BLOCK;
-    constexpr int kPer = kRows * W / 8, E = D / 32;
+    constexpr int E = D / 32;
+    const int unit_rows = a.unit_rows, per = unit_rows * W / 8;   // (multiples of 8)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w0 = W == 8 ? warp : 0;
-    const int row = W == 8 ? blockIdx.x % kPer : (blockIdx.x % kPer) * 8 + warp;
-    const padoc_cross_merge m = a.merges[blockIdx.x / kPer];
+    const int row = W == 8 ? (int)blockIdx.x % per : (int)blockIdx.x % per * 8 + warp;
+    const padoc_cross_merge m = a.merges[(int)blockIdx.x / per];
     int token, head;
     const bool in = cross_row(a, m.tok, m.ntok, row, token, head);
+    pdl_launch_dependents();
     pdl_wait_prerequisite();
     if (!in) return;
     const int n = (m.parts - w0 + W - 1) / W;   // this warp's parts: w0, w0 + W, ..
-    auto at = [&](int i) { return (size_t)(m.slot + w0 + i * W) * kRows + row; };
+    auto at = [&](int i) { return (size_t)(m.slot + w0 + i * W) * unit_rows + row; };
     float acc[E], top = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
@@ -109,9 +110,8 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const padoc_cross_args
 template <typename T, int D, bool kDq, int W>
 padoc_status launch_merge(const padoc_cross_args &a, bool pdl, cudaStream_t stream)
 {
-    constexpr int kPer = (kDq ? PADOC_CROSS_DQ_BLOCKS : PADOC_CROSS_UNIT_BLOCKS) * PADOC_CROSS_BLOCK * W / 8;
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)(a.num_merges * kPer));
+    lc.gridDim = dim3((unsigned)(a.num_merges * (a.unit_rows * W / 8)));
     lc.blockDim = dim3(256);
     lc.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -594,11 +594,13 @@ extern "C" padoc_status padoc_cross_attn(const padoc_cross_plan *info, const int
     a.ctas = info->num_ctas ? plan_dev + info->off_ctas : nullptr;
     a.num_ctas = info->num_ctas;
     a.max_parts = info->max_parts;
-    a.part_lse = a.part + (size_t)info->num_slots * (PADOC_CROSS_UNIT_BLOCKS * kB) * c.head_dim;
+    a.unit_rows = info->unit_rows;
+    a.part_lse = a.part + (size_t)info->num_slots * a.unit_rows * c.head_dim;
     cudaStream_t cs = (cudaStream_t)stream;
     if (a.num_units) {
         if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_fwd_simt<64>(a, cs) : run_fwd_simt<128>(a, cs);
-        else st = padoc_cross_launch_tc(a, c.head_dim, info->pair != 0, cs);
+        else if (info->few) st = padoc_cross_launch_few(a, c.head_dim, info->few, cs);
+        else st = padoc_cross_launch_tc(a, c.head_dim, cs);
         if (st != PADOC_OK) return st;
     }
     if (!a.num_merges) return PADOC_OK;
@@ -657,6 +659,7 @@ extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const
     a.num_units = info->num_dq_units;
     a.num_ctas = info->num_dq_ctas;
     a.max_parts = info->max_dq_parts;
+    a.unit_rows = PADOC_CROSS_DQ_BLOCKS * kB;
     a.num_merges = info->num_dq_merges;
     a.num_tiles = info->num_key_tiles;
     a.num_subs = info->num_subs;

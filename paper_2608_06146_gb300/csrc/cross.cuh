@@ -20,6 +20,7 @@ struct padoc_cross_args {
     float *lse;
     float *part, *part_lse;                    // partial results
     float *neg_lse2, *dsum;                    // -lse * log2(e) and rowsum(dO * O): [Hkv][subs][64]
+    int32_t unit_rows;                         // packed rows of a forward or dq item, and of its partial result
     int32_t num_units, num_ctas, num_merges, max_parts, num_tiles, num_subs;
     int32_t tail_begin, tail_tiles;            // key rows that the plan does not reach
     int32_t hq, hkv, group, block_tokens;      // block_tokens: 64 / group
@@ -38,6 +39,8 @@ __device__ __forceinline__ bool cross_row(const padoc_cross_args &a, int tok, in
 }
 
 // The forward's units on the tensor cores (cross_tc.cu).
-padoc_status padoc_cross_launch_tc(const padoc_cross_args &args, int head_dim, bool pair, cudaStream_t stream);
+padoc_status padoc_cross_launch_tc(const padoc_cross_args &args, int head_dim, cudaStream_t stream);
+// The same for items of at most 32 rows, each by a cluster (cross_few.cu).
+padoc_status padoc_cross_launch_few(const padoc_cross_args &args, int head_dim, int cluster, cudaStream_t stream);
 // The backward's passes on the tensor cores (cross_bwd_tc.cu); cluster: CTAs that share a dK/dV unit.
 padoc_status padoc_cross_launch_bwd_tc(const padoc_cross_args &args, int head_dim, int cluster, cudaStream_t stream);

@@ -2,7 +2,7 @@
 //
 // Rows are packed for the tensor cores as (token, query head of the KV head's group): 64-row blocks of
 // 64 / group tokens, so that every query head of a KV head reads a key tile together, whatever the group. A tile is
-// two blocks, the M = 128 of the MMAs; the forward's unit is two tiles (a CTA) or four (a pair of CTAs).
+// two blocks, the M = 128 of the MMAs; the forward's unit is two tiles.
 #pragma once
 
 #include <stdint.h>
@@ -10,10 +10,12 @@
 #include "padoc_attn.h"
 
 #define PADOC_CROSS_BLOCK 64         // rows of a block
-#define PADOC_CROSS_UNIT_BLOCKS 4    // blocks of the forward's unit (8 for a pair)
+#define PADOC_CROSS_UNIT_BLOCKS 4    // blocks of the forward's unit
 #define PADOC_CROSS_DQ_BLOCKS 2      // blocks of the dq pass's unit
 #define PADOC_CROSS_KEY_TILE 128     // keys of a tile: of the forward's steps and of the dk/dv pass's units
 #define PADOC_CROSS_DQ_STEP 64       // keys of a step of the dq pass
+#define PADOC_CROSS_FEW_ROWS 32      // most rows of a unit of the kernel for few rows
+#define PADOC_CROSS_FEW_STEP 64      // keys of its tiles
 
 // Forward and dq work item: tokens of one segment, one KV head, a part of the segment's keys. 32 bytes.
 struct padoc_cross_unit {

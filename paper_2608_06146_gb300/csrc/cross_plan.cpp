@@ -1,6 +1,6 @@
 // cross_plan.cpp -- the host planner of cross attention (integers only).
 //
-// Forward: every segment's rows are cut into chunks of 256 packed rows (512 for CTA pairs), each with the segment's
+// Forward: every segment's rows are cut into chunks of 256 packed rows, each with the segment's
 // whole key range for every KV head. They are work items as they are, or, where that leaves the chip idle, the sequence
 // of all their steps is cut into runs of equal time, one for each SM, and the parts of a chunk are joined. Backward: the
 // dq pass has chunks of 128 rows cut the same way; the dk/dv pass has key tiles with the segments that see them.
@@ -20,11 +20,14 @@ namespace {
 
 typedef padoc_cross_segment Segment;
 
+int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
+
 // Costs of a pass, in units of one step of a full item.
 struct Costs {
     float start;    // an item's start and end
-    float part;     // what a partial result's traffic adds
-    float merge;    // the launch that joins them
+    float part;     // what writing a partial result adds
+    float merge;    // the launch that joins them, and ...
+    float read;     // ... what reading a partial result adds to it
     float half;     // a step of an item that is at most half full
     int32_t step;   // keys of a step
     int32_t least;  // fewest steps of a piece that is cut off
@@ -43,7 +46,7 @@ struct Work {
     int32_t slots = 0, max_parts = 0;
 };
 
-// Time of items, longest first on `lanes` SMs (or pairs): the greedy schedule that the launch order and the kernels'
+// Time of items, longest first on `lanes` SMs: the greedy schedule that the launch order and the kernels'
 // taking over of pending items come close to.
 float makespan(std::vector<float> cost, int lanes)
 {
@@ -65,6 +68,8 @@ float makespan(std::vector<float> cost, int lanes)
     }
     return end;
 }
+
+bool longer(const padoc_cross_unit &x, const padoc_cross_unit &y) { return x.nk > y.nk; }
 
 struct Piece {
     int32_t chunk, g, first, steps, cta;
@@ -121,9 +126,10 @@ void make_work(const std::vector<Chunk> &chunks, const std::vector<Piece> &piece
 }
 
 // The items of a pass: whole chunks, taken as SMs get free, or, where that leaves the chip idle, equal runs of the
-// sequence of all steps, a list for each CTA, with chunks cut where a run ends. `lists` false (fp32, whose kernels
-// run a CTA per 64 rows): the runs' pieces without the lists.
-float plan_work(const std::vector<Chunk> &chunks, int hkv, int lanes, const Costs &k, bool lists, Work &w)
+// sequence of all steps, a list for each CTA, with chunks cut where a run ends. kPieces (fp32, whose kernels run a
+// CTA per 64 rows): the runs' pieces without the lists.
+enum Cuts { kPieces, kLists };
+float plan_work(const std::vector<Chunk> &chunks, int hkv, int lanes, const Costs &k, Cuts cuts_allowed, Work &w)
 {
     std::vector<float> cost;
     std::vector<Piece> whole;
@@ -139,27 +145,30 @@ float plan_work(const std::vector<Chunk> &chunks, int hkv, int lanes, const Cost
     if (chunks.empty()) return 0.f;
     const float plain = makespan(cost, lanes);
     float lo = (float)(total / lanes), hi = std::max(longest, 2.f * lo) + 4.f * (k.start + k.part);
-    if (cut_runs(chunks, hkv, lanes, k, hi, nullptr) && lo + k.merge < 0.97f * plain) {
+    if (lo < 0.97f * plain && cut_runs(chunks, hkv, lanes, k, hi, nullptr)) {
         for (int i = 0; i < 16 && hi - lo > 0.01f * hi; ++i) {
             const float mid = 0.5f * (lo + hi);
             (cut_runs(chunks, hkv, lanes, k, mid, nullptr) ? hi : lo) = mid;
         }
         std::vector<Piece> pieces;
         cut_runs(chunks, hkv, lanes, k, hi, &pieces);
-        const bool split = pieces.size() > whole.size();
-        if (hi + (split ? k.merge : 0.f) < 0.97f * plain) {
+        // (the merge's reads: two parts or more of each row block that was cut)
+        const size_t cuts = pieces.size() - whole.size();
+        const float time = hi + (cuts ? k.merge + k.read * (float)(cuts + std::min(cuts, whole.size())) : 0.f);
+        if (time < 0.97f * plain) {
             make_work(chunks, pieces, k, w);
-            if (lists) {
+            if (cuts_allowed == kLists) {
                 for (size_t i = 0; i < pieces.size(); ++i)
                     while ((int32_t)w.ctas.size() <= pieces[i].cta) w.ctas.push_back((int32_t)i);
                 w.ctas.push_back((int32_t)pieces.size());
+            } else {
+                std::stable_sort(w.units.begin(), w.units.end(), longer);
             }
-            return hi + (split ? k.merge : 0.f);
+            return time;
         }
     }
     make_work(chunks, whole, k, w);
-    std::stable_sort(w.units.begin(), w.units.end(),
-                     [](const padoc_cross_unit &x, const padoc_cross_unit &y) { return x.nk > y.nk; });
+    std::stable_sort(w.units.begin(), w.units.end(), longer);
     return plain;
 }
 
@@ -191,7 +200,50 @@ padoc_status check(const Segment *seg, int32_t n, const padoc_cross_config *cfg)
     return PADOC_OK;
 }
 
-int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
+// The forward's items for few rows, where that is faster than `time` (us): 16 or 32 rows an item, by clusters of 1 to 8
+// CTAs that join their parts of the keys themselves, or keys cut into parts.
+template <typename F>
+void plan_few(const Segment *seg, int32_t n, int32_t group, int32_t head_dim, int32_t hkv, int32_t sms, float time,
+              const F &chunks_of, Work &fwd, padoc_cross_plan &info, int32_t &per)
+{
+    int32_t most = 0;   // rows of the largest segment
+    for (int32_t i = 0; i < n; ++i)
+        if (seg[i].k_len) most = std::max(most, std::min(seg[i].q_len, 2 * PADOC_CROSS_FEW_ROWS) * group);
+    const int32_t rows = most <= 16 ? 16 : PADOC_CROSS_FEW_ROWS;
+    const int32_t an_sm = head_dim == 64 ? 3 : 2, lanes = sms * an_sm;   // CTAs
+    const float step = (float)an_sm * PADOC_CROSS_FEW_STEP * head_dim * 4 / 45e3f;
+    const Costs k = {3.f / step, 0.3f / step, 3.f / step, 0.001f / step, 1.f, PADOC_CROSS_FEW_STEP, 2};
+    const std::vector<Chunk> chunks = chunks_of(rows / group, k);
+    if (chunks.size() * hkv > (size_t)64 * lanes) return;
+    Work w;
+    int few = 1;
+    float best = step * plan_work(chunks, hkv, lanes, k, kPieces, w);
+    bool parts = w.slots > 0;
+    for (int nc = 1; nc <= 8; nc *= 2) {
+        std::vector<float> cost;
+        for (const Chunk &c : chunks)
+            for (int32_t g = 0; g < hkv; ++g) cost.push_back(ceil_div(c.steps, nc) + (nc > 1 ? 1.f / step : 0.f) + k.start);
+        const float t = step * makespan(cost, std::max(1, lanes / nc));
+        if (t < best) {
+            best = t;
+            few = nc;
+            parts = false;
+        }
+    }
+    if (best >= time) return;
+    if (!parts) {
+        w = Work();
+        std::vector<Piece> whole;
+        for (size_t c = 0; c < chunks.size(); ++c)
+            for (int32_t g = 0; g < hkv; ++g) whole.push_back({(int32_t)c, g, 0, chunks[c].steps, 0});
+        make_work(chunks, whole, k, w);
+        std::stable_sort(w.units.begin(), w.units.end(), longer);
+    }
+    fwd = w;
+    info.few = few;
+    info.unit_rows = rows;
+    per = rows / group;
+}
 
 padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, Built &b)
 {
@@ -222,9 +274,8 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
     // blocks, and steps over them, are counted in 32 bits on the device
     if (blocks * hkv > (int64_t)1 << 24 || k_end > (int64_t)1 << 29) return PADOC_ERR_UNSUPPORTED;
 
-    auto chunks_of = [&](int32_t unit_blocks, const Costs &k) {
+    auto chunks_of = [&](int32_t per, const Costs &k) {   // of `per` tokens
         std::vector<Chunk> c;
-        const int32_t per = unit_blocks * block;
         for (int32_t i = 0; i < n; ++i) {
             if (seg[i].q_len == 0 || seg[i].k_len == 0) continue;
             for (int32_t t = 0; t < seg[i].q_len; t += per) {
@@ -235,25 +286,31 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
         }
         return c;
     };
-    auto empty_rows = [&](int32_t unit_blocks, std::vector<padoc_cross_merge> &merges) {
-        const int32_t per = unit_blocks * block;
+    auto empty_rows = [&](int32_t per, std::vector<padoc_cross_merge> &merges) {
         for (int32_t i = 0; i < n; ++i)
             if (seg[i].k_len == 0)
                 for (int32_t t = 0; t < seg[i].q_len; t += per)
                     for (int32_t g = 0; g < hkv; ++g)
                         merges.push_back({seg[i].q_begin + t, std::min(per, seg[i].q_len - t), 0, 0, g, {0, 0, 0}});
     };
-    const bool lists = cfg->dtype == PADOC_DTYPE_BF16;
+    const Cuts cuts = cfg->dtype == PADOC_DTYPE_BF16 ? kLists : kPieces;
 
-    // forward (a step of two 128-row tiles lasts about 1.6 us)
-    const Costs fwd = {1.5f, 0.5f, 2.0f, 0.65f, PADOC_CROSS_KEY_TILE, 1};
-    plan_work(chunks_of(PADOC_CROSS_UNIT_BLOCKS, fwd), hkv, lanes, fwd, lists, b.fwd);
-    empty_rows(PADOC_CROSS_UNIT_BLOCKS, b.fwd.merges);
+    // Forward. Times in us: of two 128-row tiles' steps of 128 keys, and for few rows of a 64-key tile's bytes at the
+    // SM's share of the memory bandwidth (45 KB a us), which its CTAs share.
+    int32_t per = PADOC_CROSS_UNIT_BLOCKS * block;
+    {
+        const Costs tc = {1.8f, 1.5f, 2.f, 0.012f, 0.65f, PADOC_CROSS_KEY_TILE, 1};
+        const float time = 1.65f * plan_work(chunks_of(per, tc), hkv, lanes, tc, cuts, b.fwd);
+        info.unit_rows = PADOC_CROSS_UNIT_BLOCKS * PADOC_CROSS_BLOCK;
+        if (cfg->dtype == PADOC_DTYPE_BF16 && group <= PADOC_CROSS_FEW_ROWS && !b.fwd.units.empty())
+            plan_few(seg, n, group, cfg->head_dim, hkv, sms, time, chunks_of, b.fwd, info, per);
+    }
+    empty_rows(per, b.fwd.merges);
 
     if (cfg->backward) {
-        const Costs bwd = {6.f, 1.f, 4.f, 1.f, PADOC_CROSS_DQ_STEP, 4};   // (a step of a tile lasts about 0.55 us)
-        plan_work(chunks_of(PADOC_CROSS_DQ_BLOCKS, bwd), hkv, lanes, bwd, lists, b.dq);
-        empty_rows(PADOC_CROSS_DQ_BLOCKS, b.dq.merges);
+        const Costs bwd = {6.f, 2.f, 6.f, 0.018f, 1.f, PADOC_CROSS_DQ_STEP, 4};   // (a step of a tile lasts about 0.55 us)
+        plan_work(chunks_of(PADOC_CROSS_DQ_BLOCKS * block, bwd), hkv, lanes, bwd, cuts, b.dq);
+        empty_rows(PADOC_CROSS_DQ_BLOCKS * block, b.dq.merges);
 
         // Key tiles: ranges that overlap are tiled together, from the first one's begin; between them lie keys that
         // nobody sees.
@@ -393,9 +450,9 @@ extern "C" padoc_status padoc_build_cross_plan(const padoc_cross_segment *segmen
 
 extern "C" padoc_status padoc_cross_workspace_size(const padoc_cross_plan *info, size_t *bytes)
 {
-    if (!info || !bytes || info->num_slots < 0) return PADOC_ERR_INVALID_ARGUMENT;
-    // partial outputs [slots][256][d] and their log-sum-exps [slots][256], fp32
-    const size_t rows = (size_t)info->num_slots * (PADOC_CROSS_UNIT_BLOCKS * PADOC_CROSS_BLOCK);
+    if (!info || !bytes || info->num_slots < 0 || info->unit_rows < 0) return PADOC_ERR_INVALID_ARGUMENT;
+    // partial outputs [slots][unit_rows][d] and their log-sum-exps [slots][unit_rows], fp32
+    const size_t rows = (size_t)info->num_slots * info->unit_rows;
     *bytes = rows * (info->cfg.head_dim + 1) * sizeof(float);
     return PADOC_OK;
 }

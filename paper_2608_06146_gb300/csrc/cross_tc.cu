@@ -1,7 +1,7 @@
 // cross_tc.cu -- cross attention forward on the 5th-generation tensor cores: S = Q K^T, online softmax, O = P V.
 //
-// A unit is 256 packed rows of one KV head (two 128-row tiles of (token, head of the group) rows; 512 for a CTA
-// pair) over a segment's keys or a part of them. All rows of a unit see the same keys, so the only mask is the end of
+// A unit is 256 packed rows of one KV head (two 128-row tiles of (token, head of the group) rows) over a segment's
+// keys or a part of them. All rows of a unit see the same keys, so the only mask is the end of
 // the last 128-key tile: its scores past the end become -inf, and its V rows there zeros, because what lies behind a
 // segment's keys may be anything (0 x NaN would reach the output).
 //
@@ -12,7 +12,7 @@
 // For a tile and half the MMAs run S(t) -> P(t) -> P V(t) -> S(t + 1). O is rescaled only when a row's maximum has
 // grown by more than 2^8 since the last time, which keeps P <= 256.
 //
-// The grid has one CTA (pair) per unit, most keys first; a running one takes over units not yet launched (cluster
+// The grid has one CTA per unit, most keys first; a running one takes over units not yet launched (cluster
 // launch control). Where the planner cut the steps into equal runs, each CTA has a list of units. The next unit's
 // queries and first scores come under the last one's output. A unit of at most 128 rows is run by tile 0's warps alone.
 // Every wait is bounded; a wait that runs out records an error, all roles leave their loops, the issuers wait for
@@ -30,35 +30,34 @@ constexpr int kPanel = 128 * 128;      // [128 rows][64 bf16]
 constexpr int kBlk = PADOC_CROSS_BLOCK;
 constexpr int kKT = PADOC_CROSS_KEY_TILE;
 
-template <int D, int CG>
+template <int D>
 struct Cfg {
     static constexpr int kPanels = D / 64;
     static constexpr int kTile = kPanels * kPanel;
-    static constexpr int kStages = D == 64 ? 4 : CG == 2 ? 3 : 2;
-    static constexpr int kHalf = kTile / CG;         // a CTA's part of a K or V tile
-    static constexpr int kKPanel = kPanel / 2 / CG;  // 64 dims of its keys of one half
+    static constexpr int kStages = D == 64 ? 4 : 2;
+    static constexpr int kKPanel = kPanel / 2;       // 64 dims of the keys of one half
     static constexpr int kOutBytes = 8 * 4096;       // [32 rows][64 dims] a softmax warp
     enum {
         B_QFULL = 0,                    // [tile]
         B_QEMPTY = 2,                   // [tile]
         B_SFULL = 4,                    // [tile][half]
-        B_PFULL = 8,                    // [tile][half], one arrival per warp of the tile (both CTAs')
+        B_PFULL = 8,                    // [tile][half], one arrival per warp of the tile
         B_PVDONE = 12,                  // [tile][half]
-        B_OFREE = 16,                   // [tile], one arrival per warp of the tile (both CTAs')
+        B_OFREE = 16,                   // [tile], one arrival per warp of the tile
         B_UFULL = 18,                   // [slot]: the announced unit
-        B_UEMPTY = 20,                  // [slot], one arrival per reading warp (both CTAs')
+        B_UEMPTY = 20,                  // [slot], one arrival per reading warp
         B_NEXT = 22,                    // the launch control's answer
         B_FINAL = 23,                   // [tile]
-        B_VTAIL = 25,                   // this CTA's part of a unit's last V tile, where keys end inside it
+        B_VTAIL = 25,                   // a unit's last V tile, where keys end inside it
         B_KFULL = 26,                   // [stage]
         B_KEMPTY = B_KFULL + kStages,   // [stage], one arrival per tile
         B_VFULL = B_KEMPTY + kStages,   // [stage]
         B_VEMPTY = B_VFULL + kStages,   // [stage], one arrival per tile
         B_COUNT = B_VEMPTY + kStages
     };
-    static constexpr int kReaders = CG == 2 ? 19 : 10;   // softmax warps, MMA warps, the second CTA's producer
-    static constexpr size_t kSmemBytes = 1024 + 2 * (size_t)kTile + 2 * (size_t)kStages * kHalf + kOutBytes + 96 + B_COUNT * 8 + 16;
-    static_assert(kSmemBytes <= 227 * 1024 && (CG == 1 || D == 128), "");
+    static constexpr int kReaders = 10;   // softmax and MMA warps
+    static constexpr size_t kSmemBytes = 1024 + 2 * (size_t)kTile + 2 * (size_t)kStages * kTile + kOutBytes + 96 + B_COUNT * 8 + 16;
+    static_assert(kSmemBytes <= 227 * 1024, "");
 };
 
 // A unit as the producer announces it; tiles < 0 ends the CTA.
@@ -67,29 +66,28 @@ struct Unit {
     int32_t g, slot, tiles, two;   // tiles: 128-key tiles; two: whether the second tile has rows
 };
 
-template <bool kCluster>
 __device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, int *err, int site, volatile int *abort_flag)
 {
-    if (kCluster ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
+    if (mbar_try_wait(bar, parity)) return true;
     if (*abort_flag) return false;
-    if (kCluster ? mbar_wait_bounded_cluster(bar, parity, err, site) : mbar_wait_bounded(bar, parity, err, site)) return true;
+    if (mbar_wait_bounded(bar, parity, err, site)) return true;
     *abort_flag = 1;
     return false;
 }
 
-template <int D, int CG>
+template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                 const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
 {
-    using C = Cfg<D, CG>;
+    using C = Cfg<D>;
     constexpr int kStages = C::kStages, kTile = C::kTile;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t *sq = smem;                       // [2 tiles][panel][128 rows]
-    uint8_t *sk = sq + 2 * kTile;             // [kStages][key half][panel] (CG 2: this CTA's half of the keys)
-    uint8_t *sv = sk + kStages * C::kHalf;    // [kStages][panel] (CG 2: this CTA's 64 dims)
-    uint8_t *so = sv + kStages * C::kHalf;    // [8 warps][32][128 bytes]
+    uint8_t *sk = sq + 2 * kTile;             // [kStages][key half][panel]
+    uint8_t *sv = sk + kStages * kTile;    // [kStages][panel]
+    uint8_t *so = sv + kStages * kTile;    // [8 warps][32][128 bytes]
     Unit *units = (Unit *)(so + C::kOutBytes);   // [2]
     uint8_t *answer = (uint8_t *)(units + 2); // 16 bytes
     uint64_t *bars = (uint64_t *)(so + C::kOutBytes + 96);
@@ -98,22 +96,14 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (a value the compiler knows to be warp-uniform)
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const int tile_tokens = 2 * a.block_tokens;
     pdl_launch_dependents();   // the joining of split rows, where there is one, may take the SMs that run out of work
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
-    // a barrier of the pair's first CTA, which issues the MMAs and announces the units
-    auto lead_bar = [&](int i) { return CG == 2 ? cluster_map(bar(i), 0) : bar(i); };
-    auto arrive_lead = [&](int i) {
-        if (CG == 2) mbar_arrive_cluster<false>(lead_bar(i));
-        else mbar_arrive(bar(i));
-    };
-
     if (tid == 0) {
         for (int i = 0; i < C::B_COUNT; ++i) {
             int n = 1;
-            if (i >= C::B_PFULL && i < C::B_PFULL + 4) n = 4 * CG;
-            if (i == C::B_OFREE || i == C::B_OFREE + 1) n = 4 * CG;
+            if (i >= C::B_PFULL && i < C::B_PFULL + 4) n = 4;
+            if (i == C::B_OFREE || i == C::B_OFREE + 1) n = 4;
             if (i >= C::B_KEMPTY && i < C::B_KEMPTY + kStages) n = 2;
             if (i >= C::B_VEMPTY && i < C::B_VEMPTY + kStages) n = 2;
             if (i == C::B_UEMPTY || i == C::B_UEMPTY + 1) n = C::kReaders;
@@ -121,6 +111,19 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
         }
         *abort_flag = 0;
         fence_barrier_init();
+    }
+    // items of this CTA: x and, of a list, those up to xe; the first one is on its way while the barriers are set
+    // up (a small call waits for each global read in turn)
+    int x = 0, xe = 0;
+    padoc_cross_unit item = {};
+    if (warp == 8 && lane == 0) {
+        x = (int)blockIdx.x;
+        pdl_wait_prerequisite();   // nothing in global memory is touched before (the other roles' work follows from this)
+        if (a.ctas) {
+            xe = a.ctas[x + 1];
+            x = a.ctas[x];
+        }
+        item = a.units[x];
     }
     // rows of a block that hold no (token, head): no copy writes them
     const int used = a.block_tokens * a.group;
@@ -132,17 +135,16 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
         fence_proxy_async_smem();
     }
     if (warp == 9) {
-        tmem_alloc<CG>(smem_u32(tmem_slot), kTmemCols);
-        tmem_relinquish<CG>();
+        tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+        tmem_relinquish();
     }
     tc_fence_before();
     __syncthreads();
-    if (CG == 2) cluster_sync();   // no arrival or copy for the other CTA before its barriers are set up
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     // the n-th unit, as every lane of a reading warp sees it
     auto read_unit = [&](int n, Unit &u, int site) {
-        const bool r = wait_or_abort<CG == 2>(bar(C::B_UFULL + (n & 1)), (n >> 1) & 1, a.err, site, abort_flag);
+        const bool r = wait_or_abort(bar(C::B_UFULL + (n & 1)), (n >> 1) & 1, a.err, site, abort_flag);
         if (!__all_sync(0xffffffffu, r)) return false;
         const Unit v = units[n & 1];
         u.tok = __shfl_sync(0xffffffffu, v.tok, 0);
@@ -153,7 +155,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
         u.tiles = __shfl_sync(0xffffffffu, v.tiles, 0);
         u.two = __shfl_sync(0xffffffffu, v.two, 0);
         __syncwarp();   // (every lane's read has returned before the arrival lets the slot be written again)
-        if (lane == 0) arrive_lead(C::B_UEMPTY + (n & 1));
+        if (lane == 0) mbar_arrive(bar(C::B_UEMPTY + (n & 1)));
         return true;
     };
     // the next unit that tile i takes part in; ring: K and V tiles so far, of all units
@@ -172,44 +174,28 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             tma_prefetch_desc(&kmap);
             tma_prefetch_desc(&vmap);
             auto wait = [&](int b, uint32_t parity, int site) {
-                return wait_or_abort<false>(bar(b), parity, a.err, site, abort_flag);
+                return wait_or_abort(bar(b), parity, a.err, site, abort_flag);
             };
-            // the first CTA's barrier counts both CTAs' bytes
-            auto expect = [&](int b, uint32_t bytes) {
-                if (rank == 0) mbar_arrive_expect_tx(bar(b), CG * bytes);
-            };
-            auto box = [&](uint8_t *dst, const CUtensorMap *map, int x, int y, int b) {
-                if (CG == 2) tma_load_2d_pair(smem_u32(dst), map, x, y, lead_bar(b));
-                else tma_load_2d(smem_u32(dst), map, x, y, bar(b));
-            };
-            // items: x and, of a list, those up to xe
-            int x = (int)blockIdx.x / CG, xe = 0;
-            if (a.ctas) {
-                xe = a.ctas[x + 1];
-                x = a.ctas[x];
-            }
-            int tk = 0, nq[2] = {0, 0}, tails = 0;   // K and V tiles, queries per tile, V tails issued so far
+            int tk = 0, tv = 0, nq[2] = {0, 0}, tails = 0;   // K and V tiles, queries per tile, V tails issued so far
             bool ok = true, more = true, asked = false;
             // asked with the unit's last tile, a few tiles ahead of the MMAs: early enough for the answer,
             // and late enough that no CTA holds a second unit while others run out of work
             auto ask = [&]() {
-                if (rank != 0 || a.ctas) return;
+                if (a.ctas) return;
                 mbar_arrive_expect_tx(bar(C::B_NEXT), 16);
                 launch_control_ask(smem_u32(answer), bar(C::B_NEXT));
                 asked = true;
             };
             auto load_q = [&](int i, const Unit &u) {
                 if (nq[i] && !wait(C::B_QEMPTY + i, (nq[i] - 1) & 1, 120)) return false;
-                const int t0 = u.tok + (2 * (int)rank + i) * tile_tokens;
-                expect(C::B_QFULL + i, 2 * C::kPanels * used * 128);
+                const int t0 = u.tok + i * tile_tokens;
+                mbar_arrive_expect_tx(bar(C::B_QFULL + i), 2 * C::kPanels * used * 128);
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int p = 0; p < C::kPanels; ++p) {
                         const uint32_t dst = smem_u32(sq + i * kTile + p * kPanel + b * kBlk * 128);
-                        const int y = u.g * a.group, z = t0 + b * a.block_tokens;
-                        if (CG == 2) tma_load_3d_pair(dst, &qmap, 64 * p, y, z, lead_bar(C::B_QFULL + i));
-                        else tma_load_3d(dst, &qmap, 64 * p, y, z, bar(C::B_QFULL + i));
+                        tma_load_3d(dst, &qmap, 64 * p, u.g * a.group, t0 + b * a.block_tokens, bar(C::B_QFULL + i));
                     }
                 ++nq[i];
                 return true;
@@ -217,125 +203,80 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             int n = 0, asks = 0;   // units announced, questions answered
             for (;; ++n) {
                 Unit u = {0, 0, 0, 0, 0, 0, -1, 0};
-                if (rank == 0) {
-                    if (n >= 2 && !wait(C::B_UEMPTY + (n & 1), ((n >> 1) - 1) & 1, 124)) break;
-                    if (more) {
-                        const padoc_cross_unit w = a.units[x];
-                        u.tok = w.tok;
-                        u.ntok = w.ntok;
-                        u.k0 = w.k0;
-                        u.nk = w.nk;
-                        u.g = w.g;
-                        u.slot = w.slot;
-                        u.tiles = (w.nk + kKT - 1) / kKT;
-                        u.two = CG == 2 || w.ntok > tile_tokens;
-                    }
-                    units[n & 1] = u;
-                    mbar_arrive(bar(C::B_UFULL + (n & 1)));
-                    if (CG == 2) {
-                        const uint32_t to = cluster_map(smem_u32(&units[n & 1]), 1);
-                        st_cluster_v4(to, make_int4(u.tok, u.ntok, u.k0, u.nk));
-                        st_cluster_v4(to + 16, make_int4(u.g, u.slot, u.tiles, u.two));
-                        mbar_arrive_cluster<true>(cluster_map(bar(C::B_UFULL + (n & 1)), 1));
-                    }
-                } else {
-                    if (!wait_or_abort<true>(bar(C::B_UFULL + (n & 1)), (n >> 1) & 1, a.err, 125, abort_flag)) break;
-                    u = units[n & 1];
+                if (n >= 2 && !wait(C::B_UEMPTY + (n & 1), ((n >> 1) - 1) & 1, 124)) break;
+                if (more) {
+                    u = {item.tok, item.ntok, item.k0, item.nk, item.g, item.slot, (item.nk + kKT - 1) / kKT, item.ntok > tile_tokens};
+                    if (a.ctas && (more = ++x < xe)) item = a.units[x];   // (a list's next item is known at once)
                 }
+                units[n & 1] = u;
+                mbar_arrive(bar(C::B_UFULL + (n & 1)));
                 if (u.tiles < 0) break;
-                for (int j = 0; j < u.tiles; ++j, ++tk) {
+                for (int j = 0; j < u.tiles; ++j) {
                     if (j + 1 == u.tiles) ask();
                     // (the first K tile between the two tiles' queries: S_0 needs it first)
                     if (j == 0 && !(ok = load_q(0, u))) break;
                     const int s = tk % kStages, row = u.k0 + j * kKT;
                     if (tk >= kStages && !(ok = wait(C::B_KEMPTY + s, (tk / kStages - 1) & 1, 121))) break;
-                    uint8_t *kb = sk + s * C::kHalf;
-                    expect(C::B_KFULL + s, C::kHalf);
+                    uint8_t *kb = sk + s * kTile;
+                    mbar_arrive_expect_tx(bar(C::B_KFULL + s), kTile);
                     if (!u.two) mbar_arrive(bar(C::B_KEMPTY + s));   // (for the second tile, which has no part)
 #pragma unroll
                     for (int b = 0; b < 2 * C::kPanels; ++b)   // [key half][panel]
-                        box(kb + b * C::kKPanel, &kmap, u.g * D + 64 * (b % C::kPanels),
-                            row + 64 * (b / C::kPanels) + 64 / CG * (int)rank, C::B_KFULL + s);
-                    if (j == 0 && u.two && !(ok = load_q(1, u))) { ++tk; break; }
-                    if (tk >= kStages && !(ok = wait(C::B_VEMPTY + s, (tk / kStages - 1) & 1, 123))) { ++tk; break; }
-                    uint8_t *vb = sv + s * C::kHalf;
+                        tma_load_2d(smem_u32(kb + b * C::kKPanel), &kmap, u.g * D + 64 * (b % C::kPanels), row + 64 * (b / C::kPanels),
+                                    bar(C::B_KFULL + s));
+                    ++tk;
+                    if (j == 0 && u.two && !(ok = load_q(1, u))) break;
+                    if (tv >= kStages && !(ok = wait(C::B_VEMPTY + s, (tv / kStages - 1) & 1, 123))) break;
+                    uint8_t *vb = sv + s * kTile;
+                    // a tail completes on a barrier of its own: the softmax warps zero its rows past the end
                     const bool tail = u.nk - j * kKT < kKT;
-                    if (tail) {   // completes on this CTA's own barrier: the softmax warps zero its rows past the end
-                        if (rank == 0) mbar_arrive(bar(C::B_VFULL + s));
-                        mbar_arrive_expect_tx(bar(C::B_VTAIL), C::kHalf);
+                    const uint32_t vbar = bar(tail ? (int)C::B_VTAIL : C::B_VFULL + s);
+                    if (tail) {
+                        mbar_arrive(bar(C::B_VFULL + s));
                         ++tails;
-                    } else {
-                        expect(C::B_VFULL + s, C::kHalf);
                     }
+                    mbar_arrive_expect_tx(vbar, kTile);
                     if (!u.two) mbar_arrive(bar(C::B_VEMPTY + s));
 #pragma unroll
-                    for (int p = 0; p < C::kPanels / CG; ++p) {
-                        const int col = u.g * D + 64 * (CG == 2 ? (int)rank : p);
-                        if (tail) tma_load_2d(smem_u32(vb + p * kPanel), &vmap, col, row, bar(C::B_VTAIL));
-                        else box(vb + p * kPanel, &vmap, col, row, C::B_VFULL + s);
-                    }
+                    for (int p = 0; p < C::kPanels; ++p) tma_load_2d(smem_u32(vb + p * kPanel), &vmap, u.g * D + 64 * p, row, vbar);
+                    ++tv;
                 }
                 if (!ok) break;
-                if (rank != 0) {
-                    // Only now may the first CTA write this slot of ours again (it does two units on): with
-                    // cluster scope, so that its stores come after the reads above.
-                    mbar_arrive_cluster<true>(lead_bar(C::B_UEMPTY + (n & 1)));
-                } else if (a.ctas) {
-                    more = ++x < xe;
-                } else {
+                if (!a.ctas) {
                     if (!wait(C::B_NEXT, asks & 1, 126)) break;
                     ++asks;
                     asked = false;
                     int y;
                     more = launch_control_answer(smem_u32(answer), x, y);
-                    x /= CG;
+                    if (more) item = a.units[x];
                     fence_proxy_async_smem();   // the answer is read before the next one may be written
                 }
             }
-            // copies still in flight must land before the CTA's shared memory is released (CG 2: the first
-            // CTA sees both CTAs' land, and both stay until the cluster barrier below; after a wait that
-            // ran out the other CTA may never issue its part, so the copies get a millisecond to land)
+            // copies still in flight must land before the CTA's shared memory is released
             if (asked) mbar_wait_bounded(bar(C::B_NEXT), asks & 1, a.err, 127);
-            if (CG == 2 && *abort_flag) {
-                const uint64_t t0 = padoc_globaltimer();
-                while (padoc_globaltimer() - t0 < 1000000ull) {
-                }
-            } else {
-                if (tails) mbar_wait_bounded(bar(C::B_VTAIL), (tails - 1) & 1, a.err, 127);
-                if (rank == 0) {
-                    for (int i = 0; i < 2; ++i)
-                        if (nq[i]) mbar_wait_bounded(bar(C::B_QFULL + i), (nq[i] - 1) & 1, a.err, 127);
-                    for (int t = max(tk - kStages, 0); t < tk; ++t)
-                        mbar_wait_bounded(bar(C::B_KFULL + t % kStages), (t / kStages) & 1, a.err, 128);
-                    // (after a wait that ran out between a tile's K and its V the last phase was never opened)
-                    for (int t = max(tk - kStages, 0); t < tk && !*abort_flag; ++t)
-                        mbar_wait_bounded(bar(C::B_VFULL + t % kStages), (t / kStages) & 1, a.err, 129);
-                }
-                if (*abort_flag) {
-                    const uint64_t t0 = padoc_globaltimer();
-                    while (padoc_globaltimer() - t0 < 1000000ull) {
-                    }
-                }
-            }
-        } else if (warp >= 9 && warp < 11 && rank == 0) {
+            for (int i = 0; i < 2; ++i)
+                if (nq[i]) mbar_wait_bounded(bar(C::B_QFULL + i), (nq[i] - 1) & 1, a.err, 127);
+            for (int t = max(tk - kStages, 0); t < tk; ++t)
+                mbar_wait_bounded(bar(C::B_KFULL + t % kStages), (t / kStages) & 1, a.err, 128);
+            if (tails) mbar_wait_bounded(bar(C::B_VTAIL), (tails - 1) & 1, a.err, 127);
+            for (int t = max(tv - kStages, 0); t < tv; ++t)
+                mbar_wait_bounded(bar(C::B_VFULL + t % kStages), (t / kStages) & 1, a.err, 129);
+        } else if (warp >= 9 && warp < 11) {
             // ------------------------------------------------------------ MMA issuers (a whole warp per tile)
             const int i = warp - 9;
-            constexpr uint32_t idS = umma_idesc_bf16(128 * CG, 64, false);
-            constexpr uint32_t idPV = umma_idesc_bf16(128 * CG, D, true);
+            constexpr uint32_t idS = umma_idesc_bf16(128, 64, false);
+            constexpr uint32_t idPV = umma_idesc_bf16(128, D, true);
             const uint64_t dq = umma_desc_sw128(smem_u32(sq + i * kTile), 16, 1024);
             const uint64_t dk = umma_desc_sw128(smem_u32(sk), 16, 1024), dv = umma_desc_sw128(smem_u32(sv), kPanel, 1024);
             const uint32_t tS = tmem + 128 * i, tO = tmem + 256 + 128 * i;
             auto wait = [&](int b, uint32_t parity, int site) {
                 return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
             };
-            auto commit = [&](int b) {
-                if (CG == 2) umma_commit_pair_warp(bar(b));
-                else umma_commit_warp(bar(b));
-            };
+            auto commit = [&](int b) { umma_commit_warp(bar(b)); };
             // S_i over half h of the tile in the given stage; the last tile of a unit frees Q_i
             auto issue_s = [&](int stage, int h, bool last) {
-                const uint64_t b = dk + ((stage * C::kHalf + h * C::kPanels * C::kKPanel) >> 4);
-                if constexpr (D == 128) umma_bf16_ss_k128_warp<CG, kPanel, C::kKPanel>(tS + 64 * h, dq, b, idS);
+                const uint64_t b = dk + ((stage * kTile + h * C::kPanels * C::kKPanel) >> 4);
+                if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kPanel, C::kKPanel>(tS + 64 * h, dq, b, idS);
                 else umma_bf16_ss_k64_warp(tS + 64 * h, dq, b, idS);
                 commit(C::B_SFULL + 2 * i + h);
                 if (h == 1) {
@@ -355,11 +296,10 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 return true;
             };
             // O_i += P_i V over half h of the tile
-            auto issue_pv = [&](int s, int h, bool first, bool tail) {
+            auto issue_pv = [&](int s, int h, bool first) {
                 if (!wait(C::B_PFULL + 2 * i + h, t & 1, 135)) return false;
-                if (CG == 2 && tail) asm volatile("fence.acq_rel.cluster;" ::: "memory");   // (V's zeros of both CTAs)
                 tc_fence_after();
-                umma_bf16_ts_k64_mn_warp<CG>(tO, tS + 64 * h, dv + ((s * C::kHalf + h * 8192) >> 4), idPV, !first);
+                umma_bf16_ts_k64_mn_warp<1>(tO, tS + 64 * h, dv + ((s * kTile + h * 8192) >> 4), idPV, !first);
                 commit(C::B_PVDONE + 2 * i + h);
                 if (h == 1) commit(C::B_VEMPTY + s);
                 return true;
@@ -368,19 +308,18 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             for (int w = 0; ok && u.tiles > 0; ++w) {
                 if (w > 0) ok = wait(C::B_OFREE + i, (w - 1) & 1, 134);
                 const int ne = u.tiles;
-                const bool cut = u.nk % kKT != 0;
                 for (int j = 0; ok && j + 1 < ne; ++j, ++t, ++ring) {
                     const int s = ring % kStages, sn = (ring + 1) % kStages;
                     // (while the tensor cores still run the S of this tile)
                     ok = wait(C::B_VFULL + s, (ring / kStages) & 1, 133) && wait(C::B_KFULL + sn, ((ring + 1) / kStages) & 1, 136);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        if (ok && (ok = issue_pv(s, h, j == 0 && h == 0, false))) issue_s(sn, h, j + 2 == ne);
+                        if (ok && (ok = issue_pv(s, h, j == 0 && h == 0))) issue_s(sn, h, j + 2 == ne);
                 }
                 if (!ok) break;
                 // the unit's last tile, then the first S of the next unit, under this one's epilogue
                 const int s = ring % kStages;
-                ok = wait(C::B_VFULL + s, (ring / kStages) & 1, 133) && issue_pv(s, 0, ne == 1, cut) && issue_pv(s, 1, false, cut);
+                ok = wait(C::B_VFULL + s, (ring / kStages) & 1, 133) && issue_pv(s, 0, ne == 1) && issue_pv(s, 1, false);
                 if (!ok) break;
                 ++t;
                 ++ring;
@@ -389,8 +328,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 ok = first_s(w + 1);
             }
             // every MMA issued above must complete before TMEM is released
-            if (CG == 2) umma_commit_pair_warp(bar(C::B_FINAL + i));
-            else umma_commit_warp(bar(C::B_FINAL + i));
+            umma_commit_warp(bar(C::B_FINAL + i));
             mbar_wait_bounded(bar(C::B_FINAL + i), 0, a.err, 138);
         }
     } else {
@@ -419,7 +357,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
         while (ok && next.tiles > 0) {
             const Unit u = next;
             int token, head;
-            const bool in = cross_row(a, u.tok, u.ntok, (2 * (int)rank + hi) * 128 + row, token, head);
+            const bool in = cross_row(a, u.tok, u.ntok, hi * 128 + row, token, head);
             const bool idle = !__any_sync(0xffffffffu, in);   // a warp without rows only keeps the others' pace
             float m_ref = -INFINITY, l = 0.f;   // m_ref in raw score units
             for (int j = 0; j < u.tiles; ++j, ++t_tile, ++ring) {
@@ -501,10 +439,10 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     if (tail) {   // V's rows past the end (both tiles' warps write the same zeros)
                         if (!wait_all(C::B_VTAIL, tails & 1, 142)) { ok = false; break; }
                         ++tails;
-                        uint8_t *vb = sv + ring % kStages * C::kHalf + row * 128;
+                        uint8_t *vb = sv + ring % kStages * kTile + row * 128;
                         if (row >= left)
 #pragma unroll
-                            for (int p = 0; p < C::kPanels / CG; ++p)
+                            for (int p = 0; p < C::kPanels; ++p)
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(vb + p * kPanel + 16 * i) = make_uint4(0, 0, 0, 0);
                         fence_proxy_async_smem();
@@ -512,10 +450,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
-                        if (CG == 2 && tail) mbar_arrive_cluster<true>(lead_bar(C::B_PFULL + 2 * hi + half));
-                        else arrive_lead(C::B_PFULL + 2 * hi + half);
-                    }
+                    if (lane == 0) mbar_arrive(bar(C::B_PFULL + 2 * hi + half));
                 }
                 if (!ok) break;
             }
@@ -537,7 +472,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 if (half == C::kPanels - 1) {
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) arrive_lead(C::B_OFREE + hi);
+                    if (lane == 0) mbar_arrive(bar(C::B_OFREE + hi));
                 }
                 auto v = [&](int i) { return __uint_as_float(o[i >> 5][i & 31]) * inv; };
                 if (u.slot >= 0) {
@@ -573,47 +508,43 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
-    // neither CTA leaves while the other may still reach its shared memory, barriers or tensor memory
-    if (CG == 2) cluster_sync();
     if (warp == 9) {
         tc_fence_after();
-        tmem_dealloc<CG>(tmem, kTmemCols);
+        tmem_dealloc(tmem, kTmemCols);
     }
 }
 
-template <int D, int CG>
+template <int D>
 padoc_status launch(const padoc_cross_args &a, cudaStream_t stream)
 {
-    auto kernel = cross_tc_kernel<D, CG>;
-    constexpr size_t bytes = Cfg<D, CG>::kSmemBytes;
+    auto kernel = cross_tc_kernel<D>;
+    constexpr size_t bytes = Cfg<D>::kSmemBytes;
     if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)bytes)) return st;
     CUtensorMap qmap, kmap, vmap;
     if (!padoc_make_tmap_bf16_heads(&qmap, a.q, D, a.hq, a.query_rows, a.q_stride * 2, a.group, a.block_tokens) ||
-        !padoc_make_tmap_bf16(&kmap, a.k, (uint64_t)a.hkv * D, a.key_rows, a.k_stride * 2, 64, 64 / CG) ||
+        !padoc_make_tmap_bf16(&kmap, a.k, (uint64_t)a.hkv * D, a.key_rows, a.k_stride * 2, 64, 64) ||
         !padoc_make_tmap_bf16(&vmap, a.v, (uint64_t)a.hkv * D, a.key_rows, a.v_stride * 2, 64, kKT))
         return PADOC_ERR_CUDA;
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)((a.ctas ? a.num_ctas : a.num_units) * CG));
+    lc.gridDim = dim3((unsigned)(a.ctas ? a.num_ctas : a.num_units));
     lc.blockDim = dim3(kThreads);
     lc.dynamicSmemBytes = bytes;
     lc.stream = stream;
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // set up behind the last kernel's end
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = attr;
-    lc.numAttrs = CG == 1 ? 0 : 1;
+    lc.numAttrs = 1;
     PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, qmap, kmap, vmap, a));
     return padoc_launch_status();
 }
 
 }  // namespace
 
-padoc_status padoc_cross_launch_tc(const padoc_cross_args &args, int head_dim, bool pair, cudaStream_t stream)
+padoc_status padoc_cross_launch_tc(const padoc_cross_args &args, int head_dim, cudaStream_t stream)
 {
     padoc_cross_args a = args;
     a.err = padoc_device_error_word();
     if (!a.err) return PADOC_ERR_CUDA;
-    if (head_dim == 64) return launch<64, 1>(a, stream);
-    return pair ? launch<128, 2>(a, stream) : launch<128, 1>(a, stream);
+    return head_dim == 64 ? launch<64>(a, stream) : launch<128>(a, stream);
 }

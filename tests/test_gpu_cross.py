@@ -137,6 +137,26 @@ def test_few_rows_over_long_keys(dtype, ctas, keys):
     check_backward(segments, 4, 2, 64, dtype, ctas=ctas)
 
 
+@pytest.mark.parametrize("keys", [1, 15, 16, 17, 63, 64, 65, 129, 961, 20_000])
+@pytest.mark.parametrize("hq,hkv,d", [(16, 2, 128), (16, 16, 64), (8, 8, 128), (32, 1, 64), (10, 2, 64), (3, 1, 128)])
+def test_single_tokens(hq, hkv, d, keys):
+    check_forward([(0, 1, 3, keys)], hq, hkv, d, BF16)
+    check_forward([(1, 3, 2, keys), (4, 2, 0, 0), (6, 5, 1, keys + 7)], hq, hkv, d, BF16)
+
+
+def test_every_way_of_few_rows():
+    # a cluster of each size and keys cut into parts, tiles of 16 and of 32 rows
+    seen = set()
+    for heads in ((16, 2, 128), (4, 4, 64), (2, 2, 128)):
+        for segments in ([(0, 2, 1, 900)], [(3 * i, 3, 40 * i, 30 + 9 * i) for i in range(20)], [(0, 1, 0, 30_000)],
+                         [(17 * i, 17, 200 * i, 200) for i in range(40)], [(i, 1, 100 * i, 90) for i in range(90)],
+                         [(i, 1, 0, 400) for i in range(16)]):
+            info = check_forward(segments, *heads, BF16).info
+            seen.add((info.few, info.num_slots > 0, info.unit_rows))
+    assert {s[0] for s in seen} >= {0, 1, 2, 4, 8} and {s[2] for s in seen} >= {16, 32}, seen
+    assert (1, True) in {s[:2] for s in seen}, seen
+
+
 def test_document_of_many_states():
     check_forward([(0, 24, 7, 50_003)], 16, 2, 128, BF16)
 
