@@ -29,6 +29,9 @@ constexpr uint32_t kTmemCols = 512;
 constexpr int kPanel = 128 * 128;      // [128 rows][64 bf16]
 constexpr int kBlk = PADOC_CROSS_BLOCK;
 constexpr int kKT = PADOC_CROSS_KEY_TILE;
+// V tails that may have landed before a softmax warp has waited for the first of them: of the unit that it is in and,
+// as a unit is announced once every warp has read the one two before it, of two more.
+constexpr int kTails = 3;
 
 template <int D>
 struct Cfg {
@@ -48,8 +51,8 @@ struct Cfg {
         B_UEMPTY = 20,                  // [slot], one arrival per reading warp
         B_NEXT = 22,                    // the launch control's answer
         B_FINAL = 23,                   // [tile]
-        B_VTAIL = 25,                   // a unit's last V tile, where keys end inside it
-        B_KFULL = 26,                   // [stage]
+        B_VTAIL = 25,                   // [tail % 3]: a unit's last V tile, where keys end inside it
+        B_KFULL = 28,                   // [stage]
         B_KEMPTY = B_KFULL + kStages,   // [stage], one arrival per tile
         B_VFULL = B_KEMPTY + kStages,   // [stage]
         B_VEMPTY = B_VFULL + kStages,   // [stage], one arrival per tile
@@ -230,7 +233,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     uint8_t *vb = sv + s * kTile;
                     // a tail completes on a barrier of its own: the softmax warps zero its rows past the end
                     const bool tail = u.nk - j * kKT < kKT;
-                    const uint32_t vbar = bar(tail ? (int)C::B_VTAIL : C::B_VFULL + s);
+                    const uint32_t vbar = bar(tail ? C::B_VTAIL + tails % kTails : C::B_VFULL + s);
                     if (tail) {
                         mbar_arrive(bar(C::B_VFULL + s));
                         ++tails;
@@ -258,7 +261,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 if (nq[i]) mbar_wait_bounded(bar(C::B_QFULL + i), (nq[i] - 1) & 1, a.err, 127);
             for (int t = max(tk - kStages, 0); t < tk; ++t)
                 mbar_wait_bounded(bar(C::B_KFULL + t % kStages), (t / kStages) & 1, a.err, 128);
-            if (tails) mbar_wait_bounded(bar(C::B_VTAIL), (tails - 1) & 1, a.err, 127);
+            for (int t = max(tails - kTails, 0); t < tails; ++t)
+                mbar_wait_bounded(bar(C::B_VTAIL + t % kTails), (t / kTails) & 1, a.err, 127);
             for (int t = max(tv - kStages, 0); t < tv; ++t)
                 mbar_wait_bounded(bar(C::B_VFULL + t % kStages), (t / kStages) & 1, a.err, 129);
         } else if (warp >= 9 && warp < 11) {
@@ -343,14 +347,18 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
         };
         int t_tile = 0, ring = 0, n = 0, tails = 0;   // this tile's K tiles, all units', units read, V tails passed
+        auto wait_tail = [&](int site) {
+            const int t = tails++;
+            return wait_all(C::B_VTAIL + t % kTails, (t / kTails) & 1, site);
+        };
         Unit next = {};
         auto next_of_tile = [&]() {
             for (;;) {
                 if (!read_unit(n++, next, 139)) return false;
                 if (next.tiles < 0 || hi == 0 || next.two) return true;
                 ring += next.tiles;
-                // (its V tail comes by the same barrier, whose phases are waited for one by one)
-                if (next.nk % kKT != 0 && !wait_all(C::B_VTAIL, tails++ & 1, 144)) return false;
+                // (its V tail comes by the same barriers, whose phases are waited for one by one)
+                if (next.nk % kKT != 0 && !wait_tail(144)) return false;
             }
         };
         bool ok = next_of_tile();
@@ -437,8 +445,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     }
                     const bool tail = half == 0 && left < kKT;
                     if (tail) {   // V's rows past the end (both tiles' warps write the same zeros)
-                        if (!wait_all(C::B_VTAIL, tails & 1, 142)) { ok = false; break; }
-                        ++tails;
+                        if (!wait_tail(142)) { ok = false; break; }
                         uint8_t *vb = sv + ring % kStages * kTile + row * 128;
                         if (row >= left)
 #pragma unroll

@@ -176,6 +176,18 @@ def test_many_rows(hq, hkv, d):
     check_backward(segments, hq, hkv, d, BF16, poison=False)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(16, 16, 64), (16, 2, 128), (8, 8, 64)])
+@pytest.mark.parametrize("keys", [1, 70, 130, 250])
+def test_many_short_items(hq, hkv, d, keys):
+    # items of a tile or two, each ending inside one, taken one after the other by every CTA; some with one tile of rows
+    segments = [(40 * i, 40 if i % 3 else 7, keys * i % 900, keys) for i in range(150)]
+    check_forward(segments, hq, hkv, d, BF16, poison=False)
+    check_backward(segments, hq, hkv, d, BF16, poison=False)
+    segments = [(600 * i, 600, keys * i, keys) for i in range(12)]
+    check_forward(segments, hq, hkv, d, BF16, poison=False)
+    check_backward(segments, hq, hkv, d, BF16, poison=False)
+
+
 def test_many_rows_f32():
     segments = [(0, 700, 0, 400), (700, 311, 400, 300)]
     check_forward(segments, 4, 1, 64, F32)
