@@ -1585,80 +1585,109 @@ def padoc_cross_bwd_workspace_size(info: padoc_cross_plan) -> int:
     return n.value
 
 
-def _cross_heads(t, name, heads, info, device):
-    """(address, elements between rows, rows) of rows of heads, which may lie apart."""
-    c = info.cfg
-    if t.get_device() != device:
-        raise ValueError(f"{name} must be a CUDA tensor on the current device, {device}")
-    if _dtype_code(t) != c.dtype:
-        raise TypeError(f"{name} must have the plan's dtype")
-    sh = t.shape
-    if len(sh) != 3 or sh[1] != heads or sh[2] != c.head_dim:
-        raise ValueError(f"{name} must be [rows][{heads}][{c.head_dim}]")
-    s = t.stride()
-    if sh[0] and (s[2] != 1 or (heads > 1 and s[1] != c.head_dim)):
-        raise ValueError(f"{name}: a row's heads must lie behind one another")
-    return t.data_ptr(), s[0] if sh[0] > 1 else heads * c.head_dim, sh[0]
+class _CrossShape:
+    """What a cross plan's calls look up, as plain attributes (reading them from the ctypes structure costs more than
+    the checks)."""
+
+    __slots__ = ("hq", "hkv", "d", "dtype", "f32", "i32", "ref", "words", "q_width", "k_width")
+
+    def __init__(self, info):
+        import torch
+        c = info.cfg
+        self.hq, self.hkv, self.d = int(c.num_q_heads), int(c.num_kv_heads), int(c.head_dim)
+        self.dtype = torch.bfloat16 if c.dtype == PADOC_DTYPE_BF16 else torch.float32
+        self.f32, self.i32 = torch.float32, torch.int32
+        self.ref, self.words = ctypes.byref(info), int(info.plan_ints)
+        self.q_width, self.k_width = self.hq * self.d, self.hkv * self.d
+
+    def holds(self, plan_dev, device) -> bool:
+        """Whether a tensor can be the plan's words on the device."""
+        return plan_dev.get_device() == device and plan_dev.dtype is self.i32 and plan_dev.is_contiguous() and \
+            plan_dev.numel() >= self.words
 
 
-def _cross_rows(info, plan_dev, q, k, v, device):
+def _cross_shape(info: padoc_cross_plan) -> _CrossShape:
+    c = info.__dict__.get("_shape")
+    if c is None:
+        c = info._shape = _CrossShape(info)
+    return c
+
+
+def _refuse_cross(info, device, plan_dev, heads, like):
+    """Raises what is wrong with a call's tensors: heads [(tensor, name, heads)], like [(tensor, name, shape, dtype)]."""
     import torch
+    c = _cross_shape(info)
     if plan_dev.get_device() != device or plan_dev.dtype is not torch.int32 or not plan_dev.is_contiguous() or \
-            plan_dev.numel() < info.plan_ints:
+            plan_dev.numel() < c.words:
         raise ValueError("plan_dev must hold the plan's int32 words on the current device")
-    c = info.cfg
-    qp, qs, qn = _cross_heads(q, "q", c.num_q_heads, info, device)
-    kp, ks, kn = _cross_heads(k, "k", c.num_kv_heads, info, device)
-    vp, vs, vn = _cross_heads(v, "v", c.num_kv_heads, info, device)
-    if kn != vn:
-        raise ValueError("k and v must have as many rows")
-    return _CROSS_ROWS.pack(qp, kp, vp, qs, ks, vs, qn, kn)
-
-
-def _cross_like(t, name, shape, dtype, device):
-    if tuple(t.shape) != tuple(shape) or t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype} {list(shape)}")
-    return _on(t, name, device)
-
-
-def _cross_workspace(t, device):
-    if t is None:
-        return None, 0
-    return _on(t, "workspace", device), t.numel() * t.element_size()
+    for t, name, n in heads:
+        if t.get_device() != device:
+            raise ValueError(f"{name} must be a CUDA tensor on the current device, {device}")
+        if t.dtype is not c.dtype:
+            raise TypeError(f"{name} must have the plan's dtype, {c.dtype}")
+        if t.dim() != 3 or t.shape[1] != n or t.shape[2] != c.d:
+            raise ValueError(f"{name} must be [rows][{n}][{c.d}]")
+        if t.shape[0] and (t.stride(2) != 1 or (n > 1 and t.stride(1) != c.d)):
+            raise ValueError(f"{name}: a row's heads must lie behind one another")
+    for t, name, shape, dtype in like:
+        if tuple(t.shape) != tuple(shape) or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor {list(shape)} on device {device}")
+    raise ValueError("k and v, and gradients and what they are of, must have as many rows")
 
 
 def padoc_cross_attn(info: padoc_cross_plan, plan_dev, q, k, v, scale, out, lse, workspace=None, stream=None):
     """q [rows][Hq][d], k / v [key rows][Hkv][d] (rows may lie apart); out [rows][Hq][d], lse fp32 [rows][Hq], both
     contiguous; workspace: padoc_cross_workspace_size bytes (None when that is 0)."""
-    import torch
-    dev = _current_device()
-    rows = _cross_rows(info, plan_dev, q, k, v, dev)
-    o = _cross_like(out, "out", q.shape, q.dtype, dev)
-    l = _cross_like(lse, "lse", q.shape[:2], torch.float32, dev)
-    ws, n = _cross_workspace(workspace, dev)
-    _check("padoc_cross_attn", load_library().padoc_cross_attn(ctypes.byref(info), plan_dev.data_ptr(), rows, scale, o, l,
-                                                               ws, n, _stream_ptr(stream)))
+    c, dev = _cross_shape(info), _current_device()
+    dt, f32 = c.dtype, c.f32
+    qs, ks, qt, kt, vt = q.shape, k.shape, q.stride(), k.stride(), v.stride()
+    if not (len(qs) == 3 and len(ks) == 3 and qs[1] == c.hq and qs[2] == c.d and ks[1] == c.hkv and ks[2] == c.d and
+            v.shape == ks and out.shape == qs and lse.shape == qs[:2] and
+            q.dtype is dt and k.dtype is dt and v.dtype is dt and out.dtype is dt and lse.dtype is f32 and
+            q.get_device() == dev and k.get_device() == dev and v.get_device() == dev and out.get_device() == dev and
+            lse.get_device() == dev and c.holds(plan_dev, dev) and out.is_contiguous() and lse.is_contiguous() and
+            (qt[2] == 1 and (qt[1] == c.d or c.hq == 1) or not qs[0]) and
+            (kt[2] == 1 and vt[2] == 1 and (kt[1] == c.d and vt[1] == c.d or c.hkv == 1) or not ks[0])):
+        _refuse_cross(info, dev, plan_dev, ((q, "q", c.hq), (k, "k", c.hkv), (v, "v", c.hkv)),
+                      ((out, "out", q.shape, dt), (lse, "lse", q.shape[:2], f32)))
+    rows, keys = qs[0], ks[0]
+    ws, n = (None, 0) if workspace is None else (_on(workspace, "workspace", dev), workspace.nbytes)
+    st = load_library().padoc_cross_attn(
+        c.ref, plan_dev.data_ptr(),
+        _CROSS_ROWS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), qt[0] if rows > 1 else c.q_width,
+                         kt[0] if keys > 1 else c.k_width, vt[0] if keys > 1 else c.k_width, rows, keys),
+        scale, out.data_ptr(), lse.data_ptr(), ws, n, _stream_ptr(stream))
+    if st:
+        _check("padoc_cross_attn", st)
 
 
 def padoc_cross_attn_bwd(info: padoc_cross_plan, plan_dev, q, k, v, out, dout, lse, scale, dq, dk, dv, workspace=None,
                          stream=None):
     """Gradients of padoc_cross_attn: q, k, v, dq, dk, dv rows that may lie apart; out, dout, lse contiguous."""
-    import torch
-    dev = _current_device()
-    rows = _cross_rows(info, plan_dev, q, k, v, dev)
-    o = _cross_like(out, "out", q.shape, q.dtype, dev)
-    g = _cross_like(dout, "dout", q.shape, q.dtype, dev)
-    l = _cross_like(lse, "lse", q.shape[:2], torch.float32, dev)
-    if dq.shape != q.shape or dk.shape != k.shape or dv.shape != v.shape:
-        raise ValueError("dq, dk and dv must have the shapes of q, k and v")
-    c = info.cfg
-    qp, qs, _ = _cross_heads(dq, "dq", c.num_q_heads, info, dev)
-    kp, ks, _ = _cross_heads(dk, "dk", c.num_kv_heads, info, dev)
-    vp, vs, _ = _cross_heads(dv, "dv", c.num_kv_heads, info, dev)
-    ws, n = _cross_workspace(workspace, dev)
-    _check("padoc_cross_attn_bwd",
-           load_library().padoc_cross_attn_bwd(ctypes.byref(info), plan_dev.data_ptr(), rows, o, g, l, scale,
-                                               _CROSS_GRADS.pack(qp, kp, vp, qs, ks, vs), ws, n, _stream_ptr(stream)))
+    c, dev = _cross_shape(info), _current_device()
+    dt, f32 = c.dtype, c.f32
+    qs, ks = q.shape, k.shape
+    ok = (len(qs) == 3 and len(ks) == 3 and qs[1] == c.hq and qs[2] == c.d and ks[1] == c.hkv and ks[2] == c.d and
+          v.shape == ks and dk.shape == ks and dv.shape == ks and dq.shape == qs and out.shape == qs and dout.shape == qs and
+          lse.shape == qs[:2] and lse.dtype is f32 and lse.get_device() == dev and c.holds(plan_dev, dev) and
+          out.is_contiguous() and dout.is_contiguous() and lse.is_contiguous())
+    for t in (q, k, v, out, dout, dq, dk, dv):
+        s = t.stride()
+        ok = ok and t.dtype is dt and t.get_device() == dev and (s[2] == 1 and (s[1] == c.d or t.shape[1] == 1) or not t.shape[0])
+    if not ok:
+        _refuse_cross(info, dev, plan_dev, ((q, "q", c.hq), (k, "k", c.hkv), (v, "v", c.hkv), (dq, "dq", c.hq),
+                                            (dk, "dk", c.hkv), (dv, "dv", c.hkv)),
+                      ((out, "out", q.shape, dt), (dout, "dout", q.shape, dt), (lse, "lse", q.shape[:2], f32)))
+    rows, keys = qs[0], ks[0]
+    qw = lambda t: t.stride(0) if rows > 1 else c.q_width
+    kw = lambda t: t.stride(0) if keys > 1 else c.k_width
+    ws, n = (None, 0) if workspace is None else (_on(workspace, "workspace", dev), workspace.nbytes)
+    st = load_library().padoc_cross_attn_bwd(
+        c.ref, plan_dev.data_ptr(), _CROSS_ROWS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), qw(q), kw(k), kw(v), rows, keys),
+        out.data_ptr(), dout.data_ptr(), lse.data_ptr(), scale,
+        _CROSS_GRADS.pack(dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), qw(dq), kw(dk), kw(dv)), ws, n, _stream_ptr(stream))
+    if st:
+        _check("padoc_cross_attn_bwd", st)
 
 
 def padoc_selftest_tcgen05(a, bk, v, c1, c2, c3, stream=None):

@@ -196,7 +196,7 @@ def test_calls_are_refused_before_any_launch(lib):
     for name in ("q", "k", "v", "out", "lse"):
         assert fwd(**{name: None}) == 1
         assert fwd(**{name: A + 2}) == 1
-    assert fwd(qs=2040) == 1 and fwd(qs=2052) == 1 and fwd(ks=128) == 1 and fwd(vs=0) == 1 and fwd(ks=-256) == 1
+    assert fwd(qs=2040) == 1 and fwd(qs=2050) == 1 and fwd(ks=128) == 1 and fwd(vs=0) == 1 and fwd(ks=-256) == 1
     assert fwd(qn=0) == 1 and fwd(kn=960) == 1 and fwd(kn=2 ** 31) == 1
     assert fwd(scale=0.0) == 1 and fwd(scale=math.nan) == 1 and fwd(scale=math.inf) == 1
     assert fwd(ws=None) == 1 and fwd(ws=64 * A + 16) == 1 and fwd(n=need - 1) == 3
@@ -204,7 +204,7 @@ def test_calls_are_refused_before_any_launch(lib):
     for name in ("q", "k", "v", "out", "dout", "lse", "dq", "dk", "dv"):
         assert bwd(**{name: None}) == 1
         assert bwd(**{name: A + 2}) == 1
-    assert bwd(dqs=2040) == 1 and bwd(dks=128) == 1 and bwd(dvs=260) == 1 and bwd(kn=960) == 1
+    assert bwd(dqs=2040) == 1 and bwd(dks=128) == 1 and bwd(dvs=258) == 1 and bwd(kn=960) == 1
     assert bwd(ws=None) == 1 and bwd(n=bneed - 1) == 3
     assert bwd(dk=9 * A) == 1 and bwd(dv=8 * A + 512 * 500) == 1 and bwd(dq=A) == 1 and bwd(dk=4 * A) == 1 and bwd(dq=6 * A) == 1
     # side by side in one buffer: not an overlap, but rows reaching into the neighbour's are
