@@ -138,6 +138,19 @@ __device__ __forceinline__ void st_cluster_v4(uint32_t addr, int4 v)
                  : "memory");
 }
 
+__device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
 // Whether the phase with the given parity has completed; never suspends.
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
 {

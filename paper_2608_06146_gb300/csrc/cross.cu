@@ -187,22 +187,24 @@ struct Simt {
     static __device__ __forceinline__ void add_product(const float *s, const float *y, float (&acc)[4][D / 16])
     {
         const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-#pragma unroll 4
-        for (int k = 0; k < kB; ++k) {
-            float w[4];
+#pragma unroll 2
+        for (int k = 0; k < kB; k += 4) {
+            float w[4][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = s[(4 * ty + i) * PS + k];
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(w[i]) = *reinterpret_cast<const float4 *>(s + (4 * ty + i) * PS + k);
 #pragma unroll
-            for (int j = 0; j < D / 64; ++j) {
-                const float4 b = *reinterpret_cast<const float4 *>(y + k * P + 64 * j + 4 * tx);
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    acc[i][4 * j] = fmaf(w[i], b.x, acc[i][4 * j]);
-                    acc[i][4 * j + 1] = fmaf(w[i], b.y, acc[i][4 * j + 1]);
-                    acc[i][4 * j + 2] = fmaf(w[i], b.z, acc[i][4 * j + 2]);
-                    acc[i][4 * j + 3] = fmaf(w[i], b.w, acc[i][4 * j + 3]);
+                for (int j = 0; j < D / 64; ++j) {
+                    const float4 b = *reinterpret_cast<const float4 *>(y + (k + e) * P + 64 * j + 4 * tx);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        acc[i][4 * j] = fmaf(w[i][e], b.x, acc[i][4 * j]);
+                        acc[i][4 * j + 1] = fmaf(w[i][e], b.y, acc[i][4 * j + 1]);
+                        acc[i][4 * j + 2] = fmaf(w[i][e], b.z, acc[i][4 * j + 2]);
+                        acc[i][4 * j + 3] = fmaf(w[i][e], b.w, acc[i][4 * j + 3]);
+                    }
                 }
-            }
         }
     }
     static __device__ __forceinline__ void zero(float (&acc)[4][D / 16])
@@ -386,14 +388,15 @@ __global__ void __launch_bounds__(256) cross_dq_simt_kernel(const padoc_cross_ar
     }
 }
 
-// dK and dV of 64 keys: the sums over every block of rows that sees them, in the covers' order.
-template <int D>
+// dK and dV of 64 keys: the sums over every block of rows that sees them, in the covers' order. A cluster of NC CTAs
+// shares out the blocks; the CTAs' sums are added through distributed shared memory in rank order.
+template <int D, int NC>
 __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_args a)
 {
     using S = Simt<D>;
     extern __shared__ __align__(16) float sm[];
     float *sq = sm, *sg = sq + S::kTile, *sk = sg + S::kTile, *sv = sk + S::kTile, *sp = sv + S::kTile, *sd = sp + kB * S::PS;
-    const int half = blockIdx.x & 1, unit = blockIdx.x >> 1, g = unit % a.hkv, i0 = unit / a.hkv;
+    const int rank = blockIdx.x % NC, part = blockIdx.x / NC, half = part & 1, unit = part >> 1, g = unit % a.hkv, i0 = unit / a.hkv;
     padoc_cross_key_tile t;
     if (i0 < a.num_tiles) t = a.tiles[i0];
     else {
@@ -402,7 +405,7 @@ __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_a
         t.cover = t.ncover = t.steps = 0;
     }
     const int k0 = t.k0 + half * kB, nk = min(kB, t.nk - half * kB), ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-    if (nk <= 0) return;
+    if (nk <= 0) return;   // (the whole cluster)
     float ak[4][D / 16], av[4][D / 16];
     S::zero(ak);
     S::zero(av);
@@ -413,10 +416,15 @@ __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_a
         S::load(sk, [&](int r) { return key_row(a.k, a.k_stride, r); });
         S::load(sv, [&](int r) { return key_row(a.v, a.v_stride, r); });
     }
-    for (int ci = 0; ci < t.ncover; ++ci) {
+    // this CTA's blocks of the tile's: from .. to
+    const int from = (int)((int64_t)t.steps * rank / NC), to = (int)((int64_t)t.steps * (rank + 1) / NC);
+    int first = 0;   // of the cover
+    for (int ci = 0; ci < t.ncover && first < to; ++ci) {
         const padoc_cross_cover c = a.covers[t.cover + ci];
+        const int b0 = max(from - first, 0), b1 = min(c.nsub, to - first);
+        first += c.nsub;
         if (c.k0 >= k0 + nk || c.k0 + c.nk <= k0) continue;
-        for (int b = 0; b < c.nsub; ++b) {
+        for (int b = b0; b < b1; ++b) {
             auto heads_row = [&](const void *base, int64_t stride, int r) -> const float * {
                 int token, head;
                 if (!cross_row(a, c.tok, c.ntok, b * kB + r, token, head)) return nullptr;
@@ -447,16 +455,43 @@ __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_a
             S::add_product(sd, sq, ak);
         }
     }
+    auto write = [&](int r, int c, float4 xk, float4 xv) {
+        store4((float *)a.dk + (size_t)(k0 + r) * a.dk_stride + (size_t)g * D + c,
+               make_float4(xk.x * a.scale, xk.y * a.scale, xk.z * a.scale, xk.w * a.scale));
+        store4((float *)a.dv + (size_t)(k0 + r) * a.dv_stride + (size_t)g * D + c, xv);
+    };
+    auto cols = [](const float (&x)[D / 16], int j) { return make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]); };
+    if constexpr (NC == 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = 4 * ty + i;
-        if (r >= nk) continue;
-        float *dk = (float *)a.dk + (size_t)(k0 + r) * a.dk_stride + (size_t)g * D, *dv = (float *)a.dv + (size_t)(k0 + r) * a.dv_stride + (size_t)g * D;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
-            store4(dk + 64 * j + 4 * tx, make_float4(ak[i][4 * j] * a.scale, ak[i][4 * j + 1] * a.scale, ak[i][4 * j + 2] * a.scale, ak[i][4 * j + 3] * a.scale));
-            store4(dv + 64 * j + 4 * tx, make_float4(av[i][4 * j], av[i][4 * j + 1], av[i][4 * j + 2], av[i][4 * j + 3]));
+            for (int j = 0; j < D / 64; ++j)
+                if (4 * ty + i < nk) write(4 * ty + i, 64 * j + 4 * tx, cols(ak[i], j), cols(av[i], j));
+    } else {
+        __syncthreads();
+        float *xk = sm, *xv = sm + S::kTile;   // [64][P] each, over the tiles
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) {
+                *reinterpret_cast<float4 *>(xk + (4 * ty + i) * S::P + 64 * j + 4 * tx) = cols(ak[i], j);
+                *reinterpret_cast<float4 *>(xv + (4 * ty + i) * S::P + 64 * j + 4 * tx) = cols(av[i], j);
+            }
+        cluster_sync();
+        const int mine = (nk - rank + NC - 1) / NC;   // rows rank, rank + NC, ..
+        for (int i = threadIdx.x; i < mine * (D / 4); i += 256) {
+            const int r = rank + i / (D / 4) * NC, c = i % (D / 4) * 4;
+            float4 yk = make_float4(0.f, 0.f, 0.f, 0.f), yv = yk;
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                const float4 u = ld_cluster_v4(cluster_map(smem_u32(xk + r * S::P + c), n));
+                const float4 v = ld_cluster_v4(cluster_map(smem_u32(xv + r * S::P + c), n));
+                yk = make_float4(yk.x + u.x, yk.y + u.y, yk.z + u.z, yk.w + u.w);
+                yv = make_float4(yv.x + v.x, yv.y + v.y, yv.z + v.z, yv.w + v.w);
+            }
+            write(r, c, yk, yv);
         }
+        cluster_sync();   // no CTA leaves while another reads its shared memory
     }
 }
 
@@ -470,25 +505,44 @@ padoc_status run_fwd_simt(const padoc_cross_args &a, cudaStream_t cs)
     return padoc_launch_status();
 }
 
-template <int D>
-padoc_status run_bwd_simt(const padoc_cross_args &a, cudaStream_t cs)
+template <int D, int NC>
+padoc_status run_dkv_simt(const padoc_cross_args &a, cudaStream_t cs)
 {
-    constexpr int dq_bytes = (4 * Simt<D>::kTile + kB * Simt<D>::PS + 2 * kB) * 4;
-    constexpr int dkv_bytes = (4 * Simt<D>::kTile + 2 * kB * Simt<D>::PS) * 4;
+    constexpr int bytes = (4 * Simt<D>::kTile + 2 * kB * Simt<D>::PS) * 4;
+    auto kernel = cross_dkv_simt_kernel<D, NC>;
+    if (const padoc_status st = padoc_set_max_smem((const void *)kernel, bytes)) return st;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)((a.num_tiles + a.tail_tiles) * a.hkv * 2 * NC));
+    lc.blockDim = dim3(256);
+    lc.dynamicSmemBytes = bytes;
+    lc.stream = cs;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = NC;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = NC > 1 ? 1 : 0;
+    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, a));
+    return padoc_launch_status();
+}
+
+template <int D>
+padoc_status run_bwd_simt(const padoc_cross_args &a, int cluster, cudaStream_t cs)
+{
+    constexpr int bytes = (4 * Simt<D>::kTile + kB * Simt<D>::PS + 2 * kB) * 4;
     auto dq = cross_dq_simt_kernel<D>;
-    auto dkv = cross_dkv_simt_kernel<D>;
-    padoc_status st = padoc_set_max_smem((const void *)dq, dq_bytes);
-    if (st == PADOC_OK) st = padoc_set_max_smem((const void *)dkv, dkv_bytes);
-    if (st != PADOC_OK) return st;
     if (a.num_units) {
-        dq<<<(unsigned)(a.num_units * PADOC_CROSS_DQ_BLOCKS), 256, dq_bytes, cs>>>(a);
-        if ((st = padoc_launch_status()) != PADOC_OK) return st;
+        if (const padoc_status st = padoc_set_max_smem((const void *)dq, bytes)) return st;
+        dq<<<(unsigned)(a.num_units * PADOC_CROSS_DQ_BLOCKS), 256, bytes, cs>>>(a);
+        if (const padoc_status st = padoc_launch_status()) return st;
     }
-    if (a.num_tiles + a.tail_tiles) {
-        dkv<<<(unsigned)((a.num_tiles + a.tail_tiles) * a.hkv * 2), 256, dkv_bytes, cs>>>(a);
-        st = padoc_launch_status();
+    if (!(a.num_tiles + a.tail_tiles)) return PADOC_OK;
+    switch (cluster) {
+        case 8: return run_dkv_simt<D, 8>(a, cs);
+        case 4: return run_dkv_simt<D, 4>(a, cs);
+        case 2: return run_dkv_simt<D, 2>(a, cs);
+        default: return run_dkv_simt<D, 1>(a, cs);
     }
-    return st;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -682,7 +736,7 @@ extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const
     a.dsum = a.neg_lse2 + stats;
     a.part = a.dsum + stats;
     cudaStream_t cs = (cudaStream_t)stream;
-    if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_bwd_simt<64>(a, cs) : run_bwd_simt<128>(a, cs);
+    if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_bwd_simt<64>(a, info->cluster, cs) : run_bwd_simt<128>(a, info->cluster, cs);
     else st = padoc_cross_launch_bwd_tc(a, c.head_dim, info->cluster, cs);
     if (st != PADOC_OK) return st;
     if (!a.num_merges) return PADOC_OK;

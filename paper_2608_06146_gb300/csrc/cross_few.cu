@@ -33,19 +33,6 @@ struct Few {
     static_assert((size_t)(kWarps + 1) * kRows * (kPitch + 2) * 4 <= kRing, "");
 };
 
-__device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float ld_cluster(uint32_t addr)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-
 template <int D, int kTiles, int NC>
 __global__ void __launch_bounds__(32 * kWarps, Few<D, kTiles>::kCtas)
 cross_few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)

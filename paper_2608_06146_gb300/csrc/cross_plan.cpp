@@ -254,9 +254,8 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
     info.cfg = *cfg;
     info.num_segments = n;
     const int32_t hkv = cfg->num_kv_heads, group = cfg->num_q_heads / hkv, block = PADOC_CROSS_BLOCK / group;
-    // fp32 runs a CTA per 64 rows, a few of them on an SM: about two units' worth at a time
     const int32_t sms = cfg->ctas ? cfg->ctas : padoc_default_ctas();
-    const int32_t lanes = cfg->dtype == PADOC_DTYPE_F32 ? std::max(1, sms / 2) : sms;
+    const bool f32 = cfg->dtype == PADOC_DTYPE_F32;
 
     int64_t q_end = 0, k_end = 0, subs = 0, blocks = 0;
     std::vector<int32_t> first_sub((size_t)n, 0);
@@ -293,23 +292,29 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
                     for (int32_t g = 0; g < hkv; ++g)
                         merges.push_back({seg[i].q_begin + t, std::min(per, seg[i].q_len - t), 0, 0, g, {0, 0, 0}});
     };
-    const Cuts cuts = cfg->dtype == PADOC_DTYPE_BF16 ? kLists : kPieces;
+    const Cuts cuts = f32 ? kPieces : kLists;
+    // fp32: a CTA per 64 rows, 5 us a 64-key step with 64 dims and 8 with 128 (the backward's half as long again)
+    const Costs simt = {0.5f, 0.2f, 0.6f, 0.002f, 1.f, 64, 1};
 
     // Forward. Times in us: of two 128-row tiles' steps of 128 keys, and for few rows of a 64-key tile's bytes at the
     // SM's share of the memory bandwidth (45 KB a us), which its CTAs share.
     int32_t per = PADOC_CROSS_UNIT_BLOCKS * block;
     {
         const Costs tc = {1.8f, 1.5f, 2.f, 0.012f, 0.65f, PADOC_CROSS_KEY_TILE, 1};
-        const float time = 1.65f * plan_work(chunks_of(per, tc), hkv, lanes, tc, cuts, b.fwd);
+        const Costs &k = f32 ? simt : tc;
+        const int32_t lanes = f32 ? std::max(1, sms / PADOC_CROSS_UNIT_BLOCKS) : sms;
+        const float time = 1.65f * plan_work(chunks_of(per, k), hkv, lanes, k, cuts, b.fwd);
         info.unit_rows = PADOC_CROSS_UNIT_BLOCKS * PADOC_CROSS_BLOCK;
-        if (cfg->dtype == PADOC_DTYPE_BF16 && group <= PADOC_CROSS_FEW_ROWS && !b.fwd.units.empty())
+        if (!f32 && group <= PADOC_CROSS_FEW_ROWS && !b.fwd.units.empty())
             plan_few(seg, n, group, cfg->head_dim, hkv, sms, time, chunks_of, b.fwd, info, per);
     }
     empty_rows(per, b.fwd.merges);
 
     if (cfg->backward) {
         const Costs bwd = {6.f, 2.f, 6.f, 0.018f, 1.f, PADOC_CROSS_DQ_STEP, 4};   // (a step of a tile lasts about 0.55 us)
-        plan_work(chunks_of(PADOC_CROSS_DQ_BLOCKS * block, bwd), hkv, lanes, bwd, cuts, b.dq);
+        const Costs &k = f32 ? simt : bwd;
+        const int32_t lanes = f32 ? std::max(1, sms / PADOC_CROSS_DQ_BLOCKS) : sms;
+        plan_work(chunks_of(PADOC_CROSS_DQ_BLOCKS * block, k), hkv, lanes, k, cuts, b.dq);
         empty_rows(PADOC_CROSS_DQ_BLOCKS * block, b.dq.merges);
 
         // Key tiles: ranges that overlap are tiled together, from the first one's begin; between them lie keys that
@@ -350,10 +355,12 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
         info.num_subs = (int32_t)subs;
 
         // The CTAs that share a key tile's steps: few tiles seen by many rows leave most of the chip idle, but each
-        // sharing costs its exchange (in steps of 0.8 us).
-        static const float start[] = {6.f, 12.f, 13.f, 16.f};
+        // sharing costs its exchange (in steps of 0.8 us)
+        // (fp32: in steps of 12 us, two clusters a tile).
+        static const float start_tc[] = {6.f, 12.f, 13.f, 16.f}, start_simt[] = {0.4f, 0.6f, 0.6f, 0.7f};
+        const float *start = f32 ? start_simt : start_tc;
         float best = 0.f;
-        for (int i = 0; i < (cfg->head_dim == 128 ? 4 : 3); ++i) {
+        for (int i = 0; i < (f32 || cfg->head_dim == 128 ? 4 : 3); ++i) {
             const int nc = 1 << i;
             std::vector<float> cost;
             for (const padoc_cross_key_tile &t : b.tiles)
