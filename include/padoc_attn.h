@@ -966,7 +966,9 @@ typedef struct {
     int32_t num_subs;        /* blocks of 64 packed rows whose statistics the backward keeps, for each KV head */
     int32_t num_key_tiles;   /* backward: key tiles of at most 128 rows */
     int32_t num_covers;      /* (key tile, segment that sees some of it) pairs */
-    int32_t cluster;         /* CTAs that share a key tile in the backward */
+    int32_t cluster;         /* CTAs of a cluster that share a key tile in the backward */
+    int32_t parts;           /* or CTAs that share it and leave partial sums (1: none do) */
+    int32_t reserved;
     int64_t pairs;           /* visible (query row, key row) pairs */
     int64_t plan_ints;       /* int32 words in the plan blob */
     int64_t off_units;       /* offsets (int32 words) of the blob's arrays */

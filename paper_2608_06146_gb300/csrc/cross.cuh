@@ -19,6 +19,8 @@ struct padoc_cross_args {
     void *o, *dq, *dk, *dv;
     float *lse;
     float *part, *part_lse;                    // partial results
+    float *part_dkv;                           // of key tiles: [tile][Hkv][parts][128][dV | dK]
+    int32_t parts;                             // CTAs that share a key tile and leave their sums there (1: none do)
     float *neg_lse2, *dsum;                    // -lse * log2(e) and rowsum(dO * O): [Hkv][subs][64]
     int32_t unit_rows;                         // packed rows of a forward or dq item, and of its partial result
     int32_t num_units, num_ctas, num_merges, max_parts, num_tiles, num_subs;

@@ -7,7 +7,9 @@
 //   them (parts are joined by a later kernel). It walks 64-key steps: S = Q K^T (Q in tensor memory), dP = dO V^T (dO in
 //   shared memory), dS as bf16 over S, dQ += dS K. It also writes -lse2 and D of its rows for the other pass. A
 //   running CTA takes over units not yet launched (cluster launch control).
-// dK/dV pass: a unit is a tile of at most 128 keys and a KV head, run by a cluster of 1 to 8 CTAs that share out its steps and add their fp32 sums through distributed shared memory, in rank order. A step is a
+// dK/dV pass: a unit is a tile of at most 128 keys and a KV head, run by a cluster of 1 to 8
+//   CTAs that share out its steps and add their fp32 sums through distributed shared memory, in rank order (or by more
+//   CTAs whose sums a later kernel adds). A step is a
 //   block of 64 packed rows: S^T = K Q^T, dP^T = V dO^T (V in tensor memory), P^T and dS^T as bf16 over S^T, dV += P^T dO,
 //   dK += dS^T Q. Query heads of the group and the segments that share keys are thus summed in a fixed order.
 //
@@ -34,7 +36,6 @@
 namespace {
 
 constexpr int kThreads = 384;
-constexpr uint32_t kTmemCols = 512;
 constexpr int kBlk = PADOC_CROSS_BLOCK;
 
 __device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, int *err, int site, volatile int *abort_flag)
@@ -61,6 +62,9 @@ __device__ __forceinline__ void store_row_bf16(__nv_bfloat16 *dst, const float (
         *reinterpret_cast<uint4 *>(dst + i) = w;
     }
 }
+
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld32(taddr, r); }
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) { tmem_ld16(taddr, r); }
 
 // A thread's 16-byte pieces of a row of D / 2 dims, its column half of the row (panels of 64 dims, 128-byte swizzle),
 // and the same as the A operand in tensor memory.
@@ -91,7 +95,14 @@ struct HalfRow {
 namespace dkv {
 constexpr int kKT = PADOC_CROSS_KEY_TILE;   // 128 keys: the M of every MMA
 constexpr int kStages = 4;
-constexpr uint32_t kColS = 0, kColDP = 128, kColV = 192, kColAcc = 256;   // kColS: two buffers; kColAcc: dV, then dK
+// Tensor memory: S (two buffers), dP, V as an A operand, dV and dK. With 64 dims two CTAs share an SM, which hides one's
+// hand-overs under the other's work better than a second S buffer does: S, dP, dV and dK in 256 columns, V from
+// shared memory.
+template <int D>
+struct Cols {
+    static constexpr int kCtas = D == 64 ? 2 : 1, kBuffers = D == 64 ? 1 : 2;
+    static constexpr uint32_t kS = 0, kDP = 64 * kBuffers, kV = 192, kAcc = 2 * kDP, kAll = 512 / kCtas;
+};
 constexpr int kKPanel = kKT * 128;           // [128 rows][64 bf16]
 constexpr int kQPanel = kBlk * 128;          // [64 rows][64 bf16]
 constexpr int kAuxBytes = 2 * kBlk * 4;      // -lse2[64], D[64]
@@ -99,9 +110,9 @@ enum {
     B_KV = 0,
     B_QFULL = 1,                  // [stage]
     B_QEMPTY = 1 + kStages,       // [stage]
-    B_SFULL = 1 + 2 * kStages,    // [step parity]
-    B_PFULL = 3 + 2 * kStages,    // [step parity], an arrival per softmax warp
-    B_ACC = 5 + 2 * kStages,      // [step parity]: the step's accumulating MMAs are done
+    B_SFULL = 1 + 2 * kStages,    // [S buffer]
+    B_PFULL = 3 + 2 * kStages,    // [S buffer], an arrival per softmax warp
+    B_ACC = 5 + 2 * kStages,      // [S buffer]: the step's accumulating MMAs are done
     B_DPFREE = 7 + 2 * kStages,   // dP is read (an arrival per softmax warp)
     B_VT = 8 + 2 * kStages,       // V is in tensor memory (an arrival per softmax warp)
     B_FINAL = 9 + 2 * kStages,    // [issuing warp]
@@ -134,14 +145,17 @@ struct Steps {
     __device__ __forceinline__ int tokens(const padoc_cross_args &a) const { return min(a.block_tokens, c.ntok - b * a.block_tokens); }
 };
 
-// NC: the CTAs of a unit's cluster.
-template <int D, int NC>
-__global__ void __launch_bounds__(kThreads, 1)
+// NC: the CTAs of a unit's cluster. kParts: the steps are shared out over a.parts CTAs that know nothing of one another;
+// their fp32 sums go to the workspace, where cross_dkv_sum_kernel adds them in order (few tiles that many rows see).
+template <int D, int NC, bool kParts>
+__global__ void __launch_bounds__(kThreads, dkv::Cols<D>::kCtas)
 cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap gmap,
                  const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
 {
     using namespace dkv;
-    constexpr int kPanels = D / 64, kKTile = kPanels * kKPanel, kQTile = kPanels * kQPanel;
+    using T = Cols<D>;
+    constexpr int kPanels = D / 64, kKTile = kPanels * kKPanel, kQTile = kPanels * kQPanel, kBuf = T::kBuffers;
+    constexpr uint32_t kColS = T::kS, kColDP = T::kDP, kColV = T::kV, kColAcc = T::kAcc;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t *sk = smem;
@@ -156,7 +170,9 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (a value the compiler knows to be warp-uniform)
     // the cluster's unit, and this CTA's steps of it: ub .. ub + nu - 1
-    const int unit = (int)blockIdx.x / NC, rank = (int)blockIdx.x % NC, g = unit % a.hkv, ti = unit / a.hkv;
+    static_assert(!kParts || NC == 1, "");
+    const int share = kParts ? a.parts : NC;
+    const int unit = (int)blockIdx.x / share, rank = (int)blockIdx.x % share, g = unit % a.hkv, ti = unit / a.hkv;
     padoc_cross_key_tile t;
     if (ti < a.num_tiles) {
         t = a.tiles[ti];
@@ -177,7 +193,11 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         return;
     }
     const int k0 = __shfl_sync(0xffffffffu, t.k0, 0), steps = __shfl_sync(0xffffffffu, t.steps, 0);
-    const int ub = (int)((int64_t)steps * rank / NC), nu = (int)((int64_t)steps * (rank + 1) / NC) - ub;
+    const int ub = (int)((int64_t)steps * rank / share), nu = (int)((int64_t)steps * (rank + 1) / share) - ub;
+    if (kParts && nu == 0) {   // (not read either)
+        pdl_wait_prerequisite();
+        return;
+    }
     const int used = a.block_tokens * a.group;   // rows of a block that its copies write
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
 
@@ -195,7 +215,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         fence_proxy_async_smem();
     }
     if (warp == 9) {
-        tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+        tmem_alloc(smem_u32(tmem_slot), T::kAll);
         tmem_relinquish();
     }
     tc_fence_before();
@@ -259,17 +279,18 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 bool ok = wait_w(B_KV, 0, 160);
                 for (int u = 0; ok && u < nu; ++u) {
                     const int s = u % kStages;
-                    const uint32_t b = (uint32_t)(u & 1) * 64;
-                    ok = wait_w(B_QFULL + s, (u / kStages) & 1, 161) && (u < 2 || wait_w(B_ACC + (u & 1), ((u >> 1) - 1) & 1, 163));
+                    const uint32_t b = (uint32_t)(u % kBuf) * 64;
+                    ok = wait_w(B_QFULL + s, (u / kStages) & 1, 161) && (u < kBuf || wait_w(B_ACC + u % kBuf, (u / kBuf - 1) & 1, 163));
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t dq = umma_desc_sw128(smem_u32(sq + s * kQTile), 16, 1024);
                     if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kKPanel, kQPanel>(tmem + kColS + b, dK, dq, idS);
                     else umma_bf16_ss_k64_warp(tmem + kColS + b, dK, dq, idS);
-                    umma_commit_warp(bar(B_SFULL + (u & 1)));
+                    umma_commit_warp(bar(B_SFULL + u % kBuf));
                 }
             } else if (warp == 11) {
-                bool ok = wait_w(B_VT, 0, 166);
+                const uint64_t dV = umma_desc_sw128(smem_u32(sv), 16, 1024);   // (64 dims)
+                bool ok = D == 64 ? wait_w(B_KV, 0, 166) : wait_w(B_VT, 0, 166);
                 for (int u = 0; ok && u < nu; ++u) {
                     const int s = u % kStages;
                     ok = wait_w(B_QFULL + s, (u / kStages) & 1, 167) && (u == 0 || wait_w(B_DPFREE, (u - 1) & 1, 165));
@@ -277,22 +298,22 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     tc_fence_after();
                     const uint64_t dg = umma_desc_sw128(smem_u32(sg + s * kQTile), 16, 1024);
                     if constexpr (D == 128) umma_bf16_ts_k128_warp<kQPanel>(tmem + kColDP, tmem + kColV, dg, idS);
-                    else umma_bf16_ts_k64_warp(tmem + kColDP, tmem + kColV, dg, idS);
-                    umma_commit_warp(bar(B_SFULL + (u & 1)));
+                    else umma_bf16_ss_k64_warp(tmem + kColDP, dV, dg, idS);
+                    umma_commit_warp(bar(B_SFULL + u % kBuf));
                 }
             } else {
                 bool ok = true;
                 for (int u = 0; ok && u < nu; ++u) {
                     const int s = u % kStages;
-                    const uint32_t b = (uint32_t)(u & 1) * 64;
-                    if (!(ok = wait_w(B_PFULL + (u & 1), (u >> 1) & 1, 162))) break;
+                    const uint32_t b = (uint32_t)(u % kBuf) * 64;
+                    if (!(ok = wait_w(B_PFULL + u % kBuf, (u / kBuf) & 1, 162))) break;
                     tc_fence_after();
                     // the step's Q and dO as MN-major B operands (N = head dim, K = the 64 rows)
                     const uint64_t gmn = umma_desc_sw128(smem_u32(sg + s * kQTile), kQPanel, 1024);
                     const uint64_t qmn = umma_desc_sw128(smem_u32(sq + s * kQTile), kQPanel, 1024);
                     umma_bf16_ts_k64_mn_warp<1, slice_col(1), slice_col(2), slice_col(3)>(tmem + kColAcc, tmem + kColS + b, gmn, idAcc, u > 0);
                     umma_bf16_ts_k64_mn_warp<1, slice_col(1), slice_col(2), slice_col(3)>(tmem + kColAcc + D, tmem + kColS + b + 16, qmn, idAcc, u > 0);
-                    umma_commit_warp(bar(B_ACC + (u & 1)));
+                    umma_commit_warp(bar(B_ACC + u % kBuf));
                     umma_commit_warp(bar(B_QEMPTY + s));
                 }
             }
@@ -307,7 +328,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
         };
         bool ok = true;
-        if (nu > 0 && (ok = wait_all(B_KV, 0, 173))) {   // V's rows into tensor memory, half of the dims a thread
+        if (D == 128 && nu > 0 && (ok = wait_all(B_KV, 0, 173))) {   // V's rows into tensor memory, half of the dims a thread
             HalfRow<D>::to_tmem(tmem + lanes + kColV, sv, ch, lq * 32 + lane, kKPanel);
             tmem_st_wait();
             tc_fence_before();
@@ -317,23 +338,18 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         Steps st(a, t, nu > 0 ? ub : 0);
         for (int u = 0; ok && u < nu; ++u) {
             const int s = u % kStages;
-            const uint32_t b = (uint32_t)(u & 1) * 64 + 32 * ch;
+            const uint32_t b = (uint32_t)(u % kBuf) * 64 + 32 * ch;
             const int rows = __shfl_sync(0xffffffffu, st.tokens(a), 0) * a.group;
             const bool partial = rows < used;
             // keys of the tile that the segment does not see
             const int key = k0 + lq * 32 + lane;
             const bool blind = key < st.c.k0 || key >= st.c.k0 + st.c.nk;
-            if (!wait_all(B_QFULL + s, (u / kStages) & 1, 171) || !wait_all(B_SFULL + (u & 1), (u >> 1) & 1, 170)) {
+            if (!wait_all(B_QFULL + s, (u / kStages) & 1, 171) || !wait_all(B_SFULL + u % kBuf, (u / kBuf) & 1, 170)) {
                 ok = false;
                 break;
             }
             tc_fence_after();
             st.next(u + 1 < nu);
-            uint32_t sr[32], dr[32];
-            tmem_ld32(tmem + lanes + kColS + b, sr);
-            tmem_ld32(tmem + lanes + kColDP + 32 * ch, dr);
-            const float4 *la = reinterpret_cast<const float4 *>(aux + s * kAuxBytes) + 8 * ch;
-            const float4 *da = reinterpret_cast<const float4 *>(aux + s * kAuxBytes + kBlk * 4) + 8 * ch;
             uint32_t vis = 0xffffffffu;
             if (partial) {
                 // the block's rows past the segment's, which the products below sum over: zeros (S and dP, which
@@ -346,42 +362,55 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 }
                 fence_proxy_async_smem();
             }
-            tmem_ld_wait();
-            tc_fence_before();
-            __syncwarp();
-            mbar_arrive_warp(bar(B_DPFREE));
-            uint32_t pk[16], dk[16];
+            const float4 *la = reinterpret_cast<const float4 *>(aux + s * kAuxBytes) + 8 * ch;
+            const float4 *da = reinterpret_cast<const float4 *>(aux + s * kAuxBytes + kBlk * 4) + 8 * ch;
             const uint64_t c2 = f2_pack(c, c);
-            // two row columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D), both rounded to the MMAs'
-            // operand type (half a step, 2^-9 of a value on average)
-            auto column_pairs = [&](auto masked) {
+            const bool any_blind = __any_sync(0xffffffffu, blind);
+            // kCols row columns at a time: all 32, or 16 where two CTAs share the registers
+            constexpr int kCols = T::kCtas == 2 ? 16 : 32;
+            uint32_t pk[16], dk[16];
 #pragma unroll
-                for (int i4 = 0; i4 < 8; ++i4) {
-                    const float4 l4 = la[i4], d4 = da[i4];
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int i = 4 * i4 + 2 * j;
-                        float x0, x1;
-                        f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2,
-                                         j ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y)), x0, x1);
-                        float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-                        const uint64_t e = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])),
-                                                  j ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y));
-                        float d0, d1;
-                        f2_unpack(f2_mul(f2_pack(p0, p1), e), d0, d1);
-                        if (decltype(masked)::value) {
-                            p0 = (vis >> i) & 1u ? p0 : 0.f;
-                            p1 = (vis >> (i + 1)) & 1u ? p1 : 0.f;
-                            d0 = (vis >> i) & 1u ? d0 : 0.f;
-                            d1 = (vis >> (i + 1)) & 1u ? d1 : 0.f;
-                        }
-                        pk[i >> 1] = pack_bf16x2(p0, p1);
-                        dk[i >> 1] = pack_bf16x2(d0, d1);
-                    }
+            for (int h = 0; h < 32; h += kCols) {
+                uint32_t sr[kCols], dr[kCols];
+                tmem_ld_cols(tmem + lanes + kColS + b + h, sr);
+                tmem_ld_cols(tmem + lanes + kColDP + 32 * ch + h, dr);
+                tmem_ld_wait();
+                if (h + kCols == 32) {
+                    tc_fence_before();
+                    __syncwarp();
+                    mbar_arrive_warp(bar(B_DPFREE));
                 }
-            };
-            if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
-            if (__any_sync(0xffffffffu, blind)) {
+                // two row columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D), both rounded to the
+                // MMAs' operand type (half a step, 2^-9 of a value on average)
+                auto column_pairs = [&](auto masked) {
+#pragma unroll
+                    for (int i4 = 0; i4 < kCols / 4; ++i4) {
+                        const float4 l4 = la[h / 4 + i4], d4 = da[h / 4 + i4];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int i = 4 * i4 + 2 * j;
+                            float x0, x1;
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2,
+                                             j ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y)), x0, x1);
+                            float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+                            const uint64_t e = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])),
+                                                      j ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y));
+                            float d0, d1;
+                            f2_unpack(f2_mul(f2_pack(p0, p1), e), d0, d1);
+                            if (decltype(masked)::value) {
+                                p0 = (vis >> (h + i)) & 1u ? p0 : 0.f;
+                                p1 = (vis >> (h + i + 1)) & 1u ? p1 : 0.f;
+                                d0 = (vis >> (h + i)) & 1u ? d0 : 0.f;
+                                d1 = (vis >> (h + i + 1)) & 1u ? d1 : 0.f;
+                            }
+                            pk[(h + i) >> 1] = pack_bf16x2(p0, p1);
+                            dk[(h + i) >> 1] = pack_bf16x2(d0, d1);
+                        }
+                    }
+                };
+                if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
+            }
+            if (any_blind) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     pk[i] = blind ? 0u : pk[i];
@@ -393,7 +422,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            mbar_arrive_warp(bar(B_PFULL + (u & 1)));
+            mbar_arrive_warp(bar(B_PFULL + u % kBuf));
         }
         sums = ok && (nu == 0 || wait_all(B_FINAL + 1, 0, 172));
         tc_fence_after();
@@ -443,7 +472,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
 #pragma unroll 1
         for (int c = 0; c < kHalfPart; c += 16) {
             uint32_t own[16];
-            part(rank, c, own);
+            part(kParts ? 0 : rank, c, own);
             float acc[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[i] = 0.f;
@@ -451,7 +480,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             for (int from = 0; from < NC; ++from)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
-                    const float4 x = from == rank ? make_float4(__uint_as_float(own[i]), __uint_as_float(own[i + 1]),
+                    const float4 x = kParts || from == rank ? make_float4(__uint_as_float(own[i]), __uint_as_float(own[i + 1]),
                                                                 __uint_as_float(own[i + 2]), __uint_as_float(own[i + 3]))
                                                   : *reinterpret_cast<const float4 *>(smem + slot(from, rank, c + i));
                     acc[i] += x.x;
@@ -459,7 +488,15 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     acc[i + 2] += x.z;
                     acc[i + 3] += x.w;
                 }
-            const int col = kPart * rank + kHalfPart * ch + c, r = lq * 32 + lane;
+            const int col = (kParts ? 0 : kPart * rank) + kHalfPart * ch + c, r = lq * 32 + lane;
+            if constexpr (kParts) {
+                float *dst = a.part_dkv + ((size_t)blockIdx.x * kKT + r) * (2 * D) + col;
+                if (r < t.nk) {
+                    st_global_v8(dst, acc[0], acc[1], acc[2], acc[3], acc[4], acc[5], acc[6], acc[7]);
+                    st_global_v8(dst + 8, acc[8], acc[9], acc[10], acc[11], acc[12], acc[13], acc[14], acc[15]);
+                }
+                continue;
+            }
             const bool isk = col >= D;                       // dV first, then dK (times scale)
             if (r < t.nk)
                 store_row_bf16(isk ? (__nv_bfloat16 *)a.dk + (size_t)(k0 + r) * a.dk_stride + g * D + (col - D)
@@ -471,8 +508,32 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     __syncthreads();
     if (warp == 9) {
         tc_fence_after();
-        tmem_dealloc(tmem, kTmemCols);
+        tmem_dealloc(tmem, T::kAll);
     }
+}
+
+// Four columns of a key row's dV | dK a thread: the parts' sums in their order (a part without steps wrote none).
+template <int D>
+__global__ void __launch_bounds__(256) cross_dkv_sum_kernel(const padoc_cross_args a)
+{
+    constexpr int kPer = dkv::kKT * 2 * D / 4 / 256;   // CTAs of a tile
+    const int unit = blockIdx.x / kPer, g = unit % a.hkv;
+    const padoc_cross_key_tile t = a.tiles[unit / a.hkv];
+    const int i = blockIdx.x % kPer * 256 + threadIdx.x, r = i / (D / 2), col = i % (D / 2) * 4;
+    if (r >= t.nk || t.steps == 0) return;
+    const float *src = a.part_dkv + ((size_t)unit * a.parts * dkv::kKT + r) * (2 * D) + col;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int p = 0; p < a.parts; ++p) {
+        if ((int)((int64_t)t.steps * (p + 1) / a.parts) == (int)((int64_t)t.steps * p / a.parts)) continue;
+        const float4 y = *reinterpret_cast<const float4 *>(src + (size_t)p * dkv::kKT * (2 * D));
+        x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+    }
+    const bool isk = col >= D;
+    const float mul = isk ? a.scale : 1.f;
+    __nv_bfloat16 *dst = isk ? (__nv_bfloat16 *)a.dk + (size_t)(t.k0 + r) * a.dk_stride + g * D + (col - D)
+                             : (__nv_bfloat16 *)a.dv + (size_t)(t.k0 + r) * a.dv_stride + g * D + col;
+    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16x2(x.x * mul, x.y * mul), pack_bf16x2(x.z * mul, x.w * mul));
 }
 
 // ================================================================================================
@@ -481,11 +542,18 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
 namespace dqp {
 constexpr int kQT = PADOC_CROSS_DQ_BLOCKS * kBlk;   // 128 rows: the M of every MMA
 constexpr int kW = PADOC_CROSS_DQ_STEP;             // 64 keys per step
-constexpr int kStages = 4;
+constexpr int kMaxStages = 4;
+constexpr int kMaxSlots = 3;
 constexpr int kQPanel = kQT * 128;           // [128 rows][64 bf16]
 constexpr int kKPanel = kW * 128;            // [64 rows][64 bf16]
-constexpr int kSlots = 3;                    // S buffers; a step's dS takes its S's place
-constexpr uint32_t kColQ = 0, kColS = 64, kColDP = 256, kColDQ = 384;   // Q (A operand), S x 3, dP x 2, dQ
+// Tensor memory: Q as an A operand, S (a step's dS takes its S's place), dP, dQ; three S and two dP buffers, or with 64
+// dims, where two CTAs share an SM, one of each in 256 columns.
+template <int D>
+struct Cols {
+    static constexpr int kCtas = D == 64 ? 2 : 1, kSlots = D == 64 ? 1 : 3, kDPs = D == 64 ? 1 : 2, kStages = D == 64 ? 3 : 4;
+    static constexpr uint32_t kQ = 0, kS = D / 2, kDP = kS + 64 * kSlots, kDQ = kDP + 64 * kDPs, kAll = 512 / kCtas;
+    static_assert(kDQ + D <= kAll, "");
+};
 enum {
     B_QROWS = 0,                   // the unit's Q has landed
     B_GROWS = 1,                   // its dO and O have landed
@@ -500,13 +568,13 @@ enum {
     B_UFULL = 10,                  // [unit parity]
     B_UEMPTY = 12,                 // [unit parity], an arrival per reading warp
     B_KFULL = 14,                  // [stage]
-    B_KEMPTY = 14 + kStages,       // [stage]
-    B_SFULL = 14 + 2 * kStages,    // [slot]: S and dP (an arrival each)
-    B_PFULL = 17 + 2 * kStages,    // [slot]: dS (an arrival per softmax warp)
-    B_ACC = 20 + 2 * kStages,      // [slot]: the accumulating MMAs that read it are done
-    B_DPFREE = 23 + 2 * kStages,   // [step parity]: dP is read (an arrival per softmax warp)
-    B_FINAL = 25 + 2 * kStages,    // [issuing warp]
-    B_COUNT = 28 + 2 * kStages
+    B_KEMPTY = 14 + kMaxStages,       // [stage]
+    B_SFULL = 14 + 2 * kMaxStages,    // [slot]: S and dP (an arrival each)
+    B_PFULL = 17 + 2 * kMaxStages,    // [slot]: dS (an arrival per softmax warp)
+    B_ACC = 20 + 2 * kMaxStages,      // [slot]: the accumulating MMAs that read it are done
+    B_DPFREE = 23 + 2 * kMaxStages,   // [step parity]: dP is read (an arrival per softmax warp)
+    B_FINAL = 25 + 2 * kMaxStages,    // [issuing warp]
+    B_COUNT = 28 + 2 * kMaxStages
 };
 struct Unit {   // steps < 0: no more units
     int32_t tok, ntok, k0, nk;
@@ -516,19 +584,21 @@ constexpr int kReaders = 11;       // softmax and issuing warps
 template <int D>
 constexpr size_t smem_bytes()
 {
-    return 1024 + 3 * (size_t)(D / 64) * kQPanel + 2 * (size_t)kStages * (D / 64) * kKPanel + 2 * sizeof(Unit) + 16 + B_COUNT * 8 + 32 + 2 * kQT * 4;
+    return 1024 + 3 * (size_t)(D / 64) * kQPanel + 2 * (size_t)Cols<D>::kStages * (D / 64) * kKPanel + 2 * sizeof(Unit) + 16 + B_COUNT * 8 + 32 + 2 * kQT * 4;
 }
-static_assert(smem_bytes<128>() <= 232448, "shared memory per CTA");
+static_assert(smem_bytes<128>() <= 232448 && 2 * (smem_bytes<64>() + 1024) <= 233472, "shared memory of an SM");
 }  // namespace dqp
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, dqp::Cols<D>::kCtas)
 cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap gmap,
                 const __grid_constant__ CUtensorMap omap, const __grid_constant__ CUtensorMap kmap,
                 const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
 {
     using namespace dqp;
-    constexpr int kPanels = D / 64, kQTile = kPanels * kQPanel, kKTile = kPanels * kKPanel;
+    using T = Cols<D>;
+    constexpr int kPanels = D / 64, kQTile = kPanels * kQPanel, kKTile = kPanels * kKPanel, kStages = T::kStages, kSlots = T::kSlots, kDPs = T::kDPs;
+    constexpr uint32_t kColQ = T::kQ, kColS = T::kS, kColDP = T::kDP, kColDQ = T::kDQ;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t *sq = smem;                        // Q, dO and O rows; dQ leaves by way of Q's place
@@ -552,8 +622,8 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     if (tid == 0) {
         for (int i = 0; i < B_COUNT; ++i) {
             const bool soft = i == B_QT || i == B_D || i == B_DREAD || i == B_QFREE || i == B_DQFREE ||
-                              (i >= B_PFULL && i < B_PFULL + kSlots) || i == B_DPFREE || i == B_DPFREE + 1;
-            mbar_init(bar(i), soft ? 8 : i == B_UEMPTY || i == B_UEMPTY + 1 ? kReaders : i >= B_SFULL && i < B_SFULL + kSlots ? 2 : 1);
+                              (i >= B_PFULL && i < B_PFULL + kMaxSlots) || i == B_DPFREE || i == B_DPFREE + 1;
+            mbar_init(bar(i), soft ? 8 : i == B_UEMPTY || i == B_UEMPTY + 1 ? kReaders : i >= B_SFULL && i < B_SFULL + kMaxSlots ? 2 : 1);
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -566,7 +636,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
         fence_proxy_async_smem();
     }
     if (warp == 9) {
-        tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+        tmem_alloc(smem_u32(tmem_slot), T::kAll);
         tmem_relinquish();
     }
     tc_fence_before();
@@ -704,12 +774,12 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 for (int u = 0; ok && u < un.steps; ++u, next_step()) {
                     const int s = c % kStages;
                     ok = wait_w(B_KFULL + s, (c / kStages) & 1, 198) &&
-                         (c < 2 || wait_w(B_DPFREE + (c & 1), ((c >> 1) - 1) & 1, 199));
+                         (c < kDPs || wait_w(B_DPFREE + c % kDPs, (c / kDPs - 1) & 1, 199));
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t dv = umma_desc_sw128(smem_u32(sv + s * kKTile), 16, 1024);
-                    if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kQPanel, kKPanel>(tmem + kColDP + 64 * (c & 1), dg, dv, idS);
-                    else umma_bf16_ss_k64_warp(tmem + kColDP + 64 * (c & 1), dg, dv, idS);
+                    if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kQPanel, kKPanel>(tmem + kColDP + 64 * (c % kDPs), dg, dv, idS);
+                    else umma_bf16_ss_k64_warp(tmem + kColDP + 64 * (c % kDPs), dg, dv, idS);
                     umma_commit_warp(bar(B_SFULL + slot));
                 }
                 umma_commit_warp(bar(B_GFREE));
@@ -841,9 +911,6 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 const bool partial = left < kW;
                 if (!(ok = wait_w(B_SFULL + slot, ph, 195))) break;
                 tc_fence_after();
-                uint32_t sr[32], dr[32];
-                tmem_ld32(b, sr);
-                tmem_ld32(tmem + lanes + kColDP + 64 * (c & 1) + 32 * ch, dr);
                 uint32_t vis = 0xffffffffu;
                 if (partial) {
                     // K's rows past the end, which dQ's product sums over: zeros (S, which has read them, is done)
@@ -854,29 +921,38 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                             make_uint4(0, 0, 0, 0);
                     fence_proxy_async_smem();
                 }
-                tmem_ld_wait();
-                tc_fence_before();
-                __syncwarp();
-                mbar_arrive_warp(bar(B_DPFREE + (c & 1)));
                 uint32_t dk[16];
-                // two key columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D)
-                auto column_pairs = [&](auto masked) {
+                constexpr int kCols = T::kCtas == 2 ? 16 : 32;
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        float x0, x1;
-                        f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2, nl2), x0, x1);
-                        const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-                        const uint64_t t2 = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])), d2);
-                        float d0, d1;
-                        f2_unpack(f2_mul(f2_pack(p0, p1), t2), d0, d1);
-                        if (decltype(masked)::value) {
-                            d0 = (vis >> i) & 1u ? d0 : 0.f;
-                            d1 = (vis >> (i + 1)) & 1u ? d1 : 0.f;
-                        }
-                        dk[i >> 1] = pack_bf16x2(d0, d1);
+                for (int h = 0; h < 32; h += kCols) {
+                    uint32_t sr[kCols], dr[kCols];
+                    tmem_ld_cols(b + h, sr);
+                    tmem_ld_cols(tmem + lanes + kColDP + 64 * (c % kDPs) + 32 * ch + h, dr);
+                    tmem_ld_wait();
+                    if (h + kCols == 32) {
+                        tc_fence_before();
+                        __syncwarp();
+                        mbar_arrive_warp(bar(B_DPFREE + c % kDPs));
                     }
-                };
-                if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
+                    // two key columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D)
+                    auto column_pairs = [&](auto masked) {
+#pragma unroll
+                        for (int i = 0; i < kCols; i += 2) {
+                            float x0, x1;
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2, nl2), x0, x1);
+                            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+                            const uint64_t t2 = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])), d2);
+                            float d0, d1;
+                            f2_unpack(f2_mul(f2_pack(p0, p1), t2), d0, d1);
+                            if (decltype(masked)::value) {
+                                d0 = (vis >> (h + i)) & 1u ? d0 : 0.f;
+                                d1 = (vis >> (h + i + 1)) & 1u ? d1 : 0.f;
+                            }
+                            dk[(h + i) >> 1] = pack_bf16x2(d0, d1);
+                        }
+                    };
+                    if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
+                }
                 tmem_st16(b, dk);   // over the first half of this thread's own S columns
                 tmem_st_wait();
                 tc_fence_before();
@@ -890,21 +966,21 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     __syncthreads();
     if (warp == 9) {
         tc_fence_after();
-        tmem_dealloc(tmem, kTmemCols);
+        tmem_dealloc(tmem, T::kAll);
     }
 }
 
-template <int D, int NC>
+template <int D, int NC, bool kParts = false>
 padoc_status launch_dkv(const CUtensorMap &qmap, const CUtensorMap &gmap, const padoc_cross_args &a, bool after, cudaStream_t stream)
 {
     CUtensorMap kmap, vmap;
     if (!padoc_make_tmap_bf16(&kmap, a.k, (uint64_t)a.hkv * D, a.key_rows, a.k_stride * 2, 64, dkv::kKT) ||
         !padoc_make_tmap_bf16(&vmap, a.v, (uint64_t)a.hkv * D, a.key_rows, a.v_stride * 2, 64, dkv::kKT))
         return PADOC_ERR_CUDA;
-    auto kernel = cross_dkv_kernel<D, NC>;
+    auto kernel = cross_dkv_kernel<D, NC, kParts>;
     if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dkv::smem_bytes<D>())) return st;
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)((a.num_tiles + a.tail_tiles) * a.hkv * NC));
+    lc.gridDim = dim3((unsigned)((a.num_tiles + a.tail_tiles) * a.hkv * (kParts ? a.parts : NC)));
     lc.blockDim = dim3(kThreads);
     lc.dynamicSmemBytes = dkv::smem_bytes<D>();
     lc.stream = stream;
@@ -928,7 +1004,7 @@ padoc_status run(const padoc_cross_args &a, int cluster, cudaStream_t stream)
     if (!a.num_units) {   // no row sees a key: the key rows' zeros alone, which read nothing
         CUtensorMap none = {};
         CUtensorMap kv = {};
-        auto kernel = cross_dkv_kernel<D, 1>;
+        auto kernel = cross_dkv_kernel<D, 1, false>;
         if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dkv::smem_bytes<D>())) return st;
         if (a.num_tiles + a.tail_tiles)
             kernel<<<(unsigned)((a.num_tiles + a.tail_tiles) * a.hkv), kThreads, dkv::smem_bytes<D>(), stream>>>(none, none, kv, kv, a);
@@ -945,6 +1021,11 @@ padoc_status run(const padoc_cross_args &a, int cluster, cudaStream_t stream)
     kernel<<<(unsigned)(a.ctas ? a.num_ctas : a.num_units), kThreads, dqp::smem_bytes<D>(), stream>>>(qmap, gmap, omap, kmap, vmap, a);
     const padoc_status st = padoc_launch_status();
     if (st != PADOC_OK) return st;
+    if (a.parts > 1) {
+        if (const padoc_status s2 = launch_dkv<D, 1, true>(qmap, gmap, a, true, stream)) return s2;
+        cross_dkv_sum_kernel<D><<<(unsigned)(a.num_tiles * a.hkv * (dkv::kKT * 2 * D / 4 / 256)), 256, 0, stream>>>(a);
+        return padoc_launch_status();
+    }
     switch (cluster) {
         case 8:
             if constexpr (D == 128) return launch_dkv<D, 8>(qmap, gmap, a, true, stream);

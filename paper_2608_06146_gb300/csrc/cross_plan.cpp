@@ -298,13 +298,15 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
 
     // Forward. Times in us: of two 128-row tiles' steps of 128 keys, and for few rows of a 64-key tile's bytes at the
     // SM's share of the memory bandwidth (45 KB a us), which its CTAs share.
-    int32_t per = PADOC_CROSS_UNIT_BLOCKS * block;
+    // With 64 dims an item is one tile and two CTAs share an SM, in the forward and in the backward.
+    const int32_t an_sm = !f32 && cfg->head_dim == 64 ? 2 : 1, unit_blocks = PADOC_CROSS_UNIT_BLOCKS / an_sm;
+    int32_t per = unit_blocks * block;
     {
-        const Costs tc = {1.8f, 1.5f, 2.f, 0.012f, 0.65f, PADOC_CROSS_KEY_TILE, 1};
+        const Costs tc = {1.8f, 1.5f, 2.f, 0.012f / an_sm, an_sm == 2 ? 1.f : 0.65f, PADOC_CROSS_KEY_TILE, 1};
         const Costs &k = f32 ? simt : tc;
-        const int32_t lanes = f32 ? std::max(1, sms / PADOC_CROSS_UNIT_BLOCKS) : sms;
+        const int32_t lanes = f32 ? std::max(1, sms / PADOC_CROSS_UNIT_BLOCKS) : sms * an_sm;
         const float time = 1.65f * plan_work(chunks_of(per, k), hkv, lanes, k, cuts, b.fwd);
-        info.unit_rows = PADOC_CROSS_UNIT_BLOCKS * PADOC_CROSS_BLOCK;
+        info.unit_rows = unit_blocks * PADOC_CROSS_BLOCK;
         if (!f32 && group <= PADOC_CROSS_FEW_ROWS && !b.fwd.units.empty())
             plan_few(seg, n, group, cfg->head_dim, hkv, sms, time, chunks_of, b.fwd, info, per);
     }
@@ -313,7 +315,7 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
     if (cfg->backward) {
         const Costs bwd = {6.f, 2.f, 6.f, 0.018f, 1.f, PADOC_CROSS_DQ_STEP, 4};   // (a step of a tile lasts about 0.55 us)
         const Costs &k = f32 ? simt : bwd;
-        const int32_t lanes = f32 ? std::max(1, sms / PADOC_CROSS_DQ_BLOCKS) : sms;
+        const int32_t lanes = f32 ? std::max(1, sms / PADOC_CROSS_DQ_BLOCKS) : sms * an_sm;
         plan_work(chunks_of(PADOC_CROSS_DQ_BLOCKS * block, k), hkv, lanes, k, cuts, b.dq);
         empty_rows(PADOC_CROSS_DQ_BLOCKS * block, b.dq.merges);
 
@@ -369,6 +371,23 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
             if (i == 0 || time < best) {
                 best = time;
                 info.cluster = nc;
+            }
+        }
+        // Or parts for the whole chip, whose sums a later kernel adds (2 steps' time a part to write, a launch, and
+        // reading them all at some 6 TB/s).
+        info.parts = 1;
+        const int64_t tiles = (int64_t)b.tiles.size() * hkv;
+        if (!f32 && tiles > 0 && tiles <= lanes / 2) {
+            const int32_t parts = (int32_t)(lanes / tiles);
+            std::vector<float> cost;
+            for (const padoc_cross_key_tile &t : b.tiles)
+                for (int32_t g = 0; g < hkv && t.steps; ++g)
+                    for (int32_t p = 0; p < std::min(parts, t.steps); ++p) cost.push_back((float)ceil_div(t.steps, parts) + start[0] + 2.f);
+            const float read = (float)cost.size() * cfg->head_dim * 1e-3f / 6.f / 0.8f;
+            const float time = makespan(cost, lanes) + 4.f + read;
+            if (time < best) {
+                info.cluster = 1;
+                info.parts = parts;
             }
         }
     }
@@ -467,9 +486,10 @@ extern "C" padoc_status padoc_cross_workspace_size(const padoc_cross_plan *info,
 extern "C" padoc_status padoc_cross_bwd_workspace_size(const padoc_cross_plan *info, size_t *bytes)
 {
     if (!info || !bytes || !info->cfg.backward || info->num_dq_slots < 0 || info->num_subs < 0) return PADOC_ERR_INVALID_ARGUMENT;
-    // -lse2 and D, [Hkv][subs][64] each, then partial dq [slots][128][d], fp32
+    // -lse2 and D, [Hkv][subs][64] each, partial dq [slots][128][d], partial dv and dk [tiles][Hkv][parts][128][2 d], fp32
     const size_t stats = (size_t)info->num_subs * info->cfg.num_kv_heads * PADOC_CROSS_BLOCK;
     const size_t rows = (size_t)info->num_dq_slots * (PADOC_CROSS_DQ_BLOCKS * PADOC_CROSS_BLOCK);
-    *bytes = (2 * stats + rows * info->cfg.head_dim) * sizeof(float);
+    const size_t tiles = info->parts > 1 ? (size_t)info->num_key_tiles * info->cfg.num_kv_heads * info->parts : 0;
+    *bytes = (2 * stats + rows * info->cfg.head_dim + tiles * PADOC_CROSS_KEY_TILE * 2 * info->cfg.head_dim) * sizeof(float);
     return PADOC_OK;
 }

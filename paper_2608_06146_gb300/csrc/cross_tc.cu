@@ -1,20 +1,20 @@
 // cross_tc.cu -- cross attention forward on the 5th-generation tensor cores: S = Q K^T, online softmax, O = P V.
 //
-// A unit is 256 packed rows of one KV head (two 128-row tiles of (token, head of the group) rows) over a segment's
-// keys or a part of them. All rows of a unit see the same keys, so the only mask is the end of
+// A unit is 256 packed rows of one KV head (two 128-row tiles of (token, head of the group) rows), or with 64 dims 128
+// rows, over a segment's keys or a part of them. All rows of a unit see the same keys, so the only mask is the end of
 // the last 128-key tile: its scores past the end become -inf, and its V rows there zeros, because what lies behind a
 // segment's keys may be anything (0 x NaN would reach the output).
 //
-// Warp roles (384 threads): warps 0-3 / 4-7 softmax and epilogue of tile 0 / 1 (TMEM lane = row: row max and sum need
-// no shuffles); warp 8 TMA producer, which also announces the units; warps 9, 10 the MMA issuers of tile 0 / 1 (a
-// converged warp, one elected lane); warp 9 also allocates tensor memory. Tensor memory: tile i keeps S in two halves
-// of 64 keys at columns 128 i + 64 h, with P as packed bf16 over the first 32 columns of its half, and O at 256 + 128 i.
-// For a tile and half the MMAs run S(t) -> P(t) -> P V(t) -> S(t + 1). O is rescaled only when a row's maximum has
-// grown by more than 2^8 since the last time, which keeps P <= 256.
+// Warp roles: four warps a tile for softmax and epilogue (TMEM lane = row: row max and sum need no shuffles); then the
+// TMA producer, which also announces the units; then an MMA issuer a tile (a converged warp, one elected lane), the first
+// of which also allocates tensor memory. Tensor memory: tile i keeps S in two halves of 64 keys, with P as packed bf16
+// over the first 32 columns of its half, and O behind the tiles' S. For a tile and half the MMAs run
+// S(t) -> P(t) -> P V(t) -> S(t + 1). O is rescaled only when a row's maximum has grown by more than 2^8 since the last
+// time, which keeps P <= 256.
 //
-// The grid has one CTA per unit, most keys first; a running one takes over units not yet launched (cluster
-// launch control). Where the planner cut the steps into equal runs, each CTA has a list of units. The next unit's
-// queries and first scores come under the last one's output. A unit of at most 128 rows is run by tile 0's warps alone.
+// The grid has one CTA per unit, most keys first; a running one takes over units not yet launched (cluster launch
+// control). Where the planner cut the steps into equal runs, each CTA has a list of units. The next unit's queries and
+// first scores come under the last one's output. A unit of at most 128 rows is run by tile 0's warps alone.
 // Every wait is bounded; a wait that runs out records an error, all roles leave their loops, the issuers wait for
 // their MMAs, the producer for its copies, and tensor memory is released.
 #include <math.h>
@@ -24,8 +24,6 @@
 
 namespace {
 
-constexpr int kThreads = 384;
-constexpr uint32_t kTmemCols = 512;
 constexpr int kPanel = 128 * 128;      // [128 rows][64 bf16]
 constexpr int kBlk = PADOC_CROSS_BLOCK;
 constexpr int kKT = PADOC_CROSS_KEY_TILE;
@@ -37,9 +35,14 @@ template <int D>
 struct Cfg {
     static constexpr int kPanels = D / 64;
     static constexpr int kTile = kPanels * kPanel;
-    static constexpr int kStages = D == 64 ? 4 : 2;
+    static constexpr int kTiles = D == 64 ? 1 : 2;   // 128-row tiles of a unit; with 64 dims two CTAs share an SM
+    static constexpr int kCtas = D == 64 ? 2 : 1;
+    static constexpr int kSoft = 4 * kTiles;         // softmax warps
+    static constexpr int kThreads = 32 * (kSoft + kTiles + (kTiles == 2 ? 2 : 1));
+    static constexpr uint32_t kTmemCols = 256 * kTiles;
+    static constexpr int kStages = 2;
     static constexpr int kKPanel = kPanel / 2;       // 64 dims of the keys of one half
-    static constexpr int kOutBytes = 8 * 4096;       // [32 rows][64 dims] a softmax warp
+    static constexpr int kOutBytes = kSoft * 4096;   // [32 rows][64 dims] a softmax warp
     enum {
         B_QFULL = 0,                    // [tile]
         B_QEMPTY = 2,                   // [tile]
@@ -58,9 +61,9 @@ struct Cfg {
         B_VEMPTY = B_VFULL + kStages,   // [stage], one arrival per tile
         B_COUNT = B_VEMPTY + kStages
     };
-    static constexpr int kReaders = 10;   // softmax and MMA warps
-    static constexpr size_t kSmemBytes = 1024 + 2 * (size_t)kTile + 2 * (size_t)kStages * kTile + kOutBytes + 96 + B_COUNT * 8 + 16;
-    static_assert(kSmemBytes <= 227 * 1024, "");
+    static constexpr int kReaders = kSoft + kTiles;   // softmax and MMA warps
+    static constexpr size_t kSmemBytes = 1024 + kTiles * (size_t)kTile + 2 * (size_t)kStages * kTile + kOutBytes + 96 + B_COUNT * 8 + 16;
+    static_assert(kCtas * (kSmemBytes + 1024) <= 228 * 1024, "");
 };
 
 // A unit as the producer announces it; tiles < 0 ends the CTA.
@@ -79,18 +82,18 @@ __device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, int
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Cfg<D>::kThreads, Cfg<D>::kCtas)
 cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                 const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
 {
     using C = Cfg<D>;
-    constexpr int kStages = C::kStages, kTile = C::kTile;
+    constexpr int kStages = C::kStages, kTile = C::kTile, kThreads = C::kThreads, kSoft = C::kSoft;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *sq = smem;                       // [2 tiles][panel][128 rows]
-    uint8_t *sk = sq + 2 * kTile;             // [kStages][key half][panel]
+    uint8_t *sq = smem;                       // [tile][panel][128 rows]
+    uint8_t *sk = sq + C::kTiles * kTile;             // [kStages][key half][panel]
     uint8_t *sv = sk + kStages * kTile;    // [kStages][panel]
-    uint8_t *so = sv + kStages * kTile;    // [8 warps][32][128 bytes]
+    uint8_t *so = sv + kStages * kTile;    // [softmax warp][32][128 bytes]
     Unit *units = (Unit *)(so + C::kOutBytes);   // [2]
     uint8_t *answer = (uint8_t *)(units + 2); // 16 bytes
     uint64_t *bars = (uint64_t *)(so + C::kOutBytes + 96);
@@ -107,8 +110,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             int n = 1;
             if (i >= C::B_PFULL && i < C::B_PFULL + 4) n = 4;
             if (i == C::B_OFREE || i == C::B_OFREE + 1) n = 4;
-            if (i >= C::B_KEMPTY && i < C::B_KEMPTY + kStages) n = 2;
-            if (i >= C::B_VEMPTY && i < C::B_VEMPTY + kStages) n = 2;
+            if (i >= C::B_KEMPTY && i < C::B_KEMPTY + kStages) n = C::kTiles;
+            if (i >= C::B_VEMPTY && i < C::B_VEMPTY + kStages) n = C::kTiles;
             if (i == C::B_UEMPTY || i == C::B_UEMPTY + 1) n = C::kReaders;
             mbar_init(bar(i), n);
         }
@@ -119,7 +122,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     // up (a small call waits for each global read in turn)
     int x = 0, xe = 0;
     padoc_cross_unit item = {};
-    if (warp == 8 && lane == 0) {
+    if (warp == kSoft && lane == 0) {
         x = (int)blockIdx.x;
         pdl_wait_prerequisite();   // nothing in global memory is touched before (the other roles' work follows from this)
         if (a.ctas) {
@@ -131,14 +134,14 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     // rows of a block that hold no (token, head): no copy writes them
     const int used = a.block_tokens * a.group;
     if (used < kBlk) {
-        for (int i = tid; i < 4 * C::kPanels * (kBlk - used) * 8; i += kThreads) {
+        for (int i = tid; i < 2 * C::kTiles * C::kPanels * (kBlk - used) * 8; i += kThreads) {
             const int r = i / 8 % (kBlk - used) + used, b = i / 8 / (kBlk - used);
             *reinterpret_cast<uint4 *>(sq + b * kBlk * 128 + r * 128 + i % 8 * 16) = make_uint4(0, 0, 0, 0);
         }
         fence_proxy_async_smem();
     }
-    if (warp == 9) {
-        tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    if (warp == kSoft + 1) {
+        tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
         tmem_relinquish();
     }
     tc_fence_before();
@@ -165,13 +168,13 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     auto next_unit = [&](int i, int &n, Unit &u, int &ring, int site) {
         for (;;) {
             if (!read_unit(n++, u, site)) return false;
-            if (u.tiles < 0 || i == 0 || u.two) return true;
+            if (u.tiles < 0 || C::kTiles == 1 || i == 0 || u.two) return true;
             ring += u.tiles;
         }
     };
 
-    if (warp >= 8) {
-        if (warp == 8 && lane == 0) {
+    if (warp >= kSoft) {
+        if (warp == kSoft && lane == 0) {
             // ------------------------------------------------------------ TMA producer
             tma_prefetch_desc(&qmap);
             tma_prefetch_desc(&kmap);
@@ -208,7 +211,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 Unit u = {0, 0, 0, 0, 0, 0, -1, 0};
                 if (n >= 2 && !wait(C::B_UEMPTY + (n & 1), ((n >> 1) - 1) & 1, 124)) break;
                 if (more) {
-                    u = {item.tok, item.ntok, item.k0, item.nk, item.g, item.slot, (item.nk + kKT - 1) / kKT, item.ntok > tile_tokens};
+                    u = {item.tok, item.ntok, item.k0, item.nk, item.g, item.slot, (item.nk + kKT - 1) / kKT, C::kTiles == 2 && item.ntok > tile_tokens};
                     if (a.ctas && (more = ++x < xe)) item = a.units[x];   // (a list's next item is known at once)
                 }
                 units[n & 1] = u;
@@ -222,7 +225,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     if (tk >= kStages && !(ok = wait(C::B_KEMPTY + s, (tk / kStages - 1) & 1, 121))) break;
                     uint8_t *kb = sk + s * kTile;
                     mbar_arrive_expect_tx(bar(C::B_KFULL + s), kTile);
-                    if (!u.two) mbar_arrive(bar(C::B_KEMPTY + s));   // (for the second tile, which has no part)
+                    if (C::kTiles == 2 && !u.two) mbar_arrive(bar(C::B_KEMPTY + s));   // (for the second tile, which has no part)
 #pragma unroll
                     for (int b = 0; b < 2 * C::kPanels; ++b)   // [key half][panel]
                         tma_load_2d(smem_u32(kb + b * C::kKPanel), &kmap, u.g * D + 64 * (b % C::kPanels), row + 64 * (b / C::kPanels),
@@ -239,7 +242,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                         ++tails;
                     }
                     mbar_arrive_expect_tx(vbar, kTile);
-                    if (!u.two) mbar_arrive(bar(C::B_VEMPTY + s));
+                    if (C::kTiles == 2 && !u.two) mbar_arrive(bar(C::B_VEMPTY + s));
 #pragma unroll
                     for (int p = 0; p < C::kPanels; ++p) tma_load_2d(smem_u32(vb + p * kPanel), &vmap, u.g * D + 64 * p, row, vbar);
                     ++tv;
@@ -257,7 +260,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             }
             // copies still in flight must land before the CTA's shared memory is released
             if (asked) mbar_wait_bounded(bar(C::B_NEXT), asks & 1, a.err, 127);
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < C::kTiles; ++i)
                 if (nq[i]) mbar_wait_bounded(bar(C::B_QFULL + i), (nq[i] - 1) & 1, a.err, 127);
             for (int t = max(tk - kStages, 0); t < tk; ++t)
                 mbar_wait_bounded(bar(C::B_KFULL + t % kStages), (t / kStages) & 1, a.err, 128);
@@ -265,14 +268,14 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 mbar_wait_bounded(bar(C::B_VTAIL + t % kTails), (t / kTails) & 1, a.err, 127);
             for (int t = max(tv - kStages, 0); t < tv; ++t)
                 mbar_wait_bounded(bar(C::B_VFULL + t % kStages), (t / kStages) & 1, a.err, 129);
-        } else if (warp >= 9 && warp < 11) {
+        } else if (warp > kSoft && warp <= kSoft + C::kTiles) {
             // ------------------------------------------------------------ MMA issuers (a whole warp per tile)
-            const int i = warp - 9;
+            const int i = warp - kSoft - 1;
             constexpr uint32_t idS = umma_idesc_bf16(128, 64, false);
             constexpr uint32_t idPV = umma_idesc_bf16(128, D, true);
             const uint64_t dq = umma_desc_sw128(smem_u32(sq + i * kTile), 16, 1024);
             const uint64_t dk = umma_desc_sw128(smem_u32(sk), 16, 1024), dv = umma_desc_sw128(smem_u32(sv), kPanel, 1024);
-            const uint32_t tS = tmem + 128 * i, tO = tmem + 256 + 128 * i;
+            const uint32_t tS = tmem + 128 * i, tO = tmem + 128 * (C::kTiles + i);
             auto wait = [&](int b, uint32_t parity, int site) {
                 return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
             };
@@ -340,7 +343,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
         const int hi = warp / 4;                    // tile inside the unit
         const int row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + lanes + 128 * hi, tO = tmem + lanes + 256 + 128 * hi;
+        const uint32_t tS = tmem + lanes + 128 * hi, tO = tmem + lanes + 128 * (C::kTiles + hi);
         const float c = a.scale_log2;
         // every decision below is warp-uniform: the TMEM loads and stores are warp-collective
         auto wait_all = [&](int b, uint32_t parity, int site) {
@@ -355,7 +358,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
         auto next_of_tile = [&]() {
             for (;;) {
                 if (!read_unit(n++, next, 139)) return false;
-                if (next.tiles < 0 || hi == 0 || next.two) return true;
+                if (next.tiles < 0 || C::kTiles == 1 || hi == 0 || next.two) return true;
                 ring += next.tiles;
                 // (its V tail comes by the same barriers, whose phases are waited for one by one)
                 if (next.nk % kKT != 0 && !wait_tail(144)) return false;
@@ -468,7 +471,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             // keys, in fp32 with the part's log-sum-exp. O_i is free for the next unit's PV as soon as it is read.
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m_ref * c + log2f(l);
             const int64_t at = in ? ((int64_t)token * a.hq + u.g * a.group + head) * D : -1;
-            const size_t pr = (size_t)max(u.slot, 0) * (PADOC_CROSS_UNIT_BLOCKS * kBlk) + hi * 128 + row;
+            const size_t pr = (size_t)max(u.slot, 0) * (C::kTiles * 128) + hi * 128 + row;
             uint8_t *stage = so + warp * 4096;
 #pragma unroll
             for (int half = 0; half < C::kPanels; ++half) {
@@ -515,9 +518,9 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == kSoft + 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, kTmemCols);
+        tmem_dealloc(tmem, C::kTmemCols);
     }
 }
 
@@ -534,7 +537,7 @@ padoc_status launch(const padoc_cross_args &a, cudaStream_t stream)
         return PADOC_ERR_CUDA;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)(a.ctas ? a.num_ctas : a.num_units));
-    lc.blockDim = dim3(kThreads);
+    lc.blockDim = dim3(Cfg<D>::kThreads);
     lc.dynamicSmemBytes = bytes;
     lc.stream = stream;
     cudaLaunchAttribute attr[1];

@@ -141,7 +141,7 @@ class padoc_cross_plan(ctypes.Structure):
     _fields_ = [("cfg", padoc_cross_config)] + [(n, ctypes.c_int32) for n in (
         "num_segments", "query_rows", "key_rows", "few", "unit_rows", "num_units", "num_ctas", "num_merges", "num_slots", "max_parts",
         "num_dq_units", "num_dq_ctas", "num_dq_merges", "num_dq_slots", "max_dq_parts", "num_subs", "num_key_tiles",
-        "num_covers", "cluster")] + [(n, ctypes.c_int64) for n in (
+        "num_covers", "cluster", "parts", "reserved")] + [(n, ctypes.c_int64) for n in (
             "pairs", "plan_ints", "off_units", "off_ctas", "off_merges", "off_dq_units", "off_dq_ctas", "off_dq_merges",
             "off_key_tiles", "off_covers")]
 

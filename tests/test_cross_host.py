@@ -124,6 +124,7 @@ def test_plan_covers_every_pair_once(heads, seed):
             assert cn >= 1 and k0 <= ck and ck + cn <= k0 + nk and sub == place[tok]
             got[tok:tok + nt, ck:ck + cn] += 1
     assert (tiled == 1).all() and (got == want).all()
+    assert info.parts >= 1 and (info.parts == 1 or info.cluster == 1)
     assert info.cluster in (1, 2, 4, 8) and (info.cluster < 8 or cfg.head_dim == 128 or cfg.dtype == pa.PADOC_DTYPE_F32)
 
 

@@ -176,6 +176,15 @@ def test_many_rows(hq, hkv, d):
     check_backward(segments, hq, hkv, d, BF16, poison=False)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(16, 2, 128), (4, 1, 64), (7, 1, 128)])
+def test_few_keys_that_many_rows_see(hq, hkv, d):
+    # a key tile's rows shared out over the whole chip, or over clusters; key rows between that nobody sees
+    plan = check_backward([(0, 900, 5, 70), (900, 60, 400, 200), (960, 3, 300, 10)], hq, hkv, d, BF16)
+    assert plan.info.parts > 1
+    for segments in ([(0, 900, 0, 700)], [(0, 130, 3, 128)], [(0, 2, 0, 100)]):
+        check_backward(segments, hq, hkv, d, BF16)
+
+
 @pytest.mark.parametrize("hq,hkv,d", [(16, 16, 64), (16, 2, 128), (8, 8, 64)])
 @pytest.mark.parametrize("keys", [1, 70, 130, 250])
 def test_many_short_items(hq, hkv, d, keys):
