@@ -21,10 +21,10 @@
 // MMAs are issued by a warp each; P and dS share S's columns, so dP's buffer is free as soon as it is read; waits and
 // roles are uniform per warp. A softmax warp owns 32 TMEM lanes (rows) and one 32-column half of a step; its bf16
 // results go to the first 16 columns of its own half of S (dS of the dK/dV pass to the other 16).
-// Warp roles (384 threads): warps 0-7 softmax and epilogue, warp 8 TMA producer, warp 9 TMEM allocation and S, warp 10
-// the accumulating MMAs, warp 11 dP (converged warps, one elected lane issues). Every wait is bounded; a wait that
-// runs out records an error and all roles leave their loops, the MMA warps wait for their MMAs, the producer for its
-// copies, and tensor memory is released.
+// Warp roles: eight softmax and epilogue warps (or two groups of eight), then the TMA producer, S (and TMEM allocation),
+// the accumulating MMAs, dP (converged warps, one elected lane issues). Every wait is bounded; a wait that runs out records
+// an error and all roles leave their loops, the MMA warps wait for their MMAs, the producer for its copies, and tensor
+// memory is released.
 #include <math.h>
 
 #include <algorithm>
@@ -35,7 +35,6 @@
 
 namespace {
 
-constexpr int kThreads = 384;
 constexpr int kBlk = PADOC_CROSS_BLOCK;
 
 __device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, int *err, int site, volatile int *abort_flag)
@@ -94,14 +93,21 @@ struct HalfRow {
 // ================================================================================================
 namespace dkv {
 constexpr int kKT = PADOC_CROSS_KEY_TILE;   // 128 keys: the M of every MMA
-constexpr int kStages = 4;
-// Tensor memory: S (two buffers), dP, V as an A operand, dV and dK. With 64 dims two CTAs share an SM, which hides one's
-// hand-overs under the other's work better than a second S buffer does: S, dP, dV and dK in 256 columns, V from
-// shared memory.
+constexpr int kMaxStages = 10;
+// With 64 dims two groups of eight softmax warps take the steps in turn (9 pages of 16 heads 110 -> 98 us): one group's
+// work on a step lasts longer than its 16 MMAs. With 128 dims, 24 MMAs, one group with all registers is faster (937 us
+// against 983 for 32768 rows over 8 x 2560 states).
+// Tensor memory: S buffers, dP buffers, V as an A operand (128 dims; with 64 it is read from shared memory), dV and dK.
 template <int D>
 struct Cols {
-    static constexpr int kCtas = D == 64 ? 2 : 1, kBuffers = D == 64 ? 1 : 2;
-    static constexpr uint32_t kS = 0, kDP = 64 * kBuffers, kV = 192, kAcc = 2 * kDP, kAll = 512 / kCtas;
+    static constexpr int kGroups = D == 64 ? 2 : 1, kSoft = 8 * kGroups, kThreads = 32 * (kSoft + 4);
+    static constexpr int kBuffers = 2 * kGroups, kDPs = kGroups;
+    static constexpr uint32_t kDP = 64 * kBuffers, kV = 192, kAcc = D == 64 ? 384 : 256;
+    static_assert(kAcc + 2 * D <= 512 && kDP + 64 * kDPs <= (D == 64 ? kAcc : kV), "");
+    // Steps on their way: a step of 64 dims copies 16 KB in the time of 16 MMAs, and with four stages it waited for them
+    // (128 -> 98 us).
+    static constexpr int kStages = D == 64 ? 10 : 4;
+    static_assert(kStages <= kMaxStages && kStages % kGroups == 0, "a stage belongs to one group");
 };
 constexpr int kKPanel = kKT * 128;           // [128 rows][64 bf16]
 constexpr int kQPanel = kBlk * 128;          // [64 rows][64 bf16]
@@ -109,17 +115,17 @@ constexpr int kAuxBytes = 2 * kBlk * 4;      // -lse2[64], D[64]
 enum {
     B_KV = 0,
     B_QFULL = 1,                  // [stage]
-    B_QEMPTY = 1 + kStages,       // [stage]
-    B_SFULL = 1 + 2 * kStages,    // [S buffer]
-    B_PFULL = 3 + 2 * kStages,    // [S buffer], an arrival per softmax warp
-    B_ACC = 5 + 2 * kStages,      // [S buffer]: the step's accumulating MMAs are done
-    B_DPFREE = 7 + 2 * kStages,   // dP is read (an arrival per softmax warp)
-    B_VT = 8 + 2 * kStages,       // V is in tensor memory (an arrival per softmax warp)
-    B_FINAL = 9 + 2 * kStages,    // [issuing warp]
-    B_COUNT = 12 + 2 * kStages
+    B_QEMPTY = 1 + kMaxStages,       // [stage]
+    B_SFULL = 1 + 2 * kMaxStages,    // [S buffer]
+    B_PFULL = 5 + 2 * kMaxStages,    // [S buffer], an arrival per softmax warp of a group
+    B_ACC = 9 + 2 * kMaxStages,      // [S buffer]: the step's accumulating MMAs are done
+    B_DPFREE = 13 + 2 * kMaxStages,  // [dP buffer]: dP is read (an arrival per softmax warp of a group)
+    B_VT = 15 + 2 * kMaxStages,      // V is in tensor memory (an arrival per softmax warp of the first group)
+    B_FINAL = 16 + 2 * kMaxStages,   // [issuing warp]
+    B_COUNT = 19 + 2 * kMaxStages
 };
 template <int D>
-constexpr size_t smem_bytes() { return 1024 + 2 * (size_t)(D / 64) * kKPanel + 2 * (size_t)kStages * (D / 64) * kQPanel + (size_t)kStages * kAuxBytes + B_COUNT * 8 + 64; }
+constexpr size_t smem_bytes() { return 1024 + 2 * (size_t)(D / 64) * kKPanel + 2 * (size_t)Cols<D>::kStages * (D / 64) * kQPanel + (size_t)Cols<D>::kStages * kAuxBytes + B_COUNT * 8 + 64; }
 }  // namespace dkv
 
 // The blocks of rows that a key tile's steps are, one after the other.
@@ -148,14 +154,15 @@ struct Steps {
 // NC: the CTAs of a unit's cluster. kParts: the steps are shared out over a.parts CTAs that know nothing of one another;
 // their fp32 sums go to the workspace, where cross_dkv_sum_kernel adds them in order (few tiles that many rows see).
 template <int D, int NC, bool kParts>
-__global__ void __launch_bounds__(kThreads, dkv::Cols<D>::kCtas)
+__global__ void __launch_bounds__(dkv::Cols<D>::kThreads, 1)
 cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap gmap,
                  const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
 {
     using namespace dkv;
     using T = Cols<D>;
-    constexpr int kPanels = D / 64, kKTile = kPanels * kKPanel, kQTile = kPanels * kQPanel, kBuf = T::kBuffers;
-    constexpr uint32_t kColS = T::kS, kColDP = T::kDP, kColV = T::kV, kColAcc = T::kAcc;
+    constexpr int kPanels = D / 64, kKTile = kPanels * kKPanel, kQTile = kPanels * kQPanel, kBuf = T::kBuffers, kDPs = T::kDPs, kStages = T::kStages,
+                  kGroups = T::kGroups, kSoft = T::kSoft;
+    constexpr uint32_t kColS = 0, kColDP = T::kDP, kColV = T::kV, kColAcc = T::kAcc;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t *sk = smem;
@@ -183,7 +190,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     }
     if (t.steps == 0) {   // keys that no row sees
         if (rank == 0)
-            for (int i = tid; i < t.nk * (D / 8); i += kThreads) {
+            for (int i = tid; i < t.nk * (D / 8); i += T::kThreads) {
                 const size_t r = (size_t)(t.k0 + i / (D / 8));
                 const int c = g * D + i % (D / 8) * 8;
                 *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.dk + r * a.dk_stride + c) = make_uint4(0, 0, 0, 0);
@@ -201,32 +208,32 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     const int used = a.block_tokens * a.group;   // rows of a block that its copies write
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
 
-    if (tid == 0) {
-        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), (i == B_PFULL || i == B_PFULL + 1 || i == B_DPFREE || i == B_VT) ? 8
-                                                                  : i == B_SFULL || i == B_SFULL + 1 ? 2 : 1);
-        *abort_flag = 0;
+    if (tid < B_COUNT) {
+        const int i = tid;
+        mbar_init(bar(i), (i >= B_PFULL && i < B_ACC) || (i >= B_DPFREE && i <= B_VT) ? 8 : i >= B_SFULL && i < B_PFULL ? 2 : 1);
+        if (i == 0) *abort_flag = 0;
         fence_barrier_init();
     }
     if (used < kBlk) {   // the others are zeros throughout: they are summed over
-        for (int i = tid; i < 2 * kStages * kPanels * (kBlk - used) * 8; i += kThreads) {
+        for (int i = tid; i < 2 * kStages * kPanels * (kBlk - used) * 8; i += T::kThreads) {
             const int r = i / 8 % (kBlk - used) + used, b = i / 8 / (kBlk - used);
             *reinterpret_cast<uint4 *>(sq + b * kQPanel + r * 128 + i % 8 * 16) = make_uint4(0, 0, 0, 0);
         }
         fence_proxy_async_smem();
     }
-    if (warp == 9) {
-        tmem_alloc(smem_u32(tmem_slot), T::kAll);
+    if (warp == kSoft + 1) {
+        tmem_alloc(smem_u32(tmem_slot), 512);
         tmem_relinquish();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-    const int lq = warp & 3, ch = warp >> 2;          // softmax warps: TMEM lane quarter, column half
+    const int lq = warp & 3, ch = warp >> 2 & 1, grp = warp >> 3;   // softmax warps: TMEM lane quarter, column half, group
     const uint32_t lanes = (uint32_t)(lq * 32) << 16;
     bool sums = false;                                // softmax warps: this CTA's dV and dK are complete
 
-    if (warp == 8) {
+    if (warp == kSoft) {
         // ---------------------------------------------------------------- TMA producer
         if (lane == 0 && nu == 0) pdl_wait_prerequisite();
         if (lane == 0 && nu > 0) {
@@ -267,14 +274,14 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             for (int u = (issued > kStages ? issued - kStages : 0); u < issued; ++u)
                 mbar_wait_bounded(bar(B_QFULL + u % kStages), (u / kStages) & 1, a.err, 152);
         }
-    } else if (warp >= 9) {
+    } else if (warp > kSoft) {
         // ---------------------------------------------------------------- MMA issuers (whole warps)
         if (nu > 0) {
             auto wait_w = [&](int b, uint32_t parity, int site) {
                 return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
             };
             constexpr uint32_t idS = umma_idesc_bf16(128, kBlk, false), idAcc = umma_idesc_bf16(128, D, true);
-            if (warp == 9) {
+            if (warp == kSoft + 1) {
                 const uint64_t dK = umma_desc_sw128(smem_u32(sk), 16, 1024);
                 bool ok = wait_w(B_KV, 0, 160);
                 for (int u = 0; ok && u < nu; ++u) {
@@ -288,17 +295,17 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     else umma_bf16_ss_k64_warp(tmem + kColS + b, dK, dq, idS);
                     umma_commit_warp(bar(B_SFULL + u % kBuf));
                 }
-            } else if (warp == 11) {
+            } else if (warp == kSoft + 3) {
                 const uint64_t dV = umma_desc_sw128(smem_u32(sv), 16, 1024);   // (64 dims)
                 bool ok = D == 64 ? wait_w(B_KV, 0, 166) : wait_w(B_VT, 0, 166);
                 for (int u = 0; ok && u < nu; ++u) {
                     const int s = u % kStages;
-                    ok = wait_w(B_QFULL + s, (u / kStages) & 1, 167) && (u == 0 || wait_w(B_DPFREE, (u - 1) & 1, 165));
+                    ok = wait_w(B_QFULL + s, (u / kStages) & 1, 167) && (u < kDPs || wait_w(B_DPFREE + u % kDPs, (u / kDPs - 1) & 1, 165));
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t dg = umma_desc_sw128(smem_u32(sg + s * kQTile), 16, 1024);
-                    if constexpr (D == 128) umma_bf16_ts_k128_warp<kQPanel>(tmem + kColDP, tmem + kColV, dg, idS);
-                    else umma_bf16_ss_k64_warp(tmem + kColDP, dV, dg, idS);
+                    if constexpr (D == 128) umma_bf16_ts_k128_warp<kQPanel>(tmem + kColDP + 64 * (u % kDPs), tmem + kColV, dg, idS);
+                    else umma_bf16_ss_k64_warp(tmem + kColDP + 64 * (u % kDPs), dV, dg, idS);
                     umma_commit_warp(bar(B_SFULL + u % kBuf));
                 }
             } else {
@@ -318,8 +325,8 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 }
             }
             // every MMA issued above must complete before tensor memory is read or released
-            umma_commit_warp(bar(B_FINAL + warp - 9));
-            mbar_wait_bounded(bar(B_FINAL + warp - 9), 0, a.err, 164);
+            umma_commit_warp(bar(B_FINAL + warp - kSoft - 1));
+            mbar_wait_bounded(bar(B_FINAL + warp - kSoft - 1), 0, a.err, 164);
         }
     } else {
         // ---------------------------------------------------------------- softmax + epilogue
@@ -328,15 +335,15 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
         };
         bool ok = true;
-        if (D == 128 && nu > 0 && (ok = wait_all(B_KV, 0, 173))) {   // V's rows into tensor memory, half of the dims a thread
+        if (D == 128 && grp == 0 && nu > 0 && (ok = wait_all(B_KV, 0, 173))) {   // V's rows into tensor memory, half of the dims a thread
             HalfRow<D>::to_tmem(tmem + lanes + kColV, sv, ch, lq * 32 + lane, kKPanel);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
             mbar_arrive_warp(bar(B_VT));
         }
-        Steps st(a, t, nu > 0 ? ub : 0);
-        for (int u = 0; ok && u < nu; ++u) {
+        Steps st(a, t, grp < nu ? ub + grp : 0);
+        for (int u = grp; ok && u < nu; u += kGroups) {
             const int s = u % kStages;
             const uint32_t b = (uint32_t)(u % kBuf) * 64 + 32 * ch;
             const int rows = __shfl_sync(0xffffffffu, st.tokens(a), 0) * a.group;
@@ -349,13 +356,13 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 break;
             }
             tc_fence_after();
-            st.next(u + 1 < nu);
+            for (int i = 1; i <= kGroups; ++i) st.next(u + i < nu);
             uint32_t vis = 0xffffffffu;
             if (partial) {
                 // the block's rows past the segment's, which the products below sum over: zeros (S and dP, which
                 // have read them, are done)
                 vis = interval_bits(0, rows, 32 * ch);
-                for (int i = tid; i < (kBlk - rows) * 8 * kPanels; i += 256) {
+                for (int i = tid & 255; i < (kBlk - rows) * 8 * kPanels; i += 256) {
                     const int r = rows + i / 8 % (kBlk - rows), p = i / 8 / (kBlk - rows), o = p * kQPanel + r * 128 + i % 8 * 16;
                     *reinterpret_cast<uint4 *>(sq + s * kQTile + o) = make_uint4(0, 0, 0, 0);
                     *reinterpret_cast<uint4 *>(sg + s * kQTile + o) = make_uint4(0, 0, 0, 0);
@@ -366,19 +373,18 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             const float4 *da = reinterpret_cast<const float4 *>(aux + s * kAuxBytes + kBlk * 4) + 8 * ch;
             const uint64_t c2 = f2_pack(c, c);
             const bool any_blind = __any_sync(0xffffffffu, blind);
-            // kCols row columns at a time: all 32, or 16 where two CTAs share the registers
-            constexpr int kCols = T::kCtas == 2 ? 16 : 32;
+            constexpr int kCols = kGroups == 2 ? 16 : 32;   // row columns at a time (96 registers a thread with two groups)
             uint32_t pk[16], dk[16];
 #pragma unroll
             for (int h = 0; h < 32; h += kCols) {
                 uint32_t sr[kCols], dr[kCols];
                 tmem_ld_cols(tmem + lanes + kColS + b + h, sr);
-                tmem_ld_cols(tmem + lanes + kColDP + 32 * ch + h, dr);
+                tmem_ld_cols(tmem + lanes + kColDP + 64 * (u % kDPs) + 32 * ch + h, dr);
                 tmem_ld_wait();
                 if (h + kCols == 32) {
                     tc_fence_before();
                     __syncwarp();
-                    mbar_arrive_warp(bar(B_DPFREE));
+                    mbar_arrive_warp(bar(B_DPFREE + u % kDPs));
                 }
                 // two row columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D), both rounded to the
                 // MMAs' operand type (half a step, 2^-9 of a value on average)
@@ -428,13 +434,16 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         tc_fence_after();
     }
     // Epilogue. The 2 D columns of dV | dK are split over the cluster's CTAs: each one's softmax threads
-    // (a key row and half of the columns each) send the other CTAs' parts to their shared memory, which
+    // (a key row and some of the columns each) send the other CTAs' parts to their shared memory, which
     // nothing else uses any more, add what they receive to their own part in rank order and write it.
-    constexpr int kPart = 2 * D / NC, kHalfPart = kPart / 2;   // columns of a CTA, of a thread
+    // Both groups' warps take part where their shares are 16 columns or more, else the first's.
+    constexpr int kPart = 2 * D / NC, kShares = kGroups == 2 && kPart >= 64 ? 4 : 2, kHalfPart = kPart / kShares;   // columns of a CTA, of a thread
+    const int cs = kShares == 4 ? 2 * grp + ch : ch;
+    sums = sums && (kShares == 4 || grp == 0);
     static_assert(kHalfPart % 16 == 0, "");
     auto part = [&](int p, int c, uint32_t (&o)[16]) {       // 16 of this CTA's sums of part p
         if (nu > 0) {
-            tmem_ld16(tmem + lanes + kColAcc + kPart * p + kHalfPart * ch + c, o);
+            tmem_ld16(tmem + lanes + kColAcc + kPart * p + kHalfPart * cs + c, o);
             tmem_ld_wait();
         } else {
 #pragma unroll
@@ -444,7 +453,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     // the place of a thread's 16 columns from CTA `from` in the receiver's shared memory
     auto slot = [&](int from, int to, int c) {
         const int n = from < to ? from : from - 1;
-        return (uint32_t)(n * kPart * kKT * 4 + (kHalfPart * ch + c) * kKT * 4 + (lq * 32 + lane) * 16);
+        return (uint32_t)(n * kPart * kKT * 4 + (kHalfPart * cs + c) * kKT * 4 + (lq * 32 + lane) * 16);
     };
     static_assert((NC - 1) * kPart * kKT * 4 <= 2 * kKTile + 2 * kStages * kQTile, "");
     if (NC > 1) {
@@ -488,7 +497,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     acc[i + 2] += x.z;
                     acc[i + 3] += x.w;
                 }
-            const int col = (kParts ? 0 : kPart * rank) + kHalfPart * ch + c, r = lq * 32 + lane;
+            const int col = (kParts ? 0 : kPart * rank) + kHalfPart * cs + c, r = lq * 32 + lane;
             if constexpr (kParts) {
                 float *dst = a.part_dkv + ((size_t)blockIdx.x * kKT + r) * (2 * D) + col;
                 if (r < t.nk) {
@@ -506,29 +515,37 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == kSoft + 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, T::kAll);
+        tmem_dealloc(tmem, 512);
     }
 }
 
-// Four columns of a key row's dV | dK a thread: the parts' sums in their order (a part without steps wrote none).
+// 32 pieces of four columns of a key row's dV | dK a CTA, the parts' sums by eight warps (each an eighth of the parts, in
+// their order), then the warps' in theirs. A part without steps wrote none.
 template <int D>
 __global__ void __launch_bounds__(256) cross_dkv_sum_kernel(const padoc_cross_args a)
 {
-    constexpr int kPer = dkv::kKT * 2 * D / 4 / 256;   // CTAs of a tile
-    const int unit = blockIdx.x / kPer, g = unit % a.hkv;
+    constexpr int kRow = 2 * D / 4 / 32;   // CTAs of a row
+    __shared__ float4 sums[8][32];
+    const int unit = blockIdx.x / (dkv::kKT * kRow), g = unit % a.hkv, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const padoc_cross_key_tile t = a.tiles[unit / a.hkv];
-    const int i = blockIdx.x % kPer * 256 + threadIdx.x, r = i / (D / 2), col = i % (D / 2) * 4;
+    const int r = blockIdx.x / kRow % dkv::kKT, col = (blockIdx.x % kRow * 32 + lane) * 4;
     if (r >= t.nk || t.steps == 0) return;
     const float *src = a.part_dkv + ((size_t)unit * a.parts * dkv::kKT + r) * (2 * D) + col;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int p = 0; p < a.parts; ++p) {
-        if ((int)((int64_t)t.steps * (p + 1) / a.parts) == (int)((int64_t)t.steps * p / a.parts)) continue;
-        const float4 y = *reinterpret_cast<const float4 *>(src + (size_t)p * dkv::kKT * (2 * D));
+#pragma unroll 4
+    for (int p = warp; p < a.parts; p += 8) {
+        const bool some = (int)((int64_t)t.steps * (p + 1) / a.parts) != (int)((int64_t)t.steps * p / a.parts);
+        const float4 y = some ? *reinterpret_cast<const float4 *>(src + (size_t)p * dkv::kKT * (2 * D)) : make_float4(0.f, 0.f, 0.f, 0.f);
         x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
     }
+    sums[warp][lane] = x;
+    __syncthreads();
+    if (warp) return;
+    x = sums[0][lane];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) x = make_float4(x.x + sums[w][lane].x, x.y + sums[w][lane].y, x.z + sums[w][lane].z, x.w + sums[w][lane].w);
     const bool isk = col >= D;
     const float mul = isk ? a.scale : 1.f;
     __nv_bfloat16 *dst = isk ? (__nv_bfloat16 *)a.dk + (size_t)(t.k0 + r) * a.dk_stride + g * D + (col - D)
@@ -542,18 +559,15 @@ __global__ void __launch_bounds__(256) cross_dkv_sum_kernel(const padoc_cross_ar
 namespace dqp {
 constexpr int kQT = PADOC_CROSS_DQ_BLOCKS * kBlk;   // 128 rows: the M of every MMA
 constexpr int kW = PADOC_CROSS_DQ_STEP;             // 64 keys per step
-constexpr int kMaxStages = 4;
-constexpr int kMaxSlots = 3;
+constexpr int kThreads = 384;
+constexpr int kMaxStages = 10;
 constexpr int kQPanel = kQT * 128;           // [128 rows][64 bf16]
 constexpr int kKPanel = kW * 128;            // [64 rows][64 bf16]
-// Tensor memory: Q as an A operand, S (a step's dS takes its S's place), dP, dQ; three S and two dP buffers, or with 64
-// dims, where two CTAs share an SM, one of each in 256 columns.
+// Tensor memory columns: Q as an A operand, three S buffers (a step's dS takes its S's place), two dP, dQ.
+constexpr int kSlots = 3;
+constexpr uint32_t kColQ = 0, kColS = 64, kColDP = 256, kColDQ = 384;
 template <int D>
-struct Cols {
-    static constexpr int kCtas = D == 64 ? 2 : 1, kSlots = D == 64 ? 1 : 3, kDPs = D == 64 ? 1 : 2, kStages = D == 64 ? 3 : 4;
-    static constexpr uint32_t kQ = 0, kS = D / 2, kDP = kS + 64 * kSlots, kDQ = kDP + 64 * kDPs, kAll = 512 / kCtas;
-    static_assert(kDQ + D <= kAll, "");
-};
+constexpr int stages() { return D == 64 ? 10 : 4; }   // (with 64 dims 81 -> 65 us, as in the dK/dV pass)
 enum {
     B_QROWS = 0,                   // the unit's Q has landed
     B_GROWS = 1,                   // its dO and O have landed
@@ -584,21 +598,19 @@ constexpr int kReaders = 11;       // softmax and issuing warps
 template <int D>
 constexpr size_t smem_bytes()
 {
-    return 1024 + 3 * (size_t)(D / 64) * kQPanel + 2 * (size_t)Cols<D>::kStages * (D / 64) * kKPanel + 2 * sizeof(Unit) + 16 + B_COUNT * 8 + 32 + 2 * kQT * 4;
+    return 1024 + 3 * (size_t)(D / 64) * kQPanel + 2 * (size_t)stages<D>() * (D / 64) * kKPanel + 2 * sizeof(Unit) + 16 + B_COUNT * 8 + 32 + 2 * kQT * 4;
 }
-static_assert(smem_bytes<128>() <= 232448 && 2 * (smem_bytes<64>() + 1024) <= 233472, "shared memory of an SM");
+static_assert(smem_bytes<128>() <= 232448 && smem_bytes<64>() <= 232448, "shared memory per CTA");
 }  // namespace dqp
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, dqp::Cols<D>::kCtas)
+__global__ void __launch_bounds__(dqp::kThreads, 1)
 cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap gmap,
                 const __grid_constant__ CUtensorMap omap, const __grid_constant__ CUtensorMap kmap,
                 const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
 {
     using namespace dqp;
-    using T = Cols<D>;
-    constexpr int kPanels = D / 64, kQTile = kPanels * kQPanel, kKTile = kPanels * kKPanel, kStages = T::kStages, kSlots = T::kSlots, kDPs = T::kDPs;
-    constexpr uint32_t kColQ = T::kQ, kColS = T::kS, kColDP = T::kDP, kColDQ = T::kDQ;
+    constexpr int kPanels = D / 64, kQTile = kPanels * kQPanel, kKTile = kPanels * kKPanel, kStages = stages<D>();
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t *sq = smem;                        // Q, dO and O rows; dQ leaves by way of Q's place
@@ -619,13 +631,12 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     pdl_launch_dependents();   // the dK/dV pass may take the SMs that run out of work here
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
 
-    if (tid == 0) {
-        for (int i = 0; i < B_COUNT; ++i) {
-            const bool soft = i == B_QT || i == B_D || i == B_DREAD || i == B_QFREE || i == B_DQFREE ||
-                              (i >= B_PFULL && i < B_PFULL + kMaxSlots) || i == B_DPFREE || i == B_DPFREE + 1;
-            mbar_init(bar(i), soft ? 8 : i == B_UEMPTY || i == B_UEMPTY + 1 ? kReaders : i >= B_SFULL && i < B_SFULL + kMaxSlots ? 2 : 1);
-        }
-        *abort_flag = 0;
+    if (tid < B_COUNT) {
+        const int i = tid;
+        const bool soft = i == B_QT || i == B_D || i == B_DREAD || i == B_QFREE || i == B_DQFREE ||
+                          (i >= B_PFULL && i < B_PFULL + kSlots) || i == B_DPFREE || i == B_DPFREE + 1;
+        mbar_init(bar(i), soft ? 8 : i == B_UEMPTY || i == B_UEMPTY + 1 ? kReaders : i >= B_SFULL && i < B_SFULL + kSlots ? 2 : 1);
+        if (i == 0) *abort_flag = 0;
         fence_barrier_init();
     }
     if (used < kBlk) {   // rows that no copy writes (dQ's way out puts what it likes there)
@@ -636,7 +647,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
         fence_proxy_async_smem();
     }
     if (warp == 9) {
-        tmem_alloc(smem_u32(tmem_slot), T::kAll);
+        tmem_alloc(smem_u32(tmem_slot), 512);
         tmem_relinquish();
     }
     tc_fence_before();
@@ -675,8 +686,9 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             }
             int tk = 0, nq = 0, ng = 0;   // K/V tiles, Q tiles, dO and O tiles issued so far
             bool ok = true, more = true, asked = false;
-            // asked with the unit's last tile: early enough for the answer, and late enough that no CTA
-            // holds a second unit while others run out of work
+            // asked eight steps before the unit's last copies: early enough for the answer and the next unit's rows, and
+            // late enough that no CTA holds a second unit for long while others run out of work
+            constexpr int kAsk = 8;
             auto ask = [&]() {
                 if (a.ctas) return;
                 mbar_arrive_expect_tx(bar(B_NEXT), 16);
@@ -700,12 +712,19 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                         tma_load_3d(smem_u32(dst) + (i >> 1) * kQPanel + (i & 1) * kBlk * 128, map, 64 * (i >> 1), u.g * a.group,
                                     u.tok + (i & 1) * a.block_tokens, bar(b));
                 };
+                // (dO and O cannot be copied before the unit before has used its own: their way from memory starts now)
+                if (n > 0)
+#pragma unroll
+                    for (int i = 0; i < 2 * kPanels; ++i) {
+                        tma_prefetch_l2_3d(&gmap, 64 * (i >> 1), u.g * a.group, u.tok + (i & 1) * a.block_tokens);
+                        tma_prefetch_l2_3d(&omap, 64 * (i >> 1), u.g * a.group, u.tok + (i & 1) * a.block_tokens);
+                    }
                 if (n > 0 && !wait(B_QFREE, (n - 1) & 1, 184)) break;
                 mbar_arrive_expect_tx(bar(B_QROWS), 2 * kPanels * used * 128);
                 rows(sq, &qmap, B_QROWS);
                 ++nq;
                 for (int j = 0; j < u.steps; ++j, ++tk) {
-                    if (j + 1 == u.steps) ask();
+                    if (j == max(u.steps - kAsk, 0)) ask();
                     const int s = tk % kStages;
                     if (tk >= kStages && !(ok = wait(B_KEMPTY + s, (tk / kStages - 1) & 1, 180))) break;
                     const int row = u.k0 + j * kW;
@@ -774,12 +793,12 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 for (int u = 0; ok && u < un.steps; ++u, next_step()) {
                     const int s = c % kStages;
                     ok = wait_w(B_KFULL + s, (c / kStages) & 1, 198) &&
-                         (c < kDPs || wait_w(B_DPFREE + c % kDPs, (c / kDPs - 1) & 1, 199));
+                         (c < 2 || wait_w(B_DPFREE + (c & 1), ((c >> 1) - 1) & 1, 199));
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t dv = umma_desc_sw128(smem_u32(sv + s * kKTile), 16, 1024);
-                    if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kQPanel, kKPanel>(tmem + kColDP + 64 * (c % kDPs), dg, dv, idS);
-                    else umma_bf16_ss_k64_warp(tmem + kColDP + 64 * (c % kDPs), dg, dv, idS);
+                    if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kQPanel, kKPanel>(tmem + kColDP + 64 * (c & 1), dg, dv, idS);
+                    else umma_bf16_ss_k64_warp(tmem + kColDP + 64 * (c & 1), dg, dv, idS);
                     umma_commit_warp(bar(B_SFULL + slot));
                 }
                 umma_commit_warp(bar(B_GFREE));
@@ -921,38 +940,31 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                             make_uint4(0, 0, 0, 0);
                     fence_proxy_async_smem();
                 }
-                uint32_t dk[16];
-                constexpr int kCols = T::kCtas == 2 ? 16 : 32;
+                uint32_t sr[32], dr[32], dk[16];
+                tmem_ld32(b, sr);
+                tmem_ld32(tmem + lanes + kColDP + 64 * (c & 1) + 32 * ch, dr);
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_warp(bar(B_DPFREE + (c & 1)));
+                // two key columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D)
+                auto column_pairs = [&](auto masked) {
 #pragma unroll
-                for (int h = 0; h < 32; h += kCols) {
-                    uint32_t sr[kCols], dr[kCols];
-                    tmem_ld_cols(b + h, sr);
-                    tmem_ld_cols(tmem + lanes + kColDP + 64 * (c % kDPs) + 32 * ch + h, dr);
-                    tmem_ld_wait();
-                    if (h + kCols == 32) {
-                        tc_fence_before();
-                        __syncwarp();
-                        mbar_arrive_warp(bar(B_DPFREE + c % kDPs));
-                    }
-                    // two key columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D)
-                    auto column_pairs = [&](auto masked) {
-#pragma unroll
-                        for (int i = 0; i < kCols; i += 2) {
-                            float x0, x1;
-                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2, nl2), x0, x1);
-                            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-                            const uint64_t t2 = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])), d2);
-                            float d0, d1;
-                            f2_unpack(f2_mul(f2_pack(p0, p1), t2), d0, d1);
-                            if (decltype(masked)::value) {
-                                d0 = (vis >> (h + i)) & 1u ? d0 : 0.f;
-                                d1 = (vis >> (h + i + 1)) & 1u ? d1 : 0.f;
-                            }
-                            dk[(h + i) >> 1] = pack_bf16x2(d0, d1);
+                    for (int i = 0; i < 32; i += 2) {
+                        float x0, x1;
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2, nl2), x0, x1);
+                        const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+                        const uint64_t t2 = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])), d2);
+                        float d0, d1;
+                        f2_unpack(f2_mul(f2_pack(p0, p1), t2), d0, d1);
+                        if (decltype(masked)::value) {
+                            d0 = (vis >> i) & 1u ? d0 : 0.f;
+                            d1 = (vis >> (i + 1)) & 1u ? d1 : 0.f;
                         }
-                    };
-                    if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
-                }
+                        dk[i >> 1] = pack_bf16x2(d0, d1);
+                    }
+                };
+                if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
                 tmem_st16(b, dk);   // over the first half of this thread's own S columns
                 tmem_st_wait();
                 tc_fence_before();
@@ -966,7 +978,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     __syncthreads();
     if (warp == 9) {
         tc_fence_after();
-        tmem_dealloc(tmem, T::kAll);
+        tmem_dealloc(tmem, 512);
     }
 }
 
@@ -981,7 +993,7 @@ padoc_status launch_dkv(const CUtensorMap &qmap, const CUtensorMap &gmap, const 
     if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dkv::smem_bytes<D>())) return st;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)((a.num_tiles + a.tail_tiles) * a.hkv * (kParts ? a.parts : NC)));
-    lc.blockDim = dim3(kThreads);
+    lc.blockDim = dim3(dkv::Cols<D>::kThreads);
     lc.dynamicSmemBytes = dkv::smem_bytes<D>();
     lc.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -1007,7 +1019,7 @@ padoc_status run(const padoc_cross_args &a, int cluster, cudaStream_t stream)
         auto kernel = cross_dkv_kernel<D, 1, false>;
         if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dkv::smem_bytes<D>())) return st;
         if (a.num_tiles + a.tail_tiles)
-            kernel<<<(unsigned)((a.num_tiles + a.tail_tiles) * a.hkv), kThreads, dkv::smem_bytes<D>(), stream>>>(none, none, kv, kv, a);
+            kernel<<<(unsigned)((a.num_tiles + a.tail_tiles) * a.hkv), dkv::Cols<D>::kThreads, dkv::smem_bytes<D>(), stream>>>(none, none, kv, kv, a);
         return padoc_launch_status();
     }
     if (!padoc_make_tmap_bf16_heads(&qmap, a.q, D, a.hq, a.query_rows, a.q_stride * 2, a.group, a.block_tokens) ||
@@ -1018,12 +1030,12 @@ padoc_status run(const padoc_cross_args &a, int cluster, cudaStream_t stream)
         return PADOC_ERR_CUDA;
     auto kernel = cross_dq_kernel<D>;
     if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dqp::smem_bytes<D>())) return st;
-    kernel<<<(unsigned)(a.ctas ? a.num_ctas : a.num_units), kThreads, dqp::smem_bytes<D>(), stream>>>(qmap, gmap, omap, kmap, vmap, a);
+    kernel<<<(unsigned)(a.ctas ? a.num_ctas : a.num_units), dqp::kThreads, dqp::smem_bytes<D>(), stream>>>(qmap, gmap, omap, kmap, vmap, a);
     const padoc_status st = padoc_launch_status();
     if (st != PADOC_OK) return st;
     if (a.parts > 1) {
         if (const padoc_status s2 = launch_dkv<D, 1, true>(qmap, gmap, a, true, stream)) return s2;
-        cross_dkv_sum_kernel<D><<<(unsigned)(a.num_tiles * a.hkv * (dkv::kKT * 2 * D / 4 / 256)), 256, 0, stream>>>(a);
+        cross_dkv_sum_kernel<D><<<(unsigned)(a.num_tiles * a.hkv * (dkv::kKT * 2 * D / 128)), 256, 0, stream>>>(a);
         return padoc_launch_status();
     }
     switch (cluster) {

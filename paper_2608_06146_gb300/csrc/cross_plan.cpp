@@ -298,7 +298,7 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
 
     // Forward. Times in us: of two 128-row tiles' steps of 128 keys, and for few rows of a 64-key tile's bytes at the
     // SM's share of the memory bandwidth (45 KB a us), which its CTAs share.
-    // With 64 dims an item is one tile and two CTAs share an SM, in the forward and in the backward.
+    // With 64 dims an item is one tile and two CTAs share an SM.
     const int32_t an_sm = !f32 && cfg->head_dim == 64 ? 2 : 1, unit_blocks = PADOC_CROSS_UNIT_BLOCKS / an_sm;
     int32_t per = unit_blocks * block;
     {
@@ -315,7 +315,7 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
     if (cfg->backward) {
         const Costs bwd = {6.f, 2.f, 6.f, 0.018f, 1.f, PADOC_CROSS_DQ_STEP, 4};   // (a step of a tile lasts about 0.55 us)
         const Costs &k = f32 ? simt : bwd;
-        const int32_t lanes = f32 ? std::max(1, sms / PADOC_CROSS_DQ_BLOCKS) : sms * an_sm;
+        const int32_t lanes = f32 ? std::max(1, sms / PADOC_CROSS_DQ_BLOCKS) : sms;
         plan_work(chunks_of(PADOC_CROSS_DQ_BLOCKS * block, k), hkv, lanes, k, cuts, b.dq);
         empty_rows(PADOC_CROSS_DQ_BLOCKS * block, b.dq.merges);
 

@@ -105,17 +105,16 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     const int tile_tokens = 2 * a.block_tokens;
     pdl_launch_dependents();   // the joining of split rows, where there is one, may take the SMs that run out of work
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
-    if (tid == 0) {
-        for (int i = 0; i < C::B_COUNT; ++i) {
-            int n = 1;
-            if (i >= C::B_PFULL && i < C::B_PFULL + 4) n = 4;
-            if (i == C::B_OFREE || i == C::B_OFREE + 1) n = 4;
-            if (i >= C::B_KEMPTY && i < C::B_KEMPTY + kStages) n = C::kTiles;
-            if (i >= C::B_VEMPTY && i < C::B_VEMPTY + kStages) n = C::kTiles;
-            if (i == C::B_UEMPTY || i == C::B_UEMPTY + 1) n = C::kReaders;
-            mbar_init(bar(i), n);
-        }
-        *abort_flag = 0;
+    if (tid < C::B_COUNT) {
+        const int i = tid;
+        int n = 1;
+        if (i >= C::B_PFULL && i < C::B_PFULL + 4) n = 4;
+        if (i == C::B_OFREE || i == C::B_OFREE + 1) n = 4;
+        if (i >= C::B_KEMPTY && i < C::B_KEMPTY + kStages) n = C::kTiles;
+        if (i >= C::B_VEMPTY && i < C::B_VEMPTY + kStages) n = C::kTiles;
+        if (i == C::B_UEMPTY || i == C::B_UEMPTY + 1) n = C::kReaders;
+        mbar_init(bar(i), n);
+        if (i == 0) *abort_flag = 0;
         fence_barrier_init();
     }
     // items of this CTA: x and, of a list, those up to xe; the first one is on its way while the barriers are set
