@@ -75,14 +75,16 @@ def forward_bounds(segments, q, k, v, scale):
     return bo, bl
 
 
-def backward_bounds(segments, q, k, v, out, dout, scale):
-    """Largest |error| of dq, dk and dv for an out given in the inputs' type (r its half step) and an lse in fp32.
+def backward_bounds(segments, q, k, v, out, dout, scale, off=None):
+    """Largest |error| of dq, dk and dv for an out given in the inputs' type (r its half step; off by at most `off` more) and
+    an lse in fp32.
 
     P is off by eP = 2 e + (|lse| + 4) 2^-21 of itself; D = dout . out by r |dout|.|out| (out's rounding) and d 2^-24
     of that; dP by d 2^-24 |dout|.|v|; dS = P (dP - D) by P (those) + eP |dS|, and by r |dS| when it is rounded; so
       |dq error| <= scale sum_j (|dS error|_ij + r |dS_ij|) |k_j| + r |dq|, sums of n terms adding n 2^-24 of |.|."""
     r = HALF[q.dtype]
     q, k, v, out, dout = (t.double() for t in (q, k, v, out, dout))
+    off = torch.zeros_like(out) if off is None else off
     bq, bk, bv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
     d = q.shape[2]
     rows = sum(s[1] for s in segments) * q.shape[1]     # (no key's sum has more terms)
@@ -93,7 +95,7 @@ def backward_bounds(segments, q, k, v, out, dout, scale):
         ep = 2 * e + (lse.abs() + 4) * 2.0 ** -21
         p, dp = torch.softmax(s, 1), dout[a, h] @ v[b, g].T
         ds = p * (dp - (p * dp).sum(1, keepdim=True))
-        dd = (r + (d + 4) * 2.0 ** -24) * (dout[a, h].abs() * out[a, h].abs()).sum(1, keepdim=True)
+        dd = ((r + (d + 4) * 2.0 ** -24) * dout[a, h].abs() * out[a, h].abs() + dout[a, h].abs() * off[a, h]).sum(1, keepdim=True)
         eds = p * (dd + (d + 4) * 2.0 ** -24 * (dout[a, h].abs() @ v[b, g].abs().T)) + (ep + 2.0 ** -22) * \
             (p * (dp.abs() + (p * dp).sum(1, keepdim=True).abs())) + \
             FLUSHED * (1 + dp.abs() + (p * dp).sum(1, keepdim=True).abs())

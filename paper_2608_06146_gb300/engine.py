@@ -202,6 +202,9 @@ class MaskedParallelLoop:
     Between steps a branch can be forked with its history (fork_stream), streams and pages dropped, and the
     pool compacted or replaced by one of another size (compact, resize).
 
+    With an encoder a page is admitted with the rows of its image's states (states); its branches have them too, or a
+    range of their own (set_states: a region's crop), and cross_step is the step's cross attention over them.
+
     Memory that a call needs more of is allocated on that call's stream. Calls on different streams are ordered by
     the caller, the first one behind the stream that was current when the loop was made (its pool is zeroed there)."""
 
@@ -230,6 +233,11 @@ class MaskedParallelLoop:
         self.last_stage = None
         self.h2d_bytes = 0
         self._runner = None
+        self._states = np.zeros((0, 2), np.int32)   # each stream's key rows (first, number), by stream id
+        self._step_ids = None
+        self._cross_ints = torch.empty(1024, dtype=torch.int32, device=device)
+        self._cross_workspace = torch.empty(256, dtype=torch.uint8, device=device)
+        self._cross_plan = None                     # (segments, config) and summary of the plan in _cross_ints
 
     def _grow(self, name, rows, stream):
         """Makes the array ``name`` at least rows long for use on ``stream``, where the old one may still be in use."""
@@ -240,7 +248,7 @@ class MaskedParallelLoop:
                 new = torch.empty((max(rows, 2 * old.shape[0]),) + tuple(old.shape[1:]), dtype=old.dtype, device=self.device)
             setattr(self, name, new)
 
-    def _room(self, sizes, stream):
+    def _room(self, sizes, stream, to="_ints"):
         """Room for an upload of arrays of these sizes on ``stream``; returns their places and the words."""
         offs, n = [], 0
         for size in sizes:
@@ -251,24 +259,25 @@ class MaskedParallelLoop:
             self._stage_free[b].synchronize()
             self._stage[b] = torch.empty(max(n, 2 * (0 if self._stage[b] is None else self._stage[b].numel()), 4096),
                                          dtype=torch.int32).pin_memory()
-        self._grow("_ints", n, stream)
+        self._grow(to, n, stream)
         return offs, n
 
-    def _upload(self, parts, stream):
-        """Copies int32 host arrays to the device in one transfer, each starting on a 128-byte
-        boundary; returns device views."""
-        offs, n = self._room([a.size for a in parts], stream)
+    def _upload(self, parts, stream, to="_ints"):
+        """Copies int32 host arrays to the device (into the array ``to``) in one transfer, each starting on a
+        128-byte boundary; returns device views."""
+        offs, n = self._room([a.size for a in parts], stream, to)
         b = self._turn & 1
         self._turn += 1
         self._stage_free[b].synchronize()
         host = self._stage[b].numpy()
         for a, o in zip(parts, offs):
             host[o:o + a.size] = a.reshape(-1)
+        dev = getattr(self, to)
         with torch.cuda.stream(stream):
-            self._ints[:n].copy_(self._stage[b][:n], non_blocking=True)
+            dev[:n].copy_(self._stage[b][:n], non_blocking=True)
         self._stage_free[b].record(stream)
         self.h2d_bytes = 4 * n
-        return [self._ints[o:o + a.size] for a, o in zip(parts, offs)]
+        return [dev[o:o + a.size] for a, o in zip(parts, offs)]
 
     def _check_rows(self, k_src, q_src, v_src, pos_src):
         """Refuses source rows that the append with rotary would refuse (by an append of none of them)."""
@@ -278,11 +287,12 @@ class MaskedParallelLoop:
                                       q_src=q_src, q_dst=self.q_step, count=0)
 
     def add_page(self, prefix_len: int, num_forks: int, layout_eos: bool, k_src, v_src, src_rows, stream=None,
-                 pos_src=None):
+                 pos_src=None, states=(0, 0)):
         """Admits a page: its prefix K/V (rows src_rows of k_src / v_src, device tensors [rows][Hkv][d])
-        go into the blocks the scheduler gives it. pos_src: int32 [rows][axes], with rotary. Returns (page
-        id, new stream ids)."""
+        go into the blocks the scheduler gives it. pos_src: int32 [rows][axes], with rotary. states: (first, number)
+        of the encoder's rows that the page's streams see in cross_step. Returns (page id, new stream ids)."""
         stream = stream or torch.cuda.current_stream()
+        states = self._range(*states)
         if self.rotary is not None and prefix_len > 0:   # before the scheduler admits the page
             self._check_rows(k_src, None, v_src, pos_src)
             if len(src_rows) != prefix_len:
@@ -300,7 +310,73 @@ class MaskedParallelLoop:
             else:
                 pa.padoc_append_inputs(self.k_pool, self.v_pool, k_src, v_src, slots_d, src_rows=rows_d, count=prefix_len,
                                        stream=stream)
+        self._give_states(new, states)
         return pid, new
+
+    @staticmethod
+    def _range(first, number):
+        if first < 0 or number < 0 or first + number > 2 ** 31 - 1024:
+            raise ValueError("states: a range of rows")
+        return int(first), int(number)
+
+    def _give_states(self, ids, states):
+        ids = [i for i in ids if i >= 0]
+        if len(ids) == 0 or (states[1] == 0 and len(self._states) == 0):   # (none so far: all are empty)
+            return
+        if max(ids) >= len(self._states):
+            more = np.zeros((max(max(ids) + 1, 2 * len(self._states), 64), 2), np.int32)
+            more[:len(self._states)] = self._states
+            self._states = more
+        self._states[ids] = states
+
+    def set_states(self, stream_id: int, first: int, number: int):
+        """The encoder's rows that a live stream sees in cross_step from now on (and branches forked from it)."""
+        if stream_id < 0:
+            raise ValueError("no such stream")
+        states = self._range(first, number)
+        if stream_id >= len(self._states):
+            self._give_states([stream_id], (0, 1))   # (room, also for an empty range)
+        self._states[stream_id] = states
+
+    def states_of(self, stream_id: int):
+        """(first, number) of the encoder's rows that the stream sees."""
+        return tuple(int(x) for x in self._states[stream_id]) if 0 <= stream_id < len(self._states) else (0, 0)
+
+    def cross_step(self, ids, q, k, v, scale: float, out=None, lse=None, stream=None):
+        """Cross attention of a step's tokens: row i of q [C][Hq][d] is stream ids[i]'s (in the step's order), k and v
+        [rows][Hkv][d] are the encoder's (rows may lie apart). Streams that follow one another and see the same rows
+        read them together. Returns (out [C][Hq][d], lse fp32 [C][Hq]). The plan is built and copied anew only when the
+        streams or their states have changed."""
+        stream = stream or torch.cuda.current_stream()
+        ids = np.asarray(ids, np.int64)
+        if q.shape[0] != ids.size or (ids.size and ids.min() < 0):
+            raise ValueError("q needs a row for each stream")
+        if out is None or lse is None:
+            with torch.cuda.stream(stream):
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+                lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
+        if ids.size == 0:
+            return out, lse
+        if ids.max() >= len(self._states):
+            self._give_states([int(ids.max())], (0, 1))
+            self._states[int(ids.max())] = 0
+        mine = self._states[ids]
+        first = np.flatnonzero(np.concatenate(([True], (mine[1:] != mine[:-1]).any(1))))
+        segments = np.empty((first.size, 4), np.int32)
+        segments[:, 0] = first
+        segments[:, 1] = np.diff(np.append(first, ids.size))
+        segments[:, 2:] = mine[first]
+        key = (segments.tobytes(), q.shape[1], k.shape[1], q.shape[2], q.dtype)
+        if self._cross_plan is None or self._cross_plan[0] != key:
+            cfg = pa.make_cross_config(q.shape[1], k.shape[1], q.shape[2], q.dtype)
+            plan, info = pa.padoc_build_cross_plan(segments, cfg)
+            self._cross_plan = None
+            self._upload([plan], stream, "_cross_ints")
+            self._cross_plan = (key, info)
+        info = self._cross_plan[1]
+        self._grow("_cross_workspace", pa.padoc_cross_workspace_size(info), stream)
+        pa.padoc_cross_attn(info, self._cross_ints, q, k, v, scale, out, lse, self._cross_workspace, stream)
+        return out, lse
 
     def step(self, k_src, v_src, q_src, rows_of, scale: float, out=None, lse=None, stream=None, pos_src=None):
         """One iteration: every live stream appends its next input (rows_of(stream ids) gives the rows
@@ -329,7 +405,7 @@ class MaskedParallelLoop:
                 self._stage[b] = torch.empty(2 * int(need.total_words), dtype=torch.int32).pin_memory()
         host = self._stage[b].numpy()
         C = int(st.num_streams)
-        ids = host[st.off_stream_ids:st.off_stream_ids + C].copy()
+        self._step_ids = ids = host[st.off_stream_ids:st.off_stream_ids + C].copy()
         host[st.off_rows:st.off_rows + C] = rows_of(ids)
         n = int(st.upload_words)
         self._grow("_ints", n, stream)
@@ -371,6 +447,7 @@ class MaskedParallelLoop:
             self._runner.set_rotary(self.rotary, pos_src)
         n, ids = self._runner.step(k_src, v_src, q_src, row_of_stream, scale, out, lse, stream)
         self.h2d_bytes = self._runner.upload_bytes
+        self._step_ids = ids
         return n, ids
 
     def last_run_step(self):
@@ -379,7 +456,11 @@ class MaskedParallelLoop:
 
     def end_step(self, num_forks=None, eos=None, num_streams=None):
         """Each stream's output event (forks, EOS) in step order; returns the new branches' ids."""
-        return self.mpd.end_step(num_forks, eos, num_streams)
+        new = self.mpd.end_step(num_forks, eos, num_streams)
+        if len(new) and len(self._states) and self._step_ids is not None:   # branches see what their stream sees
+            for parent, child in zip(np.repeat(self._step_ids[:len(num_forks)], num_forks), new):
+                self._give_states([int(child)], self.states_of(int(parent)))
+        return new
 
     def _before_copies(self, pairs, stream):
         """Refuses what a copy of up to ``pairs`` blocks within the pool would refuse, and makes its room: the
@@ -404,6 +485,7 @@ class MaskedParallelLoop:
         self._before_copies(max(0, min(num_copies, self.status()[2])), stream)   # (a copy takes a free block)
         new, src, dst = self.mpd.fork_stream(stream_id, num_copies)
         self._copy_blocks(src, dst, stream)
+        self._give_states([int(i) for i in new], self.states_of(int(stream_id)))
         return new
 
     def drop_stream(self, stream_id: int):

@@ -189,10 +189,10 @@ def test_few_keys_that_many_rows_see(hq, hkv, d):
 @pytest.mark.parametrize("keys", [1, 70, 130, 250])
 def test_many_short_items(hq, hkv, d, keys):
     # items of a tile or two, each ending inside one, taken one after the other by every CTA; some with one tile of rows
-    segments = [(40 * i, 40 if i % 3 else 7, keys * i % 900, keys) for i in range(150)]
+    segments = [(40 * i, 40 if i % 3 else 7, keys * i % 900, keys) for i in range(60)]
     check_forward(segments, hq, hkv, d, BF16, poison=False)
     check_backward(segments, hq, hkv, d, BF16, poison=False)
-    segments = [(600 * i, 600, keys * i, keys) for i in range(12)]
+    segments = [(600 * i, 600, keys * i, keys) for i in range(5)]
     check_forward(segments, hq, hkv, d, BF16, poison=False)
     check_backward(segments, hq, hkv, d, BF16, poison=False)
 
@@ -287,6 +287,96 @@ def test_gradients_against_differences(dtype):
             ends.append((oc.forward(segments, *at, 0.125)[0] * dout.double()).sum().item())
         slope = (ends[0] - ends[1]) / 2e-5
         assert abs((got.double() * way).sum().item() - slope) <= (bound * way.abs()).sum().item() + 1e-6 * abs(slope) + 1e-6
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(16, 2, 128, BF16), (16, 16, 64, BF16), (4, 1, 64, F32)])
+def test_a_training_step(hq, hkv, d, dtype):
+    # forward, then the gradients with what it left; k and v, and dk and dv, as slices of fused projections
+    segments = [(0, 200, 0, 150), (200, 30, 40, 60), (230, 77, 150, 301), (307, 9, 0, 0)]
+    q, k, v, dout = inputs(segments, hq, hkv, d, dtype, rows=316, keys=460, wide=hkv)
+    plan = CrossPlan(segments, hq, hkv, d, dtype, DEV, training=True)
+    out, lse = torch.empty_like(dout), torch.empty((316, hq), device=DEV)
+    scale = 1 / math.sqrt(d)
+    plan.run(q, k, v, scale, out, lse)
+    dq, dkv = torch.empty_like(dout), torch.empty((460, 2 * hkv, d), dtype=dtype, device=DEV)
+    plan.run_bwd(q, k, v, out, dout, lse, scale, dq, dkv[:, :hkv], dkv[:, hkv:])
+    pa.padoc_check_device_errors()
+    off, _ = oc.forward_bounds(segments, q, k, v, scale)
+    for got, want, bound in zip((dq, dkv[:, :hkv], dkv[:, hkv:]), oc.backward(segments, q, k, v, dout, scale),
+                                oc.backward_bounds(segments, q, k, v, out, dout, scale, off)):
+        within(got, want, bound)
+
+
+@pytest.mark.parametrize("segments,hq,hkv,d", [
+    ([(0, 1, 0, 961)], 16, 2, 128),                                         # a cluster
+    ([(0, 24, 0, 9001)], 16, 2, 128),                                       # lists of items, joined parts
+    ([(0, 3, 0, 30_000)], 4, 4, 64),                                        # few rows, joined parts
+    ([(0, 700, 0, 300), (700, 40, 300, 1000)], 16, 16, 64),
+    ([(0, 900, 5, 70)], 16, 2, 128)])
+def test_captured_and_replayed(segments, hq, hkv, d):
+    plan = CrossPlan(segments, hq, hkv, d, BF16, DEV, training=True)
+    q, k, v, dout = inputs(segments, hq, hkv, d, BF16, poison=False)
+    out, lse = torch.zeros_like(dout), torch.zeros(q.shape[:2], device=DEV)
+    dq, dk, dv = torch.zeros_like(dout), torch.zeros_like(k), torch.zeros_like(k)
+
+    def both():
+        plan.run(q, k, v, 0.1, out, lse)
+        plan.run_bwd(q, k, v, out, dout, lse, 0.1, dq, dk, dv)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        both()
+        both()
+    for seed in (7, 8):
+        for t, n in zip((q, k, v, dout), inputs(segments, hq, hkv, d, BF16, seed=seed, poison=False)):
+            t.copy_(n)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, lse, dq, dk, dv)]
+        both()
+        pa.padoc_check_device_errors()
+        assert all(torch.equal(a, b) for a, b in zip(got, (out, lse, dq, dk, dv)))
+
+
+def test_two_streams_at_once():
+    # a plan each: the workspaces are a plan's own
+    segments, hq, hkv, d = [(0, 24, 0, 20_001), (24, 300, 20_001, 500)], 16, 2, 128
+    sets = []
+    for seed in (1, 2):
+        q, k, v, dout = inputs(segments, hq, hkv, d, BF16, seed=seed, poison=False)
+        sets.append((CrossPlan(segments, hq, hkv, d, BF16, DEV, training=True), torch.cuda.Stream(), q, k, v, dout,
+                     torch.zeros_like(dout), torch.zeros(q.shape[:2], device=DEV), torch.zeros_like(dout),
+                     torch.zeros_like(k), torch.zeros_like(k)))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for plan, s, q, k, v, dout, out, lse, dq, dk, dv in sets:
+            plan.run(q, k, v, 0.1, out, lse, stream=s)
+            plan.run_bwd(q, k, v, out, dout, lse, 0.1, dq, dk, dv, stream=s)
+    torch.cuda.synchronize()
+    pa.padoc_check_device_errors()
+    for plan, _, q, k, v, dout, *outs in sets:
+        got = [t.clone() for t in outs]
+        plan.run(q, k, v, 0.1, outs[0], outs[1])
+        plan.run_bwd(q, k, v, outs[0], dout, outs[1], 0.1, *outs[2:])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, outs))
+
+
+def test_another_current_device_is_refused(monkeypatch):
+    segments = [(0, 4, 0, 9)]
+    plan = CrossPlan(segments, 4, 2, 64, BF16, DEV, training=True)
+    q, k, v, dout = inputs(segments, 4, 2, 64, BF16)
+    out, lse = torch.empty_like(dout), torch.empty(q.shape[:2], device=DEV)
+    with monkeypatch.context() as m:
+        m.setattr(pa, "_current_device", lambda: 1)   # (as if another GPU were current)
+        with pytest.raises(ValueError, match="device"):
+            plan.run(q, k, v, 0.1, out, lse)
+        with pytest.raises(ValueError, match="device"):
+            plan.run_bwd(q, k, v, out, dout, lse, 0.1, out.clone(), k.clone(), v.clone())
 
 
 def test_python_refusals():
