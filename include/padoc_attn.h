@@ -966,9 +966,12 @@ typedef struct {
     int32_t num_subs;        /* blocks of 64 packed rows whose statistics the backward keeps, for each KV head */
     int32_t num_key_tiles;   /* backward: key tiles of at most 128 rows */
     int32_t num_covers;      /* (key tile, segment that sees some of it) pairs */
-    int32_t cluster;         /* CTAs of a cluster that share a key tile in the backward */
-    int32_t parts;           /* or CTAs that share it and leave partial sums (1: none do) */
-    int32_t reserved;
+    int32_t num_gap_tiles;   /* ... the last of them: tiles that no row sees */
+    int32_t cluster;         /* f32: CTAs of a cluster that share a key tile */
+    int32_t num_dkv_units;   /* bf16: key tiles, or parts of the rows that see one, for each KV head */
+    int32_t num_dkv_ctas;    /* CTAs that have a list of them each */
+    int32_t num_dkv_sums;    /* key tiles in parts */
+    int32_t num_dkv_slots;   /* the parts */
     int64_t pairs;           /* visible (query row, key row) pairs */
     int64_t plan_ints;       /* int32 words in the plan blob */
     int64_t off_units;       /* offsets (int32 words) of the blob's arrays */
@@ -979,6 +982,9 @@ typedef struct {
     int64_t off_dq_merges;
     int64_t off_key_tiles;
     int64_t off_covers;
+    int64_t off_dkv;
+    int64_t off_dkv_ctas;
+    int64_t off_dkv_sums;
 } padoc_cross_plan;
 
 /* Size in int32 words of the plan blob. Errors as padoc_build_cross_plan. */

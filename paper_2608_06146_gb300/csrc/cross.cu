@@ -720,9 +720,7 @@ extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const
     // the key tiles reach to the last key that a row sees; behind it the gradients are zero
     a.tail_begin = info->key_rows;
     a.tail_tiles = (int32_t)((rows->key_rows - info->key_rows + PADOC_CROSS_KEY_TILE - 1) / PADOC_CROSS_KEY_TILE);
-    if (info->parts < 1 || info->cluster < 1 ||
-        (int64_t)(a.num_tiles + (int64_t)a.tail_tiles) * a.hkv * (info->parts > 8 ? info->parts : 8) > INT32_MAX)
-        return PADOC_ERR_UNSUPPORTED;
+    if ((int64_t)(a.num_tiles + (int64_t)a.tail_tiles) * a.hkv * 16 > INT32_MAX) return PADOC_ERR_UNSUPPORTED;
     if (a.num_units + a.num_merges + a.num_tiles + a.tail_tiles == 0) return PADOC_OK;
     a.out = out;
     a.dout = dout;
@@ -737,11 +735,17 @@ extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const
     a.neg_lse2 = (float *)workspace;
     a.dsum = a.neg_lse2 + stats;
     a.part = a.dsum + stats;
-    a.parts = info->parts;
+    a.dkv = (const padoc_cross_dkv *)(plan_dev + info->off_dkv);
+    a.dkv_ctas = plan_dev + info->off_dkv_ctas;
+    a.dkv_sums = (const padoc_cross_dkv_sum *)(plan_dev + info->off_dkv_sums);
+    a.num_dkv_ctas = info->num_dkv_ctas;
+    a.num_dkv_sums = info->num_dkv_sums;
+    a.num_dkv_slots = info->num_dkv_slots;
+    a.gap_tile = info->num_key_tiles - info->num_gap_tiles;
     a.part_dkv = a.part + (size_t)info->num_dq_slots * a.unit_rows * c.head_dim;
     cudaStream_t cs = (cudaStream_t)stream;
     if (c.dtype == PADOC_DTYPE_F32) st = c.head_dim == 64 ? run_bwd_simt<64>(a, info->cluster, cs) : run_bwd_simt<128>(a, info->cluster, cs);
-    else st = padoc_cross_launch_bwd_tc(a, c.head_dim, info->cluster, cs);
+    else st = padoc_cross_launch_bwd_tc(a, c.head_dim, cs);
     if (st != PADOC_OK) return st;
     if (!a.num_merges) return PADOC_OK;
     return c.dtype == PADOC_DTYPE_F32 ? merge_rows<float, true>(a, c.head_dim, false, cs)

@@ -19,8 +19,12 @@ struct padoc_cross_args {
     void *o, *dq, *dk, *dv;
     float *lse;
     float *part, *part_lse;                    // partial results
-    float *part_dkv;                           // of key tiles: [tile][Hkv][parts][128][dV | dK]
-    int32_t parts;                             // CTAs that share a key tile and leave their sums there (1: none do)
+    float *part_dkv;                           // of key tiles: [slot][128][dV | dK]
+    const padoc_cross_dkv *dkv;                // dk/dv items (bf16), each CTA's list of them, and what joins parts
+    const int32_t *dkv_ctas;
+    const padoc_cross_dkv_sum *dkv_sums;
+    int32_t num_dkv_ctas, num_dkv_sums, num_dkv_slots;
+    int32_t gap_tile;                          // first of the tiles that no row sees (the last ones)
     float *neg_lse2, *dsum;                    // -lse * log2(e) and rowsum(dO * O): [Hkv][subs][64]
     int32_t unit_rows;                         // packed rows of a forward or dq item, and of its partial result
     int32_t num_units, num_ctas, num_merges, max_parts, num_tiles, num_subs;
@@ -44,5 +48,5 @@ __device__ __forceinline__ bool cross_row(const padoc_cross_args &a, int tok, in
 padoc_status padoc_cross_launch_tc(const padoc_cross_args &args, int head_dim, cudaStream_t stream);
 // The same for items of at most 32 rows, each by a cluster (cross_few.cu).
 padoc_status padoc_cross_launch_few(const padoc_cross_args &args, int head_dim, int cluster, cudaStream_t stream);
-// The backward's passes on the tensor cores (cross_bwd_tc.cu); cluster: CTAs that share a dK/dV unit.
-padoc_status padoc_cross_launch_bwd_tc(const padoc_cross_args &args, int head_dim, int cluster, cudaStream_t stream);
+// The backward's passes on the tensor cores (cross_bwd_tc.cu).
+padoc_status padoc_cross_launch_bwd_tc(const padoc_cross_args &args, int head_dim, cudaStream_t stream);

@@ -7,11 +7,11 @@
 //   them (parts are joined by a later kernel). It walks 64-key steps: S = Q K^T (Q in tensor memory), dP = dO V^T (dO in
 //   shared memory), dS as bf16 over S, dQ += dS K. It also writes -lse2 and D of its rows for the other pass. A
 //   running CTA takes over units not yet launched (cluster launch control).
-// dK/dV pass: a unit is a tile of at most 128 keys and a KV head, run by a cluster of 1 to 8
-//   CTAs that share out its steps and add their fp32 sums through distributed shared memory, in rank order (or by more
-//   CTAs whose sums a later kernel adds). A step is a
-//   block of 64 packed rows: S^T = K Q^T, dP^T = V dO^T (V in tensor memory), P^T and dS^T as bf16 over S^T, dV += P^T dO,
-//   dK += dS^T Q. Query heads of the group and the segments that share keys are thus summed in a fixed order.
+// dK/dV pass: a unit is a tile of at most 128 keys and a KV head, or a part of the rows that see it (whose sums a later
+//   kernel adds in order). Each CTA has a list of units of about equal time. A step is a block of 64 packed rows:
+//   S^T = K Q^T, dP^T = V dO^T, P^T and dS^T as bf16 over S^T, dV += P^T dO, dK += dS^T Q. Query heads of the group and the
+//   segments that share keys are thus summed in a fixed order. The next unit's K, V and first rows come while this one's
+//   steps run, its first scores while this one's sums are written.
 //
 // Masks are needed at ends only: where a segment's keys (dQ) or rows (dK/dV) end inside a step, the weights past the end
 // become 0 and the operand rows there zeros, because what lies behind may be anything; and keys of a tile that the
@@ -93,10 +93,13 @@ struct HalfRow {
 // ================================================================================================
 namespace dkv {
 constexpr int kKT = PADOC_CROSS_KEY_TILE;   // 128 keys: the M of every MMA
-constexpr int kMaxStages = 10;
-// With 64 dims two groups of eight softmax warps take the steps in turn (9 pages of 16 heads 110 -> 98 us): one group's
-// work on a step lasts longer than its 16 MMAs. With 128 dims, 24 MMAs, one group with all registers is faster (937 us
-// against 983 for 32768 rows over 8 x 2560 states).
+constexpr int kMaxStages = 8;
+constexpr int kKPanel = kKT * 128;           // [128 rows][64 bf16]
+constexpr int kQPanel = kBlk * 128;          // [64 rows][64 bf16]
+constexpr int kAuxBytes = 2 * kBlk * 4;      // -lse2[64], D[64]
+// With 64 dims two groups of eight softmax warps take the steps in turn: one group's work on a step lasts longer than its
+// 16 MMAs (98 us against 110 for 9 pages of 16 heads). With 128 dims, 24 MMAs, one group with all registers is faster
+// (937 us against 983 for 32768 rows over 8 x 2560 states).
 // Tensor memory: S buffers, dP buffers, V as an A operand (128 dims; with 64 it is read from shared memory), dV and dK.
 template <int D>
 struct Cols {
@@ -105,27 +108,42 @@ struct Cols {
     static constexpr uint32_t kDP = 64 * kBuffers, kV = 192, kAcc = D == 64 ? 384 : 256;
     static_assert(kAcc + 2 * D <= 512 && kDP + 64 * kDPs <= (D == 64 ? kAcc : kV), "");
     // Steps on their way: a step of 64 dims copies 16 KB in the time of 16 MMAs, and with four stages it waited for them
-    // (128 -> 98 us).
-    static constexpr int kStages = D == 64 ? 10 : 4;
+    // (128 us against 98 with ten, before units came in lists).
+    static constexpr int kStages = D == 64 ? 8 : 4, kKBufs = D == 64 ? 2 : 1;   // K and V of the unit, and of the next
     static_assert(kStages <= kMaxStages && kStages % kGroups == 0, "a stage belongs to one group");
+    static constexpr int kShare = 2 * D / (kSoft / 4);                          // columns of dV | dK a softmax thread writes
 };
-constexpr int kKPanel = kKT * 128;           // [128 rows][64 bf16]
-constexpr int kQPanel = kBlk * 128;          // [64 rows][64 bf16]
-constexpr int kAuxBytes = 2 * kBlk * 4;      // -lse2[64], D[64]
+struct Unit {   // steps < 0: no more units
+    int32_t k0, nk, cover, g;
+    int32_t first, steps, slot, pad;
+};
 enum {
-    B_KV = 0,
-    B_QFULL = 1,                  // [stage]
-    B_QEMPTY = 1 + kMaxStages,       // [stage]
-    B_SFULL = 1 + 2 * kMaxStages,    // [S buffer]
-    B_PFULL = 5 + 2 * kMaxStages,    // [S buffer], an arrival per softmax warp of a group
-    B_ACC = 9 + 2 * kMaxStages,      // [S buffer]: the step's accumulating MMAs are done
-    B_DPFREE = 13 + 2 * kMaxStages,  // [dP buffer]: dP is read (an arrival per softmax warp of a group)
-    B_VT = 15 + 2 * kMaxStages,      // V is in tensor memory (an arrival per softmax warp of the first group)
-    B_FINAL = 16 + 2 * kMaxStages,   // [issuing warp]
-    B_COUNT = 19 + 2 * kMaxStages
+    B_UFULL = 0,                      // [unit parity]
+    B_UEMPTY = 2,                     // [unit parity], an arrival per reading warp
+    B_KFULL = 4,                      // [K buffer]
+    B_KFREE = 6,                      // [K buffer]: the unit's last S is done
+    B_VFULL = 8,                      // [V buffer]
+    B_VFREE = 10,                     // [V buffer]: V is in tensor memory (an arrival per softmax warp) or its last dP is done
+    B_VT = 12,                        // V is in tensor memory (an arrival per softmax warp)
+    B_DPLAST = 13,                    // the unit's last dP is done
+    B_ACCFULL = 14,                   // the unit's dV and dK are complete
+    B_ACCFREE = 15,                   // ... and read (an arrival per softmax warp)
+    B_FINAL = 16,                     // [issuing warp]
+    B_SFULL = 19,                     // [S buffer]
+    B_PFULL = 23,                     // [S buffer], an arrival per softmax warp of a group
+    B_ACC = 27,                       // [S buffer]: the step's accumulating MMAs are done
+    B_DPFREE = 31,                    // [dP buffer]: dP is read (an arrival per softmax warp of a group)
+    B_QFULL = 33,                     // [stage]
+    B_QEMPTY = 33 + kMaxStages,       // [stage]
+    B_COUNT = 33 + 2 * kMaxStages
 };
 template <int D>
-constexpr size_t smem_bytes() { return 1024 + 2 * (size_t)(D / 64) * kKPanel + 2 * (size_t)Cols<D>::kStages * (D / 64) * kQPanel + (size_t)Cols<D>::kStages * kAuxBytes + B_COUNT * 8 + 64; }
+constexpr size_t smem_bytes()
+{
+    return 1024 + 2 * (size_t)Cols<D>::kKBufs * (D / 64) * kKPanel + 2 * (size_t)Cols<D>::kStages * (D / 64) * kQPanel +
+           (size_t)Cols<D>::kStages * kAuxBytes + 2 * sizeof(Unit) + B_COUNT * 8 + 16;
+}
+static_assert(smem_bytes<64>() <= 232448 && smem_bytes<128>() <= 232448, "shared memory per CTA");
 }  // namespace dkv
 
 // The blocks of rows that a key tile's steps are, one after the other.
@@ -133,7 +151,7 @@ struct Steps {
     const padoc_cross_cover *covers;
     padoc_cross_cover c;
     int i, b;
-    __device__ __forceinline__ Steps(const padoc_cross_args &a, const padoc_cross_key_tile &t, int first) : covers(a.covers + t.cover), i(0), b(first)
+    __device__ __forceinline__ Steps(const padoc_cross_args &a, int cover, int first) : covers(a.covers + cover), i(0), b(first)
     {
         c = covers[0];
         while (b >= c.nsub) {
@@ -151,66 +169,68 @@ struct Steps {
     __device__ __forceinline__ int tokens(const padoc_cross_args &a) const { return min(a.block_tokens, c.ntok - b * a.block_tokens); }
 };
 
-// NC: the CTAs of a unit's cluster. kParts: the steps are shared out over a.parts CTAs that know nothing of one another;
-// their fp32 sums go to the workspace, where cross_dkv_sum_kernel adds them in order (few tiles that many rows see).
-template <int D, int NC, bool kParts>
+// Key rows that no row sees: gap tiles of the plan, then those it does not reach.
+template <int D>
+__device__ __forceinline__ void zero_gaps(const padoc_cross_args &a, int first, int stride, int thread, int threads)
+{
+    const int gaps = a.num_tiles - a.gap_tile;
+    for (int n = first; n < (gaps + a.tail_tiles) * a.hkv; n += stride) {
+        const int i = n / a.hkv, g = n % a.hkv;
+        int k0 = a.tail_begin + (i - gaps) * PADOC_CROSS_KEY_TILE, nk = (int)min((int64_t)PADOC_CROSS_KEY_TILE, a.key_rows - k0);
+        if (i < gaps) {
+            k0 = a.tiles[a.gap_tile + i].k0;
+            nk = a.tiles[a.gap_tile + i].nk;
+        }
+        for (int t = thread; t < nk * (D / 8); t += threads) {
+            const size_t r = (size_t)(k0 + t / (D / 8));
+            const int c = g * D + t % (D / 8) * 8;
+            *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.dk + r * a.dk_stride + c) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.dv + r * a.dv_stride + c) = make_uint4(0, 0, 0, 0);
+        }
+    }
+}
+template <int D>
+__global__ void __launch_bounds__(256) cross_zero_kernel(const padoc_cross_args a)
+{
+    zero_gaps<D>(a, blockIdx.x, gridDim.x, threadIdx.x, 256);
+}
+
+template <int D>
 __global__ void __launch_bounds__(dkv::Cols<D>::kThreads, 1)
 cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap gmap,
                  const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const padoc_cross_args a)
 {
     using namespace dkv;
     using T = Cols<D>;
-    constexpr int kPanels = D / 64, kKTile = kPanels * kKPanel, kQTile = kPanels * kQPanel, kBuf = T::kBuffers, kDPs = T::kDPs, kStages = T::kStages,
-                  kGroups = T::kGroups, kSoft = T::kSoft;
+    constexpr int kPanels = D / 64, kKTile = kPanels * kKPanel, kQTile = kPanels * kQPanel, kBuf = T::kBuffers, kDPs = T::kDPs,
+                  kStages = T::kStages, kKBufs = T::kKBufs, kGroups = T::kGroups, kSoft = T::kSoft;
     constexpr uint32_t kColS = 0, kColDP = T::kDP, kColV = T::kV, kColAcc = T::kAcc;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *sk = smem;
-    uint8_t *sv = sk + kKTile;
-    uint8_t *sq = sv + kKTile;                 // [stage] Q step tiles
+    uint8_t *sk = smem;                        // [buffer]
+    uint8_t *sv = sk + kKBufs * kKTile;        // [buffer]
+    uint8_t *sq = sv + kKBufs * kKTile;        // [stage] Q step tiles
     uint8_t *sg = sq + kStages * kQTile;       // [stage] dO step tiles
     uint8_t *aux = sg + kStages * kQTile;      // [stage] -lse2, D
-    uint64_t *bars = (uint64_t *)(aux + kStages * kAuxBytes);
+    Unit *units = (Unit *)(aux + kStages * kAuxBytes);   // [2]
+    uint64_t *bars = (uint64_t *)(units + 2);
     uint32_t *tmem_slot = (uint32_t *)(bars + B_COUNT);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (a value the compiler knows to be warp-uniform)
-    // the cluster's unit, and this CTA's steps of it: ub .. ub + nu - 1
-    static_assert(!kParts || NC == 1, "");
-    const int share = kParts ? a.parts : NC;
-    const int unit = (int)blockIdx.x / share, rank = (int)blockIdx.x % share, g = unit % a.hkv, ti = unit / a.hkv;
-    padoc_cross_key_tile t;
-    if (ti < a.num_tiles) {
-        t = a.tiles[ti];
-    } else {   // key rows that the plan does not reach
-        t.k0 = a.tail_begin + (ti - a.num_tiles) * kKT;
-        t.nk = (int)min((int64_t)kKT, a.key_rows - t.k0);
-        t.cover = t.ncover = t.steps = 0;
-    }
-    if (t.steps == 0) {   // keys that no row sees
-        if (rank == 0)
-            for (int i = tid; i < t.nk * (D / 8); i += T::kThreads) {
-                const size_t r = (size_t)(t.k0 + i / (D / 8));
-                const int c = g * D + i % (D / 8) * 8;
-                *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.dk + r * a.dk_stride + c) = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.dv + r * a.dv_stride + c) = make_uint4(0, 0, 0, 0);
-            }
-        pdl_wait_prerequisite();
-        return;
-    }
-    const int k0 = __shfl_sync(0xffffffffu, t.k0, 0), steps = __shfl_sync(0xffffffffu, t.steps, 0);
-    const int ub = (int)((int64_t)steps * rank / share), nu = (int)((int64_t)steps * (rank + 1) / share) - ub;
-    if (kParts && nu == 0) {   // (not read either)
-        pdl_wait_prerequisite();
-        return;
-    }
     const int used = a.block_tokens * a.group;   // rows of a block that its copies write
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
 
     if (tid < B_COUNT) {
         const int i = tid;
-        mbar_init(bar(i), (i >= B_PFULL && i < B_ACC) || (i >= B_DPFREE && i <= B_VT) ? 8 : i >= B_SFULL && i < B_PFULL ? 2 : 1);
+        int n = 1;
+        if (i == B_UEMPTY || i == B_UEMPTY + 1) n = kSoft + 3;
+        if (i == B_VFREE || i == B_VFREE + 1) n = D == 128 ? 8 : 1;
+        if (i == B_VT || (i >= B_PFULL && i < B_ACC) || i == B_DPFREE || i == B_DPFREE + 1) n = 8;
+        if (i == B_ACCFREE) n = kSoft;
+        if (i >= B_SFULL && i < B_PFULL) n = 2;
+        mbar_init(bar(i), n);
         if (i == 0) *abort_flag = 0;
         fence_barrier_init();
     }
@@ -229,76 +249,120 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-    const int lq = warp & 3, ch = warp >> 2 & 1, grp = warp >> 3;   // softmax warps: TMEM lane quarter, column half, group
-    const uint32_t lanes = (uint32_t)(lq * 32) << 16;
-    bool sums = false;                                // softmax warps: this CTA's dV and dK are complete
+    auto wait_w = [&](int b, uint32_t parity, int site) {
+        return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
+    };
+    // the n-th unit, as every lane of a reading warp sees it
+    auto read_unit = [&](int n, Unit &u, int site) {
+        if (!wait_w(B_UFULL + (n & 1), (n >> 1) & 1, site)) return false;
+        const Unit v = units[n & 1];
+        u.k0 = __shfl_sync(0xffffffffu, v.k0, 0);
+        u.nk = __shfl_sync(0xffffffffu, v.nk, 0);
+        u.cover = __shfl_sync(0xffffffffu, v.cover, 0);
+        u.g = __shfl_sync(0xffffffffu, v.g, 0);
+        u.first = __shfl_sync(0xffffffffu, v.first, 0);
+        u.steps = __shfl_sync(0xffffffffu, v.steps, 0);
+        u.slot = __shfl_sync(0xffffffffu, v.slot, 0);
+        __syncwarp();   // (every lane's read has returned before the slot may be written again)
+        mbar_arrive_warp(bar(B_UEMPTY + (n & 1)));
+        return true;
+    };
 
     if (warp == kSoft) {
         // ---------------------------------------------------------------- TMA producer
-        if (lane == 0 && nu == 0) pdl_wait_prerequisite();
-        if (lane == 0 && nu > 0) {
+        if (lane == 0) {
             tma_prefetch_desc(&qmap);
             tma_prefetch_desc(&gmap);
             tma_prefetch_desc(&kmap);
             tma_prefetch_desc(&vmap);
+            auto wait = [&](int b, uint32_t parity, int site) {
+                return wait_or_abort(bar(b), parity, a.err, site, abort_flag);
+            };
             pdl_wait_prerequisite();   // -lse2 and D are the dQ pass's
-            mbar_arrive_expect_tx(bar(B_KV), 2 * kKTile);
-#pragma unroll
-            for (int p = 0; p < kPanels; ++p) {
-                tma_load_2d(smem_u32(sk) + p * kKPanel, &kmap, g * D + 64 * p, k0, bar(B_KV));
-                tma_load_2d(smem_u32(sv) + p * kKPanel, &vmap, g * D + 64 * p, k0, bar(B_KV));
-            }
-            int issued = 0;
-            Steps st(a, t, ub);
-            for (int u = 0; u < nu; ++u) {
-                const int s = u % kStages;
-                if (u >= kStages && !wait_or_abort(bar(B_QEMPTY + s), (u / kStages - 1) & 1, a.err, 150, abort_flag)) break;
-                const int tok = st.c.tok + st.b * a.block_tokens;
-                const size_t at = ((size_t)g * a.num_subs + st.c.sub + st.b) * kBlk;
-                const uint32_t fb = bar(B_QFULL + s);
-                const uint32_t qb = smem_u32(sq + s * kQTile), gb = smem_u32(sg + s * kQTile);
-                const uint32_t ab = smem_u32(aux + s * kAuxBytes);
-                mbar_arrive_expect_tx(fb, 2 * kPanels * used * 128 + kAuxBytes);
-#pragma unroll
-                for (int p = 0; p < kPanels; ++p) {
-                    tma_load_3d(qb + p * kQPanel, &qmap, 64 * p, g * a.group, tok, fb);
-                    tma_load_3d(gb + p * kQPanel, &gmap, 64 * p, g * a.group, tok, fb);
+            int x = a.dkv_ctas[blockIdx.x];
+            const int xe = a.dkv_ctas[blockIdx.x + 1];
+            int issued = 0, nk = 0;    // steps, K and V tiles issued so far
+            bool ok = true;
+            for (int n = 0; ok; ++n, ++x) {
+                if (n >= 2 && !(ok = wait(B_UEMPTY + (n & 1), ((n >> 1) - 1) & 1, 149))) break;
+                Unit un = {0, 0, 0, 0, 0, -1, 0, 0};
+                if (x < xe) {
+                    const padoc_cross_dkv w = a.dkv[x];
+                    un = {w.k0, w.nk, w.cover, w.g, w.first, w.steps, w.slot, 0};
                 }
-                bulk_load(ab, a.neg_lse2 + at, kBlk * 4, fb);
-                bulk_load(ab + kBlk * 4, a.dsum + at, kBlk * 4, fb);
-                issued = u + 1;
-                st.next(issued < nu);
+                units[n & 1] = un;
+                mbar_arrive(bar(B_UFULL + (n & 1)));
+                if (un.steps < 0) break;
+                Steps st(a, un.cover, un.first);
+                for (int j = 0; j < un.steps; ++j) {
+                    const int s = issued % kStages;
+                    if (issued >= kStages && !(ok = wait(B_QEMPTY + s, (issued / kStages - 1) & 1, 150))) break;
+                    const int tok = st.c.tok + st.b * a.block_tokens;
+                    const size_t at = ((size_t)un.g * a.num_subs + st.c.sub + st.b) * kBlk;
+                    const uint32_t fb = bar(B_QFULL + s);
+                    const uint32_t qb = smem_u32(sq + s * kQTile), gb = smem_u32(sg + s * kQTile);
+                    const uint32_t ab = smem_u32(aux + s * kAuxBytes);
+                    mbar_arrive_expect_tx(fb, 2 * kPanels * used * 128 + kAuxBytes);
+#pragma unroll
+                    for (int p = 0; p < kPanels; ++p) {
+                        tma_load_3d(qb + p * kQPanel, &qmap, 64 * p, un.g * a.group, tok, fb);
+                        tma_load_3d(gb + p * kQPanel, &gmap, 64 * p, un.g * a.group, tok, fb);
+                    }
+                    bulk_load(ab, a.neg_lse2 + at, kBlk * 4, fb);
+                    bulk_load(ab + kBlk * 4, a.dsum + at, kBlk * 4, fb);
+                    ++issued;
+                    st.next(j + 1 < un.steps);
+                    if (j == 0) {   // (K's and V's places may be free later than the first step's)
+                        const int kb = n % kKBufs;
+                        if (n >= kKBufs && !(ok = wait(B_KFREE + kb, (n / kKBufs - 1) & 1, 147) && wait(B_VFREE + kb, (n / kKBufs - 1) & 1, 148)))
+                            break;
+                        mbar_arrive_expect_tx(bar(B_KFULL + kb), kKTile);
+                        mbar_arrive_expect_tx(bar(B_VFULL + kb), kKTile);
+#pragma unroll
+                        for (int p = 0; p < kPanels; ++p) {
+                            tma_load_2d(smem_u32(sk + kb * kKTile) + p * kKPanel, &kmap, un.g * D + 64 * p, un.k0, bar(B_KFULL + kb));
+                            tma_load_2d(smem_u32(sv + kb * kKTile) + p * kKPanel, &vmap, un.g * D + 64 * p, un.k0, bar(B_VFULL + kb));
+                        }
+                        ++nk;
+                    }
+                }
             }
             // copies still in flight must land before the CTA's shared memory is released
-            mbar_wait_bounded(bar(B_KV), 0, a.err, 151);
-            for (int u = (issued > kStages ? issued - kStages : 0); u < issued; ++u)
+            for (int i = max(nk - kKBufs, 0); i < nk; ++i) {
+                mbar_wait_bounded(bar(B_KFULL + i % kKBufs), (i / kKBufs) & 1, a.err, 151);
+                mbar_wait_bounded(bar(B_VFULL + i % kKBufs), (i / kKBufs) & 1, a.err, 151);
+            }
+            for (int u = max(issued - kStages, 0); u < issued; ++u)
                 mbar_wait_bounded(bar(B_QFULL + u % kStages), (u / kStages) & 1, a.err, 152);
         }
     } else if (warp > kSoft) {
         // ---------------------------------------------------------------- MMA issuers (whole warps)
-        if (nu > 0) {
-            auto wait_w = [&](int b, uint32_t parity, int site) {
-                return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
-            };
-            constexpr uint32_t idS = umma_idesc_bf16(128, kBlk, false), idAcc = umma_idesc_bf16(128, D, true);
+        // the first S, the third dP, the second the accumulating MMAs; u counts the steps of all units
+        constexpr uint32_t idS = umma_idesc_bf16(128, kBlk, false), idAcc = umma_idesc_bf16(128, D, true);
+        int u = 0;
+        bool ok = true;
+        Unit un;
+        for (int n = 0; ok && (ok = read_unit(n, un, 159)) && un.steps >= 0; ++n) {
+            const int kb = n % kKBufs;
+            const uint32_t kph = n / kKBufs & 1;
             if (warp == kSoft + 1) {
-                const uint64_t dK = umma_desc_sw128(smem_u32(sk), 16, 1024);
-                bool ok = wait_w(B_KV, 0, 160);
-                for (int u = 0; ok && u < nu; ++u) {
-                    const int s = u % kStages;
-                    const uint32_t b = (uint32_t)(u % kBuf) * 64;
-                    ok = wait_w(B_QFULL + s, (u / kStages) & 1, 161) && (u < kBuf || wait_w(B_ACC + u % kBuf, (u / kBuf - 1) & 1, 163));
+                const uint64_t dK = umma_desc_sw128(smem_u32(sk + kb * kKTile), 16, 1024);
+                ok = wait_w(B_KFULL + kb, kph, 160);
+                for (int j = 0; ok && j < un.steps; ++j, ++u) {
+                    const int s = u % kStages, b = u % kBuf;
+                    ok = wait_w(B_QFULL + s, (u / kStages) & 1, 161) && (u < kBuf || wait_w(B_ACC + b, (u / kBuf - 1) & 1, 163));
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t dq = umma_desc_sw128(smem_u32(sq + s * kQTile), 16, 1024);
-                    if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kKPanel, kQPanel>(tmem + kColS + b, dK, dq, idS);
-                    else umma_bf16_ss_k64_warp(tmem + kColS + b, dK, dq, idS);
-                    umma_commit_warp(bar(B_SFULL + u % kBuf));
+                    if constexpr (D == 128) umma_bf16_ss_k128_warp<1, kKPanel, kQPanel>(tmem + kColS + 64 * b, dK, dq, idS);
+                    else umma_bf16_ss_k64_warp(tmem + kColS + 64 * b, dK, dq, idS);
+                    umma_commit_warp(bar(B_SFULL + b));
                 }
+                umma_commit_warp(bar(B_KFREE + kb));
             } else if (warp == kSoft + 3) {
-                const uint64_t dV = umma_desc_sw128(smem_u32(sv), 16, 1024);   // (64 dims)
-                bool ok = D == 64 ? wait_w(B_KV, 0, 166) : wait_w(B_VT, 0, 166);
-                for (int u = 0; ok && u < nu; ++u) {
+                const uint64_t dV = umma_desc_sw128(smem_u32(sv + kb * kKTile), 16, 1024);
+                ok = D == 64 ? wait_w(B_VFULL + kb, kph, 166) : wait_w(B_VT, n & 1, 166);
+                for (int j = 0; ok && j < un.steps; ++j, ++u) {
                     const int s = u % kStages;
                     ok = wait_w(B_QFULL + s, (u / kStages) & 1, 167) && (u < kDPs || wait_w(B_DPFREE + u % kDPs, (u / kDPs - 1) & 1, 165));
                     if (!ok) break;
@@ -308,209 +372,172 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     else umma_bf16_ss_k64_warp(tmem + kColDP + 64 * (u % kDPs), dV, dg, idS);
                     umma_commit_warp(bar(B_SFULL + u % kBuf));
                 }
+                if (D == 64) umma_commit_warp(bar(B_VFREE + kb));
+                else umma_commit_warp(bar(B_DPLAST));
             } else {
-                bool ok = true;
-                for (int u = 0; ok && u < nu; ++u) {
-                    const int s = u % kStages;
-                    const uint32_t b = (uint32_t)(u % kBuf) * 64;
-                    if (!(ok = wait_w(B_PFULL + u % kBuf, (u / kBuf) & 1, 162))) break;
+                for (int j = 0; ok && j < un.steps; ++j, ++u) {
+                    const int s = u % kStages, b = u % kBuf;
+                    // (the sums of the unit before are read before this one's first products overwrite them)
+                    ok = wait_w(B_PFULL + b, (u / kBuf) & 1, 162) && (j > 0 || n == 0 || wait_w(B_ACCFREE, (n - 1) & 1, 158));
+                    if (!ok) break;
                     tc_fence_after();
                     // the step's Q and dO as MN-major B operands (N = head dim, K = the 64 rows)
                     const uint64_t gmn = umma_desc_sw128(smem_u32(sg + s * kQTile), kQPanel, 1024);
                     const uint64_t qmn = umma_desc_sw128(smem_u32(sq + s * kQTile), kQPanel, 1024);
-                    umma_bf16_ts_k64_mn_warp<1, slice_col(1), slice_col(2), slice_col(3)>(tmem + kColAcc, tmem + kColS + b, gmn, idAcc, u > 0);
-                    umma_bf16_ts_k64_mn_warp<1, slice_col(1), slice_col(2), slice_col(3)>(tmem + kColAcc + D, tmem + kColS + b + 16, qmn, idAcc, u > 0);
-                    umma_commit_warp(bar(B_ACC + u % kBuf));
+                    umma_bf16_ts_k64_mn_warp<1, slice_col(1), slice_col(2), slice_col(3)>(tmem + kColAcc, tmem + kColS + 64 * b, gmn, idAcc, j > 0);
+                    umma_bf16_ts_k64_mn_warp<1, slice_col(1), slice_col(2), slice_col(3)>(tmem + kColAcc + D, tmem + kColS + 64 * b + 16, qmn, idAcc, j > 0);
+                    umma_commit_warp(bar(B_ACC + b));
                     umma_commit_warp(bar(B_QEMPTY + s));
                 }
+                umma_commit_warp(bar(B_ACCFULL));
             }
-            // every MMA issued above must complete before tensor memory is read or released
-            umma_commit_warp(bar(B_FINAL + warp - kSoft - 1));
-            mbar_wait_bounded(bar(B_FINAL + warp - kSoft - 1), 0, a.err, 164);
         }
+        // every MMA issued above must complete before tensor memory is released
+        umma_commit_warp(bar(B_FINAL + warp - kSoft - 1));
+        mbar_wait_bounded(bar(B_FINAL + warp - kSoft - 1), 0, a.err, 164);
     } else {
         // ---------------------------------------------------------------- softmax + epilogue
-        const float c = a.scale_log2;
-        auto wait_all = [&](int b, uint32_t parity, int site) {
-            return mbar_wait_warp(bar(b), parity, a.err, site, abort_flag);
-        };
+        const int lq = warp & 3, ch = warp >> 2 & 1, grp = warp >> 3;   // TMEM lane quarter, column half, group
+        const int row = lq * 32 + lane;
+        const uint32_t lanes = (uint32_t)(lq * 32) << 16;
+        const uint64_t c2 = f2_pack(a.scale_log2, a.scale_log2);
+        zero_gaps<D>(a, blockIdx.x, gridDim.x, tid, 32 * kSoft);   // (while the first unit is on its way)
+        int u0 = 0;             // steps of the units before
+        Unit un, last = {};
         bool ok = true;
-        if (D == 128 && grp == 0 && nu > 0 && (ok = wait_all(B_KV, 0, 173))) {   // V's rows into tensor memory, half of the dims a thread
-            HalfRow<D>::to_tmem(tmem + lanes + kColV, sv, ch, lq * 32 + lane, kKPanel);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            mbar_arrive_warp(bar(B_VT));
-        }
-        Steps st(a, t, grp < nu ? ub + grp : 0);
-        for (int u = grp; ok && u < nu; u += kGroups) {
-            const int s = u % kStages;
-            const uint32_t b = (uint32_t)(u % kBuf) * 64 + 32 * ch;
-            const int rows = __shfl_sync(0xffffffffu, st.tokens(a), 0) * a.group;
-            const bool partial = rows < used;
-            // keys of the tile that the segment does not see
-            const int key = k0 + lq * 32 + lane;
-            const bool blind = key < st.c.k0 || key >= st.c.k0 + st.c.nk;
-            if (!wait_all(B_QFULL + s, (u / kStages) & 1, 171) || !wait_all(B_SFULL + u % kBuf, (u / kBuf) & 1, 170)) {
-                ok = false;
-                break;
+        for (int n = 0; ok && (ok = read_unit(n, un, 157)); ++n) {
+            if (D == 128 && un.steps >= 0) {   // V's rows into tensor memory, half of the dims a thread
+                if (!(ok = wait_w(B_VFULL, n & 1, 173) && (n == 0 || wait_w(B_DPLAST, (n - 1) & 1, 174)))) break;
+                tc_fence_after();
+                HalfRow<D>::to_tmem(tmem + lanes + kColV, sv, ch, row, kKPanel);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_warp(bar(B_VT));
+                mbar_arrive_warp(bar(B_VFREE));
             }
-            tc_fence_after();
-            for (int i = 1; i <= kGroups; ++i) st.next(u + i < nu);
-            uint32_t vis = 0xffffffffu;
-            if (partial) {
-                // the block's rows past the segment's, which the products below sum over: zeros (S and dP, which
-                // have read them, are done)
-                vis = interval_bits(0, rows, 32 * ch);
-                for (int i = tid & 255; i < (kBlk - rows) * 8 * kPanels; i += 256) {
-                    const int r = rows + i / 8 % (kBlk - rows), p = i / 8 / (kBlk - rows), o = p * kQPanel + r * 128 + i % 8 * 16;
-                    *reinterpret_cast<uint4 *>(sq + s * kQTile + o) = make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4 *>(sg + s * kQTile + o) = make_uint4(0, 0, 0, 0);
-                }
-                fence_proxy_async_smem();
-            }
-            const float4 *la = reinterpret_cast<const float4 *>(aux + s * kAuxBytes) + 8 * ch;
-            const float4 *da = reinterpret_cast<const float4 *>(aux + s * kAuxBytes + kBlk * 4) + 8 * ch;
-            const uint64_t c2 = f2_pack(c, c);
-            const bool any_blind = __any_sync(0xffffffffu, blind);
-            constexpr int kCols = kGroups == 2 ? 16 : 32;   // row columns at a time (96 registers a thread with two groups)
-            uint32_t pk[16], dk[16];
+            // The unit before's sums, kShare columns of dV | dK a thread: dV, and dK times scale, or both in fp32 as parts.
+            if (n > 0) {
+                if (!(ok = wait_w(B_ACCFULL, (n - 1) & 1, 172))) break;
+                tc_fence_after();
+                const int c0 = T::kShare * (warp >> 2);
+#pragma unroll 1
+                for (int c = 0; c < T::kShare; c += 16) {
+                    uint32_t o[16];
+                    tmem_ld16(tmem + lanes + kColAcc + c0 + c, o);
+                    tmem_ld_wait();
+                    if (c + 16 == T::kShare) {
+                        tc_fence_before();
+                        __syncwarp();
+                        mbar_arrive_warp(bar(B_ACCFREE));
+                    }
+                    float x[16];
 #pragma unroll
-            for (int h = 0; h < 32; h += kCols) {
-                uint32_t sr[kCols], dr[kCols];
-                tmem_ld_cols(tmem + lanes + kColS + b + h, sr);
-                tmem_ld_cols(tmem + lanes + kColDP + 64 * (u % kDPs) + 32 * ch + h, dr);
-                tmem_ld_wait();
-                if (h + kCols == 32) {
-                    tc_fence_before();
-                    __syncwarp();
-                    mbar_arrive_warp(bar(B_DPFREE + u % kDPs));
-                }
-                // two row columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D), both rounded to the
-                // MMAs' operand type (half a step, 2^-9 of a value on average)
-                auto column_pairs = [&](auto masked) {
-#pragma unroll
-                    for (int i4 = 0; i4 < kCols / 4; ++i4) {
-                        const float4 l4 = la[h / 4 + i4], d4 = da[h / 4 + i4];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const int i = 4 * i4 + 2 * j;
-                            float x0, x1;
-                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2,
-                                             j ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y)), x0, x1);
-                            float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-                            const uint64_t e = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])),
-                                                      j ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y));
-                            float d0, d1;
-                            f2_unpack(f2_mul(f2_pack(p0, p1), e), d0, d1);
-                            if (decltype(masked)::value) {
-                                p0 = (vis >> (h + i)) & 1u ? p0 : 0.f;
-                                p1 = (vis >> (h + i + 1)) & 1u ? p1 : 0.f;
-                                d0 = (vis >> (h + i)) & 1u ? d0 : 0.f;
-                                d1 = (vis >> (h + i + 1)) & 1u ? d1 : 0.f;
-                            }
-                            pk[(h + i) >> 1] = pack_bf16x2(p0, p1);
-                            dk[(h + i) >> 1] = pack_bf16x2(d0, d1);
+                    for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(o[i]);
+                    const int col = c0 + c;
+                    if (row < last.nk) {
+                        if (last.slot >= 0) {
+                            float *dst = a.part_dkv + ((size_t)last.slot * kKT + row) * (2 * D) + col;
+                            st_global_v8(dst, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]);
+                            st_global_v8(dst + 8, x[8], x[9], x[10], x[11], x[12], x[13], x[14], x[15]);
+                        } else {
+                            const bool isk = col >= D;                       // dV first, then dK (times scale)
+                            store_row_bf16(isk ? (__nv_bfloat16 *)a.dk + (size_t)(last.k0 + row) * a.dk_stride + last.g * D + (col - D)
+                                               : (__nv_bfloat16 *)a.dv + (size_t)(last.k0 + row) * a.dv_stride + last.g * D + col,
+                                           x, isk ? a.scale : 1.f);
                         }
                     }
-                };
-                if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
-            }
-            if (any_blind) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    pk[i] = blind ? 0u : pk[i];
-                    dk[i] = blind ? 0u : dk[i];
                 }
             }
-            tmem_st16(tmem + lanes + kColS + b, pk);
-            tmem_st16(tmem + lanes + kColS + b + 16, dk);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            mbar_arrive_warp(bar(B_PFULL + u % kBuf));
-        }
-        sums = ok && (nu == 0 || wait_all(B_FINAL + 1, 0, 172));
-        tc_fence_after();
-    }
-    // Epilogue. The 2 D columns of dV | dK are split over the cluster's CTAs: each one's softmax threads
-    // (a key row and some of the columns each) send the other CTAs' parts to their shared memory, which
-    // nothing else uses any more, add what they receive to their own part in rank order and write it.
-    // Both groups' warps take part where their shares are 16 columns or more, else the first's.
-    constexpr int kPart = 2 * D / NC, kShares = kGroups == 2 && kPart >= 64 ? 4 : 2, kHalfPart = kPart / kShares;   // columns of a CTA, of a thread
-    const int cs = kShares == 4 ? 2 * grp + ch : ch;
-    sums = sums && (kShares == 4 || grp == 0);
-    static_assert(kHalfPart % 16 == 0, "");
-    auto part = [&](int p, int c, uint32_t (&o)[16]) {       // 16 of this CTA's sums of part p
-        if (nu > 0) {
-            tmem_ld16(tmem + lanes + kColAcc + kPart * p + kHalfPart * cs + c, o);
-            tmem_ld_wait();
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = 0u;
-        }
-    };
-    // the place of a thread's 16 columns from CTA `from` in the receiver's shared memory
-    auto slot = [&](int from, int to, int c) {
-        const int n = from < to ? from : from - 1;
-        return (uint32_t)(n * kPart * kKT * 4 + (kHalfPart * cs + c) * kKT * 4 + (lq * 32 + lane) * 16);
-    };
-    static_assert((NC - 1) * kPart * kKT * 4 <= 2 * kKTile + 2 * kStages * kQTile, "");
-    if (NC > 1) {
-        tc_fence_before();
-        cluster_sync();
-        if (sums) {
-            tc_fence_after();
-#pragma unroll 1
-            for (int d = 1; d < NC; ++d) {
-                const int p = (rank + d) % NC;
-                const uint32_t dst = cluster_map(smem_u32(smem), p);
-#pragma unroll 1
-                for (int c = 0; c < kHalfPart; c += 16) {
-                    uint32_t o[16];
-                    part(p, c, o);
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4)
-                        st_cluster_v4(dst + slot(rank, p, c + i), make_int4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+            if (un.steps < 0) break;
+            last = un;
+            // this group's steps
+            const int j0 = kGroups == 2 ? (u0 & 1) ^ grp : 0;
+            Steps st(a, un.cover, un.first + (j0 < un.steps ? j0 : 0));
+            for (int j = j0; ok && j < un.steps; j += kGroups) {
+                const int u = u0 + j, s = u % kStages, sb = u % kBuf;
+                const uint32_t b = (uint32_t)sb * 64 + 32 * ch;
+                const int rows = __shfl_sync(0xffffffffu, st.tokens(a), 0) * a.group;
+                const bool partial = rows < used;
+                // keys of the tile that the segment does not see
+                const int key = un.k0 + row;
+                const bool blind = key < st.c.k0 || key >= st.c.k0 + st.c.nk;
+                if (!(ok = wait_w(B_QFULL + s, (u / kStages) & 1, 171) && wait_w(B_SFULL + sb, (u / kBuf) & 1, 170))) break;
+                tc_fence_after();
+                for (int i = 1; i <= kGroups; ++i) st.next(j + i < un.steps);
+                uint32_t vis = 0xffffffffu;
+                if (partial) {
+                    // the block's rows past the segment's, which the products below sum over: zeros (S and dP, which
+                    // have read them, are done)
+                    vis = interval_bits(0, rows, 32 * ch);
+                    for (int i = tid & 255; i < (kBlk - rows) * 8 * kPanels; i += 256) {
+                        const int r = rows + i / 8 % (kBlk - rows), p = i / 8 / (kBlk - rows), o = p * kQPanel + r * 128 + i % 8 * 16;
+                        *reinterpret_cast<uint4 *>(sq + s * kQTile + o) = make_uint4(0, 0, 0, 0);
+                        *reinterpret_cast<uint4 *>(sg + s * kQTile + o) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
                 }
+                const float4 *la = reinterpret_cast<const float4 *>(aux + s * kAuxBytes) + 8 * ch;
+                const float4 *da = reinterpret_cast<const float4 *>(aux + s * kAuxBytes + kBlk * 4) + 8 * ch;
+                const bool any_blind = __any_sync(0xffffffffu, blind);
+                constexpr int kCols = kGroups == 2 ? 16 : 32;   // row columns at a time (96 registers a thread with two groups)
+                uint32_t pk[16], dk[16];
+#pragma unroll
+                for (int h = 0; h < 32; h += kCols) {
+                    uint32_t sr[kCols], dr[kCols];
+                    tmem_ld_cols(tmem + lanes + kColS + b + h, sr);
+                    tmem_ld_cols(tmem + lanes + kColDP + 64 * (u % kDPs) + 32 * ch + h, dr);
+                    tmem_ld_wait();
+                    if (h + kCols == 32) {
+                        tc_fence_before();
+                        __syncwarp();
+                        mbar_arrive_warp(bar(B_DPFREE + u % kDPs));
+                    }
+                    // two row columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D), both rounded to the
+                    // MMAs' operand type (half a step, 2^-9 of a value on average)
+                    auto column_pairs = [&](auto masked) {
+#pragma unroll
+                        for (int i4 = 0; i4 < kCols / 4; ++i4) {
+                            const float4 l4 = la[h / 4 + i4], d4 = da[h / 4 + i4];
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int i = 4 * i4 + 2 * k;
+                                float x0, x1;
+                                f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2,
+                                                 k ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y)), x0, x1);
+                                float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+                                const uint64_t e = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])),
+                                                          k ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y));
+                                float d0, d1;
+                                f2_unpack(f2_mul(f2_pack(p0, p1), e), d0, d1);
+                                if (decltype(masked)::value) {
+                                    p0 = (vis >> (h + i)) & 1u ? p0 : 0.f;
+                                    p1 = (vis >> (h + i + 1)) & 1u ? p1 : 0.f;
+                                    d0 = (vis >> (h + i)) & 1u ? d0 : 0.f;
+                                    d1 = (vis >> (h + i + 1)) & 1u ? d1 : 0.f;
+                                }
+                                pk[(h + i) >> 1] = pack_bf16x2(p0, p1);
+                                dk[(h + i) >> 1] = pack_bf16x2(d0, d1);
+                            }
+                        }
+                    };
+                    if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
+                }
+                if (any_blind) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        pk[i] = blind ? 0u : pk[i];
+                        dk[i] = blind ? 0u : dk[i];
+                    }
+                }
+                tmem_st16(tmem + lanes + kColS + b, pk);
+                tmem_st16(tmem + lanes + kColS + b + 16, dk);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_warp(bar(B_PFULL + sb));
             }
-        }
-        cluster_sync();
-    }
-    if (sums) {
-#pragma unroll 1
-        for (int c = 0; c < kHalfPart; c += 16) {
-            uint32_t own[16];
-            part(kParts ? 0 : rank, c, own);
-            float acc[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-#pragma unroll
-            for (int from = 0; from < NC; ++from)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const float4 x = kParts || from == rank ? make_float4(__uint_as_float(own[i]), __uint_as_float(own[i + 1]),
-                                                                __uint_as_float(own[i + 2]), __uint_as_float(own[i + 3]))
-                                                  : *reinterpret_cast<const float4 *>(smem + slot(from, rank, c + i));
-                    acc[i] += x.x;
-                    acc[i + 1] += x.y;
-                    acc[i + 2] += x.z;
-                    acc[i + 3] += x.w;
-                }
-            const int col = (kParts ? 0 : kPart * rank) + kHalfPart * cs + c, r = lq * 32 + lane;
-            if constexpr (kParts) {
-                float *dst = a.part_dkv + ((size_t)blockIdx.x * kKT + r) * (2 * D) + col;
-                if (r < t.nk) {
-                    st_global_v8(dst, acc[0], acc[1], acc[2], acc[3], acc[4], acc[5], acc[6], acc[7]);
-                    st_global_v8(dst + 8, acc[8], acc[9], acc[10], acc[11], acc[12], acc[13], acc[14], acc[15]);
-                }
-                continue;
-            }
-            const bool isk = col >= D;                       // dV first, then dK (times scale)
-            if (r < t.nk)
-                store_row_bf16(isk ? (__nv_bfloat16 *)a.dk + (size_t)(k0 + r) * a.dk_stride + g * D + (col - D)
-                                   : (__nv_bfloat16 *)a.dv + (size_t)(k0 + r) * a.dv_stride + g * D + col,
-                               acc, isk ? a.scale : 1.f);
+            u0 += un.steps;
         }
     }
     tc_fence_before();
@@ -521,35 +548,42 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     }
 }
 
-// 32 pieces of four columns of a key row's dV | dK a CTA, the parts' sums by eight warps (each an eighth of the parts, in
-// their order), then the warps' in theirs. A part without steps wrote none.
-template <int D>
+// Parts' sums: four columns of a key row's dV | dK a thread, in the order of the parts. With W = 8 a warp adds an eighth of
+// the parts and the warps' sums follow in their order: a tile in 76 parts 26 -> 4 us, while tiles in two or three (104 of
+// them, 128 dims) took 26 us that way and take 8 with one thread for all parts.
+template <int D, int W>
 __global__ void __launch_bounds__(256) cross_dkv_sum_kernel(const padoc_cross_args a)
 {
-    constexpr int kRow = 2 * D / 4 / 32;   // CTAs of a row
-    __shared__ float4 sums[8][32];
-    const int unit = blockIdx.x / (dkv::kKT * kRow), g = unit % a.hkv, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const padoc_cross_key_tile t = a.tiles[unit / a.hkv];
-    const int r = blockIdx.x / kRow % dkv::kKT, col = (blockIdx.x % kRow * 32 + lane) * 4;
-    if (r >= t.nk || t.steps == 0) return;
-    const float *src = a.part_dkv + ((size_t)unit * a.parts * dkv::kKT + r) * (2 * D) + col;
+    constexpr int kThreadsOut = 256 / W, kRow = 2 * D / 4;   // sums of a CTA, of a row
+    __shared__ float4 sums[W][kThreadsOut];
+    const int w = threadIdx.x / kThreadsOut, at = blockIdx.x * kThreadsOut + threadIdx.x % kThreadsOut;
+    const padoc_cross_dkv_sum t = a.dkv_sums[at / (dkv::kKT * kRow)];
+    const int r = at / kRow % dkv::kKT, col = at % kRow * 4;
+    pdl_wait_prerequisite();
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < t.nk) {
+        const float *src = a.part_dkv + ((size_t)t.slot * dkv::kKT + r) * (2 * D) + col;
 #pragma unroll 4
-    for (int p = warp; p < a.parts; p += 8) {
-        const bool some = (int)((int64_t)t.steps * (p + 1) / a.parts) != (int)((int64_t)t.steps * p / a.parts);
-        const float4 y = some ? *reinterpret_cast<const float4 *>(src + (size_t)p * dkv::kKT * (2 * D)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+        for (int p = w; p < t.parts; p += W) {
+            const float4 y = *reinterpret_cast<const float4 *>(src + (size_t)p * dkv::kKT * (2 * D));
+            x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+        }
     }
-    sums[warp][lane] = x;
-    __syncthreads();
-    if (warp) return;
-    x = sums[0][lane];
+    if constexpr (W > 1) {
+        sums[w][threadIdx.x % kThreadsOut] = x;
+        __syncthreads();
+        if (w) return;
 #pragma unroll
-    for (int w = 1; w < 8; ++w) x = make_float4(x.x + sums[w][lane].x, x.y + sums[w][lane].y, x.z + sums[w][lane].z, x.w + sums[w][lane].w);
+        for (int i = 1; i < W; ++i) {
+            const float4 y = sums[i][threadIdx.x];
+            x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+        }
+    }
+    if (r >= t.nk) return;
     const bool isk = col >= D;
     const float mul = isk ? a.scale : 1.f;
-    __nv_bfloat16 *dst = isk ? (__nv_bfloat16 *)a.dk + (size_t)(t.k0 + r) * a.dk_stride + g * D + (col - D)
-                             : (__nv_bfloat16 *)a.dv + (size_t)(t.k0 + r) * a.dv_stride + g * D + col;
+    __nv_bfloat16 *dst = isk ? (__nv_bfloat16 *)a.dk + (size_t)(t.k0 + r) * a.dk_stride + t.g * D + (col - D)
+                             : (__nv_bfloat16 *)a.dv + (size_t)(t.k0 + r) * a.dv_stride + t.g * D + col;
     *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16x2(x.x * mul, x.y * mul), pack_bf16x2(x.z * mul, x.w * mul));
 }
 
@@ -982,77 +1016,58 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     }
 }
 
-template <int D, int NC, bool kParts = false>
-padoc_status launch_dkv(const CUtensorMap &qmap, const CUtensorMap &gmap, const padoc_cross_args &a, bool after, cudaStream_t stream)
-{
-    CUtensorMap kmap, vmap;
-    if (!padoc_make_tmap_bf16(&kmap, a.k, (uint64_t)a.hkv * D, a.key_rows, a.k_stride * 2, 64, dkv::kKT) ||
-        !padoc_make_tmap_bf16(&vmap, a.v, (uint64_t)a.hkv * D, a.key_rows, a.v_stride * 2, 64, dkv::kKT))
-        return PADOC_ERR_CUDA;
-    auto kernel = cross_dkv_kernel<D, NC, kParts>;
-    if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dkv::smem_bytes<D>())) return st;
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)((a.num_tiles + a.tail_tiles) * a.hkv * (kParts ? a.parts : NC)));
-    lc.blockDim = dim3(dkv::Cols<D>::kThreads);
-    lc.dynamicSmemBytes = dkv::smem_bytes<D>();
-    lc.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = NC;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see the producer's wait
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = attr;
-    lc.numAttrs = after ? 2 : 1;
-    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, qmap, gmap, kmap, vmap, a));
-    return padoc_launch_status();
-}
-
 template <int D>
-padoc_status run(const padoc_cross_args &a, int cluster, cudaStream_t stream)
+padoc_status run(const padoc_cross_args &a, cudaStream_t stream)
 {
-    const uint64_t row = (uint64_t)a.hq * D * 2;
-    CUtensorMap qmap, gmap, omap, kmap, vmap;
-    if (!a.num_units) {   // no row sees a key: the key rows' zeros alone, which read nothing
-        CUtensorMap none = {};
-        CUtensorMap kv = {};
-        auto kernel = cross_dkv_kernel<D, 1, false>;
-        if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dkv::smem_bytes<D>())) return st;
-        if (a.num_tiles + a.tail_tiles)
-            kernel<<<(unsigned)((a.num_tiles + a.tail_tiles) * a.hkv), dkv::Cols<D>::kThreads, dkv::smem_bytes<D>(), stream>>>(none, none, kv, kv, a);
+    if (!a.num_units) {   // no row sees a key: the key rows' zeros alone
+        const int64_t n = (int64_t)(a.num_tiles - a.gap_tile + a.tail_tiles) * a.hkv;
+        if (n) cross_zero_kernel<D><<<(unsigned)(n < 4096 ? n : 4096), 256, 0, stream>>>(a);
         return padoc_launch_status();
     }
+    const uint64_t row = (uint64_t)a.hq * D * 2, cols = (uint64_t)a.hkv * D;
+    CUtensorMap qmap, gmap, omap, kmap, vmap, kmap2, vmap2;
     if (!padoc_make_tmap_bf16_heads(&qmap, a.q, D, a.hq, a.query_rows, a.q_stride * 2, a.group, a.block_tokens) ||
         !padoc_make_tmap_bf16_heads(&gmap, a.dout, D, a.hq, a.query_rows, row, a.group, a.block_tokens) ||
         !padoc_make_tmap_bf16_heads(&omap, a.out, D, a.hq, a.query_rows, row, a.group, a.block_tokens) ||
-        !padoc_make_tmap_bf16(&kmap, a.k, (uint64_t)a.hkv * D, a.key_rows, a.k_stride * 2, 64, dqp::kW) ||
-        !padoc_make_tmap_bf16(&vmap, a.v, (uint64_t)a.hkv * D, a.key_rows, a.v_stride * 2, 64, dqp::kW))
+        !padoc_make_tmap_bf16(&kmap, a.k, cols, a.key_rows, a.k_stride * 2, 64, dqp::kW) ||
+        !padoc_make_tmap_bf16(&vmap, a.v, cols, a.key_rows, a.v_stride * 2, 64, dqp::kW) ||
+        !padoc_make_tmap_bf16(&kmap2, a.k, cols, a.key_rows, a.k_stride * 2, 64, dkv::kKT) ||
+        !padoc_make_tmap_bf16(&vmap2, a.v, cols, a.key_rows, a.v_stride * 2, 64, dkv::kKT))
         return PADOC_ERR_CUDA;
-    auto kernel = cross_dq_kernel<D>;
-    if (const padoc_status st = padoc_set_max_smem((const void *)kernel, (int)dqp::smem_bytes<D>())) return st;
-    kernel<<<(unsigned)(a.ctas ? a.num_ctas : a.num_units), dqp::kThreads, dqp::smem_bytes<D>(), stream>>>(qmap, gmap, omap, kmap, vmap, a);
-    const padoc_status st = padoc_launch_status();
+    auto dq = cross_dq_kernel<D>;
+    auto dkv = cross_dkv_kernel<D>;
+    padoc_status st = padoc_set_max_smem((const void *)dq, (int)dqp::smem_bytes<D>());
+    if (st == PADOC_OK) st = padoc_set_max_smem((const void *)dkv, (int)dkv::smem_bytes<D>());
     if (st != PADOC_OK) return st;
-    if (a.parts > 1) {
-        if (const padoc_status s2 = launch_dkv<D, 1, true>(qmap, gmap, a, true, stream)) return s2;
-        cross_dkv_sum_kernel<D><<<(unsigned)(a.num_tiles * a.hkv * (dkv::kKT * 2 * D / 128)), 256, 0, stream>>>(a);
-        return padoc_launch_status();
-    }
-    switch (cluster) {
-        case 8:
-            if constexpr (D == 128) return launch_dkv<D, 8>(qmap, gmap, a, true, stream);
-        case 4: return launch_dkv<D, 4>(qmap, gmap, a, true, stream);
-        case 2: return launch_dkv<D, 2>(qmap, gmap, a, true, stream);
-        default: return launch_dkv<D, 1>(qmap, gmap, a, true, stream);
-    }
+    dq<<<(unsigned)(a.ctas ? a.num_ctas : a.num_units), dqp::kThreads, dqp::smem_bytes<D>(), stream>>>(qmap, gmap, omap, kmap, vmap, a);
+    if ((st = padoc_launch_status()) != PADOC_OK) return st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see the producer's wait
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)a.num_dkv_ctas);
+    lc.blockDim = dim3(dkv::Cols<D>::kThreads);
+    lc.dynamicSmemBytes = dkv::smem_bytes<D>();
+    lc.stream = stream;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, dkv, qmap, gmap, kmap2, vmap2, a));
+    if ((st = padoc_launch_status()) != PADOC_OK || !a.num_dkv_sums) return st;
+    const bool many = a.num_dkv_slots > 8 * a.num_dkv_sums;
+    auto sum = many ? cross_dkv_sum_kernel<D, 8> : cross_dkv_sum_kernel<D, 1>;
+    lc.gridDim = dim3((unsigned)(a.num_dkv_sums * (dkv::kKT * 2 * D / 4 / 256) * (many ? 8 : 1)));
+    lc.blockDim = dim3(256);
+    lc.dynamicSmemBytes = 0;
+    PADOC_CUDA_TRY(cudaLaunchKernelEx(&lc, sum, a));
+    return padoc_launch_status();
 }
 
 }  // namespace
 
-padoc_status padoc_cross_launch_bwd_tc(const padoc_cross_args &args, int head_dim, int cluster, cudaStream_t stream)
+padoc_status padoc_cross_launch_bwd_tc(const padoc_cross_args &args, int head_dim, cudaStream_t stream)
 {
     padoc_cross_args a = args;
     a.err = padoc_device_error_word();
     if (!a.err) return PADOC_ERR_CUDA;
-    return head_dim == 64 ? run<64>(a, cluster, stream) : run<128>(a, cluster, stream);
+    return head_dim == 64 ? run<64>(a, stream) : run<128>(a, stream);
 }

@@ -45,4 +45,18 @@ struct padoc_cross_cover {
     int32_t pad[2];
 };
 
+// dk/dv work item (bf16): steps first .. first + steps - 1 of a key tile for one KV head. 32 bytes.
+struct padoc_cross_dkv {
+    int32_t k0, nk, cover;
+    int32_t first, steps;
+    int32_t g;
+    int32_t slot;         // partial sums, -1: all of the tile's steps, written as the gradients
+    int32_t pad;
+};
+// A key tile's sums joined from parts slot .. slot + parts - 1. 32 bytes.
+struct padoc_cross_dkv_sum {
+    int32_t k0, nk, g, slot, parts;
+    int32_t pad[3];
+};
+
 // Blocks of the statistics, lse and D: [Hkv][num_subs][64] floats each.

@@ -176,8 +176,70 @@ struct Built {
     Work fwd, dq;
     std::vector<padoc_cross_key_tile> tiles;
     std::vector<padoc_cross_cover> covers;
+    std::vector<padoc_cross_dkv> dkv;
+    std::vector<int32_t> dkv_ctas;
+    std::vector<padoc_cross_dkv_sum> sums;
     padoc_cross_plan info;
 };
+
+// The dk/dv pass's items: key tiles, or parts of their steps, in a list for each CTA. Costs in steps (0.8 us with 128
+// dims, 0.4 with 64): whole tiles to the CTA that is free first, or equal runs of all steps, whichever is shorter.
+void plan_dkv(Built &b, int hkv, int lanes, int head_dim)
+{
+    const Costs k = head_dim == 128 ? Costs{3.f, 1.5f, 5.f, 0.02f, 1.f, 1, 4} : Costs{4.f, 2.f, 10.f, 0.02f, 1.f, 1, 8};
+    std::vector<Chunk> chunks;
+    for (const padoc_cross_key_tile &t : b.tiles)
+        if (t.steps) chunks.push_back({t.k0, t.nk, t.cover, 0, t.steps, 0, 1.f});
+    std::vector<Piece> pieces;
+    // whole tiles, longest first (the tiles' order)
+    std::priority_queue<std::pair<float, int32_t>, std::vector<std::pair<float, int32_t>>, std::greater<std::pair<float, int32_t>>> free;
+    for (int32_t c = 0; c < lanes; ++c) free.push({0.f, c});
+    float plain = 0.f;
+    double total = 0;
+    for (size_t c = 0; c < chunks.size(); ++c)
+        for (int32_t g = 0; g < hkv; ++g) {
+            const std::pair<float, int32_t> f = free.top();
+            free.pop();
+            const float end = f.first + chunks[c].steps + k.start;
+            free.push({end, f.second});
+            pieces.push_back({(int32_t)c, g, 0, chunks[c].steps, f.second});
+            plain = std::max(plain, end);
+            total += chunks[c].steps + k.start;
+        }
+    float lo = (float)(total / lanes), hi = std::max(plain, 2.f * lo) + 4.f * (k.start + k.part);
+    if (lo < 0.97f * plain && cut_runs(chunks, hkv, lanes, k, hi, nullptr)) {
+        for (int i = 0; i < 16 && hi - lo > 0.01f * hi; ++i) {
+            const float mid = 0.5f * (lo + hi);
+            (cut_runs(chunks, hkv, lanes, k, mid, nullptr) ? hi : lo) = mid;
+        }
+        std::vector<Piece> runs;
+        cut_runs(chunks, hkv, lanes, k, hi, &runs);
+        const size_t cuts = runs.size() - pieces.size();
+        if (hi + (cuts ? k.merge + k.read * (float)(cuts + std::min(cuts, pieces.size())) : 0.f) < 0.97f * plain) pieces = runs;
+    }
+    // slots in the order of the tiles' steps, then the lists
+    std::vector<padoc_cross_dkv> items;
+    for (size_t i = 0; i < pieces.size();) {
+        size_t n = i + 1;
+        while (n < pieces.size() && pieces[n].chunk == pieces[i].chunk && pieces[n].g == pieces[i].g) ++n;
+        const Chunk &c = chunks[pieces[i].chunk];
+        const int32_t parts = (int32_t)(n - i);
+        if (parts > 1) b.sums.push_back({c.tok, c.ntok, pieces[i].g, b.info.num_dkv_slots, parts, {0, 0, 0}});
+        for (size_t p = i; p < n; ++p)
+            items.push_back({c.tok, c.ntok, c.k0, pieces[p].first, pieces[p].steps, pieces[p].g,
+                             parts > 1 ? b.info.num_dkv_slots++ : -1, pieces[p].cta});
+        i = n;
+    }
+    std::stable_sort(items.begin(), items.end(), [](const padoc_cross_dkv &x, const padoc_cross_dkv &y) { return x.pad < y.pad; });
+    int32_t cta = -1;
+    for (size_t i = 0; i < items.size(); ++i) {
+        if (items[i].pad != cta) b.dkv_ctas.push_back((int32_t)i);
+        cta = items[i].pad;
+        items[i].pad = 0;
+    }
+    if (!items.empty()) b.dkv_ctas.push_back((int32_t)items.size());
+    b.dkv = items;
+}
 
 padoc_status check(const Segment *seg, int32_t n, const padoc_cross_config *cfg)
 {
@@ -209,6 +271,7 @@ void plan_few(const Segment *seg, int32_t n, int32_t group, int32_t head_dim, in
     int32_t most = 0;   // rows of the largest segment
     for (int32_t i = 0; i < n; ++i)
         if (seg[i].k_len) most = std::max(most, std::min(seg[i].q_len, 2 * PADOC_CROSS_FEW_ROWS) * group);
+    if (most > 2 * PADOC_CROSS_FEW_ROWS) return;   // (each 32 rows read the keys anew)
     const int32_t rows = most <= 16 ? 16 : PADOC_CROSS_FEW_ROWS;
     const int32_t an_sm = head_dim == 64 ? 3 : 2, lanes = sms * an_sm;   // CTAs
     const float step = (float)an_sm * PADOC_CROSS_FEW_STEP * head_dim * 4 / 45e3f;
@@ -356,42 +419,29 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
                          [](const padoc_cross_key_tile &x, const padoc_cross_key_tile &y) { return x.steps > y.steps; });
         info.num_subs = (int32_t)subs;
 
-        // The CTAs that share a key tile's steps: few tiles seen by many rows leave most of the chip idle, but each
-        // sharing costs its exchange (in steps of 0.8 us)
-        // (fp32: in steps of 12 us, two clusters a tile).
-        static const float start_tc[] = {6.f, 12.f, 13.f, 16.f}, start_simt[] = {0.4f, 0.6f, 0.6f, 0.7f};
-        const float *start = f32 ? start_simt : start_tc;
-        float best = 0.f;
-        for (int i = 0; i < (f32 || cfg->head_dim == 128 ? 4 : 3); ++i) {
-            const int nc = 1 << i;
-            std::vector<float> cost;
-            for (const padoc_cross_key_tile &t : b.tiles)
-                for (int32_t g = 0; g < hkv && t.steps; ++g) cost.push_back((float)ceil_div(t.steps, nc) + start[i]);
-            const float time = makespan(cost, std::max(1, lanes / nc));
-            if (i == 0 || time < best) {
-                best = time;
-                info.cluster = nc;
+        for (const padoc_cross_key_tile &t : b.tiles) info.num_gap_tiles += t.steps == 0;
+        if (f32) {
+            // The CTAs that share a key tile's steps: few tiles seen by many rows leave most of the chip idle, but each
+            // sharing costs its exchange (in steps of 12 us; two clusters a tile).
+            static const float start[] = {0.4f, 0.6f, 0.6f, 0.7f};
+            float best = 0.f;
+            for (int i = 0; i < 4; ++i) {
+                const int nc = 1 << i;
+                std::vector<float> cost;
+                for (const padoc_cross_key_tile &t : b.tiles)
+                    for (int32_t g = 0; g < hkv && t.steps; ++g) cost.push_back((float)ceil_div(t.steps, nc) + start[i]);
+                const float time = makespan(cost, std::max(1, lanes / nc));
+                if (i == 0 || time < best) {
+                    best = time;
+                    info.cluster = nc;
+                }
             }
-        }
-        // Or parts for the whole chip, whose sums a later kernel adds (2 steps' time a part to write, a launch, and
-        // reading them all at some 6 TB/s).
-        info.parts = 1;
-        const int64_t tiles = (int64_t)b.tiles.size() * hkv;
-        if (!f32 && tiles > 0 && tiles <= lanes / 2) {
-            const int32_t parts = (int32_t)(lanes / tiles);
-            std::vector<float> cost;
-            for (const padoc_cross_key_tile &t : b.tiles)
-                for (int32_t g = 0; g < hkv && t.steps; ++g)
-                    for (int32_t p = 0; p < std::min(parts, t.steps); ++p) cost.push_back((float)ceil_div(t.steps, parts) + start[0] + 2.f);
-            const float read = (float)cost.size() * cfg->head_dim * 1e-3f / 6.f / 0.8f;
-            const float time = makespan(cost, lanes) + 4.f + read;
-            if (time < best) {
-                info.cluster = 1;
-                info.parts = parts;
-            }
+        } else {
+            plan_dkv(b, hkv, sms, cfg->head_dim);
         }
     }
-    if ((int64_t)std::max(b.fwd.units.size(), b.dq.units.size()) * 4 > INT32_MAX || (int64_t)b.tiles.size() * hkv * 8 > INT32_MAX ||
+    if ((int64_t)b.sums.size() * PADOC_CROSS_KEY_TILE * cfg->head_dim > INT32_MAX ||
+        (int64_t)std::max(b.fwd.units.size(), b.dq.units.size()) * 4 > INT32_MAX || (int64_t)b.tiles.size() * hkv * 8 > INT32_MAX ||
         (int64_t)std::max(b.fwd.merges.size(), b.dq.merges.size()) * 512 > INT32_MAX)
         return PADOC_ERR_UNSUPPORTED;   // (grid sizes)
 
@@ -421,6 +471,12 @@ padoc_status make(const Segment *seg, int32_t n, const padoc_cross_config *cfg, 
     info.off_dq_merges = place(b.dq.merges.size(), sizeof(padoc_cross_merge));
     info.off_key_tiles = place(b.tiles.size(), sizeof(padoc_cross_key_tile));
     info.off_covers = place(b.covers.size(), sizeof(padoc_cross_cover));
+    info.num_dkv_units = (int32_t)b.dkv.size();
+    info.num_dkv_ctas = b.dkv_ctas.empty() ? 0 : (int32_t)b.dkv_ctas.size() - 1;
+    info.num_dkv_sums = (int32_t)b.sums.size();
+    info.off_dkv = place(b.dkv.size(), sizeof(padoc_cross_dkv));
+    info.off_dkv_ctas = place(b.dkv_ctas.size(), sizeof(int32_t));
+    info.off_dkv_sums = place(b.sums.size(), sizeof(padoc_cross_dkv_sum));
     info.plan_ints = at;
     return PADOC_OK;
 }
@@ -470,6 +526,9 @@ extern "C" padoc_status padoc_build_cross_plan(const padoc_cross_segment *segmen
     put(b.info.off_dq_merges, b.dq.merges.data(), b.dq.merges.size() * sizeof(padoc_cross_merge));
     put(b.info.off_key_tiles, b.tiles.data(), b.tiles.size() * sizeof(padoc_cross_key_tile));
     put(b.info.off_covers, b.covers.data(), b.covers.size() * sizeof(padoc_cross_cover));
+    put(b.info.off_dkv, b.dkv.data(), b.dkv.size() * sizeof(padoc_cross_dkv));
+    put(b.info.off_dkv_ctas, b.dkv_ctas.data(), b.dkv_ctas.size() * sizeof(int32_t));
+    put(b.info.off_dkv_sums, b.sums.data(), b.sums.size() * sizeof(padoc_cross_dkv_sum));
     *info = b.info;
     return PADOC_OK;
 }
@@ -485,11 +544,10 @@ extern "C" padoc_status padoc_cross_workspace_size(const padoc_cross_plan *info,
 
 extern "C" padoc_status padoc_cross_bwd_workspace_size(const padoc_cross_plan *info, size_t *bytes)
 {
-    if (!info || !bytes || !info->cfg.backward || info->num_dq_slots < 0 || info->num_subs < 0) return PADOC_ERR_INVALID_ARGUMENT;
-    // -lse2 and D, [Hkv][subs][64] each, partial dq [slots][128][d], partial dv and dk [tiles][Hkv][parts][128][2 d], fp32
+    if (!info || !bytes || !info->cfg.backward || info->num_dq_slots < 0 || info->num_subs < 0 || info->num_dkv_slots < 0) return PADOC_ERR_INVALID_ARGUMENT;
+    // -lse2 and D, [Hkv][subs][64] each, partial dq [slots][128][d], partial dv and dk [slots][128][2 d], fp32
     const size_t stats = (size_t)info->num_subs * info->cfg.num_kv_heads * PADOC_CROSS_BLOCK;
     const size_t rows = (size_t)info->num_dq_slots * (PADOC_CROSS_DQ_BLOCKS * PADOC_CROSS_BLOCK);
-    const size_t tiles = info->parts > 1 ? (size_t)info->num_key_tiles * info->cfg.num_kv_heads * info->parts : 0;
-    *bytes = (2 * stats + rows * info->cfg.head_dim + tiles * PADOC_CROSS_KEY_TILE * 2 * info->cfg.head_dim) * sizeof(float);
+    *bytes = (2 * stats + rows * info->cfg.head_dim + (size_t)info->num_dkv_slots * PADOC_CROSS_KEY_TILE * 2 * info->cfg.head_dim) * sizeof(float);
     return PADOC_OK;
 }

@@ -141,9 +141,9 @@ class padoc_cross_plan(ctypes.Structure):
     _fields_ = [("cfg", padoc_cross_config)] + [(n, ctypes.c_int32) for n in (
         "num_segments", "query_rows", "key_rows", "few", "unit_rows", "num_units", "num_ctas", "num_merges", "num_slots", "max_parts",
         "num_dq_units", "num_dq_ctas", "num_dq_merges", "num_dq_slots", "max_dq_parts", "num_subs", "num_key_tiles",
-        "num_covers", "cluster", "parts", "reserved")] + [(n, ctypes.c_int64) for n in (
+        "num_covers", "num_gap_tiles", "cluster", "num_dkv_units", "num_dkv_ctas", "num_dkv_sums", "num_dkv_slots")] + [(n, ctypes.c_int64) for n in (
             "pairs", "plan_ints", "off_units", "off_ctas", "off_merges", "off_dq_units", "off_dq_ctas", "off_dq_merges",
-            "off_key_tiles", "off_covers")]
+            "off_key_tiles", "off_covers", "off_dkv", "off_dkv_ctas", "off_dkv_sums")]
 
 
 class padoc_cross_rows(ctypes.Structure):

@@ -124,8 +124,42 @@ def test_plan_covers_every_pair_once(heads, seed):
             assert cn >= 1 and k0 <= ck and ck + cn <= k0 + nk and sub == place[tok]
             got[tok:tok + nt, ck:ck + cn] += 1
     assert (tiled == 1).all() and (got == want).all()
-    assert info.parts >= 1 and (info.parts == 1 or info.cluster == 1)
-    assert info.cluster in (1, 2, 4, 8) and (info.cluster < 8 or cfg.head_dim == 128 or cfg.dtype == pa.PADOC_DTYPE_F32)
+    gaps = [t for t in _units(plan, info.off_key_tiles, info.num_key_tiles) if t[4] == 0]
+    assert len(gaps) == info.num_gap_tiles
+    if cfg.dtype == pa.PADOC_DTYPE_F32:
+        assert info.cluster in (1, 2, 4, 8) and info.num_dkv_units == 0
+        return
+    # dk/dv items: every step of every tile and KV head once, parts joined in the steps' order
+    tiles = {(int(t[0]), int(t[1])): t for t in _units(plan, info.off_key_tiles, info.num_key_tiles) if t[4]}
+    items = _units(plan, info.off_dkv, info.num_dkv_units)
+    ends = plan[info.off_dkv_ctas:info.off_dkv_ctas + info.num_dkv_ctas + 1] if info.num_dkv_ctas else np.zeros(1, np.int32)
+    assert ends[0] == 0 and ends[-1] == info.num_dkv_units and (np.diff(ends) > 0).all()
+    assert info.num_dkv_ctas <= max(1, cfg.ctas or 152)
+    done, parts = {}, {}
+    for k0, nk, cover, first, steps, g, slot, _ in items:
+        t = tiles[int(k0), int(nk)]
+        assert cover == t[2] and steps >= 1 and 0 <= first and first + steps <= t[4]
+        done.setdefault((k0, g), []).append((first, steps))
+        if slot >= 0:
+            assert slot not in parts
+            parts[slot] = (k0, nk, g, first)
+        else:
+            assert steps == t[4]
+    assert len(done) == len(tiles) * hkv
+    for (k0, g), runs in done.items():
+        at = 0
+        for first, steps in sorted(runs):
+            assert first == at
+            at += steps
+        assert at == [t for t in tiles.values() if t[0] == k0][0][4]
+    assert sorted(parts) == list(range(info.num_dkv_slots))
+    joined = 0
+    for k0, nk, g, slot, n in _units(plan, info.off_dkv_sums, info.num_dkv_sums)[:, :5]:
+        assert n == len(done[k0, g]) > 1
+        mine = [parts[p] for p in range(slot, slot + n)]
+        assert all(m[:3] == (k0, nk, g) for m in mine) and [m[3] for m in mine] == sorted(m[3] for m in mine)
+        joined += n
+    assert joined == info.num_dkv_slots
 
 
 def test_few_rows_are_split_over_the_chip():

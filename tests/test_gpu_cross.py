@@ -178,9 +178,9 @@ def test_many_rows(hq, hkv, d):
 
 @pytest.mark.parametrize("hq,hkv,d", [(16, 2, 128), (4, 1, 64), (7, 1, 128)])
 def test_few_keys_that_many_rows_see(hq, hkv, d):
-    # a key tile's rows shared out over the whole chip, or over clusters; key rows between that nobody sees
+    # a key tile's rows shared out over the whole chip; key rows between that nobody sees
     plan = check_backward([(0, 900, 5, 70), (900, 60, 400, 200), (960, 3, 300, 10)], hq, hkv, d, BF16)
-    assert plan.info.parts > 1
+    assert plan.info.num_dkv_sums > 0 and plan.info.num_gap_tiles > 0
     for segments in ([(0, 900, 0, 700)], [(0, 130, 3, 128)], [(0, 2, 0, 100)]):
         check_backward(segments, hq, hkv, d, BF16)
 
