@@ -185,6 +185,17 @@ def test_few_keys_that_many_rows_see(hq, hkv, d):
         check_backward(segments, hq, hkv, d, BF16)
 
 
+@pytest.mark.parametrize("hq,hkv,d,dtype,rows,keys,ctas,cut", [
+    (16, 2, 128, BF16, 700, 1490, 7, "fwd"), (16, 2, 128, BF16, 290, 2500, 7, "dq"), (4, 4, 64, BF16, 290, 1500, 5, "both"),
+    (4, 4, 64, F32, 200, 501, 7, "dq")])
+def test_the_last_round_is_cut(hq, hkv, d, dtype, rows, keys, ctas, cut):
+    segments = [(3, rows, 10, keys)]
+    check_forward(segments, hq, hkv, d, dtype, ctas=ctas)
+    info = check_backward(segments, hq, hkv, d, dtype, ctas=ctas).info
+    assert cut == "dq" or (info.num_ctas == 0 and info.num_slots > 0)
+    assert cut == "fwd" or (info.num_dq_ctas == 0 and info.num_dq_slots > 0)
+
+
 @pytest.mark.parametrize("hq,hkv,d", [(16, 16, 64), (16, 2, 128), (8, 8, 64)])
 @pytest.mark.parametrize("keys", [1, 70, 130, 250])
 def test_many_short_items(hq, hkv, d, keys):
