@@ -941,7 +941,8 @@ typedef struct {
     int32_t head_dim;       /* 64 or 128 */
     padoc_dtype dtype;
     int32_t backward;       /* 1: the plan also serves padoc_cross_attn_bwd */
-    int32_t ctas;           /* CTAs the work is balanced over; 0: the current device's multiprocessor count */
+    int32_t ctas;           /* CTAs the work is balanced over, at most 65535; 0: the current device's multiprocessor
+                             * count */
 } padoc_cross_config;
 
 /* Host summary of a cross-attention plan, filled by padoc_build_cross_plan. The int32 plan blob it describes must be

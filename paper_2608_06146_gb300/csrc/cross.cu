@@ -6,6 +6,8 @@
 //   P = exp(S - lse),  D = rowsum(dO * O),  dS = P (dO V^T - D),  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.
 #include <math.h>
 
+#include <algorithm>
+
 #include "cross.cuh"
 
 namespace {
@@ -134,6 +136,8 @@ padoc_status merge_rows(const padoc_cross_args &a, int head_dim, bool pdl, cudaS
 // fp32: 64 packed rows a CTA of 256 threads, in steps of 64 keys. Tiles lie in shared memory, rows four
 // floats further apart than their length (a quarter warp's 16-byte reads of eight rows then meet no bank twice); a
 // thread keeps four rows by four columns of a 64 x 64 product, or four rows by D / 16 columns of a 64 x D one.
+// Meant for small pages: bound by the chain of a step (5 us with 64 dims: two products, three barriers), so keys are cut
+// until every SM has an item (368 rows of 4 heads over 260 states 33 -> 16 us, parts joined by a second kernel).
 // ------------------------------------------------------------------------------------------------
 
 constexpr int kB = PADOC_CROSS_BLOCK;
@@ -581,7 +585,10 @@ padoc_status check_rows(const padoc_cross_plan *info, const int32_t *plan, const
     const int64_t e = c.dtype == PADOC_DTYPE_F32 ? 4 : 2;
     const int64_t most = (int64_t)1 << 39;   // (a tensor map's strides have 40 bits)
     for (const int64_t s : {r->q_stride, r->k_stride, r->v_stride})
-        if (s < 0 || s * e % 16 || s > most / e) return PADOC_ERR_INVALID_ARGUMENT;
+        if (s < 0 || s > most / e || s * e % 16) return PADOC_ERR_INVALID_ARGUMENT;
+    // (what the overlap checks add up stays in 64 bits)
+    if (r->q_stride * e > INT64_MAX / 4 / (r->query_rows + 1) || std::max(r->k_stride, r->v_stride) * e > INT64_MAX / 4 / (r->key_rows + 1))
+        return PADOC_ERR_INVALID_ARGUMENT;
     if (r->q_stride < (int64_t)c.num_q_heads * c.head_dim || r->k_stride < (int64_t)c.num_kv_heads * c.head_dim ||
         r->v_stride < (int64_t)c.num_kv_heads * c.head_dim)
         return PADOC_ERR_INVALID_ARGUMENT;
@@ -673,7 +680,10 @@ extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const
     const padoc_cross_config &c = info->cfg;
     const int64_t e = c.dtype == PADOC_DTYPE_F32 ? 4 : 2;
     for (const int64_t s : {grads->dq_stride, grads->dk_stride, grads->dv_stride})
-        if (s < 0 || s * e % 16 || s > ((int64_t)1 << 39) / e) return PADOC_ERR_INVALID_ARGUMENT;
+        if (s < 0 || s > ((int64_t)1 << 39) / e || s * e % 16) return PADOC_ERR_INVALID_ARGUMENT;
+    if (grads->dq_stride * e > INT64_MAX / 4 / (rows->query_rows + 1) ||
+        std::max(grads->dk_stride, grads->dv_stride) * e > INT64_MAX / 4 / (rows->key_rows + 1))
+        return PADOC_ERR_INVALID_ARGUMENT;
     if (grads->dq_stride < (int64_t)c.num_q_heads * c.head_dim || grads->dk_stride < (int64_t)c.num_kv_heads * c.head_dim ||
         grads->dv_stride < (int64_t)c.num_kv_heads * c.head_dim)
         return PADOC_ERR_INVALID_ARGUMENT;

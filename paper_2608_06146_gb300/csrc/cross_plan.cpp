@@ -125,6 +125,55 @@ void make_work(const std::vector<Chunk> &chunks, const std::vector<Piece> &piece
     }
 }
 
+// Whole chunks but for the shortest, those of the last round, cut so that they fill it (164 items of 8 steps on 152 SMs:
+// 36.0 -> 33.5 us; not where the last round matters little: 2048 items of 20 steps 447 -> 457). Returns the time, which
+// is `plain` where nothing is cut (out is empty then).
+float cut_ends(const std::vector<Chunk> &chunks, const std::vector<Piece> &whole, const std::vector<float> &cost, int lanes,
+               const Costs &k, double total, float plain, std::vector<Piece> &out)
+{
+    const size_t tail = whole.size() % (size_t)lanes;
+    if (whole.size() <= (size_t)lanes || whole.size() > (size_t)16 * lanes || !tail || (float)(total / lanes) >= 0.95f * plain) return plain;
+    std::vector<size_t> order(whole.size());
+    for (size_t i = 0; i < order.size(); ++i) order[i] = i;
+    std::stable_sort(order.begin(), order.end(), [&](size_t x, size_t y) { return cost[x] > cost[y]; });
+    auto parts_of = [&](size_t i, int32_t p) { return std::min(p, std::max(1, whole[i].steps / k.least)); };
+    float best = 0.97f * plain;
+    int32_t into = 0;
+    for (const int32_t p : {2, 3, 4, 6, 8, 12, 16}) {
+        std::vector<float> time = cost;
+        size_t cuts = 0;
+        double sum = total;
+        for (size_t o = order.size() - tail; o < order.size(); ++o) {
+            const size_t i = order[o];
+            const int32_t parts = parts_of(i, p);
+            if (parts == 1) continue;
+            sum -= time[i];
+            time[i] = ceil_div(whole[i].steps, parts) * chunks[whole[i].chunk].step_cost + k.start + k.part;
+            time.insert(time.end(), parts - 1, time[i]);
+            cuts += parts;
+            sum += parts * time[i];
+        }
+        const float join = k.merge + k.read * (float)cuts;
+        if (!cuts || (float)(sum / lanes) + join >= best) break;   // (more parts cost more)
+        const float t = makespan(time, lanes) + join;
+        if (t < best) {
+            best = t;
+            into = p;
+        }
+    }
+    if (!into) return plain;
+    std::vector<char> cut(whole.size(), 0);
+    for (size_t o = order.size() - tail; o < order.size(); ++o) cut[order[o]] = 1;
+    for (size_t i = 0; i < whole.size(); ++i) {
+        const int32_t steps = whole[i].steps, parts = cut[i] ? parts_of(i, into) : 1;
+        for (int32_t q = 0; q < parts; ++q) {
+            const int32_t a = (int32_t)((int64_t)steps * q / parts), b = (int32_t)((int64_t)steps * (q + 1) / parts);
+            out.push_back({whole[i].chunk, whole[i].g, a, b - a, 0});
+        }
+    }
+    return best;
+}
+
 // The items of a pass: whole chunks, taken as SMs get free, the last ones perhaps cut, or, where that leaves the chip idle,
 // equal runs of the sequence of all steps, a list for each CTA, with chunks cut where a run ends. kPieces (fp32, whose kernels run a
 // CTA per 64 rows): the runs' pieces without the lists.
@@ -145,46 +194,8 @@ float plan_work(const std::vector<Chunk> &chunks, int hkv, int lanes, const Cost
     if (chunks.empty()) return 0.f;
     float plain = makespan(cost, lanes);
     const float lowest = (float)(total / lanes);
-    // Whole chunks but for the shortest, those of the last round, cut so that they fill it (164 items of 8 steps on 152
-    // SMs: 36.0 -> 33.5 us; not for a last round that matters little: 2048 items of 20 steps 447 -> 457).
     std::vector<Piece> ends;
-    const size_t tail = whole.size() % (size_t)lanes;
-    if (whole.size() > (size_t)lanes && whole.size() <= (size_t)16 * lanes && tail && lowest < 0.95f * plain) {
-        std::vector<size_t> order(whole.size());
-        for (size_t i = 0; i < order.size(); ++i) order[i] = i;
-        std::stable_sort(order.begin(), order.end(), [&](size_t x, size_t y) { return cost[x] > cost[y]; });
-        float best = 0.97f * plain;
-        int32_t into = 0;
-        for (int32_t p = 2; p <= 16; ++p) {
-            std::vector<float> time = cost;
-            size_t cuts = 0;
-            for (size_t i = order.size() - tail; i < order.size(); ++i) {
-                const Chunk &c = chunks[whole[order[i]].chunk];
-                const int32_t parts = std::min(p, std::max(1, c.steps / k.least));
-                if (parts == 1) continue;
-                time[order[i]] = ceil_div(c.steps, parts) * c.step_cost + k.start + k.part;
-                time.insert(time.end(), parts - 1, time[order[i]]);
-                cuts += parts;
-            }
-            const float t = makespan(time, lanes) + k.merge + k.read * (float)cuts;
-            if (cuts && t < best) {
-                best = t;
-                into = p;
-            }
-        }
-        if (into) {
-            std::vector<char> cut(whole.size(), 0);
-            for (size_t i = order.size() - tail; i < order.size(); ++i) cut[order[i]] = 1;
-            for (size_t i = 0; i < whole.size(); ++i) {
-                const int32_t steps = whole[i].steps, parts = cut[i] ? std::min(into, std::max(1, steps / k.least)) : 1;
-                for (int32_t q = 0; q < parts; ++q) {
-                    const int32_t a = (int32_t)((int64_t)steps * q / parts), b = (int32_t)((int64_t)steps * (q + 1) / parts);
-                    ends.push_back({whole[i].chunk, whole[i].g, a, b - a, 0});
-                }
-            }
-            plain = best;
-        }
-    }
+    plain = cut_ends(chunks, whole, cost, lanes, k, total, plain, ends);
     float lo = lowest, hi = std::max(longest, 2.f * lo) + 4.f * (k.start + k.part);
     if (lo < 0.97f * plain && cut_runs(chunks, hkv, lanes, k, hi, nullptr)) {
         for (int i = 0; i < 16 && hi - lo > 0.01f * hi; ++i) {
@@ -223,40 +234,63 @@ struct Built {
     padoc_cross_plan info;
 };
 
-// The dk/dv pass's items: key tiles, or parts of their steps, in a list for each CTA. Costs in steps (0.8 us with 128
-// dims, 0.4 with 64): whole tiles to the CTA that is free first, or equal runs of all steps, whichever is shorter.
+// The dk/dv pass's items: key tiles, or parts of their steps, in a list for each CTA. Costs in steps (0.87 us with 128
+// dims, 0.6 with 64). More tiles than CTAs: whole ones, those of the last round cut where that pays, longest first to the
+// CTA that is free first. They all begin with a segment's first rows, which the CTAs thus fetch at about the same time:
+// equal runs of all steps, in which every CTA begins elsewhere, took 1750 us instead of 1640 for 320 tiles of 512 steps.
+// Else equal runs, where they are shorter (120 tiles of up to 184 steps, 9510 in all, by clusters of CTAs 82 us, in runs
+// 69 and their sums 8).
 void plan_dkv(Built &b, int hkv, int lanes, int head_dim)
 {
     const Costs k = head_dim == 128 ? Costs{3.f, 1.5f, 5.f, 0.02f, 1.f, 1, 4} : Costs{4.f, 2.f, 10.f, 0.02f, 1.f, 1, 8};
     std::vector<Chunk> chunks;
-    for (const padoc_cross_key_tile &t : b.tiles)
-        if (t.steps) chunks.push_back({t.k0, t.nk, t.cover, 0, t.steps, 0, 1.f});
     std::vector<Piece> pieces;
-    // whole tiles, longest first (the tiles' order)
-    std::priority_queue<std::pair<float, int32_t>, std::vector<std::pair<float, int32_t>>, std::greater<std::pair<float, int32_t>>> free;
-    for (int32_t c = 0; c < lanes; ++c) free.push({0.f, c});
-    float plain = 0.f;
+    std::vector<float> cost;
     double total = 0;
-    for (size_t c = 0; c < chunks.size(); ++c)
-        for (int32_t g = 0; g < hkv; ++g) {
+    for (const padoc_cross_key_tile &t : b.tiles)
+        if (t.steps) {
+            for (int32_t g = 0; g < hkv; ++g) {
+                pieces.push_back({(int32_t)chunks.size(), g, 0, t.steps, 0});
+                cost.push_back(t.steps + k.start);
+                total += t.steps + k.start;
+            }
+            chunks.push_back({t.k0, t.nk, t.cover, 0, t.steps, 0, 1.f});
+        }
+    if (pieces.empty()) return;
+    float plain = makespan(cost, lanes);
+    bool runs = false;
+    if (pieces.size() > (size_t)lanes) {
+        std::vector<Piece> ends;
+        cut_ends(chunks, pieces, cost, lanes, k, total, plain, ends);
+        if (!ends.empty()) pieces = ends;
+    } else {
+        float lo = (float)(total / lanes), hi = std::max(plain, 2.f * lo) + 4.f * (k.start + k.part);
+        if (lo < 0.97f * plain && cut_runs(chunks, hkv, lanes, k, hi, nullptr)) {
+            for (int i = 0; i < 16 && hi - lo > 0.01f * hi; ++i) {
+                const float mid = 0.5f * (lo + hi);
+                (cut_runs(chunks, hkv, lanes, k, mid, nullptr) ? hi : lo) = mid;
+            }
+            std::vector<Piece> cut;
+            cut_runs(chunks, hkv, lanes, k, hi, &cut);
+            const size_t cuts = cut.size() - pieces.size();
+            if (hi + (cuts ? k.merge + k.read * (float)(cuts + std::min(cuts, pieces.size())) : 0.f) < 0.97f * plain) {
+                pieces = cut;
+                runs = true;
+            }
+        }
+    }
+    std::vector<int32_t> place(pieces.size());   // the lists' order
+    for (size_t i = 0; i < pieces.size(); ++i) place[i] = (int32_t)i;
+    if (!runs) {
+        std::stable_sort(place.begin(), place.end(), [&](int32_t x, int32_t y) { return pieces[x].steps > pieces[y].steps; });
+        std::priority_queue<std::pair<float, int32_t>, std::vector<std::pair<float, int32_t>>, std::greater<std::pair<float, int32_t>>> free;
+        for (int32_t c = 0; c < lanes; ++c) free.push({0.f, c});
+        for (const int32_t i : place) {
             const std::pair<float, int32_t> f = free.top();
             free.pop();
-            const float end = f.first + chunks[c].steps + k.start;
-            free.push({end, f.second});
-            pieces.push_back({(int32_t)c, g, 0, chunks[c].steps, f.second});
-            plain = std::max(plain, end);
-            total += chunks[c].steps + k.start;
+            pieces[i].cta = f.second;
+            free.push({f.first + pieces[i].steps + k.start, f.second});
         }
-    float lo = (float)(total / lanes), hi = std::max(plain, 2.f * lo) + 4.f * (k.start + k.part);
-    if (lo < 0.97f * plain && cut_runs(chunks, hkv, lanes, k, hi, nullptr)) {
-        for (int i = 0; i < 16 && hi - lo > 0.01f * hi; ++i) {
-            const float mid = 0.5f * (lo + hi);
-            (cut_runs(chunks, hkv, lanes, k, mid, nullptr) ? hi : lo) = mid;
-        }
-        std::vector<Piece> runs;
-        cut_runs(chunks, hkv, lanes, k, hi, &runs);
-        const size_t cuts = runs.size() - pieces.size();
-        if (hi + (cuts ? k.merge + k.read * (float)(cuts + std::min(cuts, pieces.size())) : 0.f) < 0.97f * plain) pieces = runs;
     }
     // slots in the order of the tiles' steps, then the lists
     std::vector<padoc_cross_dkv> items;
@@ -268,24 +302,21 @@ void plan_dkv(Built &b, int hkv, int lanes, int head_dim)
         if (parts > 1) b.sums.push_back({c.tok, c.ntok, pieces[i].g, b.info.num_dkv_slots, parts, {0, 0, 0}});
         for (size_t p = i; p < n; ++p)
             items.push_back({c.tok, c.ntok, c.k0, pieces[p].first, pieces[p].steps, pieces[p].g,
-                             parts > 1 ? b.info.num_dkv_slots++ : -1, pieces[p].cta});
+                             parts > 1 ? b.info.num_dkv_slots++ : -1, 0});
         i = n;
     }
-    std::stable_sort(items.begin(), items.end(), [](const padoc_cross_dkv &x, const padoc_cross_dkv &y) { return x.pad < y.pad; });
-    int32_t cta = -1;
-    for (size_t i = 0; i < items.size(); ++i) {
-        if (items[i].pad != cta) b.dkv_ctas.push_back((int32_t)i);
-        cta = items[i].pad;
-        items[i].pad = 0;
+    std::stable_sort(place.begin(), place.end(), [&](int32_t x, int32_t y) { return pieces[x].cta < pieces[y].cta; });
+    for (size_t i = 0; i < place.size(); ++i) {
+        if (i == 0 || pieces[place[i]].cta != pieces[place[i - 1]].cta) b.dkv_ctas.push_back((int32_t)i);
+        b.dkv.push_back(items[place[i]]);
     }
-    if (!items.empty()) b.dkv_ctas.push_back((int32_t)items.size());
-    b.dkv = items;
+    b.dkv_ctas.push_back((int32_t)b.dkv.size());
 }
 
 padoc_status check(const Segment *seg, int32_t n, const padoc_cross_config *cfg)
 {
     if (!cfg || n < 0 || (n > 0 && !seg)) return PADOC_ERR_INVALID_ARGUMENT;
-    if (cfg->num_q_heads < 1 || cfg->num_kv_heads < 1 || cfg->num_q_heads % cfg->num_kv_heads || cfg->ctas < 0 ||
+    if (cfg->num_q_heads < 1 || cfg->num_kv_heads < 1 || cfg->num_q_heads % cfg->num_kv_heads || cfg->ctas < 0 || cfg->ctas > 65535 ||
         cfg->backward < 0 || cfg->backward > 1)
         return PADOC_ERR_INVALID_ARGUMENT;
     if (cfg->dtype != PADOC_DTYPE_F32 && cfg->dtype != PADOC_DTYPE_BF16) return PADOC_ERR_UNSUPPORTED;
@@ -312,13 +343,16 @@ void plan_few(const Segment *seg, int32_t n, int32_t group, int32_t head_dim, in
     int32_t most = 0;   // rows of the largest segment
     for (int32_t i = 0; i < n; ++i)
         if (seg[i].k_len) most = std::max(most, std::min(seg[i].q_len, 2 * PADOC_CROSS_FEW_ROWS) * group);
-    if (most > 2 * PADOC_CROSS_FEW_ROWS) return;   // (each 32 rows read the keys anew)
     const int32_t rows = most <= 16 ? 16 : PADOC_CROSS_FEW_ROWS;
     const int32_t an_sm = head_dim == 64 ? 3 : 2, lanes = sms * an_sm;   // CTAs
+    // (many blocks of rows, each reading the keys anew, cannot win: planning them would be most of the planner's time)
+    int64_t items = 0;
+    for (int32_t i = 0; i < n; ++i)
+        if (seg[i].k_len) items += ((int64_t)seg[i].q_len * group + rows - 1) / rows * hkv;
+    if (items > (most > PADOC_CROSS_FEW_ROWS ? 4 : 64) * (int64_t)lanes) return;
     const float step = (float)an_sm * PADOC_CROSS_FEW_STEP * head_dim * 4 / 45e3f;
     const Costs k = {3.f / step, 0.3f / step, 3.f / step, 0.001f / step, 1.f, PADOC_CROSS_FEW_STEP, 2};
     const std::vector<Chunk> chunks = chunks_of(rows / group, k);
-    if (chunks.size() * hkv > (size_t)64 * lanes) return;
     Work w;
     int few = 1;
     float best = step * plan_work(chunks, hkv, lanes, k, kPieces, w);

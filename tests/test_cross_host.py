@@ -186,7 +186,7 @@ def test_plan_refusals(lib):
     assert status([(0, 4, 2 ** 31 - 1000, 10)], cfg()) == 1
     assert status([(0, 4, 2 ** 30, 10)], cfg(backward=True)) == 2
     assert status([(0, 2 ** 30, 0, 10)], cfg()) == 2
-    for bad in (dict(num_q_heads=0), dict(num_kv_heads=0), dict(num_q_heads=15), dict(ctas=-1)):
+    for bad in (dict(num_q_heads=0), dict(num_kv_heads=0), dict(num_q_heads=15), dict(ctas=-1), dict(ctas=65536)):
         assert status(seg, cfg(**bad)) == 1
     for bad in (dict(head_dim=96), dict(num_q_heads=130), dict(dtype=7)):
         assert status(seg, cfg(**bad)) == 2
@@ -233,6 +233,7 @@ def test_calls_are_refused_before_any_launch(lib):
         assert fwd(**{name: A + 2}) == 1
     assert fwd(qs=2040) == 1 and fwd(qs=2050) == 1 and fwd(ks=128) == 1 and fwd(vs=0) == 1 and fwd(ks=-256) == 1
     assert fwd(qn=0) == 1 and fwd(kn=960) == 1 and fwd(kn=2 ** 31) == 1
+    assert fwd(qs=2 ** 62) == 1 and fwd(ks=2 ** 37, kn=2 ** 30) == 1 and bwd(dqs=2 ** 62) == 1 and bwd(dvs=2 ** 37, kn=2 ** 30) == 1
     assert fwd(scale=0.0) == 1 and fwd(scale=math.nan) == 1 and fwd(scale=math.inf) == 1
     assert fwd(ws=None) == 1 and fwd(ws=64 * A + 16) == 1 and fwd(n=need - 1) == 3
     assert fwd(out=A) == 1 and fwd(out=4 * A + 512 * 960) == 1 and fwd(lse=5 * A) == 1 and fwd(lse=2 * A) == 1   # overlaps
