@@ -26,10 +26,11 @@
 // an error and all roles leave their loops, the MMA warps wait for their MMAs, the producer for its copies, and tensor
 // memory is released.
 //
-// Measured: 32768 rows over 8 x 2560 states of 16 query and 2 KV heads of 128 dims 1545 us, dQ 585 and dK/dV 935 (1560
-// TFLOP/s over the seven products made, 90% of what a library product sustains); 8 pages of 25 segments over 1601 states
-// 135 us (62 and 69, sums 8); 9 pages of 16 heads of 64 dims 152 (63 and 89). The short calls lose an item's start and
-// end (3 to 4 us) and the launches.
+// Measured: 32768 rows over 8 x 2560 states of 16 query and 2 KV heads of 128 dims 1441 us, dQ 589 and dK/dV 848 (1670
+// TFLOP/s over the seven products made, 96% of what a library product sustains). A step of 64 rows of the dK/dV pass lasts
+// 1460 cycles, of which the tensor cores work 1020 and shared memory is read or written some 1150; one of 64 keys of the
+// dQ pass 1005, 770 and 900. 8 pages of 25 segments over 1601 states 135 us (62 and 69, sums 8); 9 pages of 16 heads of 64
+// dims 152 (63 and 89). The short calls lose an item's start and end (3 to 4 us) and the launches.
 #include <math.h>
 
 #include <algorithm>
@@ -104,7 +105,7 @@ constexpr int kQPanel = kBlk * 128;          // [64 rows][64 bf16]
 constexpr int kAuxBytes = 2 * kBlk * 4;      // -lse2[64], D[64]
 // With 64 dims two groups of eight softmax warps take the steps in turn: one group's work on a step lasts longer than its
 // 16 MMAs (98 us against 110 for 9 pages of 16 heads, both before items came in lists). With 128 dims, 24 MMAs, one group with all registers is faster
-// (937 us against 983 for 32768 rows over 8 x 2560 states).
+// (937 us against 983 for 32768 rows over 8 x 2560 states, before items came in lists).
 // Tensor memory: S buffers, dP buffers, V as an A operand (128 dims; with 64 it is read from shared memory), dV and dK.
 template <int D>
 struct Cols {
@@ -826,7 +827,9 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                     umma_commit_warp(bar(B_SFULL + slot));
                 }
             } else if (warp == 11) {
-                // dP = dO V^T, both from shared memory
+                // dP = dO V^T, both from shared memory (dO in tensor memory as Q is: 32768 rows over 8 x 2560 states 1548 ->
+                // 1521 us, as the product's 48 KB a step take longer than its MMAs, but an item then begins later and there
+                // is one dP buffer: 8 pages of 25 segments 137 -> 140 us, 9 pages of 16 heads 156 -> 157.5)
                 const uint64_t dg = umma_desc_sw128(smem_u32(sg), 16, 1024);
                 ok = wait_w(B_GROWS, n & 1, 197);
                 for (int u = 0; ok && u < un.steps; ++u, next_step()) {
