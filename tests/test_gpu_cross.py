@@ -234,6 +234,39 @@ def test_scores_of_far_apart_sizes(dtype):
         within(got, ref, bound)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_offsets_past_32_bits(dtype):
+    # the last rows of arrays of more than 2^31 elements, and the zeros of all key rows before them
+    rows, stride, hq, hkv, d, scale = 36_000, 65_536, 8, 2, 128, 1 / math.sqrt(128)
+    seg, near = [(rows - 20, 20, rows - 300, 300)], [(0, 20, 0, 300)]
+    x = [torch.empty(rows * stride, dtype=dtype, device=DEV) for _ in range(2)]
+    part = lambda b, at, h: x[b][at:].as_strided((rows, h, d), (stride, d, 1))
+    q, k, v = part(0, 0, hq), part(0, hq * d, hkv), part(0, (hq + hkv) * d, hkv)
+    dq, dk, dv = part(1, 0, hq), part(1, hq * d, hkv), part(1, (hq + hkv) * d, hkv)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    nq, nk, nv, ng = (torch.randn((n, h, d), generator=g, device=DEV).to(dtype) for n, h in ((20, hq), (300, hkv), (300, hkv), (20, hq)))
+    q[-20:], k[-300:], v[-300:] = nq, nk, nv
+    dk.fill_(77)
+    dv.fill_(77)
+    out, dout = (torch.zeros((rows, hq, d), dtype=dtype, device=DEV) for _ in range(2))
+    lse = torch.zeros((rows, hq), device=DEV)
+    dout[-20:] = ng
+    plan = CrossPlan(seg, hq, hkv, d, dtype, DEV, training=True)
+    plan.run(q, k, v, scale, out, lse)
+    pa.padoc_check_device_errors()
+    want, wl, _ = oc.forward(near, nq, nk, nv, scale)
+    bo, bl = oc.forward_bounds(near, nq, nk, nv, scale)
+    within(out[-20:], want, bo)
+    within(lse[-20:], wl, bl)
+    out[-20:], lse[-20:] = want.to(dtype), wl.float()
+    plan.run_bwd(q, k, v, out, dout, lse, scale, dq, dk, dv)
+    pa.padoc_check_device_errors()
+    for got, ref, bound in zip((dq[-20:], dk[-300:], dv[-300:]), oc.backward(near, nq, nk, nv, ng, scale),
+                               oc.backward_bounds(near, nq, nk, nv, out[-20:], ng, scale)):
+        within(got, ref, bound)
+    assert not dk[:-300].any() and not dv[:-300].any()
+
+
 def test_segments_without_keys_alone():
     segments = [(0, 4, 0, 0), (6, 2, 9, 0)]
     q, k, v, dout = inputs(segments, 16, 2, 128, BF16, keys=5)
