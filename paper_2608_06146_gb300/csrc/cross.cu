@@ -744,7 +744,7 @@ extern "C" padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const
     const size_t stats = (size_t)info->num_subs * a.hkv * kB;
     a.neg_lse2 = (float *)workspace;
     a.dsum = a.neg_lse2 + stats;
-    a.part = a.dsum + stats;
+    a.part = a.dsum + (c.dtype == PADOC_DTYPE_F32 ? 1 : 4) * stats;   // (bf16: 16 bytes a row)
     a.dkv = (const padoc_cross_dkv *)(plan_dev + info->off_dkv);
     a.dkv_ctas = plan_dev + info->off_dkv_ctas;
     a.dkv_sums = (const padoc_cross_dkv_sum *)(plan_dev + info->off_dkv_sums);

@@ -25,7 +25,7 @@ struct padoc_cross_args {
     const padoc_cross_dkv_sum *dkv_sums;
     int32_t num_dkv_ctas, num_dkv_sums, num_dkv_slots;
     int32_t gap_tile;                          // first of the tiles that no row sees (the last ones)
-    float *neg_lse2, *dsum;                    // -lse * log2(e) and rowsum(dO * O): [Hkv][subs][64]
+    float *neg_lse2, *dsum;                    // -lse * log2(e) and rowsum(dO * O) (bf16: 16 bytes of its negative): [Hkv][subs][64]
     int32_t unit_rows;                         // packed rows of a forward or dq item, and of its partial result
     int32_t num_units, num_ctas, num_merges, max_parts, num_tiles, num_subs;
     int32_t tail_begin, tail_tiles;            // key rows that the plan does not reach

@@ -102,7 +102,11 @@ constexpr int kKT = PADOC_CROSS_KEY_TILE;   // 128 keys: the M of every MMA
 constexpr int kMaxStages = 8;
 constexpr int kKPanel = kKT * 128;           // [128 rows][64 bf16]
 constexpr int kQPanel = kBlk * 128;          // [64 rows][64 bf16]
-constexpr int kAuxBytes = 2 * kBlk * 4;      // -lse2[64], D[64]
+// -lse2[64], then -D of each row as eight bf16, the first three of which add up to it. They are a B operand: a last product
+// of 16 (with ones for these three, zeros for the rest) subtracts D from dP. Read as fp32 like -lse2, each value by a whole
+// warp, D kept shared memory busy for 256 cycles a step more (1439 -> 1340 us for 32768 rows over 8 x 2560 states).
+constexpr int kAuxBytes = kBlk * 4 + kBlk * 16;
+constexpr int kSelBytes = 2 * kKT * 16;      // ... that product's A: 128 rows of three ones, 128 of zeros
 // With 64 dims two groups of eight softmax warps take the steps in turn: one group's work on a step lasts longer than its
 // 16 MMAs (98 us against 110 for 9 pages of 16 heads, both before items came in lists). With 128 dims, 24 MMAs, one group with all registers is faster
 // (937 us against 983 for 32768 rows over 8 x 2560 states, before items came in lists).
@@ -147,7 +151,7 @@ template <int D>
 constexpr size_t smem_bytes()
 {
     return 1024 + 2 * (size_t)Cols<D>::kKBufs * (D / 64) * kKPanel + 2 * (size_t)Cols<D>::kStages * (D / 64) * kQPanel +
-           (size_t)Cols<D>::kStages * kAuxBytes + 2 * sizeof(Unit) + B_COUNT * 8 + 16;
+           (size_t)Cols<D>::kStages * kAuxBytes + kSelBytes + 2 * sizeof(Unit) + B_COUNT * 8 + 16;
 }
 static_assert(smem_bytes<64>() <= 232448 && smem_bytes<128>() <= 232448, "shared memory per CTA");
 }  // namespace dkv
@@ -217,8 +221,9 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     uint8_t *sv = sk + kKBufs * kKTile;        // [buffer]
     uint8_t *sq = sv + kKBufs * kKTile;        // [stage] Q step tiles
     uint8_t *sg = sq + kStages * kQTile;       // [stage] dO step tiles
-    uint8_t *aux = sg + kStages * kQTile;      // [stage] -lse2, D
-    Unit *units = (Unit *)(aux + kStages * kAuxBytes);   // [2]
+    uint8_t *aux = sg + kStages * kQTile;      // [stage] -lse2, -D
+    uint8_t *sel = aux + kStages * kAuxBytes;
+    Unit *units = (Unit *)(sel + kSelBytes);   // [2]
     uint64_t *bars = (uint64_t *)(units + 2);
     uint32_t *tmem_slot = (uint32_t *)(bars + B_COUNT);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
@@ -245,8 +250,9 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             const int r = i / 8 % (kBlk - used) + used, b = i / 8 / (kBlk - used);
             *reinterpret_cast<uint4 *>(sq + b * kQPanel + r * 128 + i % 8 * 16) = make_uint4(0, 0, 0, 0);
         }
-        fence_proxy_async_smem();
     }
+    if (tid < 2 * kKT) reinterpret_cast<uint4 *>(sel)[tid] = tid < kKT ? make_uint4(0x3f803f80u, 0x3f80u, 0, 0) : make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
     if (warp == kSoft + 1) {
         tmem_alloc(smem_u32(tmem_slot), 512);
         tmem_relinquish();
@@ -315,7 +321,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                         tma_load_3d(gb + p * kQPanel, &gmap, 64 * p, un.g * a.group, tok, fb);
                     }
                     bulk_load(ab, a.neg_lse2 + at, kBlk * 4, fb);
-                    bulk_load(ab + kBlk * 4, a.dsum + at, kBlk * 4, fb);
+                    bulk_load(ab + kBlk * 4, a.dsum + 4 * at, kBlk * 16, fb);
                     ++issued;
                     st.next(j + 1 < un.steps);
                     if (j == 0) {   // (K's and V's places may be free later than the first step's)
@@ -366,7 +372,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 }
                 umma_commit_warp(bar(B_KFREE + kb));
             } else if (warp == kSoft + 3) {
-                const uint64_t dV = umma_desc_sw128(smem_u32(sv + kb * kKTile), 16, 1024);
+                const uint64_t dV = umma_desc_sw128(smem_u32(sv + kb * kKTile), 16, 1024), ds = umma_desc_plain(smem_u32(sel), kKT * 16, 128);
                 ok = D == 64 ? wait_w(B_VFULL + kb, kph, 166) : wait_w(B_VT, n & 1, 166);
                 for (int j = 0; ok && j < un.steps; ++j, ++u) {
                     const int s = u % kStages;
@@ -376,6 +382,8 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     const uint64_t dg = umma_desc_sw128(smem_u32(sg + s * kQTile), 16, 1024);
                     if constexpr (D == 128) umma_bf16_ts_k128_warp<kQPanel>(tmem + kColDP + 64 * (u % kDPs), tmem + kColV, dg, idS);
                     else umma_bf16_ss_k64_warp(tmem + kColDP + 64 * (u % kDPs), dV, dg, idS);
+                    // (the eight further values that the zeros meet are the first again)
+                    umma_bf16_ss_k16_add_warp(tmem + kColDP + 64 * (u % kDPs), ds, umma_desc_plain(smem_u32(aux + s * kAuxBytes + kBlk * 4), 0, 128), idS);
                     umma_commit_warp(bar(B_SFULL + u % kBuf));
                 }
                 if (D == 64) umma_commit_warp(bar(B_VFREE + kb));
@@ -484,7 +492,6 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     fence_proxy_async_smem();
                 }
                 const float4 *la = reinterpret_cast<const float4 *>(aux + s * kAuxBytes) + 8 * ch;
-                const float4 *da = reinterpret_cast<const float4 *>(aux + s * kAuxBytes + kBlk * 4) + 8 * ch;
                 const bool any_blind = __any_sync(0xffffffffu, blind);
                 constexpr int kCols = kGroups == 2 ? 16 : 32;   // row columns at a time (96 registers a thread with two groups)
                 uint32_t pk[16], dk[16];
@@ -499,12 +506,12 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                         __syncwarp();
                         mbar_arrive_warp(bar(B_DPFREE + u % kDPs));
                     }
-                    // two row columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D), both rounded to the
-                    // MMAs' operand type (half a step, 2^-9 of a value on average)
+                    // two row columns per packed instruction: P = exp2(S c - lse2), dS = P (dP - D), where dP has lost D
+                    // already, both rounded to the MMAs' operand type (half a step, 2^-9 of a value on average)
                     auto column_pairs = [&](auto masked) {
 #pragma unroll
                         for (int i4 = 0; i4 < kCols / 4; ++i4) {
-                            const float4 l4 = la[h / 4 + i4], d4 = da[h / 4 + i4];
+                            const float4 l4 = la[h / 4 + i4];
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
                                 const int i = 4 * i4 + 2 * k;
@@ -512,10 +519,8 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                                 f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c2,
                                                  k ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y)), x0, x1);
                                 float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-                                const uint64_t e = f2_sub(f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1])),
-                                                          k ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y));
                                 float d0, d1;
-                                f2_unpack(f2_mul(f2_pack(p0, p1), e), d0, d1);
+                                f2_unpack(f2_mul(f2_pack(p0, p1), f2_pack(__uint_as_float(dr[i]), __uint_as_float(dr[i + 1]))), d0, d1);
                                 if (decltype(masked)::value) {
                                     p0 = (vis >> (h + i)) & 1u ? p0 : 0.f;
                                     p1 = (vis >> (h + i + 1)) & 1u ? p1 : 0.f;
@@ -963,7 +968,9 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
             if (ch == 0 && un.sub >= 0 && row / kBlk * a.block_tokens < un.ntok) {
                 const size_t at = ((size_t)un.g * a.num_subs + un.sub) * kBlk + row;
                 a.neg_lse2[at] = nlrow;
-                a.dsum[at] = drow;
+                // -D as three bf16, which hold its 24 bits
+                const float x = -drow, x1 = x - __bfloat162float(__float2bfloat16_rn(x)), x2 = x1 - __bfloat162float(__float2bfloat16_rn(x1));
+                reinterpret_cast<uint4 *>(a.dsum)[at] = make_uint4(pack_bf16x2(x, x1), pack_bf16x2(x2, 0.f), 0, 0);
             }
             const uint64_t nl2 = f2_pack(nlrow, nlrow), d2 = f2_pack(drow, drow);
             for (int u = 0; ok && u < un.steps; ++u, ++c) {

@@ -27,6 +27,18 @@ __device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t smem_addr, uint32_t
     return d;
 }
 
+// K-major without swizzle: core matrices of 8 rows by 16 bytes (rows 16 bytes apart), sbo apart along the rows and lbo
+// apart along K.
+__device__ __forceinline__ uint64_t umma_desc_plain(uint32_t smem_addr, uint32_t lbo_bytes, uint32_t sbo_bytes)
+{
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)((lbo_bytes >> 4) & 0x3FFFu) << 16;
+    d |= (uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32;
+    d |= (uint64_t)1 << 46;   // descriptor version of sm_100-family tcgen05
+    return d;
+}
+
 // kind::f16 instruction descriptor: bf16 A and B, fp32 accumulator, A K-major, B K-major or MN-major.
 __host__ __device__ constexpr uint32_t umma_idesc_bf16(int M, int N, bool b_mn_major)
 {
@@ -157,6 +169,13 @@ __device__ __forceinline__ void umma_bf16_ss_k128_warp(uint32_t d_tmem, uint64_t
             : "memory");
 }
 // Four K-steps (64 elements, one panel) of a K-major product, D = A[smem] . B[smem]^T.
+__device__ __forceinline__ void umma_bf16_ss_k16_add_warp(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc)
+{
+    asm volatile(
+        "{\n .reg .pred e, t;\n elect.sync _|e, 0xffffffff;\n setp.eq.u32 t, 0, 0;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, t;\n}" ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc)
+        : "memory");
+}
 __device__ __forceinline__ void umma_bf16_ss_k64_warp(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc)
 {
     asm volatile(
