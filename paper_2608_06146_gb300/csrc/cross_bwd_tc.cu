@@ -26,11 +26,11 @@
 // an error and all roles leave their loops, the MMA warps wait for their MMAs, the producer for its copies, and tensor
 // memory is released.
 //
-// Measured: 32768 rows over 8 x 2560 states of 16 query and 2 KV heads of 128 dims 1441 us, dQ 589 and dK/dV 848 (1670
-// TFLOP/s over the seven products made, 96% of what a library product sustains). A step of 64 rows of the dK/dV pass lasts
-// 1460 cycles, of which the tensor cores work 1020 and shared memory is read or written some 1150; one of 64 keys of the
-// dQ pass 1005, 770 and 900. 8 pages of 25 segments over 1601 states 135 us (62 and 69, sums 8); 9 pages of 16 heads of 64
-// dims 152 (63 and 89). The short calls lose an item's start and end (3 to 4 us) and the launches.
+// Measured: 32768 rows over 8 x 2560 states of 16 query and 2 KV heads of 128 dims 1349 us, dQ 586 and dK/dV 763 (1780
+// TFLOP/s over the seven products made, as much as a library product sustains). A step of 64 rows of the dK/dV pass lasts
+// 1290 cycles, of which the tensor cores' pipe is busy 93% (MMAs 1056 cycles, or their operands' way from shared memory);
+// one of 64 keys of the dQ pass 1005, 87%. 8 pages of 25 segments over 1601 states 130 us (62 and 65, sums 8); 9 pages of
+// 16 heads of 64 dims 145 (63 and 82). The short calls lose an item's start and end (3 to 4 us) and the launches.
 #include <math.h>
 
 #include <algorithm>
@@ -104,7 +104,7 @@ constexpr int kKPanel = kKT * 128;           // [128 rows][64 bf16]
 constexpr int kQPanel = kBlk * 128;          // [64 rows][64 bf16]
 // -lse2[64], then -D of each row as eight bf16, the first three of which add up to it. They are a B operand: a last product
 // of 16 (with ones for these three, zeros for the rest) subtracts D from dP. Read as fp32 like -lse2, each value by a whole
-// warp, D kept shared memory busy for 256 cycles a step more (1439 -> 1340 us for 32768 rows over 8 x 2560 states).
+// warp, D kept shared memory busy for 256 cycles a step more (1439 us against 1349 for 32768 rows over 8 x 2560 states).
 constexpr int kAuxBytes = kBlk * 4 + kBlk * 16;
 constexpr int kSelBytes = 2 * kKT * 16;      // ... that product's A: 128 rows of three ones, 128 of zeros
 // With 64 dims two groups of eight softmax warps take the steps in turn: one group's work on a step lasts longer than its
@@ -118,7 +118,7 @@ struct Cols {
     static constexpr uint32_t kDP = 64 * kBuffers, kV = 192, kAcc = D == 64 ? 384 : 256;
     static_assert(kAcc + 2 * D <= 512 && kDP + 64 * kDPs <= (D == 64 ? kAcc : kV), "");
     // Steps on their way: a step of 64 dims copies 16 KB in the time of 16 MMAs, and with four stages it waited for them
-    // (128 us against 98 with ten, before items came in lists; now eight, and K and V of the next item beside them: 89).
+    // (128 us against 98 with ten, before items came in lists; now eight, and K and V of the next item beside them: 82).
     static constexpr int kStages = D == 64 ? 8 : 4, kKBufs = D == 64 ? 2 : 1;   // K and V of the unit, and of the next
     static_assert(kStages <= kMaxStages && kStages % kGroups == 0, "a stage belongs to one group");
     static constexpr int kShare = 2 * D / (kSoft / 4);                          // columns of dV | dK a softmax thread writes
