@@ -108,8 +108,8 @@ constexpr int kQPanel = kBlk * 128;          // [64 rows][64 bf16]
 constexpr int kAuxBytes = kBlk * 4 + kBlk * 16;
 constexpr int kSelBytes = 2 * kKT * 16;      // ... that product's A: 128 rows of three ones, 128 of zeros
 // With 64 dims two groups of eight softmax warps take the steps in turn: one group's work on a step lasts longer than its
-// 16 MMAs (98 us against 110 for 9 pages of 16 heads, both before items came in lists). With 128 dims, 24 MMAs, one group with all registers is faster
-// (937 us against 983 for 32768 rows over 8 x 2560 states, before items came in lists).
+// 16 MMAs (98 us against 110 for 9 pages of 16 heads, both before items came in lists). With 128 dims, 24 MMAs, one group
+// with all registers is faster (937 us against 983 for 32768 rows over 8 x 2560 states, before the lists too).
 // Tensor memory: S buffers, dP buffers, V as an A operand (128 dims; with 64 it is read from shared memory), dV and dK.
 template <int D>
 struct Cols {
@@ -383,7 +383,8 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     if constexpr (D == 128) umma_bf16_ts_k128_warp<kQPanel>(tmem + kColDP + 64 * (u % kDPs), tmem + kColV, dg, idS);
                     else umma_bf16_ss_k64_warp(tmem + kColDP + 64 * (u % kDPs), dV, dg, idS);
                     // (the eight further values that the zeros meet are the first again)
-                    umma_bf16_ss_k16_add_warp(tmem + kColDP + 64 * (u % kDPs), ds, umma_desc_plain(smem_u32(aux + s * kAuxBytes + kBlk * 4), 0, 128), idS);
+                    const uint64_t db = umma_desc_plain(smem_u32(aux + s * kAuxBytes + kBlk * 4), 0, 128);
+                    umma_bf16_ss_k16_add_warp(tmem + kColDP + 64 * (u % kDPs), ds, db, idS);
                     umma_commit_warp(bar(B_SFULL + u % kBuf));
                 }
                 if (D == 64) umma_commit_warp(bar(B_VFREE + kb));
@@ -643,7 +644,8 @@ constexpr int kReaders = 11;       // softmax and issuing warps
 template <int D>
 constexpr size_t smem_bytes()
 {
-    return 1024 + 3 * (size_t)(D / 64) * kQPanel + 2 * (size_t)stages<D>() * (D / 64) * kKPanel + 2 * sizeof(Unit) + 16 + B_COUNT * 8 + 32 + 2 * kQT * 4;
+    return 1024 + 3 * (size_t)(D / 64) * kQPanel + 2 * (size_t)stages<D>() * (D / 64) * kKPanel + 2 * sizeof(Unit) + 16 +
+           B_COUNT * 8 + 32 + 2 * kQT * 4;
 }
 static_assert(smem_bytes<128>() <= 232448 && smem_bytes<64>() <= 232448, "shared memory per CTA");
 }  // namespace dqp

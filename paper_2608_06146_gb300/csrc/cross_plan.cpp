@@ -619,11 +619,13 @@ extern "C" padoc_status padoc_cross_workspace_size(const padoc_cross_plan *info,
 
 extern "C" padoc_status padoc_cross_bwd_workspace_size(const padoc_cross_plan *info, size_t *bytes)
 {
-    if (!info || !bytes || !info->cfg.backward || info->num_dq_slots < 0 || info->num_subs < 0 || info->num_dkv_slots < 0) return PADOC_ERR_INVALID_ARGUMENT;
+    if (!info || !bytes || !info->cfg.backward || info->num_dq_slots < 0 || info->num_subs < 0 || info->num_dkv_slots < 0)
+        return PADOC_ERR_INVALID_ARGUMENT;
     // -lse2 and D (bf16: four words), [Hkv][subs][64] each, partial dq [slots][128][d], partial dv and dk [slots][128][2 d], fp32
     const bool f32 = info->cfg.dtype == PADOC_DTYPE_F32;
     const size_t stats = (size_t)info->num_subs * info->cfg.num_kv_heads * PADOC_CROSS_BLOCK;
     const size_t rows = (size_t)info->num_dq_slots * (PADOC_CROSS_DQ_BLOCKS * PADOC_CROSS_BLOCK);
-    *bytes = ((f32 ? 2 : 5) * stats + rows * info->cfg.head_dim + (size_t)info->num_dkv_slots * PADOC_CROSS_KEY_TILE * 2 * info->cfg.head_dim) * sizeof(float);
+    const size_t keys = (size_t)info->num_dkv_slots * PADOC_CROSS_KEY_TILE * 2;
+    *bytes = ((f32 ? 2 : 5) * stats + (rows + keys) * info->cfg.head_dim) * sizeof(float);
     return PADOC_OK;
 }

@@ -19,8 +19,9 @@
 // their MMAs, the producer for its copies, and tensor memory is released.
 //
 // What bounds it: with 128 dims the MMAs and, over a long call, the chip's power (32768 rows over 8 x 2560 states of 16
-// query heads: 450 us, 1530 TFLOP/s, 88% of what a library product of this type sustains; a step of both tiles 1.40 us,
-// 1.23 of them without any softmax). With 64 dims the softmax: a key costs half the MMAs and the same exponentials and
+// query heads: 450 us, 1530 TFLOP/s, 88% of what a library product of this type sustains; a step of both tiles 1.40 to 1.5 us,
+// 1.23 of them without any softmax: the MMAs take 2048 cycles, and 2560 with their operands' way from shared memory, where
+// Q is read for each half of the keys). With 64 dims the softmax: a key costs half the MMAs and the same exponentials and
 // conversions (1.27 us a step of two CTAs, 0.74 without; 9 pages of 16 heads 57 us). One CTA with two tiles took 63 us
 // there, sixteen softmax warps 75. Few steps an item: its start and end, some 3 us. Pairs of CTAs that share K and V by
 // cta_group::2 were slower with 128 dims (434 -> 459 us, one more hand-over a step).
@@ -217,7 +218,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
                 Unit u = {0, 0, 0, 0, 0, 0, -1, 0};
                 if (n >= 2 && !wait(C::B_UEMPTY + (n & 1), ((n >> 1) - 1) & 1, 124)) break;
                 if (more) {
-                    u = {item.tok, item.ntok, item.k0, item.nk, item.g, item.slot, (item.nk + kKT - 1) / kKT, C::kTiles == 2 && item.ntok > tile_tokens};
+                    u = {item.tok, item.ntok, item.k0, item.nk, item.g, item.slot, (item.nk + kKT - 1) / kKT,
+                         C::kTiles == 2 && item.ntok > tile_tokens};
                     if (a.ctas && (more = ++x < xe)) item = a.units[x];   // (a list's next item is known at once)
                 }
                 units[n & 1] = u;
