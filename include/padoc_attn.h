@@ -57,7 +57,8 @@ extern "C" {
  * merge key list to the decode plan (padoc_decode_plan.off_merge_keys, num_merge_keys). 5 adds the
  * loop's step runner (padoc_mpd_runner_*). 6 adds padoc_mpd_step.off_first_blocks and stores the
  * split-K partials in bf16 (the decode workspace's size changes with it). The rotary calls, the block
- * copies and padoc_mpd_fork_stream .. padoc_mpd_resize only add symbols and leave the number. */
+ * copies, padoc_mpd_fork_stream .. padoc_mpd_resize and the cross attention calls only add symbols and
+ * leave the number. */
 #define PADOC_ATTN_VERSION 6
 
 /* A CUDA stream handle; identical to cudaStream_t. */
@@ -952,8 +953,8 @@ typedef struct {
     int32_t num_segments;
     int32_t query_rows;      /* query rows the segments reach to (their largest q_begin + q_len) */
     int32_t key_rows;        /* key rows they reach to */
-    int32_t few;             /* forward: > 0: items of few rows, each by a cluster of that many CTAs; 0: of 256 packed rows */
-    int32_t unit_rows;       /* packed (token, query head) rows of a forward item at most: 16, 32 or 256 */
+    int32_t few;             /* forward: > 0: items of few rows, each by a cluster of that many CTAs; 0: of 128 or 256 rows */
+    int32_t unit_rows;       /* packed (token, query head) rows of a forward item at most: 16, 32, 128 or 256 */
     int32_t num_units;       /* forward: work items */
     int32_t num_ctas;        /* CTAs that have a list of items each; 0: a CTA an item, taken as SMs get free */
     int32_t num_merges;      /* row blocks whose key range is split over several items, or empty */

@@ -47,8 +47,8 @@ int *padoc_device_error_word()
 namespace {
 
 // The last few 2-D maps this thread encoded, by their arguments: a decoding loop encodes the same
-// pool's maps every step, and an encoding is a pure function of its arguments. A backward takes ten, a cross attention and its
-// gradients as many.
+// pool's maps every step, and an encoding is a pure function of its arguments. A backward takes ten, a
+// cross attention and its gradients as many.
 constexpr int kTmaps = 32;
 struct TmapKey {
     int dtype;

@@ -1561,13 +1561,13 @@ def padoc_build_cross_plan(segments, cfg: padoc_cross_config, out=None):
     """The plan of segments (q_begin, q_len, k_begin, k_len), in ascending order of q_begin. Returns (plan blob int32,
     padoc_cross_plan); ``out`` as in padoc_build_decode_plan."""
     lib, a, info = load_library(), _cross_segments(segments), padoc_cross_plan()
-    buf = np.zeros(16384 + 24 * a.shape[0], np.int32) if out is None else out   # (room enough saves planning twice)
+    buf = np.empty(16384 + 24 * a.shape[0], np.int32) if out is None else out   # (room enough saves planning twice)
     for _ in range(2):
         st = lib.padoc_build_cross_plan(a.ctypes.data, a.shape[0], ctypes.byref(cfg), buf.ctypes.data_as(_i32p), buf.size,
                                         ctypes.byref(info))
         if st != 6 or info.plan_ints <= buf.size:
             break
-        buf = np.zeros(int(info.plan_ints), np.int32)
+        buf = np.empty(int(info.plan_ints), np.int32)
     _check("padoc_build_cross_plan", st)
     return buf[:info.plan_ints], info
 
