@@ -148,10 +148,11 @@ float cut_ends(const std::vector<Chunk> &chunks, const std::vector<Piece> &whole
             const int32_t parts = parts_of(i, p);
             if (parts == 1) continue;
             sum -= time[i];
-            time[i] = ceil_div(whole[i].steps, parts) * chunks[whole[i].chunk].step_cost + k.start + k.part;
-            time.insert(time.end(), parts - 1, time[i]);
+            const float part = ceil_div(whole[i].steps, parts) * chunks[whole[i].chunk].step_cost + k.start + k.part;
+            time[i] = part;
+            time.insert(time.end(), parts - 1, part);
             cuts += parts;
-            sum += parts * time[i];
+            sum += parts * part;
         }
         const float join = k.merge + k.read * (float)cuts;
         if (!cuts || (float)(sum / lanes) + join >= best) break;   // (more parts cost more)
