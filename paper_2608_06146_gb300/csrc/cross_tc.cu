@@ -19,8 +19,8 @@
 // their MMAs, the producer for its copies, and tensor memory is released.
 //
 // What bounds it: with 128 dims the MMAs and, over a long call, the chip's power (32768 rows over 8 x 2560 states of 16
-// query heads: 450 us, 1530 TFLOP/s, 88% of what a library product of this type sustains; a step of both tiles 1.40 to 1.5 us,
-// 1.23 of them without any softmax: the MMAs take 2048 cycles, and 2560 with their operands' way from shared memory, where
+// query heads: 428 us, 1605 TFLOP/s, 93% of what a library product of this type sustains; a step of both tiles 1.40 us, 1.23
+// of them without any softmax: the MMAs take 2048 cycles, and 2560 with their operands' way from shared memory, where
 // Q is read for each half of the keys). With 64 dims the softmax: a key costs half the MMAs and the same exponentials and
 // conversions (1.27 us a step of two CTAs, 0.74 without; 9 pages of 16 heads 57 us). One CTA with two tiles took 63 us
 // there, sixteen softmax warps 75. Few steps an item: its start and end, some 3 us. Pairs of CTAs that share K and V by
@@ -131,6 +131,9 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     padoc_cross_unit item = {};
     if (warp == kSoft && lane == 0) {
         x = (int)blockIdx.x;
+        tma_prefetch_desc(&qmap);
+        tma_prefetch_desc(&kmap);
+        tma_prefetch_desc(&vmap);
         pdl_wait_prerequisite();   // nothing in global memory is touched before (the other roles' work follows from this)
         if (a.ctas) {
             xe = a.ctas[x + 1];
@@ -183,9 +186,6 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant_
     if (warp >= kSoft) {
         if (warp == kSoft && lane == 0) {
             // ------------------------------------------------------------ TMA producer
-            tma_prefetch_desc(&qmap);
-            tma_prefetch_desc(&kmap);
-            tma_prefetch_desc(&vmap);
             auto wait = [&](int b, uint32_t parity, int site) {
                 return wait_or_abort(bar(b), parity, a.err, site, abort_flag);
             };
