@@ -235,15 +235,15 @@ struct Built {
     padoc_cross_plan info;
 };
 
-// The dk/dv pass's items: key tiles, or parts of their steps, in a list for each CTA. Costs in steps (0.87 us with 128
-// dims, 0.6 with 64). More tiles than CTAs: whole ones, those of the last round cut where that pays, longest first to the
-// CTA that is free first. They all begin with a segment's first rows, which the CTAs thus fetch at about the same time:
-// equal runs of all steps, in which every CTA begins elsewhere, took 1750 us instead of 1640 for 320 tiles of 512 steps.
-// Else equal runs, where they are shorter (120 tiles of up to 184 steps, 9510 in all, by clusters of CTAs 82 us, in runs
-// 69 and their sums 8).
+// The dk/dv pass's items: key tiles, or parts of their steps, in a list for each CTA. Costs in steps (0.7 us with 128
+// dims, 0.6 with 64, where cheaper cuts were better: 2 pages of 1500 rows over 400 states 19.5 -> 17.2 us). More tiles
+// than CTAs: whole ones, those of the last round cut where that pays, longest first to the CTA that is free first. They
+// all begin with a segment's first rows, which the CTAs thus fetch at about the same time: equal runs of all steps, in
+// which every CTA begins elsewhere, took 1750 us instead of 1640 for 320 tiles of 512 steps. Else equal runs, where they
+// are shorter (120 tiles of up to 184 steps, 9510 in all, by clusters of CTAs 82 us, in runs 69 and their sums 8).
 void plan_dkv(Built &b, int hkv, int lanes, int head_dim)
 {
-    const Costs k = head_dim == 128 ? Costs{3.f, 1.5f, 5.f, 0.02f, 1.f, 1, 4} : Costs{4.f, 2.f, 10.f, 0.02f, 1.f, 1, 8};
+    const Costs k = head_dim == 128 ? Costs{5.f, 2.f, 5.f, 0.02f, 1.f, 1, 4} : Costs{4.f, 1.f, 5.f, 0.01f, 1.f, 1, 4};
     std::vector<Chunk> chunks;
     std::vector<Piece> pieces;
     std::vector<float> cost;

@@ -1,4 +1,4 @@
-"""Cross attention's host side: the planner against a plain count, the refusals, and the checker itself (its gradients
+"""Cross attention's host side: the planner against a plain count, the refusals, and the oracle itself (its gradients
 against differences and autograd)."""
 import ctypes
 import math
@@ -251,7 +251,7 @@ def test_calls_are_refused_before_any_launch(lib):
     assert fwd(i=nothing) == 0 and bwd(i=nothing, kn=0) == 0     # nothing to do
 
 
-def test_the_checker():
+def test_the_oracle():
     g = torch.Generator().manual_seed(1)
     segments = [(0, 3, 2, 5), (3, 2, 0, 0), (6, 4, 4, 6), (10, 1, 0, 1)]
     q = torch.randn(12, 4, 8, generator=g, dtype=torch.float64)

@@ -87,7 +87,7 @@ def check_backward(segments, hq, hkv, d, dtype, ctas=0, **kw):
     plan.bwd_workspace.fill_(255)
     plan.run_bwd(q, k, v, out, dout, lse, scale, dq, dk, dv)
     pa.padoc_check_device_errors()
-    # NaN of unnamed rows does not reach the checker either: it reads the segments' rows alone
+    # NaN of unnamed rows does not reach the oracle either: it reads the segments' rows alone
     gq, gk, gv = oc.backward(segments, q, k, v, dout, scale)
     bq, bk, bv = oc.backward_bounds(segments, q, k, v, out, dout, scale)
     within(dq, gq, bq, rows)
@@ -311,7 +311,7 @@ def test_nan_and_infinity_stay_with_the_rows_that_see_them(dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_gradients_against_differences(dtype):
-    # the forward's own change along a direction, in 64 bits' differences of the checker at the same inputs
+    # the forward's own change along a direction, in 64 bits' differences of the oracle at the same inputs
     segments, hq, hkv, d = [(0, 30, 0, 90), (30, 10, 50, 60)], 4, 2, 64
     q, k, v, dout = inputs(segments, hq, hkv, d, dtype, rows=40, keys=110)
     plan = CrossPlan(segments, hq, hkv, d, dtype, DEV, training=True)
