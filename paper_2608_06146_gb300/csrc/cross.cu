@@ -36,12 +36,13 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const padoc_cross_args
     const int unit_rows = a.unit_rows, per = unit_rows * W / 8;   // (multiples of 8)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w0 = W == 8 ? warp : 0;
     const int row = W == 8 ? (int)blockIdx.x % per : (int)blockIdx.x % per * 8 + warp;
+    pdl_launch_dependents();
+    // The plan too is read behind the wait: the forward lets this kernel start before it has itself waited for the one
+    // before it, which may have written the plan.
+    pdl_wait_prerequisite();
     const padoc_cross_merge m = a.merges[(int)blockIdx.x / per];
     int token, head;
-    const bool in = cross_row(a, m.tok, m.ntok, row, token, head);
-    pdl_launch_dependents();
-    pdl_wait_prerequisite();
-    if (!in) return;
+    if (!cross_row(a, m.tok, m.ntok, row, token, head)) return;
     const int n = (m.parts - w0 + W - 1) / W;   // this warp's parts: w0, w0 + W, ..
     auto at = [&](int i) { return (size_t)(m.slot + w0 + i * W) * unit_rows + row; };
     float acc[E], top = -INFINITY, sum = 0.f;

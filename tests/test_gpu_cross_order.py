@@ -1,0 +1,64 @@
+"""Cross attention behind the kernels before it in the stream: a plan that one of them writes, and one that lasts long."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_06146_gb300 import build as pbuild
+from paper_2608_06146_gb300 import padoc_attn as pa
+from paper_2608_06146_gb300.engine import CrossPlan
+
+pytestmark = pytest.mark.gpu
+DEV, BF16, F32 = "cuda:0", torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _build():
+    pbuild.build()
+    pa.load_library()
+
+
+def inputs(segments, hq, hkv, d, dtype, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    rows, keys = max(s[0] + s[1] for s in segments), max(s[2] + s[3] for s in segments)
+    new = lambda n, h: torch.randn((n, h, d), generator=g, device=DEV).to(dtype)   # noqa: E731
+    return new(rows, hq), new(keys, hkv), new(keys, hkv), new(rows, hq)
+
+
+@pytest.mark.parametrize("segments,hq,hkv,d,dtype", [
+    ([(0, 24, 0, 9001)], 16, 2, 128, BF16),                  # lists of items, joined parts
+    ([(0, 3, 0, 30_000)], 4, 4, 64, BF16),                   # few rows, joined parts
+    ([(0, 40, 0, 700), (40, 5, 0, 0)], 4, 1, 64, F32),       # fp32, joined parts, rows without keys
+    ([(0, 700, 0, 300), (700, 40, 300, 1000)], 16, 16, 64, BF16)])
+def test_a_plan_that_the_kernel_before_writes(segments, hq, hkv, d, dtype):
+    # the block copy lets the next kernel start before it has written anything, the plan's words last
+    plan = CrossPlan(segments, hq, hkv, d, dtype, DEV, training=True)
+    q, k, v, dout = inputs(segments, hq, hkv, d, dtype)
+    want, wl = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+    grads = [torch.empty_like(t) for t in (q, k, v)]
+    plan.run(q, k, v, 0.1, want, wl)
+    plan.run_bwd(q, k, v, want, dout, wl, 0.1, *grads)
+    block = 2 * 16 * 128                                     # words
+    words, blocks = int(plan.info.plan_ints), 20_000
+    own = -(-words // block)
+    src, dst = (torch.zeros((blocks, 2, 16, 128), device=DEV) for _ in range(2))
+    src.view(torch.int32).view(-1)[(blocks - own) * block:][:words] = plan.plan_dev[:words]
+    there = dst.view(torch.int32).view(-1)[(blocks - own) * block:][:words]
+    spare = [torch.zeros((blocks, 2, 16, 128), device=DEV) for _ in range(2)]
+    to, of = pa.KvPools([(spare[0], dst)]), pa.KvPools([(spare[1], src)])
+    order = torch.arange(blocks, dtype=torch.int32, device=DEV)
+    for _ in range(3):
+        out, lse = torch.full_like(q, 77.0), torch.full_like(wl, 77.0)
+        got = [torch.full_like(t, 77.0) for t in grads]
+        there.zero_()
+        torch.cuda.synchronize()
+        pa.padoc_copy_kv_blocks(to, order, order, of)
+        pa.padoc_cross_attn(plan.info, there, q, k, v, 0.1, out, lse, plan.workspace)
+        torch.cuda.synchronize()
+        there.zero_()
+        torch.cuda.synchronize()
+        pa.padoc_copy_kv_blocks(to, order, order, of)
+        pa.padoc_cross_attn_bwd(plan.info, there, q, k, v, out, dout, lse, 0.1, *got, plan.bwd_workspace)
+        pa.padoc_check_device_errors()
+        assert np.array_equal(there.cpu().numpy(), plan.plan_dev[:words].cpu().numpy())
+        assert torch.equal(out, want) and torch.equal(lse, wl)
+        assert all(torch.equal(a, b) for a, b in zip(got, grads))
