@@ -1043,9 +1043,10 @@ typedef struct {
 
 /* Gradients of padoc_cross_attn for an upstream gradient dout [query_rows][Hq][head_dim], with the forward's out and
  * lse: dq of the segments' rows (others are not written), dk and dv of every key row, summed in a fixed order over all
- * segments and query heads that see it (0 where none does). The plan must have been built with cfg.backward. Where
- * key ranges overlap, a dout that is not finite may reach the gradients of up to 127 keys next to those its row sees. No
- * output overlaps an input or another output. workspace and errors as above. */
+ * segments and query heads that see it (0 where none does). The plan must have been built with cfg.backward. A row
+ * whose q or dout is not finite makes dk and dv of the keys that it sees NaN or infinite (where key ranges overlap, in all
+ * dims), those of no others; a row whose lse is -inf has no gradients. No output overlaps an input or another output.
+ * workspace and errors as above. */
 padoc_status padoc_cross_attn_bwd(const padoc_cross_plan *info, const int32_t *plan_dev, const padoc_cross_rows *rows,
                                   const void *out, const void *dout, const float *lse, float scale,
                                   const padoc_cross_grads *grads, void *workspace, size_t workspace_bytes,

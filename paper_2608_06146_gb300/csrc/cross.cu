@@ -443,14 +443,29 @@ __global__ void __launch_bounds__(256) cross_dkv_simt_kernel(const padoc_cross_a
             S::dots(sk, sq, s);
             S::dots(sv, sg, dp);
             const size_t at = ((size_t)g * a.num_subs + c.sub + b) * kB;
+            // Rows whose q or dO is not finite, where a key does not see them: as 0 x NaN would reach the key's sums all the
+            // same, the rows become zeros and the weights of the keys that see them NaN. Such a row's lse or D is not
+            // finite; where nothing is left of its scores (lse = -inf, finite D) its weights stay zeros.
+            const bool some_blind = c.k0 > k0 || c.k0 + c.nk < k0 + nk;
+            if (some_blind) {
+                __syncthreads();   // (both products have read the rows)
+                const int r = threadIdx.x >> 2;
+                if (!isfinite(a.neg_lse2[at + r]) || !isfinite(a.dsum[at + r]))
+                    for (int e = threadIdx.x & 3; e < D / 4; e += 4)
+                        *reinterpret_cast<float4 *>(sq + r * S::P + 4 * e) = *reinterpret_cast<float4 *>(sg + r * S::P + 4 * e) =
+                            make_float4(0.f, 0.f, 0.f, 0.f);
+                __syncthreads();
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int r = tx + 16 * j;
                 const float l = a.neg_lse2[at + r], d = a.dsum[at + r];
+                const bool odd_nan = some_blind && (isnan(l) || !isfinite(d));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const bool sees = k0 + 4 * ty + i >= c.k0 && k0 + 4 * ty + i < c.k0 + c.nk;
-                    const float p = sees ? exp2f(fmaf(s[i][j], a.scale_log2, l)) : 0.f;   // (rows past the segment's: l = -inf)
+                    // (rows past the segment's: l = -inf)
+                    const float p = !sees ? 0.f : odd_nan ? NAN : exp2f(fmaf(s[i][j], a.scale_log2, l));
                     sp[(4 * ty + i) * S::PS + r] = p;
                     sd[(4 * ty + i) * S::PS + r] = sees ? p * (dp[i][j] - d) : 0.f;
                 }

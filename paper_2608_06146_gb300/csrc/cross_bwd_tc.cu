@@ -15,7 +15,8 @@
 //
 // Masks are needed at ends only: where a segment's keys (dQ) or rows (dK/dV) end inside a step, the weights past the end
 // become 0 and the operand rows there zeros, because what lies behind may be anything; and keys of a tile that the
-// step's segment does not see (key ranges that overlap) get weights 0.
+// step's segment does not see (key ranges that overlap) get weights 0. Rows of such a segment that are not finite get zeros
+// as operands and NaN as the weights of the keys that see them.
 //
 // A step is bound by its chain S -> softmax -> accumulation -> S more than by its MMAs, so S, dP and the accumulating
 // MMAs are issued by a warp each; P and dS share S's columns, so dP's buffer is free as soon as it is read; waits and
@@ -477,6 +478,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 // keys of the tile that the segment does not see
                 const int key = un.k0 + row;
                 const bool blind = key < st.c.k0 || key >= st.c.k0 + st.c.nk;
+                const bool some_blind = __any_sync(0xffffffffu, st.c.k0 > un.k0 || st.c.k0 + st.c.nk < un.k0 + un.nk);
                 if (!(ok = wait_w(B_QFULL + s, (u / kStages) & 1, 171) && wait_w(B_SFULL + sb, (u / kBuf) & 1, 170))) break;
                 tc_fence_after();
                 for (int i = 1; i <= kGroups; ++i) st.next(j + i < un.steps);
@@ -493,7 +495,6 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     fence_proxy_async_smem();
                 }
                 const float4 *la = reinterpret_cast<const float4 *>(aux + s * kAuxBytes) + 8 * ch;
-                const bool any_blind = __any_sync(0xffffffffu, blind);
                 constexpr int kCols = kGroups == 2 ? 16 : 32;   // row columns at a time (96 registers a thread with two groups)
                 uint32_t pk[16], dk[16];
 #pragma unroll
@@ -535,7 +536,29 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                     };
                     if (partial) column_pairs(std::true_type{}); else column_pairs(std::false_type{});
                 }
-                if (any_blind) {
+                if (some_blind) {
+                    // Rows whose q or dO is not finite: 0 x NaN would reach the sums of the keys that do not see them, so their
+                    // operand rows become zeros and the weights of the keys that see them NaN. Such a row's lse or D is
+                    // not finite; where nothing is left of its scores (lse = -inf, finite D) its weights stay zeros.
+                    const int r = 32 * ch + lane;
+                    const uint8_t *stats = aux + s * kAuxBytes;
+                    const float l = reinterpret_cast<const float *>(stats)[r];
+                    const float d = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(stats + kBlk * 4 + r * 16) << 16);
+                    const uint32_t odd = __ballot_sync(0xffffffffu, r < rows && !(isfinite(l) && isfinite(d)));
+                    if (odd) {
+                        const uint32_t nan = __ballot_sync(0xffffffffu, r < rows && (isnan(l) || !isfinite(d)));
+                        for (int i = 0; i < 32; ++i)   // (the four warps of a column half write the same zeros)
+                            if (((odd >> i) & 1u) && lane < 16 * kPanels)
+                                *reinterpret_cast<uint4 *>((lane < 8 * kPanels ? sq : sg) + s * kQTile + (lane >> 3) % kPanels * kQPanel +
+                                                           (32 * ch + i) * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_smem();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t w = (((nan >> (2 * i)) & 1u) ? 0x7fffu : 0u) | (((nan >> (2 * i)) & 2u) ? 0x7fff0000u : 0u);
+                            pk[i] |= w;
+                            dk[i] |= w;
+                        }
+                    }
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         pk[i] = blind ? 0u : pk[i];
