@@ -231,7 +231,8 @@ class MaskedParallelLoop:
         self.last_info = None
         self.last_step = None
         self.last_stage = None
-        self.h2d_bytes = 0
+        self.h2d_bytes = 0                          # copied to the device by the last step, admission or move ...
+        self.cross_h2d_bytes = 0                    # ... and, for its plan, by the last cross_step
         self._runner = None
         self._states = np.zeros((0, 2), np.int32)   # each stream's key rows (first, number), by stream id
         self._step_ids = None
@@ -262,9 +263,9 @@ class MaskedParallelLoop:
         self._grow(to, n, stream)
         return offs, n
 
-    def _upload(self, parts, stream, to="_ints"):
+    def _upload(self, parts, stream, to="_ints", count="h2d_bytes"):
         """Copies int32 host arrays to the device (into the array ``to``) in one transfer, each starting on a
-        128-byte boundary; returns device views."""
+        128-byte boundary, and notes its bytes in ``count``; returns device views."""
         offs, n = self._room([a.size for a in parts], stream, to)
         b = self._turn & 1
         self._turn += 1
@@ -276,7 +277,7 @@ class MaskedParallelLoop:
         with torch.cuda.stream(stream):
             dev[:n].copy_(self._stage[b][:n], non_blocking=True)
         self._stage_free[b].record(stream)
-        self.h2d_bytes = 4 * n
+        setattr(self, count, 4 * n)
         return [dev[o:o + a.size] for a, o in zip(parts, offs)]
 
     def _check_rows(self, k_src, q_src, v_src, pos_src):
@@ -355,6 +356,7 @@ class MaskedParallelLoop:
             with torch.cuda.stream(stream):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
                 lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
+        self.cross_h2d_bytes = 0
         if ids.size == 0:
             return out, lse
         if ids.max() >= len(self._states):
@@ -371,7 +373,7 @@ class MaskedParallelLoop:
             cfg = pa.make_cross_config(q.shape[1], k.shape[1], q.shape[2], q.dtype)
             plan, info = pa.padoc_build_cross_plan(segments, cfg)
             self._cross_plan = None
-            self._upload([plan], stream, "_cross_ints")
+            self._upload([plan], stream, "_cross_ints", "cross_h2d_bytes")
             self._cross_plan = (key, info)
         info = self._cross_plan[1]
         self._grow("_cross_workspace", pa.padoc_cross_workspace_size(info), stream)

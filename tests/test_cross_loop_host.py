@@ -1,0 +1,47 @@
+"""CPU tests of the decoding loop's cross attention: what a call copies and what it leaves of the step's own counts. The
+loop runs over CPU tensors with the streams, events and launches of test_loop_host; the cross attention call is noted."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_06146_gb300 import padoc_attn as pa
+
+from .test_loop_host import BF16, D, HKV, HQ, cuda, make   # noqa: F401 (cuda: a fixture)
+
+
+@pytest.fixture
+def calls(cuda, monkeypatch):                              # noqa: F811
+    noted = []
+    monkeypatch.setattr(pa, "padoc_cross_attn", lambda info, plan, *a: noted.append((int(info.plan_ints), plan.data_ptr())))
+    return noted
+
+
+def _step(loop):
+    rows = [torch.zeros((64, h, D), dtype=BF16) for h in (HKV, HKV, HQ)]
+    ids, _, _ = loop.step(*rows, lambda i: i % 64, 0.1, torch.zeros((64, HQ, D), dtype=BF16), torch.zeros((64, HQ)))
+    return ids
+
+
+def _cross(loop, ids):
+    q, k = torch.zeros((len(ids), HQ, D), dtype=BF16), torch.zeros((1000, HKV, D), dtype=BF16)
+    return loop.cross_step(ids, q, k, k, 0.1)
+
+
+def test_the_steps_bytes_are_not_those_of_the_plan(calls):
+    loop = make(200)[0]
+    for i in range(3):
+        loop.set_states(i, 100 * i, 90)
+    ids = _step(loop)
+    step = loop.h2d_bytes
+    assert step > 0
+    _cross(loop, ids)
+    (words, _), = calls
+    assert loop.h2d_bytes == step and loop.cross_h2d_bytes == 4 * (-(-words // 32) * 32)
+    _cross(loop, ids)                                      # the plan is kept
+    assert loop.h2d_bytes == step and loop.cross_h2d_bytes == 0
+    loop.end_step(np.zeros(len(ids), np.int32), np.zeros(len(ids), np.uint8))
+    loop.set_states(0, 5, 6)
+    ids = _step(loop)
+    step = loop.h2d_bytes
+    _cross(loop, ids)
+    assert loop.h2d_bytes == step and loop.cross_h2d_bytes == 4 * (-(-calls[-1][0] // 32) * 32)
