@@ -347,8 +347,12 @@ class MaskedParallelLoop:
         """Cross attention of a step's tokens: row i of q [C][Hq][d] is stream ids[i]'s (in the step's order), k and v
         [rows][Hkv][d] are the encoder's (rows may lie apart). Streams that follow one another and see the same rows
         read them together. Returns (out [C][Hq][d], lse fp32 [C][Hq]). The plan is built and copied anew only when the
-        streams or their states have changed."""
+        streams or their states have changed. It lies in the loop's own memory, where a later call puts another, so a
+        call on a stream that is being captured is refused: capture a CrossPlan over the streams' segments instead."""
         stream = stream or torch.cuda.current_stream()
+        with torch.cuda.stream(stream):
+            if torch.cuda.is_current_stream_capturing():
+                raise ValueError("cross_step cannot be captured: capture a CrossPlan over the streams' segments")
         ids = np.asarray(ids, np.int64)
         if q.shape[0] != ids.size or (ids.size and ids.min() < 0):
             raise ValueError("q needs a row for each stream")

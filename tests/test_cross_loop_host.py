@@ -12,6 +12,7 @@ from .test_loop_host import BF16, D, HKV, HQ, cuda, make   # noqa: F401 (cuda: a
 @pytest.fixture
 def calls(cuda, monkeypatch):                              # noqa: F811
     noted = []
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     monkeypatch.setattr(pa, "padoc_cross_attn", lambda info, plan, *a: noted.append((int(info.plan_ints), plan.data_ptr())))
     return noted
 
@@ -45,3 +46,21 @@ def test_the_steps_bytes_are_not_those_of_the_plan(calls):
     step = loop.h2d_bytes
     _cross(loop, ids)
     assert loop.h2d_bytes == step and loop.cross_h2d_bytes == 4 * (-(-calls[-1][0] // 32) * 32)
+
+
+def test_a_captured_call_is_refused(calls, cuda, monkeypatch):   # noqa: F811
+    # a replay would run the captured grid over whatever plan the loop's later calls have left in its place
+    loop = make(200)[0]
+    loop.set_states(0, 0, 90)
+    ids = _step(loop)
+    _cross(loop, ids)
+    kept = loop._cross_plan
+    for asked in (cuda.current, cuda.side):
+        with monkeypatch.context() as m:
+            m.setattr(torch.cuda, "is_current_stream_capturing", lambda: cuda.current is asked)
+            with pytest.raises(ValueError, match="CrossPlan"):
+                loop.cross_step(ids, torch.zeros((len(ids), HQ, D), dtype=BF16), *[torch.zeros((1000, HKV, D), dtype=BF16)] * 2, 0.1,
+                                stream=asked)
+    assert len(calls) == 1 and loop._cross_plan is kept
+    _cross(loop, ids)
+    assert len(calls) == 2

@@ -1,11 +1,12 @@
-"""Cross attention behind the kernels before it in the stream: a plan that one of them writes, and one that lasts long."""
+"""Cross attention behind the kernels before it in the stream, and in a capture: a plan that the kernel before writes, a
+loop's step that is captured."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2608_06146_gb300 import build as pbuild
 from paper_2608_06146_gb300 import padoc_attn as pa
-from paper_2608_06146_gb300.engine import CrossPlan
+from paper_2608_06146_gb300.engine import CrossPlan, MaskedParallelLoop
 
 pytestmark = pytest.mark.gpu
 DEV, BF16, F32 = "cuda:0", torch.bfloat16, torch.float32
@@ -62,3 +63,31 @@ def test_a_plan_that_the_kernel_before_writes(segments, hq, hkv, d, dtype):
         assert np.array_equal(there.cpu().numpy(), plan.plan_dev[:words].cpu().numpy())
         assert torch.equal(out, want) and torch.equal(lse, wl)
         assert all(torch.equal(a, b) for a, b in zip(got, grads))
+
+
+def test_a_loops_captured_step_is_refused_and_a_plan_of_its_streams_captured():
+    loop = MaskedParallelLoop(100, 16, 2, 128, BF16, DEV)
+    q, k, v, _ = inputs([(0, 8, 0, 900)], 16, 2, 128, BF16)
+    loop.add_page(4, 2, False, k, v, np.arange(4), states=(100, 700))
+    ids, o, _ = loop.step(k, v, q, lambda i: i % 8, 0.1)
+    loop.end_step(num_streams=len(ids))
+    want, wl = loop.cross_step(ids, o, k, v, 0.1)
+    plan = CrossPlan([(0, len(ids), 100, 700)], 16, 2, 128, BF16, DEV)
+    out, lse = torch.zeros_like(want), torch.zeros_like(wl)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        plan.run(o, k, v, 0.1, out, lse)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        with pytest.raises(ValueError, match="CrossPlan"):
+            loop.cross_step(ids, o, k, v, 0.1, out, lse)
+        plan.run(o, k, v, 0.1, out, lse)
+    out.zero_()
+    loop.set_states(int(ids[0]), 0, 5)
+    loop.cross_step(ids, o, k, v, 0.1)            # another plan in the loop's memory
+    graph.replay()
+    torch.cuda.synchronize()
+    pa.padoc_check_device_errors()
+    assert torch.equal(out, want) and torch.equal(lse, wl)
