@@ -464,7 +464,9 @@ class MaskedParallelLoop:
         """Each stream's output event (forks, EOS) in step order; returns the new branches' ids."""
         new = self.mpd.end_step(num_forks, eos, num_streams)
         if len(new) and len(self._states) and self._step_ids is not None:   # branches see what their stream sees
-            for parent, child in zip(np.repeat(self._step_ids[:len(num_forks)], num_forks), new):
+            forks = np.asarray(num_forks)           # (one number for all streams, or one each)
+            ids = self._step_ids[:num_streams if forks.ndim == 0 else len(forks)]
+            for parent, child in zip(np.repeat(ids, forks), new):
                 self._give_states([int(child)], self.states_of(int(parent)))
         return new
 

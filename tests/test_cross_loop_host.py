@@ -64,3 +64,21 @@ def test_a_captured_call_is_refused(calls, cuda, monkeypatch):   # noqa: F811
     assert len(calls) == 1 and loop._cross_plan is kept
     _cross(loop, ids)
     assert len(calls) == 2
+
+
+def _layouts(cuda):                                        # noqa: F811
+    """A loop of three pages with a layout stream each, over states of their own."""
+    loop, rows = make(200, forks=0)
+    loop.set_states(0, 10, 20)
+    for i in (1, 2):
+        loop.add_page(20, 0, False, rows[1], rows[2], np.zeros(20, np.int32), states=(100 * i, 30 + i))
+    return loop
+
+
+def test_branches_of_every_layout_stream_at_once(calls, cuda):   # noqa: F811
+    # one number of forks for all streams, as the scheduler takes it
+    loop = _layouts(cuda)
+    ids = _step(loop)
+    new = loop.end_step(2, num_streams=len(ids))
+    assert [loop.states_of(i) for i in new] == [loop.states_of(p) for p in ids for _ in range(2)]
+    assert loop.states_of(new[-1]) == (200, 32)
