@@ -451,7 +451,12 @@ class MaskedParallelLoop:
             self._runner = pa.MpdRunner(self.mpd, self.cfg, self._pool)
         if self.rotary is not None and not self._runner.rotates(self.rotary, pos_src) and self.status()[1]:
             self._runner.set_rotary(self.rotary, pos_src)
-        n, ids = self._runner.step(k_src, v_src, q_src, row_of_stream, scale, out, lse, stream)
+        try:
+            n, ids = self._runner.step(k_src, v_src, q_src, row_of_stream, scale, out, lse, stream)
+        except pa.PadocError as e:
+            if e.status in (2, 4):   # past the planning: the step has begun, with the streams that the runner noted
+                self._step_ids = self._runner._ids
+            raise
         self.h2d_bytes = self._runner.upload_bytes
         self._step_ids = ids
         return n, ids

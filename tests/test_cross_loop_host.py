@@ -82,3 +82,41 @@ def test_branches_of_every_layout_stream_at_once(calls, cuda):   # noqa: F811
     new = loop.end_step(2, num_streams=len(ids))
     assert [loop.states_of(i) for i in new] == [loop.states_of(p) for p in ids for _ in range(2)]
     assert loop.states_of(new[-1]) == (200, 32)
+
+
+@pytest.mark.parametrize("status", [2, 4])
+def test_branches_of_a_step_that_could_not_be_launched(calls, cuda, status):   # noqa: F811
+    # past the planning such a step has begun and is the caller's to end: its branches see what its streams see
+    loop = _layouts(cuda)
+    ids = _step(loop)
+    loop.end_step(num_streams=len(ids))
+    loop.drop_page(0)
+
+    class Runner:
+        _ids = np.zeros(64, np.int32)
+
+        def step(self, *a):
+            begun, _ = loop.mpd.begin_step()
+            self._ids[:len(begun)] = begun
+            raise pa.PadocError("padoc_mpd_runner_step", status)
+    loop._runner = Runner()
+    with pytest.raises(pa.PadocError):
+        loop.run_step(None, None, None, None, 0.1, None, None)
+    new = loop.end_step([1, 2])
+    assert [loop.states_of(i) for i in new] == [(100, 31), (200, 32), (200, 32)]
+
+
+def test_a_refused_step_leaves_the_begun_ones_order(calls, cuda):   # noqa: F811
+    loop = _layouts(cuda)
+    ids = _step(loop)
+
+    class Runner:
+        _ids = np.full(64, 2, np.int32)
+
+        def step(self, *a):
+            raise pa.PadocError("padoc_mpd_runner_step", 1)   # a step is begun already
+    loop._runner = Runner()
+    with pytest.raises(pa.PadocError):
+        loop.run_step(None, None, None, None, 0.1, None, None)
+    new = loop.end_step([0, 1, 0])
+    assert [loop.states_of(i) for i in new] == [loop.states_of(ids[1])]
