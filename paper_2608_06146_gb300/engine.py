@@ -349,10 +349,13 @@ class MaskedParallelLoop:
         read them together. Returns (out [C][Hq][d], lse fp32 [C][Hq]). The plan is built and copied anew only when the
         streams or their states have changed. It lies in the loop's own memory, where a later call puts another, so a
         call on a stream that is being captured is refused: capture a CrossPlan over the streams' segments instead."""
-        stream = stream or torch.cuda.current_stream()
-        with torch.cuda.stream(stream):
-            if torch.cuda.is_current_stream_capturing():
-                raise ValueError("cross_step cannot be captured: capture a CrossPlan over the streams' segments")
+        if stream is None:
+            stream, capturing = torch.cuda.current_stream(), torch.cuda.is_current_stream_capturing()
+        else:
+            with torch.cuda.stream(stream):
+                capturing = torch.cuda.is_current_stream_capturing()
+        if capturing:
+            raise ValueError("cross_step cannot be captured: capture a CrossPlan over the streams' segments")
         ids = np.asarray(ids, np.int64)
         if q.shape[0] != ids.size or (ids.size and ids.min() < 0):
             raise ValueError("q needs a row for each stream")
