@@ -995,8 +995,10 @@ padoc_status padoc_cross_plan_size(const padoc_cross_segment *segments, int32_t 
 
 /* Builds the plan (host): the forward's items, heavier ones first, with key ranges split over the chip where there
  * are few rows, and for training the backward's. plan: (host) int32 [capacity_ints]; info: (host) summary.
- * Errors: INVALID_ARGUMENT (also segments out of order or sharing query rows, rows past 2^31 - 1024); UNSUPPORTED;
- * CAPACITY when capacity_ints is too small. */
+ * Errors: INVALID_ARGUMENT (also segments out of order or sharing query rows, rows past 2^31 - 1024); UNSUPPORTED (also
+ * more than 4096 query heads, key rows past 2^29, more than 2^24 blocks of 64 packed rows over all KV heads or, with
+ * backward, of (key tile, segment) pairs); CAPACITY when capacity_ints is too small (info then says what is needed), or
+ * when host memory runs out. */
 padoc_status padoc_build_cross_plan(const padoc_cross_segment *segments, int32_t num_segments,
                                     const padoc_cross_config *cfg, int32_t *plan, int64_t capacity_ints,
                                     padoc_cross_plan *info);
@@ -1007,8 +1009,9 @@ padoc_status padoc_cross_bwd_workspace_size(const padoc_cross_plan *info, size_t
 
 /* Query, key and value rows (device), e.g. slices of a projection's output: row r's query heads start at
  * q + r * q_stride elements, [Hq][head_dim], its key and value heads at k + r * k_stride and v + r * v_stride,
- * [Hkv][head_dim]. Bases and strides are multiples of 16 bytes, a stride at least a row's heads. Rows that no
- * segment names are not read, whatever they hold. */
+ * [Hkv][head_dim]. Bases and strides are multiples of 16 bytes, a stride at least a row's heads. Rows that no segment
+ * names may be fetched with their neighbours, so that all query_rows and key_rows must be readable, but reach no result,
+ * whatever they hold. */
 typedef struct {
     const void *q;
     const void *k;
@@ -1021,9 +1024,11 @@ typedef struct {
 } padoc_cross_rows;
 
 /* Cross attention of every segment: out [query_rows][Hq][head_dim] (device) in the rows' dtype, lse fp32
- * [query_rows][Hq] (device). Query rows in no segment are neither read nor written. The serving form for single
+ * [query_rows][Hq] (device). Query rows in no segment are not written. The serving form for single
  * tokens is the same call with a plan of the live streams' rows (few rows, long key ranges: split and joined).
  * bf16: head_dim 64 or 128 on the tensor cores, P rounded to bf16 before its product, fp32 sums; f32: fp32 throughout.
+ * A row whose scores are all -infinite has out 0 and lse -inf, as one without keys.
+ * The plan's words may be written by earlier work in the stream.
  * workspace: (device) >= padoc_cross_workspace_size bytes, 256-byte aligned (NULL when that is 0); calls that may run
  * at the same time need one each. Outputs overlap no input. Errors: INVALID_ARGUMENT, UNSUPPORTED,
  * WORKSPACE_TOO_SMALL, CUDA. */
@@ -1043,7 +1048,8 @@ typedef struct {
 
 /* Gradients of padoc_cross_attn for an upstream gradient dout [query_rows][Hq][head_dim], with the forward's out and
  * lse: dq of the segments' rows (others are not written), dk and dv of every key row, summed in a fixed order over all
- * segments and query heads that see it (0 where none does). The plan must have been built with cfg.backward. A row
+ * segments and query heads that see it (0 where none does). The plan must have been built with cfg.backward. bf16: P and dS
+ * are rounded to bf16 before their products, D = rowsum(dout * out) and all sums are fp32; f32: fp32 throughout. A row
  * whose q or dout is not finite makes dk and dv of the keys that it sees NaN or infinite (where key ranges overlap, in all
  * dims), those of no others; a row whose lse is -inf has no gradients. No output overlaps an input or another output.
  * workspace and errors as above. */

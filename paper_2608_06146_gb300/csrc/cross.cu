@@ -138,7 +138,9 @@ padoc_status merge_rows(const padoc_cross_args &a, int head_dim, bool pdl, cudaS
 // floats further apart than their length (a quarter warp's 16-byte reads of eight rows then meet no bank twice); a
 // thread keeps four rows by four columns of a 64 x 64 product, or four rows by D / 16 columns of a 64 x D one.
 // Meant for small pages: bound by the chain of a step (5 us with 64 dims: two products, three barriers), so keys are cut
-// until every SM has an item (368 rows of 4 heads over 260 states 33 -> 16 us, parts joined by a second kernel).
+// until every four SMs have an item of four such CTAs, in the dQ pass every two one of two (368 rows of 4 heads over 260
+// states 33 -> 14 us, parts joined by a second kernel). Where a segment has few rows, an item's other CTAs end at once and
+// their SMs stay idle: a token over 150001 states is 38 items with one CTA at work each.
 // ------------------------------------------------------------------------------------------------
 
 constexpr int kB = PADOC_CROSS_BLOCK;

@@ -27,11 +27,11 @@
 // an error and all roles leave their loops, the MMA warps wait for their MMAs, the producer for its copies, and tensor
 // memory is released.
 //
-// Measured: 32768 rows over 8 x 2560 states of 16 query and 2 KV heads of 128 dims 1349 us, dQ 586 and dK/dV 763 (1780
-// TFLOP/s over the seven products made, as much as a library product sustains). A step of 64 rows of the dK/dV pass lasts
-// 1290 cycles, of which the tensor cores' pipe is busy 93% (MMAs 1056 cycles, or their operands' way from shared memory);
-// one of 64 keys of the dQ pass 1005, 87%. 8 pages of 25 segments over 1601 states 130 us (62 and 65, sums 8); 9 pages of
-// 16 heads of 64 dims 145 (63 and 82). The short calls lose an item's start and end (3 to 4 us) and the launches.
+// Measured: 32768 rows over 8 x 2560 states of 16 query and 2 KV heads of 128 dims 1357 to 1387 us, by themselves dQ 586 and
+// dK/dV 781 (1735 to 1770 TFLOP/s over the seven products made, as much as a library product sustains). A step of 64 rows
+// of the dK/dV pass lasts 1290 cycles, of which the tensor cores' pipe is busy 93% (MMAs 1056 cycles, or their operands' way
+// from shared memory); one of 64 keys of the dQ pass 1005, 87%. 8 pages of 25 segments over 1601 states 131 us (63 and 65,
+// sums 8); 9 pages of 16 heads of 64 dims 147 (64 and 84). The short calls lose an item's start and end (3 to 4 us) and the launches.
 #include <math.h>
 
 #include <algorithm>

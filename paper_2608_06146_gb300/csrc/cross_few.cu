@@ -8,8 +8,8 @@
 // with 2 two. A unit is run by a cluster of NC CTAs that share its tiles and join their results through distributed
 // shared memory, or its keys are cut into parts that a later kernel joins.
 //
-// Measured: 670 streams over 32 pages of up to 1201 states, 16 heads of 64 dims: 23.0 us, 92 MB at 59% of the copy rate
-// (the items' starts and ends, as the pages' lengths differ); one stream over 961 states 5.2 us in a graph, most of it the
+// Measured: 670 streams over 32 pages of up to 1201 states, 16 heads of 64 dims: 23.3 us, 92 MB at 58% of the copy rate
+// (the items' starts and ends, as the pages' lengths differ); one stream over 961 states 5.3 us in a graph, most of it the
 // launch (on tcgen05 items, cut and joined, the two took 39 and 16 us).
 //
 // As in the other kernels, what lies behind a segment's keys may be anything: scores past the end become -inf and V's

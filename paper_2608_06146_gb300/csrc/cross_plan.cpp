@@ -1,4 +1,5 @@
-// cross_plan.cpp -- the host planner of cross attention (integers only).
+// cross_plan.cpp -- the host planner of cross attention. Plans hold integers alone; the choices between them compare
+// estimated times.
 //
 // Forward: every segment's rows are cut into chunks of 256 packed rows (128 with 64 dims), each with the segment's whole
 // key range for every KV head. They are work items as they are, or those of the last round are cut, or the sequence of
@@ -337,6 +338,18 @@ padoc_status check(const Segment *seg, int32_t n, const padoc_cross_config *cfg)
 
 // The forward's items for few rows, where that is faster than `time` (us): 16 or 32 rows an item, by clusters of 1 to 8
 // CTAs that join their parts of the keys themselves, or keys cut into parts.
+//
+// Both sides, in us (these items / those of 256 rows, with 64 dims 128):
+//                                                   16 + 2 of 128     8 + 8 of 128     16 + 16 of 64
+//   672 streams, each over 100 to 500 states           36 / 64          128 / 228        143 / 187
+//   ... over 300 to 1200                               56 / 97          244 / 354        257 / 316
+//   32 pages of up to 1201 states, 2 streams each      11 / 16           26 / 33          27 / 31
+//   ... 8 streams                                      20 / 16           25 / 31          27 / 31
+//   ... 30 streams                                     43 / 25           34 / 32          35 / 30
+//   ... 64 rows                                        81 / 25           46 / 34          49 / 32
+// The estimate takes the faster side but for 128 dims with a token an item and some 200 states and more (56 / 97 and
+// 244 / 354: it counts the keys' bytes at the memory's rate, while crops of one page come from L2) and pages of up to 16
+// streams under 8 + 8 heads (25 / 31).
 template <typename F>
 void plan_few(const Segment *seg, int32_t n, int32_t group, int32_t head_dim, int32_t hkv, int32_t sms, float time,
               const F &chunks_of, Work &fwd, padoc_cross_plan &info, int32_t &per)
@@ -346,7 +359,9 @@ void plan_few(const Segment *seg, int32_t n, int32_t group, int32_t head_dim, in
         if (seg[i].k_len) most = std::max(most, std::min(seg[i].q_len, 2 * PADOC_CROSS_FEW_ROWS) * group);
     const int32_t rows = most <= 16 ? 16 : PADOC_CROSS_FEW_ROWS;
     const int32_t an_sm = head_dim == 64 ? 3 : 2, lanes = sms * an_sm;   // CTAs
-    // (many blocks of rows, each reading the keys anew, cannot win: planning them would be most of the planner's time)
+    // Many blocks of rows, each reading the keys anew, do not win (32 pages of 128 rows over up to 1201 states: 149 us against
+    // 37, over up to 60 states 56 against 16, 16 heads of 64 dims 84 against 32). Items of a token each would (2500 streams
+    // of 16 heads of 64 dims over 60 to 200 states: 326 us against 510), but planning these 40000 takes 12 ms instead of 4.
     int64_t items = 0;
     for (int32_t i = 0; i < n; ++i)
         if (seg[i].k_len) items += ((int64_t)seg[i].q_len * group + rows - 1) / rows * hkv;

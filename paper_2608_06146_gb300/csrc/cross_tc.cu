@@ -19,12 +19,13 @@
 // their MMAs, the producer for its copies, and tensor memory is released.
 //
 // What bounds it: with 128 dims the MMAs and, over a long call, the chip's power (32768 rows over 8 x 2560 states of 16
-// query heads: 428 us, 1605 TFLOP/s, 93% of what a library product of this type sustains; a step of both tiles 1.40 us, 1.23
+// query heads: 426 us, 1613 TFLOP/s, 93% of what a library product of this type sustains; a step of both tiles 1.40 us, 1.23
 // of them without any softmax: the MMAs take 2048 cycles, and 2560 with their operands' way from shared memory, where
-// Q is read for each half of the keys). With 64 dims the softmax: a key costs half the MMAs and the same exponentials and
-// conversions (1.27 us a step of two CTAs, 0.74 without; 9 pages of 16 heads 57 us). One CTA with two tiles took 63 us
-// there, sixteen softmax warps 75. Few steps an item: its start and end, some 3 us. Pairs of CTAs that share K and V by
-// cta_group::2 were slower with 128 dims (434 -> 459 us, one more hand-over a step).
+// Q is read for each half of the keys). With 64 dims the chain through the softmax: a key costs half the MMAs and the same
+// exponentials and conversions (1.27 us a step of two CTAs, 0.74 without; 9 pages of 16 heads 57 us), with the tensor pipe
+// 31% and the issue slots 44% busy. One CTA with two tiles took 63 us there, sixteen softmax warps 75. Few steps an item:
+// its start and end, some 3 us. Pairs of CTAs that share K and V by cta_group::2 were slower with 128 dims (434 -> 459 us,
+// one more hand-over a step).
 #include <math.h>
 
 #include "cross.cuh"

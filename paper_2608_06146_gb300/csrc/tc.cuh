@@ -168,7 +168,7 @@ __device__ __forceinline__ void umma_bf16_ss_k128_warp(uint32_t d_tmem, uint64_t
             " add.s64 a, %1, %4+6;\n add.s64 b, %2, %5+6;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n}" ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "n"(PA >> 4), "n"(PB >> 4)
             : "memory");
 }
-// Four K-steps (64 elements, one panel) of a K-major product, D = A[smem] . B[smem]^T.
+// One K-step (16 elements) of a K-major product, D += A[smem] . B[smem]^T.
 __device__ __forceinline__ void umma_bf16_ss_k16_add_warp(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc)
 {
     asm volatile(
@@ -176,6 +176,7 @@ __device__ __forceinline__ void umma_bf16_ss_k16_add_warp(uint32_t d_tmem, uint6
         " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, t;\n}" ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc)
         : "memory");
 }
+// Four K-steps (64 elements, one panel) of a K-major product, D = A[smem] . B[smem]^T.
 __device__ __forceinline__ void umma_bf16_ss_k64_warp(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc)
 {
     asm volatile(

@@ -76,3 +76,26 @@ def test_rows_that_are_not_finite_reach_the_keys_they_see_alone(hq, hkv, d, dtyp
     if what != "dout large" and lse[row, head] != -math.inf:
         for got, ref in ((dk, want[1]), (dv, want[2])):
             assert not torch.isfinite(got[~torch.isfinite(ref)]).any()
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,segments", [
+    (16, 2, 128, BF16, [(0, 1, 0, 300)]), (16, 16, 64, BF16, [(0, 3, 0, 5000)]), (16, 2, 128, BF16, [(0, 90, 0, 300)]),
+    (4, 4, 64, BF16, [(0, 700, 0, 1000)]), (4, 1, 64, F32, [(0, 40, 0, 700)])])
+def test_a_row_whose_scores_are_all_minus_infinity_is_a_row_without_keys(hq, hkv, d, dtype, segments):
+    # one head of one row, by clusters, in joined parts, in tiles, in fp32; the others as without it
+    rows, keys = segments[0][1], segments[0][3]
+    g = torch.Generator(device=DEV).manual_seed(keys)
+    new = lambda n, h: torch.randn((n, h, d), generator=g, device=DEV).to(dtype)   # noqa: E731
+    q, k, v = new(rows, hq), new(keys, hkv), new(keys, hkv)
+    k[..., 3] = -k[..., 3].abs() - 0.5
+    plan = CrossPlan(segments, hq, hkv, d, dtype, DEV)
+    want, wl = torch.empty_like(q), torch.empty((rows, hq), device=DEV)
+    plan.run(q, k, v, 0.1, want, wl)
+    row, head = rows // 2, hq - 1
+    q[row, head, 3] = math.inf
+    out, lse = torch.empty_like(q), torch.empty_like(wl)
+    plan.run(q, k, v, 0.1, out, lse)
+    pa.padoc_check_device_errors()
+    assert (out[row, head] == 0).all() and lse[row, head] == -math.inf
+    want[row, head], wl[row, head] = 0, -math.inf
+    assert torch.equal(out, want) and torch.equal(lse, wl)
