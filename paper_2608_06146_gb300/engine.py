@@ -137,7 +137,8 @@ class RotaryPrefill:
 class CrossPlan:
     """Cross attention of query rows over an encoder's states: the plan of segments (q_begin, q_len, k_begin, k_len)
     on the device, with its workspaces. Calls that may run at the same time (two streams, two captured graphs) need a
-    CrossPlan each."""
+    CrossPlan each. It may be dropped while its calls still run, on whatever streams, but not before the last replay of
+    a graph that has captured one."""
 
     def __init__(self, segments, num_q_heads: int, num_kv_heads: int, head_dim: int, dtype: torch.dtype, device,
                  training: bool = False, ctas: int = 0):
@@ -147,18 +148,32 @@ class CrossPlan:
         new = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device=device)
         self.workspace = new(pa.padoc_cross_workspace_size(self.info))
         self.bwd_workspace = new(pa.padoc_cross_bwd_workspace_size(self.info)) if training else None
+        self._streams = set()   # whose work keeps the memory above from being given to others
+
+    def _keep_for(self, raw):
+        stream = torch.cuda.ExternalStream(raw, device=self.plan_dev.device) if raw else \
+            torch.cuda.default_stream(self.plan_dev.device)
+        for t in (self.plan_dev, self.workspace, self.bwd_workspace):
+            if t is not None:
+                t.record_stream(stream)
+        self._streams.add(raw)
 
     def run(self, q, k, v, scale, out, lse, stream=None):
         """q [rows][Hq][d]; k, v [key rows][Hkv][d] (rows may lie apart); out like q, lse fp32 [rows][Hq]. Rows in no
         segment are left as they are."""
-        pa.padoc_cross_attn(self.info, self.plan_dev, q, k, v, scale, out, lse, self.workspace, stream)
+        raw = pa._stream_ptr(stream)
+        pa.padoc_cross_attn(self.info, self.plan_dev, q, k, v, scale, out, lse, self.workspace, raw)
+        if raw not in self._streams:
+            self._keep_for(raw)
 
     def run_bwd(self, q, k, v, out, dout, lse, scale, dq, dk, dv, stream=None):
         """Gradients of run for its out and lse: dq of the segments' rows, dk and dv of every key row."""
         if self.bwd_workspace is None:
             raise ValueError("gradients need training=True")
-        pa.padoc_cross_attn_bwd(self.info, self.plan_dev, q, k, v, out, dout, lse, scale, dq, dk, dv, self.bwd_workspace,
-                                stream)
+        raw = pa._stream_ptr(stream)
+        pa.padoc_cross_attn_bwd(self.info, self.plan_dev, q, k, v, out, dout, lse, scale, dq, dk, dv, self.bwd_workspace, raw)
+        if raw not in self._streams:
+            self._keep_for(raw)
 
 
 class ChunkPrefillPlan:

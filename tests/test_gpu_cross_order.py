@@ -91,3 +91,31 @@ def test_a_loops_captured_step_is_refused_and_a_plan_of_its_streams_captured():
     torch.cuda.synchronize()
     pa.padoc_check_device_errors()
     assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+@pytest.mark.parametrize("current", [False, True])
+def test_a_plan_dropped_while_another_stream_runs_its_calls(current):
+    segments, hq, hkv, d = [(0, 24, 0, 9001), (24, 300, 100, 500)], 16, 2, 128
+    q, k, v, dout = inputs(segments, hq, hkv, d, BF16)
+    plan = CrossPlan(segments, hq, hkv, d, BF16, DEV, training=True)
+    want = [torch.empty_like(t) for t in (q, q, k, v)] + [torch.empty(q.shape[:2], device=DEV)]
+    got = [torch.zeros_like(t) for t in want]
+    plan.run(q, k, v, 0.1, want[0], want[4])
+    plan.run_bwd(q, k, v, want[0], dout, want[4], 0.1, *want[1:4])
+    sizes = [t.nbytes for t in (plan.plan_dev, plan.workspace, plan.bwd_workspace)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    del plan
+    plan = CrossPlan(segments, hq, hkv, d, BF16, DEV, training=True)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+        stream = None if current else side
+        plan.run(q, k, v, 0.1, got[0], got[4], stream=stream)
+        plan.run_bwd(q, k, v, got[0], dout, got[4], 0.1, *got[1:4], stream=stream)
+    del plan
+    for _ in range(4):      # what is allocated now lies elsewhere
+        for n in sizes:
+            torch.empty(n, dtype=torch.uint8, device=DEV).fill_(255)
+    torch.cuda.synchronize()
+    pa.padoc_check_device_errors()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
