@@ -151,7 +151,8 @@ class CrossPlan:
         self._streams = set()   # whose work keeps the memory above from being given to others
 
     def _keep_for(self, raw):
-        stream = torch.cuda.ExternalStream(raw, device=self.plan_dev.device) if raw else \
+        # (0 and 1 are the default stream's handles)
+        stream = torch.cuda.ExternalStream(raw, device=self.plan_dev.device) if raw > 1 else \
             torch.cuda.default_stream(self.plan_dev.device)
         for t in (self.plan_dev, self.workspace, self.bwd_workspace):
             if t is not None:

@@ -27,7 +27,7 @@ def test_memory_is_kept_for_the_streams_of_the_calls(monkeypatch, training):
     class Side:
         cuda_stream = 9
     used = []
-    for stream in (None, 8, Side(), 0, None, 8):
+    for stream in (None, 8, Side(), 0, None, 8, 1):
         plan.run(None, None, None, 0.1, None, None, stream)
         used.append(pa._stream_ptr(stream))
         if training:
@@ -36,4 +36,5 @@ def test_memory_is_kept_for_the_streams_of_the_calls(monkeypatch, training):
     current[0] = 11                               # the current stream has changed
     plan.run(None, None, None, 0.1, None, None)
     assert calls == used + [11]
-    assert {(p, s) for p in own for s in (7, 8, 9, 0, 11)} == set(kept) and len(kept) == len(own) * 5
+    assert {(p, s) for p in own for s in (7, 8, 9, 0, 11)} == set(kept)   # (1 is the default stream, too)
+    assert len(kept) == len(own) * 6
